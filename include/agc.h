@@ -57,7 +57,8 @@ extern "C" {
 
 #define AGC_MAX_WORKERS 256   /* n <= 256: per-worker arguments travel in the kernel argument block */
 #define AGC_MAX_BITS 16
-#define AGC_MAX_LAYERS 256    /* layer-wise scales: at most this many layers */
+#define AGC_MAX_LAYERS 256    /* layer-wise scales: at most this many layers; matrices of one agc_muon_update */
+#define AGC_MAX_MATRIX 32768  /* sides of the matrices of agc_muon_update */
 
 typedef struct agc_ctx agc_ctx; /* opaque; owns device workspace and a copy of B */
 
@@ -279,6 +280,31 @@ agc_status agc_gd_update(float *beta_dev, const float *ghat_dev, float lr, int64
 agc_status agc_adam_update(float *beta_dev, float *m1_dev, float *m2_dev, const float *ghat_dev,
                            const float *ghat2_dev, float lr, float beta1, float beta2, float eps,
                            int64_t t, int64_t d, void *hip_stream);
+
+/* --------------------------------------------------------------------------------------
+ * Token models: two producers of rows of G and a consumer of g_hat
+ * ------------------------------------------------------------------------------------ */
+/* Orthogonalised update of n_mats matrices of one shape that lie inside the parameter vector.  For each,
+ *   M <- momentum * M + g_hat;   U = g_hat + momentum * M (nesterov) or M;   X = U / (|U|_F + 1e-7);
+ *   `steps` times  A = X X^T,  X <- a X + (b A + c A A) X,  a, b, c = 3.4445, -4.7750, 2.0315;
+ *   beta <- (1 - lr * weight_decay) * beta - lr * scale * X
+ * (products on the matrix's short side; five steps bring the singular values near 1).  `scale` is the caller's rule for
+ * the shape, for instance sqrt(max(1, rows / cols)).
+ *   beta_dev, m1_dev, ghat_dev  device, the vectors; matrix i is the rows * cols floats from offset_host[i] on,
+ *              row-major.  beta and the average m1 are updated in place; matrices must not overlap
+ *   offset_host  host, n_mats offsets in elements, in any order
+ *   beta_bf16_dev  device, a vector of the same layout in bfloat16 that receives the updated matrices rounded to
+ *              nearest even (what agc_gated_forward reads), or NULL
+ *   workspace_dev  device, agc_muon_workspace_bytes(...) bytes, 256-byte aligned; scratch
+ * Products are taken on operands of 22 bits (pairs of binary16), sums are binary32 in a fixed order, the norm is
+ * binary64: the result is reproducible run to run and as near to the exact one as binary32 products come.  A zero
+ * gradient gives X = 0; NaN or infinity in g_hat makes its own matrix NaN and no other.
+ * 1 <= rows, cols <= AGC_MAX_MATRIX, 1 <= n_mats <= AGC_MAX_LAYERS (AGC_ESHAPE; the workspace size is 0 then),
+ * 1 <= steps <= 32 (AGC_EINVAL). */
+int64_t agc_muon_workspace_bytes(int rows, int cols, int n_mats);
+agc_status agc_muon_update(float *beta_dev, float *m1_dev, const float *ghat_dev, const int64_t *offset_host, int n_mats,
+                           int rows, int cols, float lr, float momentum, int nesterov, float weight_decay, float scale,
+                           int steps, void *beta_bf16_dev, void *workspace_dev, void *hip_stream);
 
 /* --------------------------------------------------------------------------------------
  * Host-side design routines (no GPU work; run once per change of the system statistics)

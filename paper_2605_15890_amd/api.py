@@ -23,6 +23,7 @@ EXPORTS = [
     "agc_create", "agc_destroy", "agc_set_code", "agc_code_path", "agc_code_bytes", "agc_last_error",
     "agc_encode_quantize", "agc_decode", "agc_step", "agc_profile_enable", "agc_profile_read",
     "agc_scales_per_worker", "agc_set_layers", "agc_decode2", "agc_decode_noalloc", "agc_adam_update", "agc_second_moment_decoder",
+    "agc_muon_workspace_bytes", "agc_muon_update",
     "agc_calibration_copy", "agc_debug_force_long", "agc_debug_sketch", "agc_debug_sketch_last", "agc_debug_sketch_max", "agc_debug_stream_rows", "agc_ls_workspace_floats", "agc_ls_partial_gradients", "agc_gd_update",
     "agc_phi_coef_balanced", "agc_alloc_bits", "agc_alloc_bits_dp", "agc_alloc_objective",
     "agc_build_code", "agc_build_cyclic_code", "agc_build_cyclic_code_opt", "agc_check_unbiased",
@@ -103,6 +104,11 @@ def load():
     L.agc_ls_partial_gradients.restype = C.c_int
     L.agc_gd_update.argtypes = [_vp, _vp, C.c_float, C.c_int64, _vp]
     L.agc_gd_update.restype = C.c_int
+    L.agc_muon_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
+    L.agc_muon_workspace_bytes.restype = C.c_int64
+    L.agc_muon_update.argtypes = [_vp, _vp, _vp, _vp, C.c_int, C.c_int, C.c_int, C.c_float, C.c_float, C.c_int,
+                                  C.c_float, C.c_float, C.c_int, _vp, _vp, _vp]
+    L.agc_muon_update.restype = C.c_int
     L.agc_calibration_copy.argtypes = [_vp, _vp, C.c_int64, _vp]
     L.agc_calibration_copy.restype = C.c_int
     L.agc_debug_stream_rows.argtypes = [_vp, C.c_int64, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, _vp, _vp]
@@ -463,6 +469,32 @@ def agc_adam_update(beta, m1, m2, ghat, ghat2, lr, beta1, beta2, eps, t, stream=
                                 _stream_handle(stream))
     if st != AGC_OK:
         raise AgcError(st, "agc_adam_update")
+
+
+def agc_muon_workspace_bytes(rows, cols, n_mats):
+    return int(load().agc_muon_workspace_bytes(int(rows), int(cols), int(n_mats)))
+
+
+def agc_muon_update(beta, m1, ghat, offsets, rows, cols, lr, momentum, nesterov, weight_decay, scale, steps, workspace,
+                    beta_bf16=None, stream=None, check=True):
+    """Orthogonalised update of the rows x cols matrices that start at `offsets` (elements) of the parameter vector
+    beta; m1 and ghat have its layout, and so has beta_bf16 (bfloat16), which receives the new matrices if given."""
+    L = load()
+    off = [int(o) for o in offsets]
+    size = int(rows) * int(cols)
+    end = max(off, default=0) + size
+    for t, width in ((beta, 4), (m1, 4), (ghat, 4), (beta_bf16, 2)):
+        if t is not None and (t.numel() < end or t.element_size() != width or not t.is_contiguous()):
+            raise AgcError(AGC_ESHAPE, "agc_muon_update: a vector is smaller than the matrices reach, or of another type")
+    if workspace.numel() * workspace.element_size() < L.agc_muon_workspace_bytes(rows, cols, len(off)):
+        raise AgcError(AGC_ESHAPE, "agc_muon_update: the workspace is too small")
+    st = L.agc_muon_update(beta.data_ptr(), m1.data_ptr(), ghat.data_ptr(), struct.pack(f"{len(off)}q", *off), len(off),
+                           rows, cols, lr, momentum, int(bool(nesterov)), weight_decay, scale, steps,
+                           None if beta_bf16 is None else beta_bf16.data_ptr(), workspace.data_ptr(),
+                           _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
 
 
 def agc_decode_noalloc(n, d, bucket, codes, scales, bits, w, mask, ghat, stream=None, check=True):

@@ -13,6 +13,7 @@
 #include "../../include/agc.h"
 #include "../../include/agc_debug.h"
 #include "agc_kernels.h"
+#include "agc_operators.h"
 
 namespace {
 
@@ -273,6 +274,8 @@ bool use_sketch(const agc_ctx* c, const agc::CodeDev& code, const uint8_t* bits)
 }
 
 }  // namespace
+
+int agc::note_failure(int status, const char* message) { return fail(nullptr, (agc_status)status, message); }
 
 extern "C" {
 

@@ -1,0 +1,400 @@
+// Orthogonalised update of the matrices inside the parameter vector (the optimizer that consumes g_hat):
+//   M <- mu M + g;   U = g + mu M  or  M;   X = U / (|U| + eps)
+//   S times   A = X X^T,  B = a I + b A + c A A,  X <- B X       (p(x) = a x + b x^3 + c x^5 on the singular values)
+//   beta <- keep * beta - rate * X
+// with X taken as m x n, m <= n (the transpose of a tall matrix).
+//
+// Range and rounding.  With a, b, c = 3.4445, -4.7750, 2.0315, p maps [0, 1.21] into itself and the first X has
+// singular values of at most 1, so |X| < 1.21, |A| < 1.47 and |B| <= a: every entry of each has a bound that is known
+// before, and each is kept as a pair of binary16 values (hi + lo, 22 bits) scaled by a fixed power of two that fills
+// the range.  Entries far below the bound lose relative but not absolute accuracy, 2^-25 of the unit 2^-14, which is
+// below the rounding of binary32 sums of the products that they enter.  Three matrix products on the 16-bit units
+// (hi hi + hi lo + lo hi) then stand for one in binary32: 1/3 of 2.5 PFLOP/s, where binary32 operands reach 0.157.
+// X itself goes through this, not a rounded copy of it: single 16-bit values would leave errors that the products
+// amplify by up to a^S = 485 in the directions of small singular values.
+//
+// Each product writes its result for the next one in the order in which that one reads it: X along n (for X X^T) and
+// along m (for B X); A and B are symmetric, so half the tiles are formed and written twice.  The last product
+// updates beta from its sums; X is not written.
+#include "agc_operators.h"
+#include "agc_tile.h"
+
+namespace agc {
+
+namespace {
+
+constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
+constexpr double kMuonEps = 1e-7;
+constexpr float kUnitX = 16384.0f;   // 2^14 * 1.21 < 65504
+constexpr float kUnitA = 16384.0f;   // 2^14 * 1.47
+constexpr float kUnitB = 8192.0f;    // 2^13 * 3.45
+constexpr int kSumBlock = 256;       // threads of the elementwise passes
+constexpr int kMostSums = 1024;      // partial sums of squares of a matrix
+
+struct MuonGeom {
+    int m, n;            // short and long side
+    int tall;            // the matrix has more rows than columns: X is its transpose
+    int mats;
+    int64_t pitch_n;     // bytes of a split row of n values
+    int64_t pitch_m;     // of m values
+    int64_t size_x, size_t, size_a;   // bytes of a matrix stored along n, along m, and of A
+};
+
+MuonGeom muon_geom(int rows, int cols, int n_mats)
+{
+    MuonGeom g{};
+    g.tall = rows > cols;
+    g.m = g.tall ? cols : rows;
+    g.n = g.tall ? rows : cols;
+    g.mats = n_mats;
+    g.pitch_n = round_up(g.n, 32) * 4;
+    g.pitch_m = round_up(g.m, 32) * 4;
+    g.size_x = g.m * g.pitch_n;
+    g.size_t = g.n * g.pitch_m;
+    g.size_a = g.m * g.pitch_m;
+    return g;
+}
+
+int muon_sums(int64_t count)
+{
+    const int64_t blocks = (count + 16383) / 16384;
+    return (int)(blocks < kMostSums ? blocks : kMostSums);
+}
+
+__device__ __forceinline__ double block_sum(double v, double* lds)
+{
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// M <- mu M + g and the sum of the squares of U in binary64, one partial sum a workgroup (added in a fixed order
+// by k_muon_start).  Bound by memory: 12 bytes a value.
+__global__ __launch_bounds__(kSumBlock) void k_muon_momentum(const MuonCall c, int64_t count, double* sums)
+{
+    __shared__ double lds[4];
+    const int64_t off = c.offset[blockIdx.y];
+    const float* g = c.ghat + off;
+    float* m = c.m1 + off;
+    const float mu = c.momentum;
+    double sum = 0.0;
+    auto one = [&](float gv, float mv) {
+        mv = fmaf(mu, mv, gv);
+        const float u = c.nesterov ? fmaf(mu, mv, gv) : mv;
+        sum = fma((double)u, (double)u, sum);
+        return mv;
+    };
+    const int64_t step = (int64_t)gridDim.x * kSumBlock, at = (int64_t)blockIdx.x * kSumBlock + threadIdx.x;
+    int64_t done = 0;
+    if (((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(m)) & 15) == 0) {
+        const int64_t quads = count / 4;
+        for (int64_t i = at; i < quads; i += step) {
+            const float4 gv = reinterpret_cast<const float4*>(g)[i];
+            float4 mv = reinterpret_cast<const float4*>(m)[i];
+            mv.x = one(gv.x, mv.x), mv.y = one(gv.y, mv.y), mv.z = one(gv.z, mv.z), mv.w = one(gv.w, mv.w);
+            reinterpret_cast<float4*>(m)[i] = mv;
+        }
+        done = quads * 4;
+    }
+    for (int64_t i = done + at; i < count; i += step) m[i] = one(g[i], m[i]);
+    const double s = block_sum(sum, lds);
+    if (threadIdx.x == 0) sums[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
+}
+
+// X = U / (|U| + eps) as binary16 pairs, stored along both sides.  A workgroup turns one 64 x 64 tile of U in LDS.
+__global__ __launch_bounds__(kSumBlock) void k_muon_start(const MuonCall c, MuonGeom geo, const double* sums, int n_sums,
+                                                          char* along_cols, char* along_rows)
+{
+    __shared__ double lds_sum[4];
+    __shared__ float tile[64][65];
+    const int mat = blockIdx.z, tid = threadIdx.x;
+    double s = 0.0;
+    for (int i = tid; i < n_sums; i += kSumBlock) s += sums[(int64_t)mat * n_sums + i];
+    s = block_sum(s, lds_sum);
+    const float unit = (float)((double)kUnitX / (sqrt(s) + kMuonEps));
+
+    const float* g = c.ghat + c.offset[mat];
+    const float* m = c.m1 + c.offset[mat];
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+    for (int i = tid; i < 4096; i += kSumBlock) {
+        const int r = r0 + (i >> 6), col = c0 + (i & 63);
+        float u = 0.0f;
+        if (r < c.rows && col < c.cols) {
+            const int64_t at = (int64_t)r * c.cols + col;
+            u = (c.nesterov ? fmaf(c.momentum, m[at], g[at]) : m[at]) * unit;
+        }
+        tile[i >> 6][i & 63] = u;
+    }
+    __syncthreads();
+    const int64_t pitch_cols = geo.tall ? geo.pitch_m : geo.pitch_n, pitch_rows = geo.tall ? geo.pitch_n : geo.pitch_m;
+    const int64_t cols_up = pitch_cols / 4, rows_up = pitch_rows / 4;
+    char* by_row = along_cols + (int64_t)mat * c.rows * pitch_cols;
+    char* by_col = along_rows + (int64_t)mat * c.cols * pitch_rows;
+    for (int i = tid; i < 512; i += kSumBlock) {
+        const int a = i >> 3, b = (i & 7) * 8;
+        float v[8];
+        if (r0 + a < c.rows && c0 + b < cols_up) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = tile[a][b + e];
+            split_store8(by_row + (int64_t)(r0 + a) * pitch_cols, c0 + b, v);
+        }
+        if (c0 + a < c.cols && r0 + b < rows_up) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = tile[b + e][a];
+            split_store8(by_col + (int64_t)(c0 + a) * pitch_rows, r0 + b, v);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ the three products of a step
+// A = X X^T, or B = a I + b A + c A A: symmetric, from rows of one matrix; tiles of the lower triangle.
+struct SymJob {
+    static constexpr TilePair kPair = kSplit;
+    const char* src;          // X along n, or A
+    char* dst;                // A or B
+    int64_t pitch, size;      // of src
+    int64_t pitch_dst, size_dst;
+    int m, steps, tiles, side, total;   // tiles of one matrix, tile edge, of all
+    int poly;
+
+    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    {
+        const int t = xcd_order(id, total);
+        p.batch = t / tiles;
+        int mi, ni;
+        triangle_order(t - p.batch * tiles, mi, ni);
+        p.m0 = mi * side, p.n0 = ni * side, p.steps = steps;
+        return true;
+    }
+    __device__ __forceinline__ const char* row(const TilePos& p, int r) const
+    {
+        return src + p.batch * size + (int64_t)(r < m ? r : m - 1) * pitch;
+    }
+    __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const { return row(p, p.m0 + r); }
+    __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const { return row(p, p.n0 + r); }
+    __device__ __forceinline__ void piece(const TilePos& p, int mb, int nb, float* s, int lane) const
+    {
+        char* out = dst + p.batch * size_dst;
+        const int up = (int)(pitch_dst / 4), sub = lane >> 3, run = (lane & 7) * 8;
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int r = it * 8 + sub, gr = mb + r, gc = nb + run;
+            float v[8];
+            piece_row8(s, r, run, v);
+            if (poly) {
+                float a[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] = 0.0f;
+                if (gr < m && gc < up) split_load8(src + p.batch * size + (int64_t)gr * pitch, gc, a);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    // units: sums 2^28, A 2^14, B 2^13
+                    float b = fmaf(kNsC * (kUnitB / (kUnitA * kUnitA)), v[e], kNsB * (kUnitB / kUnitA) * a[e]);
+                    if (gr == gc + e) b += kNsA * kUnitB;
+                    v[e] = b;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= kUnitA / (kUnitX * kUnitX);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (gr >= m || gc + e >= m) v[e] = 0.0f;
+            if (gr < m && gc < up) split_store8(out + (int64_t)gr * pitch_dst, gc, v);
+            piece_put_row8(s, r, run, v);
+        }
+        if (p.m0 == p.n0) return;   // a tile on the diagonal holds both halves
+        wave_lds_fence();
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int cc = it * 8 + sub, gc = nb + cc, gr = mb + run;
+            float v[8];
+            piece_col8(s, run, cc, v);
+            if (gc < m && gr < up) split_store8(out + (int64_t)gc * pitch_dst, gr, v);
+        }
+    }
+};
+
+// X <- B X, or, of the last step, beta <- keep * beta - rate * B X.
+template <bool LAST>
+struct ApplyJob {
+    static constexpr TilePair kPair = kSplit;
+    const char* b;           // m x m
+    const char* xt;          // X along m: n rows
+    char* out_x;             // along n
+    char* out_t;             // along m
+    MuonGeom g;
+    int mt, nt, side_m, side_n, total;
+    MuonCall call;           // of the last step
+
+    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    {
+        const int t = xcd_order(id, total);
+        p.batch = t / (mt * nt);
+        int mi, ni;
+        tile_order(t - p.batch * mt * nt, mt, nt, mi, ni);
+        p.m0 = mi * side_m, p.n0 = ni * side_n, p.steps = (int)(g.pitch_m / 128);
+        return true;
+    }
+    __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
+    {
+        const int at = p.m0 + r < g.m ? p.m0 + r : g.m - 1;
+        return b + p.batch * g.size_a + (int64_t)at * g.pitch_m;
+    }
+    __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const
+    {
+        const int at = p.n0 + r < g.n ? p.n0 + r : g.n - 1;
+        return xt + p.batch * g.size_t + (int64_t)at * g.pitch_m;
+    }
+    // `count` of eight consecutive parameters from index at on
+    __device__ __forceinline__ void update(int64_t at, int count, const float v[8]) const
+    {
+        float* beta = call.beta + at;
+        const float rate = call.rate * (1.0f / (kUnitB * kUnitX));
+        float w[8];
+        if (count == 8 && (reinterpret_cast<uintptr_t>(beta) & 15) == 0) {
+            tile_f32x4* q = reinterpret_cast<tile_f32x4*>(beta);
+            const tile_f32x4 x = q[0], y = q[1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = fmaf(-rate, v[e], call.keep * x[e]);
+                w[4 + e] = fmaf(-rate, v[4 + e], call.keep * y[e]);
+            }
+            q[0] = tile_f32x4{w[0], w[1], w[2], w[3]};
+            q[1] = tile_f32x4{w[4], w[5], w[6], w[7]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < count) beta[e] = w[e] = fmaf(-rate, v[e], call.keep * beta[e]);
+        }
+        if (call.beta_bf16) {
+            uint16_t* o = call.beta_bf16 + at;
+            if (count == 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+                *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(w);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < count) o[e] = (uint16_t)bf16_bits(w[e]);
+            }
+        }
+    }
+    __device__ __forceinline__ void piece(const TilePos& p, int mb, int nb, float* s, int lane) const
+    {
+        const int sub = lane >> 3, run = (lane & 7) * 8;
+        const int up_n = (int)(g.pitch_n / 4), up_m = (int)(g.pitch_m / 4);
+        if (LAST) {
+            const int64_t off = call.offset[p.batch];
+#pragma unroll
+            for (int it = 0; it < 8; ++it) {
+                float v[8];
+                if (!g.tall) {
+                    const int gr = mb + it * 8 + sub, gc = nb + run;
+                    piece_row8(s, it * 8 + sub, run, v);
+                    if (gr < g.m && gc < g.n) update(off + (int64_t)gr * g.n + gc, g.n - gc < 8 ? g.n - gc : 8, v);
+                } else {
+                    const int gc = nb + it * 8 + sub, gr = mb + run;
+                    piece_col8(s, run, it * 8 + sub, v);
+                    if (gc < g.n && gr < g.m) update(off + (int64_t)gc * g.m + gr, g.m - gr < 8 ? g.m - gr : 8, v);
+                }
+            }
+            return;
+        }
+        char* ox = out_x + p.batch * g.size_x;
+        char* ot = out_t + p.batch * g.size_t;
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int gr = mb + it * 8 + sub, gc = nb + run;
+            float v[8];
+            piece_row8(s, it * 8 + sub, run, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gc + e < g.n ? v[e] * (1.0f / kUnitB) : 0.0f;
+            if (gr < g.m && gc < up_n) split_store8(ox + (int64_t)gr * g.pitch_n, gc, v);
+        }
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int gc = nb + it * 8 + sub, gr = mb + run;
+            float v[8];
+            piece_col8(s, run, it * 8 + sub, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gr + e < g.m ? v[e] * (1.0f / kUnitB) : 0.0f;
+            if (gc < g.n && gr < up_m) split_store8(ot + (int64_t)gc * g.pitch_m, gr, v);
+        }
+    }
+};
+
+hipError_t launch_sym(SymJob j, int mats, hipStream_t stream)
+{
+    const int big = (j.m + 255) / 256, small = (j.m + 127) / 128;
+    const int64_t tiles_big = (int64_t)mats * big * (big + 1) / 2, tiles_small = (int64_t)mats * small * (small + 1) / 2;
+    const bool use_big = (tiles_big + 255) / 256 * 4 <= (tiles_small + 511) / 512 * 2;
+    j.side = use_big ? 256 : 128;
+    const int across = use_big ? big : small;
+    j.tiles = across * (across + 1) / 2;
+    j.total = mats * j.tiles;
+    if (use_big) hipLaunchKernelGGL((k_tile<SymJob, 256, 256, 2, 4>), dim3(j.total), dim3(512), 0, stream, j);
+    else hipLaunchKernelGGL((k_tile<SymJob, 128, 128, 2, 2>), dim3(j.total), dim3(256), 0, stream, j);
+    return hipGetLastError();
+}
+
+template <bool LAST>
+hipError_t launch_apply(ApplyJob<LAST> j, hipStream_t stream)
+{
+    const int64_t bm = (j.g.m + 255) / 256, bn = (j.g.n + 255) / 256, sm = (j.g.m + 127) / 128, sn = (j.g.n + 127) / 128;
+    const bool use_big = (j.g.mats * bm * bn + 255) / 256 * 4 <= (j.g.mats * sm * sn + 511) / 512 * 2;
+    j.side_m = j.side_n = use_big ? 256 : 128;
+    j.mt = (int)(use_big ? bm : sm);
+    j.nt = (int)(use_big ? bn : sn);
+    j.total = j.g.mats * j.mt * j.nt;
+    if (use_big) hipLaunchKernelGGL((k_tile<ApplyJob<LAST>, 256, 256, 2, 4>), dim3(j.total), dim3(512), 0, stream, j);
+    else hipLaunchKernelGGL((k_tile<ApplyJob<LAST>, 128, 128, 2, 2>), dim3(j.total), dim3(256), 0, stream, j);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// sums | X along n, twice | X along m, twice | A | B
+int64_t muon_workspace_bytes(int rows, int cols, int n_mats)
+{
+    const MuonGeom g = muon_geom(rows, cols, n_mats);
+    const int64_t sums = round_up((int64_t)n_mats * muon_sums((int64_t)rows * cols) * 8, 256);
+    return sums + 2 * (round_up(n_mats * g.size_x, 256) + round_up(n_mats * g.size_t, 256) + round_up(n_mats * g.size_a, 256));
+}
+
+hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
+{
+    const MuonGeom g = muon_geom(c.rows, c.cols, c.n_mats);
+    const int64_t count = (int64_t)c.rows * c.cols;
+    const int n_sums = muon_sums(count);
+    double* sums = reinterpret_cast<double*>(c.workspace);
+    char* at = c.workspace + round_up((int64_t)c.n_mats * n_sums * 8, 256);
+    auto take = [&](int64_t bytes) {
+        char* p = at;
+        at += round_up(bytes, 256);
+        return p;
+    };
+    char* x[2] = {take(c.n_mats * g.size_x), take(c.n_mats * g.size_x)};
+    char* t[2] = {take(c.n_mats * g.size_t), take(c.n_mats * g.size_t)};
+    char *a = take(c.n_mats * g.size_a), *b = take(c.n_mats * g.size_a);
+
+    hipLaunchKernelGGL(k_muon_momentum, dim3(n_sums, c.n_mats), dim3(kSumBlock), 0, stream, c, count, sums);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_muon_start, dim3((c.cols + 63) / 64, (c.rows + 63) / 64, c.n_mats), dim3(kSumBlock), 0, stream, c, g,
+                       sums, n_sums, g.tall ? t[0] : x[0], g.tall ? x[0] : t[0]);
+    e = hipGetLastError();
+    for (int s = 0; s < c.steps && e == hipSuccess; ++s) {
+        const int in = s & 1, out = in ^ 1;
+        SymJob gram{x[in], a, g.pitch_n, g.size_x, g.pitch_m, g.size_a, g.m, (int)(g.pitch_n / 128), 0, 0, 0, 0};
+        e = launch_sym(gram, c.n_mats, stream);
+        if (e != hipSuccess) return e;
+        SymJob poly{a, b, g.pitch_m, g.size_a, g.pitch_m, g.size_a, g.m, (int)(g.pitch_m / 128), 0, 0, 0, 1};
+        e = launch_sym(poly, c.n_mats, stream);
+        if (e != hipSuccess) return e;
+        if (s + 1 < c.steps) e = launch_apply(ApplyJob<false>{b, t[in], x[out], t[out], g, 0, 0, 0, 0, 0, c}, stream);
+        else e = launch_apply(ApplyJob<true>{b, t[in], nullptr, nullptr, g, 0, 0, 0, 0, 0, c}, stream);
+    }
+    return e;
+}
+
+}  // namespace agc

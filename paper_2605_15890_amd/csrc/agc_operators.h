@@ -1,0 +1,32 @@
+// Launch interface between the C ABI (agc_operators.cpp) and the kernels of the operators round the coded step:
+// orthogonalised update, gated block, embedding.  Every pointer is a device pointer unless it says host.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace agc {
+
+// Leaves a message for agc_last_error(NULL) and returns the status (agc_api.cpp).
+int note_failure(int status, const char* message);
+
+constexpr int kMostMatrices = 256;   // of one update; their offsets travel as kernel arguments
+constexpr int kMostParts = 256;      // partitions; their ends travel as kernel arguments
+
+inline int64_t round_up(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
+
+// ------------------------------------------------------------------ orthogonalised update
+struct MuonCall {
+    float* beta;
+    float* m1;
+    const float* ghat;
+    uint16_t* beta_bf16;               // may be null
+    int64_t offset[kMostMatrices];     // of each matrix in the vectors, in elements
+    int n_mats, rows, cols, nesterov, steps;
+    float momentum, keep, rate;        // beta <- keep * beta - rate * X
+    char* workspace;
+};
+int64_t muon_workspace_bytes(int rows, int cols, int n_mats);
+hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream);
+
+}  // namespace agc

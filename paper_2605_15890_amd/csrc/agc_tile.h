@@ -1,0 +1,267 @@
+// Matrix products of the gated block and of the Newton-Schulz products: one tile loop for all of them.
+//
+// Every product here is C[m,n] = sum_k A[m,k] * B[n,k] with 16-bit operands whose rows are contiguous in k,
+// held in groups of 128 bytes ("k-steps"); operands that come in another order or with another end are laid out
+// by a pass of their own before.  A k-step is either
+//   plain   64 values, bfloat16:                       C += A0 B0 + A1 B1     (its two halves of 32)
+//   split   32 values as binary16 pairs, 32 high parts and 32 low parts (x = hi + lo to 22 bits):
+//                                                      C += A0 B0 + A0 B1 + A1 B0   (lo * lo is below 2^-22)
+// so that the same loads feed both.  Products are v_mfma_f32_16x16x32, sums binary32.
+//
+// A workgroup of WM x WN waves owns a TM x TN tile of C and holds two k-steps of both operands in LDS, filled by
+// loads that go from memory to LDS directly while the other k-step is multiplied.  Row r of a k-step lies at
+// r * 128 bytes with its eight 16-byte chunks permuted by r & 7, which the loads do by choosing whose chunk a lane
+// fetches: the sixteen rows that a wave reads at once then fall on all banks.
+// After the loop every wave stages its part of C, 64 x 64 values at a time, in its own 16 KB of the same LDS and
+// hands it to the job, which reads it along rows or along columns, eight values a lane, and writes what it needs.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace agc {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 tile_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float tile_f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t tile_u32x4 __attribute__((ext_vector_type(4)));
+
+enum TilePair { kPlain, kSplit };
+
+struct TilePos {
+    int m0, n0;    // first row and column of the tile
+    int batch;     // matrix or partition
+    int steps;     // k-steps
+};
+
+// Workgroup id -> place in the order of the tiles.  Workgroups go to the eight XCDs in turn; each XCD gets a
+// contiguous run of tiles, so that the rows its tiles share stay in its own L2.
+__device__ __forceinline__ int xcd_order(int id, int total)
+{
+    const int x = id & 7, per = total >> 3, rem = total & 7;
+    return x * per + (x < rem ? x : rem) + (id >> 3);
+}
+
+// Place in the order -> (row tile, column tile) of mt x nt tiles: columns of up to kGroup row tiles, so that the 32
+// tiles that an XCD works on at once form a block and not a line.
+__device__ __forceinline__ void tile_order(int t, int mt, int nt, int& mi, int& ni)
+{
+    constexpr int kGroup = 8;
+    const int block = t / (kGroup * nt), in = t - block * kGroup * nt;
+    const int rows = mt - block * kGroup < kGroup ? mt - block * kGroup : kGroup;
+    ni = in / rows;
+    mi = block * kGroup + in - ni * rows;
+}
+
+// Place in the order -> (row tile, column tile <= row tile) of the lower triangle of a square of tiles.
+__device__ __forceinline__ void triangle_order(int t, int& mi, int& ni)
+{
+    int r = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+    while ((r + 1) * (r + 2) / 2 <= t) ++r;      // the root is near, not exact
+    while (r * (r + 1) / 2 > t) --r;
+    mi = r;
+    ni = t - r * (r + 1) / 2;
+}
+
+// ------------------------------------------------------------------ the staged part of C
+// Value (r, c) of a 64 x 64 piece: the column is permuted by what the row's bits say, so that the writes from the
+// matrix units' layout (4 x 16 rows and columns a wave), reads along rows and reads along columns (8 x 8 of them)
+// each fall on all 64 banks.
+__device__ __forceinline__ int piece_at(int r, int c)
+{
+    return r * 64 + (c ^ ((((r >> 2) & 3) << 4) ^ (((r >> 4) & 1) << 3) ^ (((r >> 5) & 1) << 4)));
+}
+
+__device__ __forceinline__ void piece_row8(const float* s, int r, int c, float v[8])
+{
+    const tile_f32x4* p = reinterpret_cast<const tile_f32x4*>(s + piece_at(r, c));
+    const tile_f32x4 a = p[0], b = p[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+}
+
+__device__ __forceinline__ void piece_put_row8(float* s, int r, int c, const float v[8])
+{
+    tile_f32x4* p = reinterpret_cast<tile_f32x4*>(s + piece_at(r, c));
+    p[0] = tile_f32x4{v[0], v[1], v[2], v[3]};
+    p[1] = tile_f32x4{v[4], v[5], v[6], v[7]};
+}
+
+__device__ __forceinline__ void piece_col8(const float* s, int r, int c, float v[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = s[piece_at(r + i, c)];
+}
+
+// Lanes of one wave hand values to each other through LDS: nothing may move across.
+__device__ __forceinline__ void wave_lds_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// ------------------------------------------------------------------ 16-bit stores
+__device__ __forceinline__ uint32_t bf16_bits(float v)
+{
+    return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v);   // to nearest even
+}
+
+__device__ __forceinline__ tile_u32x4 bf16_pack8(const float v[8])
+{
+    tile_u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
+    return o;
+}
+
+__device__ __forceinline__ void bf16_unpack8(const tile_u32x4& u, float v[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+}
+
+// Eight values as binary16 pairs at element k (a multiple of 8) of a split row.
+__device__ __forceinline__ void split_store8(char* row, int k, const float v[8])
+{
+    f16x8 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        hi[i] = (_Float16)v[i];
+        lo[i] = (_Float16)(v[i] - (float)hi[i]);
+    }
+    char* p = row + (int64_t)(k >> 5) * 128 + (k & 31) * 2;
+    *reinterpret_cast<f16x8*>(p) = hi;
+    *reinterpret_cast<f16x8*>(p + 64) = lo;
+}
+
+__device__ __forceinline__ void split_load8(const char* row, int k, float v[8])
+{
+    const char* p = row + (int64_t)(k >> 5) * 128 + (k & 31) * 2;
+    const f16x8 hi = *reinterpret_cast<const f16x8*>(p), lo = *reinterpret_cast<const f16x8*>(p + 64);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)hi[i] + (float)lo[i];
+}
+
+// ------------------------------------------------------------------ the loop
+template <TilePair PAIR>
+__device__ __forceinline__ tile_f32x4 tile_mfma(const tile_u32x4& a, const tile_u32x4& b, const tile_f32x4& c)
+{
+    if constexpr (PAIR == kPlain)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(tile_bf16x8, a),
+                                                       __builtin_bit_cast(tile_bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+}
+
+__device__ __forceinline__ void load16_to_lds(const char* src, char* dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                     (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+// JOB: kPair; bool place(int id, TilePos&); const char* a_row(pos, r), b_row(pos, r): where row r of the tile starts
+// (rows past the matrix name a row inside it; their results are not used); void piece(pos, m, n, float* s, lane): what
+// becomes of the 64 x 64 values staged at s, the first of them C[m, n].
+template <class JOB, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64, (TM == 256 && TN == 256) ? 2 : 2) void k_tile(const JOB job)
+{
+    constexpr int kThreads = WM * WN * 64;
+    constexpr int kWaveM = TM / WM, kWaveN = TN / WN, kFm = kWaveM / 16, kFn = kWaveN / 16;
+    constexpr int kStep = (TM + TN) * 128;
+    constexpr int kLds = 2 * kStep > WM * WN * 16384 ? 2 * kStep : WM * WN * 16384;
+    constexpr int kIssueA = TM * 8 / kThreads, kIssueB = TN * 8 / kThreads, kIssueRows = kThreads / 8;
+    static_assert(kWaveM % 64 == 0 && kWaveN == 64, "a wave stages pieces of 64 x 64");
+    __shared__ __attribute__((aligned(1024))) char lds[kLds];
+
+    TilePos pos;
+    if (!job.place((int)blockIdx.x, pos)) return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave - wm * WN;
+
+    const char *src_a[kIssueA], *src_b[kIssueB];
+    const int chunk = ((tid & 7) ^ ((tid >> 3) & 7)) * 16;
+#pragma unroll
+    for (int i = 0; i < kIssueA; ++i) src_a[i] = job.a_row(pos, i * kIssueRows + (tid >> 3)) + chunk;
+#pragma unroll
+    for (int i = 0; i < kIssueB; ++i) src_b[i] = job.b_row(pos, i * kIssueRows + (tid >> 3)) + chunk;
+
+    auto issue = [&](int half) {
+        char* base = lds + half * kStep + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < kIssueA; ++i) {
+            load16_to_lds(src_a[i], base + i * kIssueRows * 128);
+            src_a[i] += 128;
+        }
+#pragma unroll
+        for (int i = 0; i < kIssueB; ++i) {
+            load16_to_lds(src_b[i], base + TM * 128 + i * kIssueRows * 128);
+            src_b[i] += 128;
+        }
+    };
+
+    tile_f32x4 acc[kFm][kFn];
+#pragma unroll
+    for (int i = 0; i < kFm; ++i)
+#pragma unroll
+        for (int j = 0; j < kFn; ++j) acc[i][j] = tile_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const int row = (lane & 15) * 128, q = lane >> 4;
+    const int at0 = row + ((q ^ (lane & 7)) << 4), at1 = row + (((4 + q) ^ (lane & 7)) << 4);
+    auto multiply = [&](int half) {
+        const char* a = lds + half * kStep + wm * kWaveM * 128;
+        const char* b = lds + half * kStep + TM * 128 + wn * kWaveN * 128;
+        tile_u32x4 b0[kFn], b1[kFn];
+#pragma unroll
+        for (int j = 0; j < kFn; ++j) {
+            b0[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at0);
+            b1[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at1);
+        }
+#pragma unroll
+        for (int i = 0; i < kFm; ++i) {
+            const tile_u32x4 a0 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at0);
+            const tile_u32x4 a1 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at1);
+#pragma unroll
+            for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a0, b0[j], acc[i][j]);
+            if constexpr (JOB::kPair == kPlain) {
+#pragma unroll
+                for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a1, b1[j], acc[i][j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a0, b1[j], acc[i][j]);
+#pragma unroll
+                for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a1, b0[j], acc[i][j]);
+            }
+        }
+    };
+
+    if (pos.steps > 0) issue(0);
+    for (int k = 0; k < pos.steps; ++k) {
+        __syncthreads();   // this k-step has arrived, and nobody reads the other half any more
+        if (k + 1 < pos.steps) issue((k + 1) & 1);
+        multiply(k & 1);
+    }
+
+    __syncthreads();
+    float* mine = reinterpret_cast<float*>(lds) + wave * 4096;
+#pragma unroll
+    for (int p = 0; p < kWaveM / 64; ++p) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    mine[piece_at(i * 16 + q * 4 + e, j * 16 + (lane & 15))] = acc[p * 4 + i][j][e];
+        wave_lds_fence();
+        job.piece(pos, pos.m0 + wm * kWaveM + p * 64, pos.n0 + wn * 64, mine, lane);
+        wave_lds_fence();
+    }
+}
+
+}  // namespace agc
