@@ -284,6 +284,42 @@ agc_status agc_adam_update(float *beta_dev, float *m1_dev, float *m2_dev, const 
 /* --------------------------------------------------------------------------------------
  * Token models: two producers of rows of G and a consumer of g_hat
  * ------------------------------------------------------------------------------------ */
+typedef enum {
+    AGC_ACT_SILU = 0, /* a / (1 + exp(-a)) */
+    AGC_ACT_GELU = 1  /* a * Phi(a), by erf */
+} agc_activation;
+
+/* Gated feed-forward block in bfloat16:  h = act(x Wg^T) * (x Wu^T), sums and activation in binary32, h rounded once.
+ *   x_dev      device, n_tokens x d_in, row stride ldx elements
+ *   w_gate_dev, w_up_dev  device, d_ff x d_in, row stride ldw (their sections of the parameter vector, rounded to
+ *              bfloat16, for instance)
+ *   h_dev      device, n_tokens x d_ff, row stride ldh; overwritten
+ *   workspace_dev  device, agc_gated_workspace_bytes(n_tokens, d_in, d_ff, 0) bytes, 256-byte aligned; scratch
+ * Any alignment of the operands and any sizes: 0 <= n_tokens <= 2^26, 1 <= d_in, d_ff <= 65536.  Up to 64 tokens take
+ * a form that is bound by the one read of the weights; rows that are not whole multiples of 128 bytes, 16-byte
+ * aligned, are copied to the workspace first when there are more. */
+int64_t agc_gated_workspace_bytes(int64_t n_tokens, int d_in, int d_ff, int k_parts);
+agc_status agc_gated_forward(const void *x_dev, int64_t ldx, const void *w_gate_dev, const void *w_up_dev, int64_t ldw,
+                             int64_t n_tokens, int d_in, int d_ff, int act, void *h_dev, int64_t ldh, void *workspace_dev,
+                             void *hip_stream);
+/* Its partial gradients (Sec. II-A: g_j = grad L(D_j, beta)): with a = x Wg^T, u = x Wu^T, which are formed again,
+ *   da = dh u act'(a),  du = dh act(a),  dx = da Wg + du Wu,
+ * and for every data partition p (a run of tokens)  G_gate[p] = da_p^T x_p,  G_up[p] = du_p^T x_p, binary32.
+ *   dh_dev     device, n_tokens x d_ff bfloat16, row stride lddh
+ *   part_end_host  host, k_parts ends of the partitions in tokens, not descending, the last n_tokens; partition p is
+ *              [part_end[p-1], part_end[p]) and may be empty: its gradients are zeros
+ *   dx_dev     device, n_tokens x d_in bfloat16, row stride lddx; overwritten.  NULL: not wanted
+ *   G_gate_dev, G_up_dev  device, where row 0 of G holds the d_ff x d_in gradients of Wg and of Wu (row-major);
+ *              row p lies p * ldg floats on; overwritten
+ *   workspace_dev  device, agc_gated_workspace_bytes(n_tokens, d_in, d_ff, k_parts) bytes, 256-byte aligned
+ * da and du enter dx rounded to bfloat16, and G as pairs of bfloat16 (16 bits); sums are binary32 in a fixed order.
+ * 1 <= k_parts <= 256; ldg >= d_in * d_ff. */
+agc_status agc_gated_partial_gradients(const void *x_dev, int64_t ldx, const void *w_gate_dev, const void *w_up_dev,
+                                       int64_t ldw, const void *dh_dev, int64_t lddh, int64_t n_tokens,
+                                       const int64_t *part_end_host, int k_parts, int d_in, int d_ff, int act, void *dx_dev,
+                                       int64_t lddx, float *G_gate_dev, float *G_up_dev, int64_t ldg, void *workspace_dev,
+                                       void *hip_stream);
+
 /* Orthogonalised update of n_mats matrices of one shape that lie inside the parameter vector.  For each,
  *   M <- momentum * M + g_hat;   U = g_hat + momentum * M (nesterov) or M;   X = U / (|U|_F + 1e-7);
  *   `steps` times  A = X X^T,  X <- a X + (b A + c A A) X,  a, b, c = 3.4445, -4.7750, 2.0315;

@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libagc.so")
 AGC_OK = 0
 AGC_EINVAL, AGC_ESHAPE, AGC_EBITS, AGC_EALIGN, AGC_ENOMEM, AGC_EHIP, AGC_ESTATE = -1, -2, -3, -4, -5, -6, -7
 AGC_SCALE_L2, AGC_SCALE_MAXABS = 0, 1
+AGC_ACT_SILU, AGC_ACT_GELU = 0, 1
 AGC_MAX_WORKERS, AGC_MAX_BITS, AGC_NUM_KERNELS, AGC_MAX_LAYERS = 256, 16, 4, 256
 KERNEL_NAMES = ("scale_pass", "scale_finalize", "quantize", "decode")
 
@@ -23,6 +24,7 @@ EXPORTS = [
     "agc_create", "agc_destroy", "agc_set_code", "agc_code_path", "agc_code_bytes", "agc_last_error",
     "agc_encode_quantize", "agc_decode", "agc_step", "agc_profile_enable", "agc_profile_read",
     "agc_scales_per_worker", "agc_set_layers", "agc_decode2", "agc_decode_noalloc", "agc_adam_update", "agc_second_moment_decoder",
+    "agc_gated_workspace_bytes", "agc_gated_forward", "agc_gated_partial_gradients",
     "agc_muon_workspace_bytes", "agc_muon_update",
     "agc_calibration_copy", "agc_debug_force_long", "agc_debug_sketch", "agc_debug_sketch_last", "agc_debug_sketch_max", "agc_debug_stream_rows", "agc_ls_workspace_floats", "agc_ls_partial_gradients", "agc_gd_update",
     "agc_phi_coef_balanced", "agc_alloc_bits", "agc_alloc_bits_dp", "agc_alloc_objective",
@@ -104,6 +106,15 @@ def load():
     L.agc_ls_partial_gradients.restype = C.c_int
     L.agc_gd_update.argtypes = [_vp, _vp, C.c_float, C.c_int64, _vp]
     L.agc_gd_update.restype = C.c_int
+    L.agc_gated_workspace_bytes.argtypes = [C.c_int64, C.c_int, C.c_int, C.c_int]
+    L.agc_gated_workspace_bytes.restype = C.c_int64
+    L.agc_gated_forward.argtypes = [_vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_int, _vp,
+                                    C.c_int64, _vp, _vp]
+    L.agc_gated_forward.restype = C.c_int
+    L.agc_gated_partial_gradients.argtypes = [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, C.c_int64, C.c_int64, _vp,
+                                              C.c_int, C.c_int, C.c_int, C.c_int, _vp, C.c_int64, _vp, _vp, C.c_int64,
+                                              _vp, _vp]
+    L.agc_gated_partial_gradients.restype = C.c_int
     L.agc_muon_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
     L.agc_muon_workspace_bytes.restype = C.c_int64
     L.agc_muon_update.argtypes = [_vp, _vp, _vp, _vp, C.c_int, C.c_int, C.c_int, C.c_float, C.c_float, C.c_int,
@@ -147,6 +158,16 @@ def load():
     L.agc_check_unbiased.restype = C.c_int
     _lib = L
     return L
+
+
+def _bfloat16():
+    import torch
+    return torch.bfloat16
+
+
+def _float32():
+    import torch
+    return torch.float32
 
 
 def _np(a, dtype):
@@ -469,6 +490,65 @@ def agc_adam_update(beta, m1, m2, ghat, ghat2, lr, beta1, beta2, eps, t, stream=
                                 _stream_handle(stream))
     if st != AGC_OK:
         raise AgcError(st, "agc_adam_update")
+
+
+_ACTS = {"silu": AGC_ACT_SILU, "gelu": AGC_ACT_GELU}
+
+
+def _rows_of(t, rows, cols, dtype, what):
+    """Row stride of a (rows, cols) row-major view; AGC_ESHAPE if it is none, or smaller, or of another type."""
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or t.dtype != dtype or (cols > 1 and t.stride(1) != 1):
+        raise AgcError(AGC_ESHAPE, f"{what} must be a ({rows}, {cols}) row-major view of {dtype}, got "
+                                   f"{tuple(t.shape)} of {t.dtype}")
+    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def agc_gated_workspace_bytes(n_tokens, d_in, d_ff, k_parts=0):
+    """k_parts = 0: of agc_gated_forward alone."""
+    return int(load().agc_gated_workspace_bytes(int(n_tokens), int(d_in), int(d_ff), int(k_parts)))
+
+
+def agc_gated_forward(x, w_gate, w_up, act, h, workspace, stream=None, check=True):
+    """h = act(x w_gate^T) * (x w_up^T), all bfloat16; x (tokens, d_in), weights (d_ff, d_in), h (tokens, d_ff)."""
+    L = load()
+    (tokens, d_in), d_ff, bf16 = x.shape, w_gate.shape[0], w_gate.dtype
+    ldw = _rows_of(w_gate, d_ff, d_in, _bfloat16(), "w_gate")
+    if _rows_of(w_up, d_ff, d_in, bf16, "w_up") != ldw:
+        raise AgcError(AGC_ESHAPE, "w_gate and w_up must have one row stride")
+    ldx, ldh = _rows_of(x, tokens, d_in, bf16, "x"), _rows_of(h, tokens, d_ff, bf16, "h")
+    if workspace.numel() * workspace.element_size() < L.agc_gated_workspace_bytes(tokens, d_in, d_ff, 0):
+        raise AgcError(AGC_ESHAPE, "agc_gated_forward: the workspace is too small")
+    st = L.agc_gated_forward(x.data_ptr(), ldx, w_gate.data_ptr(), w_up.data_ptr(), ldw, tokens, d_in, d_ff,
+                             _ACTS.get(act, act), h.data_ptr(), ldh, workspace.data_ptr(), _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
+
+
+def agc_gated_partial_gradients(x, w_gate, w_up, act, dh, part_end, dx, G_gate, G_up, workspace, stream=None, check=True):
+    """dx (bfloat16, or None) and, for each partition of the tokens, the gradients of both weights: G_gate and G_up are
+    (k_parts, d_ff * d_in) float32 views of the same rows of G."""
+    L = load()
+    (tokens, d_in), d_ff, bf16 = x.shape, w_gate.shape[0], w_gate.dtype
+    ldw = _rows_of(w_gate, d_ff, d_in, _bfloat16(), "w_gate")
+    if _rows_of(w_up, d_ff, d_in, bf16, "w_up") != ldw:
+        raise AgcError(AGC_ESHAPE, "w_gate and w_up must have one row stride")
+    ldx, lddh = _rows_of(x, tokens, d_in, bf16, "x"), _rows_of(dh, tokens, d_ff, bf16, "dh")
+    lddx = d_in if dx is None else _rows_of(dx, tokens, d_in, bf16, "dx")
+    k = len(part_end)
+    ldg = _rows_of(G_gate, k, d_ff * d_in, _float32(), "G_gate")
+    if _rows_of(G_up, k, d_ff * d_in, _float32(), "G_up") != ldg:
+        raise AgcError(AGC_ESHAPE, "G_gate and G_up must have one row stride")
+    if workspace.numel() * workspace.element_size() < L.agc_gated_workspace_bytes(tokens, d_in, d_ff, k):
+        raise AgcError(AGC_ESHAPE, "agc_gated_partial_gradients: the workspace is too small")
+    st = L.agc_gated_partial_gradients(x.data_ptr(), ldx, w_gate.data_ptr(), w_up.data_ptr(), ldw, dh.data_ptr(), lddh,
+                                       tokens, struct.pack(f"{k}q", *[int(e) for e in part_end]), k, d_in, d_ff,
+                                       _ACTS.get(act, act), None if dx is None else dx.data_ptr(), lddx,
+                                       G_gate.data_ptr(), G_up.data_ptr(), ldg, workspace.data_ptr(),
+                                       _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
 
 
 def agc_muon_workspace_bytes(rows, cols, n_mats):

@@ -1,0 +1,578 @@
+// Gated feed-forward block, bfloat16:  a = x Wg^T, u = x Wu^T, h = act(a) * u, and its gradients by data partition
+// (rows of G).  x is tokens x d_in, Wg and Wu are d_ff x d_in, all row-major.
+//
+// Forward: one product whose columns take 16 rows of Wg and 16 rows of Wu in turn, so that a wave ends with a and u of
+// the same places; activation and product follow from the binary32 sums, h is rounded once.
+//
+// Gradients: a and u are formed again (4 T D F operations, less than storing them in binary32 would save), and
+//   da = dh u act'(a), du = dh act(a)          in the same pass
+//   dx = da Wg + du Wu                          one product over 2 F
+//   dWg_p = da_p^T x_p, dWu_p = du_p^T x_p      one product of 2 F rows a partition, written into row p of G
+// da and du enter dx rounded to bfloat16, as dx itself is; they enter G, which is binary32, as pairs of bfloat16
+// (16 bits, off by at most 2^-16): rounded once they would leave up to 2^-8 in every term of G.
+// The tile loop wants both operands contiguous along the sum: x and the weights are turned by passes of their own, da
+// and du are written both ways.  A partition starts at a multiple of 32 in the turned order, the places between are
+// zeros; `map` gives each place its token, or -1.
+#include "agc_operators.h"
+#include "agc_tile.h"
+
+namespace agc {
+
+namespace {
+
+constexpr int kBlock = 256;
+
+// what the kernels know of the partitions: first place and first token of each
+struct GatedParts {
+    int place[kMostParts + 1];
+    int token[kMostParts + 1];
+    int k;
+};
+
+struct Activation {
+    int gelu;
+    // activation and its derivative
+    __device__ __forceinline__ void at(float a, float& value, float& slope) const
+    {
+        if (gelu) {
+            const float cdf = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
+            value = a * cdf;
+            slope = fmaf(a * 0.39894228040143268f, expf(-0.5f * a * a), cdf);
+        } else {
+            const float sig = 1.0f / (1.0f + expf(-a));
+            value = a * sig;
+            slope = sig * fmaf(a, 1.0f - sig, 1.0f);
+        }
+    }
+    __device__ __forceinline__ float operator()(float a) const
+    {
+        return gelu ? a * (0.5f * (1.0f + erff(a * 0.70710678118654752f))) : a / (1.0f + expf(-a));
+    }
+};
+
+__device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// `count` of eight consecutive bfloat16 values, rounded
+__device__ __forceinline__ void store_bf16(uint16_t* o, int count, const float v[8])
+{
+    if (count >= 8 && aligned16(o)) {
+        *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < count) o[e] = (uint16_t)bf16_bits(v[e]);
+    }
+}
+
+__device__ __forceinline__ void load_bf16(const uint16_t* o, int count, float v[8])
+{
+    if (count >= 8 && aligned16(o)) {
+        bf16_unpack8(*reinterpret_cast<const tile_u32x4*>(o), v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < count ? __uint_as_float((uint32_t)o[e] << 16) : 0.0f;
+    }
+}
+
+// The 16 bytes of a bfloat16 row from element k on; elements from `end` on are zeros.
+__device__ __forceinline__ tile_u32x4 load_bits8(const uint16_t* row, int k, int end)
+{
+    const uint16_t* p = row + k;
+    if (k + 8 <= end && aligned16(p)) return *reinterpret_cast<const tile_u32x4*>(p);
+    tile_u32x4 o = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (k + e < end) o[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+    return o;
+}
+
+// ------------------------------------------------------------------ laying operands out
+// Rows whose width or alignment the tile loop's loads do not take: copied to rows of a whole number of k-steps.
+__global__ __launch_bounds__(kBlock) void k_pack_rows(const uint16_t* src, int64_t ld, int64_t rows, int width, int up,
+                                                      uint16_t* dst)
+{
+    const int per = up / 8;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int c = threadIdx.x; c < per; c += kBlock)
+            *reinterpret_cast<tile_u32x4*>(dst + r * up + c * 8) = load_bits8(src + r * ld, c * 8, width);
+}
+
+__global__ __launch_bounds__(kBlock) void k_gated_map(const GatedParts parts, int places, int* map)
+{
+    const int i = blockIdx.x * kBlock + threadIdx.x;
+    if (i >= places) return;
+    int lo = 0, hi = parts.k - 1;   // the last partition that starts at or before i
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (parts.place[mid] <= i) lo = mid;
+        else hi = mid - 1;
+    }
+    const int t = parts.token[lo] + (i - parts.place[lo]);
+    map[i] = t < parts.token[lo + 1] ? t : -1;
+}
+
+// dst row c = column c of src, along the rows of src (through `map`, if given; -1 and rows past the end are zeros),
+// `up` of them.  TWICE: in groups of 32, each twice, as the second operand of pairs.
+template <bool TWICE>
+__global__ __launch_bounds__(kBlock) void k_turn(const uint16_t* src, int64_t ld, int rows, int cols, int up, const int* map,
+                                                 char* dst, int64_t pitch)
+{
+    __shared__ uint16_t tile[64][66];
+    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, tid = threadIdx.x;
+    for (int i = tid; i < 512; i += kBlock) {
+        const int r = i >> 3, c = (i & 7) * 8;
+        int from = r0 + r < rows ? r0 + r : -1;
+        if (map && from >= 0) from = map[from];
+        tile_u32x4 v = {0u, 0u, 0u, 0u};
+        if (from >= 0 && c0 + c < cols) v = load_bits8(src + (int64_t)from * ld, c0 + c, cols);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(&tile[r][c + 2 * e]) = v[e];
+    }
+    __syncthreads();
+    for (int i = tid; i < 512; i += kBlock) {
+        const int c = i >> 3, r = (i & 7) * 8;
+        if (c0 + c >= cols || r0 + r >= up) continue;
+        tile_u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (uint32_t)tile[r + 2 * e][c] | ((uint32_t)tile[r + 2 * e + 1][c] << 16);
+        char* row = dst + (int64_t)(c0 + c) * pitch;
+        const int at = r0 + r;
+        if (TWICE) {
+            char* p = row + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
+            *reinterpret_cast<tile_u32x4*>(p) = v;
+            *reinterpret_cast<tile_u32x4*>(p + 64) = v;
+        } else {
+            *reinterpret_cast<tile_u32x4*>(row + (int64_t)at * 2) = v;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ few tokens
+// Up to NT * 16 tokens: bound by the one read of the weights.  A workgroup takes 16 rows of Wg and of Wu, its four
+// waves take turns along the sum, 128 bytes of every row at a time, straight from memory into the matrix units'
+// layout (weights as the 16 rows, tokens as the 16 columns); the waves' sums meet in LDS.
+// WHOLE: every 16 bytes of every row may be loaded as they are (d_in a multiple of 64, rows aligned).
+template <int NT, bool WHOLE>
+__global__ __launch_bounds__(kBlock) void k_gated_few(const uint16_t* x, int64_t ldx, const uint16_t* wg, const uint16_t* wu,
+                                                      int64_t ldw, int tokens, int d_in, int d_ff, Activation act,
+                                                      uint16_t* h, int64_t ldh)
+{
+    __shared__ float part[4][2][NT][256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int f0 = blockIdx.x * 16, q = lane >> 4;
+    const int f = f0 + (lane & 15) < d_ff ? f0 + (lane & 15) : d_ff - 1;
+    const uint16_t *rg = wg + f * ldw, *ru = wu + f * ldw;
+    const uint16_t* rx[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int tok = t * 16 + (lane & 15);
+        rx[t] = x + (int64_t)(tok < tokens ? tok : tokens - 1) * ldx;
+    }
+    tile_f32x4 acc[2][NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[0][t] = acc[1][t] = tile_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (WHOLE) {
+        // four turns' loads at once; turns past the end load the last one again and count as zeros
+        const tile_u32x4 zero = {0u, 0u, 0u, 0u};
+        for (int k0 = wave * 64; k0 < d_in; k0 += 1024) {
+            tile_u32x4 a[8], b[8], v[8][NT];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int k1 = k0 + (i >> 1) * 256, k = (k1 < d_in ? k1 : d_in - 64) + q * 16 + (i & 1) * 8;
+                a[i] = *reinterpret_cast<const tile_u32x4*>(rg + k);
+                b[i] = *reinterpret_cast<const tile_u32x4*>(ru + k);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) v[i][t] = *reinterpret_cast<const tile_u32x4*>(rx[t] + k);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool on = k0 + (i >> 1) * 256 < d_in;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const tile_u32x4 w = on ? v[i][t] : zero;
+                    acc[0][t] = tile_mfma<kPlain>(on ? a[i] : zero, w, acc[0][t]);
+                    acc[1][t] = tile_mfma<kPlain>(on ? b[i] : zero, w, acc[1][t]);
+                }
+            }
+        }
+    } else {
+        for (int k0 = wave * 64; k0 < d_in; k0 += 256) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int k = k0 + q * 16 + s * 8;
+                const tile_u32x4 a = load_bits8(rg, k, d_in), b = load_bits8(ru, k, d_in);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const tile_u32x4 v = load_bits8(rx[t], k, d_in);
+                    acc[0][t] = tile_mfma<kPlain>(a, v, acc[0][t]);
+                    acc[1][t] = tile_mfma<kPlain>(b, v, acc[1][t]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            part[wave][0][t][(lane & 15) * 16 + q * 4 + e] = acc[0][t][e];
+            part[wave][1][t][(lane & 15) * 16 + q * 4 + e] = acc[1][t][e];
+        }
+    __syncthreads();
+    const int tok = tid >> 4, ff = f0 + (tid & 15);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (t * 16 + tok >= tokens || ff >= d_ff) continue;
+        const float a = (part[0][0][t][tid] + part[1][0][t][tid]) + (part[2][0][t][tid] + part[3][0][t][tid]);
+        const float u = (part[0][1][t][tid] + part[1][1][t][tid]) + (part[2][1][t][tid] + part[3][1][t][tid]);
+        h[(int64_t)(t * 16 + tok) * ldh + ff] = (uint16_t)bf16_bits(act(a) * u);
+    }
+}
+
+// ------------------------------------------------------------------ products
+// x against both weights.  GRAD: da and du, both ways; otherwise h.
+template <bool GRAD>
+struct GateJob {
+    static constexpr TilePair kPair = kPlain;
+    const uint16_t *x, *wg, *wu;      // rows of whole k-steps
+    int64_t ldx, ldg, ldu;
+    int rows, d_ff, steps;            // rows: tokens, or places of `map`
+    Activation act;
+    const int* map;
+    // forward
+    uint16_t* h;
+    int64_t ldh;
+    // gradient
+    const uint16_t* dh;
+    int64_t lddh;
+    char* by_token;                   // places x 2 fp: da | du
+    int fp;
+    char* by_feature;                 // 2 d_ff rows of pairs along the places
+    int64_t pitch;
+    int mt, nt, side_m, side_n, total;
+
+    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    {
+        int mi, ni;
+        tile_order(xcd_order(id, total), mt, nt, mi, ni);
+        p.batch = 0, p.m0 = mi * side_m, p.n0 = ni * side_n, p.steps = steps;
+        return true;
+    }
+    __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
+    {
+        int at = p.m0 + r < rows ? p.m0 + r : rows - 1;
+        if (GRAD) at = map[at] < 0 ? 0 : map[at];
+        return reinterpret_cast<const char*>(x + at * ldx);
+    }
+    __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const
+    {
+        const int i = p.n0 + r, at = (i >> 5) * 16 + (i & 15);
+        const int64_t f = at < d_ff ? at : d_ff - 1;
+        return reinterpret_cast<const char*>((i & 16) ? wu + f * ldu : wg + f * ldg);
+    }
+    __device__ __forceinline__ void piece(const TilePos&, int mb, int nb, float* s, int lane) const
+    {
+        const int j = lane & 3, ca = (j >> 1) * 32 + (j & 1) * 8, f = nb / 2 + j * 8;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int r = it * 16 + (lane >> 2), row = mb + r;
+            float a[8], u[8];
+            piece_row8(s, r, ca, a);
+            piece_row8(s, r, ca + 16, u);
+            if (!GRAD) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] = act(a[e]) * u[e];
+                if (row < rows && f < d_ff) store_bf16(h + row * ldh + f, d_ff - f, a);
+                continue;
+            }
+            float da[8], du[8], g[8];
+            const int t = row < rows ? map[row] : -1;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) da[e] = du[e] = 0.0f;
+            if (t >= 0 && f < d_ff) {
+                load_bf16(dh + t * lddh + f, d_ff - f, g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float value, slope;
+                    act.at(a[e], value, slope);
+                    if (f + e < d_ff) da[e] = g[e] * u[e] * slope, du[e] = g[e] * value;
+                }
+            }
+            if (row < rows && f < fp) {
+                uint16_t* o = reinterpret_cast<uint16_t*>(by_token) + (int64_t)row * 2 * fp + f;
+                *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(da);
+                *reinterpret_cast<tile_u32x4*>(o + fp) = bf16_pack8(du);
+            }
+            piece_put_row8(s, r, ca, da);
+            piece_put_row8(s, r, ca + 16, du);
+        }
+        if (!GRAD) return;
+        wave_lds_fence();
+        const int run = (lane & 7) * 8, at = mb + run;
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int c = it * 8 + (lane >> 3), ff = nb / 2 + (c >> 5) * 16 + (c & 15);
+            if (ff >= d_ff || at >= rows) continue;   // rows is a multiple of 32
+            float v[8], hi[8], lo[8];
+            piece_col8(s, run, c, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                hi[e] = __uint_as_float(bf16_bits(v[e]) << 16);
+                lo[e] = v[e] - hi[e];
+            }
+            char* o = by_feature + (int64_t)(((c & 16) ? d_ff : 0) + ff) * pitch + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
+            *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(hi);
+            *reinterpret_cast<tile_u32x4*>(o + 64) = bf16_pack8(lo);
+        }
+    }
+};
+
+// dx = [da | du] [Wg | Wu]^T
+struct InputJob {
+    static constexpr TilePair kPair = kPlain;
+    const char *a, *b;
+    int64_t pitch;
+    int rows, d_in, steps;
+    const int* map;
+    uint16_t* dx;
+    int64_t lddx;
+    int mt, nt, side_m, side_n, total;
+
+    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    {
+        int mi, ni;
+        tile_order(xcd_order(id, total), mt, nt, mi, ni);
+        p.batch = 0, p.m0 = mi * side_m, p.n0 = ni * side_n, p.steps = steps;
+        return true;
+    }
+    __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
+    {
+        return a + (p.m0 + r < rows ? p.m0 + r : rows - 1) * pitch;
+    }
+    __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const
+    {
+        return b + (p.n0 + r < d_in ? p.n0 + r : d_in - 1) * pitch;
+    }
+    __device__ __forceinline__ void piece(const TilePos&, int mb, int nb, float* s, int lane) const
+    {
+        const int run = (lane & 7) * 8, c = nb + run;
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int r = it * 8 + (lane >> 3), row = mb + r;
+            const int t = row < rows ? map[row] : -1;
+            if (t < 0 || c >= d_in) continue;
+            float v[8];
+            piece_row8(s, r, run, v);
+            store_bf16(dx + t * lddx + c, d_in - c, v);
+        }
+    }
+};
+
+// Row p of G: [da | du]_p^T x_p
+struct WeightJob {
+    static constexpr TilePair kPair = kPlain;
+    const char *a, *b;        // 2 d_ff and d_in rows along the places
+    int64_t pitch;
+    int d_ff, d_in;
+    float *gate, *up;
+    int64_t ldg;
+    int mt, nt, side_m, side_n, total;
+    GatedParts parts;
+
+    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    {
+        const int t = xcd_order(id, total);
+        p.batch = t / (mt * nt);
+        int mi, ni;
+        tile_order(t - p.batch * mt * nt, mt, nt, mi, ni);
+        p.m0 = mi * side_m, p.n0 = ni * side_n;
+        p.steps = (parts.place[p.batch + 1] - parts.place[p.batch]) >> 5;
+        return true;
+    }
+    __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
+    {
+        return a + (int64_t)(p.m0 + r < 2 * d_ff ? p.m0 + r : 2 * d_ff - 1) * pitch + (int64_t)parts.place[p.batch] * 4;
+    }
+    __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const
+    {
+        return b + (int64_t)(p.n0 + r < d_in ? p.n0 + r : d_in - 1) * pitch + (int64_t)parts.place[p.batch] * 4;
+    }
+    __device__ __forceinline__ void piece(const TilePos& p, int mb, int nb, float* s, int lane) const
+    {
+        const int run = (lane & 7) * 8, c = nb + run;
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int r = it * 8 + (lane >> 3), row = mb + r;
+            if (row >= 2 * d_ff || c >= d_in) continue;
+            float v[8];
+            piece_row8(s, r, run, v);
+            float* o = (row < d_ff ? gate + (int64_t)row * d_in : up + (int64_t)(row - d_ff) * d_in) + p.batch * ldg + c;
+            if (d_in - c >= 8 && aligned16(o)) {
+                reinterpret_cast<tile_f32x4*>(o)[0] = tile_f32x4{v[0], v[1], v[2], v[3]};
+                reinterpret_cast<tile_f32x4*>(o)[1] = tile_f32x4{v[4], v[5], v[6], v[7]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < d_in) o[e] = v[e];
+            }
+        }
+    }
+};
+
+// 256 x 256 tiles where they fill the 256 compute units about as well as 128 x 128 tiles do, two of which share one
+template <class JOB>
+hipError_t launch_product(JOB j, int batch, int64_t m, int64_t n, hipStream_t stream)
+{
+    const int64_t bm = (m + 255) / 256, bn = (n + 255) / 256, sm = (m + 127) / 128, sn = (n + 127) / 128;
+    const bool big = (batch * bm * bn + 255) / 256 * 4 <= (batch * sm * sn + 511) / 512 * 2;
+    const int64_t total = batch * (big ? bm * bn : sm * sn);
+    if (total > INT32_MAX) return hipErrorInvalidConfiguration;
+    j.side_m = j.side_n = big ? 256 : 128;
+    j.mt = (int)(big ? bm : sm);
+    j.nt = (int)(big ? bn : sn);
+    j.total = (int)total;
+    if (big) hipLaunchKernelGGL((k_tile<JOB, 256, 256, 2, 4>), dim3(j.total), dim3(512), 0, stream, j);
+    else hipLaunchKernelGGL((k_tile<JOB, 128, 128, 2, 2>), dim3(j.total), dim3(256), 0, stream, j);
+    return hipGetLastError();
+}
+
+struct Rows {
+    const uint16_t* p;
+    int64_t ld;
+};
+
+bool takes_whole_loads(const void* p, int64_t ld) { return (ld & 7) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Rows that the tile loop's loads take as they are, or a copy of them in `room`.
+Rows whole_steps(const void* src, int64_t ld, int64_t rows, int width, char*& room, hipStream_t stream)
+{
+    const int up = (int)round_up(width, 64);
+    char* mine = room;
+    room += round_up(rows * up * 2, 256);
+    const uint16_t* p = static_cast<const uint16_t*>(src);
+    if (up == width && takes_whole_loads(src, ld)) return Rows{p, ld};
+    const int64_t blocks = rows < 8192 ? rows : 8192;
+    hipLaunchKernelGGL(k_pack_rows, dim3((unsigned)blocks), dim3(kBlock), 0, stream, p, ld, rows, width, up,
+                       reinterpret_cast<uint16_t*>(mine));
+    return Rows{reinterpret_cast<uint16_t*>(mine), up};
+}
+
+int64_t packed_bytes(int64_t tokens, int d_in, int d_ff)
+{
+    const int64_t up = round_up(d_in, 64) * 2;
+    return round_up(tokens * up, 256) + 2 * round_up(d_ff * up, 256);
+}
+
+constexpr int kFewTokens = 64;
+
+template <int NT, bool WHOLE>
+hipError_t launch_few(const GatedCall& c, hipStream_t stream)
+{
+    hipLaunchKernelGGL((k_gated_few<NT, WHOLE>), dim3((c.d_ff + 15) / 16), dim3(kBlock), 0, stream,
+                       static_cast<const uint16_t*>(c.x), c.ldx, static_cast<const uint16_t*>(c.wg),
+                       static_cast<const uint16_t*>(c.wu), c.ldw, (int)c.tokens, c.d_in, c.d_ff, Activation{c.gelu},
+                       static_cast<uint16_t*>(c.h), c.ldh);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// packed x, Wg, Wu | map | da, du by token | by feature | x turned | weights turned
+int64_t gated_workspace_bytes(int64_t tokens, int d_in, int d_ff, int k_parts)
+{
+    int64_t bytes = packed_bytes(tokens, d_in, d_ff);
+    if (k_parts > 0) {
+        const int64_t places = round_up(tokens + 31 * (int64_t)k_parts, 32), fp = round_up(d_ff, 64);
+        bytes += round_up(places * 4, 256) + round_up(places * fp * 4, 256) + round_up(2 * d_ff * places * 4, 256) +
+                 round_up(d_in * places * 4, 256) + round_up(d_in * fp * 4, 256);
+    }
+    return bytes > 256 ? bytes : 256;
+}
+
+hipError_t launch_gated_forward(const GatedCall& c, hipStream_t stream)
+{
+    if (c.tokens <= kFewTokens) {
+        const bool whole = (c.d_in & 63) == 0 && takes_whole_loads(c.x, c.ldx) && takes_whole_loads(c.wg, c.ldw) &&
+                           takes_whole_loads(c.wu, c.ldw);
+        if (c.tokens <= 16) return whole ? launch_few<1, true>(c, stream) : launch_few<1, false>(c, stream);
+        if (c.tokens <= 32) return whole ? launch_few<2, true>(c, stream) : launch_few<2, false>(c, stream);
+        return whole ? launch_few<4, true>(c, stream) : launch_few<4, false>(c, stream);
+    }
+    const Activation act{c.gelu};
+    char* room = c.workspace;
+    const Rows x = whole_steps(c.x, c.ldx, c.tokens, c.d_in, room, stream);
+    const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, stream);
+    const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, stream);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    GateJob<false> j{};
+    j.x = x.p, j.ldx = x.ld, j.wg = wg.p, j.ldg = wg.ld, j.wu = wu.p, j.ldu = wu.ld;
+    j.rows = (int)c.tokens, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act;
+    j.h = static_cast<uint16_t*>(c.h), j.ldh = c.ldh;
+    return launch_product(j, 1, c.tokens, round_up(c.d_ff, 16) * 2, stream);
+}
+
+hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
+{
+    const Activation act{c.gelu};
+    GatedParts parts{};
+    parts.k = c.k_parts;
+    for (int p = 0; p < c.k_parts; ++p) {
+        parts.token[p + 1] = (int)c.part_end[p];
+        parts.place[p + 1] = parts.place[p] + (int)round_up(parts.token[p + 1] - parts.token[p], 32);
+    }
+    const int places = parts.place[c.k_parts];
+    const int64_t fp = round_up(c.d_ff, 64), pitch = (int64_t)places * 4;
+    char* room = c.workspace;
+    auto take = [&](int64_t bytes) {
+        char* p = room;
+        room += round_up(bytes, 256);
+        return p;
+    };
+    char *by_feature = nullptr, *x_turned = nullptr;
+    hipError_t e = hipSuccess;
+    if (places > 0) {
+        const Rows x = whole_steps(c.x, c.ldx, c.tokens, c.d_in, room, stream);
+        const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, stream);
+        const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, stream);
+        int* map = reinterpret_cast<int*>(take((int64_t)places * 4));
+        char* by_token = take(places * fp * 4);
+        by_feature = take(2 * c.d_ff * pitch);
+        x_turned = take(c.d_in * pitch);
+        char* w_turned = take(c.d_in * fp * 4);
+        hipLaunchKernelGGL(k_gated_map, dim3((places + kBlock - 1) / kBlock), dim3(kBlock), 0, stream, parts, places, map);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        GateJob<true> j{};
+        j.x = x.p, j.ldx = x.ld, j.wg = wg.p, j.ldg = wg.ld, j.wu = wu.p, j.ldu = wu.ld;
+        j.rows = places, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act, j.map = map;
+        j.dh = static_cast<const uint16_t*>(c.dh), j.lddh = c.lddh;
+        j.by_token = by_token, j.fp = (int)fp, j.by_feature = by_feature, j.pitch = pitch;
+        e = launch_product(j, 1, places, fp * 2, stream);
+        if (e != hipSuccess) return e;
+        const unsigned across = (c.d_in + 63) / 64;
+        if (c.dx) {
+            const unsigned down = (unsigned)(fp / 64);
+            hipLaunchKernelGGL((k_turn<false>), dim3(down, across), dim3(kBlock), 0, stream,
+                               static_cast<const uint16_t*>(c.wg), c.ldw, c.d_ff, c.d_in, (int)fp, (const int*)nullptr,
+                               w_turned, fp * 4);
+            hipLaunchKernelGGL((k_turn<false>), dim3(down, across), dim3(kBlock), 0, stream,
+                               static_cast<const uint16_t*>(c.wu), c.ldw, c.d_ff, c.d_in, (int)fp, (const int*)nullptr,
+                               w_turned + fp * 2, fp * 4);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            InputJob d{by_token, w_turned, fp * 4, places, c.d_in, (int)(fp / 32), map, static_cast<uint16_t*>(c.dx), c.lddx};
+            e = launch_product(d, 1, places, c.d_in, stream);
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL((k_turn<true>), dim3((places + 63) / 64, across), dim3(kBlock), 0, stream,
+                           static_cast<const uint16_t*>(c.x), c.ldx, places, c.d_in, places, map, x_turned, pitch);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    WeightJob w{};
+    w.a = by_feature, w.b = x_turned, w.pitch = pitch, w.d_ff = c.d_ff, w.d_in = c.d_in;
+    w.gate = c.g_gate, w.up = c.g_up, w.ldg = c.ldg, w.parts = parts;
+    return launch_product(w, c.k_parts, 2 * (int64_t)c.d_ff, c.d_in, stream);
+}
+
+}  // namespace agc

@@ -22,6 +22,34 @@ agc_status launched(hipError_t e, const char* what)
 
 bool misaligned(const void* p, uintptr_t unit) { return (reinterpret_cast<uintptr_t>(p) & (unit - 1)) != 0; }
 
+constexpr int64_t kMostTokens = (int64_t)1 << 26;
+constexpr int kMostWidth = 65536;
+
+// Data partitions as the ends of consecutive runs of tokens, empty ones among them.
+agc_status partitions(const char* name, const int64_t* end, int k, int64_t n_tokens)
+{
+    if (!end) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (k < 1 || k > agc::kMostParts) return refuse(AGC_ESHAPE, std::string(name) + ": k_parts must be 1..256");
+    int64_t last = 0;
+    for (int p = 0; p < k; ++p) {
+        if (end[p] < last) return refuse(AGC_ESHAPE, std::string(name) + ": the partitions' ends must not descend");
+        last = end[p];
+    }
+    return last == n_tokens ? AGC_OK : refuse(AGC_ESHAPE, std::string(name) + ": the last partition must end at n_tokens");
+}
+
+agc_status gated_arguments(const char* name, const agc::GatedCall& c, int act)
+{
+    if ((!c.x && c.tokens > 0) || !c.wg || !c.wu || !c.workspace) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (act != AGC_ACT_SILU && act != AGC_ACT_GELU) return refuse(AGC_EINVAL, std::string(name) + ": unknown activation");
+    if (c.tokens < 0 || c.tokens > kMostTokens || c.d_in < 1 || c.d_in > kMostWidth || c.d_ff < 1 || c.d_ff > kMostWidth)
+        return refuse(AGC_ESHAPE, std::string(name) + ": n_tokens must be 0..2^26, d_in and d_ff 1..65536");
+    if (c.ldx < c.d_in || c.ldw < c.d_in) return refuse(AGC_ESHAPE, std::string(name) + ": a row stride is smaller than the row");
+    if (misaligned(c.x, 2) || misaligned(c.wg, 2) || misaligned(c.wu, 2) || misaligned(c.workspace, 256))
+        return refuse(AGC_EALIGN, std::string(name) + ": operands need 2-byte alignment, the workspace 256 bytes");
+    return AGC_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -60,6 +88,57 @@ agc_status agc_muon_update(float* beta_dev, float* m1_dev, const float* ghat_dev
     c.rate = lr * scale;
     c.workspace = static_cast<char*>(workspace_dev);
     return launched(agc::launch_muon_update(c, reinterpret_cast<hipStream_t>(hip_stream)), "agc_muon_update");
+}
+
+int64_t agc_gated_workspace_bytes(int64_t n_tokens, int d_in, int d_ff, int k_parts)
+{
+    if (n_tokens < 0 || n_tokens > kMostTokens || d_in < 1 || d_in > kMostWidth || d_ff < 1 || d_ff > kMostWidth || k_parts < 0 ||
+        k_parts > agc::kMostParts)
+        return 0;
+    return agc::gated_workspace_bytes(n_tokens, d_in, d_ff, k_parts);
+}
+
+agc_status agc_gated_forward(const void* x_dev, int64_t ldx, const void* w_gate_dev, const void* w_up_dev, int64_t ldw,
+                             int64_t n_tokens, int d_in, int d_ff, int act, void* h_dev, int64_t ldh, void* workspace_dev,
+                             void* hip_stream)
+{
+    agc::GatedCall c{};
+    c.x = x_dev, c.wg = w_gate_dev, c.wu = w_up_dev, c.ldx = ldx, c.ldw = ldw;
+    c.tokens = n_tokens, c.d_in = d_in, c.d_ff = d_ff, c.gelu = act == AGC_ACT_GELU;
+    c.workspace = static_cast<char*>(workspace_dev);
+    const agc_status st = gated_arguments("agc_gated_forward", c, act);
+    if (st != AGC_OK) return st;
+    if (!h_dev && n_tokens > 0) return refuse(AGC_EINVAL, "agc_gated_forward: null pointer");
+    if (ldh < d_ff) return refuse(AGC_ESHAPE, "agc_gated_forward: ldh is smaller than d_ff");
+    if (misaligned(h_dev, 2)) return refuse(AGC_EALIGN, "agc_gated_forward: h needs 2-byte alignment");
+    if (n_tokens == 0) return AGC_OK;
+    c.h = h_dev, c.ldh = ldh;
+    return launched(agc::launch_gated_forward(c, reinterpret_cast<hipStream_t>(hip_stream)), "agc_gated_forward");
+}
+
+agc_status agc_gated_partial_gradients(const void* x_dev, int64_t ldx, const void* w_gate_dev, const void* w_up_dev,
+                                       int64_t ldw, const void* dh_dev, int64_t lddh, int64_t n_tokens,
+                                       const int64_t* part_end_host, int k_parts, int d_in, int d_ff, int act, void* dx_dev,
+                                       int64_t lddx, float* G_gate_dev, float* G_up_dev, int64_t ldg, void* workspace_dev,
+                                       void* hip_stream)
+{
+    const char* const name = "agc_gated_partial_gradients";
+    agc::GatedCall c{};
+    c.x = x_dev, c.wg = w_gate_dev, c.wu = w_up_dev, c.ldx = ldx, c.ldw = ldw;
+    c.tokens = n_tokens, c.d_in = d_in, c.d_ff = d_ff, c.gelu = act == AGC_ACT_GELU;
+    c.workspace = static_cast<char*>(workspace_dev);
+    agc_status st = gated_arguments(name, c, act);
+    if (st != AGC_OK) return st;
+    st = partitions(name, part_end_host, k_parts, n_tokens);
+    if (st != AGC_OK) return st;
+    if ((!dh_dev && n_tokens > 0) || !G_gate_dev || !G_up_dev) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (lddh < d_ff || (dx_dev && lddx < d_in)) return refuse(AGC_ESHAPE, std::string(name) + ": a row stride is smaller than the row");
+    if (ldg < (int64_t)d_in * d_ff) return refuse(AGC_ESHAPE, std::string(name) + ": ldg is smaller than a weight matrix");
+    if (misaligned(dh_dev, 2) || misaligned(dx_dev, 2) || misaligned(G_gate_dev, 4) || misaligned(G_up_dev, 4))
+        return refuse(AGC_EALIGN, std::string(name) + ": a pointer is not aligned to its elements");
+    c.dh = dh_dev, c.lddh = lddh, c.part_end = part_end_host, c.k_parts = k_parts, c.dx = dx_dev, c.lddx = lddx;
+    c.g_gate = G_gate_dev, c.g_up = G_up_dev, c.ldg = ldg;
+    return launched(agc::launch_gated_gradients(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
 }
 
 }  // extern "C"

@@ -29,4 +29,28 @@ struct MuonCall {
 int64_t muon_workspace_bytes(int rows, int cols, int n_mats);
 hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream);
 
+// ------------------------------------------------------------------ gated block
+struct GatedCall {
+    const void *x, *wg, *wu;
+    int64_t ldx, ldw;
+    int64_t tokens;
+    int d_in, d_ff, gelu;
+    // forward
+    void* h;
+    int64_t ldh;
+    // gradients
+    const void* dh;
+    int64_t lddh;
+    const int64_t* part_end;   // host
+    int k_parts;
+    void* dx;                  // may be null
+    int64_t lddx;
+    float *g_gate, *g_up;
+    int64_t ldg;
+    char* workspace;
+};
+int64_t gated_workspace_bytes(int64_t tokens, int d_in, int d_ff, int k_parts);   // k_parts 0: forward alone
+hipError_t launch_gated_forward(const GatedCall& c, hipStream_t stream);
+hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream);
+
 }  // namespace agc
