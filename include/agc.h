@@ -285,6 +285,35 @@ agc_status agc_adam_update(float *beta_dev, float *m1_dev, float *m2_dev, const 
  * Token models: two producers of rows of G and a consumer of g_hat
  * ------------------------------------------------------------------------------------ */
 typedef enum {
+    AGC_TYPE_F32 = 0,
+    AGC_TYPE_BF16 = 1 /* upper halves of binary32 */
+} agc_type;
+
+/* Embedding with scaling:  out[t,:] = scale * E[id_t,:], one binary32 product a value, rounded once to out's type.  An id
+ * outside [0, vocab) is an empty place (padding): its row of out is zeros.
+ *   table_dev  device, vocab x dim of table_type, row-major (its section of the parameter vector, for instance)
+ *   tokens_dev device, n_tokens ids of token_bytes = 4 or 8 bytes (signed)
+ *   out_dev    device, n_tokens x dim of out_type, row stride ldo elements; overwritten
+ * 0 <= n_tokens <= 2^26, 1 <= dim <= 65536, 1 <= vocab < 2^31; any alignment of the rows. */
+agc_status agc_embed_forward(const void *table_dev, int table_type, int64_t vocab, int dim, const void *tokens_dev,
+                             int token_bytes, int64_t n_tokens, float scale, void *out_dev, int out_type, int64_t ldo,
+                             void *hip_stream);
+/* Its partial gradients (Sec. II-A): for every data partition p (a run of tokens) and every id v
+ *   G[p, v * dim + c] = scale * sum of dout[t, c] over the tokens t of p with id_t = v,
+ * binary32, in a fixed order (the result is reproducible run to run); rows of ids that do not occur are zeros, empty
+ * places count for nothing, whatever their dout holds.
+ *   dout_dev   device, n_tokens x dim of dout_type, row stride lddout
+ *   part_end_host  host, k_parts ends of the partitions in tokens, not descending, the last n_tokens
+ *   G_dev      device, where row 0 of G holds the gradient of the table; row p lies p * ldg floats on; overwritten
+ *   workspace_dev  device, agc_embed_workspace_bytes(...) bytes, 256-byte aligned; scratch
+ * 1 <= k_parts <= 256, k_parts * vocab < 2^31; ldg >= vocab * dim. */
+int64_t agc_embed_workspace_bytes(int64_t n_tokens, int64_t vocab, int dim, int k_parts);
+agc_status agc_embed_partial_gradients(const void *dout_dev, int dout_type, int64_t lddout, const void *tokens_dev,
+                                       int token_bytes, int64_t n_tokens, const int64_t *part_end_host, int k_parts,
+                                       int64_t vocab, int dim, float scale, float *G_dev, int64_t ldg, void *workspace_dev,
+                                       void *hip_stream);
+
+typedef enum {
     AGC_ACT_SILU = 0, /* a / (1 + exp(-a)) */
     AGC_ACT_GELU = 1  /* a * Phi(a), by erf */
 } agc_activation;

@@ -17,6 +17,7 @@ AGC_OK = 0
 AGC_EINVAL, AGC_ESHAPE, AGC_EBITS, AGC_EALIGN, AGC_ENOMEM, AGC_EHIP, AGC_ESTATE = -1, -2, -3, -4, -5, -6, -7
 AGC_SCALE_L2, AGC_SCALE_MAXABS = 0, 1
 AGC_ACT_SILU, AGC_ACT_GELU = 0, 1
+AGC_TYPE_F32, AGC_TYPE_BF16 = 0, 1
 AGC_MAX_WORKERS, AGC_MAX_BITS, AGC_NUM_KERNELS, AGC_MAX_LAYERS = 256, 16, 4, 256
 KERNEL_NAMES = ("scale_pass", "scale_finalize", "quantize", "decode")
 
@@ -24,6 +25,7 @@ EXPORTS = [
     "agc_create", "agc_destroy", "agc_set_code", "agc_code_path", "agc_code_bytes", "agc_last_error",
     "agc_encode_quantize", "agc_decode", "agc_step", "agc_profile_enable", "agc_profile_read",
     "agc_scales_per_worker", "agc_set_layers", "agc_decode2", "agc_decode_noalloc", "agc_adam_update", "agc_second_moment_decoder",
+    "agc_embed_forward", "agc_embed_workspace_bytes", "agc_embed_partial_gradients",
     "agc_gated_workspace_bytes", "agc_gated_forward", "agc_gated_partial_gradients",
     "agc_muon_workspace_bytes", "agc_muon_update",
     "agc_calibration_copy", "agc_debug_force_long", "agc_debug_sketch", "agc_debug_sketch_last", "agc_debug_sketch_max", "agc_debug_stream_rows", "agc_ls_workspace_floats", "agc_ls_partial_gradients", "agc_gd_update",
@@ -106,6 +108,14 @@ def load():
     L.agc_ls_partial_gradients.restype = C.c_int
     L.agc_gd_update.argtypes = [_vp, _vp, C.c_float, C.c_int64, _vp]
     L.agc_gd_update.restype = C.c_int
+    L.agc_embed_forward.argtypes = [_vp, C.c_int, C.c_int64, C.c_int, _vp, C.c_int, C.c_int64, C.c_float, _vp, C.c_int,
+                                    C.c_int64, _vp]
+    L.agc_embed_forward.restype = C.c_int
+    L.agc_embed_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int, C.c_int]
+    L.agc_embed_workspace_bytes.restype = C.c_int64
+    L.agc_embed_partial_gradients.argtypes = [_vp, C.c_int, C.c_int64, _vp, C.c_int, C.c_int64, _vp, C.c_int, C.c_int64,
+                                              C.c_int, C.c_float, _vp, C.c_int64, _vp, _vp]
+    L.agc_embed_partial_gradients.restype = C.c_int
     L.agc_gated_workspace_bytes.argtypes = [C.c_int64, C.c_int, C.c_int, C.c_int]
     L.agc_gated_workspace_bytes.restype = C.c_int64
     L.agc_gated_forward.argtypes = [_vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_int, _vp,
@@ -501,6 +511,62 @@ def _rows_of(t, rows, cols, dtype, what):
         raise AgcError(AGC_ESHAPE, f"{what} must be a ({rows}, {cols}) row-major view of {dtype}, got "
                                    f"{tuple(t.shape)} of {t.dtype}")
     return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _type_of(t, what):
+    if t.dtype == _float32():
+        return AGC_TYPE_F32
+    if t.dtype == _bfloat16():
+        return AGC_TYPE_BF16
+    raise AgcError(AGC_EINVAL, f"{what} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _ids(tokens):
+    """Bytes of an id; AGC_ESHAPE unless tokens is a contiguous vector of int32 or int64."""
+    width = tokens.element_size()
+    if tokens.dim() != 1 or not tokens.is_contiguous() or tokens.is_floating_point() or width not in (4, 8):
+        raise AgcError(AGC_ESHAPE, "tokens must be a contiguous vector of int32 or int64")
+    return width
+
+
+def agc_embed_forward(table, tokens, scale, out, stream=None, check=True):
+    """out[t] = scale * table[tokens[t]]; zeros where the id is outside the table.  table (vocab, dim) contiguous, out
+    (tokens, dim) row-major, each float32 or bfloat16."""
+    L = load()
+    kind, width, n = _type_of(table, "table"), _ids(tokens), tokens.numel()
+    if table.dim() != 2 or not table.is_contiguous():
+        raise AgcError(AGC_ESHAPE, "table must be (vocab, dim), contiguous")
+    vocab, dim = table.shape
+    ldo = _rows_of(out, n, dim, out.dtype, "out")
+    st = L.agc_embed_forward(table.data_ptr(), kind, vocab, dim, tokens.data_ptr(), width, n, scale, out.data_ptr(),
+                             _type_of(out, "out"), ldo, _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
+
+
+def agc_embed_workspace_bytes(n_tokens, vocab, dim, k_parts):
+    return int(load().agc_embed_workspace_bytes(int(n_tokens), int(vocab), int(dim), int(k_parts)))
+
+
+def agc_embed_partial_gradients(dout, tokens, part_end, vocab, scale, G, workspace, stream=None, check=True):
+    """For each partition of the tokens the gradient of the table: G is a (k_parts, vocab * dim) float32 view of rows of
+    G; dout (tokens, dim) is float32 or bfloat16."""
+    L = load()
+    kind, width, n, k = _type_of(dout, "dout"), _ids(tokens), tokens.numel(), len(part_end)
+    if dout.dim() != 2:
+        raise AgcError(AGC_ESHAPE, "dout must be (tokens, dim)")
+    dim = dout.shape[1]
+    ldd = _rows_of(dout, n, dim, dout.dtype, "dout")
+    ldg = _rows_of(G, k, vocab * dim, _float32(), "G")
+    if workspace.numel() * workspace.element_size() < L.agc_embed_workspace_bytes(n, vocab, dim, k):
+        raise AgcError(AGC_ESHAPE, "agc_embed_partial_gradients: the workspace is too small")
+    st = L.agc_embed_partial_gradients(dout.data_ptr(), kind, ldd, tokens.data_ptr(), width, n,
+                                       struct.pack(f"{k}q", *[int(e) for e in part_end]), k, vocab, dim, scale,
+                                       G.data_ptr(), ldg, workspace.data_ptr(), _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
 
 
 def agc_gated_workspace_bytes(n_tokens, d_in, d_ff, k_parts=0):

@@ -1,0 +1,462 @@
+// Embedding of tokens and its partial gradients (rows of G).
+//   out[t] = scale * E[id_t]             a zero row where id_t is outside [0, vocab)
+//   G[p, v] = scale * sum of dout[t] over the tokens t of partition p with id_t = v, ascending in t
+//
+// The gradient writes all k * vocab rows of the table, most of them zeros, so it is bound by the write of G.  Tokens are
+// put in order of (partition, id) by a radix sort that keeps equal keys in place; a row's tokens are then one run of the
+// order, found by searching it, and are summed by whoever writes the row: no atomics on values, no clearing before.
+// Rows with long runs (few ids, or the commonest one) would leave one wave with all the work: runs are first summed in
+// pieces of 64 places of the order and those in pieces of 32, so that a row of n tokens takes about n / 2048 + 190 steps.
+#include "agc_operators.h"
+
+namespace agc {
+
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kDigitBits = 11, kDigits = 1 << kDigitBits;
+constexpr int kSortTile = 2048;    // keys of one workgroup in a pass of the sort
+constexpr int kPiece = 64;         // places of a first-level piece
+constexpr int kGroup = 32;         // pieces of a second-level piece
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct EmbedParts {
+    int end[kMostParts];
+    int k;
+};
+
+__device__ __forceinline__ float from_bf16(uint32_t bits) { return __uint_as_float(bits << 16); }
+__device__ __forceinline__ uint32_t to_bf16(float v) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v); }
+
+// Four values from element c on of a row of T (float or bfloat16 bits); WHOLE: one aligned load, else element by
+// element below `width`.
+template <class T, bool WHOLE>
+__device__ __forceinline__ f32x4 load4(const T* row, int c, int width)
+{
+    if constexpr (WHOLE && sizeof(T) == 4) return *reinterpret_cast<const f32x4*>(row + c);
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (WHOLE && sizeof(T) == 2) {
+        const u32x2 u = *reinterpret_cast<const u32x2*>(row + c);
+        v = f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
+                  __uint_as_float(u.y & 0xFFFF0000u)};
+    }
+    if constexpr (!WHOLE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < width) {
+                if constexpr (sizeof(T) == 4) v[e] = row[c + e];
+                else v[e] = from_bf16(row[c + e]);
+            }
+    }
+    return v;
+}
+
+template <class T, bool WHOLE>
+__device__ __forceinline__ void store4(T* row, int c, int width, const f32x4& v)
+{
+    if constexpr (WHOLE && sizeof(T) == 4) {
+        *reinterpret_cast<f32x4*>(row + c) = v;
+    } else if constexpr (WHOLE) {
+        *reinterpret_cast<u32x2*>(row + c) = u32x2{to_bf16(v.x) | (to_bf16(v.y) << 16), to_bf16(v.z) | (to_bf16(v.w) << 16)};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < width) {
+                if constexpr (sizeof(T) == 4) row[c + e] = v[e];
+                else row[c + e] = (T)to_bf16(v[e]);
+            }
+    }
+}
+
+// ------------------------------------------------------------------ forward
+// `lanes` (a power of two up to 64) lanes walk over one row.
+template <class TABLE, class OUT, class ID, bool WHOLE>
+__global__ __launch_bounds__(kBlock) void k_embed(const TABLE* table, int64_t vocab, int dim, const ID* tokens, int64_t n,
+                                                  float scale, OUT* out, int64_t ldo, int lanes)
+{
+    const int per = kBlock / lanes, mine = threadIdx.x / lanes, lane = threadIdx.x & (lanes - 1);
+    for (int64_t t = (int64_t)blockIdx.x * per + mine; t < n; t += (int64_t)gridDim.x * per) {
+        const int64_t id = (int64_t)tokens[t];
+        const bool held = id >= 0 && id < vocab;
+        const TABLE* row = table + (held ? id : 0) * dim;
+        for (int c = lane * 4; c < dim; c += lanes * 4) {
+            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (held) v = load4<TABLE, WHOLE>(row, c, dim) * scale;
+            store4<OUT, WHOLE>(out + t * ldo, c, dim, v);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ order of the tokens
+// key = partition * vocab + id, or `none` (above all keys) at an empty place
+template <class ID>
+__global__ __launch_bounds__(kBlock) void k_embed_keys(const ID* tokens, int n, const EmbedParts parts, int64_t vocab,
+                                                       uint32_t none, uint32_t* key, uint32_t* place)
+{
+    const int t = blockIdx.x * kBlock + threadIdx.x;
+    if (t >= n) return;
+    int lo = 0, hi = parts.k - 1;   // the first partition that ends after t
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (parts.end[mid] > t) hi = mid;
+        else lo = mid + 1;
+    }
+    const int64_t id = (int64_t)tokens[t];
+    key[t] = id >= 0 && id < vocab ? (uint32_t)(lo * vocab + id) : none;
+    place[t] = (uint32_t)t;
+}
+
+// Lanes of the wave whose digit equals mine, among those that hold a key.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool valid)
+{
+    uint64_t same = __ballot(valid);
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+        const uint64_t ones = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? ones : ~ones;
+    }
+    return same;
+}
+
+// counts[tile][digit] of the keys' digits
+__global__ __launch_bounds__(kBlock) void k_sort_count(const uint32_t* key, int n, int shift, uint32_t* counts)
+{
+    __shared__ uint32_t bin[kDigits];
+    for (int i = threadIdx.x; i < kDigits; i += kBlock) bin[i] = 0;
+    __syncthreads();
+    const int from = blockIdx.x * kSortTile, to = min(n, from + kSortTile);
+    for (int i = from + threadIdx.x; i < to; i += kBlock) atomicAdd(&bin[(key[i] >> shift) & (kDigits - 1)], 1u);
+    __syncthreads();
+    for (int i = threadIdx.x; i < kDigits; i += kBlock) counts[(int64_t)blockIdx.x * kDigits + i] = bin[i];
+}
+
+// counts[tile][digit] -> where the tile's first key of that digit goes, less what precedes the digit; totals[digit]
+__global__ __launch_bounds__(64) void k_sort_tiles(uint32_t* counts, int tiles, uint32_t* totals)
+{
+    const int digit = blockIdx.x * 64 + threadIdx.x;
+    uint32_t sum = 0;
+    for (int t = 0; t < tiles; t += 8) {
+        uint32_t here[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) here[e] = t + e < tiles ? counts[(int64_t)(t + e) * kDigits + digit] : 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (t + e < tiles) counts[(int64_t)(t + e) * kDigits + digit] = sum;
+            sum += here[e];
+        }
+    }
+    totals[digit] = sum;
+}
+
+// Moves a tile's keys and places to where their digit puts them, equal digits in the order in which they lie.  Each
+// wave takes a quarter of the tile, 64 keys at a time.
+__global__ __launch_bounds__(kBlock) void k_sort_move(const uint32_t* key, const uint32_t* place, int n, int shift,
+                                                      const uint32_t* counts, const uint32_t* totals, uint32_t* key_out,
+                                                      uint32_t* place_out)
+{
+    __shared__ uint32_t next[4][kDigits];
+    __shared__ uint32_t carry[kBlock];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int i = tid; i < 4 * kDigits; i += kBlock) (&next[0][0])[i] = 0;
+    __syncthreads();
+    const int from = blockIdx.x * kSortTile + wave * (kSortTile / 4);
+    for (int r = 0; r < kSortTile / 4; r += 64)
+        if (from + r + lane < n) atomicAdd(&next[wave][(key[from + r + lane] >> shift) & (kDigits - 1)], 1u);
+    // what precedes a digit: eight digits a thread, then the threads before
+    constexpr int kPer = kDigits / kBlock;
+    uint32_t before[kPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        before[i] = sum;
+        sum += totals[tid * kPer + i];
+    }
+    carry[tid] = sum;
+    __syncthreads();
+    for (int d = 1; d < kBlock; d *= 2) {
+        const uint32_t add = tid >= d ? carry[tid - d] : 0;
+        __syncthreads();
+        carry[tid] += add;
+        __syncthreads();
+    }
+    const uint32_t base = carry[tid] - sum;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int digit = tid * kPer + i;
+        uint32_t at = base + before[i] + counts[(int64_t)blockIdx.x * kDigits + digit];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t here = next[w][digit];
+            next[w][digit] = at;
+            at += here;
+        }
+    }
+    __syncthreads();
+    for (int r = 0; r < kSortTile / 4; r += 64) {
+        const int i = from + r + lane;
+        const bool valid = i < n;
+        const uint32_t k = valid ? key[i] : 0, digit = (k >> shift) & (kDigits - 1);
+        const uint64_t same = same_digit(digit, valid);
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        if (valid) {
+            const uint32_t at = next[wave][digit] + rank;
+            key_out[at] = k;
+            place_out[at] = place[i];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (valid && rank == 0) next[wave][digit] += __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ------------------------------------------------------------------ sums
+struct SumArgs {
+    const uint32_t *key, *place;
+    int n, dim;
+    uint32_t none;
+    int64_t ldd;         // of dout
+    int64_t pitch;       // of the pieces' sums: dim, rounded up to 4
+    float* pieces;       // sums of kPiece places of one key, at place / kPiece
+    float* groups;       // sums of kGroup pieces of one key
+};
+
+// The sum over places [from, to) of the order, four columns from c on.
+template <class T, bool WHOLE>
+__device__ __forceinline__ f32x4 sum_tokens(const SumArgs& a, const T* dout, int from, int to, int c, f32x4 acc)
+{
+    for (int i = from; i < to; i += 4) {
+        f32x4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (i + e < to) v[e] = load4<T, WHOLE>(dout + (int64_t)a.place[i + e] * a.ldd, c, a.dim);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc += v[e];
+    }
+    return acc;
+}
+
+__device__ __forceinline__ f32x4 sum_rows(const float* rows, int64_t pitch, int from, int to, int c, f32x4 acc)
+{
+    for (int i = from; i < to; i += 4) {
+        f32x4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (i + e < to) v[e] = *reinterpret_cast<const f32x4*>(rows + (int64_t)(i + e) * pitch + c);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc += v[e];
+    }
+    return acc;
+}
+
+// Whole pieces of one key.  A wave takes a piece and 256 columns.
+template <class T, bool WHOLE>
+__global__ __launch_bounds__(64) void k_embed_pieces(const SumArgs a, const T* dout)
+{
+    const int first = blockIdx.x * kPiece;   // the grid holds whole pieces alone
+    const uint32_t key = a.key[first];
+    if (key != a.key[first + kPiece - 1] || key == a.none) return;
+    const int c = (blockIdx.y * 64 + threadIdx.x) * 4;
+    if (c >= a.dim) return;
+    const f32x4 sum = sum_tokens<T, WHOLE>(a, dout, first, first + kPiece, c, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+    *reinterpret_cast<f32x4*>(a.pieces + (int64_t)blockIdx.x * a.pitch + c) = sum;
+}
+
+__global__ __launch_bounds__(64) void k_embed_groups(const SumArgs a)
+{
+    const int first = blockIdx.x * kPiece * kGroup;
+    const uint32_t key = a.key[first];
+    if (key != a.key[first + kPiece * kGroup - 1] || key == a.none) return;
+    const int c = (blockIdx.y * 64 + threadIdx.x) * 4;
+    if (c >= a.dim) return;
+    const f32x4 sum = sum_rows(a.pieces, a.pitch, blockIdx.x * kGroup, (blockIdx.x + 1) * kGroup, c, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+    *reinterpret_cast<f32x4*>(a.groups + (int64_t)blockIdx.x * a.pitch + c) = sum;
+}
+
+__device__ __forceinline__ int lower_bound(const uint32_t* key, int n, uint32_t what)
+{
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (key[mid] < what) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// All rows of G: a wave takes `rows` (up to 64) consecutive ones, each lane searches the run of one of them.
+template <class T, bool WHOLE>
+__global__ __launch_bounds__(kBlock) void k_embed_rows(const SumArgs a, const T* dout, int64_t vocab, int64_t total, float scale,
+                                                       float* G, int64_t ldg, int rows)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t first = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * rows;
+    if (first >= total) return;
+    const int count = total - first < rows ? (int)(total - first) : rows;
+    // lane i < count: where row first + i begins; lane `count`: where the last one ends.  With 64 rows that is lane 0's.
+    int begin = lane <= count ? lower_bound(a.key, a.n, (uint32_t)(first + lane)) : 0;
+    int last = count == 64 ? lower_bound(a.key, a.n, (uint32_t)(first + 64)) : 0;
+    int64_t p = first / vocab, v = first - p * vocab;
+    for (int r = 0; r < count; ++r) {
+        const int from = __builtin_amdgcn_readlane(begin, r);
+        const int to = r == 63 ? __builtin_amdgcn_readfirstlane(last) : __builtin_amdgcn_readlane(begin, r + 1);
+        float* row = G + p * ldg + v * a.dim;
+        for (int c = lane * 4; c < a.dim; c += 256) {
+            f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (from < to) {
+                const int p0 = (from + kPiece - 1) / kPiece, p1 = to / kPiece;   // whole pieces
+                if (p0 < p1) {
+                    acc = sum_tokens<T, WHOLE>(a, dout, from, p0 * kPiece, c, acc);
+                    const int g0 = (p0 + kGroup - 1) / kGroup, g1 = p1 / kGroup;
+                    if (g0 < g1) {
+                        acc = sum_rows(a.pieces, a.pitch, p0, g0 * kGroup, c, acc);
+                        acc = sum_rows(a.groups, a.pitch, g0, g1, c, acc);
+                        acc = sum_rows(a.pieces, a.pitch, g1 * kGroup, p1, c, acc);
+                    } else {
+                        acc = sum_rows(a.pieces, a.pitch, p0, p1, c, acc);
+                    }
+                    acc = sum_tokens<T, WHOLE>(a, dout, p1 * kPiece, to, c, acc);
+                } else {
+                    acc = sum_tokens<T, WHOLE>(a, dout, from, to, c, acc);
+                }
+            }
+            if (from < to) acc = acc * scale;
+            store4<float, WHOLE>(row, c, a.dim, acc);
+        }
+        if (++v == vocab) v = 0, ++p;
+    }
+}
+
+template <class TABLE, class OUT, class ID>
+hipError_t forward_as(const EmbedCall& c, hipStream_t stream)
+{
+    const TABLE* table = static_cast<const TABLE*>(c.table);
+    OUT* out = static_cast<OUT*>(c.out);
+    const ID* tokens = static_cast<const ID*>(c.tokens);
+    const bool whole = c.dim % 4 == 0 && c.ld % 4 == 0 && reinterpret_cast<uintptr_t>(table) % (4 * sizeof(TABLE)) == 0 &&
+                       reinterpret_cast<uintptr_t>(out) % (4 * sizeof(OUT)) == 0;
+    int lanes = 1;
+    while (lanes < 64 && lanes * 4 < c.dim) lanes *= 2;
+    const int64_t blocks = (c.n + kBlock / lanes - 1) / (kBlock / lanes);
+    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
+    if (whole)
+        hipLaunchKernelGGL((k_embed<TABLE, OUT, ID, true>), grid, dim3(kBlock), 0, stream, table, c.vocab, c.dim, tokens, c.n,
+                           c.scale, out, c.ld, lanes);
+    else
+        hipLaunchKernelGGL((k_embed<TABLE, OUT, ID, false>), grid, dim3(kBlock), 0, stream, table, c.vocab, c.dim, tokens, c.n,
+                           c.scale, out, c.ld, lanes);
+    return hipGetLastError();
+}
+
+template <class TABLE, class OUT>
+hipError_t forward_with(const EmbedCall& c, hipStream_t stream)
+{
+    return c.wide_ids ? forward_as<TABLE, OUT, int64_t>(c, stream) : forward_as<TABLE, OUT, int32_t>(c, stream);
+}
+
+template <class T, bool WHOLE>
+hipError_t sums_as(const EmbedCall& c, const SumArgs& a, hipStream_t stream)
+{
+    const T* dout = static_cast<const T*>(c.dout);
+    const unsigned across = (unsigned)((c.dim + 255) / 256);
+    hipError_t e = hipSuccess;
+    if (a.n >= kPiece) {
+        hipLaunchKernelGGL((k_embed_pieces<T, WHOLE>), dim3(a.n / kPiece, across), dim3(64), 0, stream, a, dout);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (a.n >= kPiece * kGroup) {
+        hipLaunchKernelGGL(k_embed_groups, dim3(a.n / (kPiece * kGroup), across), dim3(64), 0, stream, a);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const int64_t total = c.vocab * c.k_parts;
+    int rows = 64;
+    while (rows > 1 && total / rows < 8192) rows /= 2;
+    const int64_t waves = (total + rows - 1) / rows;
+    hipLaunchKernelGGL((k_embed_rows<T, WHOLE>), dim3((unsigned)((waves + 3) / 4)), dim3(kBlock), 0, stream, a, dout, c.vocab,
+                       total, c.scale, c.G, c.ldg, rows);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t sums_with(const EmbedCall& c, const SumArgs& a, hipStream_t stream)
+{
+    const bool whole = c.dim % 4 == 0 && c.ld % 4 == 0 && c.ldg % 4 == 0 &&
+                       reinterpret_cast<uintptr_t>(c.dout) % (4 * sizeof(T)) == 0 && reinterpret_cast<uintptr_t>(c.G) % 16 == 0;
+    return whole ? sums_as<T, true>(c, a, stream) : sums_as<T, false>(c, a, stream);
+}
+
+}  // namespace
+
+// keys, places, twice | counts of the sort's tiles | totals | sums of pieces | of groups
+int64_t embed_workspace_bytes(int64_t n, int64_t vocab, int dim, int k_parts)
+{
+    (void)vocab, (void)k_parts;
+    const int64_t tiles = (n + kSortTile - 1) / kSortTile, pitch = round_up(dim, 4) * 4;
+    return 4 * round_up(n * 4, 256) + round_up(tiles * kDigits * 4, 256) + kDigits * 4 + round_up(n / kPiece * pitch, 256) +
+           round_up(n / (kPiece * kGroup) * pitch, 256) + 256;
+}
+
+hipError_t launch_embed_forward(const EmbedCall& c, hipStream_t stream)
+{
+    if (c.table_bf16)
+        return c.value_bf16 ? forward_with<uint16_t, uint16_t>(c, stream) : forward_with<uint16_t, float>(c, stream);
+    return c.value_bf16 ? forward_with<float, uint16_t>(c, stream) : forward_with<float, float>(c, stream);
+}
+
+hipError_t launch_embed_gradients(const EmbedCall& c, hipStream_t stream)
+{
+    const int n = (int)c.n, tiles = (n + kSortTile - 1) / kSortTile;
+    char* room = c.workspace;
+    auto take = [&](int64_t bytes) {
+        char* p = room;
+        room += round_up(bytes, 256);
+        return p;
+    };
+    uint32_t *key[2], *place[2];
+    for (int i = 0; i < 2; ++i) {
+        key[i] = reinterpret_cast<uint32_t*>(take((int64_t)n * 4));
+        place[i] = reinterpret_cast<uint32_t*>(take((int64_t)n * 4));
+    }
+    uint32_t* counts = reinterpret_cast<uint32_t*>(take((int64_t)tiles * kDigits * 4));
+    uint32_t* totals = reinterpret_cast<uint32_t*>(take(kDigits * 4));
+    SumArgs a{};
+    a.n = n, a.dim = c.dim, a.ldd = c.ld, a.pitch = round_up(c.dim, 4);
+    a.pieces = reinterpret_cast<float*>(take(n / kPiece * a.pitch * 4));
+    a.groups = reinterpret_cast<float*>(take(n / (kPiece * kGroup) * a.pitch * 4));
+    a.none = (uint32_t)(c.vocab * c.k_parts);
+    int now = 0;
+    if (n > 0) {
+        EmbedParts parts{};
+        parts.k = c.k_parts;
+        for (int p = 0; p < c.k_parts; ++p) parts.end[p] = (int)c.part_end[p];
+        const dim3 grid((n + kBlock - 1) / kBlock);
+        if (c.wide_ids)
+            hipLaunchKernelGGL(k_embed_keys<int64_t>, grid, dim3(kBlock), 0, stream, static_cast<const int64_t*>(c.tokens), n,
+                               parts, c.vocab, a.none, key[0], place[0]);
+        else
+            hipLaunchKernelGGL(k_embed_keys<int32_t>, grid, dim3(kBlock), 0, stream, static_cast<const int32_t*>(c.tokens), n,
+                               parts, c.vocab, a.none, key[0], place[0]);
+        for (int shift = 0; shift < 32 && (a.none >> shift) != 0; shift += kDigitBits) {
+            hipLaunchKernelGGL(k_sort_count, dim3(tiles), dim3(kBlock), 0, stream, key[now], n, shift, counts);
+            hipLaunchKernelGGL(k_sort_tiles, dim3(kDigits / 64), dim3(64), 0, stream, counts, tiles, totals);
+            hipLaunchKernelGGL(k_sort_move, dim3(tiles), dim3(kBlock), 0, stream, key[now], place[now], n, shift, counts, totals,
+                               key[now ^ 1], place[now ^ 1]);
+            now ^= 1;
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    a.key = key[now], a.place = place[now];
+    return c.value_bf16 ? sums_with<uint16_t>(c, a, stream) : sums_with<float>(c, a, stream);
+}
+
+}  // namespace agc

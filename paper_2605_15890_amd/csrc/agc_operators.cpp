@@ -38,6 +38,17 @@ agc_status partitions(const char* name, const int64_t* end, int k, int64_t n_tok
     return last == n_tokens ? AGC_OK : refuse(AGC_ESHAPE, std::string(name) + ": the last partition must end at n_tokens");
 }
 
+agc_status embed_arguments(const char* name, const agc::EmbedCall& c, int token_bytes, int type, int64_t ld)
+{
+    if (!c.tokens && c.n > 0) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if ((token_bytes != 4 && token_bytes != 8) || (type != AGC_TYPE_F32 && type != AGC_TYPE_BF16))
+        return refuse(AGC_EINVAL, std::string(name) + ": tokens have 4 or 8 bytes, values are float or bfloat16");
+    if (c.n < 0 || c.n > kMostTokens || c.vocab < 1 || c.vocab > INT32_MAX || c.dim < 1 || c.dim > kMostWidth || ld < c.dim)
+        return refuse(AGC_ESHAPE, std::string(name) + ": n_tokens must be 0..2^26, vocab 1..2^31-1, dim 1..65536 and at most the row stride");
+    if (misaligned(c.tokens, token_bytes)) return refuse(AGC_EALIGN, std::string(name) + ": tokens are not aligned to their bytes");
+    return AGC_OK;
+}
+
 agc_status gated_arguments(const char* name, const agc::GatedCall& c, int act)
 {
     if ((!c.x && c.tokens > 0) || !c.wg || !c.wu || !c.workspace) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
@@ -88,6 +99,56 @@ agc_status agc_muon_update(float* beta_dev, float* m1_dev, const float* ghat_dev
     c.rate = lr * scale;
     c.workspace = static_cast<char*>(workspace_dev);
     return launched(agc::launch_muon_update(c, reinterpret_cast<hipStream_t>(hip_stream)), "agc_muon_update");
+}
+
+agc_status agc_embed_forward(const void* table_dev, int table_type, int64_t vocab, int dim, const void* tokens_dev,
+                             int token_bytes, int64_t n_tokens, float scale, void* out_dev, int out_type, int64_t ldo,
+                             void* hip_stream)
+{
+    const char* const name = "agc_embed_forward";
+    agc::EmbedCall c{};
+    c.tokens = tokens_dev, c.wide_ids = token_bytes == 8, c.n = n_tokens, c.vocab = vocab, c.dim = dim, c.scale = scale;
+    const agc_status st = embed_arguments(name, c, token_bytes, out_type, ldo);
+    if (st != AGC_OK) return st;
+    if (table_type != AGC_TYPE_F32 && table_type != AGC_TYPE_BF16) return refuse(AGC_EINVAL, std::string(name) + ": unknown type");
+    if (!table_dev || (!out_dev && n_tokens > 0)) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (misaligned(table_dev, table_type == AGC_TYPE_F32 ? 4 : 2) || misaligned(out_dev, out_type == AGC_TYPE_F32 ? 4 : 2))
+        return refuse(AGC_EALIGN, std::string(name) + ": a pointer is not aligned to its elements");
+    if (n_tokens == 0) return AGC_OK;
+    c.table = table_dev, c.table_bf16 = table_type == AGC_TYPE_BF16, c.out = out_dev;
+    c.value_bf16 = out_type == AGC_TYPE_BF16, c.ld = ldo;
+    return launched(agc::launch_embed_forward(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
+}
+
+int64_t agc_embed_workspace_bytes(int64_t n_tokens, int64_t vocab, int dim, int k_parts)
+{
+    if (n_tokens < 0 || n_tokens > kMostTokens || vocab < 1 || dim < 1 || dim > kMostWidth || k_parts < 1 ||
+        k_parts > agc::kMostParts || vocab > INT32_MAX / k_parts)
+        return 0;
+    return agc::embed_workspace_bytes(n_tokens, vocab, dim, k_parts);
+}
+
+agc_status agc_embed_partial_gradients(const void* dout_dev, int dout_type, int64_t lddout, const void* tokens_dev,
+                                       int token_bytes, int64_t n_tokens, const int64_t* part_end_host, int k_parts,
+                                       int64_t vocab, int dim, float scale, float* G_dev, int64_t ldg, void* workspace_dev,
+                                       void* hip_stream)
+{
+    const char* const name = "agc_embed_partial_gradients";
+    agc::EmbedCall c{};
+    c.tokens = tokens_dev, c.wide_ids = token_bytes == 8, c.n = n_tokens, c.vocab = vocab, c.dim = dim, c.scale = scale;
+    agc_status st = embed_arguments(name, c, token_bytes, dout_type, lddout);
+    if (st != AGC_OK) return st;
+    st = partitions(name, part_end_host, k_parts, n_tokens);
+    if (st != AGC_OK) return st;
+    if (vocab > INT32_MAX / k_parts) return refuse(AGC_ESHAPE, std::string(name) + ": k_parts * vocab must be below 2^31");
+    if (ldg < vocab * dim) return refuse(AGC_ESHAPE, std::string(name) + ": ldg is smaller than the table");
+    if ((!dout_dev && n_tokens > 0) || !G_dev || !workspace_dev) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (misaligned(dout_dev, dout_type == AGC_TYPE_F32 ? 4 : 2) || misaligned(G_dev, 4) || misaligned(workspace_dev, 256))
+        return refuse(AGC_EALIGN, std::string(name) + ": tensors need their elements' alignment, the workspace 256 bytes");
+    c.dout = dout_dev, c.value_bf16 = dout_type == AGC_TYPE_BF16, c.ld = lddout;
+    c.part_end = part_end_host, c.k_parts = k_parts, c.G = G_dev, c.ldg = ldg;
+    c.workspace = static_cast<char*>(workspace_dev);
+    return launched(agc::launch_embed_gradients(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
 }
 
 int64_t agc_gated_workspace_bytes(int64_t n_tokens, int d_in, int d_ff, int k_parts)

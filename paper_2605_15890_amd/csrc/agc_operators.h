@@ -53,4 +53,29 @@ int64_t gated_workspace_bytes(int64_t tokens, int d_in, int d_ff, int k_parts); 
 hipError_t launch_gated_forward(const GatedCall& c, hipStream_t stream);
 hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream);
 
+// ------------------------------------------------------------------ embedding
+struct EmbedCall {
+    const void* tokens;
+    int wide_ids;              // 64-bit ids
+    int64_t n, vocab;
+    int dim;
+    float scale;
+    int value_bf16;            // out, or dout
+    int64_t ld;                // its row stride
+    // forward
+    const void* table;
+    int table_bf16;
+    void* out;
+    // gradients
+    const void* dout;
+    const int64_t* part_end;   // host
+    int k_parts;
+    float* G;
+    int64_t ldg;
+    char* workspace;
+};
+int64_t embed_workspace_bytes(int64_t n, int64_t vocab, int dim, int k_parts);
+hipError_t launch_embed_forward(const EmbedCall& c, hipStream_t stream);
+hipError_t launch_embed_gradients(const EmbedCall& c, hipStream_t stream);
+
 }  // namespace agc

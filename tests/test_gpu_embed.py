@@ -1,0 +1,222 @@
+"""Embedding on the GPU against the formulas in 64 bits on the host.
+
+Tolerances.  Forward: one binary32 product (2^-24 of the value at most) and, to bfloat16, one rounding (2^-8).  Gradient:
+binary32 sums; a value is off by at most (number of additions it went through + 1) * 2^-24 of the sum of its terms'
+magnitudes.  A run of n tokens goes through at most 64 + 64 additions at its ends, 64 + 32 inside its pieces and groups,
+64 pieces at the groups' edges and n / 2048 groups: (300 + n / 2048) * 2^-24.
+"""
+import numpy as np
+import pytest
+
+from paper_2605_15890_amd import api
+
+
+def tensors(dtype, rows, dim, pad, shift, rng):
+    import torch
+    kind = torch.bfloat16 if dtype == "bf16" else torch.float32
+    whole = torch.full((rows * (dim + pad) + shift + 8,), float("nan"), dtype=kind, device="cuda")
+    view = whole[shift:shift + rows * (dim + pad)].view(rows, dim + pad)[:, :dim]
+    view.copy_(torch.from_numpy(rng.standard_normal((rows, dim)).astype(np.float32)).to(kind))
+    return view, view.double().cpu().numpy()
+
+
+def ids_on_gpu(ids, width):
+    import torch
+    return torch.from_numpy(ids.astype(np.int64 if width == 8 else np.int32)).cuda()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("table,value", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("tokens,vocab,dim", [(1, 1, 1), (7, 5, 3), (300, 17, 64), (33, 1000, 257), (1000, 50, 768), (20, 3, 1300)])
+@pytest.mark.parametrize("width,pad,shift", [(4, 0, 0), (8, 4, 4), (8, 3, 1)])
+def test_forward(table, value, tokens, vocab, dim, width, pad, shift):
+    import torch
+    rng = np.random.default_rng(tokens + dim)
+    E, Eh = tensors(table, vocab, dim, 0, shift, rng)
+    ids = rng.integers(0, vocab, tokens)
+    ids[::5] = rng.choice([-1, vocab, vocab + 100, -2 ** 31, 2 ** 31 - 1], len(ids[::5]))
+    out = torch.full((tokens, dim + pad), 3.0, dtype=torch.bfloat16 if value == "bf16" else torch.float32, device="cuda")
+    api.agc_embed_forward(E, ids_on_gpu(ids, width), 1.7, out[:, :dim])
+    got = out.double().cpu().numpy()
+    assert np.all(got[:, dim:] == 3.0)
+    held = (ids >= 0) & (ids < vocab)
+    want = np.where(held[:, None], np.float64(np.float32(1.7)) * Eh[np.where(held, ids, 0)], 0.0)
+    assert np.all(np.abs(got[:, :dim] - want) <= np.abs(want) * (2.0 ** -24 + (2.0 ** -8 if value == "bf16" else 0)))
+
+
+@pytest.mark.gpu
+def test_forward_ids_beyond_32_bits():
+    import torch
+    E = torch.ones(4, 8, device="cuda")
+    ids = torch.tensor([2 ** 32 + 1, 1, -2 ** 33, 2 ** 62], device="cuda")
+    out = torch.empty(4, 8, device="cuda")
+    api.agc_embed_forward(E, ids, 1.0, out)
+    assert out.sum(1).tolist() == [0.0, 8.0, 0.0, 0.0]
+
+
+def host_gradient(dout, ids, ends, vocab, scale):
+    G = np.zeros((len(ends), vocab, dout.shape[1]))
+    size, count = np.zeros_like(G), np.zeros((len(ends), vocab, 1))
+    start = 0
+    for p, end in enumerate(ends):
+        for t in range(start, end):
+            if 0 <= ids[t] < vocab:
+                G[p, ids[t]] += scale * dout[t]
+                size[p, ids[t]] += scale * np.abs(dout[t])
+                count[p, ids[t]] += 1
+        start = end
+    return G, size, count
+
+
+def gradient(ids, ends, vocab, dim, value="f32", width=4, pad=0, shift=0, scale=0.75, seed=0):
+    import torch
+    rng = np.random.default_rng(seed)
+    dout, host = tensors(value, len(ids), dim, pad, shift, rng)
+    held = (ids >= 0) & (ids < vocab)
+    dout[torch.from_numpy(~held).cuda()] = float("nan")     # what an empty place holds counts for nothing
+    row = (vocab * dim + shift + 4 + 3) // 4 * 4 + (1 if shift % 4 else 0)
+    G = torch.full((len(ends), row), 7.0, device="cuda")
+    ws = torch.full((api.agc_embed_workspace_bytes(len(ids), vocab, dim, len(ends)),), 0xFF, dtype=torch.uint8, device="cuda")
+    api.agc_embed_partial_gradients(dout, ids_on_gpu(ids, width), ends, vocab, scale, G[:, shift:shift + vocab * dim], ws)
+    got = G.double().cpu().numpy()
+    assert np.all(got[:, :shift] == 7.0) and np.all(got[:, shift + vocab * dim:] == 7.0)
+    got = got[:, shift:shift + vocab * dim].reshape(len(ends), vocab, dim)
+    want, size, count = host_gradient(np.where(held[:, None], host, 0.0), ids, ends, vocab, scale)
+    assert np.all(np.abs(got - want) <= (300 + count / 2048) * 2.0 ** -24 * size)
+    return got
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,ends,vocab,dim", [
+    (1, [1], 1, 1), (1, [0, 1, 1], 4, 5), (63, [10, 63], 7, 64), (64, [64], 1, 8), (65, [65], 2, 260), (200, [0, 77, 200], 300, 48),
+    (2047, [2047], 3, 12), (2049, [1000, 2049], 11, 7), (5000, [1, 2, 4990, 5000], 90, 33), (9000, [4500, 9000], 5000, 16)])
+def test_gradient(value, tokens, ends, vocab, dim):
+    rng = np.random.default_rng(tokens + dim)
+    ids = np.minimum((np.exp(rng.random(tokens) * np.log(vocab + 1.0)) - 1).astype(np.int64), vocab - 1)
+    ids[rng.random(tokens) < 0.1] = -1
+    gradient(ids, ends, vocab, dim, value, seed=tokens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [128, 2048, 4096, 4100, 70001])
+@pytest.mark.parametrize("lead", [0, 1, 63, 64])
+def test_gradient_of_one_id(tokens, lead):
+    """All tokens name one id, after `lead` of another: whole pieces and groups, at every offset from their edges."""
+    ids = np.full(tokens, 2)
+    ids[:min(lead, tokens - 1)] = 1
+    gradient(ids, [tokens], 4, 4, seed=lead)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [2048, 3000, 1 << 22, (1 << 22) + 5])
+def test_gradient_keys_of_one_two_and_three_digits(vocab):
+    ids = np.array([vocab - 1, 0, vocab - 1, 5, -1, vocab - 2, vocab // 2, 5, 2047, vocab], dtype=np.int64)
+    got = gradient(ids, [4, 10], vocab, 2)
+    assert np.count_nonzero(np.abs(got).sum(2)) == 3 + 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("width,pad,shift,value", [(8, 0, 1, "f32"), (8, 4, 4, "f32"), (4, 3, 0, "bf16"), (8, 4, 8, "bf16"), (4, 0, 2, "bf16")])
+def test_gradient_strides_and_alignment(width, pad, shift, value):
+    ids = np.random.default_rng(1).integers(-1, 21, 500)
+    gradient(ids, [200, 500], 20, 68, value, width, pad, shift)
+
+
+@pytest.mark.gpu
+def test_nothing_but_empty_places_and_no_tokens():
+    import torch
+    gradient(np.full(300, -1), [100, 300], 9, 20)
+    ws = torch.empty(api.agc_embed_workspace_bytes(0, 9, 20, 2), dtype=torch.uint8, device="cuda")
+    G = torch.full((2, 180), 7.0, device="cuda")
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    api.agc_embed_partial_gradients(torch.empty(0, 20, device="cuda"), none, [0, 0], 9, 1.0, G, ws)
+    assert torch.all(G == 0)
+    api.agc_embed_forward(torch.ones(9, 20, device="cuda"), none, 1.0, torch.empty(0, 20, device="cuda"))
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences():
+    """The loss sum(dout * out) is linear in the table: a step along a direction changes it by the gradient's product with
+    the direction, to the rounding of the sums."""
+    import torch
+    rng = np.random.default_rng(8)
+    tokens, vocab, dim, ends = 400, 30, 24, [150, 400]
+    ids = rng.integers(-1, vocab, tokens)
+    got = gradient(ids, ends, vocab, dim, seed=9)
+    dout = tensors("f32", tokens, dim, 0, 0, np.random.default_rng(9))[1]
+    v = rng.standard_normal((vocab, dim)).astype(np.float32)
+    moved = torch.empty(tokens, dim, device="cuda")
+    api.agc_embed_forward(torch.from_numpy(v).cuda(), ids_on_gpu(ids, 4), 0.75, moved)
+    moved = moved.double().cpu().numpy()
+    start = 0
+    for p, end in enumerate(ends):
+        change = np.sum(dout[start:end] * moved[start:end])
+        assert abs(np.sum(got[p] * v) - change) < 1e-5 * np.linalg.norm(got[p]) * np.linalg.norm(v)
+        start = end
+
+
+@pytest.mark.gpu
+def test_same_result_twice_on_another_stream_and_in_a_graph():
+    import torch
+    tokens, vocab, dim, ends = 6000, 40, 96, [2000, 6000]
+    ids = torch.randint(-1, vocab, (tokens,), device="cuda")
+    dout, E = torch.randn(tokens, dim, device="cuda"), torch.randn(vocab, dim, device="cuda")
+    ws = torch.empty(api.agc_embed_workspace_bytes(tokens, vocab, dim, 2), dtype=torch.uint8, device="cuda")
+
+    def make():
+        return torch.zeros(tokens, dim, device="cuda"), torch.zeros(2, vocab * dim, device="cuda")
+
+    def call(out, G):
+        api.agc_embed_forward(E, ids, 2.0, out)
+        api.agc_embed_partial_gradients(dout, ids, ends, vocab, 2.0, G, ws)
+
+    first, second, third = make(), make(), make()
+    call(*first)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(*second)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(*third)
+    for _ in range(3):
+        for t in third:
+            t.fill_(9.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, third))
+
+
+def test_refusals():
+    """Arguments that are refused before anything reaches the GPU (addresses are never followed)."""
+    L = api.load()
+
+    def fwd(table=4096, kind=0, vocab=10, dim=8, tokens=8192, width=4, n=3, out=12288, out_kind=1, ldo=8):
+        return L.agc_embed_forward(table, kind, vocab, dim, tokens, width, n, 1.0, out, out_kind, ldo, None)
+
+    for kw in (dict(table=None), dict(tokens=None), dict(out=None), dict(kind=2), dict(out_kind=-1), dict(width=2)):
+        assert fwd(**kw) == api.AGC_EINVAL, kw
+    for kw in (dict(vocab=0), dict(vocab=1 << 31), dict(dim=0), dict(dim=65537, ldo=65537), dict(n=-1), dict(n=(1 << 26) + 1), dict(ldo=7)):
+        assert fwd(**kw) == api.AGC_ESHAPE, kw
+    for kw in (dict(table=4098), dict(table=4097, kind=1), dict(tokens=8194), dict(tokens=8196, width=8), dict(out=12289)):
+        assert fwd(**kw) == api.AGC_EALIGN, kw
+    assert fwd(n=0) == api.AGC_OK
+
+    def grad(dout=4096, kind=0, ld=8, tokens=8192, width=4, n=3, ends=(1, 3), k=2, vocab=10, dim=8, G=12288, ldg=80, ws=16384):
+        packed = None if ends is None else np.array(ends, dtype=np.int64).tobytes()
+        return L.agc_embed_partial_gradients(dout, kind, ld, tokens, width, n, packed, k, vocab, dim, 1.0, G, ldg, ws, None)
+
+    for kw in (dict(dout=None), dict(tokens=None), dict(ends=None), dict(G=None), dict(ws=None), dict(kind=2), dict(width=3)):
+        assert grad(**kw) == api.AGC_EINVAL, kw
+    for kw in (dict(ld=7), dict(ldg=79), dict(ends=(2, 1)), dict(ends=(-1, 3)), dict(ends=(1, 2)), dict(k=0), dict(k=257),
+               dict(vocab=1 << 30, ldg=1 << 40)):
+        assert grad(**kw) == api.AGC_ESHAPE, kw
+    for kw in (dict(dout=4098), dict(tokens=8193), dict(G=12290), dict(ws=16388)):
+        assert grad(**kw) == api.AGC_EALIGN, kw
+    assert b"agc_embed_partial_gradients" in L.agc_last_error(None)
+    assert api.agc_embed_workspace_bytes(4, 1 << 30, 4, 2) == 0 and api.agc_embed_workspace_bytes(-1, 4, 4, 1) == 0
+    assert api.agc_embed_workspace_bytes(0, 4, 4, 1) > 0
