@@ -280,9 +280,9 @@ __global__ __launch_bounds__(64) void k_embed_groups(const SumArgs a)
     *reinterpret_cast<f32x4*>(a.groups + (int64_t)blockIdx.x * a.pitch + c) = sum;
 }
 
-__device__ __forceinline__ int lower_bound(const uint32_t* key, int n, uint32_t what)
+// First place in [lo, hi) whose key is not below `what`; hi if none is.
+__device__ __forceinline__ int lower_bound(const uint32_t* key, int lo, int hi, uint32_t what)
 {
-    int lo = 0, hi = n;
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (key[mid] < what) lo = mid + 1;
@@ -291,47 +291,103 @@ __device__ __forceinline__ int lower_bound(const uint32_t* key, int n, uint32_t 
     return lo;
 }
 
-// All rows of G: a wave takes `rows` (up to 64) consecutive ones, each lane searches the run of one of them.
-template <class T, bool WHOLE>
-__global__ __launch_bounds__(kBlock) void k_embed_rows(const SumArgs a, const T* dout, int64_t vocab, int64_t total, float scale,
-                                                       float* G, int64_t ldg, int rows)
+// The same by a whole wave, 64 places at a time: three steps for 2^18 keys.
+__device__ __forceinline__ int wave_lower_bound(const uint32_t* key, int lo, int hi, uint32_t what, int lane)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t first = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * rows;
+    while (lo < hi) {
+        const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
+        const uint64_t below = __ballot(at < hi && key[at] < what);   // a run of ones from lane 0 on
+        const int n = __popcll(below);
+        if (n == 0) return lo;
+        const int top = lo + n * step;
+        lo = lo + (n - 1) * step + 1;
+        hi = top < hi ? top : hi;
+    }
+    return lo;
+}
+
+// Rows of G that nobody names: a wave takes `rows` (up to 64) consecutive rows and writes zeros to those whose run is
+// empty.
+template <bool WHOLE>
+__device__ __forceinline__ void fill_rows(const SumArgs& a, int64_t vocab, int64_t total, float* G, int64_t ldg, int rows,
+                                          int64_t wave, int lane)
+{
+    const int64_t first = wave * rows;
     if (first >= total) return;
     const int count = total - first < rows ? (int)(total - first) : rows;
-    // lane i < count: where row first + i begins; lane `count`: where the last one ends.  With 64 rows that is lane 0's.
-    int begin = lane <= count ? lower_bound(a.key, a.n, (uint32_t)(first + lane)) : 0;
-    int last = count == 64 ? lower_bound(a.key, a.n, (uint32_t)(first + 64)) : 0;
+    const int lo = wave_lower_bound(a.key, 0, a.n, (uint32_t)first, lane);
+    const int hi = wave_lower_bound(a.key, lo, a.n, (uint32_t)(first + count), lane);
+    uint64_t empty = ~0ull;
+    if (lo < hi) {
+        const int begin = lower_bound(a.key, lo, hi, (uint32_t)(first + lane));
+        const int end = __shfl_down(begin, 1);
+        empty = __ballot(begin == (lane < 63 ? end : hi));
+    }
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     int64_t p = first / vocab, v = first - p * vocab;
     for (int r = 0; r < count; ++r) {
-        const int from = __builtin_amdgcn_readlane(begin, r);
-        const int to = r == 63 ? __builtin_amdgcn_readfirstlane(last) : __builtin_amdgcn_readlane(begin, r + 1);
-        float* row = G + p * ldg + v * a.dim;
-        for (int c = lane * 4; c < a.dim; c += 256) {
-            f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (from < to) {
-                const int p0 = (from + kPiece - 1) / kPiece, p1 = to / kPiece;   // whole pieces
-                if (p0 < p1) {
-                    acc = sum_tokens<T, WHOLE>(a, dout, from, p0 * kPiece, c, acc);
-                    const int g0 = (p0 + kGroup - 1) / kGroup, g1 = p1 / kGroup;
-                    if (g0 < g1) {
-                        acc = sum_rows(a.pieces, a.pitch, p0, g0 * kGroup, c, acc);
-                        acc = sum_rows(a.groups, a.pitch, g0, g1, c, acc);
-                        acc = sum_rows(a.pieces, a.pitch, g1 * kGroup, p1, c, acc);
-                    } else {
-                        acc = sum_rows(a.pieces, a.pitch, p0, p1, c, acc);
-                    }
-                    acc = sum_tokens<T, WHOLE>(a, dout, p1 * kPiece, to, c, acc);
-                } else {
-                    acc = sum_tokens<T, WHOLE>(a, dout, from, to, c, acc);
-                }
-            }
-            if (from < to) acc = acc * scale;
-            store4<float, WHOLE>(row, c, a.dim, acc);
+        if ((empty >> r) & 1) {
+            float* row = G + p * ldg + v * a.dim;
+            for (int c = lane * 4; c < a.dim; c += 256) store4<float, WHOLE>(row, c, a.dim, zero);
         }
         if (++v == vocab) v = 0, ++p;
     }
+}
+
+// Rows that somebody names: a wave takes kHeads places of the order and the runs that begin there, 256 columns of them.
+constexpr int kHeads = 8;
+
+template <class T, bool WHOLE>
+__device__ __forceinline__ void sum_runs(const SumArgs& a, const T* dout, int64_t vocab, float scale, float* G, int64_t ldg,
+                                         int64_t wave, int lane)
+{
+    const int across = (a.dim + 255) >> 8;
+    const int64_t strip = wave / across;
+    const int c = ((int)(wave - strip * across) * 64 + lane) * 4;
+    const int64_t first = strip * kHeads;
+    if (first >= a.n) return;
+    const int at = (int)first + lane;
+    const uint32_t key = at < a.n ? a.key[at] : a.none;
+    const uint32_t before = at > 0 && at <= a.n ? a.key[at - 1] : ~0u;
+    const uint64_t heads = __ballot(key != before || at >= a.n);
+    for (uint64_t left = heads & ((1ull << kHeads) - 1); left; left &= left - 1) {
+        const int h = __builtin_ctzll(left);
+        const uint32_t k = __builtin_amdgcn_readlane(key, h);
+        if (k == a.none) return;   // empty places, or the end: nothing comes behind them
+        const int from = (int)first + h;
+        const uint64_t later = heads & ~((2ull << h) - 1);
+        int to = (int)first + (later ? __builtin_ctzll(later) : 64);
+        if (!later) to = wave_lower_bound(a.key, to < a.n ? to : a.n, a.n, k + 1, lane);
+        if (c >= a.dim) continue;
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int p0 = (from + kPiece - 1) / kPiece, p1 = to / kPiece;   // whole pieces
+        if (p0 < p1) {
+            acc = sum_tokens<T, WHOLE>(a, dout, from, p0 * kPiece, c, acc);
+            const int g0 = (p0 + kGroup - 1) / kGroup, g1 = p1 / kGroup;
+            if (g0 < g1) {
+                acc = sum_rows(a.pieces, a.pitch, p0, g0 * kGroup, c, acc);
+                acc = sum_rows(a.groups, a.pitch, g0, g1, c, acc);
+                acc = sum_rows(a.pieces, a.pitch, g1 * kGroup, p1, c, acc);
+            } else {
+                acc = sum_rows(a.pieces, a.pitch, p0, p1, c, acc);
+            }
+            acc = sum_tokens<T, WHOLE>(a, dout, p1 * kPiece, to, c, acc);
+        } else {
+            acc = sum_tokens<T, WHOLE>(a, dout, from, to, c, acc);
+        }
+        const int64_t p = k / (uint32_t)vocab, v = k - p * vocab;
+        store4<float, WHOLE>(G + p * ldg + v * a.dim, c, a.dim, acc * scale);
+    }
+}
+
+// All rows of G.  The first `sum_blocks` workgroups sum runs, which take longest, the others write zeros.
+template <class T, bool WHOLE>
+__global__ __launch_bounds__(kBlock) void k_embed_rows(const SumArgs a, const T* dout, int64_t vocab, int64_t total, float scale,
+                                                       float* G, int64_t ldg, int rows, unsigned sum_blocks)
+{
+    const int lane = threadIdx.x & 63, sub = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (blockIdx.x < sum_blocks) sum_runs<T, WHOLE>(a, dout, vocab, scale, G, ldg, (int64_t)blockIdx.x * 4 + sub, lane);
+    else fill_rows<WHOLE>(a, vocab, total, G, ldg, rows, (int64_t)(blockIdx.x - sum_blocks) * 4 + sub, lane);
 }
 
 template <class TABLE, class OUT, class ID>
@@ -380,9 +436,10 @@ hipError_t sums_as(const EmbedCall& c, const SumArgs& a, hipStream_t stream)
     const int64_t total = c.vocab * c.k_parts;
     int rows = 64;
     while (rows > 1 && total / rows < 8192) rows /= 2;
-    const int64_t waves = (total + rows - 1) / rows;
-    hipLaunchKernelGGL((k_embed_rows<T, WHOLE>), dim3((unsigned)((waves + 3) / 4)), dim3(kBlock), 0, stream, a, dout, c.vocab,
-                       total, c.scale, c.G, c.ldg, rows);
+    const int64_t fills = (total + rows - 1) / rows, sums = (int64_t)((a.n + kHeads - 1) / kHeads) * across;
+    const unsigned sum_blocks = (unsigned)((sums + 3) / 4);
+    hipLaunchKernelGGL((k_embed_rows<T, WHOLE>), dim3(sum_blocks + (unsigned)((fills + 3) / 4)), dim3(kBlock), 0, stream, a, dout,
+                       c.vocab, total, c.scale, c.G, c.ldg, rows, sum_blocks);
     return hipGetLastError();
 }
 
