@@ -323,6 +323,202 @@ struct ApplyJob {
     }
 };
 
+// ------------------------------------------------------------------ small matrices
+// A matrix whose X, its transpose and A fit into one workgroup's LDS (up to 64 x 256, 96 x 128): the whole update in one
+// launch, one workgroup a matrix.  Bound by the latency of its 3 * steps products, one after another: the separate
+// kernels take some 6 us for each, this one about 1.
+// Both sides are padded to 32 with zeros.  A split row lies in LDS as in memory, its 16-byte chunks permuted by the
+// row's low bits within each 128 bytes.
+// Two forms: 16 waves and one or two 16 x 16 blocks of each product a wave, or 8 waves with up to 5 of A and 9 of X.
+struct SmallNarrow {
+    static constexpr int kThreads = 1024, kPer = 8, kGram = 1, kBlocks = 2, kLds = 80 * 1024;
+    static bool takes(int64_t m, int64_t n) { return m <= 64 && m * n <= 8192; }   // 8 m n + 4 m m <= 80 KB
+};
+struct SmallWide {
+    static constexpr int kThreads = 512, kPer = 36, kGram = 5, kBlocks = 9, kLds = 152 * 1024;
+    static bool takes(int64_t m, int64_t n) { return 8 * m * n + 4 * m * m <= kLds; }   // m <= 96, m n <= 18432
+};
+
+__device__ __forceinline__ int small_at(int row, int k, int pitch)   // byte of the high part; the low part: ^ 64
+{
+    return row * pitch + (k >> 5) * 128 + (((((k & 31) >> 3)) ^ (row & 7)) << 4) + (k & 7) * 2;
+}
+
+__device__ __forceinline__ void small_put(char* base, int row, int k, int pitch, float v)
+{
+    const int at = small_at(row, k, pitch);
+    const _Float16 hi = (_Float16)v;
+    *reinterpret_cast<_Float16*>(base + at) = hi;
+    *reinterpret_cast<_Float16*>(base + (at ^ 64)) = (_Float16)(v - (float)hi);
+}
+
+// Four values of consecutive k (a multiple of 4)
+__device__ __forceinline__ void small_put4(char* base, int row, int k, int pitch, const tile_f32x4& v)
+{
+    const int at = small_at(row, k, pitch);
+    f16x4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        hi[e] = (_Float16)v[e];
+        lo[e] = (_Float16)(v[e] - (float)hi[e]);
+    }
+    *reinterpret_cast<f16x4*>(base + at) = hi;
+    *reinterpret_cast<f16x4*>(base + (at ^ 64)) = lo;
+}
+
+// 16 x 16 block (rows ra.. of a, rows rb.. of b) of a product of split rows: `c` with a lane's four values along a's
+// rows, and, if TWO, `t` with four values along b's rows (the same block, its operands exchanged), so that either can
+// be stored four values at a time.
+template <bool TWO>
+__device__ __forceinline__ void small_block(const char* a, const char* b, int ra, int rb, int pitch, int steps, int lane,
+                                            tile_f32x4& c, tile_f32x4& t)
+{
+    const tile_f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    tile_f32x4 c1 = zero, t1 = zero;
+    c = t = zero;
+    const int sub = lane & 15, chunk = ((lane >> 4) ^ (lane & 7)) << 4;   // rows start at multiples of 16
+    const char *pa = a + (ra + sub) * pitch, *pb = b + (rb + sub) * pitch;
+    for (int s = 0; s < steps; ++s, pa += 128, pb += 128) {
+        const tile_u32x4 a0 = *reinterpret_cast<const tile_u32x4*>(pa + chunk);
+        const tile_u32x4 a1 = *reinterpret_cast<const tile_u32x4*>(pa + (chunk ^ 64));
+        const tile_u32x4 b0 = *reinterpret_cast<const tile_u32x4*>(pb + chunk);
+        const tile_u32x4 b1 = *reinterpret_cast<const tile_u32x4*>(pb + (chunk ^ 64));
+        c = tile_mfma<kSplit>(a0, b0, c);
+        if (TWO) t = tile_mfma<kSplit>(b0, a0, t);
+        c1 = tile_mfma<kSplit>(a0, b1, c1);
+        if (TWO) t1 = tile_mfma<kSplit>(b0, a1, t1);
+        c1 = tile_mfma<kSplit>(a1, b0, c1);
+        if (TWO) t1 = tile_mfma<kSplit>(b1, a0, t1);
+    }
+    c += c1;
+    t += t1;
+}
+
+template <class FORM>
+__global__ __launch_bounds__(FORM::kThreads) void k_muon_small(const MuonCall c, MuonGeom g)
+{
+    constexpr int kSmallThreads = FORM::kThreads, kSmallWaves = kSmallThreads / 64, kSmallPer = FORM::kPer;
+    constexpr int kSmallGram = FORM::kGram, kSmallBlocks = FORM::kBlocks, kSmallLds = FORM::kLds;
+    __shared__ __attribute__((aligned(1024))) char lds[kSmallLds];
+    __shared__ double part[kSmallWaves];
+    const int tid = threadIdx.x, lane = tid & 63, q4 = (lane >> 4) * 4, col = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int m = g.m, n = g.n, mr = (int)(g.pitch_m / 4), nr = (int)(g.pitch_n / 4);
+    const int pitch_m = (int)g.pitch_m, pitch_n = (int)g.pitch_n;
+    char* x = lds;                       // mr rows along n
+    char* xt = x + mr * pitch_n;         // nr rows along m
+    char* a = xt + nr * pitch_m;         // mr rows along m: A, then B
+    const int64_t off = c.offset[blockIdx.x];
+
+    // M and U, a value of every kSmallThreads a register
+    const int count = m * n;
+    float u[kSmallPer], old[kSmallPer];
+#pragma unroll
+    for (int i = 0; i < kSmallPer; ++i) {
+        const int at = tid + i * kSmallThreads;
+        u[i] = old[i] = 0.0f;
+        if (at < count) u[i] = c.ghat[off + at], old[i] = c.m1[off + at];
+    }
+    for (int i = tid * 16; i < mr * pitch_n + nr * pitch_m; i += kSmallThreads * 16)
+        *reinterpret_cast<tile_u32x4*>(lds + i) = tile_u32x4{0u, 0u, 0u, 0u};
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kSmallPer; ++i) {
+        const int at = tid + i * kSmallThreads;
+        const float mv = fmaf(c.momentum, old[i], u[i]);
+        if (at < count) c.m1[off + at] = mv;
+        u[i] = c.nesterov ? fmaf(c.momentum, mv, u[i]) : mv;
+        sum = fma((double)u[i], (double)u[i], sum);
+    }
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int i = 0; i < kSmallWaves; ++i) sum += part[i];
+    const float unit = (float)((double)kUnitX / (sqrt(sum) + kMuonEps));
+#pragma unroll
+    for (int i = 0; i < kSmallPer; ++i) {
+        const int at = tid + i * kSmallThreads;
+        if (at >= count) continue;
+        const int major = at / c.cols, minor = at - major * c.cols;
+        const int r = g.tall ? minor : major, k = g.tall ? major : minor;
+        small_put(x, r, k, pitch_n, u[i] * unit);
+        small_put(xt, k, r, pitch_m, u[i] * unit);
+    }
+    __syncthreads();
+
+    const int across_m = mr / 16, across_n = nr / 16;
+    tile_f32x4 unused;
+    for (int step = 0; step < c.steps; ++step) {
+        for (int i = wave; i < across_m * across_m; i += kSmallWaves) {
+            const int bi = i / across_m * 16, bj = (i - i / across_m * across_m) * 16;
+            tile_f32x4 v;
+            small_block<false>(x, x, bi, bj, pitch_n, nr / 32, lane, v, unused);
+            small_put4(a, bj + col, bi + q4, pitch_m, v * (kUnitA / (kUnitX * kUnitX)));   // symmetric
+        }
+        __syncthreads();
+        tile_f32x4 poly[kSmallGram];
+#pragma unroll
+        for (int b = 0; b < kSmallGram; ++b) {
+            const int i = wave + b * kSmallWaves;
+            if (i >= across_m * across_m) continue;
+            const int bi = i / across_m * 16, bj = (i - i / across_m * across_m) * 16;
+            small_block<false>(a, a, bi, bj, pitch_m, mr / 32, lane, poly[b], unused);
+            const int at = small_at(bj + col, bi + q4, pitch_m);
+            const f16x4 hi = *reinterpret_cast<const f16x4*>(a + at), lo = *reinterpret_cast<const f16x4*>(a + (at ^ 64));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float v = fmaf(kNsC * (kUnitB / (kUnitA * kUnitA)), poly[b][e],
+                               kNsB * (kUnitB / kUnitA) * ((float)hi[e] + (float)lo[e]));
+                if (bj + col == bi + q4 + e) v += kNsA * kUnitB;
+                poly[b][e] = v;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < kSmallGram; ++b) {
+            const int i = wave + b * kSmallWaves;
+            if (i >= across_m * across_m) continue;
+            const int bi = i / across_m * 16, bj = (i - i / across_m * across_m) * 16;
+            small_put4(a, bj + col, bi + q4, pitch_m, poly[b]);
+        }
+        __syncthreads();
+        tile_f32x4 next[kSmallBlocks], turned[kSmallBlocks];
+#pragma unroll
+        for (int b = 0; b < kSmallBlocks; ++b) {
+            const int i = wave + b * kSmallWaves;
+            if (i >= across_m * across_n) continue;
+            const int bi = i / across_n * 16, bj = (i - i / across_n * across_n) * 16;
+            small_block<true>(a, xt, bi, bj, pitch_m, mr / 32, lane, next[b], turned[b]);
+        }
+        __syncthreads();
+        const bool last = step + 1 == c.steps;
+#pragma unroll
+        for (int b = 0; b < kSmallBlocks; ++b) {
+            const int i = wave + b * kSmallWaves;
+            if (i >= across_m * across_n) continue;
+            const int bi = i / across_n * 16, bj = (i - i / across_n * across_n) * 16;
+            if (!last) {
+                small_put4(x, bi + col, bj + q4, pitch_n, turned[b] * (1.0f / kUnitB));
+                small_put4(xt, bj + col, bi + q4, pitch_m, next[b] * (1.0f / kUnitB));
+                continue;
+            }
+            // along the rows of the matrix as it lies: four values of consecutive columns
+            const int major = (g.tall ? bj : bi) + col, minor = (g.tall ? bi : bj) + q4;
+            const tile_f32x4 v = g.tall ? next[b] : turned[b];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (major >= c.rows || minor + e >= c.cols) continue;
+                const int64_t at = off + major * c.cols + minor + e;
+                const float w = fmaf(-c.rate * (1.0f / (kUnitB * kUnitX)), v[e], c.keep * c.beta[at]);
+                c.beta[at] = w;
+                if (c.beta_bf16) c.beta_bf16[at] = (uint16_t)bf16_bits(w);
+            }
+        }
+        __syncthreads();
+    }
+}
+
 hipError_t launch_sym(SymJob j, int mats, hipStream_t stream)
 {
     const int big = (j.m + 255) / 256, small = (j.m + 127) / 128;
@@ -364,6 +560,15 @@ int64_t muon_workspace_bytes(int rows, int cols, int n_mats)
 hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
 {
     const MuonGeom g = muon_geom(c.rows, c.cols, c.n_mats);
+    const int64_t mr = round_up(g.m, 32), nr = round_up(g.n, 32);
+    if (SmallNarrow::takes(mr, nr)) {
+        hipLaunchKernelGGL(k_muon_small<SmallNarrow>, dim3(c.n_mats), dim3(SmallNarrow::kThreads), 0, stream, c, g);
+        return hipGetLastError();
+    }
+    if (SmallWide::takes(mr, nr)) {
+        hipLaunchKernelGGL(k_muon_small<SmallWide>, dim3(c.n_mats), dim3(SmallWide::kThreads), 0, stream, c, g);
+        return hipGetLastError();
+    }
     const int64_t count = (int64_t)c.rows * c.cols;
     const int n_sums = muon_sums(count);
     double* sums = reinterpret_cast<double*>(c.workspace);

@@ -21,6 +21,7 @@
 
 namespace agc {
 
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 tile_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float tile_f32x4 __attribute__((ext_vector_type(4)));
