@@ -233,9 +233,11 @@ __global__ __launch_bounds__(kBlock) void k_gated_few(const uint16_t* x, int64_t
 template <bool GRAD>
 struct GateJob {
     static constexpr TilePair kPair = kPlain;
+    static constexpr int kRowParts = 4;
+    static constexpr bool kTurned = GRAD;
     const uint16_t *x, *wg, *wu;      // rows of whole k-steps
     int64_t ldx, ldg, ldu;
-    int rows, d_ff, steps;            // rows: tokens, or places of `map`
+    int n_rows, d_ff, steps;          // rows: tokens, or places of `map`
     Activation act;
     const int* map;
     // forward
@@ -248,18 +250,17 @@ struct GateJob {
     int fp;
     char* by_feature;                 // 2 d_ff rows of pairs along the places
     int64_t pitch;
-    int mt, nt, side_m, side_n, total;
+    int mt, nt, side, total;
 
-    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    __device__ __forceinline__ void place(int id, TilePos& p) const
     {
         int mi, ni;
         tile_order(xcd_order(id, total), mt, nt, mi, ni);
-        p.batch = 0, p.m0 = mi * side_m, p.n0 = ni * side_n, p.steps = steps;
-        return true;
+        p.batch = 0, p.m0 = mi * side, p.n0 = ni * side, p.steps = steps;
     }
     __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
     {
-        int at = p.m0 + r < rows ? p.m0 + r : rows - 1;
+        int at = p.m0 + r < n_rows ? p.m0 + r : n_rows - 1;
         if (GRAD) at = map[at] < 0 ? 0 : map[at];
         return reinterpret_cast<const char*>(x + at * ldx);
     }
@@ -269,124 +270,118 @@ struct GateJob {
         const int64_t f = at < d_ff ? at : d_ff - 1;
         return reinterpret_cast<const char*>((i & 16) ? wu + f * ldu : wg + f * ldg);
     }
-    __device__ __forceinline__ void piece(const TilePos&, int mb, int nb, float* s, int lane) const
+    __device__ __forceinline__ bool turned(const TilePos&) const { return true; }
+    __device__ __forceinline__ void rows(const TilePos&, int mb, int nb, float* s, int it, int lane) const
     {
         const int j = lane & 3, ca = (j >> 1) * 32 + (j & 1) * 8, f = nb / 2 + j * 8;
+        const int r = it * 16 + (lane >> 2), row = mb + r;
+        float a[8], u[8];
+        piece_row8(s, r, ca, a);
+        piece_row8(s, r, ca + 16, u);
+        if (!GRAD) {
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const int r = it * 16 + (lane >> 2), row = mb + r;
-            float a[8], u[8];
-            piece_row8(s, r, ca, a);
-            piece_row8(s, r, ca + 16, u);
-            if (!GRAD) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = act(a[e]) * u[e];
-                if (row < rows && f < d_ff) store_bf16(h + row * ldh + f, d_ff - f, a);
-                continue;
-            }
-            float da[8], du[8], g[8];
-            const int t = row < rows ? map[row] : -1;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) da[e] = du[e] = 0.0f;
-            if (t >= 0 && f < d_ff) {
-                load_bf16(dh + t * lddh + f, d_ff - f, g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float value, slope;
-                    act.at(a[e], value, slope);
-                    if (f + e < d_ff) da[e] = g[e] * u[e] * slope, du[e] = g[e] * value;
-                }
-            }
-            if (row < rows && f < fp) {
-                uint16_t* o = reinterpret_cast<uint16_t*>(by_token) + (int64_t)row * 2 * fp + f;
-                *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(da);
-                *reinterpret_cast<tile_u32x4*>(o + fp) = bf16_pack8(du);
-            }
-            piece_put_row8(s, r, ca, da);
-            piece_put_row8(s, r, ca + 16, du);
+            for (int e = 0; e < 8; ++e) a[e] = act(a[e]) * u[e];
+            if (row < n_rows && f < d_ff) store_bf16(h + row * ldh + f, d_ff - f, a);
+            return;
         }
-        if (!GRAD) return;
-        wave_lds_fence();
-        const int run = (lane & 7) * 8, at = mb + run;
+        float da[8], du[8], g[8];
+        const int t = row < n_rows ? map[row] : -1;
 #pragma unroll
-        for (int it = 0; it < 8; ++it) {
-            const int c = it * 8 + (lane >> 3), ff = nb / 2 + (c >> 5) * 16 + (c & 15);
-            if (ff >= d_ff || at >= rows) continue;   // rows is a multiple of 32
-            float v[8], hi[8], lo[8];
-            piece_col8(s, run, c, v);
+        for (int e = 0; e < 8; ++e) da[e] = du[e] = 0.0f;
+        if (t >= 0 && f < d_ff) {
+            load_bf16(dh + t * lddh + f, d_ff - f, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                hi[e] = __uint_as_float(bf16_bits(v[e]) << 16);
-                lo[e] = v[e] - hi[e];
+                float value, slope;
+                act.at(a[e], value, slope);
+                if (f + e < d_ff) da[e] = g[e] * u[e] * slope, du[e] = g[e] * value;
             }
-            char* o = by_feature + (int64_t)(((c & 16) ? d_ff : 0) + ff) * pitch + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
-            *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(hi);
-            *reinterpret_cast<tile_u32x4*>(o + 64) = bf16_pack8(lo);
         }
+        if (row < n_rows && f < fp) {
+            uint16_t* o = reinterpret_cast<uint16_t*>(by_token) + (int64_t)row * 2 * fp + f;
+            *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(da);
+            *reinterpret_cast<tile_u32x4*>(o + fp) = bf16_pack8(du);
+        }
+        piece_put_row8(s, r, ca, da);
+        piece_put_row8(s, r, ca + 16, du);
+    }
+    __device__ __forceinline__ void cols(const TilePos&, int mb, int nb, const float* s, int it, int lane) const
+    {
+        const int run = (lane & 7) * 8, at = mb + run;
+        const int c = it * 8 + (lane >> 3), ff = nb / 2 + (c >> 5) * 16 + (c & 15);
+        if (ff >= d_ff || at >= n_rows) return;   // n_rows is a multiple of 32
+        float v[8], hi[8], lo[8];
+        piece_col8(s, run, c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            hi[e] = __uint_as_float(bf16_bits(v[e]) << 16);
+            lo[e] = v[e] - hi[e];
+        }
+        char* o = by_feature + (int64_t)(((c & 16) ? d_ff : 0) + ff) * pitch + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
+        *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(hi);
+        *reinterpret_cast<tile_u32x4*>(o + 64) = bf16_pack8(lo);
     }
 };
 
 // dx = [da | du] [Wg | Wu]^T
 struct InputJob {
     static constexpr TilePair kPair = kPlain;
+    static constexpr int kRowParts = 8;
+    static constexpr bool kTurned = false;
     const char *a, *b;
     int64_t pitch;
-    int rows, d_in, steps;
+    int n_rows, d_in, steps;
     const int* map;
     uint16_t* dx;
     int64_t lddx;
-    int mt, nt, side_m, side_n, total;
+    int mt, nt, side, total;
 
-    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    __device__ __forceinline__ void place(int id, TilePos& p) const
     {
         int mi, ni;
         tile_order(xcd_order(id, total), mt, nt, mi, ni);
-        p.batch = 0, p.m0 = mi * side_m, p.n0 = ni * side_n, p.steps = steps;
-        return true;
+        p.batch = 0, p.m0 = mi * side, p.n0 = ni * side, p.steps = steps;
     }
     __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
     {
-        return a + (p.m0 + r < rows ? p.m0 + r : rows - 1) * pitch;
+        return a + (p.m0 + r < n_rows ? p.m0 + r : n_rows - 1) * pitch;
     }
     __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const
     {
         return b + (p.n0 + r < d_in ? p.n0 + r : d_in - 1) * pitch;
     }
-    __device__ __forceinline__ void piece(const TilePos&, int mb, int nb, float* s, int lane) const
+    __device__ __forceinline__ void rows(const TilePos&, int mb, int nb, const float* s, int it, int lane) const
     {
-        const int run = (lane & 7) * 8, c = nb + run;
-#pragma unroll
-        for (int it = 0; it < 8; ++it) {
-            const int r = it * 8 + (lane >> 3), row = mb + r;
-            const int t = row < rows ? map[row] : -1;
-            if (t < 0 || c >= d_in) continue;
-            float v[8];
-            piece_row8(s, r, run, v);
-            store_bf16(dx + t * lddx + c, d_in - c, v);
-        }
+        const int run = (lane & 7) * 8, c = nb + run, r = it * 8 + (lane >> 3), row = mb + r;
+        const int t = row < n_rows ? map[row] : -1;
+        if (t < 0 || c >= d_in) return;
+        float v[8];
+        piece_row8(s, r, run, v);
+        store_bf16(dx + t * lddx + c, d_in - c, v);
     }
 };
 
 // Row p of G: [da | du]_p^T x_p
 struct WeightJob {
     static constexpr TilePair kPair = kPlain;
+    static constexpr int kRowParts = 8;
+    static constexpr bool kTurned = false;
     const char *a, *b;        // 2 d_ff and d_in rows along the places
     int64_t pitch;
     int d_ff, d_in;
     float *gate, *up;
     int64_t ldg;
-    int mt, nt, side_m, side_n, total;
+    int mt, nt, side, total;
     GatedParts parts;
 
-    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    __device__ __forceinline__ void place(int id, TilePos& p) const
     {
         const int t = xcd_order(id, total);
         p.batch = t / (mt * nt);
         int mi, ni;
         tile_order(t - p.batch * mt * nt, mt, nt, mi, ni);
-        p.m0 = mi * side_m, p.n0 = ni * side_n;
+        p.m0 = mi * side, p.n0 = ni * side;
         p.steps = (parts.place[p.batch + 1] - parts.place[p.batch]) >> 5;
-        return true;
     }
     __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
     {
@@ -396,43 +391,33 @@ struct WeightJob {
     {
         return b + (int64_t)(p.n0 + r < d_in ? p.n0 + r : d_in - 1) * pitch + (int64_t)parts.place[p.batch] * 4;
     }
-    __device__ __forceinline__ void piece(const TilePos& p, int mb, int nb, float* s, int lane) const
+    __device__ __forceinline__ void rows(const TilePos& p, int mb, int nb, const float* s, int it, int lane) const
     {
-        const int run = (lane & 7) * 8, c = nb + run;
+        const int run = (lane & 7) * 8, c = nb + run, r = it * 8 + (lane >> 3), row = mb + r;
+        if (row >= 2 * d_ff || c >= d_in) return;
+        float v[8];
+        piece_row8(s, r, run, v);
+        float* o = (row < d_ff ? gate + (int64_t)row * d_in : up + (int64_t)(row - d_ff) * d_in) + p.batch * ldg + c;
+        if (d_in - c >= 8 && aligned16(o)) {
+            reinterpret_cast<tile_f32x4*>(o)[0] = tile_f32x4{v[0], v[1], v[2], v[3]};
+            reinterpret_cast<tile_f32x4*>(o)[1] = tile_f32x4{v[4], v[5], v[6], v[7]};
+        } else {
 #pragma unroll
-        for (int it = 0; it < 8; ++it) {
-            const int r = it * 8 + (lane >> 3), row = mb + r;
-            if (row >= 2 * d_ff || c >= d_in) continue;
-            float v[8];
-            piece_row8(s, r, run, v);
-            float* o = (row < d_ff ? gate + (int64_t)row * d_in : up + (int64_t)(row - d_ff) * d_in) + p.batch * ldg + c;
-            if (d_in - c >= 8 && aligned16(o)) {
-                reinterpret_cast<tile_f32x4*>(o)[0] = tile_f32x4{v[0], v[1], v[2], v[3]};
-                reinterpret_cast<tile_f32x4*>(o)[1] = tile_f32x4{v[4], v[5], v[6], v[7]};
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (c + e < d_in) o[e] = v[e];
-            }
+            for (int e = 0; e < 8; ++e)
+                if (c + e < d_in) o[e] = v[e];
         }
     }
 };
 
-// 256 x 256 tiles where they fill the 256 compute units about as well as 128 x 128 tiles do, two of which share one
 template <class JOB>
-hipError_t launch_product(JOB j, int batch, int64_t m, int64_t n, hipStream_t stream)
+hipError_t launch_product(JOB j, int batch, int64_t m, int64_t n, int64_t steps, hipStream_t stream)
 {
-    const int64_t bm = (m + 255) / 256, bn = (n + 255) / 256, sm = (m + 127) / 128, sn = (n + 127) / 128;
-    const bool big = (batch * bm * bn + 255) / 256 * 4 <= (batch * sm * sn + 511) / 512 * 2;
-    const int64_t total = batch * (big ? bm * bn : sm * sn);
-    if (total > INT32_MAX) return hipErrorInvalidConfiguration;
-    j.side_m = j.side_n = big ? 256 : 128;
-    j.mt = (int)(big ? bm : sm);
-    j.nt = (int)(big ? bn : sn);
-    j.total = (int)total;
-    if (big) hipLaunchKernelGGL((k_tile<JOB, 256, 256, 2, 4>), dim3(j.total), dim3(512), 0, stream, j);
-    else hipLaunchKernelGGL((k_tile<JOB, 128, 128, 2, 2>), dim3(j.total), dim3(256), 0, stream, j);
-    return hipGetLastError();
+    const TileChoice c = choose_tile(batch, m, n, steps, false);
+    j.side = c.side;
+    j.mt = (int)c.mt;
+    j.nt = (int)c.nt;
+    j.total = (int)c.total;
+    return launch_tiles(j, c, stream);
 }
 
 struct Rows {
@@ -506,9 +491,9 @@ hipError_t launch_gated_forward(const GatedCall& c, hipStream_t stream)
     if (e != hipSuccess) return e;
     GateJob<false> j{};
     j.x = x.p, j.ldx = x.ld, j.wg = wg.p, j.ldg = wg.ld, j.wu = wu.p, j.ldu = wu.ld;
-    j.rows = (int)c.tokens, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act;
+    j.n_rows = (int)c.tokens, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act;
     j.h = static_cast<uint16_t*>(c.h), j.ldh = c.ldh;
-    return launch_product(j, 1, c.tokens, round_up(c.d_ff, 16) * 2, stream);
+    return launch_product(j, 1, c.tokens, round_up(c.d_ff, 16) * 2, j.steps, stream);
 }
 
 hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
@@ -544,10 +529,10 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         if (e != hipSuccess) return e;
         GateJob<true> j{};
         j.x = x.p, j.ldx = x.ld, j.wg = wg.p, j.ldg = wg.ld, j.wu = wu.p, j.ldu = wu.ld;
-        j.rows = places, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act, j.map = map;
+        j.n_rows = places, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act, j.map = map;
         j.dh = static_cast<const uint16_t*>(c.dh), j.lddh = c.lddh;
         j.by_token = by_token, j.fp = (int)fp, j.by_feature = by_feature, j.pitch = pitch;
-        e = launch_product(j, 1, places, fp * 2, stream);
+        e = launch_product(j, 1, places, fp * 2, j.steps, stream);
         if (e != hipSuccess) return e;
         const unsigned across = (c.d_in + 63) / 64;
         if (c.dx) {
@@ -561,7 +546,7 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
             e = hipGetLastError();
             if (e != hipSuccess) return e;
             InputJob d{by_token, w_turned, fp * 4, places, c.d_in, (int)(fp / 32), map, static_cast<uint16_t*>(c.dx), c.lddx};
-            e = launch_product(d, 1, places, c.d_in, stream);
+            e = launch_product(d, 1, places, c.d_in, d.steps, stream);
             if (e != hipSuccess) return e;
         }
         hipLaunchKernelGGL((k_turn<true>), dim3((places + 63) / 64, across), dim3(kBlock), 0, stream,
@@ -572,7 +557,7 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
     WeightJob w{};
     w.a = by_feature, w.b = x_turned, w.pitch = pitch, w.d_ff = c.d_ff, w.d_in = c.d_in;
     w.gate = c.g_gate, w.up = c.g_up, w.ldg = c.ldg, w.parts = parts;
-    return launch_product(w, c.k_parts, 2 * (int64_t)c.d_ff, c.d_in, stream);
+    return launch_product(w, c.k_parts, 2 * (int64_t)c.d_ff, c.d_in, places / 32 / c.k_parts, stream);
 }
 
 }  // namespace agc

@@ -151,6 +151,8 @@ __global__ __launch_bounds__(kSumBlock) void k_muon_start(const MuonCall c, Muon
 // A = X X^T, or B = a I + b A + c A A: symmetric, from rows of one matrix; tiles of the lower triangle.
 struct SymJob {
     static constexpr TilePair kPair = kSplit;
+    static constexpr int kRowParts = 8;
+    static constexpr bool kTurned = true;
     const char* src;          // X along n, or A
     char* dst;                // A or B
     int64_t pitch, size;      // of src
@@ -158,14 +160,13 @@ struct SymJob {
     int m, steps, tiles, side, total;   // tiles of one matrix, tile edge, of all
     int poly;
 
-    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    __device__ __forceinline__ void place(int id, TilePos& p) const
     {
         const int t = xcd_order(id, total);
         p.batch = t / tiles;
         int mi, ni;
         triangle_order(t - p.batch * tiles, mi, ni);
         p.m0 = mi * side, p.n0 = ni * side, p.steps = steps;
-        return true;
     }
     __device__ __forceinline__ const char* row(const TilePos& p, int r) const
     {
@@ -173,46 +174,42 @@ struct SymJob {
     }
     __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const { return row(p, p.m0 + r); }
     __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const { return row(p, p.n0 + r); }
-    __device__ __forceinline__ void piece(const TilePos& p, int mb, int nb, float* s, int lane) const
+    // a tile on the diagonal holds both halves
+    __device__ __forceinline__ bool turned(const TilePos& p) const { return p.m0 != p.n0; }
+    __device__ __forceinline__ void rows(const TilePos& p, int mb, int nb, float* s, int it, int lane) const
     {
-        char* out = dst + p.batch * size_dst;
-        const int up = (int)(pitch_dst / 4), sub = lane >> 3, run = (lane & 7) * 8;
+        const int up = (int)(pitch_dst / 4), run = (lane & 7) * 8;
+        const int r = it * 8 + (lane >> 3), gr = mb + r, gc = nb + run;
+        float v[8];
+        piece_row8(s, r, run, v);
+        if (poly) {
+            float a[8];
 #pragma unroll
-        for (int it = 0; it < 8; ++it) {
-            const int r = it * 8 + sub, gr = mb + r, gc = nb + run;
-            float v[8];
-            piece_row8(s, r, run, v);
-            if (poly) {
-                float a[8];
+            for (int e = 0; e < 8; ++e) a[e] = 0.0f;
+            if (gr < m && gc < up) split_load8(src + p.batch * size + (int64_t)gr * pitch, gc, a);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = 0.0f;
-                if (gr < m && gc < up) split_load8(src + p.batch * size + (int64_t)gr * pitch, gc, a);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    // units: sums 2^28, A 2^14, B 2^13
-                    float b = fmaf(kNsC * (kUnitB / (kUnitA * kUnitA)), v[e], kNsB * (kUnitB / kUnitA) * a[e]);
-                    if (gr == gc + e) b += kNsA * kUnitB;
-                    v[e] = b;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= kUnitA / (kUnitX * kUnitX);
+            for (int e = 0; e < 8; ++e) {
+                // units: sums 2^28, A 2^14, B 2^13
+                float b = fmaf(kNsC * (kUnitB / (kUnitA * kUnitA)), v[e], kNsB * (kUnitB / kUnitA) * a[e]);
+                if (gr == gc + e) b += kNsA * kUnitB;
+                v[e] = b;
             }
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (gr >= m || gc + e >= m) v[e] = 0.0f;
-            if (gr < m && gc < up) split_store8(out + (int64_t)gr * pitch_dst, gc, v);
-            piece_put_row8(s, r, run, v);
+            for (int e = 0; e < 8; ++e) v[e] *= kUnitA / (kUnitX * kUnitX);
         }
-        if (p.m0 == p.n0) return;   // a tile on the diagonal holds both halves
-        wave_lds_fence();
 #pragma unroll
-        for (int it = 0; it < 8; ++it) {
-            const int cc = it * 8 + sub, gc = nb + cc, gr = mb + run;
-            float v[8];
-            piece_col8(s, run, cc, v);
-            if (gc < m && gr < up) split_store8(out + (int64_t)gc * pitch_dst, gr, v);
-        }
+        for (int e = 0; e < 8; ++e)
+            if (gr >= m || gc + e >= m) v[e] = 0.0f;
+        if (gr < m && gc < up) split_store8(dst + p.batch * size_dst + (int64_t)gr * pitch_dst, gc, v);
+        piece_put_row8(s, r, run, v);
+    }
+    __device__ __forceinline__ void cols(const TilePos& p, int mb, int nb, const float* s, int it, int lane) const
+    {
+        const int run = (lane & 7) * 8, cc = it * 8 + (lane >> 3), gc = nb + cc, gr = mb + run;
+        float v[8];
+        piece_col8(s, run, cc, v);
+        if (gc < m && gr < (int)(pitch_dst / 4)) split_store8(dst + p.batch * size_dst + (int64_t)gc * pitch_dst, gr, v);
     }
 };
 
@@ -220,22 +217,23 @@ struct SymJob {
 template <bool LAST>
 struct ApplyJob {
     static constexpr TilePair kPair = kSplit;
+    static constexpr int kRowParts = 8;
+    static constexpr bool kTurned = true;
     const char* b;           // m x m
     const char* xt;          // X along m: n rows
     char* out_x;             // along n
     char* out_t;             // along m
     MuonGeom g;
-    int mt, nt, side_m, side_n, total;
+    int mt, nt, side, total;
     MuonCall call;           // of the last step
 
-    __device__ __forceinline__ bool place(int id, TilePos& p) const
+    __device__ __forceinline__ void place(int id, TilePos& p) const
     {
         const int t = xcd_order(id, total);
         p.batch = t / (mt * nt);
         int mi, ni;
         tile_order(t - p.batch * mt * nt, mt, nt, mi, ni);
-        p.m0 = mi * side_m, p.n0 = ni * side_n, p.steps = (int)(g.pitch_m / 128);
-        return true;
+        p.m0 = mi * side, p.n0 = ni * side, p.steps = (int)(g.pitch_m / 128);
     }
     __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
     {
@@ -279,47 +277,36 @@ struct ApplyJob {
             }
         }
     }
-    __device__ __forceinline__ void piece(const TilePos& p, int mb, int nb, float* s, int lane) const
+    // the last step goes along the rows of the matrix as it lies
+    __device__ __forceinline__ bool turned(const TilePos&) const { return !LAST || g.tall; }
+    __device__ __forceinline__ void rows(const TilePos& p, int mb, int nb, float* s, int it, int lane) const
     {
-        const int sub = lane >> 3, run = (lane & 7) * 8;
-        const int up_n = (int)(g.pitch_n / 4), up_m = (int)(g.pitch_m / 4);
+        const int run = (lane & 7) * 8, gr = mb + it * 8 + (lane >> 3), gc = nb + run;
+        float v[8];
         if (LAST) {
-            const int64_t off = call.offset[p.batch];
-#pragma unroll
-            for (int it = 0; it < 8; ++it) {
-                float v[8];
-                if (!g.tall) {
-                    const int gr = mb + it * 8 + sub, gc = nb + run;
-                    piece_row8(s, it * 8 + sub, run, v);
-                    if (gr < g.m && gc < g.n) update(off + (int64_t)gr * g.n + gc, g.n - gc < 8 ? g.n - gc : 8, v);
-                } else {
-                    const int gc = nb + it * 8 + sub, gr = mb + run;
-                    piece_col8(s, run, it * 8 + sub, v);
-                    if (gc < g.n && gr < g.m) update(off + (int64_t)gc * g.m + gr, g.m - gr < 8 ? g.m - gr : 8, v);
-                }
-            }
+            if (g.tall || gr >= g.m || gc >= g.n) return;
+            piece_row8(s, it * 8 + (lane >> 3), run, v);
+            update(call.offset[p.batch] + (int64_t)gr * g.n + gc, g.n - gc < 8 ? g.n - gc : 8, v);
             return;
         }
-        char* ox = out_x + p.batch * g.size_x;
-        char* ot = out_t + p.batch * g.size_t;
+        piece_row8(s, it * 8 + (lane >> 3), run, v);
 #pragma unroll
-        for (int it = 0; it < 8; ++it) {
-            const int gr = mb + it * 8 + sub, gc = nb + run;
-            float v[8];
-            piece_row8(s, it * 8 + sub, run, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = gc + e < g.n ? v[e] * (1.0f / kUnitB) : 0.0f;
-            if (gr < g.m && gc < up_n) split_store8(ox + (int64_t)gr * g.pitch_n, gc, v);
+        for (int e = 0; e < 8; ++e) v[e] = gc + e < g.n ? v[e] * (1.0f / kUnitB) : 0.0f;
+        if (gr < g.m && gc < (int)(g.pitch_n / 4)) split_store8(out_x + p.batch * g.size_x + (int64_t)gr * g.pitch_n, gc, v);
+    }
+    __device__ __forceinline__ void cols(const TilePos& p, int mb, int nb, const float* s, int it, int lane) const
+    {
+        const int run = (lane & 7) * 8, gc = nb + it * 8 + (lane >> 3), gr = mb + run;
+        float v[8];
+        piece_col8(s, run, it * 8 + (lane >> 3), v);
+        if (LAST) {
+            if (gc < g.n && gr < g.m)
+                update(call.offset[p.batch] + (int64_t)gc * g.m + gr, g.m - gr < 8 ? g.m - gr : 8, v);
+            return;
         }
 #pragma unroll
-        for (int it = 0; it < 8; ++it) {
-            const int gc = nb + it * 8 + sub, gr = mb + run;
-            float v[8];
-            piece_col8(s, run, it * 8 + sub, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = gr + e < g.m ? v[e] * (1.0f / kUnitB) : 0.0f;
-            if (gc < g.n && gr < up_m) split_store8(ot + (int64_t)gc * g.pitch_m, gr, v);
-        }
+        for (int e = 0; e < 8; ++e) v[e] = gr + e < g.m ? v[e] * (1.0f / kUnitB) : 0.0f;
+        if (gc < g.n && gr < (int)(g.pitch_m / 4)) split_store8(out_t + p.batch * g.size_t + (int64_t)gc * g.pitch_m, gr, v);
     }
 };
 
@@ -521,30 +508,22 @@ __global__ __launch_bounds__(FORM::kThreads) void k_muon_small(const MuonCall c,
 
 hipError_t launch_sym(SymJob j, int mats, hipStream_t stream)
 {
-    const int big = (j.m + 255) / 256, small = (j.m + 127) / 128;
-    const int64_t tiles_big = (int64_t)mats * big * (big + 1) / 2, tiles_small = (int64_t)mats * small * (small + 1) / 2;
-    const bool use_big = (tiles_big + 255) / 256 * 4 <= (tiles_small + 511) / 512 * 2;
-    j.side = use_big ? 256 : 128;
-    const int across = use_big ? big : small;
-    j.tiles = across * (across + 1) / 2;
-    j.total = mats * j.tiles;
-    if (use_big) hipLaunchKernelGGL((k_tile<SymJob, 256, 256, 2, 4>), dim3(j.total), dim3(512), 0, stream, j);
-    else hipLaunchKernelGGL((k_tile<SymJob, 128, 128, 2, 2>), dim3(j.total), dim3(256), 0, stream, j);
-    return hipGetLastError();
+    const TileChoice c = choose_tile(mats, j.m, j.m, j.steps, true);
+    j.side = c.side;
+    j.tiles = (int)(c.total / mats);
+    j.total = (int)c.total;
+    return launch_tiles(j, c, stream);
 }
 
 template <bool LAST>
 hipError_t launch_apply(ApplyJob<LAST> j, hipStream_t stream)
 {
-    const int64_t bm = (j.g.m + 255) / 256, bn = (j.g.n + 255) / 256, sm = (j.g.m + 127) / 128, sn = (j.g.n + 127) / 128;
-    const bool use_big = (j.g.mats * bm * bn + 255) / 256 * 4 <= (j.g.mats * sm * sn + 511) / 512 * 2;
-    j.side_m = j.side_n = use_big ? 256 : 128;
-    j.mt = (int)(use_big ? bm : sm);
-    j.nt = (int)(use_big ? bn : sn);
-    j.total = j.g.mats * j.mt * j.nt;
-    if (use_big) hipLaunchKernelGGL((k_tile<ApplyJob<LAST>, 256, 256, 2, 4>), dim3(j.total), dim3(512), 0, stream, j);
-    else hipLaunchKernelGGL((k_tile<ApplyJob<LAST>, 128, 128, 2, 2>), dim3(j.total), dim3(256), 0, stream, j);
-    return hipGetLastError();
+    const TileChoice c = choose_tile(j.g.mats, j.g.m, j.g.n, j.g.pitch_m / 128, false);
+    j.side = c.side;
+    j.mt = (int)c.mt;
+    j.nt = (int)c.nt;
+    j.total = (int)c.total;
+    return launch_tiles(j, c, stream);
 }
 
 }  // namespace
@@ -596,8 +575,8 @@ hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
         SymJob poly{a, b, g.pitch_m, g.size_a, g.pitch_m, g.size_a, g.m, (int)(g.pitch_m / 128), 0, 0, 0, 1};
         e = launch_sym(poly, c.n_mats, stream);
         if (e != hipSuccess) return e;
-        if (s + 1 < c.steps) e = launch_apply(ApplyJob<false>{b, t[in], x[out], t[out], g, 0, 0, 0, 0, 0, c}, stream);
-        else e = launch_apply(ApplyJob<true>{b, t[in], nullptr, nullptr, g, 0, 0, 0, 0, 0, c}, stream);
+        if (s + 1 < c.steps) e = launch_apply(ApplyJob<false>{b, t[in], x[out], t[out], g, 0, 0, 0, 0, c}, stream);
+        else e = launch_apply(ApplyJob<true>{b, t[in], nullptr, nullptr, g, 0, 0, 0, 0, c}, stream);
     }
     return e;
 }

@@ -165,11 +165,12 @@ __device__ __forceinline__ void load16_to_lds(const char* src, char* dst)
                                      (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
-// JOB: kPair; bool place(int id, TilePos&); const char* a_row(pos, r), b_row(pos, r): where row r of the tile starts
-// (rows past the matrix name a row inside it; their results are not used); void piece(pos, m, n, float* s, lane): what
-// becomes of the 64 x 64 values staged at s, the first of them C[m, n].
+// JOB: kPair; void place(int id, TilePos&); const char* a_row(pos, r), b_row(pos, r): where row r of the tile starts
+// (rows past the matrix name a row inside it; their results are not used); rows(pos, m, n, float* s, it, lane): what
+// becomes of part `it` of kRowParts, along rows, of the 64 x 64 values staged at s, the first of them C[m, n]; and,
+// where kTurned and turned(pos), cols(...): the same of eight parts along columns, after all rows().
 template <class JOB, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64, (TM == 256 && TN == 256) ? 2 : 2) void k_tile(const JOB job)
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_tile(const JOB job)
 {
     constexpr int kThreads = WM * WN * 64;
     constexpr int kWaveM = TM / WM, kWaveN = TN / WN, kFm = kWaveM / 16, kFn = kWaveN / 16;
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(WM * WN * 64, (TM == 256 && TN == 256) ? 2 : 2) voi
     __shared__ __attribute__((aligned(1024))) char lds[kLds];
 
     TilePos pos;
-    if (!job.place((int)blockIdx.x, pos)) return;
+    job.place((int)blockIdx.x, pos);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave - wm * WN;
@@ -260,9 +261,150 @@ __global__ __launch_bounds__(WM * WN * 64, (TM == 256 && TN == 256) ? 2 : 2) voi
                 for (int e = 0; e < 4; ++e)
                     mine[piece_at(i * 16 + q * 4 + e, j * 16 + (lane & 15))] = acc[p * 4 + i][j][e];
         wave_lds_fence();
-        job.piece(pos, pos.m0 + wm * kWaveM + p * 64, pos.n0 + wn * 64, mine, lane);
+        const int m = pos.m0 + wm * kWaveM + p * 64, n = pos.n0 + wn * 64;
+#pragma unroll
+        for (int it = 0; it < JOB::kRowParts; ++it) job.rows(pos, m, n, mine, it, lane);
+        if constexpr (JOB::kTurned) {
+            wave_lds_fence();
+            if (job.turned(pos)) {
+#pragma unroll
+                for (int it = 0; it < 8; ++it) job.cols(pos, m, n, mine, it, lane);
+            }
+        }
         wave_lds_fence();
     }
+}
+
+// The same product where there are few tiles: 64 x 64 tiles whose sum is cut among the four waves of a workgroup, every
+// fourth k-step each.  A wave fills and reads LDS of its own, so nothing waits for anybody before the end, where the
+// four parts are added in order.
+template <class JOB>
+__global__ __launch_bounds__(256, 1) void k_tile_cut(const JOB job)
+{
+    constexpr int kStep = 128 * 128;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * kStep];
+    TilePos pos;
+    job.place((int)blockIdx.x, pos);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    char* mine = lds + wave * 2 * kStep;
+
+    const char *src_a[8], *src_b[8];
+    const int chunk = ((lane & 7) ^ (lane >> 3)) * 16 + wave * 128;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        src_a[i] = job.a_row(pos, i * 8 + (lane >> 3)) + chunk;
+        src_b[i] = job.b_row(pos, i * 8 + (lane >> 3)) + chunk;
+    }
+    auto issue = [&](char* base) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            load16_to_lds(src_a[i], base + i * 1024);
+            load16_to_lds(src_b[i], base + 8192 + i * 1024);
+            src_a[i] += 512, src_b[i] += 512;
+        }
+    };
+    tile_f32x4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = tile_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int row = (lane & 15) * 128, q = lane >> 4;
+    const int at0 = row + ((q ^ (lane & 7)) << 4), at1 = row + (((4 + q) ^ (lane & 7)) << 4);
+
+    if (wave < pos.steps) issue(mine);
+    for (int k = wave, half = 0; k < pos.steps; k += 4, half ^= 1) {
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other half has been read
+        if (k + 4 < pos.steps) {
+            issue(mine + (half ^ 1) * kStep);
+            __asm__ volatile("s_waitcnt vmcnt(16)" ::: "memory");   // all but the sixteen loads just issued
+        } else {
+            __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        const char *a = mine + half * kStep, *b = a + 8192;
+        tile_u32x4 b0[4], b1[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            b0[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at0);
+            b1[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at1);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const tile_u32x4 a0 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at0);
+            const tile_u32x4 a1 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                acc[i][j] = tile_mfma<JOB::kPair>(a0, b0[j], acc[i][j]);
+                if constexpr (JOB::kPair == kPlain) {
+                    acc[i][j] = tile_mfma<JOB::kPair>(a1, b1[j], acc[i][j]);
+                } else {
+                    acc[i][j] = tile_mfma<JOB::kPair>(a0, b1[j], acc[i][j]);
+                    acc[i][j] = tile_mfma<JOB::kPair>(a1, b0[j], acc[i][j]);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                part[wave * 4096 + piece_at(i * 16 + q * 4 + e, j * 16 + (lane & 15))] = acc[i][j][e];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        tile_f32x4* p = reinterpret_cast<tile_f32x4*>(part) + i * 256 + tid;
+        p[0] = (p[0] + p[1024]) + (p[2048] + p[3072]);
+    }
+    __syncthreads();
+    for (int it = wave; it < JOB::kRowParts; it += 4) job.rows(pos, pos.m0, pos.n0, part, it, lane);
+    if constexpr (JOB::kTurned) {
+        __syncthreads();
+        if (job.turned(pos)) {
+            for (int it = wave; it < 8; it += 4) job.cols(pos, pos.m0, pos.n0, part, it, lane);
+        }
+    }
+}
+
+// Which of the three a product of `batch` matrices of m x n, `steps` k-steps each, takes, and how many tiles that are.
+// The estimates are rounds of workgroups times microseconds of a k-step and of an end, as measured at 16 to 350 steps.
+struct TileChoice {
+    int side;        // 256, 128, or 64: the cut form
+    int64_t mt, nt;  // tiles along m and n
+    int64_t total;
+};
+
+inline TileChoice choose_tile(int64_t batch, int64_t m, int64_t n, int64_t steps, bool triangle)
+{
+    TileChoice best{};
+    double least = 0.0;
+    for (int side = 256; side >= 64; side /= 2) {
+        TileChoice c{side, (m + side - 1) / side, (n + side - 1) / side, 0};
+        c.total = batch * (triangle ? c.mt * (c.mt + 1) / 2 : c.mt * c.nt);
+        const double s = (double)steps, t = (double)c.total;
+        const double slots = side == 128 ? 512.0 : 256.0;
+        const double rounds = (double)((c.total + (int64_t)slots - 1) / (int64_t)slots);
+        double us;
+        if (side == 256) us = rounds * (2.3 * s + 15.0);
+        else if (side == 128) us = rounds * ((t > 256.0 ? 1.4 : 0.9) * s + 8.0);
+        else us = rounds * (0.3 * s + 5.0);
+        if (side == 256 || us < least) best = c, least = us;
+    }
+    return best;
+}
+
+template <class JOB>
+hipError_t launch_tiles(JOB& j, const TileChoice& c, hipStream_t stream)
+{
+    if (c.total > INT32_MAX) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)c.total);
+    if (c.side == 256) hipLaunchKernelGGL((k_tile<JOB, 256, 256, 2, 4>), grid, dim3(512), 0, stream, j);
+    else if (c.side == 128) hipLaunchKernelGGL((k_tile<JOB, 128, 128, 2, 2>), grid, dim3(256), 0, stream, j);
+    else hipLaunchKernelGGL(k_tile_cut<JOB>, grid, dim3(256), 0, stream, j);
+    return hipGetLastError();
 }
 
 }  // namespace agc

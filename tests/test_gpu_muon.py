@@ -79,6 +79,36 @@ def test_orthogonal_factor(rows, cols, mats):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(96, 100), (33, 255), (570, 20), (65, 110), (97, 97), (1, 600), (1030, 3)])
+def test_orthogonal_factor_round_the_limits_of_one_launch(rows, cols):
+    got, want, m1, want_m1, at = run(rows, cols, 2, gap=1, seed=rows + cols)
+    for here in at:
+        assert off_by(got[here], want[here]) < 1e-5
+        assert np.array_equal(m1[here], want_m1[here].astype(np.float32))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,mats", [(1300, 1290, 2), (1025, 3001, 5), (4097, 2050, 4)])
+def test_orthogonal_factor_of_large_matrices(rows, cols, mats):
+    """Every tile size and its edges; the 64-bit products are taken on the GPU."""
+    import torch
+    size = rows * cols
+    g = torch.randn(mats * size, device="cuda", generator=torch.Generator("cuda").manual_seed(rows))
+    beta, m1 = torch.zeros_like(g), torch.zeros_like(g)
+    ws = torch.full((api.agc_muon_workspace_bytes(rows, cols, mats),), 0xFF, dtype=torch.uint8, device="cuda")
+    api.agc_muon_update(beta, m1, g, [i * size for i in range(mats)], rows, cols, 1.0, 0.0, False, 0.0, 1.0, 5, ws)
+    for i in (0, mats - 1):
+        u = g[i * size:(i + 1) * size].double().view(rows, cols)
+        x = u.t() if rows > cols else u
+        x = (x / (x.norm() + 1e-7)).contiguous()
+        for _ in range(5):
+            gram = x @ x.t()
+            x = A * x + (B * gram + C * (gram @ gram)) @ x
+        x = (x.t() if rows > cols else x).reshape(-1)
+        assert float((beta[i * size:(i + 1) * size].double() + x).norm() / x.norm()) < 1e-5
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,cols", [(70, 200), (200, 70), (300, 300)])
 @pytest.mark.parametrize("nesterov,decay,copy,lead", [(True, 0.1, True, 0), (False, 0.0, True, 2), (True, 0.0, False, 4)])
 def test_whole_update(rows, cols, nesterov, decay, copy, lead):
