@@ -170,16 +170,6 @@ def load():
     return L
 
 
-def _bfloat16():
-    import torch
-    return torch.bfloat16
-
-
-def _float32():
-    import torch
-    return torch.float32
-
-
 def _np(a, dtype):
     return np.ascontiguousarray(a, dtype=dtype)
 
@@ -308,10 +298,13 @@ def _check_streams(codes, bits, d):
 
 
 def _stream_handle(stream):
-    if stream is None:
-        import torch
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
-    return C.c_void_p(int(stream))
+    if stream is not None:
+        return C.c_void_p(int(stream))
+    import torch
+    # the current stream's handle without an object round it, which takes 3 us where the rest of a small call takes 6
+    if torch.cuda.is_initialized() and hasattr(torch._C, "_cuda_getCurrentRawStream"):
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
 class Context:
@@ -502,21 +495,21 @@ def agc_adam_update(beta, m1, m2, ghat, ghat2, lr, beta1, beta2, eps, t, stream=
         raise AgcError(st, "agc_adam_update")
 
 
-_ACTS = {"silu": AGC_ACT_SILU, "gelu": AGC_ACT_GELU}
-
-
 def _rows_of(t, rows, cols, dtype, what):
     """Row stride of a (rows, cols) row-major view; AGC_ESHAPE if it is none, or smaller, or of another type."""
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or t.dtype != dtype or (cols > 1 and t.stride(1) != 1):
-        raise AgcError(AGC_ESHAPE, f"{what} must be a ({rows}, {cols}) row-major view of {dtype}, got "
-                                   f"{tuple(t.shape)} of {t.dtype}")
-    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    shape = t.shape
+    if len(shape) == 2 and shape[0] >= rows and shape[1] == cols and t.dtype is dtype:
+        ld, step = t.stride()
+        if step == 1 or cols == 1:
+            return ld if rows > 1 else max(cols, ld)
+    raise AgcError(AGC_ESHAPE, f"{what} must be a ({rows}, {cols}) row-major view of {dtype}, got {tuple(shape)} of {t.dtype}")
 
 
 def _type_of(t, what):
-    if t.dtype == _float32():
+    import torch
+    if t.dtype is torch.float32:
         return AGC_TYPE_F32
-    if t.dtype == _bfloat16():
+    if t.dtype is torch.bfloat16:
         return AGC_TYPE_BF16
     raise AgcError(AGC_EINVAL, f"{what} must be float32 or bfloat16, got {t.dtype}")
 
@@ -558,8 +551,9 @@ def agc_embed_partial_gradients(dout, tokens, part_end, vocab, scale, G, workspa
         raise AgcError(AGC_ESHAPE, "dout must be (tokens, dim)")
     dim = dout.shape[1]
     ldd = _rows_of(dout, n, dim, dout.dtype, "dout")
-    ldg = _rows_of(G, k, vocab * dim, _float32(), "G")
-    if workspace.numel() * workspace.element_size() < L.agc_embed_workspace_bytes(n, vocab, dim, k):
+    import torch
+    ldg = _rows_of(G, k, vocab * dim, torch.float32, "G")
+    if workspace.nbytes < L.agc_embed_workspace_bytes(n, vocab, dim, k):
         raise AgcError(AGC_ESHAPE, "agc_embed_partial_gradients: the workspace is too small")
     st = L.agc_embed_partial_gradients(dout.data_ptr(), kind, ldd, tokens.data_ptr(), width, n,
                                        struct.pack(f"{k}q", *[int(e) for e in part_end]), k, vocab, dim, scale,
@@ -567,6 +561,24 @@ def agc_embed_partial_gradients(dout, tokens, part_end, vocab, scale, G, workspa
     if check and st != AGC_OK:
         raise AgcError(st, L.agc_last_error(None).decode())
     return st
+
+
+_ACTS = {"silu": AGC_ACT_SILU, "gelu": AGC_ACT_GELU}
+
+
+def _gated_operands(x, w_gate, w_up, workspace, k):
+    """(tokens, d_in, d_ff, ldx, ldw) of the block's operands, which are bfloat16."""
+    import torch
+    bf16 = torch.bfloat16
+    if x.dim() != 2 or w_gate.dim() != 2:
+        raise AgcError(AGC_ESHAPE, "x and the weights are matrices")
+    (tokens, d_in), d_ff = x.shape, w_gate.shape[0]
+    ldw = _rows_of(w_gate, d_ff, d_in, bf16, "w_gate")
+    if _rows_of(w_up, d_ff, d_in, bf16, "w_up") != ldw:
+        raise AgcError(AGC_ESHAPE, "w_gate and w_up must have one row stride")
+    if workspace.nbytes < _lib.agc_gated_workspace_bytes(tokens, d_in, d_ff, k):
+        raise AgcError(AGC_ESHAPE, "the workspace is too small")
+    return tokens, d_in, d_ff, _rows_of(x, tokens, d_in, bf16, "x"), ldw
 
 
 def agc_gated_workspace_bytes(n_tokens, d_in, d_ff, k_parts=0):
@@ -577,13 +589,8 @@ def agc_gated_workspace_bytes(n_tokens, d_in, d_ff, k_parts=0):
 def agc_gated_forward(x, w_gate, w_up, act, h, workspace, stream=None, check=True):
     """h = act(x w_gate^T) * (x w_up^T), all bfloat16; x (tokens, d_in), weights (d_ff, d_in), h (tokens, d_ff)."""
     L = load()
-    (tokens, d_in), d_ff, bf16 = x.shape, w_gate.shape[0], w_gate.dtype
-    ldw = _rows_of(w_gate, d_ff, d_in, _bfloat16(), "w_gate")
-    if _rows_of(w_up, d_ff, d_in, bf16, "w_up") != ldw:
-        raise AgcError(AGC_ESHAPE, "w_gate and w_up must have one row stride")
-    ldx, ldh = _rows_of(x, tokens, d_in, bf16, "x"), _rows_of(h, tokens, d_ff, bf16, "h")
-    if workspace.numel() * workspace.element_size() < L.agc_gated_workspace_bytes(tokens, d_in, d_ff, 0):
-        raise AgcError(AGC_ESHAPE, "agc_gated_forward: the workspace is too small")
+    tokens, d_in, d_ff, ldx, ldw = _gated_operands(x, w_gate, w_up, workspace, 0)
+    ldh = _rows_of(h, tokens, d_ff, x.dtype, "h")
     st = L.agc_gated_forward(x.data_ptr(), ldx, w_gate.data_ptr(), w_up.data_ptr(), ldw, tokens, d_in, d_ff,
                              _ACTS.get(act, act), h.data_ptr(), ldh, workspace.data_ptr(), _stream_handle(stream))
     if check and st != AGC_OK:
@@ -594,19 +601,15 @@ def agc_gated_forward(x, w_gate, w_up, act, h, workspace, stream=None, check=Tru
 def agc_gated_partial_gradients(x, w_gate, w_up, act, dh, part_end, dx, G_gate, G_up, workspace, stream=None, check=True):
     """dx (bfloat16, or None) and, for each partition of the tokens, the gradients of both weights: G_gate and G_up are
     (k_parts, d_ff * d_in) float32 views of the same rows of G."""
+    import torch
     L = load()
-    (tokens, d_in), d_ff, bf16 = x.shape, w_gate.shape[0], w_gate.dtype
-    ldw = _rows_of(w_gate, d_ff, d_in, _bfloat16(), "w_gate")
-    if _rows_of(w_up, d_ff, d_in, bf16, "w_up") != ldw:
-        raise AgcError(AGC_ESHAPE, "w_gate and w_up must have one row stride")
-    ldx, lddh = _rows_of(x, tokens, d_in, bf16, "x"), _rows_of(dh, tokens, d_ff, bf16, "dh")
-    lddx = d_in if dx is None else _rows_of(dx, tokens, d_in, bf16, "dx")
     k = len(part_end)
-    ldg = _rows_of(G_gate, k, d_ff * d_in, _float32(), "G_gate")
-    if _rows_of(G_up, k, d_ff * d_in, _float32(), "G_up") != ldg:
+    tokens, d_in, d_ff, ldx, ldw = _gated_operands(x, w_gate, w_up, workspace, k)
+    lddh = _rows_of(dh, tokens, d_ff, x.dtype, "dh")
+    lddx = d_in if dx is None else _rows_of(dx, tokens, d_in, x.dtype, "dx")
+    ldg = _rows_of(G_gate, k, d_ff * d_in, torch.float32, "G_gate")
+    if _rows_of(G_up, k, d_ff * d_in, torch.float32, "G_up") != ldg:
         raise AgcError(AGC_ESHAPE, "G_gate and G_up must have one row stride")
-    if workspace.numel() * workspace.element_size() < L.agc_gated_workspace_bytes(tokens, d_in, d_ff, k):
-        raise AgcError(AGC_ESHAPE, "agc_gated_partial_gradients: the workspace is too small")
     st = L.agc_gated_partial_gradients(x.data_ptr(), ldx, w_gate.data_ptr(), w_up.data_ptr(), ldw, dh.data_ptr(), lddh,
                                        tokens, struct.pack(f"{k}q", *[int(e) for e in part_end]), k, d_in, d_ff,
                                        _ACTS.get(act, act), None if dx is None else dx.data_ptr(), lddx,
@@ -632,7 +635,7 @@ def agc_muon_update(beta, m1, ghat, offsets, rows, cols, lr, momentum, nesterov,
     for t, width in ((beta, 4), (m1, 4), (ghat, 4), (beta_bf16, 2)):
         if t is not None and (t.numel() < end or t.element_size() != width or not t.is_contiguous()):
             raise AgcError(AGC_ESHAPE, "agc_muon_update: a vector is smaller than the matrices reach, or of another type")
-    if workspace.numel() * workspace.element_size() < L.agc_muon_workspace_bytes(rows, cols, len(off)):
+    if workspace.nbytes < L.agc_muon_workspace_bytes(rows, cols, len(off)):
         raise AgcError(AGC_ESHAPE, "agc_muon_update: the workspace is too small")
     st = L.agc_muon_update(beta.data_ptr(), m1.data_ptr(), ghat.data_ptr(), struct.pack(f"{len(off)}q", *off), len(off),
                            rows, cols, lr, momentum, int(bool(nesterov)), weight_decay, scale, steps,
