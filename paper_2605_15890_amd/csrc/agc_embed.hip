@@ -6,7 +6,7 @@
 // put in order of (partition, id) by a radix sort that keeps equal keys in place; a row's tokens are then one run of the
 // order, found by searching it, and are summed by whoever writes the row: no atomics on values, no clearing before.
 // Rows with long runs (few ids, or the commonest one) would leave one wave with all the work: runs are first summed in
-// pieces of 64 places of the order and those in pieces of 32, so that a row of n tokens takes about n / 2048 + 190 steps.
+// pieces of 64 places of the order and those in groups of 16, so that a row of n tokens takes about n / 1024 + 160 steps.
 #include "agc_operators.h"
 
 namespace agc {
@@ -14,10 +14,11 @@ namespace agc {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kDigitBits = 11, kDigits = 1 << kDigitBits;
-constexpr int kSortTile = 2048;    // keys of one workgroup in a pass of the sort
-constexpr int kPiece = 64;         // places of a first-level piece
-constexpr int kGroup = 32;         // pieces of a second-level piece
+constexpr int kMostBits = 11, kMostDigits = 1 << kMostBits;   // of a pass of the sort
+constexpr int kSortTile = 1024;    // keys of one workgroup in a pass
+constexpr int kFewTiles = 16;      // up to here a workgroup adds up the tiles' counts itself
+constexpr int kPiece = 64;         // places of a piece
+constexpr int kGroup = 16;         // pieces of a group
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -31,31 +32,31 @@ struct EmbedParts {
 __device__ __forceinline__ float from_bf16(uint32_t bits) { return __uint_as_float(bits << 16); }
 __device__ __forceinline__ uint32_t to_bf16(float v) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v); }
 
-// Four values from element c on of a row of T (float or bfloat16 bits); WHOLE: one aligned load, else element by
-// element below `width`.
+// Four values of a row of T (float or bfloat16 bits).  WHOLE: elements c .. c+3, one aligned load; else c + e * step, so
+// that the lanes of a wave stay side by side, and the last element of the row in place of those behind it.
 template <class T, bool WHOLE>
-__device__ __forceinline__ f32x4 load4(const T* row, int c, int width)
+__device__ __forceinline__ f32x4 load4(const T* row, int c, int step, int width)
 {
-    if constexpr (WHOLE && sizeof(T) == 4) return *reinterpret_cast<const f32x4*>(row + c);
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    if constexpr (WHOLE && sizeof(T) == 2) {
+    f32x4 v;
+    if constexpr (WHOLE && sizeof(T) == 4) {
+        v = *reinterpret_cast<const f32x4*>(row + c);
+    } else if constexpr (WHOLE) {
         const u32x2 u = *reinterpret_cast<const u32x2*>(row + c);
         v = f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
                   __uint_as_float(u.y & 0xFFFF0000u)};
-    }
-    if constexpr (!WHOLE) {
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < width) {
-                if constexpr (sizeof(T) == 4) v[e] = row[c + e];
-                else v[e] = from_bf16(row[c + e]);
-            }
+        for (int e = 0; e < 4; ++e) {
+            const int at = min(c + e * step, width - 1);
+            if constexpr (sizeof(T) == 4) v[e] = row[at];
+            else v[e] = from_bf16(row[at]);
+        }
     }
     return v;
 }
 
 template <class T, bool WHOLE>
-__device__ __forceinline__ void store4(T* row, int c, int width, const f32x4& v)
+__device__ __forceinline__ void store4(T* row, int c, int step, int width, const f32x4& v)
 {
     if constexpr (WHOLE && sizeof(T) == 4) {
         *reinterpret_cast<f32x4*>(row + c) = v;
@@ -64,9 +65,9 @@ __device__ __forceinline__ void store4(T* row, int c, int width, const f32x4& v)
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (c + e < width) {
-                if constexpr (sizeof(T) == 4) row[c + e] = v[e];
-                else row[c + e] = (T)to_bf16(v[e]);
+            if (c + e * step < width) {
+                if constexpr (sizeof(T) == 4) row[c + e * step] = v[e];
+                else row[c + e * step] = (T)to_bf16(v[e]);
             }
     }
 }
@@ -82,128 +83,170 @@ __global__ __launch_bounds__(kBlock) void k_embed(const TABLE* table, int64_t vo
         const int64_t id = (int64_t)tokens[t];
         const bool held = id >= 0 && id < vocab;
         const TABLE* row = table + (held ? id : 0) * dim;
-        for (int c = lane * 4; c < dim; c += lanes * 4) {
-            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (held) v = load4<TABLE, WHOLE>(row, c, dim) * scale;
-            store4<OUT, WHOLE>(out + t * ldo, c, dim, v);
+#pragma unroll 4
+        for (int c = WHOLE ? lane * 4 : lane; c < dim; c += lanes * 4) {
+            f32x4 v = load4<TABLE, WHOLE>(row, c, lanes, dim);   // of row 0 at an empty place
+            v = held ? v * scale : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            store4<OUT, WHOLE>(out + t * ldo, c, lanes, dim, v);
         }
     }
 }
 
 // ------------------------------------------------------------------ order of the tokens
+// Radix sort, `bits` bits a pass: count the digits of every tile of keys, then move the keys.  Per pass two launches, or
+// three above kFewTiles tiles.
+struct SortArgs {
+    int n, tiles, shift, bits;
+    uint32_t* counts;      // [tile][digit]
+    uint32_t* totals;      // [digit], above kFewTiles tiles
+    const uint32_t *key_in, *place_in;
+    uint32_t *key_out, *place_out;
+};
+
 // key = partition * vocab + id, or `none` (above all keys) at an empty place
 template <class ID>
-__global__ __launch_bounds__(kBlock) void k_embed_keys(const ID* tokens, int n, const EmbedParts parts, int64_t vocab,
-                                                       uint32_t none, uint32_t* key, uint32_t* place)
-{
-    const int t = blockIdx.x * kBlock + threadIdx.x;
-    if (t >= n) return;
-    int lo = 0, hi = parts.k - 1;   // the first partition that ends after t
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (parts.end[mid] > t) hi = mid;
-        else lo = mid + 1;
+struct KeySource {
+    const ID* tokens;
+    int64_t vocab;
+    uint32_t none;
+    uint32_t* key;
+    EmbedParts parts;
+    __device__ __forceinline__ uint32_t operator()(int t) const
+    {
+        int lo = 0, hi = parts.k - 1;   // the first partition that ends after t
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (parts.end[mid] > t) hi = mid;
+            else lo = mid + 1;
+        }
+        const int64_t id = (int64_t)tokens[t];
+        const uint32_t k = id >= 0 && id < vocab ? (uint32_t)(lo * vocab + id) : none;
+        key[t] = k;
+        return k;
     }
-    const int64_t id = (int64_t)tokens[t];
-    key[t] = id >= 0 && id < vocab ? (uint32_t)(lo * vocab + id) : none;
-    place[t] = (uint32_t)t;
-}
+};
 
-// Lanes of the wave whose digit equals mine, among those that hold a key.
-__device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool valid)
-{
-    uint64_t same = __ballot(valid);
-#pragma unroll
-    for (int b = 0; b < kDigitBits; ++b) {
-        const uint64_t ones = __ballot((digit >> b) & 1);
-        same &= (digit >> b) & 1 ? ones : ~ones;
-    }
-    return same;
-}
+struct SortedSource {
+    const uint32_t* key;
+    __device__ __forceinline__ uint32_t operator()(int t) const { return key[t]; }
+};
 
-// counts[tile][digit] of the keys' digits
-__global__ __launch_bounds__(kBlock) void k_sort_count(const uint32_t* key, int n, int shift, uint32_t* counts)
+template <class SOURCE>
+__global__ __launch_bounds__(kBlock) void k_sort_count(const SortArgs a, const SOURCE source)
 {
-    __shared__ uint32_t bin[kDigits];
-    for (int i = threadIdx.x; i < kDigits; i += kBlock) bin[i] = 0;
+    __shared__ uint32_t bin[kMostDigits];
+    const int digits = 1 << a.bits;
+    for (int i = threadIdx.x; i < digits; i += kBlock) bin[i] = 0;
     __syncthreads();
-    const int from = blockIdx.x * kSortTile, to = min(n, from + kSortTile);
-    for (int i = from + threadIdx.x; i < to; i += kBlock) atomicAdd(&bin[(key[i] >> shift) & (kDigits - 1)], 1u);
+    const int from = blockIdx.x * kSortTile, to = min(a.n, from + kSortTile);
+    for (int i = from + threadIdx.x; i < to; i += kBlock) atomicAdd(&bin[(source(i) >> a.shift) & (digits - 1)], 1u);
     __syncthreads();
-    for (int i = threadIdx.x; i < kDigits; i += kBlock) counts[(int64_t)blockIdx.x * kDigits + i] = bin[i];
+    for (int i = threadIdx.x; i < digits; i += kBlock) a.counts[(int64_t)blockIdx.x * digits + i] = bin[i];
 }
 
-// counts[tile][digit] -> where the tile's first key of that digit goes, less what precedes the digit; totals[digit]
-__global__ __launch_bounds__(64) void k_sort_tiles(uint32_t* counts, int tiles, uint32_t* totals)
+// counts[tile][digit] -> that digit's keys in the tiles before; totals[digit]
+__global__ __launch_bounds__(64) void k_sort_tiles(const SortArgs a)
 {
-    const int digit = blockIdx.x * 64 + threadIdx.x;
+    const int digits = 1 << a.bits, digit = blockIdx.x * 64 + threadIdx.x;
+    if (digit >= digits) return;
     uint32_t sum = 0;
-    for (int t = 0; t < tiles; t += 8) {
-        uint32_t here[8];
+    for (int t = 0; t < a.tiles; t += 16) {
+        uint32_t here[16];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) here[e] = t + e < tiles ? counts[(int64_t)(t + e) * kDigits + digit] : 0;
+        for (int e = 0; e < 16; ++e) here[e] = t + e < a.tiles ? a.counts[(int64_t)(t + e) * digits + digit] : 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (t + e < tiles) counts[(int64_t)(t + e) * kDigits + digit] = sum;
+        for (int e = 0; e < 16; ++e) {
+            if (t + e < a.tiles) a.counts[(int64_t)(t + e) * digits + digit] = sum;
             sum += here[e];
         }
     }
-    totals[digit] = sum;
+    a.totals[digit] = sum;
 }
 
 // Moves a tile's keys and places to where their digit puts them, equal digits in the order in which they lie.  Each
-// wave takes a quarter of the tile, 64 keys at a time.
-__global__ __launch_bounds__(kBlock) void k_sort_move(const uint32_t* key, const uint32_t* place, int n, int shift,
-                                                      const uint32_t* counts, const uint32_t* totals, uint32_t* key_out,
-                                                      uint32_t* place_out)
+// wave takes a quarter of the tile, 64 keys at a time.  FIRST: the places are 0, 1, 2, ...
+template <bool FIRST>
+__global__ __launch_bounds__(kBlock) void k_sort_move(const SortArgs a)
 {
-    __shared__ uint32_t next[4][kDigits];
-    __shared__ uint32_t carry[kBlock];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (int i = tid; i < 4 * kDigits; i += kBlock) (&next[0][0])[i] = 0;
-    __syncthreads();
-    const int from = blockIdx.x * kSortTile + wave * (kSortTile / 4);
-    for (int r = 0; r < kSortTile / 4; r += 64)
-        if (from + r + lane < n) atomicAdd(&next[wave][(key[from + r + lane] >> shift) & (kDigits - 1)], 1u);
-    // what precedes a digit: eight digits a thread, then the threads before
-    constexpr int kPer = kDigits / kBlock;
-    uint32_t before[kPer], sum = 0;
+    __shared__ uint32_t next[4][kMostDigits];
+    __shared__ uint32_t carry[4];
+    constexpr int kRounds = kSortTile / kBlock;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << a.bits;
+    const int from = blockIdx.x * kSortTile + wave * (kSortTile / 4) + lane;
+    uint32_t key[kRounds], place[kRounds];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        before[i] = sum;
-        sum += totals[tid * kPer + i];
+    for (int r = 0; r < kRounds; ++r) {
+        const int i = from + r * 64;
+        key[r] = i < a.n ? a.key_in[i] : 0;
+        place[r] = (uint32_t)i;
+        if (!FIRST && i < a.n) place[r] = a.place_in[i];
     }
-    carry[tid] = sum;
+    for (int i = tid; i < 4 * digits; i += kBlock) next[i >> a.bits][i & (digits - 1)] = 0;
     __syncthreads();
-    for (int d = 1; d < kBlock; d *= 2) {
-        const uint32_t add = tid >= d ? carry[tid - d] : 0;
-        __syncthreads();
-        carry[tid] += add;
-        __syncthreads();
-    }
-    const uint32_t base = carry[tid] - sum;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int digit = tid * kPer + i;
-        uint32_t at = base + before[i] + counts[(int64_t)blockIdx.x * kDigits + digit];
+    for (int r = 0; r < kRounds; ++r)
+        if (from + r * 64 < a.n) atomicAdd(&next[wave][(key[r] >> a.shift) & (digits - 1)], 1u);
+    // `per` digits a thread: keys of the tiles before, and of all tiles
+    constexpr int kMostPer = kMostDigits / kBlock;
+    const int per = digits > kBlock ? digits / kBlock : 1;
+    uint32_t before[kMostPer], all[kMostPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kMostPer; ++i) {
+        before[i] = all[i] = 0;
+        const int digit = tid * per + i;
+        if (i >= per || digit >= digits) continue;
+        if (a.tiles > kFewTiles) {
+            before[i] = a.counts[(int64_t)blockIdx.x * digits + digit];
+            all[i] = a.totals[digit];
+        } else {
+#pragma unroll
+            for (int t = 0; t < kFewTiles; ++t) {
+                const uint32_t c = t < a.tiles ? a.counts[t * digits + digit] : 0;
+                all[i] += c;
+                if (t < (int)blockIdx.x) before[i] += c;
+            }
+        }
+        sum += all[i];
+    }
+    // what precedes my digits: the lanes before, then the waves before
+    uint32_t scan = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t add = __shfl_up(scan, d);
+        if (lane >= d) scan += add;
+    }
+    if (lane == 63) carry[wave] = scan;
+    __syncthreads();
+    uint32_t at = scan - sum;
+    for (int w = 0; w < wave; ++w) at += carry[w];
+#pragma unroll
+    for (int i = 0; i < kMostPer; ++i) {
+        const int digit = tid * per + i;
+        if (i >= per || digit >= digits) continue;
+        uint32_t go = at + before[i];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const uint32_t here = next[w][digit];
-            next[w][digit] = at;
-            at += here;
+            next[w][digit] = go;
+            go += here;
         }
+        at += all[i];
     }
     __syncthreads();
-    for (int r = 0; r < kSortTile / 4; r += 64) {
-        const int i = from + r + lane;
-        const bool valid = i < n;
-        const uint32_t k = valid ? key[i] : 0, digit = (k >> shift) & (kDigits - 1);
-        const uint64_t same = same_digit(digit, valid);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const bool valid = from + r * 64 < a.n;
+        const uint32_t digit = (key[r] >> a.shift) & (digits - 1);
+        uint64_t same = __ballot(valid);   // the wave's lanes with my digit
+        for (int b = 0; b < a.bits; ++b) {
+            const uint64_t ones = __ballot((digit >> b) & 1);
+            same &= (digit >> b) & 1 ? ones : ~ones;
+        }
         const int rank = __popcll(same & ((1ull << lane) - 1));
         if (valid) {
-            const uint32_t at = next[wave][digit] + rank;
-            key_out[at] = k;
-            place_out[at] = place[i];
+            const uint32_t to = next[wave][digit] + rank;
+            a.key_out[to] = key[r];
+            a.place_out[to] = place[r];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -219,65 +262,79 @@ struct SumArgs {
     int n, dim;
     uint32_t none;
     int64_t ldd;         // of dout
-    int64_t pitch;       // of the pieces' sums: dim, rounded up to 4
+    int64_t pitch;       // of the pieces' sums: dim, rounded up to the 256 columns of a wave
     float* pieces;       // sums of kPiece places of one key, at place / kPiece
     float* groups;       // sums of kGroup pieces of one key
 };
 
-// The sum over places [from, to) of the order, four columns from c on.
-template <class T, bool WHOLE>
-__device__ __forceinline__ f32x4 sum_tokens(const SumArgs& a, const T* dout, int from, int to, int c, f32x4 acc)
+// The four columns of a lane in strip `strip` of 256, and where a piece's sum holds them.
+template <bool WHOLE>
+__device__ __forceinline__ int first_column(int strip, int lane) { return strip * 256 + (WHOLE ? lane * 4 : lane); }
+__device__ __forceinline__ int kept_column(int strip, int lane) { return strip * 256 + lane * 4; }
+
+// Adds the tokens at places [from, to) of the order, four columns from c on; uniform over the wave.  64 places are
+// fetched at once, a lane each, and DEEP rows are on their way together.
+template <class T, bool WHOLE, int DEEP>
+__device__ __forceinline__ f32x4 sum_tokens(const SumArgs& a, const T* dout, int from, int to, int c, int lane, f32x4 acc)
 {
-    for (int i = from; i < to; i += 4) {
-        f32x4 v[4];
+    const int col = c < a.dim ? c : 0;   // lanes behind the row add up something that nobody stores
+    for (; from < to; from += 64) {
+        const int count = to - from < 64 ? to - from : 64;
+        const uint32_t spot = a.place[from + (lane < count ? lane : 0)];
+        for (int i = 0; i < count; i += DEEP) {
+            f32x4 v[DEEP];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (i + e < to) v[e] = load4<T, WHOLE>(dout + (int64_t)a.place[i + e] * a.ldd, c, a.dim);
+            for (int e = 0; e < DEEP; ++e) {
+                const int64_t t = (uint32_t)__builtin_amdgcn_readlane(spot, (i + e) & 63);   // behind `count`: the first again
+                v[e] = load4<T, WHOLE>(dout + t * a.ldd, col, 64, a.dim);
+            }
+#pragma unroll
+            for (int e = 0; e < DEEP; ++e)
+                if (i + e < count) acc += v[e];
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc += v[e];
     }
     return acc;
 }
 
 __device__ __forceinline__ f32x4 sum_rows(const float* rows, int64_t pitch, int from, int to, int c, f32x4 acc)
 {
-    for (int i = from; i < to; i += 4) {
-        f32x4 v[4];
+    for (int i = from; i < to; i += 8) {
+        f32x4 v[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (i + e < to) v[e] = *reinterpret_cast<const f32x4*>(rows + (int64_t)(i + e) * pitch + c);
-        }
+        for (int e = 0; e < 8; ++e)
+            v[e] = *reinterpret_cast<const f32x4*>(rows + (int64_t)(i + e < to ? i + e : to - 1) * pitch + c);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc += v[e];
+        for (int e = 0; e < 8; ++e)
+            if (i + e < to) acc += v[e];
     }
     return acc;
 }
 
-// Whole pieces of one key.  A wave takes a piece and 256 columns.
+// Sums of the pieces and groups that hold one key alone.  A wave takes a piece, a workgroup a group, 256 columns of it.
 template <class T, bool WHOLE>
-__global__ __launch_bounds__(64) void k_embed_pieces(const SumArgs a, const T* dout)
+__global__ __launch_bounds__(kGroup * 64) void k_embed_pieces(const SumArgs a, const T* dout)
 {
-    const int first = blockIdx.x * kPiece;   // the grid holds whole pieces alone
-    const uint32_t key = a.key[first];
-    if (key != a.key[first + kPiece - 1] || key == a.none) return;
-    const int c = (blockIdx.y * 64 + threadIdx.x) * 4;
-    if (c >= a.dim) return;
-    const f32x4 sum = sum_tokens<T, WHOLE>(a, dout, first, first + kPiece, c, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-    *reinterpret_cast<f32x4*>(a.pieces + (int64_t)blockIdx.x * a.pitch + c) = sum;
-}
-
-__global__ __launch_bounds__(64) void k_embed_groups(const SumArgs a)
-{
-    const int first = blockIdx.x * kPiece * kGroup;
-    const uint32_t key = a.key[first];
-    if (key != a.key[first + kPiece * kGroup - 1] || key == a.none) return;
-    const int c = (blockIdx.y * 64 + threadIdx.x) * 4;
-    if (c >= a.dim) return;
-    const f32x4 sum = sum_rows(a.pieces, a.pitch, blockIdx.x * kGroup, (blockIdx.x + 1) * kGroup, c, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-    *reinterpret_cast<f32x4*>(a.groups + (int64_t)blockIdx.x * a.pitch + c) = sum;
+    __shared__ f32x4 part[kGroup][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = blockIdx.x, piece = group * kGroup + wave, first = piece * kPiece;
+    const int c = first_column<WHOLE>(blockIdx.y, lane), kept = kept_column(blockIdx.y, lane);
+    if (first + kPiece <= a.n) {
+        const uint32_t key = a.key[first];
+        if (key == a.key[first + kPiece - 1] && key != a.none) {
+            const f32x4 sum = sum_tokens<T, WHOLE, 16>(a, dout, first, first + kPiece, c, lane, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+            *reinterpret_cast<f32x4*>(a.pieces + (int64_t)piece * a.pitch + kept) = sum;
+            part[wave][lane] = sum;
+        }
+    }
+    const int64_t end = (int64_t)(group + 1) * kGroup * kPiece;
+    if (end > a.n || a.key[end - 1] != a.key[end - kGroup * kPiece] || a.key[end - 1] == a.none) return;
+    __syncthreads();   // the whole workgroup or none of it comes here, with all its pieces summed
+    if (wave == 0) {
+        f32x4 sum = part[0][lane];
+#pragma unroll
+        for (int w = 1; w < kGroup; ++w) sum += part[w][lane];
+        *reinterpret_cast<f32x4*>(a.groups + (int64_t)group * a.pitch + kept) = sum;
+    }
 }
 
 // First place in [lo, hi) whose key is not below `what`; hi if none is.
@@ -328,7 +385,7 @@ __device__ __forceinline__ void fill_rows(const SumArgs& a, int64_t vocab, int64
     for (int r = 0; r < count; ++r) {
         if ((empty >> r) & 1) {
             float* row = G + p * ldg + v * a.dim;
-            for (int c = lane * 4; c < a.dim; c += 256) store4<float, WHOLE>(row, c, a.dim, zero);
+            for (int c = first_column<WHOLE>(0, lane); c < a.dim; c += 256) store4<float, WHOLE>(row, c, 64, a.dim, zero);
         }
         if (++v == vocab) v = 0, ++p;
     }
@@ -343,7 +400,7 @@ __device__ __forceinline__ void sum_runs(const SumArgs& a, const T* dout, int64_
 {
     const int across = (a.dim + 255) >> 8;
     const int64_t strip = wave / across;
-    const int c = ((int)(wave - strip * across) * 64 + lane) * 4;
+    const int mine = (int)(wave - strip * across), c = first_column<WHOLE>(mine, lane), kept = kept_column(mine, lane);
     const int64_t first = strip * kHeads;
     if (first >= a.n) return;
     const int at = (int)first + lane;
@@ -358,25 +415,25 @@ __device__ __forceinline__ void sum_runs(const SumArgs& a, const T* dout, int64_
         const uint64_t later = heads & ~((2ull << h) - 1);
         int to = (int)first + (later ? __builtin_ctzll(later) : 64);
         if (!later) to = wave_lower_bound(a.key, to < a.n ? to : a.n, a.n, k + 1, lane);
-        if (c >= a.dim) continue;
         f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
         const int p0 = (from + kPiece - 1) / kPiece, p1 = to / kPiece;   // whole pieces
         if (p0 < p1) {
-            acc = sum_tokens<T, WHOLE>(a, dout, from, p0 * kPiece, c, acc);
+            acc = sum_tokens<T, WHOLE, 8>(a, dout, from, p0 * kPiece, c, lane, acc);
             const int g0 = (p0 + kGroup - 1) / kGroup, g1 = p1 / kGroup;
             if (g0 < g1) {
-                acc = sum_rows(a.pieces, a.pitch, p0, g0 * kGroup, c, acc);
-                acc = sum_rows(a.groups, a.pitch, g0, g1, c, acc);
-                acc = sum_rows(a.pieces, a.pitch, g1 * kGroup, p1, c, acc);
+                acc = sum_rows(a.pieces, a.pitch, p0, g0 * kGroup, kept, acc);
+                acc = sum_rows(a.groups, a.pitch, g0, g1, kept, acc);
+                acc = sum_rows(a.pieces, a.pitch, g1 * kGroup, p1, kept, acc);
             } else {
-                acc = sum_rows(a.pieces, a.pitch, p0, p1, c, acc);
+                acc = sum_rows(a.pieces, a.pitch, p0, p1, kept, acc);
             }
-            acc = sum_tokens<T, WHOLE>(a, dout, p1 * kPiece, to, c, acc);
+            acc = sum_tokens<T, WHOLE, 8>(a, dout, p1 * kPiece, to, c, lane, acc);
         } else {
-            acc = sum_tokens<T, WHOLE>(a, dout, from, to, c, acc);
+            acc = sum_tokens<T, WHOLE, 8>(a, dout, from, to, c, lane, acc);
         }
+        if (c >= a.dim) continue;
         const int64_t p = k / (uint32_t)vocab, v = k - p * vocab;
-        store4<float, WHOLE>(G + p * ldg + v * a.dim, c, a.dim, acc * scale);
+        store4<float, WHOLE>(G + p * ldg + v * a.dim, c, 64, a.dim, acc * scale);
     }
 }
 
@@ -422,15 +479,10 @@ hipError_t sums_as(const EmbedCall& c, const SumArgs& a, hipStream_t stream)
 {
     const T* dout = static_cast<const T*>(c.dout);
     const unsigned across = (unsigned)((c.dim + 255) / 256);
-    hipError_t e = hipSuccess;
     if (a.n >= kPiece) {
-        hipLaunchKernelGGL((k_embed_pieces<T, WHOLE>), dim3(a.n / kPiece, across), dim3(64), 0, stream, a, dout);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (a.n >= kPiece * kGroup) {
-        hipLaunchKernelGGL(k_embed_groups, dim3(a.n / (kPiece * kGroup), across), dim3(64), 0, stream, a);
-        e = hipGetLastError();
+        hipLaunchKernelGGL((k_embed_pieces<T, WHOLE>), dim3((a.n + kGroup * kPiece - 1) / (kGroup * kPiece), across),
+                           dim3(kGroup * 64), 0, stream, a, dout);
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     const int64_t total = c.vocab * c.k_parts;
@@ -457,8 +509,8 @@ hipError_t sums_with(const EmbedCall& c, const SumArgs& a, hipStream_t stream)
 int64_t embed_workspace_bytes(int64_t n, int64_t vocab, int dim, int k_parts)
 {
     (void)vocab, (void)k_parts;
-    const int64_t tiles = (n + kSortTile - 1) / kSortTile, pitch = round_up(dim, 4) * 4;
-    return 4 * round_up(n * 4, 256) + round_up(tiles * kDigits * 4, 256) + kDigits * 4 + round_up(n / kPiece * pitch, 256) +
+    const int64_t tiles = (n + kSortTile - 1) / kSortTile, pitch = round_up(dim, 256) * 4;
+    return 4 * round_up(n * 4, 256) + round_up(tiles * kMostDigits * 4, 256) + kMostDigits * 4 + round_up(n / kPiece * pitch, 256) +
            round_up(n / (kPiece * kGroup) * pitch, 256) + 256;
 }
 
@@ -483,10 +535,12 @@ hipError_t launch_embed_gradients(const EmbedCall& c, hipStream_t stream)
         key[i] = reinterpret_cast<uint32_t*>(take((int64_t)n * 4));
         place[i] = reinterpret_cast<uint32_t*>(take((int64_t)n * 4));
     }
-    uint32_t* counts = reinterpret_cast<uint32_t*>(take((int64_t)tiles * kDigits * 4));
-    uint32_t* totals = reinterpret_cast<uint32_t*>(take(kDigits * 4));
+    SortArgs order{};
+    order.n = n, order.tiles = tiles;
+    order.counts = reinterpret_cast<uint32_t*>(take((int64_t)tiles * kMostDigits * 4));
+    order.totals = reinterpret_cast<uint32_t*>(take(kMostDigits * 4));
     SumArgs a{};
-    a.n = n, a.dim = c.dim, a.ldd = c.ld, a.pitch = round_up(c.dim, 4);
+    a.n = n, a.dim = c.dim, a.ldd = c.ld, a.pitch = round_up(c.dim, 256);
     a.pieces = reinterpret_cast<float*>(take(n / kPiece * a.pitch * 4));
     a.groups = reinterpret_cast<float*>(take(n / (kPiece * kGroup) * a.pitch * 4));
     a.none = (uint32_t)(c.vocab * c.k_parts);
@@ -495,19 +549,26 @@ hipError_t launch_embed_gradients(const EmbedCall& c, hipStream_t stream)
         EmbedParts parts{};
         parts.k = c.k_parts;
         for (int p = 0; p < c.k_parts; ++p) parts.end[p] = (int)c.part_end[p];
-        const dim3 grid((n + kBlock - 1) / kBlock);
-        if (c.wide_ids)
-            hipLaunchKernelGGL(k_embed_keys<int64_t>, grid, dim3(kBlock), 0, stream, static_cast<const int64_t*>(c.tokens), n,
-                               parts, c.vocab, a.none, key[0], place[0]);
-        else
-            hipLaunchKernelGGL(k_embed_keys<int32_t>, grid, dim3(kBlock), 0, stream, static_cast<const int32_t*>(c.tokens), n,
-                               parts, c.vocab, a.none, key[0], place[0]);
-        for (int shift = 0; shift < 32 && (a.none >> shift) != 0; shift += kDigitBits) {
-            hipLaunchKernelGGL(k_sort_count, dim3(tiles), dim3(kBlock), 0, stream, key[now], n, shift, counts);
-            hipLaunchKernelGGL(k_sort_tiles, dim3(kDigits / 64), dim3(64), 0, stream, counts, tiles, totals);
-            hipLaunchKernelGGL(k_sort_move, dim3(tiles), dim3(kBlock), 0, stream, key[now], place[now], n, shift, counts, totals,
-                               key[now ^ 1], place[now ^ 1]);
-            now ^= 1;
+        int key_bits = 1;
+        while ((a.none >> key_bits) != 0) ++key_bits;
+        const int passes = (key_bits + kMostBits - 1) / kMostBits;
+        order.bits = (key_bits + passes - 1) / passes;
+        const dim3 grid(tiles), block(kBlock);
+        for (int pass = 0; pass < passes; ++pass, now ^= 1) {
+            order.shift = pass * order.bits;
+            order.key_in = key[now], order.place_in = place[now], order.key_out = key[now ^ 1], order.place_out = place[now ^ 1];
+            if (pass > 0)
+                hipLaunchKernelGGL(k_sort_count<SortedSource>, grid, block, 0, stream, order, SortedSource{key[now]});
+            else if (c.wide_ids)
+                hipLaunchKernelGGL(k_sort_count<KeySource<int64_t>>, grid, block, 0, stream, order,
+                                   KeySource<int64_t>{static_cast<const int64_t*>(c.tokens), c.vocab, a.none, key[0], parts});
+            else
+                hipLaunchKernelGGL(k_sort_count<KeySource<int32_t>>, grid, block, 0, stream, order,
+                                   KeySource<int32_t>{static_cast<const int32_t*>(c.tokens), c.vocab, a.none, key[0], parts});
+            if (tiles > kFewTiles)
+                hipLaunchKernelGGL(k_sort_tiles, dim3(((1 << order.bits) + 63) / 64), dim3(64), 0, stream, order);
+            if (pass == 0) hipLaunchKernelGGL(k_sort_move<true>, grid, block, 0, stream, order);
+            else hipLaunchKernelGGL(k_sort_move<false>, grid, block, 0, stream, order);
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
