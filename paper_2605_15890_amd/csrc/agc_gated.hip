@@ -31,6 +31,18 @@ struct GatedParts {
 
 struct Activation {
     int gelu;
+    // 1 / (1 + exp(-a)) by the chip's 2^x and reciprocal (an ulp each).  -a log2(e) is formed with what its rounding leaves,
+    // which would otherwise be off by up to |a| 2^-24 of the exponential.  An eighth of the time of expf and a division,
+    // which were a fifth of the forward pass.
+    static __device__ __forceinline__ float sigmoid(float a)
+    {
+        constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.69314718f;
+        const float t = -a * kLog2e;
+        const float rest = fmaf(-a, kLog2e, -t) - a * kLog2eRest;
+        const float e = __builtin_amdgcn_exp2f(t);
+        const float p = e < 1e30f ? fmaf(e, rest * kLn2, e) : e;   // an infinite power times a rest of 0 is no number
+        return __builtin_amdgcn_rcpf(1.0f + p);
+    }
     // activation and its derivative
     __device__ __forceinline__ void at(float a, float& value, float& slope) const
     {
@@ -39,14 +51,14 @@ struct Activation {
             value = a * cdf;
             slope = fmaf(a * 0.39894228040143268f, expf(-0.5f * a * a), cdf);
         } else {
-            const float sig = 1.0f / (1.0f + expf(-a));
+            const float sig = sigmoid(a);
             value = a * sig;
             slope = sig * fmaf(a, 1.0f - sig, 1.0f);
         }
     }
     __device__ __forceinline__ float operator()(float a) const
     {
-        return gelu ? a * (0.5f * (1.0f + erff(a * 0.70710678118654752f))) : a / (1.0f + expf(-a));
+        return gelu ? a * (0.5f * (1.0f + erff(a * 0.70710678118654752f))) : a * sigmoid(a);
     }
 };
 

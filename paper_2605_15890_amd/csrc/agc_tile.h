@@ -110,9 +110,12 @@ __device__ __forceinline__ uint32_t bf16_bits(float v)
 
 __device__ __forceinline__ tile_u32x4 bf16_pack8(const float v[8])
 {
+    typedef float pair_f32 __attribute__((ext_vector_type(2)));
+    typedef __bf16 pair_bf16 __attribute__((ext_vector_type(2)));
     tile_u32x4 o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
+    for (int i = 0; i < 4; ++i)   // both at once
+        o[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pair_f32{v[2 * i], v[2 * i + 1]}, pair_bf16));
     return o;
 }
 
