@@ -8,8 +8,12 @@
 //   da = dh u act'(a), du = dh act(a)          in the same pass
 //   dx = da Wg + du Wu                          one product over 2 F
 //   dWg_p = da_p^T x_p, dWu_p = du_p^T x_p      one product of 2 F rows a partition, written into row p of G
-// da and du enter dx rounded to bfloat16, as dx itself is; they enter G, which is binary32, as pairs of bfloat16
-// (16 bits, off by at most 2^-16): rounded once they would leave up to 2^-8 in every term of G.
+// da and du enter dx rounded to bfloat16, as dx itself is.  They enter G, which is binary32, as pairs of binary16 (22
+// bits), and x as binary16, which its 8 bits fit: two products, where three of bfloat16 would be needed for more than
+// 16 bits, and one would leave up to 2^-8 in every term of G.  The narrow range of binary16 is met by a power of two for
+// every partition, from the largest finite magnitudes of its dh and x and of the weights: they bound u and act(a), hence
+// da and du, and put the bound at 2^15.  Values of up to 2^-18 of the bound keep all 22 bits, smaller ones what lies above
+// 2^-40 of it; the bound is some 2^13 above the usual value for random operands 2000 wide.
 // The tile loop wants both operands contiguous along the sum: x and the weights are turned by passes of their own, da
 // and du are written both ways.  A partition starts at a multiple of 32 in the turned order, the places between are
 // zeros; `map` gives each place its token, or -1.
@@ -21,6 +25,22 @@ namespace agc {
 namespace {
 
 constexpr int kBlock = 256;
+
+// Largest magnitudes, as bfloat16 bits, of finite values: of dh and x of each partition, of Wg and of Wu.
+struct Bounds {
+    uint32_t* most;      // [2 * k + 2]
+    int k;
+    int width;           // log2 of d_in, rounded up
+    static __device__ __forceinline__ int power(uint32_t bits) { return (int)(bits >> 7) - 126; }   // below 2^power
+    // powers of two by which da and du, and x, of partition p are multiplied
+    __device__ __forceinline__ int of_x(int p) const { return 15 - power(most[2 * p + 1]); }
+    __device__ __forceinline__ int of_grad(int p) const
+    {
+        const int wg = power(most[2 * k]), wu = power(most[2 * k + 1]);
+        // |u|, |act(a)| <= d_in max|x| max|w|; |act'| < 2
+        return 14 - power(most[2 * p]) - power(most[2 * p + 1]) - (wg > wu ? wg : wu) - width;
+    }
+};
 
 // what the kernels know of the partitions: first place and first token of each
 struct GatedParts {
@@ -109,9 +129,11 @@ __global__ __launch_bounds__(kBlock) void k_pack_rows(const uint16_t* src, int64
             *reinterpret_cast<tile_u32x4*>(dst + r * up + c * 8) = load_bits8(src + r * ld, c * 8, width);
 }
 
-__global__ __launch_bounds__(kBlock) void k_gated_map(const GatedParts parts, int places, int* map)
+__global__ __launch_bounds__(kBlock) void k_gated_map(const GatedParts parts, int places, int* map, uint16_t* part,
+                                                      uint32_t* most)
 {
     const int i = blockIdx.x * kBlock + threadIdx.x;
+    for (int j = i; j < 2 * parts.k + 2; j += gridDim.x * kBlock) most[j] = 0;
     if (i >= places) return;
     int lo = 0, hi = parts.k - 1;   // the last partition that starts at or before i
     while (lo < hi) {
@@ -121,13 +143,82 @@ __global__ __launch_bounds__(kBlock) void k_gated_map(const GatedParts parts, in
     }
     const int t = parts.token[lo] + (i - parts.place[lo]);
     map[i] = t < parts.token[lo + 1] ? t : -1;
+    part[i] = (uint16_t)lo;
+}
+
+// The bounds.  A workgroup takes eight places of one partition, or eight rows of the weights.
+__global__ __launch_bounds__(kBlock) void k_gated_bounds(const uint16_t* x, int64_t ldx, const uint16_t* dh, int64_t lddh,
+                                                         const uint16_t* wg, const uint16_t* wu, int64_t ldw, int places,
+                                                         int d_in, int d_ff, const int* map, const uint16_t* part,
+                                                         const Bounds b)
+{
+    __shared__ uint32_t wave_most[4];
+    const int token_blocks = places / 8;
+    auto most_of = [&](const uint16_t* rows, int64_t ld, int first, int end, int width, const int* through, uint32_t* to) {
+        uint32_t most = 0;
+        auto look = [&](const tile_u32x4& v) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = v[e] & 0x7FFFu, hi = (v[e] >> 16) & 0x7FFFu;
+                most = lo < 0x7F80u && lo > most ? lo : most;
+                most = hi < 0x7F80u && hi > most ? hi : most;
+            }
+        };
+        const uint16_t* row[8];
+        bool whole = (width & 7) == 0;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {   // a row that is not there: the first one that is, or none
+            int at = first + r < end ? (through ? through[first + r] : first + r) : -1;
+            if (at < 0) at = through ? through[first] : first;   // a partition's places begin with its tokens
+            row[r] = at < 0 ? nullptr : rows + at * ld;
+            whole = whole && at >= 0 && aligned16(row[r]);
+        }
+        if (whole) {
+            for (int c = threadIdx.x * 8; c < width; c += kBlock * 8) {
+                tile_u32x4 v[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] = *reinterpret_cast<const tile_u32x4*>(row[r] + c);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) look(v[r]);
+            }
+        } else if (row[0]) {
+            for (int c = threadIdx.x; c < width; c += kBlock) {
+                uint32_t v[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] = row[r][c];
+#pragma unroll
+                for (int r = 0; r < 8; r += 4) look(tile_u32x4{v[r], v[r + 1], v[r + 2], v[r + 3]});
+            }
+        }
+        for (int d = 32; d >= 1; d >>= 1) {
+            const uint32_t other = __shfl_xor(most, d);
+            most = other > most ? other : most;
+        }
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) wave_most[threadIdx.x >> 6] = most;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < 4; ++w) most = wave_most[w] > most ? wave_most[w] : most;
+            if (most) atomicMax(to, most);   // the largest, in whatever order they come
+        }
+    };
+    const int id = blockIdx.x;
+    if (id < token_blocks) {
+        const int p = part[id * 8];
+        most_of(dh, lddh, id * 8, places, d_ff, map, b.most + 2 * p);
+        most_of(x, ldx, id * 8, places, d_in, map, b.most + 2 * p + 1);
+    } else {
+        most_of(wg, ldw, (id - token_blocks) * 8, d_ff, d_in, nullptr, b.most + 2 * b.k);
+        most_of(wu, ldw, (id - token_blocks) * 8, d_ff, d_in, nullptr, b.most + 2 * b.k + 1);
+    }
 }
 
 // dst row c = column c of src, along the rows of src (through `map`, if given; -1 and rows past the end are zeros),
-// `up` of them.  TWICE: in groups of 32, each twice, as the second operand of pairs.
+// `up` of them.  TWICE: as binary16 in groups of 32, each twice, as the second operand of pairs, scaled by what the
+// bounds say.
 template <bool TWICE>
 __global__ __launch_bounds__(kBlock) void k_turn(const uint16_t* src, int64_t ld, int rows, int cols, int up, const int* map,
-                                                 char* dst, int64_t pitch)
+                                                 const uint16_t* part, const Bounds bounds, char* dst, int64_t pitch)
 {
     __shared__ uint16_t tile[64][66];
     const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, tid = threadIdx.x;
@@ -150,6 +241,13 @@ __global__ __launch_bounds__(kBlock) void k_turn(const uint16_t* src, int64_t ld
         char* row = dst + (int64_t)(c0 + c) * pitch;
         const int at = r0 + r;
         if (TWICE) {
+            const int power = bounds.of_x(part[at]);
+            float f[8];
+            bf16_unpack8(v, f);
+            f16x8 half;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) half[e] = (_Float16)ldexpf(f[e], power);
+            v = __builtin_bit_cast(tile_u32x4, half);
             char* p = row + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
             *reinterpret_cast<tile_u32x4*>(p) = v;
             *reinterpret_cast<tile_u32x4*>(p + 64) = v;
@@ -262,6 +360,8 @@ struct GateJob {
     int fp;
     char* by_feature;                 // 2 d_ff rows of pairs along the places
     int64_t pitch;
+    const uint16_t* part;
+    Bounds bounds;
     int mt, nt, side, total;
 
     __device__ __forceinline__ void place(int id, TilePos& p) const
@@ -322,16 +422,12 @@ struct GateJob {
         const int run = (lane & 7) * 8, at = mb + run;
         const int c = it * 8 + (lane >> 3), ff = nb / 2 + (c >> 5) * 16 + (c & 15);
         if (ff >= d_ff || at >= n_rows) return;   // n_rows is a multiple of 32
-        float v[8], hi[8], lo[8];
+        const int power = bounds.of_grad(part[at]);
+        float v[8];
         piece_col8(s, run, c, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            hi[e] = __uint_as_float(bf16_bits(v[e]) << 16);
-            lo[e] = v[e] - hi[e];
-        }
-        char* o = by_feature + (int64_t)(((c & 16) ? d_ff : 0) + ff) * pitch + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
-        *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(hi);
-        *reinterpret_cast<tile_u32x4*>(o + 64) = bf16_pack8(lo);
+        for (int e = 0; e < 8; ++e) v[e] = ldexpf(v[e], power);
+        split_store8(by_feature + (int64_t)(((c & 16) ? d_ff : 0) + ff) * pitch, at, v);
     }
 };
 
@@ -375,7 +471,7 @@ struct InputJob {
 
 // Row p of G: [da | du]_p^T x_p
 struct WeightJob {
-    static constexpr TilePair kPair = kPlain;
+    static constexpr TilePair kPair = kHalf;
     static constexpr int kRowParts = 8;
     static constexpr bool kTurned = false;
     const char *a, *b;        // 2 d_ff and d_in rows along the places
@@ -383,6 +479,7 @@ struct WeightJob {
     int d_ff, d_in;
     float *gate, *up;
     int64_t ldg;
+    Bounds bounds;
     int mt, nt, side, total;
     GatedParts parts;
 
@@ -409,6 +506,9 @@ struct WeightJob {
         if (row >= 2 * d_ff || c >= d_in) return;
         float v[8];
         piece_row8(s, r, run, v);
+        const int power = p.steps > 0 ? -bounds.of_x(p.batch) - bounds.of_grad(p.batch) : 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = ldexpf(v[e], power);
         float* o = (row < d_ff ? gate + (int64_t)row * d_in : up + (int64_t)(row - d_ff) * d_in) + p.batch * ldg + c;
         if (d_in - c >= 8 && aligned16(o)) {
             reinterpret_cast<tile_f32x4*>(o)[0] = tile_f32x4{v[0], v[1], v[2], v[3]};
@@ -473,13 +573,13 @@ hipError_t launch_few(const GatedCall& c, hipStream_t stream)
 
 }  // namespace
 
-// packed x, Wg, Wu | map | da, du by token | by feature | x turned | weights turned
+// packed x, Wg, Wu | map, partition of each place, bounds | da, du by token | by feature | x turned | weights turned
 int64_t gated_workspace_bytes(int64_t tokens, int d_in, int d_ff, int k_parts)
 {
     int64_t bytes = packed_bytes(tokens, d_in, d_ff);
     if (k_parts > 0) {
         const int64_t places = round_up(tokens + 31 * (int64_t)k_parts, 32), fp = round_up(d_ff, 64);
-        bytes += round_up(places * 4, 256) + round_up(places * fp * 4, 256) + round_up(2 * d_ff * places * 4, 256) +
+        bytes += round_up(places * 4, 256) + round_up(places * 2, 256) + round_up((2 * k_parts + 2) * 4, 256) + round_up(places * fp * 4, 256) + round_up(2 * d_ff * places * 4, 256) +
                  round_up(d_in * places * 4, 256) + round_up(d_in * fp * 4, 256);
     }
     return bytes > 256 ? bytes : 256;
@@ -526,17 +626,25 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         return p;
     };
     char *by_feature = nullptr, *x_turned = nullptr;
+    Bounds bounds{nullptr, c.k_parts, 0};
+    while ((1 << bounds.width) < c.d_in) ++bounds.width;
     hipError_t e = hipSuccess;
     if (places > 0) {
         const Rows x = whole_steps(c.x, c.ldx, c.tokens, c.d_in, room, stream);
         const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, stream);
         const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, stream);
         int* map = reinterpret_cast<int*>(take((int64_t)places * 4));
+        uint16_t* part = reinterpret_cast<uint16_t*>(take((int64_t)places * 2));
+        bounds.most = reinterpret_cast<uint32_t*>(take((2 * c.k_parts + 2) * 4));
         char* by_token = take(places * fp * 4);
         by_feature = take(2 * c.d_ff * pitch);
         x_turned = take(c.d_in * pitch);
         char* w_turned = take(c.d_in * fp * 4);
-        hipLaunchKernelGGL(k_gated_map, dim3((places + kBlock - 1) / kBlock), dim3(kBlock), 0, stream, parts, places, map);
+        hipLaunchKernelGGL(k_gated_map, dim3((places + kBlock - 1) / kBlock), dim3(kBlock), 0, stream, parts, places, map,
+                           part, bounds.most);
+        hipLaunchKernelGGL(k_gated_bounds, dim3(places / 8 + (c.d_ff + 7) / 8), dim3(kBlock), 0, stream, x.p, x.ld,
+                           static_cast<const uint16_t*>(c.dh), c.lddh, static_cast<const uint16_t*>(c.wg),
+                           static_cast<const uint16_t*>(c.wu), c.ldw, places, c.d_in, c.d_ff, map, part, bounds);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         GateJob<true> j{};
@@ -544,6 +652,7 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         j.n_rows = places, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act, j.map = map;
         j.dh = static_cast<const uint16_t*>(c.dh), j.lddh = c.lddh;
         j.by_token = by_token, j.fp = (int)fp, j.by_feature = by_feature, j.pitch = pitch;
+        j.part = part, j.bounds = bounds;
         e = launch_product(j, 1, places, fp * 2, j.steps, stream);
         if (e != hipSuccess) return e;
         const unsigned across = (c.d_in + 63) / 64;
@@ -551,10 +660,10 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
             const unsigned down = (unsigned)(fp / 64);
             hipLaunchKernelGGL((k_turn<false>), dim3(down, across), dim3(kBlock), 0, stream,
                                static_cast<const uint16_t*>(c.wg), c.ldw, c.d_ff, c.d_in, (int)fp, (const int*)nullptr,
-                               w_turned, fp * 4);
+                               (const uint16_t*)nullptr, bounds, w_turned, fp * 4);
             hipLaunchKernelGGL((k_turn<false>), dim3(down, across), dim3(kBlock), 0, stream,
                                static_cast<const uint16_t*>(c.wu), c.ldw, c.d_ff, c.d_in, (int)fp, (const int*)nullptr,
-                               w_turned + fp * 2, fp * 4);
+                               (const uint16_t*)nullptr, bounds, w_turned + fp * 2, fp * 4);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
             InputJob d{by_token, w_turned, fp * 4, places, c.d_in, (int)(fp / 32), map, static_cast<uint16_t*>(c.dx), c.lddx};
@@ -562,13 +671,14 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
             if (e != hipSuccess) return e;
         }
         hipLaunchKernelGGL((k_turn<true>), dim3((places + 63) / 64, across), dim3(kBlock), 0, stream,
-                           static_cast<const uint16_t*>(c.x), c.ldx, places, c.d_in, places, map, x_turned, pitch);
+                           static_cast<const uint16_t*>(c.x), c.ldx, places, c.d_in, places, map, part, bounds,
+                           x_turned, pitch);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     WeightJob w{};
     w.a = by_feature, w.b = x_turned, w.pitch = pitch, w.d_ff = c.d_ff, w.d_in = c.d_in;
-    w.gate = c.g_gate, w.up = c.g_up, w.ldg = c.ldg, w.parts = parts;
+    w.gate = c.g_gate, w.up = c.g_up, w.ldg = c.ldg, w.parts = parts, w.bounds = bounds;
     return launch_product(w, c.k_parts, 2 * (int64_t)c.d_ff, c.d_in, places / 32 / c.k_parts, stream);
 }
 

@@ -3,7 +3,7 @@
 // Every product here is C[m,n] = sum_k A[m,k] * B[n,k] with 16-bit operands whose rows are contiguous in k,
 // held in groups of 128 bytes ("k-steps"); operands that come in another order or with another end are laid out
 // by a pass of their own before.  A k-step is either
-//   plain   64 values, bfloat16:                       C += A0 B0 + A1 B1     (its two halves of 32)
+//   plain   64 values, bfloat16 (or binary16: half):    C += A0 B0 + A1 B1     (its two halves of 32)
 //   split   32 values as binary16 pairs, 32 high parts and 32 low parts (x = hi + lo to 22 bits):
 //                                                      C += A0 B0 + A0 B1 + A1 B0   (lo * lo is below 2^-22)
 // so that the same loads feed both.  Products are v_mfma_f32_16x16x32, sums binary32.
@@ -27,7 +27,7 @@ typedef __bf16 tile_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float tile_f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t tile_u32x4 __attribute__((ext_vector_type(4)));
 
-enum TilePair { kPlain, kSplit };
+enum TilePair { kPlain, kHalf, kSplit };
 
 struct TilePos {
     int m0, n0;    // first row and column of the tile
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_tile(const JOB job)
             const tile_u32x4 a1 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at1);
 #pragma unroll
             for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a0, b0[j], acc[i][j]);
-            if constexpr (JOB::kPair == kPlain) {
+            if constexpr (JOB::kPair != kSplit) {
 #pragma unroll
                 for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a1, b1[j], acc[i][j]);
             } else {
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(256, 1) void k_tile_cut(const JOB job)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 acc[i][j] = tile_mfma<JOB::kPair>(a0, b0[j], acc[i][j]);
-                if constexpr (JOB::kPair == kPlain) {
+                if constexpr (JOB::kPair != kSplit) {
                     acc[i][j] = tile_mfma<JOB::kPair>(a1, b1[j], acc[i][j]);
                 } else {
                     acc[i][j] = tile_mfma<JOB::kPair>(a0, b1[j], acc[i][j]);
