@@ -13,6 +13,12 @@
 // X itself goes through this, not a rounded copy of it: single 16-bit values would leave errors that the products
 // amplify by up to a^S = 485 in the directions of small singular values.
 //
+// Two steps at once.  All factors are polynomials of the first A, so with B0 and Q the step's own
+//   A' = B0 A B0,  B1 = a I + b A' + c A' A',  Q = B1 B0,  X <- Q X
+// is two steps with one product along n each way in place of two: 3 m^2 n + 5 m^3 multiplications against 6 m^2 n + 2 m^3.
+// It is taken where n >= 2 m.  Q reaches a^2 = 11.9 where X is small and is rounded against that, so the error of
+// directions far below the largest is some a times that of single steps; longer chains would lose more.
+//
 // Each product writes its result for the next one in the order in which that one reads it: X along n (for X X^T) and
 // along m (for B X); A and B are symmetric, so half the tiles are formed and written twice.  The last product
 // updates beta from its sums; X is not written.
@@ -28,6 +34,7 @@ constexpr double kMuonEps = 1e-7;
 constexpr float kUnitX = 16384.0f;   // 2^14 * 1.21 < 65504
 constexpr float kUnitA = 16384.0f;   // 2^14 * 1.47
 constexpr float kUnitB = 8192.0f;    // 2^13 * 3.45
+constexpr float kUnitQ = 4096.0f;    // 2^12 * 3.45^2
 constexpr int kSumBlock = 256;       // threads of the elementwise passes
 constexpr int kMostSums = 1024;      // partial sums of squares of a matrix
 
@@ -148,17 +155,19 @@ __global__ __launch_bounds__(kSumBlock) void k_muon_start(const MuonCall c, Muon
 }
 
 // ------------------------------------------------------------------ the three products of a step
-// A = X X^T, or B = a I + b A + c A A: symmetric, from rows of one matrix; tiles of the lower triangle.
+// A symmetric product of rows of two matrices (X and X, or two polynomials of one A, which commute), or a I + b A + c A A:
+// tiles of the lower triangle.
 struct SymJob {
     static constexpr TilePair kPair = kSplit;
     static constexpr int kRowParts = 8;
     static constexpr bool kTurned = true;
-    const char* src;          // X along n, or A
-    char* dst;                // A or B
+    const char *src, *other;
+    char* dst;
     int64_t pitch, size;      // of src
     int64_t pitch_dst, size_dst;
     int m, steps, tiles, side, total;   // tiles of one matrix, tile edge, of all
     int poly;
+    float unit;               // of what is stored over the unit of the sums
 
     __device__ __forceinline__ void place(int id, TilePos& p) const
     {
@@ -168,12 +177,12 @@ struct SymJob {
         triangle_order(t - p.batch * tiles, mi, ni);
         p.m0 = mi * side, p.n0 = ni * side, p.steps = steps;
     }
-    __device__ __forceinline__ const char* row(const TilePos& p, int r) const
+    __device__ __forceinline__ int64_t row(const TilePos& p, int r) const
     {
-        return src + p.batch * size + (int64_t)(r < m ? r : m - 1) * pitch;
+        return p.batch * size + (int64_t)(r < m ? r : m - 1) * pitch;
     }
-    __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const { return row(p, p.m0 + r); }
-    __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const { return row(p, p.n0 + r); }
+    __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const { return src + row(p, p.m0 + r); }
+    __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const { return other + row(p, p.n0 + r); }
     // a tile on the diagonal holds both halves
     __device__ __forceinline__ bool turned(const TilePos& p) const { return p.m0 != p.n0; }
     __device__ __forceinline__ void rows(const TilePos& p, int mb, int nb, float* s, int it, int lane) const
@@ -196,7 +205,7 @@ struct SymJob {
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= kUnitA / (kUnitX * kUnitX);
+            for (int e = 0; e < 8; ++e) v[e] *= unit;
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -213,7 +222,7 @@ struct SymJob {
     }
 };
 
-// X <- B X, or, of the last step, beta <- keep * beta - rate * B X.
+// X <- B X (or Q X, with a unit of its own), or, at the end, beta <- keep * beta - rate * that.
 template <bool LAST>
 struct ApplyJob {
     static constexpr TilePair kPair = kSplit;
@@ -225,7 +234,8 @@ struct ApplyJob {
     char* out_t;             // along m
     MuonGeom g;
     int mt, nt, side, total;
-    MuonCall call;           // of the last step
+    float unit_b;            // of b
+    MuonCall call;           // at the end
 
     __device__ __forceinline__ void place(int id, TilePos& p) const
     {
@@ -249,7 +259,7 @@ struct ApplyJob {
     __device__ __forceinline__ void update(int64_t at, int count, const float v[8]) const
     {
         float* beta = call.beta + at;
-        const float rate = call.rate * (1.0f / (kUnitB * kUnitX));
+        const float rate = call.rate / (unit_b * kUnitX);
         float w[8];
         if (count == 8 && (reinterpret_cast<uintptr_t>(beta) & 15) == 0) {
             tile_f32x4* q = reinterpret_cast<tile_f32x4*>(beta);
@@ -291,7 +301,7 @@ struct ApplyJob {
         }
         piece_row8(s, it * 8 + (lane >> 3), run, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = gc + e < g.n ? v[e] * (1.0f / kUnitB) : 0.0f;
+        for (int e = 0; e < 8; ++e) v[e] = gc + e < g.n ? v[e] / unit_b : 0.0f;
         if (gr < g.m && gc < (int)(g.pitch_n / 4)) split_store8(out_x + p.batch * g.size_x + (int64_t)gr * g.pitch_n, gc, v);
     }
     __device__ __forceinline__ void cols(const TilePos& p, int mb, int nb, const float* s, int it, int lane) const
@@ -305,7 +315,7 @@ struct ApplyJob {
             return;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = gr + e < g.m ? v[e] * (1.0f / kUnitB) : 0.0f;
+        for (int e = 0; e < 8; ++e) v[e] = gr + e < g.m ? v[e] / unit_b : 0.0f;
         if (gc < g.n && gr < (int)(g.pitch_m / 4)) split_store8(out_t + p.batch * g.size_t + (int64_t)gc * g.pitch_m, gr, v);
     }
 };
@@ -528,12 +538,16 @@ hipError_t launch_apply(ApplyJob<LAST> j, hipStream_t stream)
 
 }  // namespace
 
-// sums | X along n, twice | X along m, twice | A | B
+// Whether two steps are taken at once: measured, 12 x 1024 x 4096 and 3 x 1501 x 515.
+bool muon_pairs(const MuonGeom& g) { return g.n >= 2 * (int64_t)g.m; }
+
+// sums | X along n, twice | X along m, twice | A | B | A', Q
 int64_t muon_workspace_bytes(int rows, int cols, int n_mats)
 {
     const MuonGeom g = muon_geom(rows, cols, n_mats);
     const int64_t sums = round_up((int64_t)n_mats * muon_sums((int64_t)rows * cols) * 8, 256);
-    return sums + 2 * (round_up(n_mats * g.size_x, 256) + round_up(n_mats * g.size_t, 256) + round_up(n_mats * g.size_a, 256));
+    return sums + 2 * (round_up(n_mats * g.size_x, 256) + round_up(n_mats * g.size_t, 256)) +
+           (muon_pairs(g) ? 4 : 2) * round_up(n_mats * g.size_a, 256);
 }
 
 hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
@@ -559,7 +573,9 @@ hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
     };
     char* x[2] = {take(c.n_mats * g.size_x), take(c.n_mats * g.size_x)};
     char* t[2] = {take(c.n_mats * g.size_t), take(c.n_mats * g.size_t)};
-    char *a = take(c.n_mats * g.size_a), *b = take(c.n_mats * g.size_a);
+    char *a = take(c.n_mats * g.size_a), *b = take(c.n_mats * g.size_a), *a2 = nullptr, *q = nullptr;
+    const bool pairs = muon_pairs(g);
+    if (pairs) a2 = take(c.n_mats * g.size_a), q = take(c.n_mats * g.size_a);
 
     hipLaunchKernelGGL(k_muon_momentum, dim3(n_sums, c.n_mats), dim3(kSumBlock), 0, stream, c, count, sums);
     hipError_t e = hipGetLastError();
@@ -567,18 +583,40 @@ hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
     hipLaunchKernelGGL(k_muon_start, dim3((c.cols + 63) / 64, (c.rows + 63) / 64, c.n_mats), dim3(kSumBlock), 0, stream, c, g,
                        sums, n_sums, g.tall ? t[0] : x[0], g.tall ? x[0] : t[0]);
     e = hipGetLastError();
-    for (int s = 0; s < c.steps && e == hipSuccess; ++s) {
-        const int in = s & 1, out = in ^ 1;
-        SymJob gram{x[in], a, g.pitch_n, g.size_x, g.pitch_m, g.size_a, g.m, (int)(g.pitch_n / 128), 0, 0, 0, 0};
-        e = launch_sym(gram, c.n_mats, stream);
+    if (e != hipSuccess) return e;
+
+    const int steps_m = (int)(g.pitch_m / 128), steps_n = (int)(g.pitch_n / 128);
+    auto gram = [&](const char* from, char* to) {
+        return launch_sym(SymJob{from, from, to, g.pitch_n, g.size_x, g.pitch_m, g.size_a, g.m, steps_n, 0, 0, 0, 0,
+                                 kUnitA / (kUnitX * kUnitX)}, c.n_mats, stream);
+    };
+    // the product of two symmetric matrices that commute, or a I + b A + c A A
+    auto square = [&](const char* one, const char* two, char* to, int poly, float unit) {
+        return launch_sym(SymJob{one, two, to, g.pitch_m, g.size_a, g.pitch_m, g.size_a, g.m, steps_m, 0, 0, 0, poly, unit},
+                          c.n_mats, stream);
+    };
+    int in = 0;
+    for (int s = 0; s < c.steps;) {
+        const bool two = pairs && s + 2 <= c.steps;
+        const bool last = s + (two ? 2 : 1) == c.steps;
+        e = gram(x[in], a);
+        if (e == hipSuccess) e = square(a, a, b, 1, 1.0f);
+        if (two) {
+            if (e == hipSuccess) e = square(b, a, q, 0, kUnitA / (kUnitA * kUnitB));    // B0 A
+            if (e == hipSuccess) e = square(q, b, a2, 0, kUnitA / (kUnitA * kUnitB));   // A'
+            if (e == hipSuccess) e = square(a2, a2, a, 1, 1.0f);                        // B1
+            if (e == hipSuccess) e = square(a, b, q, 0, kUnitQ / (kUnitB * kUnitB));
+        }
         if (e != hipSuccess) return e;
-        SymJob poly{a, b, g.pitch_m, g.size_a, g.pitch_m, g.size_a, g.m, (int)(g.pitch_m / 128), 0, 0, 0, 1};
-        e = launch_sym(poly, c.n_mats, stream);
+        const char* factor = two ? q : b;
+        const float unit = two ? kUnitQ : kUnitB;
+        if (last) return launch_apply(ApplyJob<true>{factor, t[in], nullptr, nullptr, g, 0, 0, 0, 0, unit, c}, stream);
+        e = launch_apply(ApplyJob<false>{factor, t[in], x[in ^ 1], t[in ^ 1], g, 0, 0, 0, 0, unit, c}, stream);
         if (e != hipSuccess) return e;
-        if (s + 1 < c.steps) e = launch_apply(ApplyJob<false>{b, t[in], x[out], t[out], g, 0, 0, 0, 0, c}, stream);
-        else e = launch_apply(ApplyJob<true>{b, t[in], nullptr, nullptr, g, 0, 0, 0, 0, c}, stream);
+        in ^= 1;
+        s += two ? 2 : 1;
     }
-    return e;
+    return hipSuccess;
 }
 
 }  // namespace agc
