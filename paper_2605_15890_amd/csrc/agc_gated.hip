@@ -42,6 +42,12 @@ struct Bounds {
     }
 };
 
+struct Rows {
+    const uint16_t* p;
+    int64_t ld;
+    int width;
+};
+
 // what the kernels know of the partitions: first place and first token of each
 struct GatedParts {
     int place[kMostParts + 1];
@@ -119,42 +125,135 @@ __device__ __forceinline__ tile_u32x4 load_bits8(const uint16_t* row, int k, int
 }
 
 // ------------------------------------------------------------------ laying operands out
-// Rows whose width or alignment the tile loop's loads do not take: copied to rows of a whole number of k-steps.
-__global__ __launch_bounds__(kBlock) void k_pack_rows(const uint16_t* src, int64_t ld, int64_t rows, int width, int up,
-                                                      uint16_t* dst)
+// Rows whose width or alignment the tile loop's loads do not take, copied to rows of a whole number of k-steps; eight
+// rows a workgroup.
+struct PackRows {
+    const uint16_t* src;
+    int64_t ld;
+    int rows, width, up;
+    uint16_t* dst;
+    __device__ __forceinline__ void run(int block) const
+    {
+        const int per = up / 8;
+        for (int i = threadIdx.x; i < 8 * per; i += kBlock) {
+            const int sub = i / per, c = (i - sub * per) * 8;
+            const int64_t r = (int64_t)block * 8 + sub;
+            if (r < rows) *reinterpret_cast<tile_u32x4*>(dst + r * up + c) = load_bits8(src + r * ld, c, width);
+        }
+    }
+};
+
+struct PlaceMap {
+    int* map;
+    uint16_t* part;
+    uint32_t* most;      // cleared for the bounds
+    int places;
+    GatedParts parts;
+    __device__ __forceinline__ void run(int block, int blocks) const
+    {
+        const int i = block * kBlock + threadIdx.x;
+        for (int j = i; j < 2 * parts.k + 2; j += blocks * kBlock) most[j] = 0;
+        if (i >= places) return;
+        int lo = 0, hi = parts.k - 1;   // the last partition that starts at or before i
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (parts.place[mid] <= i) lo = mid;
+            else hi = mid - 1;
+        }
+        const int t = parts.token[lo] + (i - parts.place[lo]);
+        map[i] = t < parts.token[lo + 1] ? t : -1;
+        part[i] = (uint16_t)lo;
+    }
+};
+
+// dst row c = column c of src, along the rows of src (through `map`, if given; -1 and rows past the end are zeros),
+// `up` of them.  TWICE: as binary16 in groups of 32, each twice, as the second operand of pairs, scaled by what the
+// bounds say.
+template <bool TWICE>
+struct Turn {
+    const uint16_t* src;
+    int64_t ld;
+    int rows, cols, up;
+    const int* map;
+    const uint16_t* part;
+    Bounds bounds;
+    char* dst;
+    int64_t pitch;
+    __device__ __forceinline__ void run(int r0, int c0) const
+    {
+        __shared__ uint16_t tile[64][66];
+        const int tid = threadIdx.x;
+        for (int i = tid; i < 512; i += kBlock) {
+            const int r = i >> 3, c = (i & 7) * 8;
+            int from = r0 + r < rows ? r0 + r : -1;
+            if (map && from >= 0) from = map[from];
+            tile_u32x4 v = {0u, 0u, 0u, 0u};
+            if (from >= 0 && c0 + c < cols) v = load_bits8(src + (int64_t)from * ld, c0 + c, cols);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(&tile[r][c + 2 * e]) = v[e];
+        }
+        __syncthreads();
+        for (int i = tid; i < 512; i += kBlock) {
+            const int c = i >> 3, r = (i & 7) * 8;
+            if (c0 + c >= cols || r0 + r >= up) continue;
+            tile_u32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (uint32_t)tile[r + 2 * e][c] | ((uint32_t)tile[r + 2 * e + 1][c] << 16);
+            char* row = dst + (int64_t)(c0 + c) * pitch;
+            const int at = r0 + r;
+            if (TWICE) {
+                const int power = bounds.of_x(part[at]);
+                float f[8];
+                bf16_unpack8(v, f);
+                f16x8 half;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) half[e] = (_Float16)ldexpf(f[e], power);
+                v = __builtin_bit_cast(tile_u32x4, half);
+                char* p = row + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
+                *reinterpret_cast<tile_u32x4*>(p) = v;
+                *reinterpret_cast<tile_u32x4*>(p + 64) = v;
+            } else {
+                *reinterpret_cast<tile_u32x4*>(row + (int64_t)at * 2) = v;
+            }
+        }
+    }
+};
+
+// All that needs nothing but the call's operands, in one launch: the copies of x, Wg, Wu that are needed, the map, and
+// the weights turned.
+struct Prepare {
+    PackRows pack[3];
+    int pack_blocks[3];
+    PlaceMap map;
+    int map_blocks;
+    Turn<false> turn[2];
+    int turn_down, turn_blocks;   // of one
+    int total() const { return pack_blocks[0] + pack_blocks[1] + pack_blocks[2] + map_blocks + 2 * turn_blocks; }
+};
+
+__global__ __launch_bounds__(kBlock) void k_gated_prepare(const Prepare a)
 {
-    const int per = up / 8;
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int c = threadIdx.x; c < per; c += kBlock)
-            *reinterpret_cast<tile_u32x4*>(dst + r * up + c * 8) = load_bits8(src + r * ld, c * 8, width);
+    int block = blockIdx.x;
+    for (int i = 0; i < 3; ++i) {
+        if (block < a.pack_blocks[i]) return a.pack[i].run(block);
+        block -= a.pack_blocks[i];
+    }
+    if (block < a.map_blocks) return a.map.run(block, a.map_blocks);
+    block -= a.map_blocks;
+    const int which = block >= a.turn_blocks ? 1 : 0, at = block - which * a.turn_blocks, across = at / a.turn_down;
+    a.turn[which].run((at - across * a.turn_down) * 64, across * 64);
 }
 
-__global__ __launch_bounds__(kBlock) void k_gated_map(const GatedParts parts, int places, int* map, uint16_t* part,
-                                                      uint32_t* most)
-{
-    const int i = blockIdx.x * kBlock + threadIdx.x;
-    for (int j = i; j < 2 * parts.k + 2; j += gridDim.x * kBlock) most[j] = 0;
-    if (i >= places) return;
-    int lo = 0, hi = parts.k - 1;   // the last partition that starts at or before i
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (parts.place[mid] <= i) lo = mid;
-        else hi = mid - 1;
-    }
-    const int t = parts.token[lo] + (i - parts.place[lo]);
-    map[i] = t < parts.token[lo + 1] ? t : -1;
-    part[i] = (uint16_t)lo;
-}
+__global__ __launch_bounds__(kBlock) void k_turn_tokens(const Turn<true> a) { a.run(blockIdx.x * 64, blockIdx.y * 64); }
 
 // The bounds.  A workgroup takes eight places of one partition, or eight rows of the weights.
-__global__ __launch_bounds__(kBlock) void k_gated_bounds(const uint16_t* x, int64_t ldx, const uint16_t* dh, int64_t lddh,
-                                                         const uint16_t* wg, const uint16_t* wu, int64_t ldw, int places,
-                                                         int d_in, int d_ff, const int* map, const uint16_t* part,
-                                                         const Bounds b)
+__global__ __launch_bounds__(kBlock) void k_gated_bounds(const Rows x, const Rows dh, const Rows wg, const Rows wu, int places,
+                                                         int d_ff, const int* map, const uint16_t* part, const Bounds b)
 {
     __shared__ uint32_t wave_most[4];
     const int token_blocks = places / 8;
-    auto most_of = [&](const uint16_t* rows, int64_t ld, int first, int end, int width, const int* through, uint32_t* to) {
+    auto most_of = [&](const Rows& rows, int first, int end, const int* through, uint32_t* to) {
+        const int width = rows.width;
         uint32_t most = 0;
         auto look = [&](const tile_u32x4& v) {
 #pragma unroll
@@ -170,7 +269,7 @@ __global__ __launch_bounds__(kBlock) void k_gated_bounds(const uint16_t* x, int6
         for (int r = 0; r < 8; ++r) {   // a row that is not there: the first one that is, or none
             int at = first + r < end ? (through ? through[first + r] : first + r) : -1;
             if (at < 0) at = through ? through[first] : first;   // a partition's places begin with its tokens
-            row[r] = at < 0 ? nullptr : rows + at * ld;
+            row[r] = at < 0 ? nullptr : rows.p + at * rows.ld;
             whole = whole && at >= 0 && aligned16(row[r]);
         }
         if (whole) {
@@ -205,55 +304,11 @@ __global__ __launch_bounds__(kBlock) void k_gated_bounds(const uint16_t* x, int6
     const int id = blockIdx.x;
     if (id < token_blocks) {
         const int p = part[id * 8];
-        most_of(dh, lddh, id * 8, places, d_ff, map, b.most + 2 * p);
-        most_of(x, ldx, id * 8, places, d_in, map, b.most + 2 * p + 1);
+        most_of(dh, id * 8, places, map, b.most + 2 * p);
+        most_of(x, id * 8, places, map, b.most + 2 * p + 1);
     } else {
-        most_of(wg, ldw, (id - token_blocks) * 8, d_ff, d_in, nullptr, b.most + 2 * b.k);
-        most_of(wu, ldw, (id - token_blocks) * 8, d_ff, d_in, nullptr, b.most + 2 * b.k + 1);
-    }
-}
-
-// dst row c = column c of src, along the rows of src (through `map`, if given; -1 and rows past the end are zeros),
-// `up` of them.  TWICE: as binary16 in groups of 32, each twice, as the second operand of pairs, scaled by what the
-// bounds say.
-template <bool TWICE>
-__global__ __launch_bounds__(kBlock) void k_turn(const uint16_t* src, int64_t ld, int rows, int cols, int up, const int* map,
-                                                 const uint16_t* part, const Bounds bounds, char* dst, int64_t pitch)
-{
-    __shared__ uint16_t tile[64][66];
-    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, tid = threadIdx.x;
-    for (int i = tid; i < 512; i += kBlock) {
-        const int r = i >> 3, c = (i & 7) * 8;
-        int from = r0 + r < rows ? r0 + r : -1;
-        if (map && from >= 0) from = map[from];
-        tile_u32x4 v = {0u, 0u, 0u, 0u};
-        if (from >= 0 && c0 + c < cols) v = load_bits8(src + (int64_t)from * ld, c0 + c, cols);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(&tile[r][c + 2 * e]) = v[e];
-    }
-    __syncthreads();
-    for (int i = tid; i < 512; i += kBlock) {
-        const int c = i >> 3, r = (i & 7) * 8;
-        if (c0 + c >= cols || r0 + r >= up) continue;
-        tile_u32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (uint32_t)tile[r + 2 * e][c] | ((uint32_t)tile[r + 2 * e + 1][c] << 16);
-        char* row = dst + (int64_t)(c0 + c) * pitch;
-        const int at = r0 + r;
-        if (TWICE) {
-            const int power = bounds.of_x(part[at]);
-            float f[8];
-            bf16_unpack8(v, f);
-            f16x8 half;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) half[e] = (_Float16)ldexpf(f[e], power);
-            v = __builtin_bit_cast(tile_u32x4, half);
-            char* p = row + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
-            *reinterpret_cast<tile_u32x4*>(p) = v;
-            *reinterpret_cast<tile_u32x4*>(p + 64) = v;
-        } else {
-            *reinterpret_cast<tile_u32x4*>(row + (int64_t)at * 2) = v;
-        }
+        most_of(wg, (id - token_blocks) * 8, d_ff, nullptr, b.most + 2 * b.k);
+        most_of(wu, (id - token_blocks) * 8, d_ff, nullptr, b.most + 2 * b.k + 1);
     }
 }
 
@@ -532,25 +587,26 @@ hipError_t launch_product(JOB j, int batch, int64_t m, int64_t n, int64_t steps,
     return launch_tiles(j, c, stream);
 }
 
-struct Rows {
-    const uint16_t* p;
-    int64_t ld;
-};
-
 bool takes_whole_loads(const void* p, int64_t ld) { return (ld & 7) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// Rows that the tile loop's loads take as they are, or a copy of them in `room`.
-Rows whole_steps(const void* src, int64_t ld, int64_t rows, int width, char*& room, hipStream_t stream)
+// Rows that the tile loop's loads take as they are, or a copy of them in `room`, made by copy `i` of `prepare`.
+Rows whole_steps(const void* src, int64_t ld, int64_t rows, int width, char*& room, Prepare& prepare, int i)
 {
     const int up = (int)round_up(width, 64);
-    char* mine = room;
+    uint16_t* mine = reinterpret_cast<uint16_t*>(room);
     room += round_up(rows * up * 2, 256);
     const uint16_t* p = static_cast<const uint16_t*>(src);
-    if (up == width && takes_whole_loads(src, ld)) return Rows{p, ld};
-    const int64_t blocks = rows < 8192 ? rows : 8192;
-    hipLaunchKernelGGL(k_pack_rows, dim3((unsigned)blocks), dim3(kBlock), 0, stream, p, ld, rows, width, up,
-                       reinterpret_cast<uint16_t*>(mine));
-    return Rows{reinterpret_cast<uint16_t*>(mine), up};
+    if (up == width && takes_whole_loads(src, ld)) return Rows{p, ld, width};
+    prepare.pack[i] = PackRows{p, ld, (int)rows, width, up, mine};
+    prepare.pack_blocks[i] = (int)((rows + 7) / 8);
+    return Rows{mine, up, up};
+}
+
+hipError_t launch_prepare(const Prepare& prepare, hipStream_t stream)
+{
+    if (prepare.total() == 0) return hipSuccess;
+    hipLaunchKernelGGL(k_gated_prepare, dim3(prepare.total()), dim3(kBlock), 0, stream, prepare);
+    return hipGetLastError();
 }
 
 int64_t packed_bytes(int64_t tokens, int d_in, int d_ff)
@@ -596,10 +652,11 @@ hipError_t launch_gated_forward(const GatedCall& c, hipStream_t stream)
     }
     const Activation act{c.gelu};
     char* room = c.workspace;
-    const Rows x = whole_steps(c.x, c.ldx, c.tokens, c.d_in, room, stream);
-    const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, stream);
-    const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, stream);
-    hipError_t e = hipGetLastError();
+    Prepare prepare{};
+    const Rows x = whole_steps(c.x, c.ldx, c.tokens, c.d_in, room, prepare, 0);
+    const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, prepare, 1);
+    const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, prepare, 2);
+    const hipError_t e = launch_prepare(prepare, stream);
     if (e != hipSuccess) return e;
     GateJob<false> j{};
     j.x = x.p, j.ldx = x.ld, j.wg = wg.p, j.ldg = wg.ld, j.wu = wu.p, j.ldu = wu.ld;
@@ -630,9 +687,11 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
     while ((1 << bounds.width) < c.d_in) ++bounds.width;
     hipError_t e = hipSuccess;
     if (places > 0) {
-        const Rows x = whole_steps(c.x, c.ldx, c.tokens, c.d_in, room, stream);
-        const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, stream);
-        const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, stream);
+        Prepare prepare{};
+        const Rows x = whole_steps(c.x, c.ldx, c.tokens, c.d_in, room, prepare, 0);
+        const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, prepare, 1);
+        const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, prepare, 2);
+        const Rows dh{static_cast<const uint16_t*>(c.dh), c.lddh, c.d_ff};
         int* map = reinterpret_cast<int*>(take((int64_t)places * 4));
         uint16_t* part = reinterpret_cast<uint16_t*>(take((int64_t)places * 2));
         bounds.most = reinterpret_cast<uint32_t*>(take((2 * c.k_parts + 2) * 4));
@@ -640,41 +699,39 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         by_feature = take(2 * c.d_ff * pitch);
         x_turned = take(c.d_in * pitch);
         char* w_turned = take(c.d_in * fp * 4);
-        hipLaunchKernelGGL(k_gated_map, dim3((places + kBlock - 1) / kBlock), dim3(kBlock), 0, stream, parts, places, map,
-                           part, bounds.most);
-        hipLaunchKernelGGL(k_gated_bounds, dim3(places / 8 + (c.d_ff + 7) / 8), dim3(kBlock), 0, stream, x.p, x.ld,
-                           static_cast<const uint16_t*>(c.dh), c.lddh, static_cast<const uint16_t*>(c.wg),
-                           static_cast<const uint16_t*>(c.wu), c.ldw, places, c.d_in, c.d_ff, map, part, bounds);
+        const int across = (c.d_in + 63) / 64;
+        prepare.map = PlaceMap{map, part, bounds.most, places, parts};
+        prepare.map_blocks = (places + kBlock - 1) / kBlock;
+        if (c.dx) {
+            prepare.turn[0] = Turn<false>{static_cast<const uint16_t*>(c.wg), c.ldw, c.d_ff, c.d_in, (int)fp, nullptr, nullptr,
+                                          bounds, w_turned, fp * 4};
+            prepare.turn[1] = prepare.turn[0];
+            prepare.turn[1].src = static_cast<const uint16_t*>(c.wu), prepare.turn[1].dst = w_turned + fp * 2;
+            prepare.turn_down = (int)(fp / 64);
+            prepare.turn_blocks = prepare.turn_down * across;
+        }
+        e = launch_prepare(prepare, stream);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(k_gated_bounds, dim3(places / 8 + (c.d_ff + 7) / 8), dim3(kBlock), 0, stream, x, dh, wg, wu, places,
+                           c.d_ff, map, part, bounds);
+        hipLaunchKernelGGL(k_turn_tokens, dim3((places + 63) / 64, across), dim3(kBlock), 0, stream,
+                           Turn<true>{static_cast<const uint16_t*>(c.x), c.ldx, places, c.d_in, places, map, part, bounds,
+                                      x_turned, pitch});
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         GateJob<true> j{};
         j.x = x.p, j.ldx = x.ld, j.wg = wg.p, j.ldg = wg.ld, j.wu = wu.p, j.ldu = wu.ld;
         j.n_rows = places, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act, j.map = map;
-        j.dh = static_cast<const uint16_t*>(c.dh), j.lddh = c.lddh;
+        j.dh = dh.p, j.lddh = dh.ld;
         j.by_token = by_token, j.fp = (int)fp, j.by_feature = by_feature, j.pitch = pitch;
         j.part = part, j.bounds = bounds;
         e = launch_product(j, 1, places, fp * 2, j.steps, stream);
         if (e != hipSuccess) return e;
-        const unsigned across = (c.d_in + 63) / 64;
         if (c.dx) {
-            const unsigned down = (unsigned)(fp / 64);
-            hipLaunchKernelGGL((k_turn<false>), dim3(down, across), dim3(kBlock), 0, stream,
-                               static_cast<const uint16_t*>(c.wg), c.ldw, c.d_ff, c.d_in, (int)fp, (const int*)nullptr,
-                               (const uint16_t*)nullptr, bounds, w_turned, fp * 4);
-            hipLaunchKernelGGL((k_turn<false>), dim3(down, across), dim3(kBlock), 0, stream,
-                               static_cast<const uint16_t*>(c.wu), c.ldw, c.d_ff, c.d_in, (int)fp, (const int*)nullptr,
-                               (const uint16_t*)nullptr, bounds, w_turned + fp * 2, fp * 4);
-            e = hipGetLastError();
-            if (e != hipSuccess) return e;
             InputJob d{by_token, w_turned, fp * 4, places, c.d_in, (int)(fp / 32), map, static_cast<uint16_t*>(c.dx), c.lddx};
             e = launch_product(d, 1, places, c.d_in, d.steps, stream);
             if (e != hipSuccess) return e;
         }
-        hipLaunchKernelGGL((k_turn<true>), dim3((places + 63) / 64, across), dim3(kBlock), 0, stream,
-                           static_cast<const uint16_t*>(c.x), c.ldx, places, c.d_in, places, map, part, bounds,
-                           x_turned, pitch);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
     }
     WeightJob w{};
     w.a = by_feature, w.b = x_turned, w.pitch = pitch, w.d_ff = c.d_ff, w.d_in = c.d_in;
