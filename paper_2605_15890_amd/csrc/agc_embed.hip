@@ -163,6 +163,95 @@ __global__ __launch_bounds__(64) void k_sort_tiles(const SortArgs a)
     a.totals[digit] = sum;
 }
 
+// All passes at once where the keys are one tile: keys and places stay in LDS, one launch in place of two or three a pass
+// (57 tokens of 1776 ids in 9 partitions: 21 us for the whole gradient, then 16).
+template <class SOURCE>
+__global__ __launch_bounds__(kBlock) void k_sort_one_tile(const SortArgs a, int passes, const SOURCE source)
+{
+    __shared__ uint32_t next[4][kMostDigits];
+    __shared__ uint32_t keys[kSortTile], places[kSortTile];
+    __shared__ uint32_t carry[4];
+    constexpr int kRounds = kSortTile / kBlock;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1 << a.bits;
+    const int from = wave * (kSortTile / 4) + lane, per = digits > kBlock ? digits / kBlock : 1;
+    uint32_t key[kRounds], place[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int i = from + r * 64;
+        key[r] = i < a.n ? source(i) : 0;
+        place[r] = (uint32_t)i;
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * a.bits;
+        for (int i = tid; i < 4 * digits; i += kBlock) next[i >> a.bits][i & (digits - 1)] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
+            if (from + r * 64 < a.n) atomicAdd(&next[wave][(key[r] >> shift) & (digits - 1)], 1u);
+        __syncthreads();
+        uint32_t sum = 0;
+        for (int i = 0; i < per; ++i) {
+            const int digit = tid * per + i;
+            if (digit < digits) sum += (next[0][digit] + next[1][digit]) + (next[2][digit] + next[3][digit]);
+        }
+        uint32_t scan = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t add = __shfl_up(scan, d);
+            if (lane >= d) scan += add;
+        }
+        if (lane == 63) carry[wave] = scan;
+        __syncthreads();
+        uint32_t at = scan - sum;
+        for (int w = 0; w < wave; ++w) at += carry[w];
+        for (int i = 0; i < per; ++i) {
+            const int digit = tid * per + i;
+            if (digit >= digits) continue;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t here = next[w][digit];
+                next[w][digit] = at;
+                at += here;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const bool valid = from + r * 64 < a.n;
+            const uint32_t digit = (key[r] >> shift) & (digits - 1);
+            uint64_t same = __ballot(valid);   // the wave's lanes with my digit
+            for (int b = 0; b < a.bits; ++b) {
+                const uint64_t ones = __ballot((digit >> b) & 1);
+                same &= (digit >> b) & 1 ? ones : ~ones;
+            }
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            if (valid) {
+                const uint32_t to = next[wave][digit] + rank;
+                keys[to] = key[r];
+                places[to] = place[r];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (valid && rank == 0) next[wave][digit] += __popcll(same);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int i = from + r * 64;
+            key[r] = i < a.n ? keys[i] : 0;
+            place[r] = i < a.n ? places[i] : 0;
+        }
+        // the next pass clears `next` before its first barrier; nobody reads `keys` after this
+    }
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int i = from + r * 64;
+        if (i < a.n) a.key_out[i] = key[r], a.place_out[i] = place[r];
+    }
+}
+
 // Moves a tile's keys and places to where their digit puts them, equal digits in the order in which they lie.  Each
 // wave takes a quarter of the tile, 64 keys at a time.  FIRST: the places are 0, 1, 2, ...
 template <bool FIRST>
@@ -554,7 +643,17 @@ hipError_t launch_embed_gradients(const EmbedCall& c, hipStream_t stream)
         const int passes = (key_bits + kMostBits - 1) / kMostBits;
         order.bits = (key_bits + passes - 1) / passes;
         const dim3 grid(tiles), block(kBlock);
-        for (int pass = 0; pass < passes; ++pass, now ^= 1) {
+        if (tiles == 1) {
+            order.key_out = key[1], order.place_out = place[1];
+            if (c.wide_ids)
+                hipLaunchKernelGGL(k_sort_one_tile<KeySource<int64_t>>, grid, block, 0, stream, order, passes,
+                                   KeySource<int64_t>{static_cast<const int64_t*>(c.tokens), c.vocab, a.none, key[0], parts});
+            else
+                hipLaunchKernelGGL(k_sort_one_tile<KeySource<int32_t>>, grid, block, 0, stream, order, passes,
+                                   KeySource<int32_t>{static_cast<const int32_t*>(c.tokens), c.vocab, a.none, key[0], parts});
+            now = 1;
+        }
+        for (int pass = 0; tiles > 1 && pass < passes; ++pass, now ^= 1) {
             order.shift = pass * order.bits;
             order.key_in = key[now], order.place_in = place[now], order.key_out = key[now ^ 1], order.place_out = place[now ^ 1];
             if (pass > 0)
