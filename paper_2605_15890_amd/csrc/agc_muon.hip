@@ -516,6 +516,85 @@ __global__ __launch_bounds__(FORM::kThreads) void k_muon_small(const MuonCall c,
     }
 }
 
+// ------------------------------------------------------------------ short sides of up to 96
+// What lies between the two products along the long side, B of one step or Q of two, in one launch: A and the
+// polynomials stay in one workgroup's LDS, where the separate launches of each pair of steps take five times 5 us:
+// 9 x 67 x 768 with 16-bit copy 120 us, then 101; 9 x 1 x 1856 116 us, then 81.
+constexpr int kChainSide = 96, kChainBlocks = 5;   // 36 blocks of 16 x 16 over 8 waves
+
+__global__ __launch_bounds__(512) void k_muon_chain(const char* gram, char* out, MuonGeom g, int two)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[3 * kChainSide * kChainSide * 4];
+    const int tid = threadIdx.x, lane = tid & 63, q4 = (lane >> 4) * 4, col = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int mr = (int)(g.pitch_m / 4), pitch = (int)g.pitch_m, across = mr / 16;
+    char *a = lds, *b = a + mr * pitch, *c = b + mr * pitch;
+    gram += blockIdx.x * g.size_a;
+    out += blockIdx.x * g.size_a;
+    for (int i = tid; i < mr * pitch / 16; i += 512) {
+        const int r = i / (pitch / 16), at = i - r * (pitch / 16);   // 16-byte chunk of a row
+        tile_u32x4 v = {0u, 0u, 0u, 0u};
+        if (r < g.m) v = *reinterpret_cast<const tile_u32x4*>(gram + (int64_t)r * pitch + at * 16);
+        *reinterpret_cast<tile_u32x4*>(a + r * pitch + ((at ^ (r & 7)) << 4)) = v;
+    }
+    __syncthreads();
+    tile_f32x4 unused;
+    // blocks of left * right, four values of consecutive rows in a column each; symmetric
+    auto product = [&](const char* left, const char* right, auto&& sink) {
+#pragma unroll
+        for (int t = 0; t < kChainBlocks; ++t) {
+            const int i = wave + t * 8;
+            if (i >= across * across) continue;
+            const int bi = i / across * 16, bj = (i - i / across * across) * 16;
+            tile_f32x4 v;
+            small_block<false>(left, right, bi, bj, pitch, mr / 32, lane, v, unused);
+            sink(bj + col, bi + q4, v);
+        }
+    };
+    auto keep = [&](const char* left, const char* right, char* to, float unit) {
+        product(left, right, [&](int r, int k, const tile_f32x4& v) { small_put4(to, r, k, pitch, v * unit); });
+        __syncthreads();
+    };
+    auto step_factor = [&](const char* from, char* to) {   // a I + b A + c A A
+        product(from, from, [&](int r, int k, tile_f32x4 v) {
+            const int at = small_at(r, k, pitch);
+            const f16x4 hi = *reinterpret_cast<const f16x4*>(from + at), lo = *reinterpret_cast<const f16x4*>(from + (at ^ 64));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = fmaf(kNsC * (kUnitB / (kUnitA * kUnitA)), v[e], kNsB * (kUnitB / kUnitA) * ((float)hi[e] + (float)lo[e]));
+                if (r == k + e) v[e] += kNsA * kUnitB;
+            }
+            small_put4(to, r, k, pitch, v);
+        });
+        __syncthreads();
+    };
+    auto write = [&](int r, int k, const tile_f32x4& v) {
+        if (r >= g.m) return;
+        f16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            hi[e] = (_Float16)v[e];
+            lo[e] = (_Float16)(v[e] - (float)hi[e]);
+        }
+        char* p = out + (int64_t)r * pitch + (k >> 5) * 128 + (k & 31) * 2;
+        *reinterpret_cast<f16x4*>(p) = hi;
+        *reinterpret_cast<f16x4*>(p + 64) = lo;
+    };
+    step_factor(a, b);
+    if (two) {
+        keep(b, a, c, 1.0f / kUnitB);   // B0 A
+        keep(c, b, a, 1.0f / kUnitB);   // A'
+        step_factor(a, c);              // B1
+        product(c, b, [&](int r, int k, const tile_f32x4& v) { write(r, k, v * (kUnitQ / (kUnitB * kUnitB))); });
+    } else {
+        for (int i = tid; i < g.m * pitch / 16; i += 512) {
+            const int r = i / (pitch / 16), at = i - r * (pitch / 16);
+            *reinterpret_cast<tile_u32x4*>(out + (int64_t)r * pitch + at * 16) =
+                *reinterpret_cast<const tile_u32x4*>(b + r * pitch + ((at ^ (r & 7)) << 4));
+        }
+    }
+}
+
 hipError_t launch_sym(SymJob j, int mats, hipStream_t stream)
 {
     const TileChoice c = choose_tile(mats, j.m, j.m, j.steps, true);
@@ -600,8 +679,13 @@ hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
         const bool two = pairs && s + 2 <= c.steps;
         const bool last = s + (two ? 2 : 1) == c.steps;
         e = gram(x[in], a);
-        if (e == hipSuccess) e = square(a, a, b, 1, 1.0f);
-        if (two) {
+        if (e == hipSuccess && mr <= kChainSide) {
+            hipLaunchKernelGGL(k_muon_chain, dim3(c.n_mats), dim3(512), 0, stream, a, two ? q : b, g, (int)two);
+            e = hipGetLastError();
+        } else if (e == hipSuccess) {
+            e = square(a, a, b, 1, 1.0f);
+        }
+        if (two && mr > kChainSide) {
             if (e == hipSuccess) e = square(b, a, q, 0, kUnitA / (kUnitA * kUnitB));    // B0 A
             if (e == hipSuccess) e = square(q, b, a2, 0, kUnitA / (kUnitA * kUnitB));   // A'
             if (e == hipSuccess) e = square(a2, a2, a, 1, 1.0f);                        // B1

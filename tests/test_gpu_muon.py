@@ -88,6 +88,16 @@ def test_orthogonal_factor_round_the_limits_of_one_launch(rows, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(96, 190), (1, 1900), (2000, 33), (64, 700), (95, 1000), (97, 1000), (700, 96)])
+@pytest.mark.parametrize("steps", [4, 5])
+def test_orthogonal_factor_of_long_matrices(rows, cols, steps):
+    """Two steps at once, and a short side of up to 96 between the long products."""
+    got, want, _, _, at = run(rows, cols, 2, gap=1, steps=steps, seed=rows + cols)
+    for here in at:
+        assert off_by(got[here], want[here]) < 1e-5
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,cols,mats", [(1300, 1290, 2), (1025, 3001, 5), (4097, 2050, 4)])
 def test_orthogonal_factor_of_large_matrices(rows, cols, mats):
     """Every tile size and its edges; the 64-bit products are taken on the GPU."""
