@@ -55,13 +55,16 @@ __device__ __forceinline__ f32x4 load4(const T* row, int c, int step, int width)
     return v;
 }
 
+// Past the caches: nothing that is written here is read here, and what is read stays (131072 x 1024 forward 109 us through
+// them, 99 us so).
 template <class T, bool WHOLE>
 __device__ __forceinline__ void store4(T* row, int c, int step, int width, const f32x4& v)
 {
     if constexpr (WHOLE && sizeof(T) == 4) {
-        *reinterpret_cast<f32x4*>(row + c) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(row + c));
     } else if constexpr (WHOLE) {
-        *reinterpret_cast<u32x2*>(row + c) = u32x2{to_bf16(v.x) | (to_bf16(v.y) << 16), to_bf16(v.z) | (to_bf16(v.w) << 16)};
+        __builtin_nontemporal_store(u32x2{to_bf16(v.x) | (to_bf16(v.y) << 16), to_bf16(v.z) | (to_bf16(v.w) << 16)},
+                                    reinterpret_cast<u32x2*>(row + c));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
