@@ -517,25 +517,82 @@ __global__ __launch_bounds__(FORM::kThreads) void k_muon_small(const MuonCall c,
 }
 
 // ------------------------------------------------------------------ short sides of up to 96
+// A = X X^T of a short side has one to three tiles, each of them a sum along the whole long side: the sum is cut into
+// pieces for workgroups of their own, whose 64 x 64 sums k_muon_chain adds in order (2 x 44 x 7095: 37 us, cut 9 us).
+struct GramPieceJob {
+    static constexpr TilePair kPair = kSplit;
+    static constexpr int kRowParts = 8;
+    static constexpr bool kTurned = false;
+    const char* x;
+    float* sums;             // [matrix][tile][piece][64 * 64]
+    int64_t pitch, size;
+    int m, steps, pieces, tiles;
+
+    __device__ __forceinline__ void place(int id, TilePos& p) const
+    {
+        const int tile = id / pieces, piece = id - tile * pieces;
+        p.batch = tile / tiles;
+        int mi, ni;
+        triangle_order(tile - p.batch * tiles, mi, ni);
+        p.m0 = mi * 64, p.n0 = ni * 64;
+        const int first = (int)((int64_t)steps * piece / pieces);
+        p.steps = (int)((int64_t)steps * (piece + 1) / pieces) - first;
+        p.extra = first, p.id = id;
+    }
+    __device__ __forceinline__ const char* row(const TilePos& p, int r) const
+    {
+        return x + p.batch * size + (int64_t)(r < m ? r : m - 1) * pitch + (int64_t)p.extra * 128;
+    }
+    __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const { return row(p, p.m0 + r); }
+    __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const { return row(p, p.n0 + r); }
+    __device__ __forceinline__ void rows(const TilePos& p, int, int, const float* s, int it, int lane) const
+    {
+        const int run = (lane & 7) * 8, r = it * 8 + (lane >> 3);
+        float v[8];
+        piece_row8(s, r, run, v);
+        tile_f32x4* o = reinterpret_cast<tile_f32x4*>(sums + (int64_t)p.id * 4096 + r * 64 + run);
+        o[0] = tile_f32x4{v[0], v[1], v[2], v[3]};
+        o[1] = tile_f32x4{v[4], v[5], v[6], v[7]};
+    }
+};
+
 // What lies between the two products along the long side, B of one step or Q of two, in one launch: A and the
 // polynomials stay in one workgroup's LDS, where the separate launches of each pair of steps take five times 5 us:
 // 9 x 67 x 768 with 16-bit copy 120 us, then 101; 9 x 1 x 1856 116 us, then 81.
 constexpr int kChainSide = 96, kChainBlocks = 5;   // 36 blocks of 16 x 16 over 8 waves
 
-__global__ __launch_bounds__(512) void k_muon_chain(const char* gram, char* out, MuonGeom g, int two)
+constexpr int kMostPieces = 16;
+
+__host__ __device__ inline int chain_pieces(const MuonGeom& g)   // of eight k-steps or more, two a wave
+{
+    const int64_t pieces = g.pitch_n / 128 / 8;
+    return pieces < 1 ? 1 : pieces < kMostPieces ? (int)pieces : kMostPieces;
+}
+
+__global__ __launch_bounds__(512) void k_muon_chain(const float* sums, char* out, MuonGeom g, int two)
 {
     __shared__ __attribute__((aligned(1024))) char lds[3 * kChainSide * kChainSide * 4];
     const int tid = threadIdx.x, lane = tid & 63, q4 = (lane >> 4) * 4, col = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int mr = (int)(g.pitch_m / 4), pitch = (int)g.pitch_m, across = mr / 16;
     char *a = lds, *b = a + mr * pitch, *c = b + mr * pitch;
-    gram += blockIdx.x * g.size_a;
     out += blockIdx.x * g.size_a;
-    for (int i = tid; i < mr * pitch / 16; i += 512) {
-        const int r = i / (pitch / 16), at = i - r * (pitch / 16);   // 16-byte chunk of a row
-        tile_u32x4 v = {0u, 0u, 0u, 0u};
-        if (r < g.m) v = *reinterpret_cast<const tile_u32x4*>(gram + (int64_t)r * pitch + at * 16);
-        *reinterpret_cast<tile_u32x4*>(a + r * pitch + ((at ^ (r & 7)) << 4)) = v;
+    const int side = (g.m + 63) / 64, tiles = side * (side + 1) / 2, pieces = chain_pieces(g);
+    sums += (int64_t)blockIdx.x * tiles * pieces * 4096;
+    for (int i = tid; i < tiles * 1024; i += 512) {
+        const int t = i >> 10, mi = t > 0 ? 1 : 0, ni = t == 2 ? 1 : 0;   // (0, 0), (1, 0), (1, 1)
+        const int r = mi * 64 + ((i & 1023) >> 4), k = ni * 64 + (i & 15) * 4;
+        const float* from = sums + (int64_t)t * pieces * 4096 + (i & 1023) * 4;
+        tile_f32x4 v = *reinterpret_cast<const tile_f32x4*>(from);
+        for (int p = 1; p < pieces; ++p) v += *reinterpret_cast<const tile_f32x4*>(from + p * 4096);
+        if (r >= mr || k >= mr) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = r < g.m && k + e < g.m ? v[e] * (kUnitA / (kUnitX * kUnitX)) : 0.0f;
+        small_put4(a, r, k, pitch, v);
+        if (mi != ni) {   // the half above the diagonal
+#pragma unroll
+            for (int e = 0; e < 4; ++e) small_put(a, k + e, r, pitch, v[e]);
+        }
     }
     __syncthreads();
     tile_f32x4 unused;
@@ -620,13 +677,21 @@ hipError_t launch_apply(ApplyJob<LAST> j, hipStream_t stream)
 // Whether two steps are taken at once: measured, 12 x 1024 x 4096 and 3 x 1501 x 515.
 bool muon_pairs(const MuonGeom& g) { return g.n >= 2 * (int64_t)g.m; }
 
-// sums | X along n, twice | X along m, twice | A | B | A', Q
+// the pieces' sums of A of one matrix with a short side of up to 96
+int64_t chain_bytes(const MuonGeom& g)
+{
+    const int64_t side = (g.m + 63) / 64;
+    return side * (side + 1) / 2 * chain_pieces(g) * 4096 * 4;
+}
+
+// sums | X along n, twice | X along m, twice | A | B | pieces of A | A', Q
 int64_t muon_workspace_bytes(int rows, int cols, int n_mats)
 {
     const MuonGeom g = muon_geom(rows, cols, n_mats);
     const int64_t sums = round_up((int64_t)n_mats * muon_sums((int64_t)rows * cols) * 8, 256);
     return sums + 2 * (round_up(n_mats * g.size_x, 256) + round_up(n_mats * g.size_t, 256)) +
-           (muon_pairs(g) ? 4 : 2) * round_up(n_mats * g.size_a, 256);
+           (muon_pairs(g) ? 4 : 2) * round_up(n_mats * g.size_a, 256) +
+           (g.m <= kChainSide ? round_up(n_mats * chain_bytes(g), 256) : 0);
 }
 
 hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
@@ -654,6 +719,8 @@ hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
     char* t[2] = {take(c.n_mats * g.size_t), take(c.n_mats * g.size_t)};
     char *a = take(c.n_mats * g.size_a), *b = take(c.n_mats * g.size_a), *a2 = nullptr, *q = nullptr;
     const bool pairs = muon_pairs(g);
+    float* pieces_sums = nullptr;
+    if (mr <= kChainSide) pieces_sums = reinterpret_cast<float*>(take(c.n_mats * chain_bytes(g)));
     if (pairs) a2 = take(c.n_mats * g.size_a), q = take(c.n_mats * g.size_a);
 
     hipLaunchKernelGGL(k_muon_momentum, dim3(n_sums, c.n_mats), dim3(kSumBlock), 0, stream, c, count, sums);
@@ -678,12 +745,15 @@ hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
     for (int s = 0; s < c.steps;) {
         const bool two = pairs && s + 2 <= c.steps;
         const bool last = s + (two ? 2 : 1) == c.steps;
-        e = gram(x[in], a);
-        if (e == hipSuccess && mr <= kChainSide) {
-            hipLaunchKernelGGL(k_muon_chain, dim3(c.n_mats), dim3(512), 0, stream, a, two ? q : b, g, (int)two);
+        if (mr <= kChainSide) {
+            const int side = (g.m + 63) / 64, tiles = side * (side + 1) / 2, pieces = chain_pieces(g);
+            hipLaunchKernelGGL(k_tile_cut<GramPieceJob>, dim3(c.n_mats * tiles * pieces), dim3(256), 0, stream,
+                               GramPieceJob{x[in], pieces_sums, g.pitch_n, g.size_x, g.m, steps_n, pieces, tiles});
+            hipLaunchKernelGGL(k_muon_chain, dim3(c.n_mats), dim3(512), 0, stream, pieces_sums, two ? q : b, g, (int)two);
             e = hipGetLastError();
-        } else if (e == hipSuccess) {
-            e = square(a, a, b, 1, 1.0f);
+        } else {
+            e = gram(x[in], a);
+            if (e == hipSuccess) e = square(a, a, b, 1, 1.0f);
         }
         if (two && mr > kChainSide) {
             if (e == hipSuccess) e = square(b, a, q, 0, kUnitA / (kUnitA * kUnitB));    // B0 A

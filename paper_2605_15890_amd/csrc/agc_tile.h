@@ -33,6 +33,7 @@ struct TilePos {
     int m0, n0;    // first row and column of the tile
     int batch;     // matrix or partition
     int steps;     // k-steps
+    int extra, id; // what a job keeps of it
 };
 
 // Workgroup id -> place in the order of the tiles.  Workgroups go to the eight XCDs in turn; each XCD gets a
@@ -391,7 +392,7 @@ inline TileChoice choose_tile(int64_t batch, int64_t m, int64_t n, int64_t steps
         const double slots = side == 128 ? 512.0 : 256.0;
         const double rounds = (double)((c.total + (int64_t)slots - 1) / (int64_t)slots);
         double us;
-        if (side == 256) us = rounds * (2.3 * s + 15.0);
+        if (side == 256) us = rounds * (2.3 * s + 20.0);
         else if (side == 128) us = rounds * ((t > 256.0 ? 1.4 : 0.9) * s + 8.0);
         else us = rounds * (0.3 * s + 5.0);
         if (side == 256 || us < least) best = c, least = us;
