@@ -234,7 +234,7 @@ struct ApplyJob {
     char* out_t;             // along m
     MuonGeom g;
     int mt, nt, side, total;
-    float unit_b;            // of b
+    float per_unit_b;        // 1 over the unit of b, a power of two
     MuonCall call;           // at the end
 
     __device__ __forceinline__ void place(int id, TilePos& p) const
@@ -259,7 +259,7 @@ struct ApplyJob {
     __device__ __forceinline__ void update(int64_t at, int count, const float v[8]) const
     {
         float* beta = call.beta + at;
-        const float rate = call.rate / (unit_b * kUnitX);
+        const float rate = call.rate * (per_unit_b * (1.0f / kUnitX));
         float w[8];
         if (count == 8 && (reinterpret_cast<uintptr_t>(beta) & 15) == 0) {
             tile_f32x4* q = reinterpret_cast<tile_f32x4*>(beta);
@@ -301,7 +301,7 @@ struct ApplyJob {
         }
         piece_row8(s, it * 8 + (lane >> 3), run, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = gc + e < g.n ? v[e] / unit_b : 0.0f;
+        for (int e = 0; e < 8; ++e) v[e] = gc + e < g.n ? v[e] * per_unit_b : 0.0f;
         if (gr < g.m && gc < (int)(g.pitch_n / 4)) split_store8(out_x + p.batch * g.size_x + (int64_t)gr * g.pitch_n, gc, v);
     }
     __device__ __forceinline__ void cols(const TilePos& p, int mb, int nb, const float* s, int it, int lane) const
@@ -315,7 +315,7 @@ struct ApplyJob {
             return;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = gr + e < g.m ? v[e] / unit_b : 0.0f;
+        for (int e = 0; e < 8; ++e) v[e] = gr + e < g.m ? v[e] * per_unit_b : 0.0f;
         if (gc < g.n && gr < (int)(g.pitch_m / 4)) split_store8(out_t + p.batch * g.size_t + (int64_t)gc * g.pitch_m, gr, v);
     }
 };
@@ -763,9 +763,9 @@ hipError_t launch_muon_update(const MuonCall& c, hipStream_t stream)
         }
         if (e != hipSuccess) return e;
         const char* factor = two ? q : b;
-        const float unit = two ? kUnitQ : kUnitB;
-        if (last) return launch_apply(ApplyJob<true>{factor, t[in], nullptr, nullptr, g, 0, 0, 0, 0, unit, c}, stream);
-        e = launch_apply(ApplyJob<false>{factor, t[in], x[in ^ 1], t[in ^ 1], g, 0, 0, 0, 0, unit, c}, stream);
+        const float per_unit = two ? 1.0f / kUnitQ : 1.0f / kUnitB;
+        if (last) return launch_apply(ApplyJob<true>{factor, t[in], nullptr, nullptr, g, 0, 0, 0, 0, per_unit, c}, stream);
+        e = launch_apply(ApplyJob<false>{factor, t[in], x[in ^ 1], t[in ^ 1], g, 0, 0, 0, 0, per_unit, c}, stream);
         if (e != hipSuccess) return e;
         in ^= 1;
         s += two ? 2 : 1;
