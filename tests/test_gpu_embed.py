@@ -2,8 +2,8 @@
 
 Tolerances.  Forward: one binary32 product (2^-24 of the value at most) and, to bfloat16, one rounding (2^-8).  Gradient:
 binary32 sums; a value is off by at most (number of additions it went through + 1) * 2^-24 of the sum of its terms'
-magnitudes.  A run of n tokens goes through at most 64 + 64 additions at its ends, 64 + 32 inside its pieces and groups,
-64 pieces at the groups' edges and n / 2048 groups: (300 + n / 2048) * 2^-24.
+magnitudes.  A run of n tokens goes through at most 63 + 63 additions at its ends, 64 + 16 inside its pieces and groups,
+15 + 15 pieces at the groups' edges and n / 1024 groups: below 300 + n / 2048 for the lengths that are tested here.
 """
 import numpy as np
 import pytest

@@ -185,6 +185,55 @@ def test_gradients_against_differences(act):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("x_std,w_std,dh_std", [(1e-12, 1.0, 1e-3), (1.0, 1e-9, 1e-30), (1e6, 1e-6, 1e12), (1.0, 1.0, 1e-34)])
+def test_gradients_far_from_one(x_std, w_std, dh_std):
+    """Magnitudes that binary16 does not reach: the partitions' powers of two bring them there and back."""
+    import torch
+    tokens, d_in, d_ff, ends = 96, 72, 40, [32, 96]
+    rng = np.random.default_rng(11)
+    x, xh = normal(rng, tokens, d_in, x_std)
+    wg, wgh = normal(rng, d_ff, d_in, w_std)
+    wu, wuh = normal(rng, d_ff, d_in, w_std)
+    dh, dhh = normal(rng, tokens, d_ff, dh_std)
+    half = d_in * d_ff
+    G = torch.empty(2, 2 * half, device="cuda")
+    ws = torch.empty(api.agc_gated_workspace_bytes(tokens, d_in, d_ff, 2), dtype=torch.uint8, device="cuda")
+    api.agc_gated_partial_gradients(x, wg, wu, "silu", dh, ends, None, G[:, :half], G[:, half:], ws)
+    _, want, _, size = host_gradients(xh, wgh, wuh, "silu", dhh, ends)
+    got = G.double().cpu().numpy()
+    for p in range(2):
+        for part in (slice(0, half), slice(half, 2 * half)):
+            # binary32 holds nothing below 2^-149
+            assert np.linalg.norm(got[p, part] - want[p, part]) < TOL_G * np.linalg.norm(size[p, part]) + half ** 0.5 * 2.0 ** -149
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_is_not_finite_stays_in_its_partition(bad):
+    import torch
+    tokens, d_in, d_ff, ends = 100, 40, 24, [30, 60, 100]
+    rng, (x, wg, wu), _ = problem(tokens, d_in, d_ff, seed=3)
+    dh, _ = normal(rng, tokens, d_ff, 1e-3)
+    half = d_in * d_ff
+    ws = torch.empty(api.agc_gated_workspace_bytes(tokens, d_in, d_ff, 3), dtype=torch.uint8, device="cuda")
+
+    def call():
+        G = torch.empty(3, 2 * half, device="cuda")
+        dx = torch.empty(tokens, d_in, dtype=torch.bfloat16, device="cuda")
+        api.agc_gated_partial_gradients(x, wg, wu, "silu", dh, ends, dx, G[:, :half], G[:, half:], ws)
+        return G, dx
+
+    G, dx = call()
+    x[45, 7] = bad
+    dh[50, 3] = bad
+    H, dy = call()
+    assert torch.equal(G[0], H[0]) and torch.equal(G[2], H[2]) and not torch.isfinite(H[1]).all()
+    others = torch.ones(tokens, dtype=torch.bool, device="cuda")
+    others[[45, 50]] = False
+    assert torch.equal(dx[others], dy[others]) and not torch.isfinite(dy[45].float()).all()
+
+
+@pytest.mark.gpu
 def test_zero_tokens():
     import torch
     bf16 = torch.bfloat16
