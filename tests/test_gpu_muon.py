@@ -98,7 +98,7 @@ def test_orthogonal_factor_of_long_matrices(rows, cols, steps):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows,cols,mats", [(1300, 1290, 2), (1025, 3001, 5), (4097, 2050, 4)])
+@pytest.mark.parametrize("rows,cols,mats", [(1300, 1290, 2), (1025, 3001, 5), (4097, 2050, 4), (1111, 1200, 12)])
 def test_orthogonal_factor_of_large_matrices(rows, cols, mats):
     """Every tile size and its edges; the 64-bit products are taken on the GPU."""
     import torch
