@@ -8,12 +8,12 @@
 //   da = dh u act'(a), du = dh act(a)          in the same pass
 //   dx = da Wg + du Wu                          one product over 2 F
 //   dWg_p = da_p^T x_p, dWu_p = du_p^T x_p      one product of 2 F rows a partition, written into row p of G
-// da and du enter dx rounded to bfloat16, as dx itself is.  They enter G, which is binary32, as pairs of binary16 (22
-// bits), and x as binary16, which its 8 bits fit: two products, where three of bfloat16 would be needed for more than
-// 16 bits, and one would leave up to 2^-8 in every term of G.  The narrow range of binary16 is met by a power of two for
-// every partition, from the largest finite magnitudes of its dh and x and of the weights: they bound u and act(a), hence
-// da and du, and put the bound at 2^15.  Values of up to 2^-18 of the bound keep all 22 bits, smaller ones what lies above
-// 2^-40 of it; the bound is some 2^13 above the usual value for random operands 2000 wide.
+// da and du enter dx rounded to bfloat16, as dx itself is.  They enter G, which is binary32, with all their bits: as three
+// bfloat16 parts, three products with x, which is bfloat16 as it is.  Any form with fewer bits of exponent (pairs of binary16
+// scaled by a power of two, two products) loses what lies far below the largest operands that its scale was made for: one
+// token's large x, masked or not, would cost its whole partition's gradient its bits.  bfloat16 has binary32's exponents; the
+// lowest part alone could fall below them, so values are lifted by 2^23 (kLift), which makes the smallest binary32 the smallest
+// normal bfloat16.  da, du and G of 2^105 and more leave binary32 that way and become infinite.
 // The tile loop wants both operands contiguous along the sum: x and the weights are turned by passes of their own, da
 // and du are written both ways.  A partition starts at a multiple of 32 in the turned order, the places between are
 // zeros; `map` gives each place its token, or -1.
@@ -26,26 +26,11 @@ namespace {
 
 constexpr int kBlock = 256;
 
-// Largest magnitudes, as bfloat16 bits, of finite values: of dh and x of each partition, of Wg and of Wu.
-struct Bounds {
-    uint32_t* most;      // [2 * k + 2]
-    int k;
-    int width;           // log2 of d_in, rounded up
-    static __device__ __forceinline__ int power(uint32_t bits) { return (int)(bits >> 7) - 126; }   // below 2^power
-    // powers of two by which da and du, and x, of partition p are multiplied
-    __device__ __forceinline__ int of_x(int p) const { return 15 - power(most[2 * p + 1]); }
-    __device__ __forceinline__ int of_grad(int p) const
-    {
-        const int wg = power(most[2 * k]), wu = power(most[2 * k + 1]);
-        // |u|, |act(a)| <= d_in max|x| max|w|; |act'| < 2
-        return 14 - power(most[2 * p]) - power(most[2 * p + 1]) - (wg > wu ? wg : wu) - width;
-    }
-};
+constexpr float kLift = 8388608.0f;   // 2^23, of da and du as they enter G
 
 struct Rows {
     const uint16_t* p;
     int64_t ld;
-    int width;
 };
 
 // what the kernels know of the partitions: first place and first token of each
@@ -145,14 +130,11 @@ struct PackRows {
 
 struct PlaceMap {
     int* map;
-    uint16_t* part;
-    uint32_t* most;      // cleared for the bounds
     int places;
     GatedParts parts;
-    __device__ __forceinline__ void run(int block, int blocks) const
+    __device__ __forceinline__ void run(int block) const
     {
         const int i = block * kBlock + threadIdx.x;
-        for (int j = i; j < 2 * parts.k + 2; j += blocks * kBlock) most[j] = 0;
         if (i >= places) return;
         int lo = 0, hi = parts.k - 1;   // the last partition that starts at or before i
         while (lo < hi) {
@@ -162,21 +144,16 @@ struct PlaceMap {
         }
         const int t = parts.token[lo] + (i - parts.place[lo]);
         map[i] = t < parts.token[lo + 1] ? t : -1;
-        part[i] = (uint16_t)lo;
     }
 };
 
 // dst row c = column c of src, along the rows of src (through `map`, if given; -1 and rows past the end are zeros),
-// `up` of them.  TWICE: as binary16 in groups of 32, each twice, as the second operand of pairs, scaled by what the
-// bounds say.
-template <bool TWICE>
+// `up` of them.
 struct Turn {
     const uint16_t* src;
     int64_t ld;
     int rows, cols, up;
     const int* map;
-    const uint16_t* part;
-    Bounds bounds;
     char* dst;
     int64_t pitch;
     __device__ __forceinline__ void run(int r0, int c0) const
@@ -199,22 +176,7 @@ struct Turn {
             tile_u32x4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = (uint32_t)tile[r + 2 * e][c] | ((uint32_t)tile[r + 2 * e + 1][c] << 16);
-            char* row = dst + (int64_t)(c0 + c) * pitch;
-            const int at = r0 + r;
-            if (TWICE) {
-                const int power = bounds.of_x(part[at]);
-                float f[8];
-                bf16_unpack8(v, f);
-                f16x8 half;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) half[e] = (_Float16)ldexpf(f[e], power);
-                v = __builtin_bit_cast(tile_u32x4, half);
-                char* p = row + (int64_t)(at >> 5) * 128 + (at & 31) * 2;
-                *reinterpret_cast<tile_u32x4*>(p) = v;
-                *reinterpret_cast<tile_u32x4*>(p + 64) = v;
-            } else {
-                *reinterpret_cast<tile_u32x4*>(row + (int64_t)at * 2) = v;
-            }
+            *reinterpret_cast<tile_u32x4*>(dst + (int64_t)(c0 + c) * pitch + (int64_t)(r0 + r) * 2) = v;
         }
     }
 };
@@ -226,7 +188,7 @@ struct Prepare {
     int pack_blocks[3];
     PlaceMap map;
     int map_blocks;
-    Turn<false> turn[2];
+    Turn turn[2];
     int turn_down, turn_blocks;   // of one
     int total() const { return pack_blocks[0] + pack_blocks[1] + pack_blocks[2] + map_blocks + 2 * turn_blocks; }
 };
@@ -238,80 +200,13 @@ __global__ __launch_bounds__(kBlock) void k_gated_prepare(const Prepare a)
         if (block < a.pack_blocks[i]) return a.pack[i].run(block);
         block -= a.pack_blocks[i];
     }
-    if (block < a.map_blocks) return a.map.run(block, a.map_blocks);
+    if (block < a.map_blocks) return a.map.run(block);
     block -= a.map_blocks;
     const int which = block >= a.turn_blocks ? 1 : 0, at = block - which * a.turn_blocks, across = at / a.turn_down;
     a.turn[which].run((at - across * a.turn_down) * 64, across * 64);
 }
 
-__global__ __launch_bounds__(kBlock) void k_turn_tokens(const Turn<true> a) { a.run(blockIdx.x * 64, blockIdx.y * 64); }
-
-// The bounds.  A workgroup takes eight places of one partition, or eight rows of the weights.  Bound by memory: 8192 x
-// (2048 + 5632) and 2 x 5632 x 2048 values in 35 us, 4.9 TB/s.
-__global__ __launch_bounds__(kBlock) void k_gated_bounds(const Rows x, const Rows dh, const Rows wg, const Rows wu, int places,
-                                                         int d_ff, const int* map, const uint16_t* part, const Bounds b)
-{
-    __shared__ uint32_t wave_most[4];
-    const int token_blocks = places / 8;
-    auto most_of = [&](const Rows& rows, int first, int end, const int* through, uint32_t* to) {
-        const int width = rows.width;
-        uint32_t most = 0;
-        auto look = [&](const tile_u32x4& v) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t lo = v[e] & 0x7FFFu, hi = (v[e] >> 16) & 0x7FFFu;
-                most = lo < 0x7F80u && lo > most ? lo : most;
-                most = hi < 0x7F80u && hi > most ? hi : most;
-            }
-        };
-        const uint16_t* row[8];
-        bool whole = (width & 7) == 0;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {   // a row that is not there: the first one that is, or none
-            int at = first + r < end ? (through ? through[first + r] : first + r) : -1;
-            if (at < 0) at = through ? through[first] : first;   // a partition's places begin with its tokens
-            row[r] = at < 0 ? nullptr : rows.p + at * rows.ld;
-            whole = whole && at >= 0 && aligned16(row[r]);
-        }
-        if (whole) {
-            for (int c = threadIdx.x * 8; c < width; c += kBlock * 8) {
-                tile_u32x4 v[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] = *reinterpret_cast<const tile_u32x4*>(row[r] + c);
-#pragma unroll
-                for (int r = 0; r < 8; ++r) look(v[r]);
-            }
-        } else if (row[0]) {
-            for (int c = threadIdx.x; c < width; c += kBlock) {
-                uint32_t v[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] = row[r][c];
-#pragma unroll
-                for (int r = 0; r < 8; r += 4) look(tile_u32x4{v[r], v[r + 1], v[r + 2], v[r + 3]});
-            }
-        }
-        for (int d = 32; d >= 1; d >>= 1) {
-            const uint32_t other = __shfl_xor(most, d);
-            most = other > most ? other : most;
-        }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) wave_most[threadIdx.x >> 6] = most;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < 4; ++w) most = wave_most[w] > most ? wave_most[w] : most;
-            if (most) atomicMax(to, most);   // the largest, in whatever order they come
-        }
-    };
-    const int id = blockIdx.x;
-    if (id < token_blocks) {
-        const int p = part[id * 8];
-        most_of(dh, id * 8, places, map, b.most + 2 * p);
-        most_of(x, id * 8, places, map, b.most + 2 * p + 1);
-    } else {
-        most_of(wg, (id - token_blocks) * 8, d_ff, nullptr, b.most + 2 * b.k);
-        most_of(wu, (id - token_blocks) * 8, d_ff, nullptr, b.most + 2 * b.k + 1);
-    }
-}
+__global__ __launch_bounds__(kBlock) void k_turn_tokens(const Turn a) { a.run(blockIdx.x * 64, blockIdx.y * 64); }
 
 // ------------------------------------------------------------------ few tokens
 // Up to NT * 16 tokens: bound by the one read of the weights.  A workgroup takes 16 rows of Wg and of Wu, its four
@@ -415,10 +310,8 @@ struct GateJob {
     int64_t lddh;
     char* by_token;                   // places x 2 fp: da | du
     int fp;
-    char* by_feature;                 // 2 d_ff rows of pairs along the places
+    char* by_feature;                 // 2 d_ff rows of three parts along the places, lifted
     int64_t pitch;
-    const uint16_t* part;
-    Bounds bounds;
     int mt, nt, side, total;
 
     __device__ __forceinline__ void place(int id, TilePos& p) const
@@ -479,12 +372,11 @@ struct GateJob {
         const int run = (lane & 7) * 8, at = mb + run;
         const int c = it * 8 + (lane >> 3), ff = nb / 2 + (c >> 5) * 16 + (c & 15);
         if (ff >= d_ff || at >= n_rows) return;   // n_rows is a multiple of 32
-        const int power = bounds.of_grad(part[at]);
         float v[8];
         piece_col8(s, run, c, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = ldexpf(v[e], power);
-        split_store8(by_feature + (int64_t)(((c & 16) ? d_ff : 0) + ff) * pitch, at, v);
+        for (int e = 0; e < 8; ++e) v[e] *= kLift;
+        parts3_store8(by_feature + (int64_t)(((c & 16) ? d_ff : 0) + ff) * pitch, at, v);
     }
 };
 
@@ -528,16 +420,15 @@ struct InputJob {
 
 // Row p of G: [da | du]_p^T x_p
 struct WeightJob {
-    static constexpr TilePair kPair = kHalf;
+    static constexpr TilePair kPair = kParts3;
     static constexpr int kRowParts = 8;
     static constexpr bool kTurned = false;
     const char *a, *b;        // 2 d_ff and d_in rows along the places
-    int64_t pitch;
+    int64_t places;
     int d_ff, d_in;
     bool whole;               // rows of G in units of four values, 16-byte aligned
     float *gate, *up;
     int64_t ldg;
-    Bounds bounds;
     int mt, nt, side, total;
     GatedParts parts;
 
@@ -552,15 +443,14 @@ struct WeightJob {
     }
     __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
     {
-        return a + (int64_t)(p.m0 + r < 2 * d_ff ? p.m0 + r : 2 * d_ff - 1) * pitch + (int64_t)parts.place[p.batch] * 4;
+        return a + ((p.m0 + r < 2 * d_ff ? p.m0 + r : 2 * d_ff - 1) * places + parts.place[p.batch]) * 6;
     }
     __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const
     {
-        return b + (int64_t)(p.n0 + r < d_in ? p.n0 + r : d_in - 1) * pitch + (int64_t)parts.place[p.batch] * 4;
+        return b + ((p.n0 + r < d_in ? p.n0 + r : d_in - 1) * places + parts.place[p.batch]) * 2;
     }
     __device__ __forceinline__ void rows(const TilePos& p, int mb, int nb, const float* s, int it, int lane) const
     {
-        const int power = p.steps > 0 ? -bounds.of_x(p.batch) - bounds.of_grad(p.batch) : 0;
         auto at = [&](int row) {
             return (row < d_ff ? gate + (int64_t)row * d_in : up + (int64_t)(row - d_ff) * d_in) + p.batch * ldg;
         };
@@ -570,7 +460,7 @@ struct WeightJob {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int r = it * 8 + e;
-                if (mb + r < 2 * d_ff && nb + lane < d_in) at(mb + r)[nb + lane] = ldexpf(s[piece_at(r, lane)], power);
+                if (mb + r < 2 * d_ff && nb + lane < d_in) at(mb + r)[nb + lane] = s[piece_at(r, lane)] * (1.0f / kLift);
             }
             return;
         }
@@ -579,7 +469,7 @@ struct WeightJob {
         float v[8];
         piece_row8(s, r, run, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = ldexpf(v[e], power);
+        for (int e = 0; e < 8; ++e) v[e] *= 1.0f / kLift;
         float* o = at(row) + c;
         *reinterpret_cast<tile_f32x4*>(o) = tile_f32x4{v[0], v[1], v[2], v[3]};
         if (c + 4 < d_in) *reinterpret_cast<tile_f32x4*>(o + 4) = tile_f32x4{v[4], v[5], v[6], v[7]};
@@ -606,10 +496,10 @@ Rows whole_steps(const void* src, int64_t ld, int64_t rows, int width, char*& ro
     uint16_t* mine = reinterpret_cast<uint16_t*>(room);
     room += round_up(rows * up * 2, 256);
     const uint16_t* p = static_cast<const uint16_t*>(src);
-    if (up == width && takes_whole_loads(src, ld)) return Rows{p, ld, width};
+    if (up == width && takes_whole_loads(src, ld)) return Rows{p, ld};
     prepare.pack[i] = PackRows{p, ld, (int)rows, width, up, mine};
     prepare.pack_blocks[i] = (int)((rows + 7) / 8);
-    return Rows{mine, up, up};
+    return Rows{mine, up};
 }
 
 hipError_t launch_prepare(const Prepare& prepare, hipStream_t stream)
@@ -639,14 +529,14 @@ hipError_t launch_few(const GatedCall& c, hipStream_t stream)
 
 }  // namespace
 
-// packed x, Wg, Wu | map, partition of each place, bounds | da, du by token | by feature | x turned | weights turned
+// packed x, Wg, Wu | map | da, du by token | by feature | x turned | weights turned
 int64_t gated_workspace_bytes(int64_t tokens, int d_in, int d_ff, int k_parts)
 {
     int64_t bytes = packed_bytes(tokens, d_in, d_ff);
     if (k_parts > 0) {
         const int64_t places = round_up(tokens + 31 * (int64_t)k_parts, 32), fp = round_up(d_ff, 64);
-        bytes += round_up(places * 4, 256) + round_up(places * 2, 256) + round_up((2 * k_parts + 2) * 4, 256) + round_up(places * fp * 4, 256) + round_up(2 * d_ff * places * 4, 256) +
-                 round_up(d_in * places * 4, 256) + round_up(d_in * fp * 4, 256);
+        bytes += round_up(places * 4, 256) + round_up(places * fp * 4, 256) + round_up(2 * d_ff * places * 6, 256) +
+                 round_up(d_in * places * 2, 256) + round_up(d_in * fp * 4, 256);
     }
     return bytes > 256 ? bytes : 256;
 }
@@ -685,7 +575,7 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         parts.place[p + 1] = parts.place[p] + (int)round_up(parts.token[p + 1] - parts.token[p], 32);
     }
     const int places = parts.place[c.k_parts];
-    const int64_t fp = round_up(c.d_ff, 64), pitch = (int64_t)places * 4;
+    const int64_t fp = round_up(c.d_ff, 64);
     char* room = c.workspace;
     auto take = [&](int64_t bytes) {
         char* p = room;
@@ -693,28 +583,22 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         return p;
     };
     char *by_feature = nullptr, *x_turned = nullptr;
-    Bounds bounds{nullptr, c.k_parts, 0};
-    while ((1 << bounds.width) < c.d_in) ++bounds.width;
     hipError_t e = hipSuccess;
     if (places > 0) {
         Prepare prepare{};
         const Rows x = whole_steps(c.x, c.ldx, c.tokens, c.d_in, room, prepare, 0);
         const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, prepare, 1);
         const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, prepare, 2);
-        const Rows dh{static_cast<const uint16_t*>(c.dh), c.lddh, c.d_ff};
         int* map = reinterpret_cast<int*>(take((int64_t)places * 4));
-        uint16_t* part = reinterpret_cast<uint16_t*>(take((int64_t)places * 2));
-        bounds.most = reinterpret_cast<uint32_t*>(take((2 * c.k_parts + 2) * 4));
         char* by_token = take(places * fp * 4);
-        by_feature = take(2 * c.d_ff * pitch);
-        x_turned = take(c.d_in * pitch);
+        by_feature = take((int64_t)places * 2 * c.d_ff * 6);
+        x_turned = take((int64_t)places * c.d_in * 2);
         char* w_turned = take(c.d_in * fp * 4);
         const int across = (c.d_in + 63) / 64;
-        prepare.map = PlaceMap{map, part, bounds.most, places, parts};
+        prepare.map = PlaceMap{map, places, parts};
         prepare.map_blocks = (places + kBlock - 1) / kBlock;
         if (c.dx) {
-            prepare.turn[0] = Turn<false>{static_cast<const uint16_t*>(c.wg), c.ldw, c.d_ff, c.d_in, (int)fp, nullptr, nullptr,
-                                          bounds, w_turned, fp * 4};
+            prepare.turn[0] = Turn{static_cast<const uint16_t*>(c.wg), c.ldw, c.d_ff, c.d_in, (int)fp, nullptr, w_turned, fp * 4};
             prepare.turn[1] = prepare.turn[0];
             prepare.turn[1].src = static_cast<const uint16_t*>(c.wu), prepare.turn[1].dst = w_turned + fp * 2;
             prepare.turn_down = (int)(fp / 64);
@@ -722,19 +606,16 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         }
         e = launch_prepare(prepare, stream);
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(k_gated_bounds, dim3(places / 8 + (c.d_ff + 7) / 8), dim3(kBlock), 0, stream, x, dh, wg, wu, places,
-                           c.d_ff, map, part, bounds);
         hipLaunchKernelGGL(k_turn_tokens, dim3((places + 63) / 64, across), dim3(kBlock), 0, stream,
-                           Turn<true>{static_cast<const uint16_t*>(c.x), c.ldx, places, c.d_in, places, map, part, bounds,
-                                      x_turned, pitch});
+                           Turn{static_cast<const uint16_t*>(c.x), c.ldx, places, c.d_in, places, map, x_turned,
+                                (int64_t)places * 2});
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         GateJob<true> j{};
         j.x = x.p, j.ldx = x.ld, j.wg = wg.p, j.ldg = wg.ld, j.wu = wu.p, j.ldu = wu.ld;
         j.n_rows = places, j.d_ff = c.d_ff, j.steps = (int)(round_up(c.d_in, 64) / 64), j.act = act, j.map = map;
-        j.dh = dh.p, j.lddh = dh.ld;
-        j.by_token = by_token, j.fp = (int)fp, j.by_feature = by_feature, j.pitch = pitch;
-        j.part = part, j.bounds = bounds;
+        j.dh = static_cast<const uint16_t*>(c.dh), j.lddh = c.lddh;
+        j.by_token = by_token, j.fp = (int)fp, j.by_feature = by_feature, j.pitch = (int64_t)places * 6;
         e = launch_product(j, 1, places, fp * 2, j.steps, stream);
         if (e != hipSuccess) return e;
         if (c.dx) {
@@ -744,10 +625,10 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         }
     }
     WeightJob w{};
-    w.a = by_feature, w.b = x_turned, w.pitch = pitch, w.d_ff = c.d_ff, w.d_in = c.d_in;
+    w.a = by_feature, w.b = x_turned, w.places = places, w.d_ff = c.d_ff, w.d_in = c.d_in;
     w.whole = c.d_in % 4 == 0 && c.ldg % 4 == 0 && reinterpret_cast<uintptr_t>(c.g_gate) % 16 == 0 &&
               reinterpret_cast<uintptr_t>(c.g_up) % 16 == 0;
-    w.gate = c.g_gate, w.up = c.g_up, w.ldg = c.ldg, w.parts = parts, w.bounds = bounds;
+    w.gate = c.g_gate, w.up = c.g_up, w.ldg = c.ldg, w.parts = parts;
     return launch_product(w, c.k_parts, 2 * (int64_t)c.d_ff, c.d_in, places / 32 / c.k_parts, stream);
 }
 

@@ -1,17 +1,20 @@
 // Matrix products of the gated block and of the Newton-Schulz products: one tile loop for all of them.
 //
 // Every product here is C[m,n] = sum_k A[m,k] * B[n,k] with 16-bit operands whose rows are contiguous in k,
-// held in groups of 128 bytes ("k-steps"); operands that come in another order or with another end are laid out
-// by a pass of their own before.  A k-step is either
-//   plain   64 values, bfloat16 (or binary16: half):    C += A0 B0 + A1 B1     (its two halves of 32)
+// held in groups ("k-steps") of parts of 64 bytes, 32 values each; operands that come in another order or with another
+// end are laid out by a pass of their own before.  A k-step is either
+//   plain   64 bfloat16 values of both operands:       C += A0 B0 + A1 B1     (its two halves of 32)
 //   split   32 values as binary16 pairs, 32 high parts and 32 low parts (x = hi + lo to 22 bits):
 //                                                      C += A0 B0 + A0 B1 + A1 B0   (lo * lo is below 2^-22)
-// so that the same loads feed both.  Products are v_mfma_f32_16x16x32, sums binary32.
+//   parts3  32 binary32 values of A as three bfloat16 parts (v = A0 + A1 + A2, all 24 bits), 32 bfloat16 values of B:
+//                                                      C += A0 B0 + A1 B0 + A2 B0
+// Products are v_mfma_f32_16x16x32, sums binary32.
 //
 // A workgroup of WM x WN waves owns a TM x TN tile of C and holds two k-steps of both operands in LDS, filled by
-// loads that go from memory to LDS directly while the other k-step is multiplied.  Row r of a k-step lies at
+// loads that go from memory to LDS directly while the other k-step is multiplied.  Row r of a k-step of two parts lies at
 // r * 128 bytes with its eight 16-byte chunks permuted by r & 7, which the loads do by choosing whose chunk a lane
-// fetches: the sixteen rows that a wave reads at once then fall on all banks.
+// fetches: the sixteen rows that a wave reads at once then fall on all banks.  Operands of one or three parts lie part
+// by part, two rows of 64 bytes in 128, these eight chunks permuted in the same way.
 // After the loop every wave stages its part of C, 64 x 64 values at a time, in its own 16 KB of the same LDS and
 // hands it to the job, which reads it along rows or along columns, eight values a lane, and writes what it needs.
 #pragma once
@@ -27,7 +30,14 @@ typedef __bf16 tile_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float tile_f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t tile_u32x4 __attribute__((ext_vector_type(4)));
 
-enum TilePair { kPlain, kHalf, kSplit };
+enum TilePair { kPlain, kSplit, kParts3 };
+
+// 64-byte parts of a row's k-step
+template <TilePair PAIR>
+struct TileStep {
+    static constexpr bool kByPart = PAIR == kParts3;
+    static constexpr int kA = PAIR == kParts3 ? 3 : 2, kB = kByPart ? 1 : 2;
+};
 
 struct TilePos {
     int m0, n0;    // first row and column of the tile
@@ -151,11 +161,33 @@ __device__ __forceinline__ void split_load8(const char* row, int k, float v[8])
     for (int i = 0; i < 8; ++i) v[i] = (float)hi[i] + (float)lo[i];
 }
 
+// Eight binary32 values as three bfloat16 parts at element k (a multiple of 8) of a row of A of parts3.  The first part is cut
+// off, so that it cannot overflow, and leaves 16 bits; the second, rounded, leaves 8, which the third holds.  Infinity has no rest.
+__device__ __forceinline__ void parts3_store8(char* row, int k, const float v[8])
+{
+    tile_u32x4 first;
+    float rest[8], second[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = __float_as_uint(v[i]);
+        rest[i] = (bits & 0x7FFFFFFFu) == 0x7F800000u ? 0.0f : v[i] - __uint_as_float(bits & 0xFFFF0000u);
+        if (i & 1) first[i >> 1] = (__float_as_uint(v[i - 1]) >> 16) | (bits & 0xFFFF0000u);
+    }
+    const tile_u32x4 mid = bf16_pack8(rest);
+    bf16_unpack8(mid, second);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] -= second[i];
+    char* p = row + (int64_t)(k >> 5) * 192 + (k & 31) * 2;
+    *reinterpret_cast<tile_u32x4*>(p) = first;
+    *reinterpret_cast<tile_u32x4*>(p + 64) = mid;
+    *reinterpret_cast<tile_u32x4*>(p + 128) = bf16_pack8(rest);
+}
+
 // ------------------------------------------------------------------ the loop
 template <TilePair PAIR>
 __device__ __forceinline__ tile_f32x4 tile_mfma(const tile_u32x4& a, const tile_u32x4& b, const tile_f32x4& c)
 {
-    if constexpr (PAIR == kPlain)
+    if constexpr (PAIR != kSplit)
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(tile_bf16x8, a),
                                                        __builtin_bit_cast(tile_bf16x8, b), c, 0, 0, 0);
     else
@@ -167,6 +199,61 @@ __device__ __forceinline__ void load16_to_lds(const char* src, char* dst)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                      (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+// Where the 16 rows of a fragment lie in LDS: the chunk of this lane (row lane & 15, values (lane >> 4) * 8 on) of the first part;
+// the second part of rows of two: ^ 64.
+template <bool BY_PART>
+__device__ __forceinline__ int tile_chunk(int lane)
+{
+    const int row = lane & 15, q = lane >> 4;
+    if (BY_PART) return (row >> 1) * 128 + ((((row & 1) * 4 + q) ^ (row >> 1)) << 4);
+    return row * 128 + ((q ^ (row & 7)) << 4);
+}
+
+// One k-step of FM x FN blocks of 16 x 16, operands in LDS; parts of A that lie by part are `plane` bytes apart.
+template <TilePair PAIR, int FM, int FN>
+__device__ __forceinline__ void tile_multiply(const char* a, const char* b, int plane, int at0, int at1, tile_f32x4 (&acc)[FM][FN])
+{
+    if constexpr (TileStep<PAIR>::kByPart) {
+        constexpr int kA = TileStep<PAIR>::kA;
+        tile_u32x4 b0[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) b0[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 1024 + at0);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            tile_u32x4 part[kA];
+#pragma unroll
+            for (int p = 0; p < kA; ++p) part[p] = *reinterpret_cast<const tile_u32x4*>(a + p * plane + i * 1024 + at0);
+#pragma unroll
+            for (int p = 0; p < kA; ++p)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = tile_mfma<PAIR>(part[p], b0[j], acc[i][j]);
+        }
+        return;
+    }
+    tile_u32x4 b0[FN], b1[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        b0[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at0);
+        b1[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at1);
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const tile_u32x4 a0 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at0);
+        const tile_u32x4 a1 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at1);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = tile_mfma<PAIR>(a0, b0[j], acc[i][j]);
+        if constexpr (PAIR != kSplit) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = tile_mfma<PAIR>(a1, b1[j], acc[i][j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = tile_mfma<PAIR>(a0, b1[j], acc[i][j]);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = tile_mfma<PAIR>(a1, b0[j], acc[i][j]);
+        }
+    }
 }
 
 // JOB: kPair; void place(int id, TilePos&); const char* a_row(pos, r), b_row(pos, r): where row r of the tile starts
@@ -182,11 +269,15 @@ __device__ __forceinline__ void load16_to_lds(const char* src, char* dst)
 template <class JOB, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_tile(const JOB job)
 {
+    using Step = TileStep<JOB::kPair>;
     constexpr int kThreads = WM * WN * 64;
     constexpr int kWaveM = TM / WM, kWaveN = TN / WN, kFm = kWaveM / 16, kFn = kWaveN / 16;
-    constexpr int kStep = (TM + TN) * 128;
+    constexpr int kStep = (TM * Step::kA + TN * Step::kB) * 64;
     constexpr int kLds = 2 * kStep > WM * WN * 16384 ? 2 * kStep : WM * WN * 16384;
-    constexpr int kIssueA = TM * 8 / kThreads, kIssueB = TN * 8 / kThreads, kIssueRows = kThreads / 8;
+    // a load fills 128 bytes: a row of two parts, or two rows of one part
+    constexpr int kRowsOf128 = Step::kByPart ? 2 : 1, kIssueLines = kThreads / 8;
+    constexpr int kIssueA = TM / kRowsOf128 / kIssueLines, kIssueB = TN / kRowsOf128 / kIssueLines;
+    constexpr int kLoadsA = Step::kByPart ? Step::kA : 1;   // of a lane for each of kIssueA
     static_assert(kWaveM % 64 == 0 && kWaveN == 64, "a wave stages pieces of 64 x 64");
     __shared__ __attribute__((aligned(1024))) char lds[kLds];
 
@@ -197,23 +288,25 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_tile(const JOB job)
     const int wm = wave / WN, wn = wave - wm * WN;
 
     const char *src_a[kIssueA], *src_b[kIssueB];
-    const int chunk = ((tid & 7) ^ ((tid >> 3) & 7)) * 16;
+    const int slot = (tid & 7) ^ ((tid >> 3) & 7);
+    const int sub = Step::kByPart ? slot >> 2 : 0, chunk = (Step::kByPart ? slot & 3 : slot) * 16;
 #pragma unroll
-    for (int i = 0; i < kIssueA; ++i) src_a[i] = job.a_row(pos, i * kIssueRows + (tid >> 3)) + chunk;
+    for (int i = 0; i < kIssueA; ++i) src_a[i] = job.a_row(pos, (i * kIssueLines + (tid >> 3)) * kRowsOf128 + sub) + chunk;
 #pragma unroll
-    for (int i = 0; i < kIssueB; ++i) src_b[i] = job.b_row(pos, i * kIssueRows + (tid >> 3)) + chunk;
+    for (int i = 0; i < kIssueB; ++i) src_b[i] = job.b_row(pos, (i * kIssueLines + (tid >> 3)) * kRowsOf128 + sub) + chunk;
 
     auto issue = [&](int half) {
         char* base = lds + half * kStep + wave * 1024;
 #pragma unroll
         for (int i = 0; i < kIssueA; ++i) {
-            load16_to_lds(src_a[i], base + i * kIssueRows * 128);
-            src_a[i] += 128;
+#pragma unroll
+            for (int p = 0; p < kLoadsA; ++p) load16_to_lds(src_a[i] + p * 64, base + p * TM * 64 + i * kIssueLines * 128);
+            src_a[i] += Step::kA * 64;
         }
 #pragma unroll
         for (int i = 0; i < kIssueB; ++i) {
-            load16_to_lds(src_b[i], base + TM * 128 + i * kIssueRows * 128);
-            src_b[i] += 128;
+            load16_to_lds(src_b[i], base + TM * Step::kA * 64 + i * kIssueLines * 128);
+            src_b[i] += Step::kB * 64;
         }
     };
 
@@ -223,33 +316,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_tile(const JOB job)
 #pragma unroll
         for (int j = 0; j < kFn; ++j) acc[i][j] = tile_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const int row = (lane & 15) * 128, q = lane >> 4;
-    const int at0 = row + ((q ^ (lane & 7)) << 4), at1 = row + (((4 + q) ^ (lane & 7)) << 4);
+    const int q = lane >> 4;
+    const int at0 = tile_chunk<Step::kByPart>(lane), at1 = at0 ^ 64;
     auto multiply = [&](int half) {
-        const char* a = lds + half * kStep + wm * kWaveM * 128;
-        const char* b = lds + half * kStep + TM * 128 + wn * kWaveN * 128;
-        tile_u32x4 b0[kFn], b1[kFn];
-#pragma unroll
-        for (int j = 0; j < kFn; ++j) {
-            b0[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at0);
-            b1[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at1);
-        }
-#pragma unroll
-        for (int i = 0; i < kFm; ++i) {
-            const tile_u32x4 a0 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at0);
-            const tile_u32x4 a1 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at1);
-#pragma unroll
-            for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a0, b0[j], acc[i][j]);
-            if constexpr (JOB::kPair != kSplit) {
-#pragma unroll
-                for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a1, b1[j], acc[i][j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a0, b1[j], acc[i][j]);
-#pragma unroll
-                for (int j = 0; j < kFn; ++j) acc[i][j] = tile_mfma<JOB::kPair>(a1, b0[j], acc[i][j]);
-            }
-        }
+        const char* a = lds + half * kStep + wm * kWaveM * (128 / kRowsOf128);
+        const char* b = lds + half * kStep + TM * Step::kA * 64 + wn * kWaveN * (128 / kRowsOf128);
+        tile_multiply<JOB::kPair, kFm, kFn>(a, b, TM * 64, at0, at1, acc);
     };
 
     if (pos.steps > 0) issue(0);
@@ -292,7 +364,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_tile(const JOB job)
 template <class JOB>
 __global__ __launch_bounds__(256, 1) void k_tile_cut(const JOB job)
 {
-    constexpr int kStep = 128 * 128;
+    using Step = TileStep<JOB::kPair>;
+    constexpr int kStep = 64 * (Step::kA + Step::kB) * 64;
+    constexpr int kRowsOf128 = Step::kByPart ? 2 : 1, kIssue = 8 / kRowsOf128, kLoadsA = Step::kByPart ? Step::kA : 1;
     __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * kStep];
     TilePos pos;
     job.place((int)blockIdx.x, pos);
@@ -300,28 +374,33 @@ __global__ __launch_bounds__(256, 1) void k_tile_cut(const JOB job)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     char* mine = lds + wave * 2 * kStep;
 
-    const char *src_a[8], *src_b[8];
-    const int chunk = ((lane & 7) ^ (lane >> 3)) * 16 + wave * 128;
+    const char *src_a[kIssue], *src_b[kIssue];
+    const int slot = (lane & 7) ^ (lane >> 3);
+    const int sub = Step::kByPart ? slot >> 2 : 0, chunk = (Step::kByPart ? slot & 3 : slot) * 16;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        src_a[i] = job.a_row(pos, i * 8 + (lane >> 3)) + chunk;
-        src_b[i] = job.b_row(pos, i * 8 + (lane >> 3)) + chunk;
+    for (int i = 0; i < kIssue; ++i) {
+        const int r = (i * 8 + (lane >> 3)) * kRowsOf128 + sub;
+        src_a[i] = job.a_row(pos, r) + chunk + wave * Step::kA * 64;
+        src_b[i] = job.b_row(pos, r) + chunk + wave * Step::kB * 64;
     }
     auto issue = [&](char* base) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            load16_to_lds(src_a[i], base + i * 1024);
-            load16_to_lds(src_b[i], base + 8192 + i * 1024);
-            src_a[i] += 512, src_b[i] += 512;
+        for (int i = 0; i < kIssue; ++i) {
+#pragma unroll
+            for (int p = 0; p < kLoadsA; ++p) load16_to_lds(src_a[i] + p * 64, base + p * 4096 + i * 1024);
+            load16_to_lds(src_b[i], base + Step::kA * 4096 + i * 1024);
+            src_a[i] += 4 * Step::kA * 64, src_b[i] += 4 * Step::kB * 64;
         }
     };
+    constexpr int kLoads = kIssue * (kLoadsA + 1);   // of one k-step
+    static_assert(kLoads == 16, "the counted wait below");
     tile_f32x4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = tile_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int row = (lane & 15) * 128, q = lane >> 4;
-    const int at0 = row + ((q ^ (lane & 7)) << 4), at1 = row + (((4 + q) ^ (lane & 7)) << 4);
+    const int q = lane >> 4;
+    const int at0 = tile_chunk<Step::kByPart>(lane), at1 = at0 ^ 64;
 
     if (wave < pos.steps) issue(mine);
     for (int k = wave, half = 0; k < pos.steps; k += 4, half ^= 1) {
@@ -332,28 +411,8 @@ __global__ __launch_bounds__(256, 1) void k_tile_cut(const JOB job)
         } else {
             __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
-        const char *a = mine + half * kStep, *b = a + 8192;
-        tile_u32x4 b0[4], b1[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            b0[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at0);
-            b1[j] = *reinterpret_cast<const tile_u32x4*>(b + j * 2048 + at1);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const tile_u32x4 a0 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at0);
-            const tile_u32x4 a1 = *reinterpret_cast<const tile_u32x4*>(a + i * 2048 + at1);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                acc[i][j] = tile_mfma<JOB::kPair>(a0, b0[j], acc[i][j]);
-                if constexpr (JOB::kPair != kSplit) {
-                    acc[i][j] = tile_mfma<JOB::kPair>(a1, b1[j], acc[i][j]);
-                } else {
-                    acc[i][j] = tile_mfma<JOB::kPair>(a0, b1[j], acc[i][j]);
-                    acc[i][j] = tile_mfma<JOB::kPair>(a1, b0[j], acc[i][j]);
-                }
-            }
-        }
+        const char* a = mine + half * kStep;
+        tile_multiply<JOB::kPair, 4, 4>(a, a + Step::kA * 4096, 4096, at0, at1, acc);
     }
     __syncthreads();
     float* part = reinterpret_cast<float*>(lds);
