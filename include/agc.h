@@ -341,7 +341,7 @@ agc_status agc_gated_forward(const void *x_dev, int64_t ldx, const void *w_gate_
  *   G_gate_dev, G_up_dev  device, where row 0 of G holds the d_ff x d_in gradients of Wg and of Wu (row-major);
  *              row p lies p * ldg floats on; overwritten
  *   workspace_dev  device, agc_gated_workspace_bytes(n_tokens, d_in, d_ff, k_parts) bytes, 256-byte aligned
- * da and du enter dx rounded to bfloat16, and G with all 24 bits of binary32, whatever the sizes of the other operands;
+ * da and du enter dx with 16 bits, so that dx is rounded once, and G with all 24 bits of binary32, whatever the sizes of the other operands;
  * sums are binary32 in a fixed order.  da, du and G of 2^105 and more become infinite.  NaN or infinity in a token reaches
  * its own row of dx and its own partition's gradients alone.
  * 1 <= k_parts <= 256; ldg >= d_in * d_ff. */

@@ -8,8 +8,9 @@
 //   da = dh u act'(a), du = dh act(a)          in the same pass
 //   dx = da Wg + du Wu                          one product over 2 F
 //   dWg_p = da_p^T x_p, dWu_p = du_p^T x_p      one product of 2 F rows a partition, written into row p of G
-// da and du enter dx rounded to bfloat16, as dx itself is.  They enter G, which is binary32, with all their bits: as three
-// bfloat16 parts, three products with x, which is bfloat16 as it is.  Any form with fewer bits of exponent (pairs of binary16
+// da and du enter dx as two bfloat16 parts: 2^-16 of a term at most, so that the rounding of dx itself, 2^-8, is the one that
+// counts (one part would add as much again: 2.35e-3 against 1.66e-3 in the 2-norm for random operands).  They enter G, which
+// is binary32, with all their bits: as three bfloat16 parts, three products with x, which is bfloat16 as it is.  Any form with fewer bits of exponent (pairs of binary16
 // scaled by a power of two, two products) loses what lies far below the largest operands that its scale was made for: one
 // token's large x, masked or not, would cost its whole partition's gradient its bits.  bfloat16 has binary32's exponents; the
 // lowest part alone could fall below them, so values are lifted by 2^23 (kLift), which makes the smallest binary32 the smallest
@@ -308,7 +309,7 @@ struct GateJob {
     // gradient
     const uint16_t* dh;
     int64_t lddh;
-    char* by_token;                   // places x 2 fp: da | du
+    char* by_token;                   // places x 2 fp, two parts: da | du
     int fp;
     char* by_feature;                 // 2 d_ff rows of three parts along the places, lifted
     int64_t pitch;
@@ -360,9 +361,9 @@ struct GateJob {
             }
         }
         if (row < n_rows && f < fp) {
-            uint16_t* o = reinterpret_cast<uint16_t*>(by_token) + (int64_t)row * 2 * fp + f;
-            *reinterpret_cast<tile_u32x4*>(o) = bf16_pack8(da);
-            *reinterpret_cast<tile_u32x4*>(o + fp) = bf16_pack8(du);
+            char* o = by_token + (int64_t)row * fp * 8;
+            parts2_store8(o, f, da);
+            parts2_store8(o, fp + f, du);
         }
         piece_put_row8(s, r, ca, da);
         piece_put_row8(s, r, ca + 16, du);
@@ -382,11 +383,11 @@ struct GateJob {
 
 // dx = [da | du] [Wg | Wu]^T
 struct InputJob {
-    static constexpr TilePair kPair = kPlain;
+    static constexpr TilePair kPair = kParts2;
     static constexpr int kRowParts = 8;
     static constexpr bool kTurned = false;
     const char *a, *b;
-    int64_t pitch;
+    int64_t pitch_a, pitch_b;
     int n_rows, d_in, steps;
     const int* map;
     uint16_t* dx;
@@ -401,11 +402,11 @@ struct InputJob {
     }
     __device__ __forceinline__ const char* a_row(const TilePos& p, int r) const
     {
-        return a + (p.m0 + r < n_rows ? p.m0 + r : n_rows - 1) * pitch;
+        return a + (p.m0 + r < n_rows ? p.m0 + r : n_rows - 1) * pitch_a;
     }
     __device__ __forceinline__ const char* b_row(const TilePos& p, int r) const
     {
-        return b + (p.n0 + r < d_in ? p.n0 + r : d_in - 1) * pitch;
+        return b + (p.n0 + r < d_in ? p.n0 + r : d_in - 1) * pitch_b;
     }
     __device__ __forceinline__ void rows(const TilePos&, int mb, int nb, const float* s, int it, int lane) const
     {
@@ -534,8 +535,9 @@ int64_t gated_workspace_bytes(int64_t tokens, int d_in, int d_ff, int k_parts)
 {
     int64_t bytes = packed_bytes(tokens, d_in, d_ff);
     if (k_parts > 0) {
-        const int64_t places = round_up(tokens + 31 * (int64_t)k_parts, 32), fp = round_up(d_ff, 64);
-        bytes += round_up(places * 4, 256) + round_up(places * fp * 4, 256) + round_up(2 * d_ff * places * 6, 256) +
+        const int64_t held = k_parts < tokens ? k_parts : tokens;   // partitions that are not empty, at most
+        const int64_t places = round_up(tokens + 31 * held, 32), fp = round_up(d_ff, 64);
+        bytes += round_up(places * 4, 256) + round_up(places * fp * 8, 256) + round_up(2 * d_ff * places * 6, 256) +
                  round_up(d_in * places * 2, 256) + round_up(d_in * fp * 4, 256);
     }
     return bytes > 256 ? bytes : 256;
@@ -590,7 +592,7 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         const Rows wg = whole_steps(c.wg, c.ldw, c.d_ff, c.d_in, room, prepare, 1);
         const Rows wu = whole_steps(c.wu, c.ldw, c.d_ff, c.d_in, room, prepare, 2);
         int* map = reinterpret_cast<int*>(take((int64_t)places * 4));
-        char* by_token = take(places * fp * 4);
+        char* by_token = take(places * fp * 8);
         by_feature = take((int64_t)places * 2 * c.d_ff * 6);
         x_turned = take((int64_t)places * c.d_in * 2);
         char* w_turned = take(c.d_in * fp * 4);
@@ -619,7 +621,7 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         e = launch_product(j, 1, places, fp * 2, j.steps, stream);
         if (e != hipSuccess) return e;
         if (c.dx) {
-            InputJob d{by_token, w_turned, fp * 4, places, c.d_in, (int)(fp / 32), map, static_cast<uint16_t*>(c.dx), c.lddx};
+            InputJob d{by_token, w_turned, fp * 8, fp * 4, places, c.d_in, (int)(fp / 16), map, static_cast<uint16_t*>(c.dx), c.lddx};
             e = launch_product(d, 1, places, c.d_in, d.steps, stream);
             if (e != hipSuccess) return e;
         }

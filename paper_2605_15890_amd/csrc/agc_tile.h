@@ -8,12 +8,13 @@
 //                                                      C += A0 B0 + A0 B1 + A1 B0   (lo * lo is below 2^-22)
 //   parts3  32 binary32 values of A as three bfloat16 parts (v = A0 + A1 + A2, all 24 bits), 32 bfloat16 values of B:
 //                                                      C += A0 B0 + A1 B0 + A2 B0
+//   parts2  the same without the third part, 16 bits:  C += A0 B0 + A1 B0
 // Products are v_mfma_f32_16x16x32, sums binary32.
 //
 // A workgroup of WM x WN waves owns a TM x TN tile of C and holds two k-steps of both operands in LDS, filled by
 // loads that go from memory to LDS directly while the other k-step is multiplied.  Row r of a k-step of two parts lies at
 // r * 128 bytes with its eight 16-byte chunks permuted by r & 7, which the loads do by choosing whose chunk a lane
-// fetches: the sixteen rows that a wave reads at once then fall on all banks.  Operands of one or three parts lie part
+// fetches: the sixteen rows that a wave reads at once then fall on all banks.  Where A and B differ in parts, both lie part
 // by part, two rows of 64 bytes in 128, these eight chunks permuted in the same way.
 // After the loop every wave stages its part of C, 64 x 64 values at a time, in its own 16 KB of the same LDS and
 // hands it to the job, which reads it along rows or along columns, eight values a lane, and writes what it needs.
@@ -30,12 +31,12 @@ typedef __bf16 tile_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float tile_f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t tile_u32x4 __attribute__((ext_vector_type(4)));
 
-enum TilePair { kPlain, kSplit, kParts3 };
+enum TilePair { kPlain, kSplit, kParts2, kParts3 };
 
 // 64-byte parts of a row's k-step
 template <TilePair PAIR>
 struct TileStep {
-    static constexpr bool kByPart = PAIR == kParts3;
+    static constexpr bool kByPart = PAIR == kParts2 || PAIR == kParts3;
     static constexpr int kA = PAIR == kParts3 ? 3 : 2, kB = kByPart ? 1 : 2;
 };
 
@@ -181,6 +182,19 @@ __device__ __forceinline__ void parts3_store8(char* row, int k, const float v[8]
     *reinterpret_cast<tile_u32x4*>(p) = first;
     *reinterpret_cast<tile_u32x4*>(p + 64) = mid;
     *reinterpret_cast<tile_u32x4*>(p + 128) = bf16_pack8(rest);
+}
+
+// Eight binary32 values as two bfloat16 parts, both rounded, at element k of a row of A of parts2.
+__device__ __forceinline__ void parts2_store8(char* row, int k, const float v[8])
+{
+    float first[8], rest[8];
+    const tile_u32x4 top = bf16_pack8(v);
+    bf16_unpack8(top, first);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = fabsf(first[i]) == INFINITY ? 0.0f : v[i] - first[i];
+    char* p = row + (int64_t)(k >> 5) * 128 + (k & 31) * 2;
+    *reinterpret_cast<tile_u32x4*>(p) = top;
+    *reinterpret_cast<tile_u32x4*>(p + 64) = bf16_pack8(rest);
 }
 
 // ------------------------------------------------------------------ the loop
@@ -393,7 +407,7 @@ __global__ __launch_bounds__(256, 1) void k_tile_cut(const JOB job)
         }
     };
     constexpr int kLoads = kIssue * (kLoadsA + 1);   // of one k-step
-    static_assert(kLoads == 16, "the counted wait below");
+    static_assert(kLoads == 16 || kLoads == 12, "the counted waits below");
     tile_f32x4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -407,7 +421,8 @@ __global__ __launch_bounds__(256, 1) void k_tile_cut(const JOB job)
         __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other half has been read
         if (k + 4 < pos.steps) {
             issue(mine + (half ^ 1) * kStep);
-            __asm__ volatile("s_waitcnt vmcnt(16)" ::: "memory");   // all but the sixteen loads just issued
+            if constexpr (kLoads == 16) __asm__ volatile("s_waitcnt vmcnt(16)" ::: "memory");   // all but the loads just issued
+            else __asm__ volatile("s_waitcnt vmcnt(12)" ::: "memory");
         } else {
             __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }

@@ -116,6 +116,30 @@ def test_rows_of_G_of_operands_of_different_sizes(kind, d_in, d_ff, act):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("tokens,d_in,d_ff,act", [(130, 64, 40, "silu"), (131, 65, 33, "gelu")])
+def test_dx_of_operands_of_different_sizes(kind, tokens, d_in, d_ff, act):
+    check_dx(kind, tokens, d_in, d_ff, act)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,d_in,d_ff", [(300, 300, 257), (1500, 770, 300), (4100, 2100, 256)])
+def test_dx_in_every_tile_size(tokens, d_in, d_ff):
+    check_dx("none", tokens, d_in, d_ff, "silu")
+
+
+def check_dx(kind, tokens, d_in, d_ff, act):
+    import torch
+    _, operands = plain(tokens, d_in, d_ff, 8)
+    spread(kind, *operands)
+    dev, host = zip(*(device(v) for v in operands))
+    dx = torch.full((tokens, d_in), 7.0, dtype=torch.bfloat16, device="cuda")
+    call(*dev, [tokens // 2, tokens], act, dx)
+    _, _, want, bound = reference(*host, [tokens // 2, tokens], act)
+    assert np.all(np.abs(dx.double().cpu().numpy() - want) <= bound)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("tokens,d_in,d_ff,k", [(70, 30, 20, 2), (96, 300, 129, 3), (2100, 520, 1100, 2), (4096, 2048, 1100, 1)])
 def test_single_terms_of_G(tokens, d_in, d_ff, k):
     """Each element of G is one product: one token of a partition has a gradient.  Gates far above zero make act(a) = a
