@@ -52,7 +52,8 @@ struct Activation {
         const float t = -a * kLog2e;
         const float rest = fmaf(-a, kLog2e, -t) - a * kLog2eRest;
         const float e = __builtin_amdgcn_exp2f(t);
-        const float p = e < 1e30f ? fmaf(e, rest * kLn2, e) : e;   // an infinite power times a rest of 0 is no number
+        // an infinite power times a rest of 0, or a power of 0 times an infinite rest, is no number
+        const float p = e > 0.0f && e < 1e30f ? fmaf(e, rest * kLn2, e) : e;
         return __builtin_amdgcn_rcpf(1.0f + p);
     }
     // activation and its derivative
