@@ -56,11 +56,13 @@ struct Activation {
         const float p = e > 0.0f && e < 1e30f ? fmaf(e, rest * kLn2, e) : e;
         return __builtin_amdgcn_rcpf(1.0f + p);
     }
+    // Phi(a) from the complement's side: 1 + erf would cancel below zero, down to nothing at a = -5.6
+    static __device__ __forceinline__ float normal_cdf(float a) { return 0.5f * erfcf(-0.70710678118654752f * a); }
     // activation and its derivative
     __device__ __forceinline__ void at(float a, float& value, float& slope) const
     {
         if (gelu) {
-            const float cdf = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
+            const float cdf = normal_cdf(a);
             value = a * cdf;
             slope = fmaf(a * 0.39894228040143268f, expf(-0.5f * a * a), cdf);
         } else {
@@ -71,7 +73,7 @@ struct Activation {
     }
     __device__ __forceinline__ float operator()(float a) const
     {
-        return gelu ? a * (0.5f * (1.0f + erff(a * 0.70710678118654752f))) : a * sigmoid(a);
+        return a * (gelu ? normal_cdf(a) : sigmoid(a));
     }
 };
 

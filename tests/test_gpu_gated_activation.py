@@ -70,3 +70,36 @@ def test_gradients_of_gates_near_the_largest_binary32():
     on = a > 0
     assert np.all(np.abs(da - dh * 0.5 * on) <= 2 * U * dh)
     assert np.all(np.abs(du - dh * a * on) <= 2 * U * np.abs(dh * a * on))
+
+
+def gelu(a):
+    """Value, derivative and the bound of a binary32 derivative's error: the arguments of erfc and exp are rounded (2 and 1
+    roundings: a^2 of their relative error each time 2, and a^2 / 2), erfc is within 16 ulp, exp within 3, and 4 operations."""
+    a = np.asarray(a)
+    cdf = np.array([0.5 * math.erfc(-v / math.sqrt(2.0)) for v in a])
+    bell = a * np.exp(-0.5 * a * a) / math.sqrt(2.0 * math.pi)
+    return a * cdf, cdf + bell, (2 * a * a + 36) * U * cdf + (2 * a * a + 10) * U * np.abs(bell)
+
+
+TAILS = [-12.0, -10.0, -9.0, -8.0, -7.0, -6.0, -5.75, -5.5, -5.25, -5.0, -4.5, -4.0, -3.0, -2.0, -1.0, -0.5, -0.01, 0.01, 1.0, 5.0, 12.0]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [3, 100])
+def test_gelu_below_zero(tokens):
+    """h is activation and one rounding to bfloat16, however small it is."""
+    import torch
+    got = forward(tokens, [[v] for v in TAILS], [1.0] * len(TAILS), "gelu")
+    a = torch.tensor(TAILS).bfloat16().double().numpy()
+    want, _, _ = gelu(a)
+    assert np.all(np.abs(got - want) <= (2.0 ** -8 + (2 * a * a + 36) * U) * np.abs(want))
+
+
+@pytest.mark.gpu
+def test_gradients_of_gelu_below_zero():
+    import torch
+    da, du, dh = gradient([[v] for v in TAILS], [1.0] * len(TAILS), "gelu", 1.0)
+    a = torch.tensor(TAILS).bfloat16().double().numpy()
+    value, slope, bound = gelu(a)
+    assert np.all(np.abs(da - slope) <= bound)
+    assert np.all(np.abs(du - value) <= (2 * a * a + 36) * U * np.abs(value))
