@@ -628,12 +628,13 @@ def agc_muon_update(beta, m1, ghat, offsets, rows, cols, lr, momentum, nesterov,
                     beta_bf16=None, stream=None, check=True):
     """Orthogonalised update of the rows x cols matrices that start at `offsets` (elements) of the parameter vector
     beta; m1 and ghat have its layout, and so has beta_bf16 (bfloat16), which receives the new matrices if given."""
+    import torch
     L = load()
     off = [int(o) for o in offsets]
     size = int(rows) * int(cols)
     end = max(off, default=0) + size
-    for t, width in ((beta, 4), (m1, 4), (ghat, 4), (beta_bf16, 2)):
-        if t is not None and (t.numel() < end or t.element_size() != width or not t.is_contiguous()):
+    for t, dtype in ((beta, torch.float32), (m1, torch.float32), (ghat, torch.float32), (beta_bf16, torch.bfloat16)):
+        if t is not None and (t.numel() < end or t.dtype is not dtype or not t.is_contiguous()):
             raise AgcError(AGC_ESHAPE, "agc_muon_update: a vector is smaller than the matrices reach, or of another type")
     if workspace.nbytes < L.agc_muon_workspace_bytes(rows, cols, len(off)):
         raise AgcError(AGC_ESHAPE, "agc_muon_update: the workspace is too small")
