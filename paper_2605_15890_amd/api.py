@@ -517,7 +517,7 @@ def _type_of(t, what):
 def _ids(tokens):
     """Bytes of an id; AGC_ESHAPE unless tokens is a contiguous vector of int32 or int64."""
     width = tokens.element_size()
-    if tokens.dim() != 1 or not tokens.is_contiguous() or tokens.is_floating_point() or width not in (4, 8):
+    if tokens.dim() != 1 or not tokens.is_contiguous() or tokens.is_floating_point() or tokens.is_complex() or width not in (4, 8):
         raise AgcError(AGC_ESHAPE, "tokens must be a contiguous vector of int32 or int64")
     return width
 
