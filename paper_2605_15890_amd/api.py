@@ -501,7 +501,7 @@ def _rows_of(t, rows, cols, dtype, what):
     if len(shape) == 2 and shape[0] >= rows and shape[1] == cols and t.dtype is dtype:
         ld, step = t.stride()
         if step == 1 or cols == 1:
-            return ld if rows > 1 else max(cols, ld)
+            return ld if rows > 1 else cols   # the stride of a single row says nothing
     raise AgcError(AGC_ESHAPE, f"{what} must be a ({rows}, {cols}) row-major view of {dtype}, got {tuple(shape)} of {t.dtype}")
 
 

@@ -28,3 +28,20 @@ def test_ids_that_are_no_whole_numbers(dtype):
     assert refused(api.agc_embed_forward, table, ids, 1.0, out) == api.AGC_ESHAPE
     ws = torch.zeros(api.agc_embed_workspace_bytes(3, 4, 8, 1), dtype=torch.uint8)
     assert refused(api.agc_embed_partial_gradients, out, ids, [3], 4, 1.0, torch.zeros(1, 32), ws) == api.AGC_ESHAPE
+
+
+@pytest.mark.gpu
+def test_strides_of_a_single_row_do_not_matter():
+    """One row of each weight, and one partition's gradients, from tensors of different strides."""
+    bf16 = torch.bfloat16
+    x = torch.randn(70, 16, device="cuda").to(bf16)
+    gate, up = torch.randn(1, 16, device="cuda").to(bf16), torch.randn(4, 40, device="cuda").to(bf16)[2:3, :16]
+    dh = torch.randn(70, 1, device="cuda").to(bf16)
+    ws = torch.empty(api.agc_gated_workspace_bytes(70, 16, 1, 1), dtype=torch.uint8, device="cuda")
+    got = []
+    for w_up, G_up in ((up, torch.zeros(3, 50, device="cuda")[1:2, :16]), (up.contiguous(), torch.zeros(1, 16, device="cuda"))):
+        h, G = torch.zeros(70, 1, dtype=bf16, device="cuda"), torch.zeros(1, 16, device="cuda")
+        api.agc_gated_forward(x, gate, w_up, "silu", h, ws)
+        api.agc_gated_partial_gradients(x, gate, w_up, "silu", dh, [70], None, G, G_up, ws)
+        got.append((h, G, G_up))
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][0].abs().sum() > 0 and got[0][2].abs().sum() > 0
