@@ -325,8 +325,8 @@ typedef enum {
  *   h_dev      device, n_tokens x d_ff, row stride ldh; overwritten
  *   workspace_dev  device, agc_gated_workspace_bytes(n_tokens, d_in, d_ff, 0) bytes, 256-byte aligned; scratch
  * Any alignment of the operands and any sizes: 0 <= n_tokens <= 2^26, 1 <= d_in, d_ff <= 65536.  Up to 64 tokens take
- * a form that is bound by the one read of the weights; rows that are not whole multiples of 128 bytes, 16-byte
- * aligned, are copied to the workspace first when there are more. */
+ * a form that is bound by the one read of the weights and needs no workspace (256 bytes are asked for); rows that are
+ * not whole multiples of 128 bytes, 16-byte aligned, are copied to the workspace first when there are more. */
 int64_t agc_gated_workspace_bytes(int64_t n_tokens, int d_in, int d_ff, int k_parts);
 agc_status agc_gated_forward(const void *x_dev, int64_t ldx, const void *w_gate_dev, const void *w_up_dev, int64_t ldw,
                              int64_t n_tokens, int d_in, int d_ff, int act, void *h_dev, int64_t ldh, void *workspace_dev,

@@ -26,7 +26,7 @@ namespace agc {
 namespace {
 
 constexpr int kBlock = 256;
-
+constexpr int kFewTokens = 64;   // up to here the forward pass is k_gated_few
 constexpr float kLift = 8388608.0f;   // 2^23, of da and du as they enter G
 
 struct Rows {
@@ -519,8 +519,6 @@ int64_t packed_bytes(int64_t tokens, int d_in, int d_ff)
     return round_up(tokens * up, 256) + 2 * round_up(d_ff * up, 256);
 }
 
-constexpr int kFewTokens = 64;
-
 template <int NT, bool WHOLE>
 hipError_t launch_few(const GatedCall& c, hipStream_t stream)
 {
@@ -536,6 +534,7 @@ hipError_t launch_few(const GatedCall& c, hipStream_t stream)
 // packed x, Wg, Wu | map | da, du by token | by feature | x turned | weights turned
 int64_t gated_workspace_bytes(int64_t tokens, int d_in, int d_ff, int k_parts)
 {
+    if (k_parts == 0 && tokens <= kFewTokens) return 256;   // nothing is laid out
     int64_t bytes = packed_bytes(tokens, d_in, d_ff);
     if (k_parts > 0) {
         const int64_t held = k_parts < tokens ? k_parts : tokens;   // partitions that are not empty, at most

@@ -45,3 +45,19 @@ def test_strides_of_a_single_row_do_not_matter():
         api.agc_gated_partial_gradients(x, gate, w_up, "silu", dh, [70], None, G, G_up, ws)
         got.append((h, G, G_up))
     assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][0].abs().sum() > 0 and got[0][2].abs().sum() > 0
+
+
+def test_workspace_of_a_forward_pass_of_few_tokens():
+    """Up to 64 tokens nothing is laid out; more never need less."""
+    sizes = [api.agc_gated_workspace_bytes(n, 1024, 4096) for n in (0, 1, 5, 64, 65, 66, 1000)]
+    assert sizes[:4] == [256] * 4 and sizes == sorted(sizes) and sizes[4] > 1 << 20
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [1, 16, 64])
+def test_forward_pass_of_few_tokens_leaves_the_workspace_alone(tokens):
+    bf16 = torch.bfloat16
+    x, w = torch.randn(tokens, 67, device="cuda").to(bf16), torch.randn(30, 67, device="cuda").to(bf16)
+    h, ws = torch.empty(tokens, 30, dtype=bf16, device="cuda"), torch.full((256,), 9, dtype=torch.uint8, device="cuda")
+    api.agc_gated_forward(x, w, w, "silu", h, ws)
+    assert torch.all(ws == 9) and torch.isfinite(h.float()).all()
