@@ -289,4 +289,15 @@ inline int ls_fold(int64_t n_rows, int64_t rows_per_part, int n_feat)
 // be eight times as many workgroups (2^17 x 8192, one part: 387 us, now 346; 65536 x 4096, 8 parts 92, now 87).
 constexpr bool ls_reduce_few(int wg_per_part) { return wg_per_part <= 16; }
 
+// A launch takes fewer than 2^32 threads along x: more workgroups lie along y as well, x * y of them or a few more.
+struct FoldedGrid {
+    unsigned x, y;
+};
+inline FoldedGrid folded_grid(int64_t workgroups, int threads)
+{
+    const int64_t most = (int64_t)UINT32_MAX / threads;
+    const int64_t y = (workgroups + most - 1) / most;
+    return y <= 1 ? FoldedGrid{(unsigned)workgroups, 1u} : FoldedGrid{(unsigned)((workgroups + y - 1) / y), (unsigned)y};
+}
+
 }  // namespace agc

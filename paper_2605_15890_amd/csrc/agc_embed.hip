@@ -7,6 +7,7 @@
 // order, found by searching it, and are summed by whoever writes the row: no atomics on values, no clearing before.
 // Rows with long runs (few ids, or the commonest one) would leave one wave with all the work: runs are first summed in
 // pieces of 64 places of the order and those in groups of 16, so that a row of n tokens takes about n / 1024 + 160 steps.
+#include "agc_dispatch.h"
 #include "agc_operators.h"
 
 namespace agc {
@@ -554,8 +555,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_rows(const SumArgs a, const T*
                                                        float* G, int64_t ldg, int rows, unsigned sum_blocks)
 {
     const int lane = threadIdx.x & 63, sub = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (blockIdx.x < sum_blocks) sum_runs<T, WHOLE>(a, dout, vocab, scale, G, ldg, (int64_t)blockIdx.x * 4 + sub, lane);
-    else fill_rows(a, vocab, total, G, ldg, rows, (int64_t)(blockIdx.x - sum_blocks) * 4 + sub, lane);
+    const unsigned id = blockIdx.y * gridDim.x + blockIdx.x;
+    if (id < sum_blocks) sum_runs<T, WHOLE>(a, dout, vocab, scale, G, ldg, (int64_t)id * 4 + sub, lane);
+    else fill_rows(a, vocab, total, G, ldg, rows, (int64_t)(id - sum_blocks) * 4 + sub, lane);
 }
 
 template <class TABLE, class OUT, class ID>
@@ -601,8 +603,9 @@ hipError_t sums_as(const EmbedCall& c, const SumArgs& a, hipStream_t stream)
     while (rows > 1 && total / rows < 8192) rows /= 2;
     const int64_t fills = (total + rows - 1) / rows, sums = (int64_t)((a.n + kHeads - 1) / kHeads) * across;
     const unsigned sum_blocks = (unsigned)((sums + 3) / 4);
-    hipLaunchKernelGGL((k_embed_rows<T, WHOLE>), dim3(sum_blocks + (unsigned)((fills + 3) / 4)), dim3(kBlock), 0, stream, a, dout,
-                       c.vocab, total, c.scale, c.G, c.ldg, rows, sum_blocks);
+    const FoldedGrid grid = folded_grid(sum_blocks + (fills + 3) / 4, kBlock);
+    hipLaunchKernelGGL((k_embed_rows<T, WHOLE>), dim3(grid.x, grid.y), dim3(kBlock), 0, stream, a, dout, c.vocab, total, c.scale,
+                       c.G, c.ldg, rows, sum_blocks);
     return hipGetLastError();
 }
 
