@@ -318,7 +318,8 @@ typedef enum {
     AGC_ACT_GELU = 1  /* a * Phi(a), by erf */
 } agc_activation;
 
-/* Gated feed-forward block in bfloat16:  h = act(x Wg^T) * (x Wu^T), sums and activation in binary32, h rounded once.
+/* Gate of a gated feed-forward block in bfloat16:  h = act(x Wg^T) * (x Wu^T), sums and activation in binary32, h rounded
+ * once.  The block's output projection, a product of h with a third matrix, is the caller's.
  *   x_dev      device, n_tokens x d_in, row stride ldx elements
  *   w_gate_dev, w_up_dev  device, d_ff x d_in, row stride ldw (their sections of the parameter vector, rounded to
  *              bfloat16, for instance)
@@ -341,9 +342,9 @@ agc_status agc_gated_forward(const void *x_dev, int64_t ldx, const void *w_gate_
  *   G_gate_dev, G_up_dev  device, where row 0 of G holds the d_ff x d_in gradients of Wg and of Wu (row-major);
  *              row p lies p * ldg floats on; overwritten
  *   workspace_dev  device, agc_gated_workspace_bytes(n_tokens, d_in, d_ff, k_parts) bytes, 256-byte aligned
- * da and du enter dx with 16 bits, so that dx is rounded once, and G with all 24 bits of binary32, whatever the sizes of the other operands;
- * sums are binary32 in a fixed order.  da, du and G of 2^105 and more become infinite.  NaN or infinity in a token reaches
- * its own row of dx and its own partition's gradients alone.
+ * da and du enter dx with 16 bits, so that dx is rounded once, and G with all 24 bits of binary32, whatever the sizes of
+ * the other operands; sums are binary32 in a fixed order.  da, du and G of 2^105 and more become infinite.  NaN or infinity
+ * in a token reaches its own row of dx and its own partition's gradients alone.
  * 1 <= k_parts <= 256; ldg >= d_in * d_ff. */
 agc_status agc_gated_partial_gradients(const void *x_dev, int64_t ldx, const void *w_gate_dev, const void *w_up_dev,
                                        int64_t ldw, const void *dh_dev, int64_t lddh, int64_t n_tokens,

@@ -549,7 +549,7 @@ __device__ __forceinline__ void sum_runs(const SumArgs& a, const T* dout, int64_
 }
 
 // All rows of G.  The first `sum_blocks` workgroups sum runs, which take longest, the others write zeros.  Bound by the
-// write of G: 8 x 32000 x 768 in 144 us, 5.5 TB/s (a fill of 4 GiB: 6.9).
+// write of G: 8 x 32000 x 768 in 156 us, 5.0 TB/s (a fill of 4 GiB: 6.9).
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_embed_rows(const SumArgs a, const T* dout, int64_t vocab, int64_t total, float scale,
                                                        float* G, int64_t ldg, int rows, unsigned sum_blocks)

@@ -1,5 +1,6 @@
-// Gated feed-forward block, bfloat16:  a = x Wg^T, u = x Wu^T, h = act(a) * u, and its gradients by data partition
-// (rows of G).  x is tokens x d_in, Wg and Wu are d_ff x d_in, all row-major.
+// Gate of a gated feed-forward block, bfloat16:  a = x Wg^T, u = x Wu^T, h = act(a) * u, and its gradients by data
+// partition (rows of G).  x is tokens x d_in, Wg and Wu are d_ff x d_in, all row-major.  The block's output projection, a
+// product of h with a third matrix, is not part of it.
 //
 // Forward: one product whose columns take 16 rows of Wg and 16 rows of Wu in turn, so that a wave ends with a and u of
 // the same places; activation and product follow from the binary32 sums, h is rounded once.
@@ -10,11 +11,14 @@
 //   dWg_p = da_p^T x_p, dWu_p = du_p^T x_p      one product of 2 F rows a partition, written into row p of G
 // da and du enter dx as two bfloat16 parts: 2^-16 of a term at most, so that the rounding of dx itself, 2^-8, is the one that
 // counts (one part would add as much again: 2.35e-3 against 1.66e-3 in the 2-norm for random operands).  They enter G, which
-// is binary32, with all their bits: as three bfloat16 parts, three products with x, which is bfloat16 as it is.  Any form with fewer bits of exponent (pairs of binary16
-// scaled by a power of two, two products) loses what lies far below the largest operands that its scale was made for: one
-// token's large x, masked or not, would cost its whole partition's gradient its bits.  bfloat16 has binary32's exponents; the
-// lowest part alone could fall below them, so values are lifted by 2^23 (kLift), which makes the smallest binary32 the smallest
-// normal bfloat16.  da, du and G of 2^105 and more leave binary32 that way and become infinite.
+// is binary32, with all their bits: as three bfloat16 parts, three products with x, which is bfloat16 as it is.  Any form
+// with fewer bits of exponent (pairs of binary16 scaled by a power of two, two products) loses what lies far below the
+// largest operands that its scale was made for: one token's large x, masked or not, would cost its whole partition's
+// gradient its bits.  bfloat16 has binary32's exponents; the lowest part alone could fall below them, so values are lifted
+// by 2^23 (kLift), which makes the smallest binary32 the smallest normal bfloat16.  da, du and G of 2^105 and more leave
+// binary32 that way and become infinite.
+// 8192 x 2048 x 5632 in 16 partitions: da, du 565 us, dx 587 us (1.29 PFLOP/s with its two products), G 1127 us (1.01, with
+// 1.5 GB of G to write), where pairs for G and one part for dx took 524, 317 and 957 us and 44 us for the scales.
 // The tile loop wants both operands contiguous along the sum: x and the weights are turned by passes of their own, da
 // and du are written both ways.  A partition starts at a multiple of 32 in the turned order, the places between are
 // zeros; `map` gives each place its token, or -1.
@@ -56,7 +60,8 @@ struct Activation {
         const float p = e > 0.0f && e < 1e30f ? fmaf(e, rest * kLn2, e) : e;
         return __builtin_amdgcn_rcpf(1.0f + p);
     }
-    // Phi(a) from the complement's side: 1 + erf would cancel below zero, down to nothing at a = -5.6
+    // Phi(a) from the complement's side: 1 + erf would cancel below zero, down to nothing at a = -5.6.  8192 x 2048 x 8192
+    // forward: 503 us where SiLU takes 460 (485 and 452 with erf, on another card).
     static __device__ __forceinline__ float normal_cdf(float a) { return 0.5f * erfcf(-0.70710678118654752f * a); }
     // activation and its derivative
     __device__ __forceinline__ void at(float a, float& value, float& slope) const
@@ -215,7 +220,7 @@ __global__ __launch_bounds__(kBlock) void k_turn_tokens(const Turn a) { a.run(bl
 // ------------------------------------------------------------------ few tokens
 // Up to NT * 16 tokens: bound by the one read of the weights.  A workgroup takes 16 rows of Wg and of Wu, its four
 // waves take turns along the sum, 128 bytes of every row at a time, straight from memory into the matrix units'
-// layout (weights as the 16 rows, tokens as the 16 columns); the waves' sums meet in LDS.  5 tokens of 1024 x 4096: 4.7 us
+// layout (weights as the 16 rows, tokens as the 16 columns); the waves' sums meet in LDS.  5 tokens of 1024 x 4096: 4.9 us
 // for 16.8 MB.
 // WHOLE: every 16 bytes of every row may be loaded as they are (d_in a multiple of 64, rows aligned).
 template <int NT, bool WHOLE>
@@ -458,8 +463,8 @@ struct WeightJob {
         auto at = [&](int row) {
             return (row < d_ff ? gate + (int64_t)row * d_in : up + (int64_t)(row - d_ff) * d_in) + p.batch * ldg;
         };
-        // rows of G that start anywhere: the lanes side by side, a value each (1999 x 519 x 1101: 44 us with eight values a
-        // lane, 39 us so)
+        // rows of G that start anywhere: the lanes side by side, a value each (1999 x 519 x 1101 in five equal partitions:
+        // 36 us with eight values a lane, 28 us so)
         if (!whole) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -623,7 +628,8 @@ hipError_t launch_gated_gradients(const GatedCall& c, hipStream_t stream)
         e = launch_product(j, 1, places, fp * 2, j.steps, stream);
         if (e != hipSuccess) return e;
         if (c.dx) {
-            InputJob d{by_token, w_turned, fp * 8, fp * 4, places, c.d_in, (int)(fp / 16), map, static_cast<uint16_t*>(c.dx), c.lddx};
+            InputJob d{by_token, w_turned, fp * 8, fp * 4, places, c.d_in, (int)(fp / 16), map,
+                       static_cast<uint16_t*>(c.dx), c.lddx};
             e = launch_product(d, 1, places, c.d_in, d.steps, stream);
             if (e != hipSuccess) return e;
         }

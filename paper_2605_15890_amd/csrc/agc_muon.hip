@@ -17,8 +17,10 @@
 //   A' = B0 A B0,  B1 = a I + b A' + c A' A',  Q = B1 B0,  X <- Q X
 // is two steps with one product along n each way in place of two: 3 m^2 n + 5 m^3 multiplications against 6 m^2 n + 2 m^3
 // (symmetric products counted half).  12 x 1024 x 4096: 2758 us in single steps, 2194 us so.
-// It is taken where n >= 2 m.  Q reaches a^2 = 11.9 where X is small and is rounded against that, so the error of
-// directions far below the largest is some a times that of single steps; longer chains would lose more.
+// It is taken where n >= 2 m.  Q reaches a^2 = 11.9 where X is small and is rounded against that; longer chains would lose
+// more.  Pairs of steps stay with five single steps whose products are binary32, error of X against 64 bits in the 2-norm:
+// 512 x 2048 1.5e-6 here, 3.2e-6 there, of rank four 4.3e-5 and 6.1e-5, singular values from 1 to 1e-6 5.9e-6 and 6.7e-6;
+// 64 x 900 2.9e-6 and 1.9e-6, of rank four 2.7e-5 and 2.4e-5.
 //
 // Each product writes its result for the next one in the order in which that one reads it: X along n (for X X^T) and
 // along m (for B X); A and B are symmetric, so half the tiles are formed and written twice.  The last product
@@ -78,7 +80,7 @@ __device__ __forceinline__ double block_sum(double v, double* lds)
 }
 
 // M <- mu M + g and the sum of the squares of U in binary64, one partial sum a workgroup (added in a fixed order
-// by k_muon_start).  Bound by memory: 12 bytes a value; 12 x 1024 x 4096 in 109 us, 5.5 TB/s.
+// by k_muon_start).  Bound by memory: 12 bytes a value; 12 x 1024 x 4096 in 114 us, 5.3 TB/s.
 __global__ __launch_bounds__(kSumBlock) void k_muon_momentum(const MuonCall c, int64_t count, double* sums)
 {
     __shared__ double lds[4];
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(kSumBlock) void k_muon_momentum(const MuonCall c, i
 }
 
 // X = U / (|U| + eps) as binary16 pairs, stored along both sides.  A workgroup turns one 64 x 64 tile of U in LDS.  Bound
-// by memory: 16 bytes a value; 12 x 1024 x 4096 in 169 us, 4.8 TB/s, the rate of a copy.
+// by memory: 16 bytes a value; 12 x 1024 x 4096 in 171 us, 4.7 TB/s, the rate of a copy.
 __global__ __launch_bounds__(kSumBlock) void k_muon_start(const MuonCall c, MuonGeom geo, const double* sums, int n_sums,
                                                           char* along_cols, char* along_rows)
 {

@@ -275,10 +275,10 @@ __device__ __forceinline__ void tile_multiply(const char* a, const char* b, int 
 // becomes of part `it` of kRowParts, along rows, of the 64 x 64 values staged at s, the first of them C[m, n]; and,
 // where kTurned and turned(pos), cols(...): the same of eight parts along columns, after all rows().
 //
-// Bound by the matrix units at the power that they are given: B X of 2 x 4096 x 4096 (three products of pairs) 596 us,
-// 1.38 PFLOP/s, and h of 8192 x 2048 x 8192 466 us, 1.18, where a library's product of 8192 x 8192 x 8192 reaches 1.41.
+// Bound by the matrix units at the power that they are given: B X of 2 x 4096 x 4096 (three products of pairs) 628 us,
+// 1.31 PFLOP/s, and h of 8192 x 2048 x 8192 474 us, 1.16, where a library's product of 8192 x 8192 x 8192 reaches 1.45.
 // 256 x 256 leaves room for one workgroup a compute unit, whose end (staging and stores, 9 to 20 us a tile) nothing
-// overlaps; two workgroups of 128 x 128 overlap theirs but read LDS twice as much a product and are 8 to 15 % slower
+// overlaps; two workgroups of 128 x 128 overlap theirs but read LDS twice as much a product and are 7 to 20 % slower
 // there.  They are taken where 256 x 256 would fill the units badly (choose_tile).
 template <class JOB, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_tile(const JOB job)
