@@ -352,6 +352,46 @@ agc_status agc_gated_partial_gradients(const void *x_dev, int64_t ldx, const voi
                                        int64_t lddx, float *G_gate_dev, float *G_up_dev, int64_t ldg, void *workspace_dev,
                                        void *hip_stream);
 
+/* Rotation of queries and keys by their positions.  The first rot_dim values of each head are rot_dim / 2 pairs, values i and
+ * i + rot_dim / 2 (AGC_ROTARY_HALF) or 2 i and 2 i + 1 (AGC_ROTARY_INTERLEAVED); pair i of token t becomes
+ *   amplitude * (a cos - b sin, a sin + b cos)  at the angle  2 pi position_t turns_i / 2^64
+ * (-angle with inverse, which is the gradient: dx = agc_rotary_apply(dout, inverse)).  Values behind them are copied.  Angles,
+ * sines and products are binary32 or better at any position, a result is rounded once.
+ *   x_dev, out_dev  device, n_tokens x (heads * head_dim) of one type, row strides ldx and ldo elements, any alignment; queries
+ *              and keys that lie side by side in a row are one call.  out may be x, with the same stride, and not overlap it otherwise
+ *   positions_dev  device, n_tokens positions of position_bytes = 4 or 8 bytes (signed)
+ *   turns_dev  device, rot_dim / 2 numbers: a position's share of a whole turn in units of 2^-64
+ * 0 <= n_tokens <= 2^26, heads * head_dim <= 65536, 2 <= rot_dim <= head_dim, rot_dim even. */
+typedef enum { AGC_ROTARY_HALF = 0, AGC_ROTARY_INTERLEAVED = 1 } agc_rotary_layout;
+agc_status agc_rotary_apply(const void* x_dev, int type, int64_t ldx, int64_t n_tokens, int heads, int head_dim, int rot_dim,
+                            const void* positions_dev, int position_bytes, const uint64_t* turns_dev, int layout,
+                            float amplitude, int inverse, void* out_dev, int64_t ldo, void* hip_stream);
+/* Its table (host): turns_out[i] = 2^64 f_i / (2 pi), rot_dim / 2 numbers, f_i = base^(-2 i / rot_dim), and for contexts `factor`
+ * times as long as original_len, the one that a model was trained for,
+ *   AGC_ROTARY_LINEAR    f_i / factor
+ *   AGC_ROTARY_BY_PARTS  f_i / factor where the pair turns once or less over original_len, f_i where it turns 32 times or more,
+ *                        a linear ramp over the pairs between;  *amplitude_out = 0.1 ln(factor) + 1 (else 1). */
+typedef enum { AGC_ROTARY_PLAIN = 0, AGC_ROTARY_LINEAR = 1, AGC_ROTARY_BY_PARTS = 2 } agc_rotary_scaling;
+agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double factor, double original_len,
+                                  uint64_t* turns_out, double* amplitude_out);
+
+/* Dropout into a residual:  out = residual + (U >= p ? x / (1 - p) : 0), one binary32 product and sum, rounded once to out's
+ * type.  The mask is not stored: it follows from (seed, step, site, row, column), whatever the types and strides, so the
+ * gradient is the same call on dout without a residual.  U = (u16 + r2 / 2^32) / 2^16 with
+ *   u16 = 16-bit field c&7 of Philox4x32-10(key = seed, counter = (site << 16 | c>>3, 2^30 | row, step lo, step hi)), fields
+ *         counted from the low half of output word 0;
+ *   r2  = word c&3 of Philox4x32-10(key = seed, counter = (site << 16 | c>>2, 2^31 | 2^30 | row, step lo, step hi)),
+ * counters that agc_encode_quantize does not use: one seed and step serve both, and 65536 sites of a model.  p counts in
+ * units of 2^-48.  A dropped x leaves no trace, NaN included.
+ *   x_dev      device, rows x cols of x_type, row stride ldx elements
+ *   residual_dev  device, rows x cols of out_type, row stride ldr, or NULL: none
+ *   out_dev    device, rows x cols of out_type, row stride ldo; may be x or the residual, with the same type and stride, and
+ *              not overlap them otherwise
+ * 0 <= rows <= 2^26, 1 <= cols <= 65536, 0 <= p <= 1; any alignment of the rows. */
+agc_status agc_dropout(const void* x_dev, int x_type, int64_t ldx, const void* residual_dev, int64_t ldr, int64_t rows, int cols,
+                       double p, uint64_t seed, uint64_t step, uint32_t site, void* out_dev, int out_type, int64_t ldo,
+                       void* hip_stream);
+
 /* Orthogonalised update of n_mats matrices of one shape that lie inside the parameter vector.  For each,
  *   M <- momentum * M + g_hat;   U = g_hat + momentum * M (nesterov) or M;   X = U / (|U|_F + 1e-7);
  *   `steps` times  A = X X^T,  X <- a X + (b A + c A A) X,  a, b, c = 3.4445, -4.7750, 2.0315;

@@ -18,6 +18,8 @@ AGC_EINVAL, AGC_ESHAPE, AGC_EBITS, AGC_EALIGN, AGC_ENOMEM, AGC_EHIP, AGC_ESTATE 
 AGC_SCALE_L2, AGC_SCALE_MAXABS = 0, 1
 AGC_ACT_SILU, AGC_ACT_GELU = 0, 1
 AGC_TYPE_F32, AGC_TYPE_BF16 = 0, 1
+AGC_ROTARY_HALF, AGC_ROTARY_INTERLEAVED = 0, 1
+AGC_ROTARY_PLAIN, AGC_ROTARY_LINEAR, AGC_ROTARY_BY_PARTS = 0, 1, 2
 AGC_MAX_WORKERS, AGC_MAX_BITS, AGC_NUM_KERNELS, AGC_MAX_LAYERS = 256, 16, 4, 256
 KERNEL_NAMES = ("scale_pass", "scale_finalize", "quantize", "decode")
 
@@ -28,6 +30,7 @@ EXPORTS = [
     "agc_embed_forward", "agc_embed_workspace_bytes", "agc_embed_partial_gradients",
     "agc_gated_workspace_bytes", "agc_gated_forward", "agc_gated_partial_gradients",
     "agc_muon_workspace_bytes", "agc_muon_update",
+    "agc_rotary_apply", "agc_rotary_frequencies", "agc_dropout",
     "agc_calibration_copy", "agc_debug_force_long", "agc_debug_sketch", "agc_debug_sketch_last", "agc_debug_sketch_max", "agc_debug_stream_rows", "agc_ls_workspace_floats", "agc_ls_partial_gradients", "agc_gd_update",
     "agc_phi_coef_balanced", "agc_alloc_bits", "agc_alloc_bits_dp", "agc_alloc_objective",
     "agc_build_code", "agc_build_cyclic_code", "agc_build_cyclic_code_opt", "agc_check_unbiased",
@@ -130,6 +133,14 @@ def load():
     L.agc_muon_update.argtypes = [_vp, _vp, _vp, _vp, C.c_int, C.c_int, C.c_int, C.c_float, C.c_float, C.c_int,
                                   C.c_float, C.c_float, C.c_int, _vp, _vp, _vp]
     L.agc_muon_update.restype = C.c_int
+    L.agc_rotary_frequencies.argtypes = [C.c_int, C.c_double, C.c_int, C.c_double, C.c_double, _vp, _f64p]
+    L.agc_rotary_frequencies.restype = C.c_int
+    L.agc_rotary_apply.argtypes = [_vp, C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_int, _vp, C.c_int, _vp, C.c_int,
+                                   C.c_float, C.c_int, _vp, C.c_int64, _vp]
+    L.agc_rotary_apply.restype = C.c_int
+    L.agc_dropout.argtypes = [_vp, C.c_int, C.c_int64, _vp, C.c_int64, C.c_int64, C.c_int, C.c_double, C.c_uint64, C.c_uint64,
+                              C.c_uint32, _vp, C.c_int, C.c_int64, _vp]
+    L.agc_dropout.restype = C.c_int
     L.agc_calibration_copy.argtypes = [_vp, _vp, C.c_int64, _vp]
     L.agc_calibration_copy.restype = C.c_int
     L.agc_debug_stream_rows.argtypes = [_vp, C.c_int64, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, _vp, _vp]
@@ -642,6 +653,72 @@ def agc_muon_update(beta, m1, ghat, offsets, rows, cols, lr, momentum, nesterov,
                            rows, cols, lr, momentum, int(bool(nesterov)), weight_decay, scale, steps,
                            None if beta_bf16 is None else beta_bf16.data_ptr(), workspace.data_ptr(),
                            _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
+
+
+def _on_current_gpu(what, *tensors):
+    """Refuses tensors that the kernels could not reach from the current GPU."""
+    import torch
+    for t in tensors:
+        if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+            raise AgcError(AGC_EINVAL, f"{what}: tensors must lie on the current GPU")
+
+
+_ROTARY_LAYOUTS = {"half": AGC_ROTARY_HALF, "interleaved": AGC_ROTARY_INTERLEAVED}
+_ROTARY_SCALINGS = {"none": AGC_ROTARY_PLAIN, "linear": AGC_ROTARY_LINEAR, "parts": AGC_ROTARY_BY_PARTS}
+
+
+def agc_rotary_frequencies(rot_dim, base=10000.0, scaling="none", factor=1.0, original_len=4096.0):
+    """(turns, amplitude): a position's share of a whole turn for each of the rot_dim / 2 pairs in units of 2^-64, as a
+    numpy vector whose 64 bits torch.from_numpy takes as they are, and the factor of the rotated values."""
+    L = load()
+    turns, amplitude = np.zeros(max(0, int(rot_dim)) // 2, dtype=np.int64), C.c_double()
+    st = L.agc_rotary_frequencies(int(rot_dim), base, _ROTARY_SCALINGS.get(scaling, -1), factor, original_len,
+                                  turns.ctypes.data, C.byref(amplitude))
+    if st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return turns, amplitude.value
+
+
+def agc_rotary_apply(x, heads, positions, turns, layout, out, amplitude=1.0, inverse=False, stream=None, check=True):
+    """Rotates the first 2 * len(turns) values of each of the heads of x, (tokens, heads * head_dim), float32 or bfloat16;
+    positions are int32 or int64, turns is agc_rotary_frequencies' table on the GPU.  out may be x."""
+    import torch
+    L = load()
+    kind, width, n = _type_of(x, "x"), _ids(positions), positions.numel()
+    if x.dim() != 2 or heads < 1 or x.shape[1] % heads:
+        raise AgcError(AGC_ESHAPE, "x must be (tokens, heads * head_dim)")
+    if turns.dim() != 1 or turns.dtype is not torch.int64 or not turns.is_contiguous():
+        raise AgcError(AGC_ESHAPE, "turns must be a contiguous vector of int64")
+    row = x.shape[1]
+    ldx, ldo = _rows_of(x, n, row, x.dtype, "x"), _rows_of(out, n, row, x.dtype, "out")
+    _on_current_gpu("agc_rotary_apply", x, positions, turns, out)
+    st = L.agc_rotary_apply(x.data_ptr(), kind, ldx, n, heads, row // heads, 2 * turns.numel(), positions.data_ptr(), width,
+                            turns.data_ptr(), _ROTARY_LAYOUTS.get(layout, layout), amplitude, int(bool(inverse)),
+                            out.data_ptr(), ldo, _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
+
+
+def agc_dropout(x, p, seed, step, site, out, residual=None, stream=None, check=True):
+    """out = residual + (x / (1 - p) where it is kept, else 0); x, out and residual are (rows, cols), float32 or bfloat16,
+    the residual of out's type.  The gradient is agc_dropout(dout, p, seed, step, site, dx)."""
+    L = load()
+    x_kind, out_kind = _type_of(x, "x"), _type_of(out, "out")
+    if x.dim() != 2:
+        raise AgcError(AGC_ESHAPE, "x must be (rows, cols)")
+    rows, cols = x.shape
+    ldx, ldo, ldr = _rows_of(x, rows, cols, x.dtype, "x"), _rows_of(out, rows, cols, out.dtype, "out"), cols
+    if residual is not None:
+        ldr = _rows_of(residual, rows, cols, out.dtype, "residual")
+        _on_current_gpu("agc_dropout", residual)
+    _on_current_gpu("agc_dropout", x, out)
+    st = L.agc_dropout(x.data_ptr(), x_kind, ldx, None if residual is None else residual.data_ptr(), ldr, rows, cols, p,
+                       seed & 0xFFFFFFFFFFFFFFFF, step & 0xFFFFFFFFFFFFFFFF, site, out.data_ptr(), out_kind, ldo,
+                       _stream_handle(stream))
     if check and st != AGC_OK:
         raise AgcError(st, L.agc_last_error(None).decode())
     return st

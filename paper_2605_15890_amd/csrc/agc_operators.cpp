@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <string>
 
 #include "../../include/agc.h"
@@ -60,6 +61,9 @@ agc_status gated_arguments(const char* name, const agc::GatedCall& c, int act)
         return refuse(AGC_EALIGN, std::string(name) + ": operands need 2-byte alignment, the workspace 256 bytes");
     return AGC_OK;
 }
+
+bool known_type(int type) { return type == AGC_TYPE_F32 || type == AGC_TYPE_BF16; }
+uintptr_t bytes_of(int type) { return type == AGC_TYPE_F32 ? 4 : 2; }
 
 }  // namespace
 
@@ -200,6 +204,87 @@ agc_status agc_gated_partial_gradients(const void* x_dev, int64_t ldx, const voi
     c.dh = dh_dev, c.lddh = lddh, c.part_end = part_end_host, c.k_parts = k_parts, c.dx = dx_dev, c.lddx = lddx;
     c.g_gate = G_gate_dev, c.g_up = G_up_dev, c.ldg = ldg;
     return launched(agc::launch_gated_gradients(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
+}
+
+agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double factor, double original_len,
+                                  uint64_t* turns_out, double* amplitude_out)
+{
+    const char* const name = "agc_rotary_frequencies";
+    if (!turns_out || !amplitude_out) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (rot_dim < 2 || rot_dim > kMostWidth || rot_dim % 2) return refuse(AGC_ESHAPE, std::string(name) + ": rot_dim must be even, 2..65536");
+    if (scaling != AGC_ROTARY_PLAIN && scaling != AGC_ROTARY_LINEAR && scaling != AGC_ROTARY_BY_PARTS)
+        return refuse(AGC_EINVAL, std::string(name) + ": unknown scaling");
+    if (!(base > 1) || !std::isfinite(base) || (scaling != AGC_ROTARY_PLAIN && (!(factor >= 1) || !std::isfinite(factor))) ||
+        (scaling == AGC_ROTARY_BY_PARTS && (!(original_len > 0) || !std::isfinite(original_len))))
+        return refuse(AGC_EINVAL, std::string(name) + ": base must be above 1, factor 1 or more, the original length positive");
+    const long double pi = 3.14159265358979323846264338327950288L, log_base = std::log((long double)base);
+    // the pair that turns `times` times over the original length
+    const auto pair_of = [&](long double times) { return rot_dim * std::log(original_len / (times * 2 * pi)) / (2 * log_base); };
+    long double low = 0, high = 0;
+    if (scaling == AGC_ROTARY_BY_PARTS) {
+        low = std::max(0.0L, std::floor(pair_of(32)));
+        high = std::min((long double)rot_dim - 1, std::ceil(pair_of(1)));
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        long double f = std::exp(-2.0L * i / rot_dim * log_base);
+        if (scaling == AGC_ROTARY_LINEAR) f /= factor;
+        if (scaling == AGC_ROTARY_BY_PARTS) {
+            const long double ramp = std::min(1.0L, std::max(0.0L, (i - low) / std::max(high - low, 1e-3L)));
+            f = f / factor * ramp + f * (1 - ramp);
+        }
+        turns_out[i] = (uint64_t)std::round(f / (2 * pi) * 18446744073709551616.0L);
+    }
+    *amplitude_out = scaling == AGC_ROTARY_BY_PARTS ? 0.1 * std::log(factor) + 1 : 1;
+    return AGC_OK;
+}
+
+agc_status agc_rotary_apply(const void* x_dev, int type, int64_t ldx, int64_t n_tokens, int heads, int head_dim, int rot_dim,
+                            const void* positions_dev, int position_bytes, const uint64_t* turns_dev, int layout,
+                            float amplitude, int inverse, void* out_dev, int64_t ldo, void* hip_stream)
+{
+    const char* const name = "agc_rotary_apply";
+    if (!known_type(type) || (position_bytes != 4 && position_bytes != 8) || (layout != AGC_ROTARY_HALF && layout != AGC_ROTARY_INTERLEAVED))
+        return refuse(AGC_EINVAL, std::string(name) + ": values are float or bfloat16, positions have 4 or 8 bytes, pairs are halves or neighbours");
+    if (n_tokens < 0 || n_tokens > kMostTokens || heads < 1 || head_dim < 2 || (int64_t)heads * head_dim > kMostWidth || rot_dim < 2 ||
+        rot_dim > head_dim || rot_dim % 2)
+        return refuse(AGC_ESHAPE, std::string(name) + ": n_tokens must be 0..2^26, heads * head_dim up to 65536, rot_dim even, 2..head_dim");
+    if (ldx < (int64_t)heads * head_dim || ldo < (int64_t)heads * head_dim)
+        return refuse(AGC_ESHAPE, std::string(name) + ": a row stride is smaller than the row");
+    if (!turns_dev || (n_tokens > 0 && (!x_dev || !out_dev || !positions_dev))) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (misaligned(x_dev, bytes_of(type)) || misaligned(out_dev, bytes_of(type)) || misaligned(positions_dev, position_bytes) ||
+        misaligned(turns_dev, 8))
+        return refuse(AGC_EALIGN, std::string(name) + ": a pointer is not aligned to its elements");
+    if (x_dev == out_dev && ldx != ldo && n_tokens > 1) return refuse(AGC_EINVAL, std::string(name) + ": in place the row strides must be equal");
+    if (n_tokens == 0) return AGC_OK;
+    agc::RotaryCall c{};
+    c.x = x_dev, c.out = out_dev, c.bf16 = type == AGC_TYPE_BF16, c.ldx = ldx, c.ldo = ldo, c.n = n_tokens;
+    c.heads = heads, c.dim = head_dim, c.rot = rot_dim, c.positions = positions_dev, c.wide_ids = position_bytes == 8;
+    c.turns = turns_dev, c.interleaved = layout == AGC_ROTARY_INTERLEAVED, c.inverse = inverse != 0, c.amplitude = amplitude;
+    return launched(agc::launch_rotary(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
+}
+
+agc_status agc_dropout(const void* x_dev, int x_type, int64_t ldx, const void* residual_dev, int64_t ldr, int64_t rows, int cols,
+                       double p, uint64_t seed, uint64_t step, uint32_t site, void* out_dev, int out_type, int64_t ldo,
+                       void* hip_stream)
+{
+    const char* const name = "agc_dropout";
+    if (!known_type(x_type) || !known_type(out_type)) return refuse(AGC_EINVAL, std::string(name) + ": values are float or bfloat16");
+    if (!(p >= 0 && p <= 1)) return refuse(AGC_EINVAL, std::string(name) + ": p must be 0..1");
+    if (rows < 0 || rows > kMostTokens || cols < 1 || cols > kMostWidth || site > 65535)
+        return refuse(AGC_ESHAPE, std::string(name) + ": rows must be 0..2^26, cols 1..65536, site 0..65535");
+    if (ldx < cols || ldo < cols || (residual_dev && ldr < cols)) return refuse(AGC_ESHAPE, std::string(name) + ": a row stride is smaller than the row");
+    if (rows > 0 && (!x_dev || !out_dev)) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (misaligned(x_dev, bytes_of(x_type)) || misaligned(out_dev, bytes_of(out_type)) || misaligned(residual_dev, bytes_of(out_type)))
+        return refuse(AGC_EALIGN, std::string(name) + ": a pointer is not aligned to its elements");
+    if (rows > 1 && ((x_dev == out_dev && (ldx != ldo || x_type != out_type)) || (residual_dev == out_dev && ldr != ldo)))
+        return refuse(AGC_EINVAL, std::string(name) + ": in place the types and row strides must be equal");
+    if (rows == 0) return AGC_OK;
+    agc::DropoutCall c{};
+    c.x = x_dev, c.residual = residual_dev, c.out = out_dev, c.x_bf16 = x_type == AGC_TYPE_BF16, c.out_bf16 = out_type == AGC_TYPE_BF16;
+    c.ldx = ldx, c.ldr = ldr, c.ldo = ldo, c.rows = rows, c.cols = cols, c.seed = seed, c.step = step, c.site = site;
+    c.drop48 = (uint64_t)std::llround(p * 281474976710656.0);
+    c.scale = p < 1 ? (float)(1 / (1 - p)) : 0.0f;
+    return launched(agc::launch_dropout(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
 }
 
 }  // extern "C"

@@ -1,5 +1,5 @@
 // Launch interface between the C ABI (agc_operators.cpp) and the kernels of the operators round the coded step:
-// orthogonalised update, gated block, embedding.  Every pointer is a device pointer unless it says host.
+// orthogonalised update, gated block, embedding, rotary positions, dropout.  Every pointer is a device pointer unless it says host.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -77,5 +77,33 @@ struct EmbedCall {
 int64_t embed_workspace_bytes(int64_t n, int64_t vocab, int dim, int k_parts);
 hipError_t launch_embed_forward(const EmbedCall& c, hipStream_t stream);
 hipError_t launch_embed_gradients(const EmbedCall& c, hipStream_t stream);
+
+// ------------------------------------------------------------------ rotary positions
+struct RotaryCall {
+    const void* x;             // may be out
+    void* out;
+    int bf16;                  // both
+    int64_t ldx, ldo, n;
+    int heads, dim, rot;
+    const void* positions;
+    int wide_ids;              // 64-bit positions
+    const uint64_t* turns;
+    int interleaved, inverse;
+    float amplitude;
+};
+hipError_t launch_rotary(const RotaryCall& c, hipStream_t stream);
+
+// ------------------------------------------------------------------ dropout
+struct DropoutCall {
+    const void *x, *residual;  // residual may be null, either may be out
+    void* out;
+    int x_bf16, out_bf16;      // the residual is of out's type
+    int64_t ldx, ldr, ldo, rows;
+    int cols;
+    uint64_t seed, step, drop48;   // p in units of 2^-48
+    uint32_t site;
+    float scale;               // 1 / (1 - p)
+};
+hipError_t launch_dropout(const DropoutCall& c, hipStream_t stream);
 
 }  // namespace agc
