@@ -375,6 +375,55 @@ typedef enum { AGC_ROTARY_PLAIN = 0, AGC_ROTARY_LINEAR = 1, AGC_ROTARY_BY_PARTS 
 agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double factor, double original_len,
                                   uint64_t* turns_out, double* amplitude_out);
 
+/* Differential attention in bfloat16: for every query head h and its key head h / (heads / kv_heads)
+ *   out = (softmax(scale q1 k1^T) - lambda_h softmax(scale q2 k2^T)) v
+ * over the keys of the query's own sequence, with `causal` over those that lie no later, the ends of both runs taken as the
+ * same place: of Lq queries and Lk keys, query i sees the keys 0 .. i + Lk - Lq.  A query that sees none gets zeros.
+ *   q_dev      device, tokens_q x (heads * 2 * head_dim): both maps' queries of a head lie side by side
+ *   k_dev, v_dev  device, tokens_k x (kv_heads * 2 * head_dim) and tokens_k x (kv_heads * value_dim)
+ *              row strides ldq, ldk, ldv elements.  Where head_dim and value_dim are D and 2 D, D = 32, 64 or 128, rows must begin at
+ *              multiples of 16 bytes (AGC_EALIGN) and are read where they lie; other widths may begin anywhere and are
+ *              copied to the workspace, widened to the next D that holds both
+ *   lambda_dev device, heads floats
+ *   q_end_dev, k_end_dev  device, n_seqs ends of the sequences in queries and in keys, not descending; sequence s has the
+ *              queries from q_end[s-1] (0 for the first) to q_end[s], and the keys alike.  Either may be empty.  Rows of out
+ *              behind the last sequence are left as they were.  Ends beyond the tensors count as their ends
+ *   k_begin_dev  device, n_seqs first keys, or NULL: the keys of sequence s are k_begin[s] .. k_end[s] - 1 instead, anywhere in
+ *              k and v, which are then a cache with room behind each sequence, or share keys
+ *   out_dev    device, tokens_q x (heads * value_dim), row stride ldo; overwritten
+ *   lse_dev    device, (2 * heads) x tokens_q floats, or NULL: receives log2 of the sum over keys of 2^(scale q_m k_m log2 e) of
+ *              map m of head h in row 2 h + m, -infinity without keys; what the gradients take
+ *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 0) bytes, 256-byte aligned
+ * Scores, maxima, sums and out are held in binary32; the maps enter their product with v as bfloat16, out is rounded once.
+ * The order of the sums is fixed.  NaN or infinity in a sequence reaches that sequence's results alone.
+ * 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads below 2^31, 1 <= n_seqs <= 2^20, heads a multiple of
+ * kv_heads, 1 <= head_dim <= 128, 1 <= value_dim <= 256. */
+int64_t agc_diff_attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int head_dim,
+                                      int value_dim, int gradients);
+agc_status agc_diff_attn_forward(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv,
+                                 int64_t tokens_q, int64_t tokens_k, int heads, int kv_heads, int head_dim, int value_dim,
+                                 const float* lambda_dev, const int32_t* q_end_dev, const int32_t* k_begin_dev,
+                                 const int32_t* k_end_dev, int n_seqs, float scale, int causal, void* out_dev, int64_t ldo,
+                                 float* lse_dev, void* workspace_dev, void* hip_stream);
+/* Its gradients, and the partial gradients of lambda (Sec. II-A): with lse as the forward pass left it,
+ *   dP = dout v^T,  D_m = sum over keys of P_m dP,  dS_1 = P_1 (dP - D_1),  dS_2 = -lambda P_2 (dP - D_2),
+ *   dq_m = scale dS_m k_m,  dk_m = scale dS_m^T q_m,  dv = (P_1 - lambda P_2)^T dout, summed over the heads that share them,
+ * and for every data partition p (a run of queries)  G_lambda[p, h] = - sum over its queries of D_2, binary32.
+ *   dout_dev   device, tokens_q x (heads * value_dim), row stride lddout, aligned as v
+ *   part_end_host  host, k_parts ends of the partitions in queries, not descending, the last tokens_q
+ *   dq_dev, dk_dev, dv_dev  device, as q, k and v, row strides lddq, lddk, lddv, any alignment; overwritten but for rows behind
+ *              the last sequence, which are left as they were
+ *   G_lambda_dev  device, where row 0 of G holds the gradients of lambda; row p lies p * ldg floats on; overwritten
+ *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 1) bytes, 256-byte aligned (enough for the forward pass too)
+ * The maps and dS enter the products as bfloat16, results are rounded once; sums are binary32 in a fixed order.  1 <= k_parts <= 256. */
+agc_status agc_diff_attn_partial_gradients(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev,
+                                           int64_t ldv, int64_t tokens_q, int64_t tokens_k, int heads, int kv_heads,
+                                           int head_dim, int value_dim, const float* lambda_dev, const int32_t* q_end_dev,
+                                           const int32_t* k_end_dev, int n_seqs, float scale, int causal, const float* lse_dev,
+                                           const void* dout_dev, int64_t lddout, const int64_t* part_end_host, int k_parts,
+                                           void* dq_dev, int64_t lddq, void* dk_dev, int64_t lddk, void* dv_dev, int64_t lddv,
+                                           float* G_lambda_dev, int64_t ldg, void* workspace_dev, void* hip_stream);
+
 /* Dropout into a residual:  out = residual + (U >= p ? x / (1 - p) : 0), one binary32 product and sum, rounded once to out's
  * type.  The mask is not stored: it follows from (seed, step, site, row, column), whatever the types and strides, so the
  * gradient is the same call on dout without a residual.  U = (u16 + r2 / 2^32) / 2^16 with

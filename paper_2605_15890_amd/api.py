@@ -30,6 +30,7 @@ EXPORTS = [
     "agc_embed_forward", "agc_embed_workspace_bytes", "agc_embed_partial_gradients",
     "agc_gated_workspace_bytes", "agc_gated_forward", "agc_gated_partial_gradients",
     "agc_muon_workspace_bytes", "agc_muon_update",
+    "agc_diff_attn_workspace_bytes", "agc_diff_attn_forward", "agc_diff_attn_partial_gradients",
     "agc_rotary_apply", "agc_rotary_frequencies", "agc_dropout",
     "agc_calibration_copy", "agc_debug_force_long", "agc_debug_sketch", "agc_debug_sketch_last", "agc_debug_sketch_max", "agc_debug_stream_rows", "agc_ls_workspace_floats", "agc_ls_partial_gradients", "agc_gd_update",
     "agc_phi_coef_balanced", "agc_alloc_bits", "agc_alloc_bits_dp", "agc_alloc_objective",
@@ -133,6 +134,15 @@ def load():
     L.agc_muon_update.argtypes = [_vp, _vp, _vp, _vp, C.c_int, C.c_int, C.c_int, C.c_float, C.c_float, C.c_int,
                                   C.c_float, C.c_float, C.c_int, _vp, _vp, _vp]
     L.agc_muon_update.restype = C.c_int
+    L.agc_diff_attn_workspace_bytes.argtypes = [C.c_int64, C.c_int64] + [C.c_int] * 6
+    L.agc_diff_attn_workspace_bytes.restype = C.c_int64
+    shapes = [_vp, C.c_int64] * 3 + [C.c_int64, C.c_int64] + [C.c_int] * 4
+    L.agc_diff_attn_forward.argtypes = shapes + [_vp, _vp, _vp, _vp, C.c_int, C.c_float, C.c_int, _vp, C.c_int64, _vp, _vp, _vp]
+    L.agc_diff_attn_forward.restype = C.c_int
+    L.agc_diff_attn_partial_gradients.argtypes = shapes + [_vp, _vp, _vp, C.c_int, C.c_float, C.c_int, _vp, _vp, C.c_int64, _vp,
+                                                           C.c_int, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp,
+                                                           C.c_int64, _vp, _vp]
+    L.agc_diff_attn_partial_gradients.restype = C.c_int
     L.agc_rotary_frequencies.argtypes = [C.c_int, C.c_double, C.c_int, C.c_double, C.c_double, _vp, _f64p]
     L.agc_rotary_frequencies.restype = C.c_int
     L.agc_rotary_apply.argtypes = [_vp, C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_int, _vp, C.c_int, _vp, C.c_int,
@@ -698,6 +708,81 @@ def agc_rotary_apply(x, heads, positions, turns, layout, out, amplitude=1.0, inv
     st = L.agc_rotary_apply(x.data_ptr(), kind, ldx, n, heads, row // heads, 2 * turns.numel(), positions.data_ptr(), width,
                             turns.data_ptr(), _ROTARY_LAYOUTS.get(layout, layout), amplitude, int(bool(inverse)),
                             out.data_ptr(), ldo, _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
+
+
+def agc_diff_attn_workspace_bytes(tokens_q, tokens_k, n_seqs, heads, kv_heads, head_dim, value_dim, gradients=False):
+    """gradients: of agc_diff_attn_partial_gradients too."""
+    return int(load().agc_diff_attn_workspace_bytes(int(tokens_q), int(tokens_k), int(n_seqs), int(heads), int(kv_heads),
+                                                    int(head_dim), int(value_dim), int(bool(gradients))))
+
+
+def _ends(t, n, what):
+    """A contiguous vector of n int32."""
+    import torch
+    if t.dim() != 1 or t.numel() != n or t.dtype is not torch.int32 or not t.is_contiguous():
+        raise AgcError(AGC_ESHAPE, f"{what} must be a contiguous vector of {n} int32")
+
+
+def _attn_operands(L, name, q, k, v, heads, kv_heads, lam, q_end, k_end, lse, workspace, gradients):
+    """The leading arguments of both attention calls, (tokens_q, head_dim, value_dim), and the number of sequences."""
+    import torch
+    bf16 = torch.bfloat16
+    if q.dim() != 2 or k.dim() != 2 or v.dim() != 2 or heads < 1 or kv_heads < 1 or q.shape[1] % (2 * heads) or v.shape[1] % kv_heads:
+        raise AgcError(AGC_ESHAPE, f"{name}: q, k and v are matrices of whole heads")
+    (nq, wide), (nk, n) = q.shape, (k.shape[0], q_end.numel())
+    d, e = wide // (2 * heads), v.shape[1] // kv_heads
+    ldq, ldk, ldv = _rows_of(q, nq, wide, bf16, "q"), _rows_of(k, nk, 2 * kv_heads * d, bf16, "k"), _rows_of(v, nk, kv_heads * e, bf16, "v")
+    if lam.dim() != 1 or lam.numel() != heads or lam.dtype is not torch.float32 or not lam.is_contiguous():
+        raise AgcError(AGC_ESHAPE, f"{name}: lam must be a contiguous vector of {heads} float32")
+    _ends(q_end, n, "q_end")
+    _ends(k_end, n, "k_end")
+    if lse is not None and (lse.numel() != 2 * heads * nq or lse.dtype is not torch.float32 or not lse.is_contiguous()):
+        raise AgcError(AGC_ESHAPE, f"{name}: lse must be ({2 * heads}, {nq}) float32, contiguous")
+    if workspace.nbytes < L.agc_diff_attn_workspace_bytes(nq, nk, n, heads, kv_heads, d, e, gradients):
+        raise AgcError(AGC_ESHAPE, f"{name}: the workspace is too small")
+    head = (q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, nq, nk, heads, kv_heads, d, e, lam.data_ptr(), q_end.data_ptr())
+    _on_current_gpu(name, q, k, v, lam, q_end, k_end, workspace)
+    return head, (nq, d, e), n
+
+
+def agc_diff_attn_forward(q, k, v, heads, kv_heads, lam, q_end, k_end, scale, causal, out, workspace, lse=None, k_begin=None,
+                          stream=None, check=True):
+    """Differential attention, all bfloat16: q (tokens_q, heads * 2 * d), k (tokens_k, kv_heads * 2 * d), v (tokens_k,
+    kv_heads * e), out (tokens_q, heads * e).  q_end, k_end (and k_begin) are int32 vectors on the GPU, an entry a sequence;
+    lse, (2 * heads, tokens_q) float32, receives what the gradients need."""
+    L = load()
+    head, (nq, d, e), n = _attn_operands(L, "agc_diff_attn_forward", q, k, v, heads, kv_heads, lam, q_end, k_end, lse, workspace, 0)
+    ldo = _rows_of(out, nq, heads * e, q.dtype, "out")
+    if k_begin is not None:
+        _ends(k_begin, n, "k_begin")
+    _on_current_gpu("agc_diff_attn_forward", *[t for t in (out, lse, k_begin) if t is not None])
+    st = L.agc_diff_attn_forward(*head, None if k_begin is None else k_begin.data_ptr(), k_end.data_ptr(), n, scale,
+                                 int(bool(causal)), out.data_ptr(), ldo, None if lse is None else lse.data_ptr(),
+                                 workspace.data_ptr(), _stream_handle(stream))
+    if check and st != AGC_OK:
+        raise AgcError(st, L.agc_last_error(None).decode())
+    return st
+
+
+def agc_diff_attn_partial_gradients(q, k, v, heads, kv_heads, lam, q_end, k_end, scale, causal, lse, dout, part_end, dq, dk, dv,
+                                    G_lambda, workspace, stream=None, check=True):
+    """dq, dk, dv (bfloat16, as q, k, v) and, for each partition of the queries, the gradient of lam: G_lambda is a
+    (k_parts, heads) float32 view of rows of G.  lse is agc_diff_attn_forward's of the same inputs."""
+    import torch
+    L = load()
+    name, parts = "agc_diff_attn_partial_gradients", len(part_end)
+    head, (nq, d, e), n = _attn_operands(L, name, q, k, v, heads, kv_heads, lam, q_end, k_end, lse, workspace, 1)
+    lddout = _rows_of(dout, nq, heads * e, q.dtype, "dout")
+    lddq, lddk, lddv = (_rows_of(g, t.shape[0], t.shape[1], q.dtype, w) for g, t, w in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
+    ldg = _rows_of(G_lambda, parts, heads, torch.float32, "G_lambda")
+    _on_current_gpu(name, lse, dout, dq, dk, dv, G_lambda)
+    st = L.agc_diff_attn_partial_gradients(*head, k_end.data_ptr(), n, scale, int(bool(causal)), lse.data_ptr(), dout.data_ptr(),
+                                           lddout, struct.pack(f"{parts}q", *[int(x) for x in part_end]), parts, dq.data_ptr(), lddq,
+                                           dk.data_ptr(), lddk, dv.data_ptr(), lddv, G_lambda.data_ptr(), ldg,
+                                           workspace.data_ptr(), _stream_handle(stream))
     if check and st != AGC_OK:
         raise AgcError(st, L.agc_last_error(None).decode())
     return st

@@ -1,0 +1,193 @@
+// Pieces of differential attention that its kernels share.
+//
+//   S_m = scale q_m k_m^T,  P_m = softmax of S_m over the keys in sight,  m = 1, 2;  out = (P_1 - lambda P_2) v
+// Query head h holds its two maps' queries side by side, and shares keys and values with the other heads of its group.  A
+// "row" is a (token, head of the group) pair: the rows of a sequence and key head are one matrix, whatever the group.
+//
+// All products are v_mfma_f32_32x32x16_bf16.  A wave owns 32 rows (or keys) as the columns of its products, so what
+// belongs to a row stays in lane & 31 and the operands of its own side stay in registers; the other side passes through LDS
+// in tiles that the whole workgroup shares.  A row of such a tile, both maps of a key or a value, has 4 D bytes; its 16-byte
+// chunks are permuted by the row's low bits so that both kinds of reads fall on all banks: 32 rows at one chunk (an operand
+// as it lies) and, by the transposing read, four rows at four neighbouring chunks (an operand turned).  Tiles come by loads
+// that go from memory to LDS directly; the permutation is made by choosing whose chunk a lane fetches.
+//
+// The score product takes its keys in an order with bits 2 and 3 of the place swapped: a lane then ends with the scores of
+// eight neighbouring keys twice, which is what the next product's operand wants, and P never leaves the registers.
+#pragma once
+
+#include "agc_operators.h"
+#include "agc_vector.h"
+
+namespace agc {
+
+typedef float attn_f32x16 __attribute__((ext_vector_type(16)));
+typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
+typedef short attn_s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.44269504088896f;
+
+// Division of row numbers by the heads of a group: n / d = n * magic >> shift for n < 2^31.
+struct Divider {
+    uint32_t d, magic, shift;
+    explicit Divider(uint32_t by) : d(by)
+    {
+        int bits = 0;
+        while ((1u << bits) < by) ++bits;
+        shift = 31 + bits;
+        magic = (uint32_t)(((uint64_t)1 << shift) / by + ((by & (by - 1)) != 0));
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (uint32_t)(((uint64_t)n * magic) >> shift); }
+};
+
+// What the kernels know of a call; operands as laid out: heads of D and 2 D values, 16-byte aligned rows.
+struct Attn {
+    const uint16_t *q, *k, *v;
+    int64_t ldq, ldk, ldv;
+    const float* lambda;
+    const int32_t *q_end, *k_begin, *k_end;
+    int n_seqs, tokens_q, tokens_k;
+    int heads, kv_heads, d, e;
+    Divider group;
+    int causal;
+    float scale;          // of the scores
+    float to_log2;        // scale * log2(e): the maps are formed with powers of two
+};
+
+// A sequence's place in a tile's coordinates.
+struct AttnSeq {
+    int q0, lq, k0, lk;
+};
+
+__device__ __forceinline__ AttnSeq attn_sequence(const Attn& a, int s)
+{
+    AttnSeq o;
+    const auto within = [](int v, int lo, int hi) { return min(max(v, lo), hi); };
+    o.q0 = s ? within(a.q_end[s - 1], 0, a.tokens_q) : 0;
+    o.lq = within(a.q_end[s], o.q0, a.tokens_q) - o.q0;
+    o.k0 = a.k_begin ? within(a.k_begin[s], 0, a.tokens_k) : s ? within(a.k_end[s - 1], 0, a.tokens_k) : 0;
+    o.lk = within(a.k_end[s], o.k0, a.tokens_k) - o.k0;
+    return o;
+}
+
+// Which sequence tile `slot` belongs to, where sequence s has the tiles from begin_s * unit / size + s on: room for its
+// ceil(length * unit / size), found without a table of them.  `end` are the sequences' ends.  Each lane looks at one end.
+__device__ __forceinline__ int attn_first_slot(const int32_t* end, int s, int most, uint32_t unit, uint32_t size)
+{
+    const uint32_t begin = s ? (uint32_t)min(max(end[s - 1], 0), most) : 0;
+    return (int)(begin * unit / size) + s;
+}
+
+__device__ __forceinline__ int attn_find(const int32_t* end, int n_seqs, int most, uint32_t unit, uint32_t size, int slot)
+{
+    const int lane = threadIdx.x & 63;
+    int count = 0;
+    for (int base = 0; base < n_seqs; base += 64) {
+        const int s = base + lane;
+        count += __popcll(__ballot(s < n_seqs && attn_first_slot(end, min(s, n_seqs - 1), most, unit, size) <= slot));
+    }
+    return max(0, min(count, n_seqs) - 1);
+}
+
+// Keys in sight of query t.
+__device__ __forceinline__ int attn_seen(const Attn& a, const AttnSeq& q, int t)
+{
+    return a.causal ? min(max(t + q.lk - q.lq + 1, 0), q.lk) : q.lk;
+}
+
+template <int D>
+struct AttnTile {
+    static constexpr int kRow = 4 * D, kChunks = kRow / 16;
+    // what the chunks of a row are permuted by
+    static __device__ __forceinline__ int mix(int row)
+    {
+        if constexpr (D == 32) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);   // two rows span the banks
+        return (row & 3) << 2 | ((row >> 2) & 3);
+    }
+
+    // Rows first .. first + ROWS - 1 of a matrix in memory, `at(row)` its address, to LDS.
+    template <int ROWS, int WAVES, typename At>
+    static __device__ __forceinline__ void load(char* lds, int wave, int lane, const At& at)
+    {
+        constexpr int kPer = 64 / kChunks;   // rows a wave fetches at once
+        constexpr int kTimes = ROWS / kPer / WAVES;
+        static_assert(ROWS % (kPer * WAVES) == 0, "every wave fetches alike");
+#pragma unroll
+        for (int i = 0; i < kTimes; ++i) {
+            const int c = i * WAVES + wave, row = c * kPer + lane / kChunks;
+            load16_to_lds(at(row) + ((lane % kChunks) ^ mix(row)) * 16, lds + c * 1024);
+        }
+    }
+
+    // Chunk c of a row: eight values as they lie.
+    static __device__ __forceinline__ tile_bf16x8 straight(const char* lds, int row, int c)
+    {
+        return *reinterpret_cast<const tile_bf16x8*>(lds + row * kRow + ((c ^ mix(row)) << 4));
+    }
+
+    // Column (lane & 31) of the 32 columns that start at chunk c, rows row0 + 8 (lane / 32) + 0 .. 7.
+    static __device__ __forceinline__ tile_bf16x8 turned(const char* lds, int row0, int c, int lane)
+    {
+        typedef __attribute__((address_space(3))) attn_s16x4* Lds;
+        const int i = lane & 15, row = row0 + 8 * (lane >> 5) + (i >> 2), chunk = c + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+        const char* p0 = lds + row * kRow + ((chunk ^ mix(row)) << 4) + (i & 1) * 8;
+        const char* p1 = lds + (row + 4) * kRow + ((chunk ^ mix(row + 4)) << 4) + (i & 1) * 8;
+        const attn_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p0), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p1);
+        return __builtin_bit_cast(tile_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// Place of a lane's operand row whose scores the lane's registers then hold in order: bits 2 and 3 swapped.
+__device__ __forceinline__ int attn_swapped(int i) { return (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1; }
+
+// Row that register r of a 32 x 32 product belongs to, with the operand's rows swapped (score products) and as they are.
+__device__ __forceinline__ int attn_row_swapped(int r, int lane) { return 16 * (r >> 3) + 8 * (lane >> 5) + (r & 7); }
+__device__ __forceinline__ int attn_row_plain(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+__device__ __forceinline__ attn_f32x16 attn_mfma(const tile_bf16x8& a, const tile_bf16x8& b, const attn_f32x16& c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// The other half's value of the same column.
+__device__ __forceinline__ float attn_other_half(float v) { return __shfl_xor(v, 32); }
+
+// Registers 8 b .. 8 b + 7 as an operand.
+__device__ __forceinline__ tile_bf16x8 attn_operand(const float v[16], int b)
+{
+    return __builtin_bit_cast(tile_bf16x8, bf16_pack8(v + 8 * b));
+}
+
+// Values of a column of C (32 rows of `acc`, times `factor`) to a row of an output, as far as `width` goes.
+__device__ __forceinline__ void attn_store(uint16_t* row, int at, int width, int lane, const attn_f32x16& acc, float factor)
+{
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+        const int c = at + attn_row_plain(r, lane);
+        if (c + 4 <= width) {
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            const u32x2 v = {bf16_bits(acc[r] * factor) | bf16_bits(acc[r + 1] * factor) << 16,
+                             bf16_bits(acc[r + 2] * factor) | bf16_bits(acc[r + 3] * factor) << 16};
+            __builtin_memcpy(row + c, &v, 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i < width) row[c + i] = (uint16_t)bf16_bits(acc[r + i] * factor);
+        }
+    }
+}
+
+__device__ __forceinline__ void attn_wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+
+// ------------------------------------------------------------------ laying operands out
+struct AttnPack {
+    const uint16_t* from;
+    uint16_t* to;
+    int64_t ld;
+    int rows, parts, width, up;   // `parts` runs of `width` values a row become runs of `up`
+};
+
+hipError_t attn_pack(const AttnPack* jobs, int n, hipStream_t stream);
+// Fills `a` from the call, copying operands of other widths to the workspace; `place` moves on behind them.
+hipError_t attn_lay_out(const AttnCall& c, Attn& a, const uint16_t*& dout, int64_t& lddout, char*& place, hipStream_t stream);
+
+}  // namespace agc

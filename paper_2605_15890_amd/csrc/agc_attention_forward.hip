@@ -1,0 +1,344 @@
+// Differential attention, forward:  out = (softmax(scale q1 k1^T) - lambda softmax(scale q2 k2^T)) v  over the keys of each
+// sequence that are in sight.  Both maps are formed in one pass over the keys with their running maxima and sums.
+#include <algorithm>
+
+#include "agc_attention.h"
+
+namespace agc {
+
+namespace {
+
+struct AttnForward {
+    Attn a;
+    uint16_t* out;
+    int64_t ldo;
+    float* lse;            // may be null
+    int slots, splits;
+    float* part;           // of splits: per (split, row) both maps' sums of 2 D values
+    tile_f32x4* stat;      // and their maxima and sums
+};
+
+// Once a row's largest score has grown by more than this many powers of two, what is summed so far is scaled down to it.
+constexpr float kGrowth = 8.0f;
+
+template <int D, int WAVES, int KT>
+__global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
+{
+    using Tile = AttnTile<D>;
+    constexpr int E = 2 * D, kSteps = D / 16, kBlocks = E / 32;
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][KT * Tile::kRow];   // buffer; keys, values
+    const Attn& a = f.a;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int total = f.slots * a.kv_heads * f.splits;
+    const int id = xcd_order(blockIdx.x, total);
+    const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
+    const uint32_t group = a.group.d;
+
+    const int s = attn_find(a.q_end, a.n_seqs, a.tokens_q, group, 32 * WAVES, slot);
+    const AttnSeq seq = attn_sequence(a, s);
+    const int first = attn_first_slot(a.q_end, s, a.tokens_q, group, 32 * WAVES);
+    const int rows = seq.lq * (int)group, tiles = (rows + 32 * WAVES - 1) / (32 * WAVES);
+    // the last tiles see most keys and come first
+    const int tile = tiles - 1 - (slot - first);
+    if (tile < 0 || tile >= tiles) return;
+
+    const int row_ = tile * 32 * WAVES + wave * 32 + (lane & 31);
+    const int row = min(row_, rows - 1), t = (int)a.group(row), g = row - t * (int)group, head = head_k * (int)group + g;
+    const int seen = attn_seen(a, seq, t);
+    const int seen_least = __builtin_amdgcn_readfirstlane(seen), seen_most = __builtin_amdgcn_readlane(seen, 31);
+    const int last_row = min(tile * 32 * WAVES + 32 * WAVES, rows) - 1;
+    const int keys = attn_seen(a, seq, (int)a.group(last_row));   // of the tile
+    const int run = (keys + f.splits * KT - 1) / (f.splits * KT) * KT;
+    const int begin = min(split * run, keys), end = min(begin + run, keys);
+
+    tile_bf16x8 q[2][kSteps];
+    {
+        const uint16_t* p = a.q + (int64_t)(seq.q0 + t) * a.ldq + (int64_t)head * E + (lane >> 5) * 8;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) q[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + m * D + i * 16);
+    }
+    const char* const keys_at = reinterpret_cast<const char*>(a.k + (int64_t)seq.k0 * a.ldk + head_k * E);
+    const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
+    const auto fetch = [&](int j0, int buffer) {
+        Tile::template load<KT, WAVES>(lds[buffer][0], wave, lane, [&](int r) { return keys_at + (int64_t)min(j0 + r, seq.lk - 1) * a.ldk * 2; });
+        Tile::template load<KT, WAVES>(lds[buffer][1], wave, lane, [&](int r) { return values_at + (int64_t)min(j0 + r, seq.lk - 1) * a.ldv * 2; });
+    };
+
+    attn_f32x16 acc[2][kBlocks];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_f32x16{};
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
+
+    if (begin < end) fetch(begin, 0);
+    int buffer = 0;
+    for (int j0 = begin; j0 < end; j0 += KT, buffer ^= 1) {
+        attn_wait_loads();
+        __syncthreads();
+        if (j0 + KT < end) fetch(j0 + KT, buffer ^ 1);
+        const char *const k_lds = lds[buffer][0], *const v_lds = lds[buffer][1];
+#pragma unroll
+        for (int sub = 0; sub < KT / 32; ++sub) {
+            const int j = j0 + sub * 32;
+            if (j >= min(seen_most, end)) break;
+            const bool masked = j + 32 > min(seen_least, end);
+            tile_bf16x8 p[2][2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                attn_f32x16 score{};
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i)
+                    score = attn_mfma(Tile::straight(k_lds, sub * 32 + attn_swapped(lane & 31), m * (D / 8) + i * 2 + (lane >> 5)), q[m][i], score);
+                float v[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) v[r] = score[r] * a.to_log2;
+                if (masked) {
+                    const int left = min(seen, end) - j;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) v[r] = attn_row_swapped(r, lane) < left ? v[r] : -INFINITY;
+                }
+                float most = v[0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) most = fmaxf(most, v[r]);
+                most = fmaxf(most, attn_other_half(most));
+                if (__any(most > top[m] + kGrowth)) {
+                    const float now = fmaxf(top[m], most);
+                    const float shrink = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[m] - now);
+                    top[m] = now;
+                    sum[m] *= shrink;
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[m][b][r] *= shrink;
+                }
+                const float from = top[m] == -INFINITY ? 0.0f : top[m];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    v[r] = __builtin_amdgcn_exp2f(v[r] - from);
+                    sum[m] += v[r];
+                }
+                p[m][0] = attn_operand(v, 0);
+                p[m][1] = attn_operand(v, 1);
+            }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const tile_bf16x8 v = Tile::turned(v_lds, sub * 32 + i * 16, b * 4, lane);
+                    acc[0][b] = attn_mfma(v, p[0][i], acc[0][b]);
+                    acc[1][b] = attn_mfma(v, p[1][i], acc[1][b]);
+                }
+        }
+    }
+
+    if (row_ >= rows) return;   // both halves of a row alike: the exchange below stays among lanes that go on
+#pragma unroll
+    for (int m = 0; m < 2; ++m) sum[m] += attn_other_half(sum[m]);
+    if (f.splits > 1) {
+        const int64_t at = (int64_t)split * a.tokens_q * a.heads + (int64_t)head_k * a.tokens_q * group + (int64_t)seq.q0 * group + row;
+        if (lane < 32) f.stat[at] = tile_f32x4{top[0], sum[0], top[1], sum[1]};
+        if (begin < end) {
+            float* o = f.part + at * 2 * E;
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4)
+                        *reinterpret_cast<tile_f32x4*>(o + m * E + b * 32 + attn_row_plain(r, lane)) =
+                            tile_f32x4{acc[m][b][r], acc[m][b][r + 1], acc[m][b][r + 2], acc[m][b][r + 3]};
+        }
+        return;
+    }
+    // a row without keys in sight is zeros
+    const float by1 = sum[0] == 0.0f ? 0.0f : 1.0f / sum[0], by2 = sum[1] == 0.0f ? 0.0f : a.lambda[head] / sum[1];
+    uint16_t* o = f.out + (int64_t)(seq.q0 + t) * f.ldo + (int64_t)head * a.e;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+        attn_f32x16 v;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[r] = acc[0][b][r] * by1 - acc[1][b][r] * by2;
+        attn_store(o, b * 32, a.e, lane, v, 1.0f);
+    }
+    if (f.lse && lane < 32) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            f.lse[(int64_t)(2 * head + m) * a.tokens_q + seq.q0 + t] = sum[m] == 0.0f ? -INFINITY : top[m] + __builtin_amdgcn_logf(sum[m]);
+    }
+}
+
+// Joins the splits of a row, a wave each: sums scaled to the largest maximum.
+template <int D>
+__global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
+{
+    constexpr int E = 2 * D, kPer = E / 64;
+    const Attn& a = f.a;
+    const int lane = threadIdx.x & 63;
+    const int64_t all = (int64_t)a.tokens_q * a.heads, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int last = min(max(a.q_end[a.n_seqs - 1], 0), a.tokens_q);
+    if (at >= all) return;
+    const int group = (int)a.group.d;
+    const int64_t of_head = (int64_t)a.tokens_q * group;
+    const int head_k = (int)(at / of_head), row = (int)(at - head_k * of_head), t = (int)a.group(row), head = head_k * group + row - t * group;
+    if (t >= last) return;   // behind the last sequence: left as it was
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f}, v[2][kPer] = {};
+    for (int s = 0; s < f.splits; ++s) {
+        const tile_f32x4 x = f.stat[s * all + at];
+        // an empty split has no largest score and no sums in memory
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            if (x[2 * m + 1] == 0.0f) continue;
+            const float now = fmaxf(top[m], x[2 * m]);
+            const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[m] - now);
+            const float add = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x[2 * m] - now);
+            top[m] = now;
+            sum[m] = sum[m] * keep + x[2 * m + 1] * add;
+            const float* o = f.part + (s * all + at) * 2 * E + m * E + lane;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) v[m][i] = v[m][i] * keep + o[i * 64] * add;
+        }
+    }
+    const float by1 = sum[0] == 0.0f ? 0.0f : 1.0f / sum[0], by2 = sum[1] == 0.0f ? 0.0f : a.lambda[head] / sum[1];
+    uint16_t* o = f.out + t * f.ldo + (int64_t)head * a.e;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (lane + i * 64 < a.e) o[lane + i * 64] = (uint16_t)bf16_bits(v[0][i] * by1 - v[1][i] * by2);
+    if (f.lse && lane < 2)
+        f.lse[(int64_t)(2 * head + lane) * a.tokens_q + t] =
+            sum[lane] == 0.0f ? -INFINITY : top[lane] + __builtin_amdgcn_logf(sum[lane]);
+}
+
+template <int D, int WAVES, int KT>
+hipError_t launch(AttnForward f, hipStream_t stream)
+{
+    k_attn_forward<D, WAVES, KT><<<f.slots * f.a.kv_heads * f.splits, 64 * WAVES, 0, stream>>>(f);
+    if (f.splits > 1) {
+        const int64_t all = (int64_t)f.a.tokens_q * f.a.heads;
+        k_attn_join<D><<<(uint32_t)((all + 3) / 4), 256, 0, stream>>>(f);
+    }
+    return hipGetLastError();
+}
+
+// Rows of a workgroup, and over how many workgroups the keys are split.
+struct Shape {
+    int waves, slots, splits;
+};
+
+Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D)
+{
+    Shape o;
+    const int64_t rows = tokens_q * (heads / kv_heads);
+    // up to 32 rows a sequence: one wave has them all
+    o.waves = rows <= (int64_t)32 * n_seqs ? 1 : D == 128 ? 4 : 8;
+    o.slots = (int)(rows / (32 * o.waves)) + n_seqs;
+    const int64_t blocks = (int64_t)o.slots * kv_heads, wanted = o.waves == 1 ? 1024 : 256;
+    const int64_t keys = tokens_k / n_seqs;
+    const int64_t most = std::max<int64_t>(1, keys / 128);
+    o.splits = (int)std::max<int64_t>(1, std::min({wanted / std::max<int64_t>(1, blocks), most, (int64_t)64}));
+    return o;
+}
+
+int64_t splits_bytes(const Shape& s, int64_t tokens_q, int heads, int D)
+{
+    return s.splits > 1 ? round_up((int64_t)s.splits * tokens_q * heads * (4 * D * 4 + 16), 256) : 0;
+}
+
+}  // namespace
+
+int attn_width(int d, int e) { return d <= 32 && e <= 64 ? 32 : d <= 64 && e <= 128 ? 64 : 128; }
+
+namespace {
+
+struct PackJobs {
+    AttnPack job[4];
+};
+
+__global__ __launch_bounds__(256) void k_attn_pack(PackJobs jobs)
+{
+    const AttnPack& j = jobs.job[blockIdx.y];
+    const int per = j.up / 8, chunks = j.parts * per, at_once = max(1, 256 / chunks);
+    const int sub = threadIdx.x / chunks, c0 = threadIdx.x - sub * chunks;
+    if (sub >= at_once) return;
+    for (int64_t r = (int64_t)blockIdx.x * at_once + sub; r < j.rows; r += (int64_t)gridDim.x * at_once)
+        for (int c = c0; c < chunks; c += 256) {
+            const int part = c / per, in = (c - part * per) * 8;
+            float v[8];
+            load8(j.from + r * j.ld + part * j.width + min(in, j.width), max(0, min(8, j.width - in)), v);
+            store16(j.to + r * j.parts * j.up + c * 8, bf16_pack8(v));
+        }
+}
+
+}  // namespace
+
+hipError_t attn_pack(const AttnPack* jobs, int n, hipStream_t stream)
+{
+    if (n == 0) return hipSuccess;
+    PackJobs all{};
+    int64_t blocks = 1;
+    for (int i = 0; i < n; ++i) {
+        all.job[i] = jobs[i];
+        const int at_once = std::max(1, 256 / (jobs[i].parts * jobs[i].up / 8));
+        blocks = std::max(blocks, ((int64_t)jobs[i].rows + at_once - 1) / at_once);
+    }
+    k_attn_pack<<<dim3((uint32_t)std::min<int64_t>(blocks, 8192), n), 256, 0, stream>>>(all);
+    return hipGetLastError();
+}
+
+hipError_t attn_lay_out(const AttnCall& c, Attn& a, const uint16_t*& dout, int64_t& lddout, char*& place, hipStream_t stream)
+{
+    const int D = attn_width(c.d, c.e), E = 2 * D;
+    a.q = static_cast<const uint16_t*>(c.q), a.k = static_cast<const uint16_t*>(c.k), a.v = static_cast<const uint16_t*>(c.v);
+    a.ldq = c.ldq, a.ldk = c.ldk, a.ldv = c.ldv;
+    a.lambda = c.lambda, a.q_end = c.q_end, a.k_begin = c.k_begin, a.k_end = c.k_end;
+    a.n_seqs = c.n_seqs, a.tokens_q = (int)c.tokens_q, a.tokens_k = (int)c.tokens_k;
+    a.heads = c.heads, a.kv_heads = c.kv_heads, a.d = c.d, a.e = c.e;
+    a.causal = c.causal, a.scale = c.scale, a.to_log2 = c.scale * kLog2e;
+    dout = static_cast<const uint16_t*>(c.dout), lddout = c.lddout;
+    AttnPack jobs[4];
+    int n = 0;
+    const auto lay = [&](const uint16_t*& p, int64_t& ld, int64_t rows, int parts, int width, int up) {
+        if (width == up) return;
+        uint16_t* to = reinterpret_cast<uint16_t*>(place);
+        if (rows > 0) jobs[n++] = {p, to, ld, (int)rows, parts, width, up};
+        p = to, ld = (int64_t)parts * up;
+        place += round_up(rows * parts * up * 2, 256);
+    };
+    lay(a.q, a.ldq, c.tokens_q, 2 * c.heads, c.d, D);
+    lay(a.k, a.ldk, c.tokens_k, 2 * c.kv_heads, c.d, D);
+    lay(a.v, a.ldv, c.tokens_k, c.kv_heads, c.e, E);
+    if (dout) lay(dout, lddout, c.tokens_q, c.heads, c.e, E);
+    return attn_pack(jobs, n, stream);
+}
+
+int64_t attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int d, int e, int gradients)
+{
+    const int D = attn_width(d, e);
+    int64_t bytes = 256;
+    if (d != D) bytes += round_up(tokens_q * heads * 4 * D, 256) + round_up(tokens_k * kv_heads * 4 * D, 256);
+    if (e != 2 * D) bytes += round_up(tokens_k * kv_heads * 4 * D, 256) + (gradients ? round_up(tokens_q * heads * 4 * D, 256) : 0);
+    if (gradients) bytes += round_up(tokens_q * heads * 8, 256);
+    return bytes + splits_bytes(shape_of(tokens_q, tokens_k, n_seqs, heads, kv_heads, D), tokens_q, heads, D);
+}
+
+hipError_t launch_attn_forward(const AttnCall& c, hipStream_t stream)
+{
+    AttnForward f{Attn{.group = Divider(c.heads / c.kv_heads)}};
+    const uint16_t* none;
+    int64_t none_ld;
+    char* place = c.workspace;
+    const hipError_t e = attn_lay_out(c, f.a, none, none_ld, place, stream);
+    if (e != hipSuccess) return e;
+    const int D = attn_width(c.d, c.e);
+    const Shape s = shape_of(c.tokens_q, c.tokens_k, c.n_seqs, c.heads, c.kv_heads, D);
+    f.out = static_cast<uint16_t*>(c.out), f.ldo = c.ldo, f.lse = c.lse, f.slots = s.slots, f.splits = s.splits;
+    f.stat = reinterpret_cast<tile_f32x4*>(place);
+    f.part = reinterpret_cast<float*>(place + (int64_t)s.splits * c.tokens_q * c.heads * 16);
+    if (D == 32) return s.waves == 1 ? launch<32, 1, 64>(f, stream) : launch<32, 8, 64>(f, stream);
+    if (D == 64) return s.waves == 1 ? launch<64, 1, 32>(f, stream) : launch<64, 8, 64>(f, stream);
+    return s.waves == 1 ? launch<128, 1, 32>(f, stream) : launch<128, 4, 64>(f, stream);
+}
+
+}  // namespace agc

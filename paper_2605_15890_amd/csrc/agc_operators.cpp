@@ -62,6 +62,34 @@ agc_status gated_arguments(const char* name, const agc::GatedCall& c, int act)
     return AGC_OK;
 }
 
+agc_status attn_arguments(const char* name, const agc::AttnCall& c, bool gradients)
+{
+    const std::string n = name;
+    if (c.tokens_q < 0 || c.tokens_q > kMostTokens || c.tokens_k < 0 || c.tokens_k > kMostTokens || c.n_seqs < 1 || c.n_seqs > (1 << 20))
+        return refuse(AGC_ESHAPE, n + ": tokens_q and tokens_k must be 0..2^26, n_seqs 1..2^20");
+    if (c.heads < 1 || c.kv_heads < 1 || c.heads > kMostWidth || c.heads % c.kv_heads || c.d < 1 || c.d > 128 || c.e < 1 || c.e > 256)
+        return refuse(AGC_ESHAPE, n + ": heads must be a multiple of kv_heads, head_dim 1..128, value_dim 1..256");
+    if (c.tokens_q * c.heads > INT32_MAX || c.tokens_k * c.kv_heads > INT32_MAX || (int64_t)c.n_seqs * c.kv_heads > (1 << 24))
+        return refuse(AGC_ESHAPE, n + ": tokens times heads must be below 2^31, n_seqs * kv_heads at most 2^24");
+    if (!std::isfinite(c.scale)) return refuse(AGC_EINVAL, n + ": scale must be finite");
+    if ((c.tokens_q > 0 && !c.q) || (c.tokens_k > 0 && (!c.k || !c.v)) || !c.lambda || !c.q_end || !c.k_end || !c.workspace)
+        return refuse(AGC_EINVAL, n + ": null pointer");
+    const int64_t row_q = (int64_t)2 * c.heads * c.d, row_k = (int64_t)2 * c.kv_heads * c.d;
+    if (c.ldq < row_q || c.ldk < row_k || c.ldv < (int64_t)c.kv_heads * c.e) return refuse(AGC_ESHAPE, n + ": a row stride is smaller than the row");
+    // heads of just the kernels' widths are read where they lie, 16 bytes at a time
+    const int D = agc::attn_width(c.d, c.e);
+    const uintptr_t unit_d = c.d == D ? 16 : 2, unit_e = c.e == 2 * D ? 16 : 2;
+    const auto strided = [](int64_t ld, int64_t rows, uintptr_t unit) { return unit == 16 && rows > 1 && ld % 8; };
+    if (misaligned(c.q, unit_d) || misaligned(c.k, unit_d) || misaligned(c.v, unit_e) || strided(c.ldq, c.tokens_q, unit_d) ||
+        strided(c.ldk, c.tokens_k, unit_d) || strided(c.ldv, c.tokens_k, unit_e) ||
+        (gradients && (misaligned(c.dout, unit_e) || strided(c.lddout, c.tokens_q, unit_e))))
+        return refuse(AGC_EALIGN, n + ": rows of heads that are read where they lie need 16-byte alignment");
+    if (misaligned(c.lambda, 4) || misaligned(c.q_end, 4) || misaligned(c.k_begin, 4) || misaligned(c.k_end, 4) || misaligned(c.lse, 4) ||
+        misaligned(c.workspace, 256))
+        return refuse(AGC_EALIGN, n + ": vectors need their elements' alignment, the workspace 256 bytes");
+    return AGC_OK;
+}
+
 bool known_type(int type) { return type == AGC_TYPE_F32 || type == AGC_TYPE_BF16; }
 uintptr_t bytes_of(int type) { return type == AGC_TYPE_F32 ? 4 : 2; }
 
@@ -285,6 +313,68 @@ agc_status agc_dropout(const void* x_dev, int x_type, int64_t ldx, const void* r
     c.drop48 = (uint64_t)std::llround(p * 281474976710656.0);
     c.scale = p < 1 ? (float)(1 / (1 - p)) : 0.0f;
     return launched(agc::launch_dropout(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
+}
+
+int64_t agc_diff_attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int head_dim,
+                                      int value_dim, int gradients)
+{
+    if (tokens_q < 0 || tokens_q > kMostTokens || tokens_k < 0 || tokens_k > kMostTokens || n_seqs < 1 || n_seqs > (1 << 20) || heads < 1 ||
+        kv_heads < 1 || heads > kMostWidth || heads % kv_heads || head_dim < 1 || head_dim > 128 || value_dim < 1 || value_dim > 256)
+        return 0;
+    return agc::attn_workspace_bytes(tokens_q, tokens_k, n_seqs, heads, kv_heads, head_dim, value_dim, gradients != 0);
+}
+
+agc_status agc_diff_attn_forward(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv,
+                                 int64_t tokens_q, int64_t tokens_k, int heads, int kv_heads, int head_dim, int value_dim,
+                                 const float* lambda_dev, const int32_t* q_end_dev, const int32_t* k_begin_dev,
+                                 const int32_t* k_end_dev, int n_seqs, float scale, int causal, void* out_dev, int64_t ldo,
+                                 float* lse_dev, void* workspace_dev, void* hip_stream)
+{
+    const char* const name = "agc_diff_attn_forward";
+    agc::AttnCall c{};
+    c.q = q_dev, c.k = k_dev, c.v = v_dev, c.ldq = ldq, c.ldk = ldk, c.ldv = ldv, c.tokens_q = tokens_q, c.tokens_k = tokens_k;
+    c.heads = heads, c.kv_heads = kv_heads, c.d = head_dim, c.e = value_dim, c.lambda = lambda_dev;
+    c.q_end = q_end_dev, c.k_begin = k_begin_dev, c.k_end = k_end_dev, c.n_seqs = n_seqs, c.causal = causal != 0, c.scale = scale;
+    c.lse = lse_dev, c.workspace = static_cast<char*>(workspace_dev);
+    const agc_status st = attn_arguments(name, c, false);
+    if (st != AGC_OK) return st;
+    if (!out_dev && tokens_q > 0) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (ldo < (int64_t)heads * value_dim) return refuse(AGC_ESHAPE, std::string(name) + ": a row stride is smaller than the row");
+    if (misaligned(out_dev, 2)) return refuse(AGC_EALIGN, std::string(name) + ": out needs 2-byte alignment");
+    if (tokens_q == 0) return AGC_OK;
+    c.out = out_dev, c.ldo = ldo;
+    return launched(agc::launch_attn_forward(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
+}
+
+agc_status agc_diff_attn_partial_gradients(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev,
+                                           int64_t ldv, int64_t tokens_q, int64_t tokens_k, int heads, int kv_heads,
+                                           int head_dim, int value_dim, const float* lambda_dev, const int32_t* q_end_dev,
+                                           const int32_t* k_end_dev, int n_seqs, float scale, int causal, const float* lse_dev,
+                                           const void* dout_dev, int64_t lddout, const int64_t* part_end_host, int k_parts,
+                                           void* dq_dev, int64_t lddq, void* dk_dev, int64_t lddk, void* dv_dev, int64_t lddv,
+                                           float* G_lambda_dev, int64_t ldg, void* workspace_dev, void* hip_stream)
+{
+    const char* const name = "agc_diff_attn_partial_gradients";
+    agc::AttnCall c{};
+    c.q = q_dev, c.k = k_dev, c.v = v_dev, c.ldq = ldq, c.ldk = ldk, c.ldv = ldv, c.tokens_q = tokens_q, c.tokens_k = tokens_k;
+    c.heads = heads, c.kv_heads = kv_heads, c.d = head_dim, c.e = value_dim, c.lambda = lambda_dev;
+    c.q_end = q_end_dev, c.k_end = k_end_dev, c.n_seqs = n_seqs, c.causal = causal != 0, c.scale = scale;
+    c.lse = const_cast<float*>(lse_dev), c.workspace = static_cast<char*>(workspace_dev);
+    c.dout = dout_dev, c.lddout = lddout;
+    agc_status st = attn_arguments(name, c, true);
+    if (st != AGC_OK) return st;
+    st = partitions(name, part_end_host, k_parts, tokens_q);
+    if (st != AGC_OK) return st;
+    if (((!dout_dev || !lse_dev || !dq_dev) && tokens_q > 0) || ((!dk_dev || !dv_dev) && tokens_k > 0) || !G_lambda_dev)
+        return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
+    if (lddout < (int64_t)heads * value_dim || lddq < (int64_t)2 * heads * head_dim || lddk < (int64_t)2 * kv_heads * head_dim ||
+        lddv < (int64_t)kv_heads * value_dim || ldg < heads)
+        return refuse(AGC_ESHAPE, std::string(name) + ": a row stride is smaller than the row");
+    if (misaligned(dq_dev, 2) || misaligned(dk_dev, 2) || misaligned(dv_dev, 2) || misaligned(G_lambda_dev, 4))
+        return refuse(AGC_EALIGN, std::string(name) + ": a pointer is not aligned to its elements");
+    c.part_end = part_end_host, c.k_parts = k_parts, c.dq = dq_dev, c.dk = dk_dev, c.dv = dv_dev;
+    c.lddq = lddq, c.lddk = lddk, c.lddv = lddv, c.G = G_lambda_dev, c.ldg = ldg;
+    return launched(agc::launch_attn_gradients(c, reinterpret_cast<hipStream_t>(hip_stream)), name);
 }
 
 }  // extern "C"

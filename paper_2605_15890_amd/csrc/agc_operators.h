@@ -1,5 +1,5 @@
 // Launch interface between the C ABI (agc_operators.cpp) and the kernels of the operators round the coded step:
-// orthogonalised update, gated block, embedding, rotary positions, dropout.  Every pointer is a device pointer unless it says host.
+// orthogonalised update, gated block, embedding, rotary positions, dropout, differential attention.  Every pointer is a device pointer unless it says host.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -105,5 +105,37 @@ struct DropoutCall {
     float scale;               // 1 / (1 - p)
 };
 hipError_t launch_dropout(const DropoutCall& c, hipStream_t stream);
+
+// ------------------------------------------------------------------ differential attention
+struct AttnCall {
+    const void *q, *k, *v;     // bfloat16
+    int64_t ldq, ldk, ldv;
+    int64_t tokens_q, tokens_k;
+    int heads, kv_heads, d, e;
+    const float* lambda;
+    const int32_t *q_end, *k_begin, *k_end;   // k_begin may be null: a sequence's keys begin where the last one's end
+    int n_seqs, causal;
+    float scale;
+    // forward
+    void* out;
+    int64_t ldo;
+    float* lse;                // may be null; an input of the gradients
+    // gradients
+    const void* dout;
+    int64_t lddout;
+    const int64_t* part_end;   // host
+    int k_parts;
+    void *dq, *dk, *dv;
+    int64_t lddq, lddk, lddv;
+    float* G;
+    int64_t ldg;
+    char* workspace;
+};
+// D of the kernels that take heads of d and e values.  Operands of exactly D and 2 D are read where they lie, others are
+// copied to the workspace.
+int attn_width(int d, int e);
+int64_t attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int d, int e, int gradients);
+hipError_t launch_attn_forward(const AttnCall& c, hipStream_t stream);
+hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream);
 
 }  // namespace agc
