@@ -394,7 +394,7 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
  *   lse_dev    device, (2 * heads) x tokens_q floats, or NULL: receives log2 of the sum over keys of 2^(scale q_m k_m log2 e) of
  *              map m of head h in row 2 h + m, -infinity without keys; what the gradients take
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 0) bytes, 256-byte aligned
- * Scores, maxima, sums and out are held in binary32; the maps enter their product with v as bfloat16, out is rounded once.
+ * scale is finite, 0 or more.  Scores, maxima, sums and out are held in binary32; the maps enter their product with v as bfloat16, out is rounded once.
  * The order of the sums is fixed.  NaN or infinity in a sequence reaches that sequence's results alone.
  * 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads below 2^31, 1 <= n_seqs <= 2^20, heads a multiple of
  * kv_heads, 1 <= head_dim <= 128, 1 <= value_dim <= 256. */

@@ -94,6 +94,9 @@ __device__ __forceinline__ int attn_seen(const Attn& a, const AttnSeq& q, int t)
     return a.causal ? min(max(t + q.lk - q.lq + 1, 0), q.lk) : q.lk;
 }
 
+// 0 .. 31 with bits 2 and 3 swapped.
+__device__ __forceinline__ int attn_swapped(int i) { return (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1; }
+
 template <int D>
 struct AttnTile {
     static constexpr int kRow = 4 * D, kChunks = kRow / 16;
@@ -118,26 +121,49 @@ struct AttnTile {
         }
     }
 
-    // Chunk c of a row: eight values as they lie.
-    static __device__ __forceinline__ tile_bf16x8 straight(const char* lds, int row, int c)
-    {
-        return *reinterpret_cast<const tile_bf16x8*>(lds + row * kRow + ((c ^ mix(row)) << 4));
-    }
+};
 
-    // Column (lane & 31) of the 32 columns that start at chunk c, rows row0 + 8 (lane / 32) + 0 .. 7.
-    static __device__ __forceinline__ tile_bf16x8 turned(const char* lds, int row0, int c, int lane)
+// A lane's places in a tile for both kinds of reads, formed once; what they differ by is a constant beyond that.
+typedef __attribute__((address_space(3))) char* AttnLds;
+
+template <int D>
+struct AttnReads {
+    using Tile = AttnTile<D>;
+    static constexpr int kWide = Tile::kChunks < 16 ? Tile::kChunks : 16;   // chunks that are permuted among each other
+    int as_it_lies[kWide / 2], across[kWide / 4][2];
+
+    __device__ __forceinline__ explicit AttnReads(int lane, int map0 = 0)
     {
-        typedef __attribute__((address_space(3))) attn_s16x4* Lds;
-        const int i = lane & 15, row = row0 + 8 * (lane >> 5) + (i >> 2), chunk = c + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
-        const char* p0 = lds + row * kRow + ((chunk ^ mix(row)) << 4) + (i & 1) * 8;
-        const char* p1 = lds + (row + 4) * kRow + ((chunk ^ mix(row + 4)) << 4) + (i & 1) * 8;
-        const attn_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p0), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p1);
+        const int row = attn_swapped(lane & 31);
+#pragma unroll
+        for (int j = 0; j < kWide / 2; ++j) as_it_lies[j] = row * Tile::kRow + (((2 * j + (lane >> 5)) ^ Tile::mix(row)) << 4) + map0 * 2 * D;
+        const int i = lane & 15, x = ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+#pragma unroll
+        for (int b = 0; b < kWide / 4; ++b)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int r = 8 * (lane >> 5) + (i >> 2) + 4 * n;
+                across[b][n] = r * Tile::kRow + (((4 * b + x) ^ Tile::mix(r)) << 4) + (i & 1) * 8;
+            }
+    }
+    // Values 16 j + 8 (lane / 32) + 0 .. 7 of a row of the 32 rows at `tile`, the row being lane & 31 with bits 2 and 3 swapped:
+    // the registers of a product of it are then eight neighbouring rows twice.  (From the second map's values on with map0 = 1.)
+    __device__ __forceinline__ tile_bf16x8 straight(AttnLds tile, int j) const
+    {
+        typedef __attribute__((address_space(3))) const tile_bf16x8* At;
+        return *reinterpret_cast<At>(tile + as_it_lies[j % (kWide / 2)] + j / (kWide / 2) * (kWide * 16));
+    }
+    // Value 32 b + (lane & 31) of the rows 8 (lane / 32) + 0 .. 7 at `tile`.
+    __device__ __forceinline__ tile_bf16x8 turned(AttnLds tile, int b) const
+    {
+        typedef __attribute__((address_space(3))) attn_s16x4* At;
+        constexpr int kMod = kWide / 4;
+        const int more = b / kMod * (kWide * 16);
+        const attn_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<At>(tile + across[b % kMod][0] + more));
+        const attn_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<At>(tile + across[b % kMod][1] + more));
         return __builtin_bit_cast(tile_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
-
-// Place of a lane's operand row whose scores the lane's registers then hold in order: bits 2 and 3 swapped.
-__device__ __forceinline__ int attn_swapped(int i) { return (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1; }
 
 // Row that register r of a 32 x 32 product belongs to, with the operand's rows swapped (score products) and as they are.
 __device__ __forceinline__ int attn_row_swapped(int r, int lane) { return 16 * (r >> 3) + 8 * (lane >> 5) + (r & 7); }

@@ -15,8 +15,15 @@ struct AttnForward {
     float* lse;            // may be null
     int slots, splits;
     float* part;           // of splits: per (split, row) both maps' sums of 2 D values
-    tile_f32x4* stat;      // and their maxima and sums
+    struct AttnStat* stat; // and their maxima and sums
 };
+
+struct AttnStat {
+    float top, sum;
+};
+
+// Wide heads are worked on by a wave for each map: both maps' sums of 256 values would take all its registers.
+constexpr int attn_maps_of_a_wave(int D) { return D == 128 ? 1 : 2; }
 
 // Once a row's largest score has grown by more than this many powers of two, what is summed so far is scaled down to it.
 constexpr float kGrowth = 8.0f;
@@ -26,36 +33,39 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = E / 32;
+    constexpr int kMaps = attn_maps_of_a_wave(D), kRows = 32 * WAVES * kMaps / 2;
     __shared__ __attribute__((aligned(1024))) char lds[2][2][KT * Tile::kRow];   // buffer; keys, values
     const Attn& a = f.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int map0 = kMaps == 2 ? 0 : wave & 1, rows_of = kMaps == 2 ? wave : wave >> 1;
     const int total = f.slots * a.kv_heads * f.splits;
     const int id = xcd_order(blockIdx.x, total);
     const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
     const uint32_t group = a.group.d;
 
-    const int s = attn_find(a.q_end, a.n_seqs, a.tokens_q, group, 32 * WAVES, slot);
+    const int s = attn_find(a.q_end, a.n_seqs, a.tokens_q, group, kRows, slot);
     const AttnSeq seq = attn_sequence(a, s);
-    const int first = attn_first_slot(a.q_end, s, a.tokens_q, group, 32 * WAVES);
-    const int rows = seq.lq * (int)group, tiles = (rows + 32 * WAVES - 1) / (32 * WAVES);
+    const int first = attn_first_slot(a.q_end, s, a.tokens_q, group, kRows);
+    const int rows = seq.lq * (int)group, tiles = (rows + kRows - 1) / kRows;
     // the last tiles see most keys and come first
-    const int tile = tiles - 1 - (slot - first);
-    if (tile < 0 || tile >= tiles) return;
+    const int tile_id = tiles - 1 - (slot - first);
+    if (tile_id < 0 || tile_id >= tiles) return;
 
-    const int row_ = tile * 32 * WAVES + wave * 32 + (lane & 31);
+    const int row_ = tile_id * kRows + rows_of * 32 + (lane & 31);
     const int row = min(row_, rows - 1), t = (int)a.group(row), g = row - t * (int)group, head = head_k * (int)group + g;
     const int seen = attn_seen(a, seq, t);
-    const int seen_least = __builtin_amdgcn_readfirstlane(seen), seen_most = __builtin_amdgcn_readlane(seen, 31);
-    const int last_row = min(tile * 32 * WAVES + 32 * WAVES, rows) - 1;
+    const int last_row = min(tile_id * kRows + kRows, rows) - 1;
     const int keys = attn_seen(a, seq, (int)a.group(last_row));   // of the tile
     const int run = (keys + f.splits * KT - 1) / (f.splits * KT) * KT;
     const int begin = min(split * run, keys), end = min(begin + run, keys);
+    // of the wave's rows: what the first and the last one see
+    const int seen_least = min(__builtin_amdgcn_readfirstlane(seen), end), seen_most = min(__builtin_amdgcn_readlane(seen, 31), end);
 
-    tile_bf16x8 q[2][kSteps];
+    tile_bf16x8 q[kMaps][kSteps];
     {
-        const uint16_t* p = a.q + (int64_t)(seq.q0 + t) * a.ldq + (int64_t)head * E + (lane >> 5) * 8;
+        const uint16_t* p = a.q + (int64_t)(seq.q0 + t) * a.ldq + (int64_t)head * E + map0 * D + (lane >> 5) * 8;
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < kMaps; ++m)
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) q[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + m * D + i * 16);
     }
@@ -66,108 +76,144 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
         Tile::template load<KT, WAVES>(lds[buffer][1], wave, lane, [&](int r) { return values_at + (int64_t)min(j0 + r, seq.lk - 1) * a.ldv * 2; });
     };
 
-    attn_f32x16 acc[2][kBlocks];
+    attn_f32x16 acc[kMaps][kBlocks];
+    // the largest scores that the sums are relative to, zero where there is none yet
+    float top[kMaps], from[kMaps], sum[kMaps];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < kMaps; ++m) {
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_f32x16{};
-    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
+        top[m] = -INFINITY, from[m] = sum[m] = 0.0f;
+    }
+    const AttnReads<D> reads(lane, map0);
 
     if (begin < end) fetch(begin, 0);
     int buffer = 0;
+#pragma unroll 1
     for (int j0 = begin; j0 < end; j0 += KT, buffer ^= 1) {
         attn_wait_loads();
         __syncthreads();
         if (j0 + KT < end) fetch(j0 + KT, buffer ^ 1);
-        const char *const k_lds = lds[buffer][0], *const v_lds = lds[buffer][1];
+        AttnLds k_tile = (AttnLds)lds[buffer][0], v_tile = (AttnLds)lds[buffer][1];
+#pragma unroll 1
+        for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow, v_tile += 32 * Tile::kRow) {
+            attn_f32x16 score[kMaps] = {};
 #pragma unroll
-        for (int sub = 0; sub < KT / 32; ++sub) {
-            const int j = j0 + sub * 32;
-            if (j >= min(seen_most, end)) break;
-            const bool masked = j + 32 > min(seen_least, end);
-            tile_bf16x8 p[2][2];
+            for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                attn_f32x16 score{};
+                for (int m = 0; m < kMaps; ++m) score[m] = attn_mfma(reads.straight(k_tile, m * kSteps + i), q[m][i], score[m]);
+            if (j + 32 > seen_least) {
+                const int left = min(seen, end) - j;
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i)
-                    score = attn_mfma(Tile::straight(k_lds, sub * 32 + attn_swapped(lane & 31), m * (D / 8) + i * 2 + (lane >> 5)), q[m][i], score);
-                float v[16];
+                for (int r = 0; r < 16; ++r) {
+                    const bool in = attn_row_swapped(r, lane) < left;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) v[r] = score[r] * a.to_log2;
-                if (masked) {
-                    const int left = min(seen, end) - j;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) v[r] = attn_row_swapped(r, lane) < left ? v[r] : -INFINITY;
+                    for (int m = 0; m < kMaps; ++m) score[m][r] = in ? score[m][r] : -INFINITY;
                 }
-                float most = v[0];
+            }
+            bool grown = false;
+            float most[kMaps];
 #pragma unroll
-                for (int r = 1; r < 16; ++r) most = fmaxf(most, v[r]);
-                most = fmaxf(most, attn_other_half(most));
-                if (__any(most > top[m] + kGrowth)) {
-                    const float now = fmaxf(top[m], most);
+            for (int m = 0; m < kMaps; ++m) {
+                most[m] = score[m][0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) most[m] = fmaxf(most[m], score[m][r]);
+                most[m] *= a.to_log2;
+                grown |= most[m] > top[m] + kGrowth;
+            }
+            if (__any(grown)) {
+#pragma unroll
+                for (int m = 0; m < kMaps; ++m) {
+                    const float now = fmaxf(top[m], fmaxf(most[m], attn_other_half(most[m])));
                     const float shrink = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[m] - now);
                     top[m] = now;
+                    from[m] = now == -INFINITY ? 0.0f : now;
                     sum[m] *= shrink;
 #pragma unroll
                     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[m][b][r] *= shrink;
                 }
-                const float from = top[m] == -INFINITY ? 0.0f : top[m];
+            }
+            tile_bf16x8 p[kMaps][2];
+#pragma unroll
+            for (int m = 0; m < kMaps; ++m) {
+                float v[16];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    v[r] = __builtin_amdgcn_exp2f(v[r] - from);
+                    v[r] = __builtin_amdgcn_exp2f(fmaf(score[m][r], a.to_log2, -from[m]));
                     sum[m] += v[r];
                 }
                 p[m][0] = attn_operand(v, 0);
                 p[m][1] = attn_operand(v, 1);
             }
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const tile_bf16x8 v = Tile::turned(v_lds, sub * 32 + i * 16, b * 4, lane);
-                    acc[0][b] = attn_mfma(v, p[0][i], acc[0][b]);
-                    acc[1][b] = attn_mfma(v, p[1][i], acc[1][b]);
+                for (int b = 0; b < kBlocks; ++b) {
+                    const tile_bf16x8 v = reads.turned(v_tile + i * 16 * Tile::kRow, b);
+#pragma unroll
+                    for (int m = 0; m < kMaps; ++m) acc[m][b] = attn_mfma(v, p[m][i], acc[m][b]);
                 }
         }
     }
 
-    if (row_ >= rows) return;   // both halves of a row alike: the exchange below stays among lanes that go on
 #pragma unroll
-    for (int m = 0; m < 2; ++m) sum[m] += attn_other_half(sum[m]);
+    for (int m = 0; m < kMaps; ++m) sum[m] += attn_other_half(sum[m]);
     if (f.splits > 1) {
+        if (row_ >= rows) return;
         const int64_t at = (int64_t)split * a.tokens_q * a.heads + (int64_t)head_k * a.tokens_q * group + (int64_t)seq.q0 * group + row;
-        if (lane < 32) f.stat[at] = tile_f32x4{top[0], sum[0], top[1], sum[1]};
-        if (begin < end) {
-            float* o = f.part + at * 2 * E;
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < kMaps; ++m) {
+            if (lane < 32) f.stat[2 * at + map0 + m] = AttnStat{top[m], sum[m]};
+            if (begin >= end) continue;
+            float* o = f.part + (2 * at + map0 + m) * E;
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
+            for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-                    for (int r = 0; r < 16; r += 4)
-                        *reinterpret_cast<tile_f32x4*>(o + m * E + b * 32 + attn_row_plain(r, lane)) =
-                            tile_f32x4{acc[m][b][r], acc[m][b][r + 1], acc[m][b][r + 2], acc[m][b][r + 3]};
+                for (int r = 0; r < 16; r += 4)
+                    *reinterpret_cast<tile_f32x4*>(o + b * 32 + attn_row_plain(r, lane)) =
+                        tile_f32x4{acc[m][b][r], acc[m][b][r + 1], acc[m][b][r + 2], acc[m][b][r + 3]};
         }
         return;
     }
     // a row without keys in sight is zeros
-    const float by1 = sum[0] == 0.0f ? 0.0f : 1.0f / sum[0], by2 = sum[1] == 0.0f ? 0.0f : a.lambda[head] / sum[1];
+    float by[kMaps];
+#pragma unroll
+    for (int m = 0; m < kMaps; ++m) {
+        by[m] = sum[m] == 0.0f ? 0.0f : 1.0f / sum[m];
+        if (f.lse && lane < 32 && row_ < rows)
+            f.lse[(int64_t)(2 * head + map0 + m) * a.tokens_q + seq.q0 + t] = sum[m] == 0.0f ? -INFINITY : top[m] + __builtin_amdgcn_logf(sum[m]);
+    }
+    const float lambda = a.lambda[head];
+    if constexpr (kMaps == 2) {
+        by[1] *= lambda;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[0][b][r] = acc[0][b][r] * by[0] - acc[1][b][r] * by[1];
+    } else {
+        // the second map's wave hands its sums to the first map's, which has the same rows
+        static_assert(WAVES / 2 * 32 * E * 4 <= (int)sizeof(lds), "they fit where the tiles were");
+        float* box = reinterpret_cast<float*>(lds) + rows_of * (32 * E) + lane;
+        __syncthreads();
+        if (map0 == 1) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) box[(b * 16 + r) * 64] = acc[0][b][r] * (by[0] * lambda);
+        }
+        __syncthreads();
+        if (map0 == 1) return;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[0][b][r] = acc[0][b][r] * by[0] - box[(b * 16 + r) * 64];
+    }
+    if (row_ >= rows) return;
     uint16_t* o = f.out + (int64_t)(seq.q0 + t) * f.ldo + (int64_t)head * a.e;
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-        attn_f32x16 v;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) v[r] = acc[0][b][r] * by1 - acc[1][b][r] * by2;
-        attn_store(o, b * 32, a.e, lane, v, 1.0f);
-    }
-    if (f.lse && lane < 32) {
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-            f.lse[(int64_t)(2 * head + m) * a.tokens_q + seq.q0 + t] = sum[m] == 0.0f ? -INFINITY : top[m] + __builtin_amdgcn_logf(sum[m]);
-    }
+    for (int b = 0; b < kBlocks; ++b) attn_store(o, b * 32, a.e, lane, acc[0][b], 1.0f);
 }
 
 // Joins the splits of a row, a wave each: sums scaled to the largest maximum.
@@ -186,16 +232,16 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
     if (t >= last) return;   // behind the last sequence: left as it was
     float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f}, v[2][kPer] = {};
     for (int s = 0; s < f.splits; ++s) {
-        const tile_f32x4 x = f.stat[s * all + at];
         // an empty split has no largest score and no sums in memory
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            if (x[2 * m + 1] == 0.0f) continue;
-            const float now = fmaxf(top[m], x[2 * m]);
+            const AttnStat x = f.stat[2 * (s * all + at) + m];
+            if (x.sum == 0.0f) continue;
+            const float now = fmaxf(top[m], x.top);
             const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[m] - now);
-            const float add = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x[2 * m] - now);
+            const float add = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.top - now);
             top[m] = now;
-            sum[m] = sum[m] * keep + x[2 * m + 1] * add;
+            sum[m] = sum[m] * keep + x.sum * add;
             const float* o = f.part + (s * all + at) * 2 * E + m * E + lane;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) v[m][i] = v[m][i] * keep + o[i * 64] * add;
@@ -224,17 +270,18 @@ hipError_t launch(AttnForward f, hipStream_t stream)
 
 // Rows of a workgroup, and over how many workgroups the keys are split.
 struct Shape {
-    int waves, slots, splits;
+    int waves, slots, splits;   // one wave for each map where D is 128
 };
 
 Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D)
 {
     Shape o;
     const int64_t rows = tokens_q * (heads / kv_heads);
-    // up to 32 rows a sequence: one wave has them all
-    o.waves = rows <= (int64_t)32 * n_seqs ? 1 : D == 128 ? 4 : 8;
-    o.slots = (int)(rows / (32 * o.waves)) + n_seqs;
-    const int64_t blocks = (int64_t)o.slots * kv_heads, wanted = o.waves == 1 ? 1024 : 256;
+    // up to 32 rows a sequence: one wave (of each map) has them all
+    const int unit = 2 / attn_maps_of_a_wave(D);
+    o.waves = rows <= (int64_t)32 * n_seqs ? unit : 8;
+    o.slots = (int)(rows / (32 * o.waves / unit)) + n_seqs;
+    const int64_t blocks = (int64_t)o.slots * kv_heads, wanted = o.waves < 8 ? 1024 : 256;
     const int64_t keys = tokens_k / n_seqs;
     const int64_t most = std::max<int64_t>(1, keys / 128);
     o.splits = (int)std::max<int64_t>(1, std::min({wanted / std::max<int64_t>(1, blocks), most, (int64_t)64}));
@@ -334,11 +381,11 @@ hipError_t launch_attn_forward(const AttnCall& c, hipStream_t stream)
     const int D = attn_width(c.d, c.e);
     const Shape s = shape_of(c.tokens_q, c.tokens_k, c.n_seqs, c.heads, c.kv_heads, D);
     f.out = static_cast<uint16_t*>(c.out), f.ldo = c.ldo, f.lse = c.lse, f.slots = s.slots, f.splits = s.splits;
-    f.stat = reinterpret_cast<tile_f32x4*>(place);
+    f.stat = reinterpret_cast<AttnStat*>(place);
     f.part = reinterpret_cast<float*>(place + (int64_t)s.splits * c.tokens_q * c.heads * 16);
-    if (D == 32) return s.waves == 1 ? launch<32, 1, 64>(f, stream) : launch<32, 8, 64>(f, stream);
-    if (D == 64) return s.waves == 1 ? launch<64, 1, 32>(f, stream) : launch<64, 8, 64>(f, stream);
-    return s.waves == 1 ? launch<128, 1, 32>(f, stream) : launch<128, 4, 64>(f, stream);
+    if (D == 32) return s.waves < 8 ? launch<32, 1, 64>(f, stream) : launch<32, 8, 64>(f, stream);
+    if (D == 64) return s.waves < 8 ? launch<64, 1, 32>(f, stream) : launch<64, 8, 64>(f, stream);
+    return s.waves < 8 ? launch<128, 2, 32>(f, stream) : launch<128, 8, 64>(f, stream);
 }
 
 }  // namespace agc

@@ -35,7 +35,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
     __shared__ __attribute__((aligned(1024))) char lds[2][2][KT * Tile::kRow];   // buffer; keys, values
     const Attn& a = f.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads);
     const int head_k = id / f.slots, slot = id - head_k * f.slots;
     const uint32_t group = a.group.d;
@@ -68,7 +68,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
     float* const stat = f.sums + (int64_t)2 * head * a.tokens_q + seq.q0 + t;
     float lse[2], mean[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int m = 0; m < 2; ++m) lse[m] = f.lse[(int64_t)(2 * head + m) * a.tokens_q + seq.q0 + t];
+    for (int m = 0; m < 2; ++m) {
+        lse[m] = f.lse[(int64_t)(2 * head + m) * a.tokens_q + seq.q0 + t];
+        lse[m] = seen <= 1 ? 0.0f : lse[m];   // without keys it is -infinity; a single key's map is 2^0
+    }
 
     const char* const keys_at = reinterpret_cast<const char*>(a.k + (int64_t)seq.k0 * a.ldk + head_k * E);
     const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
@@ -77,16 +80,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
         Tile::template load<KT, WAVES>(lds[buffer][1], wave, lane, [&](int r) { return values_at + (int64_t)min(j0 + r, seq.lk - 1) * a.ldv * 2; });
     };
 
-    attn_f32x16 acc[2][kBlocks];
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_f32x16{};
-
-    // the first turn forms D, the second dq
-#pragma unroll 1
-    for (int turn = 0; turn < 2; ++turn) {
-        __syncthreads();   // nobody reads the last turn's tiles any more
+    const AttnReads<D> reads(lane);
+    // All keys in sight, 32 at a time: both maps and dP.
+    const auto over_keys = [&](const auto& use) {
         if (keys > 0) fetch(0, 0);
         int buffer = 0;
 #pragma unroll 1
@@ -94,52 +90,63 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
             attn_wait_loads();
             __syncthreads();
             if (j0 + KT < keys) fetch(j0 + KT, buffer ^ 1);
-            const char *const k_lds = lds[buffer][0], *const v_lds = lds[buffer][1];
+            AttnLds k_tile = (AttnLds)lds[buffer][0], v_tile = (AttnLds)lds[buffer][1];
 #pragma unroll 1
-            for (int sub = 0; sub < KT / 32; ++sub) {
-                const int j = j0 + sub * 32;
-                if (j >= seen_most) break;
-                const bool masked = j + 32 > seen_least;
-                const int at = sub * 32 + attn_swapped(lane & 31), left = seen - j;
-                attn_f32x16 dp{};
+            for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow, v_tile += 32 * Tile::kRow) {
+                attn_f32x16 dp{}, score[2] = {};
 #pragma unroll
-                for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(Tile::straight(v_lds, at, i * 2 + (lane >> 5)), go[i], dp);
+                for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(reads.straight(v_tile, i), go[i], dp);
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    attn_f32x16 score{};
+                for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                    for (int i = 0; i < kSteps; ++i)
-                        score = attn_mfma(Tile::straight(k_lds, at, m * (D / 8) + i * 2 + (lane >> 5)), q[m][i], score);
-                    float v[16];
+                    for (int m = 0; m < 2; ++m) score[m] = attn_mfma(reads.straight(k_tile, m * kSteps + i), q[m][i], score[m]);
+                if (j + 32 > seen_least) {
+                    const int left = seen - j;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const float p = __builtin_amdgcn_exp2f(score[r] * a.to_log2 - lse[m]);
-                        v[r] = p * (turn == 0 ? dp[r] : dp[r] - mean[m]);
-                    }
-                    if (masked) {
+                        const bool in = attn_row_swapped(r, lane) < left;
+                        dp[r] = in ? dp[r] : 0.0f;   // nothing but zero times a map's zero is zero
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) v[r] = attn_row_swapped(r, lane) < left ? v[r] : 0.0f;
-                    }
-                    if (turn == 0) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) mean[m] += v[r];
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const tile_bf16x8 ds = attn_operand(v, i);
-#pragma unroll
-                            for (int b = 0; b < kBlocks; ++b)
-                                acc[m][b] = attn_mfma(Tile::turned(k_lds, sub * 32 + i * 16, m * (D / 8) + b * 4, lane), ds, acc[m][b]);
-                        }
+                        for (int m = 0; m < 2; ++m) score[m][r] = in ? (seen == 1 ? 0.0f : score[m][r]) : -INFINITY;
                     }
                 }
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) score[m][r] = __builtin_amdgcn_exp2f(fmaf(score[m][r], a.to_log2, -lse[m]));
+                use(k_tile, score, dp);
             }
         }
-        if (turn == 0) {
+    };
+
+    over_keys([&](AttnLds, const attn_f32x16* map, const attn_f32x16& dp) {
 #pragma unroll
-            for (int m = 0; m < 2; ++m) mean[m] += attn_other_half(mean[m]);
-        }
-    }
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mean[m] = fmaf(map[m][r], dp[r], mean[m]);
+    });
+#pragma unroll
+    for (int m = 0; m < 2; ++m) mean[m] += attn_other_half(mean[m]);
+    __syncthreads();   // nobody reads tiles any more
+
+    attn_f32x16 acc[2][kBlocks];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_f32x16{};
+    over_keys([&](AttnLds k_tile, const attn_f32x16* map, const attn_f32x16& dp) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = map[m][i * 8 + e] * (dp[i * 8 + e] - mean[m]);
+                const tile_bf16x8 ds = __builtin_bit_cast(tile_bf16x8, bf16_pack8(v));
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_mfma(reads.turned(k_tile + i * 16 * Tile::kRow, m * kBlocks + b), ds, acc[m][b]);
+            }
+    });
     if (row_ >= rows) return;
     if (lane < 32) stat[0] = mean[0], stat[a.tokens_q] = mean[1];
     const float factor[2] = {a.scale, -a.scale * a.lambda[head]};
@@ -164,9 +171,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
     __shared__ __attribute__((aligned(1024))) char lds[2][2][RT * Tile::kRow];   // buffer; queries, dout
-    __shared__ float facts[2][6][RT];
+    __shared__ __attribute__((aligned(1024))) char values[32 * WAVES * Tile::kRow];
+    __shared__ __attribute__((aligned(16))) float facts[2][6][RT];
     const Attn& a = f.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads);
     const int head_k = id / f.slots, slot = id - head_k * f.slots;
     const uint32_t group = a.group.d;
@@ -176,22 +184,23 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
     const int tile = slot - attn_first_slot(a.k_end, s, a.tokens_k, 1, 32 * WAVES);
     if (tile * 32 * WAVES >= seq.lk) return;
 
-    const int key0 = tile * 32 * WAVES + wave * 32, key_ = key0 + (lane & 31), key = min(key_, seq.lk - 1);
+    const int key0 = tile * 32 * WAVES + wave * 32, key_ = key0 + attn_swapped(lane & 31), key = min(key_, seq.lk - 1);
     const int rows = seq.lq * (int)group;
     // under the causal mask the first query that sees this tile's first key
     const int begin = (a.causal ? min(max(tile * 32 * WAVES + seq.lq - seq.lk, 0), seq.lq) * (int)group : 0) / RT * RT;
 
-    tile_bf16x8 k[2][kSteps], v[2 * kSteps];
+    // the keys stay in registers, the values in LDS, as far as the waves' registers go
+    tile_bf16x8 k[2][kSteps];
     {
         const uint16_t* p = a.k + (int64_t)(seq.k0 + key) * a.ldk + head_k * E + (lane >> 5) * 8;
-        const uint16_t* o = a.v + (int64_t)(seq.k0 + key) * a.ldv + head_k * E + (lane >> 5) * 8;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) k[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + m * D + i * 16);
-#pragma unroll
-        for (int i = 0; i < 2 * kSteps; ++i) v[i] = *reinterpret_cast<const tile_bf16x8*>(o + i * 16);
+        const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
+        Tile::template load<32 * WAVES, WAVES>(values, wave, lane, [&](int r) { return values_at + (int64_t)min(tile * 32 * WAVES + r, seq.lk - 1) * a.ldv * 2; });
     }
+    AttnLds const v_tile = (AttnLds)values + wave * 32 * Tile::kRow;
     const char* const queries_at = reinterpret_cast<const char*>(a.q + (int64_t)seq.q0 * a.ldq + (int64_t)head_k * group * E);
     const char* const douts_at = reinterpret_cast<const char*>(f.dout + (int64_t)seq.q0 * f.lddout + (int64_t)head_k * group * E);
     const auto fetch = [&](int r0, int buffer) {
@@ -214,6 +223,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
         }
         o.lambda = a.lambda[head];
         o.seen = row_ < rows ? attn_seen(a, seq, t) : 0;
+        if (o.seen <= 1) o.lse[0] = o.lse[1] = 0.0f;   // without keys it is -infinity; a single key's map is 2^0
         return o;
     };
 
@@ -221,6 +231,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) acc_k[0][b] = acc_k[1][b] = acc_v[b] = acc_v[kBlocks + b] = attn_f32x16{};
 
+    const AttnReads<D> reads(lane);
     RowFacts mine{};
     if (begin < rows) {
         fetch(begin, 0);
@@ -243,47 +254,66 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
             fetch(r0 + RT, buffer ^ 1);
             if (threadIdx.x < RT) mine = read_facts(r0 + RT);
         }
-        const char *const q_lds = lds[buffer][0], *const o_lds = lds[buffer][1];
+        AttnLds q_tile = (AttnLds)lds[buffer][0], o_tile = (AttnLds)lds[buffer][1];
 #pragma unroll 1
-        for (int sub = 0; sub < RT / 32; ++sub) {
-            const int r_first = r0 + sub * 32, r_last = r_first + 31;
-            if (r_first >= rows) break;
+        for (int r_first = r0; r_first < min(r0 + RT, rows); r_first += 32, q_tile += 32 * Tile::kRow, o_tile += 32 * Tile::kRow) {
+            const int r_last = r_first + 31, sub = r_first - r0;
             // keys in sight grow with the row
             const int seen_first = attn_seen(a, seq, (int)a.group(r_first)), seen_last = attn_seen(a, seq, (int)a.group(min(r_last, rows - 1)));
             if (seen_last <= key0) continue;
-            const bool masked = seen_first < key0 + 32 || r_last >= rows;
-            const int at = sub * 32 + attn_swapped(lane & 31);
-            attn_f32x16 dp{}, s1{}, s2{};
+            const bool masked = seen_first < max(key0 + 32, 2) || r_last >= rows;
+            const float* const fact = &facts[buffer][0][sub + 8 * (lane >> 5)];
+            // eight rows' facts: rows 16 i + 8 (lane / 32) + 0 .. 7
+            const auto fact8 = [&](int which, int i, float o[8]) {
+                const tile_f32x4* p = reinterpret_cast<const tile_f32x4*>(fact + which * RT + i * 16);
+                const tile_f32x4 lo = p[0], hi = p[1];
 #pragma unroll
-            for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(Tile::straight(o_lds, at, i * 2 + (lane >> 5)), v[i], dp);
+                for (int e = 0; e < 4; ++e) o[e] = lo[e], o[4 + e] = hi[e];
+            };
+            attn_f32x16 dp{}, score[2] = {};
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                s1 = attn_mfma(Tile::straight(q_lds, at, i * 2 + (lane >> 5)), k[0][i], s1);
-                s2 = attn_mfma(Tile::straight(q_lds, at, D / 8 + i * 2 + (lane >> 5)), k[1][i], s2);
+            for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(reads.straight(o_tile, i), reads.straight(v_tile, i), dp);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) score[m] = attn_mfma(reads.straight(q_tile, m * kSteps + i), k[m][i], score[m]);
+            if (masked) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int seen = __float_as_int(fact[5 * RT + 16 * (r >> 3) + (r & 7)]);
+                    const bool in = key_ < seen;
+                    dp[r] = in ? dp[r] : 0.0f;
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) score[m][r] = in ? (seen == 1 ? 0.0f : score[m][r]) : -INFINITY;
+                }
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {   // sixteen rows at a time, eight of them this lane's
-                float mixed[8], ds1[8], ds2[8];
-                const int r8 = sub * 32 + i * 16 + 8 * (lane >> 5);
+            for (int i = 0; i < 2; ++i) {
+                float mixed[8], ds[8], lse[8], mean[8], lambda[8];
+                fact8(0, i, lse);
+                fact8(2, i, mean);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int r = r8 + e;
-                    float p1 = __builtin_amdgcn_exp2f(s1[i * 8 + e] * a.to_log2 - facts[buffer][0][r]);
-                    float p2 = facts[buffer][4][r] * __builtin_amdgcn_exp2f(s2[i * 8 + e] * a.to_log2 - facts[buffer][1][r]);
-                    mixed[e] = p1 - p2;
-                    ds1[e] = p1 * (dp[i * 8 + e] - facts[buffer][2][r]);
-                    ds2[e] = p2 * (facts[buffer][3][r] - dp[i * 8 + e]);
-                    if (masked && key_ >= __float_as_int(facts[buffer][5][r])) mixed[e] = ds1[e] = ds2[e] = 0.0f;
+                    mixed[e] = __builtin_amdgcn_exp2f(fmaf(score[0][i * 8 + e], a.to_log2, -lse[e]));
+                    ds[e] = mixed[e] * (dp[i * 8 + e] - mean[e]);
                 }
-                const tile_bf16x8 pm = __builtin_bit_cast(tile_bf16x8, bf16_pack8(mixed));
-                const tile_bf16x8 d1 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds1)), d2 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds2));
+                const tile_bf16x8 ds1 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds));
+                fact8(1, i, lse);
+                fact8(3, i, mean);
+                fact8(4, i, lambda);
 #pragma unroll
-                for (int b = 0; b < 2 * kBlocks; ++b)
-                    acc_v[b] = attn_mfma(Tile::turned(o_lds, sub * 32 + i * 16, b * 4, lane), pm, acc_v[b]);
+                for (int e = 0; e < 8; ++e) {
+                    const float p = lambda[e] * __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
+                    ds[e] = p * (mean[e] - dp[i * 8 + e]);
+                    mixed[e] -= p;
+                }
+                const tile_bf16x8 ds2 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds)), p = __builtin_bit_cast(tile_bf16x8, bf16_pack8(mixed));
+#pragma unroll
+                for (int b = 0; b < 2 * kBlocks; ++b) acc_v[b] = attn_mfma(reads.turned(o_tile + i * 16 * Tile::kRow, b), p, acc_v[b]);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    acc_k[0][b] = attn_mfma(Tile::turned(q_lds, sub * 32 + i * 16, b * 4, lane), d1, acc_k[0][b]);
-                    acc_k[1][b] = attn_mfma(Tile::turned(q_lds, sub * 32 + i * 16, D / 8 + b * 4, lane), d2, acc_k[1][b]);
+                    acc_k[0][b] = attn_mfma(reads.turned(q_tile + i * 16 * Tile::kRow, b), ds1, acc_k[0][b]);
+                    acc_k[1][b] = attn_mfma(reads.turned(q_tile + i * 16 * Tile::kRow, kBlocks + b), ds2, acc_k[1][b]);
                 }
             }
         }

@@ -71,7 +71,7 @@ agc_status attn_arguments(const char* name, const agc::AttnCall& c, bool gradien
         return refuse(AGC_ESHAPE, n + ": heads must be a multiple of kv_heads, head_dim 1..128, value_dim 1..256");
     if (c.tokens_q * c.heads > INT32_MAX || c.tokens_k * c.kv_heads > INT32_MAX || (int64_t)c.n_seqs * c.kv_heads > (1 << 24))
         return refuse(AGC_ESHAPE, n + ": tokens times heads must be below 2^31, n_seqs * kv_heads at most 2^24");
-    if (!std::isfinite(c.scale)) return refuse(AGC_EINVAL, n + ": scale must be finite");
+    if (!std::isfinite(c.scale) || c.scale < 0) return refuse(AGC_EINVAL, n + ": scale must be finite and not negative");
     if ((c.tokens_q > 0 && !c.q) || (c.tokens_k > 0 && (!c.k || !c.v)) || !c.lambda || !c.q_end || !c.k_end || !c.workspace)
         return refuse(AGC_EINVAL, n + ": null pointer");
     const int64_t row_q = (int64_t)2 * c.heads * c.d, row_k = (int64_t)2 * c.kv_heads * c.d;

@@ -398,7 +398,7 @@ def raw(grad=False, q=256, ldq=512, k=256, ldk=256, v=256, ldv=256, nq=3, nk=4, 
     (dict(nq=-1), -2), (dict(nq=2 ** 26 + 1), -2), (dict(nk=-1), -2), (dict(nk=2 ** 26 + 1), -2), (dict(n=0), -2), (dict(n=2 ** 20 + 1), -2),
     (dict(heads=3), -2), (dict(heads=0), -2), (dict(kv=0), -2), (dict(d=0), -2), (dict(d=129), -2), (dict(e=0), -2), (dict(e=257), -2),
     (dict(nq=2 ** 26, heads=32, ldq=4096), -2), (dict(nk=2 ** 26, heads=64, kv=32, ldk=4096, ldv=4096, ldq=8192), -2),
-    (dict(n=2 ** 20, heads=32, kv=32, ldq=4096, ldk=4096, ldv=4096), -2), (dict(scale=math.inf), -1), (dict(scale=math.nan), -1),
+    (dict(n=2 ** 20, heads=32, kv=32, ldq=4096, ldk=4096, ldv=4096), -2), (dict(scale=math.inf), -1), (dict(scale=math.nan), -1), (dict(scale=-0.5), -1),
     (dict(q=0), -1), (dict(k=0), -1), (dict(v=0), -1), (dict(lam=0), -1), (dict(qe=0), -1), (dict(ke=0), -1), (dict(ws=0), -1),
     (dict(ldq=504), -2), (dict(ldk=248), -2), (dict(ldv=248), -2), (dict(q=258), -4), (dict(k=264), -4), (dict(v=258), -4), (dict(ldq=516), -4),
     (dict(ldk=257), -4), (dict(ldv=260), -4), (dict(q=257, d=60), -4), (dict(lam=6), -4), (dict(qe=2), -4), (dict(ke=2), -4), (dict(lse=2), -4), (dict(ws=128), -4)])
