@@ -123,44 +123,44 @@ struct AttnTile {
 
 };
 
-// A lane's places in a tile for both kinds of reads, formed once; what they differ by is a constant beyond that.
-typedef __attribute__((address_space(3))) char* AttnLds;
+// A lane's places in a tile for both kinds of reads.  A chunk's permutation is an exclusive or, so one place gives all of them.
+typedef uint32_t AttnLds;   // an address in LDS
+
+__device__ __forceinline__ AttnLds attn_lds(const void* p)
+{
+    return (AttnLds)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
 
 template <int D>
 struct AttnReads {
     using Tile = AttnTile<D>;
     static constexpr int kWide = Tile::kChunks < 16 ? Tile::kChunks : 16;   // chunks that are permuted among each other
-    int as_it_lies[kWide / 2], across[kWide / 4][2];
+    uint32_t as_it_lies, across;
 
     __device__ __forceinline__ explicit AttnReads(int lane, int map0 = 0)
     {
         const int row = attn_swapped(lane & 31);
-#pragma unroll
-        for (int j = 0; j < kWide / 2; ++j) as_it_lies[j] = row * Tile::kRow + (((2 * j + (lane >> 5)) ^ Tile::mix(row)) << 4) + map0 * 2 * D;
-        const int i = lane & 15, x = ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
-#pragma unroll
-        for (int b = 0; b < kWide / 4; ++b)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const int r = 8 * (lane >> 5) + (i >> 2) + 4 * n;
-                across[b][n] = r * Tile::kRow + (((4 * b + x) ^ Tile::mix(r)) << 4) + (i & 1) * 8;
-            }
+        as_it_lies = row * Tile::kRow + (((lane >> 5) ^ Tile::mix(row)) << 4) + map0 * 2 * D;
+        const int i = lane & 15, x = ((lane >> 4) & 1) * 2 + ((i & 3) >> 1), r = 8 * (lane >> 5) + (i >> 2);
+        across = r * Tile::kRow + ((x ^ Tile::mix(r)) << 4) + (i & 1) * 8;
     }
     // Values 16 j + 8 (lane / 32) + 0 .. 7 of a row of the 32 rows at `tile`, the row being lane & 31 with bits 2 and 3 swapped:
     // the registers of a product of it are then eight neighbouring rows twice.  (From the second map's values on with map0 = 1.)
     __device__ __forceinline__ tile_bf16x8 straight(AttnLds tile, int j) const
     {
         typedef __attribute__((address_space(3))) const tile_bf16x8* At;
-        return *reinterpret_cast<At>(tile + as_it_lies[j % (kWide / 2)] + j / (kWide / 2) * (kWide * 16));
+        constexpr int kMod = kWide / 2;
+        return *(At)(uintptr_t)(((tile + as_it_lies) ^ (j % kMod * 32)) + j / kMod * (kWide * 16));
     }
-    // Value 32 b + (lane & 31) of the rows 8 (lane / 32) + 0 .. 7 at `tile`.
-    __device__ __forceinline__ tile_bf16x8 turned(AttnLds tile, int b) const
+    // Value 32 b + (lane & 31) of the rows row0 + 8 (lane / 32) + 0 .. 7 at `tile`, row0 a multiple of 16.
+    __device__ __forceinline__ tile_bf16x8 turned(AttnLds tile, int row0, int b) const
     {
         typedef __attribute__((address_space(3))) attn_s16x4* At;
         constexpr int kMod = kWide / 4;
-        const int more = b / kMod * (kWide * 16);
-        const attn_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<At>(tile + across[b % kMod][0] + more));
-        const attn_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<At>(tile + across[b % kMod][1] + more));
+        const uint32_t at = tile + across, more = row0 * Tile::kRow + b / kMod * (kWide * 16), flip = b % kMod * 64;
+        const attn_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(uintptr_t)((at ^ flip) + more));
+        // four rows on the permutation differs in its lowest bit
+        const attn_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(uintptr_t)((at ^ (flip | 16)) + more + 4 * Tile::kRow));
         return __builtin_bit_cast(tile_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
@@ -200,6 +200,11 @@ __device__ __forceinline__ void attn_store(uint16_t* row, int at, int width, int
                 if (c + i < width) row[c + i] = (uint16_t)bf16_bits(acc[r + i] * factor);
         }
     }
+}
+
+__device__ __forceinline__ void load4_to_lds(const float* src, float* dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
 }
 
 __device__ __forceinline__ void attn_wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)

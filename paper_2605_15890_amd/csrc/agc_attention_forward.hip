@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
         attn_wait_loads();
         __syncthreads();
         if (j0 + KT < end) fetch(j0 + KT, buffer ^ 1);
-        AttnLds k_tile = (AttnLds)lds[buffer][0], v_tile = (AttnLds)lds[buffer][1];
+        AttnLds k_tile = attn_lds(lds[buffer][0]), v_tile = attn_lds(lds[buffer][1]);
 #pragma unroll 1
         for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow, v_tile += 32 * Tile::kRow) {
             attn_f32x16 score[kMaps] = {};
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    const tile_bf16x8 v = reads.turned(v_tile + i * 16 * Tile::kRow, b);
+                    const tile_bf16x8 v = reads.turned(v_tile, i * 16, b);
 #pragma unroll
                     for (int m = 0; m < kMaps; ++m) acc[m][b] = attn_mfma(v, p[m][i], acc[m][b]);
                 }
@@ -366,7 +366,7 @@ int64_t attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int
     int64_t bytes = 256;
     if (d != D) bytes += round_up(tokens_q * heads * 4 * D, 256) + round_up(tokens_k * kv_heads * 4 * D, 256);
     if (e != 2 * D) bytes += round_up(tokens_k * kv_heads * 4 * D, 256) + (gradients ? round_up(tokens_q * heads * 4 * D, 256) : 0);
-    if (gradients) bytes += round_up(tokens_q * heads * 8, 256);
+    if (gradients) bytes += round_up(tokens_q * heads * 16, 256);
     return bytes + splits_bytes(shape_of(tokens_q, tokens_k, n_seqs, heads, kv_heads, D), tokens_q, heads, D);
 }
 

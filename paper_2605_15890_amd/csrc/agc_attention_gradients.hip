@@ -21,7 +21,8 @@ struct AttnGradients {
     const uint16_t* dout;
     int64_t lddout;
     const float* lse;
-    float* sums;           // D_m of every (head, map, token)
+    float* facts;          // lse_m and D_m of every (head, map, token), lse as the keys' pass takes it
+    int64_t of_facts;      // values of each
     uint16_t *dq, *dk, *dv;
     int64_t lddq, lddk, lddv;
     int slots;
@@ -65,7 +66,6 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
 #pragma unroll
         for (int i = 0; i < 2 * kSteps; ++i) go[i] = *reinterpret_cast<const tile_bf16x8*>(o + i * 16);
     }
-    float* const stat = f.sums + (int64_t)2 * head * a.tokens_q + seq.q0 + t;
     float lse[2], mean[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
             attn_wait_loads();
             __syncthreads();
             if (j0 + KT < keys) fetch(j0 + KT, buffer ^ 1);
-            AttnLds k_tile = (AttnLds)lds[buffer][0], v_tile = (AttnLds)lds[buffer][1];
+            AttnLds k_tile = attn_lds(lds[buffer][0]), v_tile = attn_lds(lds[buffer][1]);
 #pragma unroll 1
             for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow, v_tile += 32 * Tile::kRow) {
                 attn_f32x16 dp{}, score[2] = {};
@@ -144,11 +144,15 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
                 for (int e = 0; e < 8; ++e) v[e] = map[m][i * 8 + e] * (dp[i * 8 + e] - mean[m]);
                 const tile_bf16x8 ds = __builtin_bit_cast(tile_bf16x8, bf16_pack8(v));
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_mfma(reads.turned(k_tile + i * 16 * Tile::kRow, m * kBlocks + b), ds, acc[m][b]);
+                for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_mfma(reads.turned(k_tile, i * 16, m * kBlocks + b), ds, acc[m][b]);
             }
     });
     if (row_ >= rows) return;
-    if (lane < 32) stat[0] = mean[0], stat[a.tokens_q] = mean[1];
+    if (lane < 32) {
+        float* fact = f.facts + (int64_t)2 * head * a.tokens_q + seq.q0 + t;
+#pragma unroll
+        for (int m = 0; m < 2; ++m, fact += a.tokens_q) fact[0] = lse[m], fact[f.of_facts] = mean[m];
+    }
     const float factor[2] = {a.scale, -a.scale * a.lambda[head]};
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -159,20 +163,15 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
 }
 
 // ------------------------------------------------------------------ dk, dv: a workgroup's keys, all rows that see them
-// What a tile's rows bring along: lse and D of both maps, lambda, keys in sight.
-struct RowFacts {
-    float lse[2], mean[2], lambda;
-    int seen;
-};
-
-template <int D, int WAVES, int RT>
+// A tile's rows bring along lse and D of both maps and, where heads share keys, lambda.
+template <int D, int WAVES, int RT, bool SHARED>
 __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
     __shared__ __attribute__((aligned(1024))) char lds[2][2][RT * Tile::kRow];   // buffer; queries, dout
     __shared__ __attribute__((aligned(1024))) char values[32 * WAVES * Tile::kRow];
-    __shared__ __attribute__((aligned(16))) float facts[2][6][RT];
+    __shared__ __attribute__((aligned(256))) float facts[2][SHARED ? 5 : 4][RT];
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads);
@@ -200,7 +199,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
         const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
         Tile::template load<32 * WAVES, WAVES>(values, wave, lane, [&](int r) { return values_at + (int64_t)min(tile * 32 * WAVES + r, seq.lk - 1) * a.ldv * 2; });
     }
-    AttnLds const v_tile = (AttnLds)values + wave * 32 * Tile::kRow;
+    const AttnLds v_tile = attn_lds(values) + wave * 32 * Tile::kRow;
     const char* const queries_at = reinterpret_cast<const char*>(a.q + (int64_t)seq.q0 * a.ldq + (int64_t)head_k * group * E);
     const char* const douts_at = reinterpret_cast<const char*>(f.dout + (int64_t)seq.q0 * f.lddout + (int64_t)head_k * group * E);
     const auto fetch = [&](int r0, int buffer) {
@@ -210,51 +209,27 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
         };
         Tile::template load<RT, WAVES>(lds[buffer][0], wave, lane, [&](int r) { return place(queries_at, a.ldq, r); });
         Tile::template load<RT, WAVES>(lds[buffer][1], wave, lane, [&](int r) { return place(douts_at, f.lddout, r); });
-    };
-    // a row's facts, read a tile ahead by one thread a row and put into LDS when its buffer is free
-    const auto read_facts = [&](int r0) {
-        RowFacts o;
-        const int row_ = r0 + (int)threadIdx.x, row = min(row_, rows - 1), t = (int)a.group(row), head = head_k * (int)group + row - t * (int)group;
-        const int64_t at = (int64_t)2 * head * a.tokens_q + seq.q0 + t;
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            o.lse[m] = f.lse[at + m * (int64_t)a.tokens_q];
-            o.mean[m] = f.sums[at + m * (int64_t)a.tokens_q];
+        // a wave a fact, a lane a row
+        for (int n = wave; n < (SHARED ? 5 : 4); n += WAVES) {
+            const int row = min(r0 + lane, rows - 1), t = (int)a.group(row), head = head_k * (int)group + row - t * (int)group;
+            const float* at = n == 4 ? a.lambda + head : f.facts + (n >> 1) * f.of_facts + (int64_t)(2 * head + (n & 1)) * a.tokens_q + seq.q0 + t;
+            if (lane < RT) load4_to_lds(at, facts[buffer][n]);
         }
-        o.lambda = a.lambda[head];
-        o.seen = row_ < rows ? attn_seen(a, seq, t) : 0;
-        if (o.seen <= 1) o.lse[0] = o.lse[1] = 0.0f;   // without keys it is -infinity; a single key's map is 2^0
-        return o;
     };
-
     attn_f32x16 acc_k[2][kBlocks], acc_v[2 * kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) acc_k[0][b] = acc_k[1][b] = acc_v[b] = acc_v[kBlocks + b] = attn_f32x16{};
 
     const AttnReads<D> reads(lane);
-    RowFacts mine{};
-    if (begin < rows) {
-        fetch(begin, 0);
-        if (threadIdx.x < RT) mine = read_facts(begin);
-    }
+    const float lambda_of_all = a.lambda[head_k * group];   // where every key head has one query head
+    if (begin < rows) fetch(begin, 0);
     int buffer = 0;
 #pragma unroll 1
     for (int r0 = begin; r0 < rows; r0 += RT, buffer ^= 1) {
-        if (threadIdx.x < RT) {
-            facts[buffer][0][threadIdx.x] = mine.lse[0];
-            facts[buffer][1][threadIdx.x] = mine.lse[1];
-            facts[buffer][2][threadIdx.x] = mine.mean[0];
-            facts[buffer][3][threadIdx.x] = mine.mean[1];
-            facts[buffer][4][threadIdx.x] = mine.lambda;
-            facts[buffer][5][threadIdx.x] = __int_as_float(mine.seen);
-        }
         attn_wait_loads();
         __syncthreads();
-        if (r0 + RT < rows) {
-            fetch(r0 + RT, buffer ^ 1);
-            if (threadIdx.x < RT) mine = read_facts(r0 + RT);
-        }
-        AttnLds q_tile = (AttnLds)lds[buffer][0], o_tile = (AttnLds)lds[buffer][1];
+        if (r0 + RT < rows) fetch(r0 + RT, buffer ^ 1);
+        AttnLds q_tile = attn_lds(lds[buffer][0]), o_tile = attn_lds(lds[buffer][1]);
 #pragma unroll 1
         for (int r_first = r0; r_first < min(r0 + RT, rows); r_first += 32, q_tile += 32 * Tile::kRow, o_tile += 32 * Tile::kRow) {
             const int r_last = r_first + 31, sub = r_first - r0;
@@ -280,7 +255,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
             if (masked) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int seen = __float_as_int(fact[5 * RT + 16 * (r >> 3) + (r & 7)]);
+                    const int row = r_first + attn_row_swapped(r, lane), seen = row < rows ? attn_seen(a, seq, (int)a.group(row)) : 0;
                     const bool in = key_ < seen;
                     dp[r] = in ? dp[r] : 0.0f;
 #pragma unroll
@@ -300,20 +275,20 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
                 const tile_bf16x8 ds1 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds));
                 fact8(1, i, lse);
                 fact8(3, i, mean);
-                fact8(4, i, lambda);
+                if constexpr (SHARED) fact8(4, i, lambda);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float p = lambda[e] * __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
+                    const float p = (SHARED ? lambda[e] : lambda_of_all) * __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
                     ds[e] = p * (mean[e] - dp[i * 8 + e]);
                     mixed[e] -= p;
                 }
                 const tile_bf16x8 ds2 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds)), p = __builtin_bit_cast(tile_bf16x8, bf16_pack8(mixed));
 #pragma unroll
-                for (int b = 0; b < 2 * kBlocks; ++b) acc_v[b] = attn_mfma(reads.turned(o_tile + i * 16 * Tile::kRow, b), p, acc_v[b]);
+                for (int b = 0; b < 2 * kBlocks; ++b) acc_v[b] = attn_mfma(reads.turned(o_tile, i * 16, b), p, acc_v[b]);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    acc_k[0][b] = attn_mfma(reads.turned(q_tile + i * 16 * Tile::kRow, b), ds1, acc_k[0][b]);
-                    acc_k[1][b] = attn_mfma(reads.turned(q_tile + i * 16 * Tile::kRow, kBlocks + b), ds2, acc_k[1][b]);
+                    acc_k[0][b] = attn_mfma(reads.turned(q_tile, i * 16, b), ds1, acc_k[0][b]);
+                    acc_k[1][b] = attn_mfma(reads.turned(q_tile, i * 16, kBlocks + b), ds2, acc_k[1][b]);
                 }
             }
         }
@@ -359,7 +334,10 @@ hipError_t launch(AttnGradients f, hipStream_t stream)
     f.slots = (int)(rows / (32 * WAVES)) + f.a.n_seqs;
     k_attn_dq<D, WAVES, KT><<<f.slots * f.a.kv_heads, 64 * WAVES, 0, stream>>>(f);
     f.slots = f.a.tokens_k / (32 * WAVES) + f.a.n_seqs;
-    k_attn_dkv<D, WAVES, RT><<<f.slots * f.a.kv_heads, 64 * WAVES, 0, stream>>>(f);
+    if (f.a.group.d > 1)
+        k_attn_dkv<D, WAVES, RT, true><<<f.slots * f.a.kv_heads, 64 * WAVES, 0, stream>>>(f);
+    else
+        k_attn_dkv<D, WAVES, RT, false><<<f.slots * f.a.kv_heads, 64 * WAVES, 0, stream>>>(f);
     return hipGetLastError();
 }
 
@@ -371,7 +349,7 @@ hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream)
     char* place = c.workspace;
     hipError_t e = attn_lay_out(c, f.a, f.dout, f.lddout, place, stream);
     if (e != hipSuccess) return e;
-    f.lse = c.lse, f.sums = reinterpret_cast<float*>(place);
+    f.lse = c.lse, f.facts = reinterpret_cast<float*>(place), f.of_facts = (int64_t)2 * c.heads * c.tokens_q;
     f.dq = static_cast<uint16_t*>(c.dq), f.dk = static_cast<uint16_t*>(c.dk), f.dv = static_cast<uint16_t*>(c.dv);
     f.lddq = c.lddq, f.lddk = c.lddk, f.lddv = c.lddv;
     const int D = attn_width(c.d, c.e);
@@ -379,7 +357,7 @@ hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream)
     if (e != hipSuccess) return e;
     AttnParts parts;
     for (int p = 0; p < c.k_parts; ++p) parts.end[p] = (int)c.part_end[p];
-    k_attn_lambda<<<dim3(c.heads, c.k_parts), 256, 0, stream>>>(parts, f.sums, f.a.tokens_q, c.q_end, c.n_seqs, c.G, c.ldg);
+    k_attn_lambda<<<dim3(c.heads, c.k_parts), 256, 0, stream>>>(parts, f.facts + f.of_facts, f.a.tokens_q, c.q_end, c.n_seqs, c.G, c.ldg);
     return hipGetLastError();
 }
 

@@ -444,5 +444,5 @@ def test_workspace():
     need = api.agc_diff_attn_workspace_bytes
     assert need(1 << 16, 1 << 16, 8, 16, 4, 64, 128) == 256
     assert need(1 << 16, 1 << 16, 8, 16, 4, 63, 128) > (1 << 16) * 20 * 256
-    assert need(1 << 16, 1 << 16, 8, 16, 4, 64, 128, True) == 256 + (1 << 16) * 16 * 8
+    assert need(1 << 16, 1 << 16, 8, 16, 4, 64, 128, True) == 256 + (1 << 16) * 16 * 16
     assert need(1, 1, 0, 1, 1, 1, 1) == 0 and need(1, 1, 1, 3, 2, 1, 1) == 0 and need(1, 1, 1, 1, 1, 129, 1) == 0
