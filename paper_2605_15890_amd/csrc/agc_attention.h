@@ -174,6 +174,42 @@ __device__ __forceinline__ attn_f32x16 attn_mfma(const tile_bf16x8& a, const til
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+// N products whose operands come from LDS, AHEAD of them read while the AHEAD before are multiplied: left to itself the compiler
+// puts each read right before its product, which then waits for it.  `start` may be called long before `run`.
+template <int N, int AHEAD, typename Read>
+struct AttnStream {
+    static_assert(N % AHEAD == 0, "whole groups");
+    const Read& read;
+    tile_bf16x8 part[2][AHEAD];
+    __device__ __forceinline__ explicit AttnStream(const Read& r) : read(r) {}
+    __device__ __forceinline__ void start()
+    {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) part[0][i] = read(i);
+    }
+    template <typename Use>
+    __device__ __forceinline__ void run(const Use& use)
+    {
+#pragma unroll
+        for (int g = 0; g < N / AHEAD; ++g) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (g + 1 < N / AHEAD) {
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) part[(g + 1) & 1][i] = read((g + 1) * AHEAD + i);
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) use(g * AHEAD + i, part[g & 1][i]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+};
+
+template <int N, int AHEAD, typename Read>
+__device__ __forceinline__ AttnStream<N, AHEAD, Read> attn_stream(const Read& read)
+{
+    return AttnStream<N, AHEAD, Read>(read);
+}
+
 // The other half's value of the same column.
 __device__ __forceinline__ float attn_other_half(float v) { return __shfl_xor(v, 32); }
 

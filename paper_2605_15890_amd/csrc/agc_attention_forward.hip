@@ -98,10 +98,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
 #pragma unroll 1
         for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow, v_tile += 32 * Tile::kRow) {
             attn_f32x16 score[kMaps] = {};
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-                for (int m = 0; m < kMaps; ++m) score[m] = attn_mfma(reads.straight(k_tile, m * kSteps + i), q[m][i], score[m]);
+            const auto read_k = [&](int n) { return reads.straight(k_tile, n % kMaps * kSteps + n / kMaps); };
+            auto of_k = attn_stream<kMaps * kSteps, 4>(read_k);
+            of_k.start();
+            of_k.run([&](int n, const tile_bf16x8& k) { score[n % kMaps] = attn_mfma(k, q[n % kMaps][n / kMaps], score[n % kMaps]); });
             if (j + 32 > seen_least) {
                 const int left = min(seen, end) - j;
 #pragma unroll
@@ -135,6 +135,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
                         for (int r = 0; r < 16; ++r) acc[m][b][r] *= shrink;
                 }
             }
+            const auto read_v = [&](int n) { return reads.turned(v_tile, n / kBlocks * 16, n % kBlocks); };
+            auto of_v = attn_stream<2 * kBlocks, kBlocks % 4 ? 2 : 4>(read_v);
+            of_v.start();
             tile_bf16x8 p[kMaps][2];
 #pragma unroll
             for (int m = 0; m < kMaps; ++m) {
@@ -147,14 +150,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
                 p[m][0] = attn_operand(v, 0);
                 p[m][1] = attn_operand(v, 1);
             }
+            of_v.run([&](int n, const tile_bf16x8& v) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    const tile_bf16x8 v = reads.turned(v_tile, i * 16, b);
-#pragma unroll
-                    for (int m = 0; m < kMaps; ++m) acc[m][b] = attn_mfma(v, p[m][i], acc[m][b]);
-                }
+                for (int m = 0; m < kMaps; ++m) acc[m][n % kBlocks] = attn_mfma(v, p[m][n / kBlocks], acc[m][n % kBlocks]);
+            });
         }
     }
 

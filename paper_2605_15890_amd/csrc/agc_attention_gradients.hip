@@ -93,13 +93,19 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
             AttnLds k_tile = attn_lds(lds[buffer][0]), v_tile = attn_lds(lds[buffer][1]);
 #pragma unroll 1
             for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow, v_tile += 32 * Tile::kRow) {
+                // two products of dP, one of each map, in turn
                 attn_f32x16 dp{}, score[2] = {};
-#pragma unroll
-                for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(reads.straight(v_tile, i), go[i], dp);
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) score[m] = attn_mfma(reads.straight(k_tile, m * kSteps + i), q[m][i], score[m]);
+                const auto read = [&](int n) {
+                    return n % 4 < 2 ? reads.straight(v_tile, n / 4 * 2 + n % 4) : reads.straight(k_tile, n % 4 % 2 * kSteps + n / 4);
+                };
+                auto stream = attn_stream<4 * kSteps, 4>(read);
+                stream.start();
+                stream.run([&](int n, const tile_bf16x8& x) {
+                    if (n % 4 < 2)
+                        dp = attn_mfma(x, go[n / 4 * 2 + n % 4], dp);
+                    else
+                        score[n % 2] = attn_mfma(x, q[n % 2][n / 4], score[n % 2]);
+                });
                 if (j + 32 > seen_least) {
                     const int left = seen - j;
 #pragma unroll
@@ -135,6 +141,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_f32x16{};
     over_keys([&](AttnLds k_tile, const attn_f32x16* map, const attn_f32x16& dp) {
+        const auto read = [&](int n) { return reads.turned(k_tile, n / (2 * kBlocks) * 16, n % (2 * kBlocks)); };
+        auto stream = attn_stream<4 * kBlocks, 2>(read);
+        stream.start();
+        tile_bf16x8 ds[2][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -142,10 +152,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = map[m][i * 8 + e] * (dp[i * 8 + e] - mean[m]);
-                const tile_bf16x8 ds = __builtin_bit_cast(tile_bf16x8, bf16_pack8(v));
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_mfma(reads.turned(k_tile, i * 16, m * kBlocks + b), ds, acc[m][b]);
+                ds[i][m] = __builtin_bit_cast(tile_bf16x8, bf16_pack8(v));
             }
+        stream.run([&](int n, const tile_bf16x8& k) {
+            const int i = n / (2 * kBlocks), m = n / kBlocks % 2, b = n % kBlocks;
+            acc[m][b] = attn_mfma(k, ds[i][m], acc[m][b]);
+        });
     });
     if (row_ >= rows) return;
     if (lane < 32) {
