@@ -396,7 +396,7 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 0) bytes, 256-byte aligned
  * scale is finite, 0 or more.  Scores, maxima, sums and out are held in binary32; the maps enter their product with v as bfloat16, out is rounded once.
  * The order of the sums is fixed.  NaN or infinity in a sequence reaches that sequence's results alone.
- * 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads below 2^31, 1 <= n_seqs <= 2^20, heads a multiple of
+ * Row strides of q, k, v up to 2^24, 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads below 2^31, 1 <= n_seqs <= 2^20, heads a multiple of
  * kv_heads, 1 <= head_dim <= 128, 1 <= value_dim <= 256. */
 int64_t agc_diff_attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int head_dim,
                                       int value_dim, int gradients);
@@ -409,7 +409,7 @@ agc_status agc_diff_attn_forward(const void* q_dev, int64_t ldq, const void* k_d
  *   dP = dout v^T,  D_m = sum over keys of P_m dP,  dS_1 = P_1 (dP - D_1),  dS_2 = -lambda P_2 (dP - D_2),
  *   dq_m = scale dS_m k_m,  dk_m = scale dS_m^T q_m,  dv = (P_1 - lambda P_2)^T dout, summed over the heads that share them,
  * and for every data partition p (a run of queries)  G_lambda[p, h] = - sum over its queries of D_2, binary32.
- *   dout_dev   device, tokens_q x (heads * value_dim), row stride lddout, aligned as v
+ *   dout_dev   device, tokens_q x (heads * value_dim), row stride lddout up to 2^24, aligned as v
  *   part_end_host  host, k_parts ends of the partitions in queries, not descending, the last tokens_q
  *   dq_dev, dk_dev, dv_dev  device, as q, k and v, row strides lddq, lddk, lddv, any alignment; overwritten but for rows behind
  *              the last sequence, which are left as they were

@@ -97,6 +97,21 @@ __device__ __forceinline__ int attn_seen(const Attn& a, const AttnSeq& q, int t)
 // 0 .. 31 with bits 2 and 3 swapped.
 __device__ __forceinline__ int attn_swapped(int i) { return (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1; }
 
+typedef __attribute__((address_space(3))) char* AttnLds;
+
+// Tiles are filled while others are read.  The compiler cannot tell the two apart and would wait for the loads before the first
+// read: a step over a tile takes the memory that it reads and the memory that it fills as two __restrict__ arguments.
+
+__device__ __forceinline__ void attn_load16(const char* src, AttnLds dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+__device__ __forceinline__ void attn_load4(const float* src, AttnLds dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
+}
+
 template <int D>
 struct AttnTile {
     static constexpr int kRow = 4 * D, kChunks = kRow / 16;
@@ -107,29 +122,43 @@ struct AttnTile {
         return (row & 3) << 2 | ((row >> 2) & 3);
     }
 
-    // Rows first .. first + ROWS - 1 of a matrix in memory, `at(row)` its address, to LDS.
-    template <int ROWS, int WAVES, typename At>
-    static __device__ __forceinline__ void load(char* lds, int wave, int lane, const At& at)
+    // Rows 0 .. ROWS - 1 of a matrix in memory, `base` the first one's address, the same for all lanes, to LDS; those from `rows` on
+    // are the last one again.  Whole tiles cost an addition a load.
+    template <int ROWS, int WAVES>
+    static __device__ __forceinline__ void load(AttnLds lds, int wave, int lane, const char* base, uint32_t stride, int rows)
     {
         constexpr int kPer = 64 / kChunks;   // rows a wave fetches at once
         constexpr int kTimes = ROWS / kPer / WAVES;
         static_assert(ROWS % (kPer * WAVES) == 0, "every wave fetches alike");
+        if (rows >= ROWS) {
 #pragma unroll
-        for (int i = 0; i < kTimes; ++i) {
-            const int c = i * WAVES + wave, row = c * kPer + lane / kChunks;
-            load16_to_lds(at(row) + ((lane % kChunks) ^ mix(row)) * 16, lds + c * 1024);
+            for (int i = 0; i < kTimes; ++i) {
+                const int c = i * WAVES + wave, row = c * kPer + lane / kChunks;
+                attn_load16(base + (int64_t)(c * kPer) * stride + ((uint32_t)(lane / kChunks) * stride + ((lane % kChunks) ^ mix(row)) * 16), lds + c * 1024);
+            }
+        } else {
+#pragma unroll 1
+            for (int c = wave; c < ROWS / kPer; c += WAVES) {
+                const int row = c * kPer + lane / kChunks;
+                attn_load16(base + ((uint32_t)min(row, rows - 1) * stride + ((lane % kChunks) ^ mix(row)) * 16), lds + c * 1024);
+            }
         }
     }
 
+    // Rows whose address is `at(row)`.
+    template <int ROWS, int WAVES, typename At>
+    static __device__ __forceinline__ void gather(AttnLds lds, int wave, int lane, const At& at)
+    {
+        constexpr int kPer = 64 / kChunks;
+#pragma unroll
+        for (int i = 0; i < ROWS / kPer / WAVES; ++i) {
+            const int c = i * WAVES + wave, row = c * kPer + lane / kChunks;
+            attn_load16(at(row) + ((lane % kChunks) ^ mix(row)) * 16, lds + c * 1024);
+        }
+    }
 };
 
 // A lane's places in a tile for both kinds of reads.  A chunk's permutation is an exclusive or, so one place gives all of them.
-typedef uint32_t AttnLds;   // an address in LDS
-
-__device__ __forceinline__ AttnLds attn_lds(const void* p)
-{
-    return (AttnLds)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
-}
 
 template <int D>
 struct AttnReads {
@@ -144,23 +173,23 @@ struct AttnReads {
         const int i = lane & 15, x = ((lane >> 4) & 1) * 2 + ((i & 3) >> 1), r = 8 * (lane >> 5) + (i >> 2);
         across = r * Tile::kRow + ((x ^ Tile::mix(r)) << 4) + (i & 1) * 8;
     }
-    // Values 16 j + 8 (lane / 32) + 0 .. 7 of a row of the 32 rows at `tile`, the row being lane & 31 with bits 2 and 3 swapped:
+    // Values 16 j + 8 (lane / 32) + 0 .. 7 of a row of the 32 rows `tile` bytes behind `lds`, the row being lane & 31 with bits 2 and 3 swapped:
     // the registers of a product of it are then eight neighbouring rows twice.  (From the second map's values on with map0 = 1.)
-    __device__ __forceinline__ tile_bf16x8 straight(AttnLds tile, int j) const
+    __device__ __forceinline__ tile_bf16x8 straight(AttnLds lds, uint32_t tile, int j) const
     {
         typedef __attribute__((address_space(3))) const tile_bf16x8* At;
         constexpr int kMod = kWide / 2;
-        return *(At)(uintptr_t)(((tile + as_it_lies) ^ (j % kMod * 32)) + j / kMod * (kWide * 16));
+        return *(At)(lds + ((tile + as_it_lies) ^ (j % kMod * 32)) + j / kMod * (kWide * 16));
     }
-    // Value 32 b + (lane & 31) of the rows row0 + 8 (lane / 32) + 0 .. 7 at `tile`, row0 a multiple of 16.
-    __device__ __forceinline__ tile_bf16x8 turned(AttnLds tile, int row0, int b) const
+    // Value 32 b + (lane & 31) of the rows row0 + 8 (lane / 32) + 0 .. 7 there, row0 a multiple of 16.
+    __device__ __forceinline__ tile_bf16x8 turned(AttnLds lds, uint32_t tile, int row0, int b) const
     {
         typedef __attribute__((address_space(3))) attn_s16x4* At;
         constexpr int kMod = kWide / 4;
         const uint32_t at = tile + across, more = row0 * Tile::kRow + b / kMod * (kWide * 16), flip = b % kMod * 64;
-        const attn_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(uintptr_t)((at ^ flip) + more));
+        const attn_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(lds + (at ^ flip) + more));
         // four rows on the permutation differs in its lowest bit
-        const attn_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(uintptr_t)((at ^ (flip | 16)) + more + 4 * Tile::kRow));
+        const attn_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(lds + (at ^ (flip | 16)) + more + 4 * Tile::kRow));
         return __builtin_bit_cast(tile_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
@@ -238,9 +267,13 @@ __device__ __forceinline__ void attn_store(uint16_t* row, int at, int width, int
     }
 }
 
-__device__ __forceinline__ void load4_to_lds(const float* src, float* dst)
+// The same in binary32, to a part of a split.
+__device__ __forceinline__ void attn_store_part(float* row, int lane, const attn_f32x16& acc, float factor)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<tile_f32x4*>(row + attn_row_plain(r, lane)) =
+            tile_f32x4{acc[r] * factor, acc[r + 1] * factor, acc[r + 2] * factor, acc[r + 3] * factor};
 }
 
 __device__ __forceinline__ void attn_wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
@@ -253,6 +286,8 @@ struct AttnPack {
     int rows, parts, width, up;   // `parts` runs of `width` values a row become runs of `up`
 };
 
+// What the gradients take of the workspace beyond that.
+int64_t attn_gradients_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D);
 hipError_t attn_pack(const AttnPack* jobs, int n, hipStream_t stream);
 // Fills `a` from the call, copying operands of other widths to the workspace; `place` moves on behind them.
 hipError_t attn_lay_out(const AttnCall& c, Attn& a, const uint16_t*& dout, int64_t& lddout, char*& place, hipStream_t stream);

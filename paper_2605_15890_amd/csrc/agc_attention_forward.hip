@@ -34,7 +34,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = E / 32;
     constexpr int kMaps = attn_maps_of_a_wave(D), kRows = 32 * WAVES * kMaps / 2;
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][KT * Tile::kRow];   // buffer; keys, values
+    constexpr int kTile = KT * Tile::kRow;
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile];   // buffer; keys, values
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int map0 = kMaps == 2 ? 0 : wave & 1, rows_of = kMaps == 2 ? wave : wave >> 1;
@@ -71,9 +72,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
     }
     const char* const keys_at = reinterpret_cast<const char*>(a.k + (int64_t)seq.k0 * a.ldk + head_k * E);
     const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
-    const auto fetch = [&](int j0, int buffer) {
-        Tile::template load<KT, WAVES>(lds[buffer][0], wave, lane, [&](int r) { return keys_at + (int64_t)min(j0 + r, seq.lk - 1) * a.ldk * 2; });
-        Tile::template load<KT, WAVES>(lds[buffer][1], wave, lane, [&](int r) { return values_at + (int64_t)min(j0 + r, seq.lk - 1) * a.ldv * 2; });
+    const auto fetch = [&](AttnLds to, int j0) {
+        Tile::template load<KT, WAVES>(to, wave, lane, keys_at + (int64_t)j0 * a.ldk * 2, (uint32_t)a.ldk * 2, seq.lk - j0);
+        Tile::template load<KT, WAVES>(to + kTile, wave, lane, values_at + (int64_t)j0 * a.ldv * 2, (uint32_t)a.ldv * 2, seq.lk - j0);
     };
 
     attn_f32x16 acc[kMaps][kBlocks];
@@ -87,18 +88,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
     }
     const AttnReads<D> reads(lane, map0);
 
-    if (begin < end) fetch(begin, 0);
-    int buffer = 0;
+    const auto step = [&](AttnLds __restrict__ from_lds, AttnLds __restrict__ to_lds, int j0) {
+        if (j0 + KT < end) fetch(to_lds, j0 + KT);
+        uint32_t k_tile = 0;
 #pragma unroll 1
-    for (int j0 = begin; j0 < end; j0 += KT, buffer ^= 1) {
-        attn_wait_loads();
-        __syncthreads();
-        if (j0 + KT < end) fetch(j0 + KT, buffer ^ 1);
-        AttnLds k_tile = attn_lds(lds[buffer][0]), v_tile = attn_lds(lds[buffer][1]);
-#pragma unroll 1
-        for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow, v_tile += 32 * Tile::kRow) {
+        for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow) {
+            const uint32_t v_tile = k_tile + kTile;
             attn_f32x16 score[kMaps] = {};
-            const auto read_k = [&](int n) { return reads.straight(k_tile, n % kMaps * kSteps + n / kMaps); };
+            const auto read_k = [&](int n) { return reads.straight(from_lds, k_tile, n % kMaps * kSteps + n / kMaps); };
             auto of_k = attn_stream<kMaps * kSteps, 4>(read_k);
             of_k.start();
             of_k.run([&](int n, const tile_bf16x8& k) { score[n % kMaps] = attn_mfma(k, q[n % kMaps][n / kMaps], score[n % kMaps]); });
@@ -135,7 +132,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
                         for (int r = 0; r < 16; ++r) acc[m][b][r] *= shrink;
                 }
             }
-            const auto read_v = [&](int n) { return reads.turned(v_tile, n / kBlocks * 16, n % kBlocks); };
+            const auto read_v = [&](int n) { return reads.turned(from_lds, v_tile, n / kBlocks * 16, n % kBlocks); };
             auto of_v = attn_stream<2 * kBlocks, kBlocks % 4 ? 2 : 4>(read_v);
             of_v.start();
             tile_bf16x8 p[kMaps][2];
@@ -155,6 +152,15 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
                 for (int m = 0; m < kMaps; ++m) acc[m][n % kBlocks] = attn_mfma(v, p[m][n / kBlocks], acc[m][n % kBlocks]);
             });
         }
+    };
+    const AttnLds all = (AttnLds)&lds[0][0][0];
+    if (begin < end) fetch(all, begin);
+    int buffer = 0;
+#pragma unroll 1
+    for (int j0 = begin; j0 < end; j0 += KT, buffer ^= 1) {
+        attn_wait_loads();
+        __syncthreads();
+        step(all + buffer * (2 * kTile), all + (buffer ^ 1) * (2 * kTile), j0);
     }
 
 #pragma unroll
@@ -168,11 +174,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
             if (begin >= end) continue;
             float* o = f.part + (2 * at + map0 + m) * E;
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4)
-                    *reinterpret_cast<tile_f32x4*>(o + b * 32 + attn_row_plain(r, lane)) =
-                        tile_f32x4{acc[m][b][r], acc[m][b][r + 1], acc[m][b][r + 2], acc[m][b][r + 3]};
+            for (int b = 0; b < kBlocks; ++b) attn_store_part(o + b * 32, lane, acc[m][b], 1.0f);
         }
         return;
     }
@@ -229,31 +231,45 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
     const int64_t of_head = (int64_t)a.tokens_q * group;
     const int head_k = (int)(at / of_head), row = (int)(at - head_k * of_head), t = (int)a.group(row), head = head_k * group + row - t * group;
     if (t >= last) return;   // behind the last sequence: left as it was
-    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f}, v[2][kPer] = {};
-    for (int s = 0; s < f.splits; ++s) {
-        // an empty split has no largest score and no sums in memory
+    // a lane a split: what its sums are multiplied with; one without keys left nothing in memory
+    float weight[2], top[2], sum[2];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const AttnStat x = f.stat[2 * (s * all + at) + m];
-            if (x.sum == 0.0f) continue;
-            const float now = fmaxf(top[m], x.top);
-            const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[m] - now);
-            const float add = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x.top - now);
-            top[m] = now;
-            sum[m] = sum[m] * keep + x.sum * add;
-            const float* o = f.part + (s * all + at) * 2 * E + m * E + lane;
+    for (int m = 0; m < 2; ++m) {
+        const AttnStat x = lane < f.splits ? f.stat[2 * (lane * all + at) + m] : AttnStat{-INFINITY, 0.0f};
+        const bool none = x.sum == 0.0f;
+        top[m] = none ? -INFINITY : x.top;
+        for (int d = 32; d > 0; d >>= 1) top[m] = fmaxf(top[m], __shfl_xor(top[m], d));
+        weight[m] = none ? 0.0f : __builtin_amdgcn_exp2f(x.top - top[m]);
+        sum[m] = none ? 0.0f : x.sum * weight[m];
+        for (int d = 32; d > 0; d >>= 1) sum[m] += __shfl_xor(sum[m], d);
+    }
+    const float by[2] = {sum[0] == 0.0f ? 0.0f : 1.0f / sum[0], sum[1] == 0.0f ? 0.0f : -a.lambda[head] / sum[1]};
+    __shared__ float weights[4][2][64];
+    float (&mine)[2][64] = weights[threadIdx.x >> 6];
+    mine[0][lane] = weight[0] * by[0], mine[1][lane] = weight[1] * by[1];
+    wave_lds_fence();
+    float v[kPer] = {};
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) v[m][i] = v[m][i] * keep + o[i * 64] * add;
+    for (int m = 0; m < 2; ++m) {
+        const float* o = f.part + (2 * at + m) * E + lane;
+#pragma unroll 8
+        for (int s = 0; s < f.splits; ++s) {
+            const float w = mine[m][s];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const float x = o[s * (2 * all * E) + i * 64];
+                v[i] = w == 0.0f ? v[i] : fmaf(x, w, v[i]);
+            }
         }
     }
-    const float by1 = sum[0] == 0.0f ? 0.0f : 1.0f / sum[0], by2 = sum[1] == 0.0f ? 0.0f : a.lambda[head] / sum[1];
     uint16_t* o = f.out + t * f.ldo + (int64_t)head * a.e;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-        if (lane + i * 64 < a.e) o[lane + i * 64] = (uint16_t)bf16_bits(v[0][i] * by1 - v[1][i] * by2);
-    if (f.lse && lane < 2)
-        f.lse[(int64_t)(2 * head + lane) * a.tokens_q + t] =
-            sum[lane] == 0.0f ? -INFINITY : top[lane] + __builtin_amdgcn_logf(sum[lane]);
+        if (lane + i * 64 < a.e) o[lane + i * 64] = (uint16_t)bf16_bits(v[i]);
+    if (f.lse && lane < 2) {
+        const float s = lane ? sum[1] : sum[0], m = lane ? top[1] : top[0];
+        f.lse[(int64_t)(2 * head + lane) * a.tokens_q + t] = s == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(s);
+    }
 }
 
 template <int D, int WAVES, int KT>
@@ -365,8 +381,9 @@ int64_t attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int
     int64_t bytes = 256;
     if (d != D) bytes += round_up(tokens_q * heads * 4 * D, 256) + round_up(tokens_k * kv_heads * 4 * D, 256);
     if (e != 2 * D) bytes += round_up(tokens_k * kv_heads * 4 * D, 256) + (gradients ? round_up(tokens_q * heads * 4 * D, 256) : 0);
-    if (gradients) bytes += round_up(tokens_q * heads * 16, 256);
-    return bytes + splits_bytes(shape_of(tokens_q, tokens_k, n_seqs, heads, kv_heads, D), tokens_q, heads, D);
+    int64_t more = splits_bytes(shape_of(tokens_q, tokens_k, n_seqs, heads, kv_heads, D), tokens_q, heads, D);
+    if (gradients) more = std::max(more, attn_gradients_bytes(tokens_q, tokens_k, n_seqs, heads, kv_heads, D));
+    return bytes + more;
 }
 
 hipError_t launch_attn_forward(const AttnCall& c, hipStream_t stream)

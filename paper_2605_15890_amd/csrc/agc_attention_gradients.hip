@@ -10,6 +10,8 @@
 // (from dout and the rounded out they would miss it by 2^-8, and a query that sees one key would get a gradient where
 // there is none), and makes D_2, whose sums are rows of G, a binary32 sum of binary32 terms.
 // dS and P enter their products as bfloat16, 2^-8 of a term at most, as the products' other operands are; sums are binary32.
+#include <algorithm>
+
 #include "agc_attention.h"
 
 namespace agc {
@@ -25,20 +27,26 @@ struct AttnGradients {
     int64_t of_facts;      // values of each
     uint16_t *dq, *dk, *dv;
     int64_t lddq, lddk, lddv;
-    int slots;
+    int slots, splits;
+    // of splits: sums of D of every (split, head, map, token), and of dq or of dk and dv of every (split, row)
+    float *part_mean, *part, *part_v;
 };
 
+// A workgroup has all keys of its rows, or the keys are split and the sums over them joined: D first, which dq needs.
+enum AttnKeys { kAll, kSplitMeans, kSplitRest };
+
 // ------------------------------------------------------------------ D and dq: a workgroup's rows, all keys in sight, twice
-template <int D, int WAVES, int KT>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
+template <int D, int WAVES, int KT, AttnKeys KEYS>
+__global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGradients f)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][KT * Tile::kRow];   // buffer; keys, values
+    constexpr int kTile = KT * Tile::kRow;
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile];   // buffer; keys, values
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads);
-    const int head_k = id / f.slots, slot = id - head_k * f.slots;
+    const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads * f.splits);
+    const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
     const uint32_t group = a.group.d;
 
     const int s = attn_find(a.q_end, a.n_seqs, a.tokens_q, group, 32 * WAVES, slot);
@@ -51,9 +59,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
     const int row_ = tile * 32 * WAVES + wave * 32 + (lane & 31);
     const int row = min(row_, rows - 1), t = (int)a.group(row), g = row - t * (int)group, head = head_k * (int)group + g;
     const int seen = attn_seen(a, seq, t);
-    const int seen_least = __builtin_amdgcn_readfirstlane(seen), seen_most = __builtin_amdgcn_readlane(seen, 31);
     const int last_row = min(tile * 32 * WAVES + 32 * WAVES, rows) - 1;
-    const int keys = attn_seen(a, seq, (int)a.group(last_row));
+    const int keys = attn_seen(a, seq, (int)a.group(last_row));   // of the tile
+    const int run = (keys + f.splits * KT - 1) / (f.splits * KT) * KT;
+    const int begin = min(split * run, keys), end = min(begin + run, keys);
+    const int seen_least = min(__builtin_amdgcn_readfirstlane(seen), end), seen_most = min(__builtin_amdgcn_readlane(seen, 31), end);
 
     tile_bf16x8 q[2][kSteps], go[2 * kSteps];
     {
@@ -75,28 +85,24 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
 
     const char* const keys_at = reinterpret_cast<const char*>(a.k + (int64_t)seq.k0 * a.ldk + head_k * E);
     const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
-    const auto fetch = [&](int j0, int buffer) {
-        Tile::template load<KT, WAVES>(lds[buffer][0], wave, lane, [&](int r) { return keys_at + (int64_t)min(j0 + r, seq.lk - 1) * a.ldk * 2; });
-        Tile::template load<KT, WAVES>(lds[buffer][1], wave, lane, [&](int r) { return values_at + (int64_t)min(j0 + r, seq.lk - 1) * a.ldv * 2; });
+    const auto fetch = [&](AttnLds to, int j0) {
+        Tile::template load<KT, WAVES>(to, wave, lane, keys_at + (int64_t)j0 * a.ldk * 2, (uint32_t)a.ldk * 2, seq.lk - j0);
+        Tile::template load<KT, WAVES>(to + kTile, wave, lane, values_at + (int64_t)j0 * a.ldv * 2, (uint32_t)a.ldv * 2, seq.lk - j0);
     };
 
     const AttnReads<D> reads(lane);
     // All keys in sight, 32 at a time: both maps and dP.
     const auto over_keys = [&](const auto& use) {
-        if (keys > 0) fetch(0, 0);
-        int buffer = 0;
+        const auto step = [&](AttnLds from_lds, AttnLds to_lds, int j0) {
+            if (j0 + KT < end) fetch(to_lds, j0 + KT);
+            uint32_t k_tile = 0;
 #pragma unroll 1
-        for (int j0 = 0; j0 < keys; j0 += KT, buffer ^= 1) {
-            attn_wait_loads();
-            __syncthreads();
-            if (j0 + KT < keys) fetch(j0 + KT, buffer ^ 1);
-            AttnLds k_tile = attn_lds(lds[buffer][0]), v_tile = attn_lds(lds[buffer][1]);
-#pragma unroll 1
-            for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow, v_tile += 32 * Tile::kRow) {
+            for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow) {
+                const uint32_t v_tile = k_tile + kTile;
                 // two products of dP, one of each map, in turn
                 attn_f32x16 dp{}, score[2] = {};
                 const auto read = [&](int n) {
-                    return n % 4 < 2 ? reads.straight(v_tile, n / 4 * 2 + n % 4) : reads.straight(k_tile, n % 4 % 2 * kSteps + n / 4);
+                    return n % 4 < 2 ? reads.straight(from_lds, v_tile, n / 4 * 2 + n % 4) : reads.straight(from_lds, k_tile, n % 4 % 2 * kSteps + n / 4);
                 };
                 auto stream = attn_stream<4 * kSteps, 4>(read);
                 stream.start();
@@ -107,7 +113,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
                         score[n % 2] = attn_mfma(x, q[n % 2][n / 4], score[n % 2]);
                 });
                 if (j + 32 > seen_least) {
-                    const int left = seen - j;
+                    const int left = min(seen, end) - j;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const bool in = attn_row_swapped(r, lane) < left;
@@ -120,28 +126,52 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) score[m][r] = __builtin_amdgcn_exp2f(fmaf(score[m][r], a.to_log2, -lse[m]));
-                use(k_tile, score, dp);
+                use(from_lds, k_tile, score, dp);
             }
+        };
+        const AttnLds all = (AttnLds)&lds[0][0][0];
+        if (begin < end) fetch(all, begin);
+        int buffer = 0;
+#pragma unroll 1
+        for (int j0 = begin; j0 < end; j0 += KT, buffer ^= 1) {
+            attn_wait_loads();
+            __syncthreads();
+            step(all + buffer * (2 * kTile), all + (buffer ^ 1) * (2 * kTile), j0);
         }
     };
 
-    over_keys([&](AttnLds, const attn_f32x16* map, const attn_f32x16& dp) {
+    const int64_t fact = (int64_t)2 * head * a.tokens_q + seq.q0 + t;
+    if constexpr (KEYS != kSplitRest) {
+        over_keys([&](AttnLds, uint32_t, const attn_f32x16* map, const attn_f32x16& dp) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) mean[m] = fmaf(map[m][r], dp[r], mean[m]);
-    });
+                for (int r = 0; r < 16; ++r) mean[m] = fmaf(map[m][r], dp[r], mean[m]);
+        });
 #pragma unroll
-    for (int m = 0; m < 2; ++m) mean[m] += attn_other_half(mean[m]);
-    __syncthreads();   // nobody reads tiles any more
+        for (int m = 0; m < 2; ++m) mean[m] += attn_other_half(mean[m]);
+        if constexpr (KEYS == kSplitMeans) {
+            if (row_ < rows && lane < 32) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) f.part_mean[split * f.of_facts + fact + m * (int64_t)a.tokens_q] = mean[m];
+            }
+            return;
+        }
+        __syncthreads();   // nobody reads tiles any more
+    } else {
+        for (int n = 0; n < f.splits; ++n) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) mean[m] += f.part_mean[n * f.of_facts + fact + m * (int64_t)a.tokens_q];
+        }
+    }
 
     attn_f32x16 acc[2][kBlocks];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) acc[m][b] = attn_f32x16{};
-    over_keys([&](AttnLds k_tile, const attn_f32x16* map, const attn_f32x16& dp) {
-        const auto read = [&](int n) { return reads.turned(k_tile, n / (2 * kBlocks) * 16, n % (2 * kBlocks)); };
+    over_keys([&](AttnLds from_lds, uint32_t k_tile, const attn_f32x16* map, const attn_f32x16& dp) {
+        const auto read = [&](int n) { return reads.turned(from_lds, k_tile, n / (2 * kBlocks) * 16, n % (2 * kBlocks)); };
         auto stream = attn_stream<4 * kBlocks, 2>(read);
         stream.start();
         tile_bf16x8 ds[2][2];
@@ -160,34 +190,44 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(AttnGradients f)
         });
     });
     if (row_ >= rows) return;
-    if (lane < 32) {
-        float* fact = f.facts + (int64_t)2 * head * a.tokens_q + seq.q0 + t;
+    if (lane < 32 && split == 0) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m, fact += a.tokens_q) fact[0] = lse[m], fact[f.of_facts] = mean[m];
+        for (int m = 0; m < 2; ++m) {
+            f.facts[fact + m * (int64_t)a.tokens_q] = lse[m];
+            f.facts[f.of_facts + fact + m * (int64_t)a.tokens_q] = mean[m];
+        }
     }
     const float factor[2] = {a.scale, -a.scale * a.lambda[head]};
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-        uint16_t* o = f.dq + (int64_t)(seq.q0 + t) * f.lddq + (int64_t)(2 * head + m) * a.d;
+        if constexpr (KEYS == kAll) {
+            uint16_t* o = f.dq + (int64_t)(seq.q0 + t) * f.lddq + (int64_t)(2 * head + m) * a.d;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) attn_store(o, b * 32, a.d, lane, acc[m][b], factor[m]);
+            for (int b = 0; b < kBlocks; ++b) attn_store(o, b * 32, a.d, lane, acc[m][b], factor[m]);
+        } else {
+            float* o = f.part + (((int64_t)split * a.tokens_q + seq.q0 + t) * a.heads + head) * E + m * D;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) attn_store_part(o + b * 32, lane, acc[m][b], factor[m]);
+        }
     }
 }
 
 // ------------------------------------------------------------------ dk, dv: a workgroup's keys, all rows that see them
 // A tile's rows bring along lse and D of both maps and, where heads share keys, lambda.
 template <int D, int WAVES, int RT, bool SHARED>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
+__global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dkv(AttnGradients f)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][RT * Tile::kRow];   // buffer; queries, dout
-    __shared__ __attribute__((aligned(1024))) char values[32 * WAVES * Tile::kRow];
-    __shared__ __attribute__((aligned(256))) float facts[2][SHARED ? 5 : 4][RT];
+    // of a buffer: queries, dout, facts
+    constexpr int kTile = RT * Tile::kRow, kFacts = SHARED ? 5 : 4, kBuffer = 2 * kTile + (kFacts * RT * 4 + 255) / 256 * 256;
+    // one array: with several, what the compiler is told of the tiles' memory is lost to what it knows of the arrays
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kBuffer + 32 * WAVES * Tile::kRow];   // two buffers, the keys' values
+    const AttnLds all = (AttnLds)&lds[0], values = all + 2 * kBuffer;
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads);
-    const int head_k = id / f.slots, slot = id - head_k * f.slots;
+    const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads * f.splits);
+    const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
     const uint32_t group = a.group.d;
 
     const int s = attn_find(a.k_end, a.n_seqs, a.tokens_k, 1, 32 * WAVES, slot);
@@ -198,7 +238,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
     const int key0 = tile * 32 * WAVES + wave * 32, key_ = key0 + attn_swapped(lane & 31), key = min(key_, seq.lk - 1);
     const int rows = seq.lq * (int)group;
     // under the causal mask the first query that sees this tile's first key
-    const int begin = (a.causal ? min(max(tile * 32 * WAVES + seq.lq - seq.lk, 0), seq.lq) * (int)group : 0) / RT * RT;
+    const int seeing = a.causal ? min(max(tile * 32 * WAVES + seq.lq - seq.lk, 0), seq.lq) * (int)group : 0;
+    const int run = (rows - seeing + f.splits * RT - 1) / (f.splits * RT) * RT;
+    const int begin = min(seeing + split * run, rows), end = min(begin + run, rows);
 
     // the keys stay in registers, the values in LDS, as far as the waves' registers go
     tile_bf16x8 k[2][kSteps];
@@ -209,23 +251,28 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) k[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + m * D + i * 16);
         const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
-        Tile::template load<32 * WAVES, WAVES>(values, wave, lane, [&](int r) { return values_at + (int64_t)min(tile * 32 * WAVES + r, seq.lk - 1) * a.ldv * 2; });
+        Tile::template load<32 * WAVES, WAVES>(values, wave, lane, values_at + (int64_t)(tile * 32 * WAVES) * a.ldv * 2, (uint32_t)a.ldv * 2,
+                                               seq.lk - tile * 32 * WAVES);
     }
-    const AttnLds v_tile = attn_lds(values) + wave * 32 * Tile::kRow;
     const char* const queries_at = reinterpret_cast<const char*>(a.q + (int64_t)seq.q0 * a.ldq + (int64_t)head_k * group * E);
     const char* const douts_at = reinterpret_cast<const char*>(f.dout + (int64_t)seq.q0 * f.lddout + (int64_t)head_k * group * E);
-    const auto fetch = [&](int r0, int buffer) {
-        const auto place = [&](const char* at, int64_t ld, int r) {
-            const int row = min(r0 + r, rows - 1), t = (int)a.group(row);
-            return at + (t * ld + (int64_t)(row - t * (int)group) * E) * 2;
-        };
-        Tile::template load<RT, WAVES>(lds[buffer][0], wave, lane, [&](int r) { return place(queries_at, a.ldq, r); });
-        Tile::template load<RT, WAVES>(lds[buffer][1], wave, lane, [&](int r) { return place(douts_at, f.lddout, r); });
+    const auto fetch = [&](AttnLds to, int r0) {
+        if constexpr (SHARED) {
+            const auto place = [&](const char* at, int64_t ld, int r) {
+                const int row = min(r0 + r, rows - 1), t = (int)a.group(row);
+                return at + (t * ld + (int64_t)(row - t * (int)group) * E) * 2;
+            };
+            Tile::template gather<RT, WAVES>(to, wave, lane, [&](int r) { return place(queries_at, a.ldq, r); });
+            Tile::template gather<RT, WAVES>(to + kTile, wave, lane, [&](int r) { return place(douts_at, f.lddout, r); });
+        } else {
+            Tile::template load<RT, WAVES>(to, wave, lane, queries_at + (int64_t)r0 * a.ldq * 2, (uint32_t)a.ldq * 2, rows - r0);
+            Tile::template load<RT, WAVES>(to + kTile, wave, lane, douts_at + (int64_t)r0 * f.lddout * 2, (uint32_t)f.lddout * 2, rows - r0);
+        }
         // a wave a fact, a lane a row
-        for (int n = wave; n < (SHARED ? 5 : 4); n += WAVES) {
-            const int row = min(r0 + lane, rows - 1), t = (int)a.group(row), head = head_k * (int)group + row - t * (int)group;
+        for (int n = wave; n < kFacts; n += WAVES) {
+            const int row = min(r0 + lane, rows - 1), t = SHARED ? (int)a.group(row) : row, head = head_k * (int)group + (SHARED ? row - t * (int)group : 0);
             const float* at = n == 4 ? a.lambda + head : f.facts + (n >> 1) * f.of_facts + (int64_t)(2 * head + (n & 1)) * a.tokens_q + seq.q0 + t;
-            if (lane < RT) load4_to_lds(at, facts[buffer][n]);
+            if (lane < RT) attn_load4(at, to + 2 * kTile + n * RT * 4);
         }
     };
     attn_f32x16 acc_k[2][kBlocks], acc_v[2 * kBlocks];
@@ -234,36 +281,33 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
 
     const AttnReads<D> reads(lane);
     const float lambda_of_all = a.lambda[head_k * group];   // where every key head has one query head
-    if (begin < rows) fetch(begin, 0);
-    int buffer = 0;
+    const auto step = [&](AttnLds from_lds, AttnLds to_lds, AttnLds v_lds, int r0) {
+        if (r0 + RT < end) fetch(to_lds, r0 + RT);
+        uint32_t q_tile = 0;
 #pragma unroll 1
-    for (int r0 = begin; r0 < rows; r0 += RT, buffer ^= 1) {
-        attn_wait_loads();
-        __syncthreads();
-        if (r0 + RT < rows) fetch(r0 + RT, buffer ^ 1);
-        AttnLds q_tile = attn_lds(lds[buffer][0]), o_tile = attn_lds(lds[buffer][1]);
-#pragma unroll 1
-        for (int r_first = r0; r_first < min(r0 + RT, rows); r_first += 32, q_tile += 32 * Tile::kRow, o_tile += 32 * Tile::kRow) {
+        for (int r_first = r0; r_first < min(r0 + RT, end); r_first += 32, q_tile += 32 * Tile::kRow) {
+            const uint32_t o_tile = q_tile + kTile;
             const int r_last = r_first + 31, sub = r_first - r0;
             // keys in sight grow with the row
             const int seen_first = attn_seen(a, seq, (int)a.group(r_first)), seen_last = attn_seen(a, seq, (int)a.group(min(r_last, rows - 1)));
             if (seen_last <= key0) continue;
             const bool masked = seen_first < max(key0 + 32, 2) || r_last >= rows;
-            const float* const fact = &facts[buffer][0][sub + 8 * (lane >> 5)];
             // eight rows' facts: rows 16 i + 8 (lane / 32) + 0 .. 7
+            typedef __attribute__((address_space(3))) const tile_f32x4* Facts;
+            const AttnLds fact = from_lds + 2 * kTile + (sub + 8 * (lane >> 5)) * 4;
             const auto fact8 = [&](int which, int i, float o[8]) {
-                const tile_f32x4* p = reinterpret_cast<const tile_f32x4*>(fact + which * RT + i * 16);
+                const Facts p = (Facts)(fact + (which * RT + i * 16) * 4);
                 const tile_f32x4 lo = p[0], hi = p[1];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = lo[e], o[4 + e] = hi[e];
             };
             attn_f32x16 dp{}, score[2] = {};
 #pragma unroll
-            for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(reads.straight(o_tile, i), reads.straight(v_tile, i), dp);
+            for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(reads.straight(from_lds, o_tile, i), reads.straight(v_lds, 0, i), dp);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) score[m] = attn_mfma(reads.straight(q_tile, m * kSteps + i), k[m][i], score[m]);
+                for (int m = 0; m < 2; ++m) score[m] = attn_mfma(reads.straight(from_lds, q_tile, m * kSteps + i), k[m][i], score[m]);
             if (masked) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -296,16 +340,33 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
                 }
                 const tile_bf16x8 ds2 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds)), p = __builtin_bit_cast(tile_bf16x8, bf16_pack8(mixed));
 #pragma unroll
-                for (int b = 0; b < 2 * kBlocks; ++b) acc_v[b] = attn_mfma(reads.turned(o_tile, i * 16, b), p, acc_v[b]);
+                for (int b = 0; b < 2 * kBlocks; ++b) acc_v[b] = attn_mfma(reads.turned(from_lds, o_tile, i * 16, b), p, acc_v[b]);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    acc_k[0][b] = attn_mfma(reads.turned(q_tile, i * 16, b), ds1, acc_k[0][b]);
-                    acc_k[1][b] = attn_mfma(reads.turned(q_tile, i * 16, kBlocks + b), ds2, acc_k[1][b]);
+                    acc_k[0][b] = attn_mfma(reads.turned(from_lds, q_tile, i * 16, b), ds1, acc_k[0][b]);
+                    acc_k[1][b] = attn_mfma(reads.turned(from_lds, q_tile, i * 16, kBlocks + b), ds2, acc_k[1][b]);
                 }
             }
         }
+    };
+    if (begin < end) fetch(all, begin);
+    int buffer = 0;
+#pragma unroll 1
+    for (int r0 = begin; r0 < end; r0 += RT, buffer ^= 1) {
+        attn_wait_loads();
+        __syncthreads();
+        step(all + buffer * kBuffer, all + (buffer ^ 1) * kBuffer, values + wave * 32 * Tile::kRow, r0);
     }
     if (key_ >= seq.lk) return;
+    if (f.splits > 1) {
+        const int64_t at = (((int64_t)split * a.tokens_k + seq.k0 + key) * a.kv_heads + head_k) * E;
+#pragma unroll
+        for (int b = 0; b < 2 * kBlocks; ++b) {
+            attn_store_part(f.part_v + at + b * 32, lane, acc_v[b], 1.0f);
+            attn_store_part(f.part + at + b * 32, lane, acc_k[b / kBlocks][b % kBlocks], a.scale);
+        }
+        return;
+    }
     uint16_t* o = f.dv + (int64_t)(seq.k0 + key) * f.lddv + (int64_t)head_k * a.e;
 #pragma unroll
     for (int b = 0; b < 2 * kBlocks; ++b) attn_store(o, b * 32, a.e, lane, acc_v[b], 1.0f);
@@ -315,6 +376,34 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(AttnGradients f)
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) attn_store(o, b * 32, a.d, lane, acc_k[m][b], a.scale);
     }
+}
+
+// ------------------------------------------------------------------ joining splits
+struct AttnSum {
+    const float* part;    // (split, row, run of `up` values)
+    uint16_t* to;         // (row, run of `width` values)
+    int64_t ld;
+    int rows, runs, width, up;
+    const int32_t* last;  // rows behind it are left as they were
+};
+
+struct AttnSums {
+    AttnSum job[2];
+};
+
+__global__ __launch_bounds__(256) void k_attn_sum(AttnSums jobs, int splits)
+{
+    const AttnSum& j = jobs.job[blockIdx.y];
+    const int per = j.runs * (j.up / 4);
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(n / per), in = (int)(n - (int64_t)row * per), run = in / (j.up / 4), c = (in - run * (j.up / 4)) * 4;
+    if (row >= min(max(*j.last, 0), j.rows)) return;
+    tile_f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < splits; ++s) sum += reinterpret_cast<const tile_f32x4*>(j.part)[s * (int64_t)j.rows * per + n];
+    uint16_t* to = j.to + row * j.ld + run * j.width + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < j.width) to[e] = (uint16_t)bf16_bits(sum[e]);
 }
 
 // ------------------------------------------------------------------ rows of G
@@ -339,21 +428,105 @@ __global__ __launch_bounds__(256) void k_attn_lambda(AttnParts parts, const floa
     if (threadIdx.x == 0) G[p * ldg + h] = (float)-all[0];
 }
 
-template <int D, int WAVES, int KT, int RT>
-hipError_t launch(AttnGradients f, hipStream_t stream)
+// Workgroups of both passes: their waves, tiles and splits.
+struct Shape {
+    int waves_q, slots_q, splits_q, waves_k, slots_k, splits_k;
+};
+
+constexpr int kFewWaves = 2;
+constexpr int most_waves(int D) { return D == 128 ? 4 : 8; }
+
+Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D)
 {
-    const int64_t rows = (int64_t)f.a.tokens_q * f.a.group.d;
-    f.slots = (int)(rows / (32 * WAVES)) + f.a.n_seqs;
-    k_attn_dq<D, WAVES, KT><<<f.slots * f.a.kv_heads, 64 * WAVES, 0, stream>>>(f);
-    f.slots = f.a.tokens_k / (32 * WAVES) + f.a.n_seqs;
+    const int64_t rows = tokens_q * (heads / kv_heads);
+    // Large workgroups read the other side least often; where they would leave compute units without work, small ones, and
+    // where those are too few, the other side split among several.
+    const auto side = [&](int64_t own, int64_t other, int& waves, int& slots, int& splits) {
+        const int64_t large = 32 * most_waves(D);
+        const bool enough = own / n_seqs >= large && own / large * kv_heads >= 192;
+        waves = enough ? most_waves(D) : kFewWaves;
+        slots = (int)(own / (32 * waves)) + n_seqs;
+        const int64_t blocks = std::max<int64_t>(own / (32 * waves), n_seqs) * kv_heads;
+        splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({640 / blocks, other / n_seqs / 256, (int64_t)16}));
+    };
+    Shape o;
+    side(rows, tokens_k, o.waves_q, o.slots_q, o.splits_q);
+    side(tokens_k, rows, o.waves_k, o.slots_k, o.splits_k);
+    return o;
+}
+
+template <int D, int WAVES, int KT>
+void launch_dq(const AttnGradients& f, const Shape& s, hipStream_t stream)
+{
+    const int blocks = s.slots_q * f.a.kv_heads * s.splits_q;
+    if (s.splits_q == 1) {
+        k_attn_dq<D, WAVES, KT, kAll><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        return;
+    }
+    if constexpr (WAVES == kFewWaves) {
+        k_attn_dq<D, WAVES, KT, kSplitMeans><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dq<D, WAVES, KT, kSplitRest><<<blocks, 64 * WAVES, 0, stream>>>(f);
+    }
+}
+
+template <int D, int WAVES, int RT>
+void launch_dkv(const AttnGradients& f, const Shape& s, hipStream_t stream)
+{
+    const int blocks = s.slots_k * f.a.kv_heads * s.splits_k;
     if (f.a.group.d > 1)
-        k_attn_dkv<D, WAVES, RT, true><<<f.slots * f.a.kv_heads, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dkv<D, WAVES, RT, true><<<blocks, 64 * WAVES, 0, stream>>>(f);
     else
-        k_attn_dkv<D, WAVES, RT, false><<<f.slots * f.a.kv_heads, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dkv<D, WAVES, RT, false><<<blocks, 64 * WAVES, 0, stream>>>(f);
+}
+
+void launch_sums(const AttnSum* job, int n, int splits, hipStream_t stream)
+{
+    AttnSums all{};
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        all.job[i] = job[i];
+        most = std::max(most, (int64_t)job[i].rows * job[i].runs * (job[i].up / 4));
+    }
+    k_attn_sum<<<dim3((uint32_t)((most + 255) / 256), n), 256, 0, stream>>>(all, splits);
+}
+
+template <int D, int KT, int RT>
+hipError_t launch(AttnGradients f, const Shape& s, hipStream_t stream)
+{
+    const Attn& a = f.a;
+    if (a.tokens_q > 0) {
+        f.slots = s.slots_q, f.splits = s.splits_q;
+        if (s.waves_q == kFewWaves)
+            launch_dq<D, kFewWaves, 32>(f, s, stream);
+        else
+            launch_dq<D, most_waves(D), KT>(f, s, stream);
+        const AttnSum dq = {f.part, f.dq, f.lddq, a.tokens_q, 2 * a.heads, a.d, D, a.q_end + a.n_seqs - 1};
+        if (s.splits_q > 1) launch_sums(&dq, 1, s.splits_q, stream);
+    }
+    if (a.tokens_k > 0) {
+        f.slots = s.slots_k, f.splits = s.splits_k;
+        f.part_v = f.part + (int64_t)s.splits_k * a.tokens_k * a.kv_heads * 2 * D;
+        if (s.waves_k == kFewWaves)
+            launch_dkv<D, kFewWaves, 32>(f, s, stream);
+        else
+            launch_dkv<D, most_waves(D), RT>(f, s, stream);
+        const AttnSum dkv[2] = {{f.part, f.dk, f.lddk, a.tokens_k, 2 * a.kv_heads, a.d, D, a.k_end + a.n_seqs - 1},
+                                {f.part_v, f.dv, f.lddv, a.tokens_k, a.kv_heads, a.e, 2 * D, a.k_end + a.n_seqs - 1}};
+        if (s.splits_k > 1) launch_sums(dkv, 2, s.splits_k, stream);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
+
+// lse and D of every row, and what splits leave: of D and dq, then of dk and dv
+int64_t attn_gradients_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D)
+{
+    const Shape s = shape_of(tokens_q, tokens_k, n_seqs, heads, kv_heads, D);
+    const int64_t q = s.splits_q > 1 ? s.splits_q * tokens_q * heads * (2 * D + 2) * 4 : 0;
+    const int64_t k = s.splits_k > 1 ? s.splits_k * tokens_k * kv_heads * 4 * D * 4 : 0;
+    return round_up(tokens_q * heads * 16, 256) + round_up(std::max(q, k), 256);
+}
 
 hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream)
 {
@@ -361,11 +534,14 @@ hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream)
     char* place = c.workspace;
     hipError_t e = attn_lay_out(c, f.a, f.dout, f.lddout, place, stream);
     if (e != hipSuccess) return e;
+    const int D = attn_width(c.d, c.e);
+    const Shape s = shape_of(c.tokens_q, c.tokens_k, c.n_seqs, c.heads, c.kv_heads, D);
     f.lse = c.lse, f.facts = reinterpret_cast<float*>(place), f.of_facts = (int64_t)2 * c.heads * c.tokens_q;
+    f.part = reinterpret_cast<float*>(place + round_up(c.tokens_q * c.heads * 16, 256));
+    f.part_mean = f.part + (int64_t)s.splits_q * c.tokens_q * c.heads * 2 * D;
     f.dq = static_cast<uint16_t*>(c.dq), f.dk = static_cast<uint16_t*>(c.dk), f.dv = static_cast<uint16_t*>(c.dv);
     f.lddq = c.lddq, f.lddk = c.lddk, f.lddv = c.lddv;
-    const int D = attn_width(c.d, c.e);
-    e = D == 32 ? launch<32, 8, 64, 64>(f, stream) : D == 64 ? launch<64, 8, 64, 64>(f, stream) : launch<128, 4, 64, 32>(f, stream);
+    e = D == 32 ? launch<32, 64, 64>(f, s, stream) : D == 64 ? launch<64, 64, 64>(f, s, stream) : launch<128, 64, 32>(f, s, stream);
     if (e != hipSuccess) return e;
     AttnParts parts;
     for (int p = 0; p < c.k_parts; ++p) parts.end[p] = (int)c.part_end[p];

@@ -76,6 +76,7 @@ agc_status attn_arguments(const char* name, const agc::AttnCall& c, bool gradien
         return refuse(AGC_EINVAL, n + ": null pointer");
     const int64_t row_q = (int64_t)2 * c.heads * c.d, row_k = (int64_t)2 * c.kv_heads * c.d;
     if (c.ldq < row_q || c.ldk < row_k || c.ldv < (int64_t)c.kv_heads * c.e) return refuse(AGC_ESHAPE, n + ": a row stride is smaller than the row");
+    if (std::max({c.ldq, c.ldk, c.ldv, c.lddout}) > (1 << 24)) return refuse(AGC_ESHAPE, n + ": row strides must be up to 2^24");
     // heads of just the kernels' widths are read where they lie, 16 bytes at a time
     const int D = agc::attn_width(c.d, c.e);
     const uintptr_t unit_d = c.d == D ? 16 : 2, unit_e = c.e == 2 * D ? 16 : 2;

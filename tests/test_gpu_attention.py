@@ -191,6 +191,7 @@ class Case:
 LENS = {
     "one": [(1, 1)], "tiny": [(3, 5), (1, 1), (2, 2)], "edge": [(31, 31), (32, 32), (33, 33), (65, 65)], "tiles": [(257, 300), (64, 64)],
     "more_queries": [(40, 7), (300, 65)], "empty": [(0, 9), (5, 0), (0, 0), (70, 70), (8, 0)], "many": [(i % 7, (3 * i) % 11) for i in range(150)],
+    "few_keys": [(700, 20), (900, 35)], "long_keys": [(33, 1500)], "long_both": [(300, 1400), (0, 3), (260, 1100)],
     "few_rows": [(1, 700), (2, 1300), (1, 64), (1, 0), (3, 2)], "one_query": [(1, 5000)],
 }
 
@@ -400,7 +401,7 @@ def raw(grad=False, q=256, ldq=512, k=256, ldk=256, v=256, ldv=256, nq=3, nk=4, 
     (dict(nq=2 ** 26, heads=32, ldq=4096), -2), (dict(nk=2 ** 26, heads=64, kv=32, ldk=4096, ldv=4096, ldq=8192), -2),
     (dict(n=2 ** 20, heads=32, kv=32, ldq=4096, ldk=4096, ldv=4096), -2), (dict(scale=math.inf), -1), (dict(scale=math.nan), -1), (dict(scale=-0.5), -1),
     (dict(q=0), -1), (dict(k=0), -1), (dict(v=0), -1), (dict(lam=0), -1), (dict(qe=0), -1), (dict(ke=0), -1), (dict(ws=0), -1),
-    (dict(ldq=504), -2), (dict(ldk=248), -2), (dict(ldv=248), -2), (dict(q=258), -4), (dict(k=264), -4), (dict(v=258), -4), (dict(ldq=516), -4),
+    (dict(ldq=2 ** 24 + 8), -2), (dict(ldk=2 ** 24 + 8), -2), (dict(ldv=2 ** 24 + 8), -2), (dict(ldq=504), -2), (dict(ldk=248), -2), (dict(ldv=248), -2), (dict(q=258), -4), (dict(k=264), -4), (dict(v=258), -4), (dict(ldq=516), -4),
     (dict(ldk=257), -4), (dict(ldv=260), -4), (dict(q=257, d=60), -4), (dict(lam=6), -4), (dict(qe=2), -4), (dict(ke=2), -4), (dict(lse=2), -4), (dict(ws=128), -4)])
 def test_refusals(grad, change, status):
     assert raw(grad, **change) == status
@@ -413,7 +414,7 @@ def test_refusals_of_the_forward_pass(change, status):
 
 @pytest.mark.parametrize("change,status", [
     (dict(parts=None), -1), (dict(parts=()), -2), (dict(parts=(2,)), -2), (dict(parts=(3, 2)), -2), (dict(parts=(2, 1, 3)), -2), (dict(parts=(3,) * 257), -2),
-    (dict(dout=0), -1), (dict(lse=0), -1), (dict(dq=0), -1), (dict(dk=0), -1), (dict(dv=0), -1), (dict(G=0), -1), (dict(lddout=504), -2), (dict(lddq=511), -2),
+    (dict(dout=0), -1), (dict(lse=0), -1), (dict(dq=0), -1), (dict(dk=0), -1), (dict(dv=0), -1), (dict(G=0), -1), (dict(lddout=504), -2), (dict(lddout=2 ** 24 + 8), -2), (dict(lddq=511), -2),
     (dict(lddk=255), -2), (dict(lddv=255), -2), (dict(ldg=3), -2), (dict(dout=258), -4), (dict(lddout=516), -4), (dict(dq=1), -4), (dict(dk=1), -4), (dict(dv=1), -4),
     (dict(G=2), -4)])
 def test_refusals_of_the_gradients(change, status):
@@ -445,4 +446,6 @@ def test_workspace():
     assert need(1 << 16, 1 << 16, 8, 16, 4, 64, 128) == 256
     assert need(1 << 16, 1 << 16, 8, 16, 4, 63, 128) > (1 << 16) * 20 * 256
     assert need(1 << 16, 1 << 16, 8, 16, 4, 64, 128, True) == 256 + (1 << 16) * 16 * 16
+    # forward and gradients share what splits leave; it does not grow with the keys
+    assert need(8, 1 << 24, 8, 16, 4, 64, 128, True) >= need(8, 1 << 24, 8, 16, 4, 64, 128) < 1 << 24
     assert need(1, 1, 0, 1, 1, 1, 1) == 0 and need(1, 1, 1, 3, 2, 1, 1) == 0 and need(1, 1, 1, 1, 1, 129, 1) == 0
