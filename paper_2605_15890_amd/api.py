@@ -671,8 +671,9 @@ def agc_muon_update(beta, m1, ghat, offsets, rows, cols, lr, momentum, nesterov,
 def _on_current_gpu(what, *tensors):
     """Refuses tensors that the kernels could not reach from the current GPU."""
     import torch
+    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2   # host memory is -1
     for t in tensors:
-        if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        if t.get_device() != device:
             raise AgcError(AGC_EINVAL, f"{what}: tensors must lie on the current GPU")
 
 

@@ -29,7 +29,7 @@ constexpr int attn_maps_of_a_wave(int D) { return D == 128 ? 1 : 2; }
 constexpr float kGrowth = 8.0f;
 
 template <int D, int WAVES, int KT>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
+__global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1 : 2) void k_attn_forward(AttnForward f)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = E / 32;
@@ -217,59 +217,66 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_forward(AttnForward f)
     for (int b = 0; b < kBlocks; ++b) attn_store(o, b * 32, a.e, lane, acc[0][b], 1.0f);
 }
 
-// Joins the splits of a row, a wave each: sums scaled to the largest maximum.
-template <int D>
+// Joins the splits: a row's 4 D sums of both maps by D threads, four each, times ABREAST splits at once, whose sums meet in LDS.
+template <int D, int ABREAST>
 __global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
 {
-    constexpr int E = 2 * D, kPer = E / 64;
+    constexpr int kRows = 256 / (D * ABREAST);
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63;
-    const int64_t all = (int64_t)a.tokens_q * a.heads, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int last = min(max(a.q_end[a.n_seqs - 1], 0), a.tokens_q);
-    if (at >= all) return;
+    const int64_t all = (int64_t)a.tokens_q * a.heads, row0 = (int64_t)blockIdx.x * kRows;
     const int group = (int)a.group.d;
-    const int64_t of_head = (int64_t)a.tokens_q * group;
-    const int head_k = (int)(at / of_head), row = (int)(at - head_k * of_head), t = (int)a.group(row), head = head_k * group + row - t * group;
-    if (t >= last) return;   // behind the last sequence: left as it was
-    // a lane a split: what its sums are multiplied with; one without keys left nothing in memory
-    float weight[2], top[2], sum[2];
+    __shared__ float weights[kRows][2][64];
+    for (int r = threadIdx.x >> 6; r < kRows && row0 + r < all; r += 4) {
+        const int64_t at = row0 + r, of_head = (int64_t)a.tokens_q * group;
+        const int head_k = (int)(at / of_head), row = (int)(at - head_k * of_head), t = (int)a.group(row), head = head_k * group + row - t * group;
+        float top[2], sum[2];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-        const AttnStat x = lane < f.splits ? f.stat[2 * (lane * all + at) + m] : AttnStat{-INFINITY, 0.0f};
-        const bool none = x.sum == 0.0f;
-        top[m] = none ? -INFINITY : x.top;
-        for (int d = 32; d > 0; d >>= 1) top[m] = fmaxf(top[m], __shfl_xor(top[m], d));
-        weight[m] = none ? 0.0f : __builtin_amdgcn_exp2f(x.top - top[m]);
-        sum[m] = none ? 0.0f : x.sum * weight[m];
-        for (int d = 32; d > 0; d >>= 1) sum[m] += __shfl_xor(sum[m], d);
-    }
-    const float by[2] = {sum[0] == 0.0f ? 0.0f : 1.0f / sum[0], sum[1] == 0.0f ? 0.0f : -a.lambda[head] / sum[1]};
-    __shared__ float weights[4][2][64];
-    float (&mine)[2][64] = weights[threadIdx.x >> 6];
-    mine[0][lane] = weight[0] * by[0], mine[1][lane] = weight[1] * by[1];
-    wave_lds_fence();
-    float v[kPer] = {};
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-        const float* o = f.part + (2 * at + m) * E + lane;
-#pragma unroll 8
-        for (int s = 0; s < f.splits; ++s) {
-            const float w = mine[m][s];
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const float x = o[s * (2 * all * E) + i * 64];
-                v[i] = w == 0.0f ? v[i] : fmaf(x, w, v[i]);
-            }
+        for (int m = 0; m < 2; ++m) {
+            // a lane a split: what its sums are multiplied with; one without keys left nothing in memory
+            const AttnStat x = lane < f.splits ? f.stat[2 * (lane * all + at) + m] : AttnStat{-INFINITY, 0.0f};
+            const bool none = x.sum == 0.0f;
+            top[m] = none ? -INFINITY : x.top;
+            for (int d = 32; d > 0; d >>= 1) top[m] = fmaxf(top[m], __shfl_xor(top[m], d));
+            const float weight = none ? 0.0f : __builtin_amdgcn_exp2f(x.top - top[m]);
+            sum[m] = none ? 0.0f : x.sum * weight;
+            for (int d = 32; d > 0; d >>= 1) sum[m] += __shfl_xor(sum[m], d);
+            const float by = sum[m] == 0.0f ? 0.0f : (m ? -a.lambda[head] : 1.0f) / sum[m];
+            weights[r][m][lane] = weight * by;
+        }
+        if (f.lse && lane < 2 && t < min(max(a.q_end[a.n_seqs - 1], 0), a.tokens_q)) {
+            const float s = lane ? sum[1] : sum[0], m = lane ? top[1] : top[0];
+            f.lse[(int64_t)(2 * head + lane) * a.tokens_q + t] = s == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(s);
         }
     }
+    __syncthreads();
+    const int in = threadIdx.x % D, sub = threadIdx.x / D % ABREAST, r = threadIdx.x / (D * ABREAST), m = in / (D / 2);
+    const int64_t at = row0 + r;
+    tile_f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (at < all) {
+        const tile_f32x4* part = reinterpret_cast<const tile_f32x4*>(f.part) + at * D + in;
+#pragma unroll 4
+        for (int s = sub; s < f.splits; s += ABREAST) {
+            const float w = weights[r][m][s];
+            const tile_f32x4 x = part[s * all * D];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = w == 0.0f ? v[i] : fmaf(x[i], w, v[i]);
+        }
+    }
+    __shared__ tile_f32x4 meet[256];
+    meet[threadIdx.x] = v;
+    __syncthreads();
+    if (at >= all || sub != 0 || m != 0) return;
+    v = tile_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < ABREAST; ++s) v += meet[threadIdx.x + s * D] + meet[threadIdx.x + s * D + D / 2];
+    const int64_t of_head = (int64_t)a.tokens_q * group;
+    const int head_k = (int)(at / of_head), row = (int)(at - head_k * of_head), t = (int)a.group(row), head = head_k * group + row - t * group;
+    if (t >= min(max(a.q_end[a.n_seqs - 1], 0), a.tokens_q)) return;   // behind the last sequence: left as it was
     uint16_t* o = f.out + t * f.ldo + (int64_t)head * a.e;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-        if (lane + i * 64 < a.e) o[lane + i * 64] = (uint16_t)bf16_bits(v[i]);
-    if (f.lse && lane < 2) {
-        const float s = lane ? sum[1] : sum[0], m = lane ? top[1] : top[0];
-        f.lse[(int64_t)(2 * head + lane) * a.tokens_q + t] = s == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(s);
-    }
+    for (int i = 0; i < 4; ++i)
+        if (in * 4 + i < a.e) o[in * 4 + i] = (uint16_t)bf16_bits(v[i]);
 }
 
 template <int D, int WAVES, int KT>
@@ -278,7 +285,10 @@ hipError_t launch(AttnForward f, hipStream_t stream)
     k_attn_forward<D, WAVES, KT><<<f.slots * f.a.kv_heads * f.splits, 64 * WAVES, 0, stream>>>(f);
     if (f.splits > 1) {
         const int64_t all = (int64_t)f.a.tokens_q * f.a.heads;
-        k_attn_join<D><<<(uint32_t)((all + 3) / 4), 256, 0, stream>>>(f);
+        if (f.splits > 8)
+            k_attn_join<D, 256 / D><<<(uint32_t)all, 256, 0, stream>>>(f);
+        else
+            k_attn_join<D, 1><<<(uint32_t)((all * D + 255) / 256), 256, 0, stream>>>(f);
     }
     return hipGetLastError();
 }
@@ -292,14 +302,16 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
 {
     Shape o;
     const int64_t rows = tokens_q * (heads / kv_heads);
-    // up to 32 rows a sequence: one wave (of each map) has them all
-    const int unit = 2 / attn_maps_of_a_wave(D);
-    o.waves = rows <= (int64_t)32 * n_seqs ? unit : 8;
-    o.slots = (int)(rows / (32 * o.waves / unit)) + n_seqs;
-    const int64_t blocks = (int64_t)o.slots * kv_heads, wanted = o.waves < 8 ? 1024 : 256;
-    const int64_t keys = tokens_k / n_seqs;
-    const int64_t most = std::max<int64_t>(1, keys / 128);
-    o.splits = (int)std::max<int64_t>(1, std::min({wanted / std::max<int64_t>(1, blocks), most, (int64_t)64}));
+    const int unit = 2 / attn_maps_of_a_wave(D);   // waves of 32 rows
+    // Large workgroups read the keys least often; small ones where those would leave compute units without work, down to
+    // one wave (of each map) that has a sequence's up to 32 rows; and where these are too few, the keys split among several.
+    const int64_t large = 32 * 8 / unit;
+    const bool enough = rows / n_seqs >= large && rows / large * kv_heads >= 192;
+    o.waves = enough ? 8 : (rows <= (int64_t)32 * n_seqs ? 1 : 2) * unit;
+    const int64_t own = 32 * o.waves / unit;
+    o.slots = (int)(rows / own) + n_seqs;
+    const int64_t blocks = std::max<int64_t>(rows / own, n_seqs) * kv_heads;
+    o.splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({(own == 32 ? 1024 : 512) / blocks, tokens_k / n_seqs / 128, (int64_t)64}));
     return o;
 }
 
@@ -399,9 +411,9 @@ hipError_t launch_attn_forward(const AttnCall& c, hipStream_t stream)
     f.out = static_cast<uint16_t*>(c.out), f.ldo = c.ldo, f.lse = c.lse, f.slots = s.slots, f.splits = s.splits;
     f.stat = reinterpret_cast<AttnStat*>(place);
     f.part = reinterpret_cast<float*>(place + (int64_t)s.splits * c.tokens_q * c.heads * 16);
-    if (D == 32) return s.waves < 8 ? launch<32, 1, 64>(f, stream) : launch<32, 8, 64>(f, stream);
-    if (D == 64) return s.waves < 8 ? launch<64, 1, 32>(f, stream) : launch<64, 8, 64>(f, stream);
-    return s.waves < 8 ? launch<128, 2, 32>(f, stream) : launch<128, 8, 64>(f, stream);
+    if (D == 32) return s.waves == 8 ? launch<32, 8, 64>(f, stream) : s.waves == 2 ? launch<32, 2, 32>(f, stream) : launch<32, 1, 64>(f, stream);
+    if (D == 64) return s.waves == 8 ? launch<64, 8, 64>(f, stream) : s.waves == 2 ? launch<64, 2, 32>(f, stream) : launch<64, 1, 32>(f, stream);
+    return s.waves == 8 ? launch<128, 8, 64>(f, stream) : s.waves == 4 ? launch<128, 4, 32>(f, stream) : launch<128, 2, 32>(f, stream);
 }
 
 }  // namespace agc

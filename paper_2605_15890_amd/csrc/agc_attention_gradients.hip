@@ -215,7 +215,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
 // ------------------------------------------------------------------ dk, dv: a workgroup's keys, all rows that see them
 // A tile's rows bring along lse and D of both maps and, where heads share keys, lambda.
 template <int D, int WAVES, int RT, bool SHARED>
-__global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dkv(AttnGradients f)
+__global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_attn_dkv(AttnGradients f)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
