@@ -671,7 +671,7 @@ def agc_muon_update(beta, m1, ghat, offsets, rows, cols, lr, momentum, nesterov,
 def _on_current_gpu(what, *tensors):
     """Refuses tensors that the kernels could not reach from the current GPU."""
     import torch
-    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2   # host memory is -1
+    device = torch._C._cuda_getDevice() if tensors[0].is_cuda else -2   # host memory is -1
     for t in tensors:
         if t.get_device() != device:
             raise AgcError(AGC_EINVAL, f"{what}: tensors must lie on the current GPU")
@@ -745,7 +745,6 @@ def _attn_operands(L, name, q, k, v, heads, kv_heads, lam, q_end, k_end, lse, wo
     if workspace.nbytes < L.agc_diff_attn_workspace_bytes(nq, nk, n, heads, kv_heads, d, e, gradients):
         raise AgcError(AGC_ESHAPE, f"{name}: the workspace is too small")
     head = (q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, nq, nk, heads, kv_heads, d, e, lam.data_ptr(), q_end.data_ptr())
-    _on_current_gpu(name, q, k, v, lam, q_end, k_end, workspace)
     return head, (nq, d, e), n
 
 
@@ -759,7 +758,7 @@ def agc_diff_attn_forward(q, k, v, heads, kv_heads, lam, q_end, k_end, scale, ca
     ldo = _rows_of(out, nq, heads * e, q.dtype, "out")
     if k_begin is not None:
         _ends(k_begin, n, "k_begin")
-    _on_current_gpu("agc_diff_attn_forward", *[t for t in (out, lse, k_begin) if t is not None])
+    _on_current_gpu("agc_diff_attn_forward", q, k, v, lam, q_end, k_end, workspace, out, *[t for t in (lse, k_begin) if t is not None])
     st = L.agc_diff_attn_forward(*head, None if k_begin is None else k_begin.data_ptr(), k_end.data_ptr(), n, scale,
                                  int(bool(causal)), out.data_ptr(), ldo, None if lse is None else lse.data_ptr(),
                                  workspace.data_ptr(), _stream_handle(stream))
@@ -779,7 +778,7 @@ def agc_diff_attn_partial_gradients(q, k, v, heads, kv_heads, lam, q_end, k_end,
     lddout = _rows_of(dout, nq, heads * e, q.dtype, "dout")
     lddq, lddk, lddv = (_rows_of(g, t.shape[0], t.shape[1], q.dtype, w) for g, t, w in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
     ldg = _rows_of(G_lambda, parts, heads, torch.float32, "G_lambda")
-    _on_current_gpu(name, lse, dout, dq, dk, dv, G_lambda)
+    _on_current_gpu(name, q, k, v, lam, q_end, k_end, workspace, lse, dout, dq, dk, dv, G_lambda)
     st = L.agc_diff_attn_partial_gradients(*head, k_end.data_ptr(), n, scale, int(bool(causal)), lse.data_ptr(), dout.data_ptr(),
                                            lddout, struct.pack(f"{parts}q", *[int(x) for x in part_end]), parts, dq.data_ptr(), lddq,
                                            dk.data_ptr(), lddk, dv.data_ptr(), lddv, G_lambda.data_ptr(), ldg,
@@ -800,8 +799,7 @@ def agc_dropout(x, p, seed, step, site, out, residual=None, stream=None, check=T
     ldx, ldo, ldr = _rows_of(x, rows, cols, x.dtype, "x"), _rows_of(out, rows, cols, out.dtype, "out"), cols
     if residual is not None:
         ldr = _rows_of(residual, rows, cols, out.dtype, "residual")
-        _on_current_gpu("agc_dropout", residual)
-    _on_current_gpu("agc_dropout", x, out)
+    _on_current_gpu("agc_dropout", x, out, x if residual is None else residual)
     st = L.agc_dropout(x.data_ptr(), x_kind, ldx, None if residual is None else residual.data_ptr(), ldr, rows, cols, p,
                        seed & 0xFFFFFFFFFFFFFFFF, step & 0xFFFFFFFFFFFFFFFF, site, out.data_ptr(), out_kind, ldo,
                        _stream_handle(stream))
