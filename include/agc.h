@@ -415,7 +415,8 @@ agc_status agc_diff_attn_forward(const void* q_dev, int64_t ldq, const void* k_d
  *              the last sequence, which are left as they were
  *   G_lambda_dev  device, where row 0 of G holds the gradients of lambda; row p lies p * ldg floats on; overwritten
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 1) bytes, 256-byte aligned (enough for the forward pass too)
- * The maps and dS enter the products as bfloat16, results are rounded once; sums are binary32 in a fixed order.  1 <= k_parts <= 256. */
+ * The maps and dS enter the products with 16 bits, so that results are rounded once; sums are binary32 in a fixed order.
+ * 1 <= k_parts <= 256. */
 agc_status agc_diff_attn_partial_gradients(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev,
                                            int64_t ldv, int64_t tokens_q, int64_t tokens_k, int heads, int kv_heads,
                                            int head_dim, int value_dim, const float* lambda_dev, const int32_t* q_end_dev,

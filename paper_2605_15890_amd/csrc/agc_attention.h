@@ -242,6 +242,26 @@ __device__ __forceinline__ AttnStream<N, AHEAD, Read> attn_stream(const Read& re
 // The other half's value of the same column.
 __device__ __forceinline__ float attn_other_half(float v) { return __shfl_xor(v, 32); }
 
+// Eight values as two bfloat16 parts, sixteen bits of each together.
+struct AttnTwo {
+    tile_bf16x8 top, rest;
+    __device__ __forceinline__ explicit AttnTwo(const float v[8])
+    {
+        float first[8], low[8];
+        const tile_u32x4 bits = bf16_pack8(v);
+        bf16_unpack8(bits, first);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) low[i] = v[i] - first[i];
+        top = __builtin_bit_cast(tile_bf16x8, bits);
+        rest = __builtin_bit_cast(tile_bf16x8, bf16_pack8(low));
+    }
+};
+
+__device__ __forceinline__ attn_f32x16 attn_mfma(const tile_bf16x8& a, const AttnTwo& b, const attn_f32x16& c)
+{
+    return attn_mfma(a, b.rest, attn_mfma(a, b.top, c));
+}
+
 // Registers 8 b .. 8 b + 7 as an operand.
 __device__ __forceinline__ tile_bf16x8 attn_operand(const float v[16], int b)
 {

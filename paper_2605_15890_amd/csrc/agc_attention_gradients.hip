@@ -9,7 +9,9 @@
 // keys twice: D comes from the same P and dP as dS, which makes the rows of dS add up to zero to the last bits of binary32
 // (from dout and the rounded out they would miss it by 2^-8, and a query that sees one key would get a gradient where
 // there is none), and makes D_2, whose sums are rows of G, a binary32 sum of binary32 terms.
-// dS and P enter their products as bfloat16, 2^-8 of a term at most, as the products' other operands are; sums are binary32.
+// dS and the difference of the maps enter their products as two bfloat16 parts, 2^-16 of a term at most: one part would add as
+// much error to a result as its own rounding does, and more where keys have a part in common, which dS, whose rows add up to
+// zero, only cancels as far as it is exact (2.5e-3 in the 2-norm where the rounding alone is 1.66e-3).  Sums are binary32.
 #include <algorithm>
 
 #include "agc_attention.h"
@@ -174,19 +176,16 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
         const auto read = [&](int n) { return reads.turned(from_lds, k_tile, n / (2 * kBlocks) * 16, n % (2 * kBlocks)); };
         auto stream = attn_stream<4 * kBlocks, 2>(read);
         stream.start();
-        tile_bf16x8 ds[2][2];
+        const auto ds = [&](int i, int m) {
+            float v[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = map[m][i * 8 + e] * (dp[i * 8 + e] - mean[m]);
-                ds[i][m] = __builtin_bit_cast(tile_bf16x8, bf16_pack8(v));
-            }
+            for (int e = 0; e < 8; ++e) v[e] = map[m][i * 8 + e] * (dp[i * 8 + e] - mean[m]);
+            return AttnTwo(v);
+        };
+        const AttnTwo d[2][2] = {{ds(0, 0), ds(0, 1)}, {ds(1, 0), ds(1, 1)}};
         stream.run([&](int n, const tile_bf16x8& k) {
             const int i = n / (2 * kBlocks), m = n / kBlocks % 2, b = n % kBlocks;
-            acc[m][b] = attn_mfma(k, ds[i][m], acc[m][b]);
+            acc[m][b] = attn_mfma(k, d[i][m], acc[m][b]);
         });
     });
     if (row_ >= rows) return;
@@ -320,25 +319,25 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float mixed[8], ds[8], lse[8], mean[8], lambda[8];
+                float p1[8], p2[8], ds[8], lse[8], mean[8], lambda[8];
                 fact8(0, i, lse);
                 fact8(2, i, mean);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    mixed[e] = __builtin_amdgcn_exp2f(fmaf(score[0][i * 8 + e], a.to_log2, -lse[e]));
-                    ds[e] = mixed[e] * (dp[i * 8 + e] - mean[e]);
+                    p1[e] = __builtin_amdgcn_exp2f(fmaf(score[0][i * 8 + e], a.to_log2, -lse[e]));
+                    ds[e] = p1[e] * (dp[i * 8 + e] - mean[e]);
                 }
-                const tile_bf16x8 ds1 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds));
+                const AttnTwo ds1(ds);
                 fact8(1, i, lse);
                 fact8(3, i, mean);
                 if constexpr (SHARED) fact8(4, i, lambda);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float p = (SHARED ? lambda[e] : lambda_of_all) * __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
-                    ds[e] = p * (mean[e] - dp[i * 8 + e]);
-                    mixed[e] -= p;
+                    p2[e] = (SHARED ? lambda[e] : lambda_of_all) * __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
+                    ds[e] = p2[e] * (mean[e] - dp[i * 8 + e]);
+                    p1[e] -= p2[e];
                 }
-                const tile_bf16x8 ds2 = __builtin_bit_cast(tile_bf16x8, bf16_pack8(ds)), p = __builtin_bit_cast(tile_bf16x8, bf16_pack8(mixed));
+                const AttnTwo ds2(ds), p(p1);
 #pragma unroll
                 for (int b = 0; b < 2 * kBlocks; ++b) acc_v[b] = attn_mfma(reads.turned(from_lds, o_tile, i * 16, b), p, acc_v[b]);
 #pragma unroll

@@ -2,13 +2,14 @@
 
 Tolerances, element by element.  With u = 2^-24 and A the largest sum of |scale q k| of a pair, a score in binary32 is off by
 (d + 4) u A at most and a map's value by as much of itself, with the sum it is divided by and the powers of two: below
-F = 4 (d + e + 32) u (1 + A) of itself for all of binary32 together.  To that come the roundings to bfloat16, 2^-8 each: one
-of every map's value in its product with v (out) and of their difference (dv), one of every dS (dq, dk), one of the result.
+F = 4 (d + e + 32) u (1 + A) of itself for all of binary32 together.  To that come the roundings to bfloat16, 2^-8 each: one of
+every map's value in its product with v (out), and one of the result.  In the gradients the difference of the maps (dv) and dS
+(dq, dk) enter as two bfloat16 parts: the first leaves 2^-8 of a value, the second 2^-8 of that.  A map's value below 2^-126 is
+no binary32 any more and becomes zero: a sum of the 8192 at most that a test holds, each times factors below 2^7 and 2^5,
+loses less than 2^-100 by it, which every bound of the gradients has on top.
     out  2^-8 |out| + (2^-8 + F) sum of (P1 + |lambda| P2) |v|
-    dv   2^-8 |dv|  + 2^-8 sum of |P1 - lambda P2| |dout| + F sum of (P1 + |lambda| P2) |dout|
-    (A map's value below 2^-126 is no binary32 any more and becomes zero.  A sum of the 1300 at most that a test holds, each
-    times factors below 2^7 and 2^5, loses less than 2^-100 by it, which every bound has on top.)
-    dq   2^-8 |dq|  + scale (2^-8 sum of |dS| |k| + F sum of T |k|),  T = P (sum |dout v| + sum over keys of P sum |dout v|)
+    dv   2^-8 |dv|  + 2^-16 sum of |P1 - lambda P2| |dout| + F sum of (P1 + |lambda| P2) |dout|
+    dq   2^-8 |dq|  + scale (2^-16 sum of |dS| |k| + F sum of T |k|),  T = P (sum |dout v| + sum over keys of P sum |dout v|)
     dk   as dq, with q;   G  F times the sum of T;   lse  (d + 8) u A log2(e) + 2^-20
 """
 import math
@@ -179,7 +180,7 @@ class Case:
         for at_q, at_k, r in self.references():
             for n, at in (("dq", at_q), ("dk", at_k), ("dv", at_k)):
                 want = r[n].reshape(len(r[n]), got[n].shape[1])
-                tol = HALF * np.abs(want) + (HALF * r[n + "_half"] + self.full(r) * r[n + "_full"]).reshape(want.shape) + 2.0 ** -100
+                tol = HALF * np.abs(want) + (HALF ** 2 * r[n + "_half"] + self.full(r) * r[n + "_full"]).reshape(want.shape) + 2.0 ** -100
                 off = np.abs(got[n][at] - want)
                 assert np.all(off <= tol), (n, np.max(off / np.maximum(tol, 1e-30)))
             share[at_q], share_full[at_q] = r["share"], self.full(r) * r["share_full"]
