@@ -22,6 +22,8 @@ struct AttnStat {
     float top, sum;
 };
 
+constexpr int kMostSplits = 256, kFewSplits = 8;   // from there on a row's splits are joined several at once
+
 // Wide heads are worked on by a wave for each map: both maps' sums of 256 values would take all its registers.
 constexpr int attn_maps_of_a_wave(int D) { return D == 128 ? 1 : 2; }
 
@@ -226,7 +228,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
     const int lane = threadIdx.x & 63;
     const int64_t all = (int64_t)a.tokens_q * a.heads, row0 = (int64_t)blockIdx.x * kRows;
     const int group = (int)a.group.d;
-    __shared__ float weights[kRows][2][64];
+    __shared__ float weights[kRows][2][ABREAST > 1 ? kMostSplits : kFewSplits];
     for (int r = threadIdx.x >> 6; r < kRows && row0 + r < all; r += 4) {
         const int64_t at = row0 + r, of_head = (int64_t)a.tokens_q * group;
         const int head_k = (int)(at / of_head), row = (int)(at - head_k * of_head), t = (int)a.group(row), head = head_k * group + row - t * group;
@@ -234,15 +236,28 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             // a lane a split: what its sums are multiplied with; one without keys left nothing in memory
-            const AttnStat x = lane < f.splits ? f.stat[2 * (lane * all + at) + m] : AttnStat{-INFINITY, 0.0f};
-            const bool none = x.sum == 0.0f;
-            top[m] = none ? -INFINITY : x.top;
+            constexpr int kEach = ABREAST > 1 ? kMostSplits / 64 : 1;
+            AttnStat x[kEach];
+            top[m] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int s = i * 64 + lane;
+                x[i] = s < f.splits ? f.stat[2 * (s * all + at) + m] : AttnStat{-INFINITY, 0.0f};
+                if (x[i].sum != 0.0f) top[m] = fmaxf(top[m], x[i].top);
+            }
             for (int d = 32; d > 0; d >>= 1) top[m] = fmaxf(top[m], __shfl_xor(top[m], d));
-            const float weight = none ? 0.0f : __builtin_amdgcn_exp2f(x.top - top[m]);
-            sum[m] = none ? 0.0f : x.sum * weight;
+            sum[m] = 0.0f;
+            float weight[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                weight[i] = x[i].sum == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(x[i].top - top[m]);
+                sum[m] += x[i].sum * weight[i];
+            }
             for (int d = 32; d > 0; d >>= 1) sum[m] += __shfl_xor(sum[m], d);
             const float by = sum[m] == 0.0f ? 0.0f : (m ? -a.lambda[head] : 1.0f) / sum[m];
-            weights[r][m][lane] = weight * by;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (i * 64 + lane < f.splits) weights[r][m][i * 64 + lane] = weight[i] * by;
         }
         if (f.lse && lane < 2 && t < min(max(a.q_end[a.n_seqs - 1], 0), a.tokens_q)) {
             const float s = lane ? sum[1] : sum[0], m = lane ? top[1] : top[0];
@@ -285,7 +300,7 @@ hipError_t launch(AttnForward f, hipStream_t stream)
     k_attn_forward<D, WAVES, KT><<<f.slots * f.a.kv_heads * f.splits, 64 * WAVES, 0, stream>>>(f);
     if (f.splits > 1) {
         const int64_t all = (int64_t)f.a.tokens_q * f.a.heads;
-        if (f.splits > 8)
+        if (f.splits > kFewSplits)
             k_attn_join<D, 256 / D><<<(uint32_t)all, 256, 0, stream>>>(f);
         else
             k_attn_join<D, 1><<<(uint32_t)((all * D + 255) / 256), 256, 0, stream>>>(f);
@@ -311,7 +326,7 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
     const int64_t own = 32 * o.waves / unit;
     o.slots = (int)(rows / own) + n_seqs;
     const int64_t blocks = std::max<int64_t>(rows / own, n_seqs) * kv_heads;
-    o.splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({(own == 32 ? 1024 : 512) / blocks, tokens_k / n_seqs / 128, (int64_t)64}));
+    o.splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({(own == 32 ? 1024 : 512) / blocks, tokens_k / n_seqs / 128, (int64_t)kMostSplits}));
     return o;
 }
 

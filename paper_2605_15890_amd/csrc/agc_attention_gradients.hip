@@ -213,6 +213,12 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
 
 // ------------------------------------------------------------------ dk, dv: a workgroup's keys, all rows that see them
 // A tile's rows bring along lse and D of both maps and, where heads share keys, lambda.
+//
+// Wide heads are worked on by two workgroups, since dk and dv of 32 keys would take a wave's registers twice over: each forms
+// both maps and dP, and has dk of one map (its own) and half of dv.  A third more products than one workgroup would need, in a
+// half of the time that it takes when registers leave for memory (8 x 2048 tokens, 8 heads of 128: 1016 instead of 2544 us).
+constexpr int attn_halves(int D) { return D == 128 ? 2 : 1; }
+
 template <int D, int WAVES, int RT, bool SHARED>
 __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_attn_dkv(AttnGradients f)
 {
@@ -225,7 +231,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
     const AttnLds all = (AttnLds)&lds[0], values = all + 2 * kBuffer;
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads * f.splits);
+    constexpr int kHalves = attn_halves(D), kValues = 2 * kBlocks / kHalves;
+    const int id_ = xcd_order(blockIdx.x, f.slots * a.kv_heads * f.splits * kHalves), half = id_ % kHalves, id = id_ / kHalves;
     const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
     const uint32_t group = a.group.d;
 
@@ -242,13 +249,13 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
     const int begin = min(seeing + split * run, rows), end = min(begin + run, rows);
 
     // the keys stay in registers, the values in LDS, as far as the waves' registers go
-    tile_bf16x8 k[2][kSteps];
+    tile_bf16x8 k[2][kSteps];   // of the own map, of the other one
     {
         const uint16_t* p = a.k + (int64_t)(seq.k0 + key) * a.ldk + head_k * E + (lane >> 5) * 8;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) k[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + m * D + i * 16);
+            for (int i = 0; i < kSteps; ++i) k[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + (m ^ half) * D + i * 16);
         const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
         Tile::template load<32 * WAVES, WAVES>(values, wave, lane, values_at + (int64_t)(tile * 32 * WAVES) * a.ldv * 2, (uint32_t)a.ldv * 2,
                                                seq.lk - tile * 32 * WAVES);
@@ -274,9 +281,11 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
             if (lane < RT) attn_load4(at, to + 2 * kTile + n * RT * 4);
         }
     };
-    attn_f32x16 acc_k[2][kBlocks], acc_v[2 * kBlocks];
+    attn_f32x16 acc_k[2 / kHalves][kBlocks], acc_v[kValues];
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) acc_k[0][b] = acc_k[1][b] = acc_v[b] = acc_v[kBlocks + b] = attn_f32x16{};
+    for (int m = 0; m < 2 / kHalves; ++m)
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) acc_k[m][b] = acc_v[m * kBlocks + b] = attn_f32x16{};
 
     const AttnReads<D> reads(lane);
     const float lambda_of_all = a.lambda[head_k * group];   // where every key head has one query head
@@ -285,7 +294,9 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
         uint32_t q_tile = 0;
 #pragma unroll 1
         for (int r_first = r0; r_first < min(r0 + RT, end); r_first += 32, q_tile += 32 * Tile::kRow) {
-            const uint32_t o_tile = q_tile + kTile;
+            // halves of wide rows lie 256 bytes apart, whole turns of the permutation
+            static_assert(kHalves == 1 || D == 128, "2 D bytes are 256");
+            const uint32_t o_tile = q_tile + kTile, q_own = q_tile + half * 256;
             const int r_last = r_first + 31, sub = r_first - r0;
             // keys in sight grow with the row
             const int seen_first = attn_seen(a, seq, (int)a.group(r_first)), seen_last = attn_seen(a, seq, (int)a.group(min(r_last, rows - 1)));
@@ -306,7 +317,10 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) score[m] = attn_mfma(reads.straight(from_lds, q_tile, m * kSteps + i), k[m][i], score[m]);
+                for (int m = 0; m < 2; ++m) {
+                    const tile_bf16x8 x = kHalves == 2 ? reads.straight(from_lds, q_tile + (m ^ half) * 256, i) : reads.straight(from_lds, q_tile, m * kSteps + i);
+                    score[m] = attn_mfma(x, k[m][i], score[m]);
+                }
             if (masked) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -319,31 +333,35 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float p1[8], p2[8], ds[8], lse[8], mean[8], lambda[8];
-                fact8(0, i, lse);
-                fact8(2, i, mean);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    p1[e] = __builtin_amdgcn_exp2f(fmaf(score[0][i * 8 + e], a.to_log2, -lse[e]));
-                    ds[e] = p1[e] * (dp[i * 8 + e] - mean[e]);
-                }
-                const AttnTwo ds1(ds);
-                fact8(1, i, lse);
-                fact8(3, i, mean);
+                float p[8], ds[8], lse[8], mean[8], lambda[8];
                 if constexpr (SHARED) fact8(4, i, lambda);
+                fact8(half, i, lse);
+                fact8(2 + half, i, mean);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    p2[e] = (SHARED ? lambda[e] : lambda_of_all) * __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
-                    ds[e] = p2[e] * (mean[e] - dp[i * 8 + e]);
-                    p1[e] -= p2[e];
+                    p[e] = __builtin_amdgcn_exp2f(fmaf(score[0][i * 8 + e], a.to_log2, -lse[e]));
+                    if (half) p[e] *= SHARED ? lambda[e] : lambda_of_all;
+                    ds[e] = p[e] * (dp[i * 8 + e] - mean[e]);
                 }
-                const AttnTwo ds2(ds), p(p1);
+                const AttnTwo own(ds);
+                fact8(1 - half, i, lse);
+                if constexpr (kHalves == 1) fact8(3, i, mean);
 #pragma unroll
-                for (int b = 0; b < 2 * kBlocks; ++b) acc_v[b] = attn_mfma(reads.turned(from_lds, o_tile, i * 16, b), p, acc_v[b]);
+                for (int e = 0; e < 8; ++e) {
+                    float other = __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
+                    if (!half) other *= SHARED ? lambda[e] : lambda_of_all;
+                    if constexpr (kHalves == 1) ds[e] = other * (mean[e] - dp[i * 8 + e]);
+                    p[e] -= other;
+                }
+                const AttnTwo mixed(p);
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    acc_k[0][b] = attn_mfma(reads.turned(from_lds, q_tile, i * 16, b), ds1, acc_k[0][b]);
-                    acc_k[1][b] = attn_mfma(reads.turned(from_lds, q_tile, i * 16, kBlocks + b), ds2, acc_k[1][b]);
+                for (int b = 0; b < kValues; ++b) acc_v[b] = attn_mfma(reads.turned(from_lds, o_tile + half * 256, i * 16, b), mixed, acc_v[b]);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) acc_k[0][b] = attn_mfma(reads.turned(from_lds, q_own, i * 16, b), own, acc_k[0][b]);
+                if constexpr (kHalves == 1) {
+                    const AttnTwo second(ds);
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) acc_k[1][b] = attn_mfma(reads.turned(from_lds, q_tile, i * 16, kBlocks + b), second, acc_k[1][b]);
                 }
             }
         }
@@ -357,23 +375,26 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
         step(all + buffer * kBuffer, all + (buffer ^ 1) * kBuffer, values + wave * 32 * Tile::kRow, r0);
     }
     if (key_ >= seq.lk) return;
+    const float sign = half ? -1.0f : 1.0f, factor = sign * a.scale;
+    const int value0 = half * (E / kHalves);
     if (f.splits > 1) {
         const int64_t at = (((int64_t)split * a.tokens_k + seq.k0 + key) * a.kv_heads + head_k) * E;
 #pragma unroll
-        for (int b = 0; b < 2 * kBlocks; ++b) {
-            attn_store_part(f.part_v + at + b * 32, lane, acc_v[b], 1.0f);
-            attn_store_part(f.part + at + b * 32, lane, acc_k[b / kBlocks][b % kBlocks], a.scale);
-        }
+        for (int b = 0; b < kValues; ++b) attn_store_part(f.part_v + at + value0 + b * 32, lane, acc_v[b], sign);
+#pragma unroll
+        for (int m = 0; m < 2 / kHalves; ++m)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) attn_store_part(f.part + at + (m + half) * D + b * 32, lane, acc_k[m][b], factor);
         return;
     }
     uint16_t* o = f.dv + (int64_t)(seq.k0 + key) * f.lddv + (int64_t)head_k * a.e;
 #pragma unroll
-    for (int b = 0; b < 2 * kBlocks; ++b) attn_store(o, b * 32, a.e, lane, acc_v[b], 1.0f);
+    for (int b = 0; b < kValues; ++b) attn_store(o, value0 + b * 32, a.e, lane, acc_v[b], sign);
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-        o = f.dk + (int64_t)(seq.k0 + key) * f.lddk + (int64_t)(2 * head_k + m) * a.d;
+    for (int m = 0; m < 2 / kHalves; ++m) {
+        o = f.dk + (int64_t)(seq.k0 + key) * f.lddk + (int64_t)(2 * head_k + m + half) * a.d;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) attn_store(o, b * 32, a.d, lane, acc_k[m][b], a.scale);
+        for (int b = 0; b < kBlocks; ++b) attn_store(o, b * 32, a.d, lane, acc_k[m][b], factor);
     }
 }
 
@@ -471,7 +492,7 @@ void launch_dq(const AttnGradients& f, const Shape& s, hipStream_t stream)
 template <int D, int WAVES, int RT>
 void launch_dkv(const AttnGradients& f, const Shape& s, hipStream_t stream)
 {
-    const int blocks = s.slots_k * f.a.kv_heads * s.splits_k;
+    const int blocks = s.slots_k * f.a.kv_heads * s.splits_k * attn_halves(D);
     if (f.a.group.d > 1)
         k_attn_dkv<D, WAVES, RT, true><<<blocks, 64 * WAVES, 0, stream>>>(f);
     else

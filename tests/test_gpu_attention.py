@@ -193,7 +193,7 @@ LENS = {
     "one": [(1, 1)], "tiny": [(3, 5), (1, 1), (2, 2)], "edge": [(31, 31), (32, 32), (33, 33), (65, 65)], "tiles": [(257, 300), (64, 64)],
     "more_queries": [(40, 7), (300, 65)], "empty": [(0, 9), (5, 0), (0, 0), (70, 70), (8, 0)], "many": [(i % 7, (3 * i) % 11) for i in range(150)],
     "few_keys": [(700, 20), (900, 35)], "long_keys": [(33, 1500)], "long_both": [(300, 1400), (0, 3), (260, 1100)],
-    "few_rows": [(1, 700), (2, 1300), (1, 64), (1, 0), (3, 2)], "one_query": [(1, 5000)],
+    "few_rows": [(1, 700), (2, 1300), (1, 64), (1, 0), (3, 2)], "one_query": [(1, 5000)], "one_query_long": [(1, 8100)],
 }
 
 
