@@ -361,7 +361,7 @@ agc_status agc_gated_partial_gradients(const void *x_dev, int64_t ldx, const voi
  *              and keys that lie side by side in a row are one call.  out may be x, with the same stride, and not overlap it otherwise
  *   positions_dev  device, n_tokens positions of position_bytes = 4 or 8 bytes (signed)
  *   turns_dev  device, rot_dim / 2 numbers: a position's share of a whole turn in units of 2^-64
- * 0 <= n_tokens <= 2^26, heads * head_dim <= 65536, 2 <= rot_dim <= head_dim, rot_dim even. */
+ * 0 <= n_tokens <= 2^26, heads * head_dim <= 65536, 2 <= rot_dim <= head_dim and 8192, rot_dim even. */
 typedef enum { AGC_ROTARY_HALF = 0, AGC_ROTARY_INTERLEAVED = 1 } agc_rotary_layout;
 agc_status agc_rotary_apply(const void* x_dev, int type, int64_t ldx, int64_t n_tokens, int heads, int head_dim, int rot_dim,
                             const void* positions_dev, int position_bytes, const uint64_t* turns_dev, int layout,

@@ -240,7 +240,7 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
 {
     const char* const name = "agc_rotary_frequencies";
     if (!turns_out || !amplitude_out) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
-    if (rot_dim < 2 || rot_dim > kMostWidth || rot_dim % 2) return refuse(AGC_ESHAPE, std::string(name) + ": rot_dim must be even, 2..65536");
+    if (rot_dim < 2 || rot_dim > agc::kMostRotary || rot_dim % 2) return refuse(AGC_ESHAPE, std::string(name) + ": rot_dim must be even, 2..8192");
     if (scaling != AGC_ROTARY_PLAIN && scaling != AGC_ROTARY_LINEAR && scaling != AGC_ROTARY_BY_PARTS)
         return refuse(AGC_EINVAL, std::string(name) + ": unknown scaling");
     if (!(base > 1) || !std::isfinite(base) || (scaling != AGC_ROTARY_PLAIN && (!(factor >= 1) || !std::isfinite(factor))) ||
@@ -275,8 +275,8 @@ agc_status agc_rotary_apply(const void* x_dev, int type, int64_t ldx, int64_t n_
     if (!known_type(type) || (position_bytes != 4 && position_bytes != 8) || (layout != AGC_ROTARY_HALF && layout != AGC_ROTARY_INTERLEAVED))
         return refuse(AGC_EINVAL, std::string(name) + ": values are float or bfloat16, positions have 4 or 8 bytes, pairs are halves or neighbours");
     if (n_tokens < 0 || n_tokens > kMostTokens || heads < 1 || head_dim < 2 || (int64_t)heads * head_dim > kMostWidth || rot_dim < 2 ||
-        rot_dim > head_dim || rot_dim % 2)
-        return refuse(AGC_ESHAPE, std::string(name) + ": n_tokens must be 0..2^26, heads * head_dim up to 65536, rot_dim even, 2..head_dim");
+        rot_dim > head_dim || rot_dim > agc::kMostRotary || rot_dim % 2)
+        return refuse(AGC_ESHAPE, std::string(name) + ": n_tokens must be 0..2^26, heads * head_dim up to 65536, rot_dim even, 2..head_dim and 8192");
     if (ldx < (int64_t)heads * head_dim || ldo < (int64_t)heads * head_dim)
         return refuse(AGC_ESHAPE, std::string(name) + ": a row stride is smaller than the row");
     if (!turns_dev || (n_tokens > 0 && (!x_dev || !out_dev || !positions_dev))) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");

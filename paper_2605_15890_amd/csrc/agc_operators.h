@@ -79,6 +79,7 @@ hipError_t launch_embed_forward(const EmbedCall& c, hipStream_t stream);
 hipError_t launch_embed_gradients(const EmbedCall& c, hipStream_t stream);
 
 // ------------------------------------------------------------------ rotary positions
+constexpr int kMostRotary = 8192;    // values of a head that turn
 struct RotaryCall {
     const void* x;             // may be out
     void* out;

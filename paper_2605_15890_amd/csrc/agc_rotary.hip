@@ -7,7 +7,11 @@
 // by whole turns.  The angle is then brought to an eighth of a turn round the nearest quarter and enters two Taylor sums
 // (sine to the ninth power, cosine to the tenth: 2e-9 and 2e-10 at pi/4).
 //
-// Bound by memory.  A thread owns the same pairs of several heads of a token and forms their sines once.
+// Bound by memory.  A workgroup has a few tokens, forms the sines of their pairs once, in LDS, and has each thread turn up to
+// four pieces of 2 x 8 values, all of them fetched before the first is stored.  (16384 tokens of 24 heads of 64 in bfloat16: 25.5 us;
+// with the sines formed by every thread 27 us, of which the sines were most.)
+#include <algorithm>
+
 #include "agc_operators.h"
 #include "agc_vector.h"
 
@@ -17,14 +21,16 @@ namespace {
 
 constexpr int kBlock = 256;
 
+constexpr int kTable = kMostRotary / 2;   // pairs whose sines fit LDS
+
 struct Rotary {
     int64_t ldx, ldo, n;
     const void* positions;
     const uint64_t* turns;
     int wide, heads, dim, rot;
-    int units, rot_units;       // pieces of 2 x 8 values of a head; those of them that turn
-    int lanes_u, lanes_h;       // units and heads that a token's threads work on at once
+    int units, rot_units;       // pieces of a head; those of them that turn
     int tokens;                 // of a workgroup
+    int pairs;                  // whose sines are in LDS: all of a token's
     float amplitude;
     int inverse;
 };
@@ -49,66 +55,81 @@ __device__ __forceinline__ void turn(uint64_t phase, float amplitude, float& c, 
     s = amplitude * (quarter & 2 ? -b : b);
 }
 
-template <typename T, bool INTERLEAVED>
+template <typename T, bool INTERLEAVED, int PIECES>
 __global__ __launch_bounds__(kBlock) void k_rotary(Rotary a, const T* x, T* out)
 {
-    const int per = a.lanes_u * a.lanes_h;
-    const int sub = threadIdx.x / per, in = threadIdx.x - sub * per;
-    const int head0 = in / a.lanes_u, unit = blockIdx.y * a.lanes_u + in - head0 * a.lanes_u;
-    const int64_t token = (int64_t)blockIdx.x * a.tokens + sub;
-    if (sub >= a.tokens || token >= a.n || unit >= a.units) return;
+    __shared__ __attribute__((aligned(16))) float table[2][kTable];   // cosines, sines
+    const int64_t token0 = (int64_t)blockIdx.x * a.tokens;
+    const int tokens = (int)min((int64_t)a.tokens, a.n - token0), half = a.rot >> 1;
 
-    const bool turns = unit < a.rot_units;
-    const int half = a.rot >> 1;
-    // two runs of up to eight values
-    int at0, at1, count0, count1;
-    if (turns && !INTERLEAVED) {
-        at0 = unit * 8, at1 = at0 + half;
-        count0 = count1 = min(8, half - at0);
-    } else {
-        at0 = turns ? unit * 16 : a.rot + (unit - a.rot_units) * 16, at1 = at0 + 8;
-        const int end = turns ? a.rot : a.dim;
-        count0 = min(8, end - at0), count1 = max(0, min(8, end - at1));
-    }
-    float c[8], s[8];
-    if (turns) {
-        const int64_t position = a.wide ? static_cast<const int64_t*>(a.positions)[token] : static_cast<const int32_t*>(a.positions)[token];
+    // pieces are numbered by token, head and place in the head
+    struct Piece {
+        const T* from;
+        T* to;
+        int at1, count0, count1, pair;   // second run behind the first; lengths of both; place in the table, -1 of what stays
+    } piece[PIECES];
+    float v[PIECES][16];
+    const int per = a.heads * a.units;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint64_t phase = (uint64_t)position * a.turns[min(unit * 8 + i, half - 1)];
-            turn(a.inverse ? 0 - phase : phase, a.amplitude, c[i], s[i]);
+    for (int i = 0; i < PIECES; ++i) {
+        const int n = (blockIdx.y * PIECES + i) * kBlock + threadIdx.x, t = n / per, in = n - t * per, h = in / a.units, unit = in - h * a.units;
+        Piece& p = piece[i];
+        p.count0 = 0;
+        if (t >= tokens) continue;
+        const bool turns = unit < a.rot_units;
+        int at;
+        if (turns && !INTERLEAVED) {
+            at = unit * 8, p.at1 = half;
+            p.count0 = p.count1 = min(8, half - at);
+        } else {
+            at = turns ? unit * 16 : a.rot + (unit - a.rot_units) * 16, p.at1 = 8;
+            const int end = turns ? a.rot : a.dim;
+            p.count0 = min(8, end - at), p.count1 = max(0, min(8, end - at - 8));
         }
+        p.pair = turns ? t * a.pairs + unit * 8 : -1;
+        p.from = x + (token0 + t) * a.ldx + h * a.dim + at;
+        p.to = out + (token0 + t) * a.ldo + h * a.dim + at;
+        load8(p.from, p.count0, v[i]);
+        load8(p.from + p.at1, p.count1, v[i] + 8);
     }
-    const T* from = x + token * a.ldx;
-    T* to = out + token * a.ldo;
-    for (int h = head0; h < a.heads; h += a.lanes_h) {
-        float v[16];
-        load8(from + h * a.dim + at0, count0, v);
-        load8(from + h * a.dim + at1, count1, v + 8);
-        if (turns) {
+    for (int n = threadIdx.x; n < tokens * a.pairs; n += kBlock) {
+        const int t = n / a.pairs, pair = min(n - t * a.pairs, half - 1);   // places behind the last pair are read, not used
+        const int64_t position = a.wide ? static_cast<const int64_t*>(a.positions)[token0 + t] : static_cast<const int32_t*>(a.positions)[token0 + t];
+        const uint64_t phase = (uint64_t)position * a.turns[pair];
+        turn(a.inverse ? 0 - phase : phase, a.amplitude, table[0][n], table[1][n]);
+    }
+    __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float& p = INTERLEAVED ? v[2 * i] : v[i];
-                float& q = INTERLEAVED ? v[2 * i + 1] : v[8 + i];
-                const float p0 = p;
-                p = fmaf(p0, c[i], -(q * s[i]));
-                q = fmaf(p0, s[i], q * c[i]);
+    for (int i = 0; i < PIECES; ++i) {
+        const Piece& p = piece[i];
+        if (p.count0 == 0) continue;
+        if (p.pair >= 0) {
+            float c[8], s[8];
+            load8(&table[0][p.pair], 8, c);
+            load8(&table[1][p.pair], 8, s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float& p0 = INTERLEAVED ? v[i][2 * e] : v[i][e];
+                float& p1 = INTERLEAVED ? v[i][2 * e + 1] : v[i][8 + e];
+                const float was = p0;
+                p0 = fmaf(was, c[e], -(p1 * s[e]));
+                p1 = fmaf(was, s[e], p1 * c[e]);
             }
         }
-        store8(to + h * a.dim + at0, count0, v);
-        store8(to + h * a.dim + at1, count1, v + 8);
+        store8(p.to, p.count0, v[i]);
+        store8(p.to + p.at1, p.count1, v[i] + 8);
     }
 }
 
-template <typename T>
+template <typename T, int PIECES>
 void launch(const Rotary& a, const RotaryCall& c, dim3 grid, hipStream_t stream)
 {
     const T* x = static_cast<const T*>(c.x);
     T* out = static_cast<T*>(c.out);
     if (c.interleaved)
-        k_rotary<T, true><<<grid, kBlock, 0, stream>>>(a, x, out);
+        k_rotary<T, true, PIECES><<<grid, kBlock, 0, stream>>>(a, x, out);
     else
-        k_rotary<T, false><<<grid, kBlock, 0, stream>>>(a, x, out);
+        k_rotary<T, false, PIECES><<<grid, kBlock, 0, stream>>>(a, x, out);
 }
 
 }  // namespace
@@ -120,13 +141,15 @@ hipError_t launch_rotary(const RotaryCall& c, hipStream_t stream)
     a.heads = c.heads, a.dim = c.dim, a.rot = c.rot, a.amplitude = c.amplitude, a.inverse = c.inverse;
     a.rot_units = (c.rot / 2 + 7) / 8;
     a.units = a.rot_units + (c.dim - c.rot + 15) / 16;
-    a.lanes_u = a.units < kBlock ? a.units : kBlock;
-    const int most = kBlock / a.lanes_u;
-    const int rounds = (c.heads + most - 1) / most;
-    a.lanes_h = (c.heads + rounds - 1) / rounds;
-    a.tokens = kBlock / (a.lanes_u * a.lanes_h);
-    const dim3 grid((uint32_t)((c.n + a.tokens - 1) / a.tokens), (uint32_t)((a.units + a.lanes_u - 1) / a.lanes_u));
-    c.bf16 ? launch<uint16_t>(a, c, grid, stream) : launch<float>(a, c, grid, stream);
+    a.pairs = a.rot_units * 8;
+    // Many tokens: as many a workgroup as have four pieces a thread and whose sines fit.  Few: a piece a thread, more workgroups.
+    const int per = a.heads * a.units, pieces = c.n * per >= 524288 ? 4 : 1;
+    a.tokens = std::max(1, std::min(kBlock * pieces / per, kTable / a.pairs));
+    const dim3 grid((uint32_t)((c.n + a.tokens - 1) / a.tokens), (uint32_t)((a.tokens * per + kBlock * pieces - 1) / (kBlock * pieces)));
+    if (pieces == 4)
+        c.bf16 ? launch<uint16_t, 4>(a, c, grid, stream) : launch<float, 4>(a, c, grid, stream);
+    else
+        c.bf16 ? launch<uint16_t, 1>(a, c, grid, stream) : launch<float, 1>(a, c, grid, stream);
     return hipGetLastError();
 }
 

@@ -40,7 +40,7 @@ def test_table(rot, base, scaling, factor, original):
 
 
 @pytest.mark.parametrize("args,status", [
-    ((3,), api.AGC_ESHAPE), ((0,), api.AGC_ESHAPE), ((65538,), api.AGC_ESHAPE), ((8, 1.0), api.AGC_EINVAL), ((8, math.inf), api.AGC_EINVAL),
+    ((3,), api.AGC_ESHAPE), ((0,), api.AGC_ESHAPE), ((8194,), api.AGC_ESHAPE), ((8, 1.0), api.AGC_EINVAL), ((8, math.inf), api.AGC_EINVAL),
     ((8, 10.0, "log"), api.AGC_EINVAL), ((8, 10.0, "linear", 0.5), api.AGC_EINVAL), ((8, 10.0, "parts", math.nan), api.AGC_EINVAL),
     ((8, 10.0, "parts", 2.0, 0.0), api.AGC_EINVAL)])
 def test_table_refusals(args, status):
@@ -55,7 +55,7 @@ def raw(x=64, kind=0, ldx=16, n=2, heads=2, dim=8, rot=8, pos=64, width=4, turns
 
 @pytest.mark.parametrize("change,status", [
     (dict(kind=2), -1), (dict(width=2), -1), (dict(layout=2), -1), (dict(n=-1), -2), (dict(n=2 ** 26 + 1), -2), (dict(heads=0), -2),
-    (dict(heads=2 ** 14, ldx=2 ** 18, ldo=2 ** 18), -2), (dict(dim=1, rot=1), -2), (dict(rot=7), -2), (dict(rot=10), -2), (dict(rot=0), -2),
+    (dict(heads=2 ** 14, ldx=2 ** 18, ldo=2 ** 18), -2), (dict(dim=1, rot=1), -2), (dict(rot=7), -2), (dict(rot=10), -2), (dict(rot=0), -2), (dict(dim=8194, rot=8194, ldx=16388, ldo=16388), -2),
     (dict(ldx=15), -2), (dict(ldo=15), -2), (dict(x=0), -1), (dict(out=0), -1), (dict(pos=0), -1), (dict(turns=0), -1),
     (dict(x=66), -4), (dict(out=130), -4), (dict(pos=66), -4), (dict(turns=68), -4), (dict(out=64, ldo=17), -1), (dict(n=0, x=0, out=0, pos=0), 0)])
 def test_refusals(change, status):
@@ -102,7 +102,7 @@ def on_gpu(x, kind, gap, shift):
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("tokens,heads,dim,rot", [(1, 1, 2, 2), (3, 2, 16, 16), (5, 3, 17, 10), (37, 4, 64, 64), (130, 5, 81, 56), (9, 24, 128, 64),
-                                                  (2, 1, 6000, 5000), (300, 1, 3, 2), (4, 200, 20, 12)])
+                                                  (2, 1, 6000, 5000), (3, 2, 9000, 8192), (700, 40, 24, 24), (300, 1, 3, 2), (4, 200, 20, 12)])
 @pytest.mark.parametrize("gap,shift,scaling,inverse", [(0, 0, "none", False), (8, 0, "parts", True), (1, 1, "linear", False), (5, 3, "parts", False)])
 def test_rotation(kind, layout, tokens, heads, dim, rot, gap, shift, scaling, inverse):
     import torch
