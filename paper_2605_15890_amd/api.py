@@ -668,13 +668,15 @@ def agc_muon_update(beta, m1, ghat, offsets, rows, cols, lr, momentum, nesterov,
     return st
 
 
-def _on_current_gpu(what, *tensors):
-    """Refuses tensors that the kernels could not reach from the current GPU."""
+def _stream_of(what, stream, tensors):
+    """The stream's handle, the current one's if it is None; refuses tensors that the kernels could not reach from the
+    current GPU."""
     import torch
     device = torch._C._cuda_getDevice() if tensors[0].is_cuda else -2   # host memory is -1
     for t in tensors:
         if t.get_device() != device:
             raise AgcError(AGC_EINVAL, f"{what}: tensors must lie on the current GPU")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else int(stream)
 
 
 _ROTARY_LAYOUTS = {"half": AGC_ROTARY_HALF, "interleaved": AGC_ROTARY_INTERLEAVED}
@@ -705,10 +707,10 @@ def agc_rotary_apply(x, heads, positions, turns, layout, out, amplitude=1.0, inv
         raise AgcError(AGC_ESHAPE, "turns must be a contiguous vector of int64")
     row = x.shape[1]
     ldx, ldo = _rows_of(x, n, row, x.dtype, "x"), _rows_of(out, n, row, x.dtype, "out")
-    _on_current_gpu("agc_rotary_apply", x, positions, turns, out)
+    stream = _stream_of("agc_rotary_apply", stream, (x, positions, turns, out))
     st = L.agc_rotary_apply(x.data_ptr(), kind, ldx, n, heads, row // heads, 2 * turns.numel(), positions.data_ptr(), width,
                             turns.data_ptr(), _ROTARY_LAYOUTS.get(layout, layout), amplitude, int(bool(inverse)),
-                            out.data_ptr(), ldo, _stream_handle(stream))
+                            out.data_ptr(), ldo, stream)
     if check and st != AGC_OK:
         raise AgcError(st, L.agc_last_error(None).decode())
     return st
@@ -758,10 +760,11 @@ def agc_diff_attn_forward(q, k, v, heads, kv_heads, lam, q_end, k_end, scale, ca
     ldo = _rows_of(out, nq, heads * e, q.dtype, "out")
     if k_begin is not None:
         _ends(k_begin, n, "k_begin")
-    _on_current_gpu("agc_diff_attn_forward", q, k, v, lam, q_end, k_end, workspace, out, *[t for t in (lse, k_begin) if t is not None])
+    stream = _stream_of("agc_diff_attn_forward", stream,
+                        (q, k, v, lam, q_end, k_end, workspace, out, q if lse is None else lse, q if k_begin is None else k_begin))
     st = L.agc_diff_attn_forward(*head, None if k_begin is None else k_begin.data_ptr(), k_end.data_ptr(), n, scale,
                                  int(bool(causal)), out.data_ptr(), ldo, None if lse is None else lse.data_ptr(),
-                                 workspace.data_ptr(), _stream_handle(stream))
+                                 workspace.data_ptr(), stream)
     if check and st != AGC_OK:
         raise AgcError(st, L.agc_last_error(None).decode())
     return st
@@ -778,11 +781,11 @@ def agc_diff_attn_partial_gradients(q, k, v, heads, kv_heads, lam, q_end, k_end,
     lddout = _rows_of(dout, nq, heads * e, q.dtype, "dout")
     lddq, lddk, lddv = (_rows_of(g, t.shape[0], t.shape[1], q.dtype, w) for g, t, w in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
     ldg = _rows_of(G_lambda, parts, heads, torch.float32, "G_lambda")
-    _on_current_gpu(name, q, k, v, lam, q_end, k_end, workspace, lse, dout, dq, dk, dv, G_lambda)
+    stream = _stream_of(name, stream, (q, k, v, lam, q_end, k_end, workspace, lse, dout, dq, dk, dv, G_lambda))
     st = L.agc_diff_attn_partial_gradients(*head, k_end.data_ptr(), n, scale, int(bool(causal)), lse.data_ptr(), dout.data_ptr(),
                                            lddout, struct.pack(f"{parts}q", *[int(x) for x in part_end]), parts, dq.data_ptr(), lddq,
                                            dk.data_ptr(), lddk, dv.data_ptr(), lddv, G_lambda.data_ptr(), ldg,
-                                           workspace.data_ptr(), _stream_handle(stream))
+                                           workspace.data_ptr(), stream)
     if check and st != AGC_OK:
         raise AgcError(st, L.agc_last_error(None).decode())
     return st
@@ -799,10 +802,10 @@ def agc_dropout(x, p, seed, step, site, out, residual=None, stream=None, check=T
     ldx, ldo, ldr = _rows_of(x, rows, cols, x.dtype, "x"), _rows_of(out, rows, cols, out.dtype, "out"), cols
     if residual is not None:
         ldr = _rows_of(residual, rows, cols, out.dtype, "residual")
-    _on_current_gpu("agc_dropout", x, out, x if residual is None else residual)
+    stream = _stream_of("agc_dropout", stream, (x, out, x if residual is None else residual))
     st = L.agc_dropout(x.data_ptr(), x_kind, ldx, None if residual is None else residual.data_ptr(), ldr, rows, cols, p,
                        seed & 0xFFFFFFFFFFFFFFFF, step & 0xFFFFFFFFFFFFFFFF, site, out.data_ptr(), out_kind, ldo,
-                       _stream_handle(stream))
+                       stream)
     if check and st != AGC_OK:
         raise AgcError(st, L.agc_last_error(None).decode())
     return st
