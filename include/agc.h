@@ -395,7 +395,8 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
  *              map m of head h in row 2 h + m, -infinity without keys; what the gradients take
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 0) bytes, 256-byte aligned
  * scale is finite, 0 or more.  Scores, maxima, sums and out are held in binary32; the maps enter their product with v as bfloat16, out is rounded once.
- * The order of the sums is fixed.  NaN or infinity in a sequence reaches that sequence's results alone.
+ * The order of the sums is fixed.  NaN or infinity in a sequence reaches that sequence's results alone.  out and lse must not
+ * overlap what is read.
  * Row strides of q, k, v up to 2^24, 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads below 2^31, 1 <= n_seqs <= 2^20, heads a multiple of
  * kv_heads, 1 <= head_dim <= 128, 1 <= value_dim <= 256. */
 int64_t agc_diff_attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int head_dim,
@@ -413,7 +414,8 @@ agc_status agc_diff_attn_forward(const void* q_dev, int64_t ldq, const void* k_d
  *   part_end_host  host, k_parts ends of the partitions in queries, not descending, the last tokens_q
  *   dq_dev, dk_dev, dv_dev  device, as q, k and v, row strides lddq, lddk, lddv, any alignment; overwritten but for rows behind
  *              the last sequence, which are left as they were
- *   G_lambda_dev  device, where row 0 of G holds the gradients of lambda; row p lies p * ldg floats on; overwritten
+ *   G_lambda_dev  device, where row 0 of G holds the gradients of lambda; row p lies p * ldg floats on; overwritten.  No result
+ *              may overlap what is read
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 1) bytes, 256-byte aligned (enough for the forward pass too)
  * The maps and dS enter the products with 16 bits, so that results are rounded once; sums are binary32 in a fixed order.
  * 1 <= k_parts <= 256. */

@@ -70,22 +70,26 @@ __device__ __forceinline__ AttnSeq attn_sequence(const Attn& a, int s)
 }
 
 // Which sequence tile `slot` belongs to, where sequence s has the tiles from begin_s * unit / size + s on: room for its
-// ceil(length * unit / size), found without a table of them.  `end` are the sequences' ends.  Each lane looks at one end.
+// ceil(length * unit / size), found without a table of them.  `end` are the sequences' ends.
 __device__ __forceinline__ int attn_first_slot(const int32_t* end, int s, int most, uint32_t unit, uint32_t size)
 {
     const uint32_t begin = s ? (uint32_t)min(max(end[s - 1], 0), most) : 0;
     return (int)(begin * unit / size) + s;
 }
 
+// The last sequence whose first tile is not behind `slot`, each lane looking at one of 64 evenly spaced ones at a time.
 __device__ __forceinline__ int attn_find(const int32_t* end, int n_seqs, int most, uint32_t unit, uint32_t size, int slot)
 {
     const int lane = threadIdx.x & 63;
-    int count = 0;
-    for (int base = 0; base < n_seqs; base += 64) {
-        const int s = base + lane;
-        count += __popcll(__ballot(s < n_seqs && attn_first_slot(end, min(s, n_seqs - 1), most, unit, size) <= slot));
+    int first = 0;
+    for (int left = n_seqs; left > 1;) {
+        const int step = (left + 63) >> 6, s = lane * step;
+        const int before = __popcll(__ballot(s < left && attn_first_slot(end, first + min(s, left - 1), most, unit, size) <= slot));
+        const int go = max(before - 1, 0) * step;
+        first += go;
+        left = min(step, left - go);
     }
-    return max(0, min(count, n_seqs) - 1);
+    return first;
 }
 
 // Keys in sight of query t.

@@ -180,7 +180,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
         }
         return;
     }
-    // a row without keys in sight is zeros
     float by[kMaps];
 #pragma unroll
     for (int m = 0; m < kMaps; ++m) {
@@ -189,12 +188,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
             f.lse[(int64_t)(2 * head + map0 + m) * a.tokens_q + seq.q0 + t] = sum[m] == 0.0f ? -INFINITY : top[m] + __builtin_amdgcn_logf(sum[m]);
     }
     const float lambda = a.lambda[head];
+    // a row without keys in sight is zeros, whatever the values that others see
+    const auto share = [&](int m, int b, int r) { return by[m] == 0.0f ? 0.0f : acc[m][b][r] * by[m]; };
     if constexpr (kMaps == 2) {
-        by[1] *= lambda;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[0][b][r] = acc[0][b][r] * by[0] - acc[1][b][r] * by[1];
+            for (int r = 0; r < 16; ++r) acc[0][b][r] = share(0, b, r) - lambda * share(1, b, r);
     } else {
         // the second map's wave hands its sums to the first map's, which has the same rows
         static_assert(WAVES / 2 * 32 * E * 4 <= (int)sizeof(lds), "they fit where the tiles were");
@@ -204,14 +204,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) box[(b * 16 + r) * 64] = acc[0][b][r] * (by[0] * lambda);
+                for (int r = 0; r < 16; ++r) box[(b * 16 + r) * 64] = lambda * share(0, b, r);
         }
         __syncthreads();
         if (map0 == 1) return;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[0][b][r] = acc[0][b][r] * by[0] - box[(b * 16 + r) * 64];
+            for (int r = 0; r < 16; ++r) acc[0][b][r] = share(0, b, r) - box[(b * 16 + r) * 64];
     }
     if (row_ >= rows) return;
     uint16_t* o = f.out + (int64_t)(seq.q0 + t) * f.ldo + (int64_t)head * a.e;

@@ -370,6 +370,51 @@ def test_graph_and_streams():
 
 
 @pytest.mark.gpu
+def test_thousands_of_sequences():
+    """Among five thousand, most of one query and one key, each finds its own."""
+    import torch
+    rng = np.random.default_rng(3)
+    lens = [(int(rng.integers(0, 3)), int(rng.integers(0, 4))) for _ in range(5000)]
+    lens[4321], lens[70] = (90, 200), (300, 33)
+    c = Case(lens, 2, 1, 32, 64, True)
+    c.check_forward(c.forward())
+    c.check_gradients(*c.gradients([1000, c.nq]), [1000, c.nq])
+
+
+@pytest.mark.gpu
+def test_rows_beyond_four_gigabytes():
+    """Keys, values and queries whose rows lie 2 MB apart."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    want, got = [], []
+    for far in (False, True):
+        c = Case([(1, 2100), (500, 300)], 2, 1, 64, 128, True)
+        if far:
+            wide = torch.empty(2400, 1 << 20, dtype=torch.bfloat16, device="cuda")
+            k, v = wide[:, 64:192], wide[:, 4096:4224]
+            k.copy_(c.k)
+            v.copy_(c.v)
+            q = torch.empty(501, 1 << 20, dtype=torch.bfloat16, device="cuda")[:, :256]
+            q.copy_(c.q)
+            c.head = (q, k, v, *c.head[3:])
+        out = c.forward()
+        dq, dk, dv, G = c.gradients([c.nq])
+        (got if far else want).extend((out, dq, dk, dv, torch.from_numpy(G)))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_queries_without_keys_get_zeros_whatever_the_values():
+    import torch
+    for d, e in ((64, 128), (128, 256), (20, 30)):
+        c = Case([(40, 12)], 2, 1, d, e, True)
+        c.v.fill_(float("nan"))
+        out = c.forward()
+        assert not out[:28].any() and torch.isnan(out[28:].float()).all()
+
+
+@pytest.mark.gpu
 def test_no_queries_or_no_keys():
     import torch
     c = Case([(0, 50)], 2, 1, 64, 128, True)

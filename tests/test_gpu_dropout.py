@@ -185,3 +185,22 @@ def test_graph_and_many_items():
         assert torch.equal(got, want)
     keep = uniforms(40001, 65, 1, 2, 3) >= round(0.1 * 2 ** 48)
     assert np.array_equal((want != 0).cpu().numpy(), keep & (x != 0).cpu().numpy())
+
+
+@pytest.mark.gpu
+def test_more_items_than_a_launch_takes():
+    """2^26 rows of 33 groups, in place; rows at both ends and round the border of the launches."""
+    import torch
+    rows, cols = 1 << 26, 264
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB")
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").fill_(1.0)
+    api.agc_dropout(x, 0.5, 11, 12, 13, x)
+    border = (2 ** 31 - 1) // 33
+    for first in (0, border - 2, rows - 4):
+        r, c = np.arange(first, first + 4, dtype=np.uint64)[:, None], np.arange(cols, dtype=np.uint64)
+        top = philox(c // np.uint64(8) + np.uint64(13 << 16), r + np.uint64(1 << 30), 12, 11)
+        word = np.take_along_axis(top, ((c // np.uint64(2)) % np.uint64(4)).astype(np.int64)[None, :, None].repeat(4, 0), 2)[..., 0]
+        u16 = (word >> (c % np.uint64(2) * np.uint64(16))) & np.uint64(0xFFFF)
+        # 0.5 is 2^15 of the first sixteen bits and nothing below: the others never decide
+        assert np.array_equal(x[first:first + 4].float().cpu().numpy(), np.where(u16 >= 1 << 15, 2.0, 0.0))
