@@ -31,7 +31,7 @@ struct AttnGradients {
     int64_t lddq, lddk, lddv;
     int slots, splits;
     // of splits: sums of D of every (split, head, map, token), and of dq or of dk and dv of every (split, row)
-    float *part_mean, *part, *part_v;
+    float *part_mean, *part, *part_v, *part_k;
 };
 
 // A workgroup has all keys of its rows, or the keys are split and the sums over them joined: D first, which dq needs.
@@ -211,6 +211,32 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
     }
 }
 
+// ------------------------------------------------------------------ rows of G
+struct AttnParts {
+    int end[kMostParts];
+    int k;
+    float* G;
+    int64_t ldg;
+};
+
+// A workgroup adds up one partition's D_2 of one head, in binary64 and a fixed order.
+template <int THREADS>
+__device__ __forceinline__ void attn_lambda(const AttnParts& parts, const Attn& a, const float* means, int at, double* meet)
+{
+    const int h = at % a.heads, p = at / a.heads, covered = min(max(a.q_end[a.n_seqs - 1], 0), a.tokens_q);
+    const int begin = p ? parts.end[p - 1] : 0, end = min(parts.end[p], covered);
+    const float* from = means + (int64_t)(2 * h + 1) * a.tokens_q;
+    double sum = 0;
+#pragma unroll 4
+    for (int t = begin + (int)threadIdx.x; t < end; t += THREADS) sum += from[t];
+    meet[threadIdx.x] = sum;
+    for (int half = THREADS / 2; half > 0; half >>= 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < half) meet[threadIdx.x] += meet[threadIdx.x + half];
+    }
+    if (threadIdx.x == 0) parts.G[p * parts.ldg + h] = (float)-meet[0];
+}
+
 // ------------------------------------------------------------------ dk, dv: a workgroup's keys, all rows that see them
 // A tile's rows bring along lse and D of both maps and, where heads share keys, lambda.
 //
@@ -220,7 +246,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
 constexpr int attn_halves(int D) { return D == 128 ? 2 : 1; }
 
 template <int D, int WAVES, int RT, bool SHARED>
-__global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_attn_dkv(AttnGradients f)
+__global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_attn_dkv(AttnGradients f, AttnParts parts)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
@@ -232,7 +258,12 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int kHalves = attn_halves(D), kValues = 2 * kBlocks / kHalves;
-    const int id_ = xcd_order(blockIdx.x, f.slots * a.kv_heads * f.splits * kHalves), half = id_ % kHalves, id = id_ / kHalves;
+    const int tiles = f.slots * a.kv_heads * f.splits * kHalves;
+    if ((int)blockIdx.x >= tiles) {   // behind the tiles: the rows of G
+        attn_lambda<64 * WAVES>(parts, a, f.facts + f.of_facts, (int)blockIdx.x - tiles, reinterpret_cast<double*>(lds));
+        return;
+    }
+    const int id_ = xcd_order(blockIdx.x, tiles), half = id_ % kHalves, id = id_ / kHalves;
     const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
     const uint32_t group = a.group.d;
 
@@ -403,15 +434,15 @@ struct AttnSum {
     const float* part;    // (split, row, run of `up` values)
     uint16_t* to;         // (row, run of `width` values)
     int64_t ld;
-    int rows, runs, width, up;
+    int rows, runs, width, up, splits;
     const int32_t* last;  // rows behind it are left as they were
 };
 
 struct AttnSums {
-    AttnSum job[2];
+    AttnSum job[3];
 };
 
-__global__ __launch_bounds__(256) void k_attn_sum(AttnSums jobs, int splits)
+__global__ __launch_bounds__(256) void k_attn_sum(AttnSums jobs)
 {
     const AttnSum& j = jobs.job[blockIdx.y];
     const int per = j.runs * (j.up / 4);
@@ -419,33 +450,11 @@ __global__ __launch_bounds__(256) void k_attn_sum(AttnSums jobs, int splits)
     const int row = (int)(n / per), in = (int)(n - (int64_t)row * per), run = in / (j.up / 4), c = (in - run * (j.up / 4)) * 4;
     if (row >= min(max(*j.last, 0), j.rows)) return;
     tile_f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < splits; ++s) sum += reinterpret_cast<const tile_f32x4*>(j.part)[s * (int64_t)j.rows * per + n];
+    for (int s = 0; s < j.splits; ++s) sum += reinterpret_cast<const tile_f32x4*>(j.part)[s * (int64_t)j.rows * per + n];
     uint16_t* to = j.to + row * j.ld + run * j.width + c;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (c + e < j.width) to[e] = (uint16_t)bf16_bits(sum[e]);
-}
-
-// ------------------------------------------------------------------ rows of G
-struct AttnParts {
-    int end[kMostParts];
-};
-
-// A workgroup adds up one partition's D_2 of one head, in binary64 and a fixed order.
-__global__ __launch_bounds__(256) void k_attn_lambda(AttnParts parts, const float* sums, int tokens, const int32_t* q_end, int n_seqs, float* G, int64_t ldg)
-{
-    const int p = blockIdx.y, h = blockIdx.x, covered = min(max(q_end[n_seqs - 1], 0), tokens);
-    const int begin = p ? parts.end[p - 1] : 0, end = min(parts.end[p], covered);
-    const float* from = sums + (int64_t)(2 * h + 1) * tokens;
-    double sum = 0;
-    for (int t = begin + (int)threadIdx.x; t < end; t += 256) sum += from[t];
-    __shared__ double all[256];
-    all[threadIdx.x] = sum;
-    for (int half = 128; half > 0; half >>= 1) {
-        __syncthreads();
-        if ((int)threadIdx.x < half) all[threadIdx.x] += all[threadIdx.x + half];
-    }
-    if (threadIdx.x == 0) G[p * ldg + h] = (float)-all[0];
 }
 
 // Workgroups of both passes: their waves, tiles and splits.
@@ -490,50 +499,52 @@ void launch_dq(const AttnGradients& f, const Shape& s, hipStream_t stream)
 }
 
 template <int D, int WAVES, int RT>
-void launch_dkv(const AttnGradients& f, const Shape& s, hipStream_t stream)
+void launch_dkv(const AttnGradients& f, const AttnParts& parts, const Shape& s, hipStream_t stream)
 {
-    const int blocks = s.slots_k * f.a.kv_heads * s.splits_k * attn_halves(D);
+    const int blocks = s.slots_k * f.a.kv_heads * s.splits_k * attn_halves(D) + f.a.heads * parts.k;
     if (f.a.group.d > 1)
-        k_attn_dkv<D, WAVES, RT, true><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dkv<D, WAVES, RT, true><<<blocks, 64 * WAVES, 0, stream>>>(f, parts);
     else
-        k_attn_dkv<D, WAVES, RT, false><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dkv<D, WAVES, RT, false><<<blocks, 64 * WAVES, 0, stream>>>(f, parts);
 }
 
-void launch_sums(const AttnSum* job, int n, int splits, hipStream_t stream)
+void launch_sums(const AttnSum* job, int n, hipStream_t stream)
 {
+    if (n == 0) return;
     AttnSums all{};
     int64_t most = 0;
     for (int i = 0; i < n; ++i) {
         all.job[i] = job[i];
         most = std::max(most, (int64_t)job[i].rows * job[i].runs * (job[i].up / 4));
     }
-    k_attn_sum<<<dim3((uint32_t)((most + 255) / 256), n), 256, 0, stream>>>(all, splits);
+    k_attn_sum<<<dim3((uint32_t)((most + 255) / 256), n), 256, 0, stream>>>(all);
 }
 
 template <int D, int KT, int RT>
-hipError_t launch(AttnGradients f, const Shape& s, hipStream_t stream)
+hipError_t launch(AttnGradients f, const AttnParts& parts, const Shape& s, hipStream_t stream)
 {
     const Attn& a = f.a;
+    AttnSum sums[3];
+    int n = 0;
     if (a.tokens_q > 0) {
         f.slots = s.slots_q, f.splits = s.splits_q;
         if (s.waves_q == kFewWaves)
             launch_dq<D, kFewWaves, 32>(f, s, stream);
         else
             launch_dq<D, most_waves(D), KT>(f, s, stream);
-        const AttnSum dq = {f.part, f.dq, f.lddq, a.tokens_q, 2 * a.heads, a.d, D, a.q_end + a.n_seqs - 1};
-        if (s.splits_q > 1) launch_sums(&dq, 1, s.splits_q, stream);
+        if (s.splits_q > 1) sums[n++] = {f.part, f.dq, f.lddq, a.tokens_q, 2 * a.heads, a.d, D, s.splits_q, a.q_end + a.n_seqs - 1};
     }
-    if (a.tokens_k > 0) {
-        f.slots = s.slots_k, f.splits = s.splits_k;
-        f.part_v = f.part + (int64_t)s.splits_k * a.tokens_k * a.kv_heads * 2 * D;
-        if (s.waves_k == kFewWaves)
-            launch_dkv<D, kFewWaves, 32>(f, s, stream);
-        else
-            launch_dkv<D, most_waves(D), RT>(f, s, stream);
-        const AttnSum dkv[2] = {{f.part, f.dk, f.lddk, a.tokens_k, 2 * a.kv_heads, a.d, D, a.k_end + a.n_seqs - 1},
-                                {f.part_v, f.dv, f.lddv, a.tokens_k, a.kv_heads, a.e, 2 * D, a.k_end + a.n_seqs - 1}};
-        if (s.splits_k > 1) launch_sums(dkv, 2, s.splits_k, stream);
+    f.slots = s.slots_k, f.splits = s.splits_k, f.part = f.part_k;
+    f.part_v = f.part + (int64_t)s.splits_k * a.tokens_k * a.kv_heads * 2 * D;
+    if (s.waves_k == kFewWaves)
+        launch_dkv<D, kFewWaves, 32>(f, parts, s, stream);
+    else
+        launch_dkv<D, most_waves(D), RT>(f, parts, s, stream);
+    if (s.splits_k > 1 && a.tokens_k > 0) {
+        sums[n++] = {f.part, f.dk, f.lddk, a.tokens_k, 2 * a.kv_heads, a.d, D, s.splits_k, a.k_end + a.n_seqs - 1};
+        sums[n++] = {f.part_v, f.dv, f.lddv, a.tokens_k, a.kv_heads, a.e, 2 * D, s.splits_k, a.k_end + a.n_seqs - 1};
     }
+    launch_sums(sums, n, stream);
     return hipGetLastError();
 }
 
@@ -545,7 +556,7 @@ int64_t attn_gradients_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int
     const Shape s = shape_of(tokens_q, tokens_k, n_seqs, heads, kv_heads, D);
     const int64_t q = s.splits_q > 1 ? s.splits_q * tokens_q * heads * (2 * D + 2) * 4 : 0;
     const int64_t k = s.splits_k > 1 ? s.splits_k * tokens_k * kv_heads * 4 * D * 4 : 0;
-    return round_up(tokens_q * heads * 16, 256) + round_up(std::max(q, k), 256);
+    return round_up(tokens_q * heads * 16, 256) + round_up(q, 256) + round_up(k, 256);
 }
 
 hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream)
@@ -558,15 +569,16 @@ hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream)
     const Shape s = shape_of(c.tokens_q, c.tokens_k, c.n_seqs, c.heads, c.kv_heads, D);
     f.lse = c.lse, f.facts = reinterpret_cast<float*>(place), f.of_facts = (int64_t)2 * c.heads * c.tokens_q;
     f.part = reinterpret_cast<float*>(place + round_up(c.tokens_q * c.heads * 16, 256));
-    f.part_mean = f.part + (int64_t)s.splits_q * c.tokens_q * c.heads * 2 * D;
+    const int64_t of_part = (int64_t)s.splits_q * c.tokens_q * c.heads;
+    f.part_mean = f.part + of_part * 2 * D;
+    f.part_k = s.splits_q > 1 ? f.part + round_up(of_part * (2 * D + 2) * 4, 256) / 4 : f.part;
     f.dq = static_cast<uint16_t*>(c.dq), f.dk = static_cast<uint16_t*>(c.dk), f.dv = static_cast<uint16_t*>(c.dv);
     f.lddq = c.lddq, f.lddk = c.lddk, f.lddv = c.lddv;
-    e = D == 32 ? launch<32, 64, 64>(f, s, stream) : D == 64 ? launch<64, 64, 64>(f, s, stream) : launch<128, 64, 32>(f, s, stream);
-    if (e != hipSuccess) return e;
     AttnParts parts;
     for (int p = 0; p < c.k_parts; ++p) parts.end[p] = (int)c.part_end[p];
-    k_attn_lambda<<<dim3(c.heads, c.k_parts), 256, 0, stream>>>(parts, f.facts + f.of_facts, f.a.tokens_q, c.q_end, c.n_seqs, c.G, c.ldg);
-    return hipGetLastError();
+    parts.k = c.k_parts, parts.G = c.G, parts.ldg = c.ldg;
+    if (D == 32) return launch<32, 64, 64>(f, parts, s, stream);
+    return D == 64 ? launch<64, 64, 64>(f, parts, s, stream) : launch<128, 64, 32>(f, parts, s, stream);
 }
 
 }  // namespace agc
