@@ -15,6 +15,8 @@
 // eight neighbouring keys twice, which is what the next product's operand wants, and P never leaves the registers.
 #pragma once
 
+#include <algorithm>
+
 #include "agc_operators.h"
 #include "agc_vector.h"
 
@@ -90,6 +92,43 @@ __device__ __forceinline__ int attn_find(const int32_t* end, int n_seqs, int mos
         left = min(step, left - go);
     }
     return first;
+}
+
+// Workgroup id -> tile, key head, split.  Workgroups go to the eight XCDs in turn.
+//
+// Without `columns` each XCD gets a contiguous run, so that tiles of the same keys meet in its L2.  Under the causal mask a
+// sequence's first tiles have most to do, and such a run ends with some of them: with columns, an XCD has whole key heads (or a
+// share of one's tiles), every sequence's first tiles come before all second ones, and the last ones fill the gaps.  Tiles
+// count as n_seqs rows of `columns` each, which they are if the sequences are alike; if not, the order is any.
+// 8 x 2048 tokens, 16 heads: forward 281 -> 258 us, rows' pass 605 -> 535, keys' pass 612 -> 552.
+struct AttnPlace {
+    int slot, head_k, split;   // slot -1: none
+};
+
+__device__ __forceinline__ AttnPlace attn_place(const Attn& a, int id, int slots, int splits, int columns)
+{
+    if (columns == 0) {
+        if (id >= slots * a.kv_heads * splits) return {-1, 0, 0};
+        id = xcd_order(id, slots * a.kv_heads * splits);
+        const int rest = id / splits, head_k = rest / slots;
+        return {rest - head_k * slots, head_k, id - rest * splits};
+    }
+    const int x = id & 7, i = id >> 3, share = max(8 / a.kv_heads, 1), rows = max(a.kv_heads / 8, 1) * a.n_seqs;
+    const int step = i / rows, row = i - step * rows, head = row / a.n_seqs, column = step * share + x % share;
+    const int slot = (row - head * a.n_seqs) * columns + column;
+    return {column < columns && slot < slots ? slot : -1, a.kv_heads >= 8 ? x * (a.kv_heads / 8) + head : x / share, 0};
+}
+
+// Columns of a launch, and its workgroups.
+inline int attn_columns(const Attn& a, int slots, int splits)
+{
+    const bool whole = a.kv_heads % 8 == 0 || 8 % a.kv_heads == 0;
+    return a.causal && splits == 1 && whole && slots * a.kv_heads >= 512 ? (slots + a.n_seqs - 1) / a.n_seqs : 0;
+}
+inline int attn_blocks(const Attn& a, int slots, int splits)
+{
+    const int columns = attn_columns(a, slots, splits), share = std::max(8 / a.kv_heads, 1);
+    return columns ? 8 * std::max(a.kv_heads / 8, 1) * a.n_seqs * ((columns + share - 1) / share) : slots * a.kv_heads * splits;
 }
 
 // Keys in sight of query t.

@@ -13,7 +13,7 @@ struct AttnForward {
     uint16_t* out;
     int64_t ldo;
     float* lse;            // may be null
-    int slots, splits;
+    int slots, splits, columns;
     float* part;           // of splits: per (split, row) both maps' sums of 2 D values
     struct AttnStat* stat; // and their maxima and sums
 };
@@ -41,9 +41,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int map0 = kMaps == 2 ? 0 : wave & 1, rows_of = kMaps == 2 ? wave : wave >> 1;
-    const int total = f.slots * a.kv_heads * f.splits;
-    const int id = xcd_order(blockIdx.x, total);
-    const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
+    const AttnPlace place = attn_place(a, blockIdx.x, f.slots, f.splits, f.columns);
+    const int slot = place.slot, head_k = place.head_k, split = place.split;
+    if (slot < 0) return;
     const uint32_t group = a.group.d;
 
     const int s = attn_find(a.q_end, a.n_seqs, a.tokens_q, group, kRows, slot);
@@ -297,7 +297,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
 template <int D, int WAVES, int KT>
 hipError_t launch(AttnForward f, hipStream_t stream)
 {
-    k_attn_forward<D, WAVES, KT><<<f.slots * f.a.kv_heads * f.splits, 64 * WAVES, 0, stream>>>(f);
+    f.columns = attn_columns(f.a, f.slots, f.splits);
+    k_attn_forward<D, WAVES, KT><<<attn_blocks(f.a, f.slots, f.splits), 64 * WAVES, 0, stream>>>(f);
     if (f.splits > 1) {
         const int64_t all = (int64_t)f.a.tokens_q * f.a.heads;
         if (f.splits > kFewSplits)

@@ -29,7 +29,7 @@ struct AttnGradients {
     int64_t of_facts;      // values of each
     uint16_t *dq, *dk, *dv;
     int64_t lddq, lddk, lddv;
-    int slots, splits;
+    int slots, splits, columns, blocks;
     // of splits: sums of D of every (split, head, map, token), and of dq or of dk and dv of every (split, row)
     float *part_mean, *part, *part_v, *part_k;
 };
@@ -47,8 +47,9 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
     __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile];   // buffer; keys, values
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int id = xcd_order(blockIdx.x, f.slots * a.kv_heads * f.splits);
-    const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
+    const AttnPlace place = attn_place(a, blockIdx.x, f.slots, f.splits, f.columns);
+    const int slot = place.slot, head_k = place.head_k, split = place.split;
+    if (slot < 0) return;
     const uint32_t group = a.group.d;
 
     const int s = attn_find(a.q_end, a.n_seqs, a.tokens_q, group, 32 * WAVES, slot);
@@ -258,13 +259,17 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int kHalves = attn_halves(D), kValues = 2 * kBlocks / kHalves;
-    const int tiles = f.slots * a.kv_heads * f.splits * kHalves;
+    const int tiles = f.blocks * kHalves;
     if ((int)blockIdx.x >= tiles) {   // behind the tiles: the rows of G
         attn_lambda<64 * WAVES>(parts, a, f.facts + f.of_facts, (int)blockIdx.x - tiles, reinterpret_cast<double*>(lds));
         return;
     }
-    const int id_ = xcd_order(blockIdx.x, tiles), half = id_ % kHalves, id = id_ / kHalves;
-    const int split = id % f.splits, rest = id / f.splits, head_k = rest / f.slots, slot = rest - head_k * f.slots;
+    // both halves on one XCD
+    const int half = kHalves == 1 ? 0 : ((int)blockIdx.x >> 3) % kHalves;
+    const int id = kHalves == 1 ? (int)blockIdx.x : ((int)blockIdx.x >> 3) / kHalves * 8 + ((int)blockIdx.x & 7);
+    const AttnPlace place = attn_place(a, id, f.slots, f.splits, f.columns);
+    const int slot = place.slot, head_k = place.head_k, split = place.split;
+    if (slot < 0) return;
     const uint32_t group = a.group.d;
 
     const int s = attn_find(a.k_end, a.n_seqs, a.tokens_k, 1, 32 * WAVES, slot);
@@ -463,31 +468,34 @@ struct Shape {
 };
 
 constexpr int kFewWaves = 2;
-constexpr int most_waves(int D) { return D == 128 ? 4 : 8; }
+// Of large ones.  Two workgroups of four waves a compute unit serve the rows' pass better than one of eight, whose first rows
+// wait for its last ones under the causal mask (506 against 534 us at 8 x 2048 tokens of 16 heads); the keys' pass has LDS for one.
+constexpr int kRowWaves = 4;
+constexpr int key_waves(int D) { return D == 128 ? 4 : 8; }
 
 Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D)
 {
     const int64_t rows = tokens_q * (heads / kv_heads);
     // Large workgroups read the other side least often; where they would leave compute units without work, small ones, and
     // where those are too few, the other side split among several.
-    const auto side = [&](int64_t own, int64_t other, int& waves, int& slots, int& splits) {
-        const int64_t large = 32 * most_waves(D);
+    const auto side = [&](int64_t own, int64_t other, int most, int& waves, int& slots, int& splits) {
+        const int64_t large = 32 * most;
         const bool enough = own / n_seqs >= large && own / large * kv_heads >= 192;
-        waves = enough ? most_waves(D) : kFewWaves;
+        waves = enough ? most : kFewWaves;
         slots = (int)(own / (32 * waves)) + n_seqs;
         const int64_t blocks = std::max<int64_t>(own / (32 * waves), n_seqs) * kv_heads;
         splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({640 / blocks, other / n_seqs / 256, (int64_t)16}));
     };
     Shape o;
-    side(rows, tokens_k, o.waves_q, o.slots_q, o.splits_q);
-    side(tokens_k, rows, o.waves_k, o.slots_k, o.splits_k);
+    side(rows, tokens_k, kRowWaves, o.waves_q, o.slots_q, o.splits_q);
+    side(tokens_k, rows, key_waves(D), o.waves_k, o.slots_k, o.splits_k);
     return o;
 }
 
 template <int D, int WAVES, int KT>
 void launch_dq(const AttnGradients& f, const Shape& s, hipStream_t stream)
 {
-    const int blocks = s.slots_q * f.a.kv_heads * s.splits_q;
+    const int blocks = attn_blocks(f.a, f.slots, f.splits);
     if (s.splits_q == 1) {
         k_attn_dq<D, WAVES, KT, kAll><<<blocks, 64 * WAVES, 0, stream>>>(f);
         return;
@@ -501,7 +509,7 @@ void launch_dq(const AttnGradients& f, const Shape& s, hipStream_t stream)
 template <int D, int WAVES, int RT>
 void launch_dkv(const AttnGradients& f, const AttnParts& parts, const Shape& s, hipStream_t stream)
 {
-    const int blocks = s.slots_k * f.a.kv_heads * s.splits_k * attn_halves(D) + f.a.heads * parts.k;
+    const int blocks = f.blocks * attn_halves(D) + f.a.heads * parts.k;
     if (f.a.group.d > 1)
         k_attn_dkv<D, WAVES, RT, true><<<blocks, 64 * WAVES, 0, stream>>>(f, parts);
     else
@@ -527,19 +535,20 @@ hipError_t launch(AttnGradients f, const AttnParts& parts, const Shape& s, hipSt
     AttnSum sums[3];
     int n = 0;
     if (a.tokens_q > 0) {
-        f.slots = s.slots_q, f.splits = s.splits_q;
+        f.slots = s.slots_q, f.splits = s.splits_q, f.columns = attn_columns(a, f.slots, f.splits);
         if (s.waves_q == kFewWaves)
             launch_dq<D, kFewWaves, 32>(f, s, stream);
         else
-            launch_dq<D, most_waves(D), KT>(f, s, stream);
+            launch_dq<D, kRowWaves, KT>(f, s, stream);
         if (s.splits_q > 1) sums[n++] = {f.part, f.dq, f.lddq, a.tokens_q, 2 * a.heads, a.d, D, s.splits_q, a.q_end + a.n_seqs - 1};
     }
-    f.slots = s.slots_k, f.splits = s.splits_k, f.part = f.part_k;
+    f.slots = s.slots_k, f.splits = s.splits_k, f.columns = attn_columns(a, f.slots, f.splits), f.part = f.part_k;
+    f.blocks = (int)round_up(attn_blocks(a, f.slots, f.splits), 8);   // the halves of eight workgroups follow each other
     f.part_v = f.part + (int64_t)s.splits_k * a.tokens_k * a.kv_heads * 2 * D;
     if (s.waves_k == kFewWaves)
         launch_dkv<D, kFewWaves, 32>(f, parts, s, stream);
     else
-        launch_dkv<D, most_waves(D), RT>(f, parts, s, stream);
+        launch_dkv<D, key_waves(D), RT>(f, parts, s, stream);
     if (s.splits_k > 1 && a.tokens_k > 0) {
         sums[n++] = {f.part, f.dk, f.lddk, a.tokens_k, 2 * a.kv_heads, a.d, D, s.splits_k, a.k_end + a.n_seqs - 1};
         sums[n++] = {f.part_v, f.dv, f.lddv, a.tokens_k, a.kv_heads, a.e, 2 * D, s.splits_k, a.k_end + a.n_seqs - 1};
