@@ -187,18 +187,6 @@ struct AttnTile {
             }
         }
     }
-
-    // Rows whose address is `at(row)`.
-    template <int ROWS, int WAVES, typename At>
-    static __device__ __forceinline__ void gather(AttnLds lds, int wave, int lane, const At& at)
-    {
-        constexpr int kPer = 64 / kChunks;
-#pragma unroll
-        for (int i = 0; i < ROWS / kPer / WAVES; ++i) {
-            const int c = i * WAVES + wave, row = c * kPer + lane / kChunks;
-            attn_load16(at(row) + ((lane % kChunks) ^ mix(row)) * 16, lds + c * 1024);
-        }
-    }
 };
 
 // A lane's places in a tile for both kinds of reads.  A chunk's permutation is an exclusive or, so one place gives all of them.

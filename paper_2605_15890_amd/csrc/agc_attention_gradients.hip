@@ -239,20 +239,20 @@ __device__ __forceinline__ void attn_lambda(const AttnParts& parts, const Attn& 
 }
 
 // ------------------------------------------------------------------ dk, dv: a workgroup's keys, all rows that see them
-// A tile's rows bring along lse and D of both maps and, where heads share keys, lambda.
+// Rows are the queries of one head after the other here.  They bring along lse and D of both maps.
 //
 // Wide heads are worked on by two workgroups, since dk and dv of 32 keys would take a wave's registers twice over: each forms
 // both maps and dP, and has dk of one map (its own) and half of dv.  A third more products than one workgroup would need, in a
 // half of the time that it takes when registers leave for memory (8 x 2048 tokens, 8 heads of 128: 1016 instead of 2544 us).
 constexpr int attn_halves(int D) { return D == 128 ? 2 : 1; }
 
-template <int D, int WAVES, int RT, bool SHARED>
+template <int D, int WAVES, int RT>
 __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_attn_dkv(AttnGradients f, AttnParts parts)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
     // of a buffer: queries, dout, facts
-    constexpr int kTile = RT * Tile::kRow, kFacts = SHARED ? 5 : 4, kBuffer = 2 * kTile + (kFacts * RT * 4 + 255) / 256 * 256;
+    constexpr int kTile = RT * Tile::kRow, kBuffer = 2 * kTile + 4 * RT * 4;
     // one array: with several, what the compiler is told of the tiles' memory is lost to what it knows of the arrays
     __shared__ __attribute__((aligned(1024))) char lds[2 * kBuffer + 32 * WAVES * Tile::kRow];   // two buffers, the keys' values
     const AttnLds all = (AttnLds)&lds[0], values = all + 2 * kBuffer;
@@ -278,11 +278,10 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
     if (tile * 32 * WAVES >= seq.lk) return;
 
     const int key0 = tile * 32 * WAVES + wave * 32, key_ = key0 + attn_swapped(lane & 31), key = min(key_, seq.lk - 1);
-    const int rows = seq.lq * (int)group;
-    // under the causal mask the first query that sees this tile's first key
-    const int seeing = a.causal ? min(max(tile * 32 * WAVES + seq.lq - seq.lk, 0), seq.lq) * (int)group : 0;
-    const int run = (rows - seeing + f.splits * RT - 1) / (f.splits * RT) * RT;
-    const int begin = min(seeing + split * run, rows), end = min(begin + run, rows);
+    // Tiles of the queries that see this tile's first key, head after head of the group; a split has a run of them.
+    const int seeing = (a.causal ? min(max(tile * 32 * WAVES + seq.lq - seq.lk, 0), seq.lq) : 0) / RT * RT;
+    const int of_head = (seq.lq - seeing + RT - 1) / RT, run = (of_head * (int)group + f.splits - 1) / f.splits;
+    const int begin = min(split * run, of_head * (int)group), end = min(begin + run, of_head * (int)group);
 
     // the keys stay in registers, the values in LDS, as far as the waves' registers go
     tile_bf16x8 k[2][kSteps];   // of the own map, of the other one
@@ -296,25 +295,24 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
         Tile::template load<32 * WAVES, WAVES>(values, wave, lane, values_at + (int64_t)(tile * 32 * WAVES) * a.ldv * 2, (uint32_t)a.ldv * 2,
                                                seq.lk - tile * 32 * WAVES);
     }
-    const char* const queries_at = reinterpret_cast<const char*>(a.q + (int64_t)seq.q0 * a.ldq + (int64_t)head_k * group * E);
-    const char* const douts_at = reinterpret_cast<const char*>(f.dout + (int64_t)seq.q0 * f.lddout + (int64_t)head_k * group * E);
-    const auto fetch = [&](AttnLds to, int r0) {
-        if constexpr (SHARED) {
-            const auto place = [&](const char* at, int64_t ld, int r) {
-                const int row = min(r0 + r, rows - 1), t = (int)a.group(row);
-                return at + (t * ld + (int64_t)(row - t * (int)group) * E) * 2;
-            };
-            Tile::template gather<RT, WAVES>(to, wave, lane, [&](int r) { return place(queries_at, a.ldq, r); });
-            Tile::template gather<RT, WAVES>(to + kTile, wave, lane, [&](int r) { return place(douts_at, f.lddout, r); });
-        } else {
-            Tile::template load<RT, WAVES>(to, wave, lane, queries_at + (int64_t)r0 * a.ldq * 2, (uint32_t)a.ldq * 2, rows - r0);
-            Tile::template load<RT, WAVES>(to + kTile, wave, lane, douts_at + (int64_t)r0 * f.lddout * 2, (uint32_t)f.lddout * 2, rows - r0);
-        }
+    // a tile's head of the group and first query, which grow without a division
+    struct Rows {
+        int head, t0;
+    };
+    const auto after = [&](Rows r) {
+        r.t0 += RT;
+        return r.t0 < seq.lq ? r : Rows{r.head + 1, seeing};
+    };
+    const auto fetch = [&](AttnLds to, Rows r) {
+        const int head = r.head, t0 = r.t0, rows = seq.lq - t0;
+        Tile::template load<RT, WAVES>(to, wave, lane, reinterpret_cast<const char*>(a.q + (int64_t)(seq.q0 + t0) * a.ldq + (int64_t)head * E),
+                                       (uint32_t)a.ldq * 2, rows);
+        Tile::template load<RT, WAVES>(to + kTile, wave, lane, reinterpret_cast<const char*>(f.dout + (int64_t)(seq.q0 + t0) * f.lddout + (int64_t)head * E),
+                                       (uint32_t)f.lddout * 2, rows);
         // a wave a fact, a lane a row
-        for (int n = wave; n < kFacts; n += WAVES) {
-            const int row = min(r0 + lane, rows - 1), t = SHARED ? (int)a.group(row) : row, head = head_k * (int)group + (SHARED ? row - t * (int)group : 0);
-            const float* at = n == 4 ? a.lambda + head : f.facts + (n >> 1) * f.of_facts + (int64_t)(2 * head + (n & 1)) * a.tokens_q + seq.q0 + t;
-            if (lane < RT) attn_load4(at, to + 2 * kTile + n * RT * 4);
+        for (int w = wave; w < 4; w += WAVES) {
+            const float* at = f.facts + (w >> 1) * f.of_facts + (int64_t)(2 * head + (w & 1)) * a.tokens_q + seq.q0 + t0;
+            if (lane < RT) attn_load4(at + min(lane, rows - 1), to + 2 * kTile + w * RT * 4);
         }
     };
     attn_f32x16 acc_k[2 / kHalves][kBlocks], acc_v[kValues];
@@ -324,20 +322,20 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
         for (int b = 0; b < kBlocks; ++b) acc_k[m][b] = acc_v[m * kBlocks + b] = attn_f32x16{};
 
     const AttnReads<D> reads(lane);
-    const float lambda_of_all = a.lambda[head_k * group];   // where every key head has one query head
-    const auto step = [&](AttnLds from_lds, AttnLds to_lds, AttnLds v_lds, int r0) {
-        if (r0 + RT < end) fetch(to_lds, r0 + RT);
+    const auto step = [&](AttnLds from_lds, AttnLds to_lds, AttnLds v_lds, Rows rows, bool more) {
+        if (more) fetch(to_lds, after(rows));
+        const int t0 = rows.t0;
+        const float lambda = a.lambda[rows.head];
         uint32_t q_tile = 0;
 #pragma unroll 1
-        for (int r_first = r0; r_first < min(r0 + RT, end); r_first += 32, q_tile += 32 * Tile::kRow) {
+        for (int t_first = t0; t_first < min(t0 + RT, seq.lq); t_first += 32, q_tile += 32 * Tile::kRow) {
             // halves of wide rows lie 256 bytes apart, whole turns of the permutation
             static_assert(kHalves == 1 || D == 128, "2 D bytes are 256");
             const uint32_t o_tile = q_tile + kTile, q_own = q_tile + half * 256;
-            const int r_last = r_first + 31, sub = r_first - r0;
-            // keys in sight grow with the row
-            const int seen_first = attn_seen(a, seq, (int)a.group(r_first)), seen_last = attn_seen(a, seq, (int)a.group(min(r_last, rows - 1)));
-            if (seen_last <= key0) continue;
-            const bool masked = seen_first < max(key0 + 32, 2) || r_last >= rows;
+            const int t_last = t_first + 31, sub = t_first - t0;
+            // keys in sight grow with the query
+            if (attn_seen(a, seq, min(t_last, seq.lq - 1)) <= key0) continue;
+            const bool masked = attn_seen(a, seq, t_first) < max(key0 + 32, 2) || t_last >= seq.lq;
             // eight rows' facts: rows 16 i + 8 (lane / 32) + 0 .. 7
             typedef __attribute__((address_space(3))) const tile_f32x4* Facts;
             const AttnLds fact = from_lds + 2 * kTile + (sub + 8 * (lane >> 5)) * 4;
@@ -360,7 +358,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
             if (masked) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int row = r_first + attn_row_swapped(r, lane), seen = row < rows ? attn_seen(a, seq, (int)a.group(row)) : 0;
+                    const int t = t_first + attn_row_swapped(r, lane), seen = t < seq.lq ? attn_seen(a, seq, t) : 0;
                     const bool in = key_ < seen;
                     dp[r] = in ? dp[r] : 0.0f;
 #pragma unroll
@@ -369,14 +367,13 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float p[8], ds[8], lse[8], mean[8], lambda[8];
-                if constexpr (SHARED) fact8(4, i, lambda);
+                float p[8], ds[8], lse[8], mean[8];
                 fact8(half, i, lse);
                 fact8(2 + half, i, mean);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     p[e] = __builtin_amdgcn_exp2f(fmaf(score[0][i * 8 + e], a.to_log2, -lse[e]));
-                    if (half) p[e] *= SHARED ? lambda[e] : lambda_of_all;
+                    if (half) p[e] *= lambda;
                     ds[e] = p[e] * (dp[i * 8 + e] - mean[e]);
                 }
                 const AttnTwo own(ds);
@@ -385,7 +382,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     float other = __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
-                    if (!half) other *= SHARED ? lambda[e] : lambda_of_all;
+                    if (!half) other *= lambda;
                     if constexpr (kHalves == 1) ds[e] = other * (mean[e] - dp[i * 8 + e]);
                     p[e] -= other;
                 }
@@ -402,13 +399,17 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
             }
         }
     };
-    if (begin < end) fetch(all, begin);
     int buffer = 0;
+    if (begin < end) {
+        const int g = begin / of_head;
+        Rows rows = {head_k * (int)group + g, seeing + (begin - g * of_head) * RT};
+        fetch(all, rows);
 #pragma unroll 1
-    for (int r0 = begin; r0 < end; r0 += RT, buffer ^= 1) {
-        attn_wait_loads();
-        __syncthreads();
-        step(all + buffer * kBuffer, all + (buffer ^ 1) * kBuffer, values + wave * 32 * Tile::kRow, r0);
+        for (int n = begin; n < end; ++n, buffer ^= 1, rows = after(rows)) {
+            attn_wait_loads();
+            __syncthreads();
+            step(all + buffer * kBuffer, all + (buffer ^ 1) * kBuffer, values + wave * 32 * Tile::kRow, rows, n + 1 < end);
+        }
     }
     if (key_ >= seq.lk) return;
     const float sign = half ? -1.0f : 1.0f, factor = sign * a.scale;
@@ -473,7 +474,7 @@ constexpr int kFewWaves = 2;
 constexpr int kRowWaves = 4;
 constexpr int key_waves(int D) { return D == 128 ? 4 : 8; }
 
-Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D)
+Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D, bool causal)
 {
     const int64_t rows = tokens_q * (heads / kv_heads);
     // Large workgroups read the other side least often; where they would leave compute units without work, small ones, and
@@ -489,6 +490,9 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
     Shape o;
     side(rows, tokens_k, kRowWaves, o.waves_q, o.slots_q, o.splits_q);
     side(tokens_k, rows, key_waves(D), o.waves_k, o.slots_k, o.splits_k);
+    // A large workgroup with a sequence's first keys has twice the mean to do under the causal mask: where there is about one a
+    // compute unit, two halves each (8 x 2048 tokens, 4 heads that 16 share: 712 with their join against 789 us).
+    if (causal && o.waves_k > kFewWaves && tokens_k / (32 * o.waves_k) * kv_heads < 400) o.splits_k = 2;
     return o;
 }
 
@@ -510,10 +514,7 @@ template <int D, int WAVES, int RT>
 void launch_dkv(const AttnGradients& f, const AttnParts& parts, const Shape& s, hipStream_t stream)
 {
     const int blocks = f.blocks * attn_halves(D) + f.a.heads * parts.k;
-    if (f.a.group.d > 1)
-        k_attn_dkv<D, WAVES, RT, true><<<blocks, 64 * WAVES, 0, stream>>>(f, parts);
-    else
-        k_attn_dkv<D, WAVES, RT, false><<<blocks, 64 * WAVES, 0, stream>>>(f, parts);
+    k_attn_dkv<D, WAVES, RT><<<blocks, 64 * WAVES, 0, stream>>>(f, parts);
 }
 
 void launch_sums(const AttnSum* job, int n, hipStream_t stream)
@@ -562,7 +563,7 @@ hipError_t launch(AttnGradients f, const AttnParts& parts, const Shape& s, hipSt
 // lse and D of every row, and what splits leave: of D and dq, then of dk and dv
 int64_t attn_gradients_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D)
 {
-    const Shape s = shape_of(tokens_q, tokens_k, n_seqs, heads, kv_heads, D);
+    const Shape s = shape_of(tokens_q, tokens_k, n_seqs, heads, kv_heads, D, true);   // which splits most
     const int64_t q = s.splits_q > 1 ? s.splits_q * tokens_q * heads * (2 * D + 2) * 4 : 0;
     const int64_t k = s.splits_k > 1 ? s.splits_k * tokens_k * kv_heads * 4 * D * 4 : 0;
     return round_up(tokens_q * heads * 16, 256) + round_up(q, 256) + round_up(k, 256);
@@ -575,7 +576,7 @@ hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream)
     hipError_t e = attn_lay_out(c, f.a, f.dout, f.lddout, place, stream);
     if (e != hipSuccess) return e;
     const int D = attn_width(c.d, c.e);
-    const Shape s = shape_of(c.tokens_q, c.tokens_k, c.n_seqs, c.heads, c.kv_heads, D);
+    const Shape s = shape_of(c.tokens_q, c.tokens_k, c.n_seqs, c.heads, c.kv_heads, D, c.causal != 0);
     f.lse = c.lse, f.facts = reinterpret_cast<float*>(place), f.of_facts = (int64_t)2 * c.heads * c.tokens_q;
     f.part = reinterpret_cast<float*>(place + round_up(c.tokens_q * c.heads * 16, 256));
     const int64_t of_part = (int64_t)s.splits_q * c.tokens_q * c.heads;

@@ -382,6 +382,40 @@ def test_thousands_of_sequences():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lens,heads,kv_heads,d,e", [([(1100, 1100)] * 12, 8, 8, 32, 64), ([(300, 300), (5000, 5000), (0, 0), (700, 700)], 4, 4, 64, 128),
+                                                     ([(2000, 2000)] * 2, 32, 16, 64, 128), ([(2100, 2100)] * 3, 3, 3, 64, 128), ([(1500, 1500)] * 4, 8, 8, 128, 256)])
+def test_large_workgroups(lens, heads, kv_heads, d, e):
+    """Sizes that take the large workgroups and both orders of tiles, against sequence after sequence by itself, which takes
+    small ones: the same formulas with sums cut in other places.  Two results, each off by its own rounding and, out, by
+    those of its maps: 2^-8 sqrt(2) of a value in the root mean square at most, half a step being the largest."""
+    import torch
+    c = Case(lens, heads, kv_heads, d, e, True)
+    out = c.forward()[:, :heads * e]
+    parts = [c.nq // 3, c.nq]
+    dq, dk, dv, G = c.gradients(parts)
+    total = np.zeros(heads)
+    i = j = 0
+    for lq, lk in lens:
+        if lq == 0:
+            continue
+        one = (c.q[i:i + lq], c.k[j:j + lk], c.v[j:j + lk], heads, kv_heads, c.lam, torch.tensor([lq], dtype=torch.int32, device="cuda"),
+               torch.tensor([lk], dtype=torch.int32, device="cuda"), c.scale, True)
+        ws = torch.empty(api.agc_diff_attn_workspace_bytes(lq, lk, 1, heads, kv_heads, d, e, True), dtype=torch.uint8, device="cuda")
+        alone, lse = torch.empty_like(out[i:i + lq]), torch.empty(2 * heads, lq, device="cuda")
+        api.agc_diff_attn_forward(*one, alone, ws, lse=lse)
+        grads = [torch.empty_like(t) for t in one[:3]]
+        g = torch.empty(1, heads, device="cuda")
+        api.agc_diff_attn_partial_gradients(*one, lse, c.dout[i:i + lq], [lq], *grads, g, ws)
+        for got, want in ((out[i:i + lq], alone), (dq[i:i + lq], grads[0]), (dk[j:j + lk], grads[1]), (dv[j:j + lk], grads[2])):
+            assert float((got.double() - want.double()).norm() / want.double().norm()) < HALF * 2 ** 0.5
+        assert float((c.lse[:, i:i + lq] - lse).abs().max()) < 2.0 ** -16
+        total += g[0].double().cpu().numpy()
+        i, j = i + lq, j + lk
+    # binary32 sums of the same terms
+    assert np.all(np.abs(G.sum(0) - total) <= 1e-5 * np.abs(G).sum(0).max())
+
+
+@pytest.mark.gpu
 def test_rows_beyond_four_gigabytes():
     """Keys, values and queries whose rows lie 2 MB apart."""
     import torch
