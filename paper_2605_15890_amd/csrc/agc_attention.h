@@ -24,22 +24,8 @@ namespace agc {
 
 typedef float attn_f32x16 __attribute__((ext_vector_type(16)));
 typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
-typedef short attn_s16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.44269504088896f;
-
-// Division of row numbers by the heads of a group: n / d = n * magic >> shift for n < 2^31.
-struct Divider {
-    uint32_t d, magic, shift;
-    explicit Divider(uint32_t by) : d(by)
-    {
-        int bits = 0;
-        while ((1u << bits) < by) ++bits;
-        shift = 31 + bits;
-        magic = (uint32_t)(((uint64_t)1 << shift) / by + ((by & (by - 1)) != 0));
-    }
-    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (uint32_t)(((uint64_t)n * magic) >> shift); }
-};
 
 // What the kernels know of a call; operands as laid out: heads of D and 2 D values, 16-byte aligned rows.
 struct Attn {
@@ -49,7 +35,7 @@ struct Attn {
     const int32_t *q_end, *k_begin, *k_end;
     int n_seqs, tokens_q, tokens_k;
     int heads, kv_heads, d, e;
-    Divider group;
+    Divider group;        // heads that share keys, and the division of row numbers by them
     int causal;
     float scale;          // of the scores
     float to_log2;        // scale * log2(e): the maps are formed with powers of two
@@ -142,9 +128,6 @@ __device__ __forceinline__ int attn_swapped(int i) { return (i & 0x13) | (i & 4)
 
 typedef __attribute__((address_space(3))) char* AttnLds;
 
-// Tiles are filled while others are read.  The compiler cannot tell the two apart and would wait for the loads before the first
-// read: a step over a tile takes the memory that it reads and the memory that it fills as two __restrict__ arguments.
-
 __device__ __forceinline__ void attn_load16(const char* src, AttnLds dst)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
@@ -190,7 +173,6 @@ struct AttnTile {
 };
 
 // A lane's places in a tile for both kinds of reads.  A chunk's permutation is an exclusive or, so one place gives all of them.
-
 template <int D>
 struct AttnReads {
     using Tile = AttnTile<D>;

@@ -1,9 +1,23 @@
-// Eight consecutive values of a row, binary32 or bfloat16, as floats: what the element-wise operators move at a time.
+// Eight consecutive values of a row, binary32 or bfloat16, as floats: what the element-wise operators move at a time; and a
+// division for their indexes.
 #pragma once
 
 #include "agc_tile.h"
 
 namespace agc {
+
+// Division by a number that the host knows: n / d = n * magic >> shift for n < 2^31, with a magic of 32 bits.
+struct Divider {
+    uint32_t d, magic, shift;
+    explicit Divider(uint32_t by) : d(by)
+    {
+        int bits = 0;
+        while ((1u << bits) < by) ++bits;
+        shift = 31 + bits;
+        magic = (uint32_t)(((uint64_t)1 << shift) / by + ((by & (by - 1)) != 0));
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (uint32_t)(((uint64_t)n * magic) >> shift); }
+};
 
 // 16 bytes from and to any address: the memory path takes unaligned vectors (a row of odd width begins anywhere), an aligned
 // one costs nothing extra.
