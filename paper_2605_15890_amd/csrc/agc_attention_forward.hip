@@ -38,17 +38,20 @@ constexpr int attn_maps_of_a_wave(int D) { return D == 128 ? 1 : 2; }
 // Once a row's largest score has grown by more than this many powers of two, what is summed so far is scaled down to it.
 constexpr float kGrowth = 8.0f;
 
-template <int D, int WAVES, int KT>
+// SHARE waves have the same rows, and every SHAREth 32 keys of them each.
+template <int D, int WAVES, int KT, int SHARE>
 __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1 : 2) void k_attn_forward(AttnForward f)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = E / 32;
-    constexpr int kMaps = attn_maps_of_a_wave(D), kRows = 32 * WAVES * kMaps / 2;
+    constexpr int kMaps = attn_maps_of_a_wave(D), kRows = 32 * WAVES * kMaps / 2 / SHARE;
     constexpr int kTile = KT * Tile::kRow;
     __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile];   // buffer; keys, values
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int map0 = kMaps == 2 ? 0 : wave & 1, rows_of = kMaps == 2 ? wave : wave >> 1;
+    const int map0 = kMaps == 2 ? 0 : wave & 1, rows_of = (kMaps == 2 ? wave : wave >> 1) / SHARE;
+    const int turn = SHARE == 1 ? 0 : wave % SHARE;
+    static_assert(SHARE == 1 || (SHARE == 2 && kMaps == 2), "a pair of waves for both maps");
     const AttnPlace place = attn_place(a, blockIdx.x, f.slots, f.splits, f.columns);
     const int slot = place.slot, head_k = place.head_k, split = place.split;
     if (slot < 0) return;
@@ -101,9 +104,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
     // __restrict__: the tile that is filled is another than the one that is read, else the first read would wait for the loads
     const auto step = [&](AttnLds __restrict__ from_lds, AttnLds __restrict__ to_lds, int j0) {
         if (j0 + KT < end) fetch(to_lds, j0 + KT);
-        uint32_t k_tile = 0;
+        uint32_t k_tile = turn * 32 * Tile::kRow;
 #pragma unroll 1
-        for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow) {
+        for (int j = j0 + turn * 32; j < min(j0 + KT, seen_most); j += 32 * SHARE, k_tile += 32 * SHARE * Tile::kRow) {
             const uint32_t v_tile = k_tile + kTile;
             attn_f32x16 score[kMaps] = {};
             const auto read_k = [&](int n) { return reads.straight(from_lds, k_tile, n % kMaps * kSteps + n / kMaps); };
@@ -174,6 +177,36 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
         step(all + buffer * (2 * kTile), all + (buffer ^ 1) * (2 * kTile), j0);
     }
 
+    if constexpr (SHARE == 2) {
+        // the second wave hands its sums to the first, where the tiles were
+        __shared__ float stats[WAVES / 2][2][2][64];
+        static_assert(WAVES / 2 * 2 * kBlocks * 16 * 64 * 4 <= (int)sizeof(lds), "they fit");
+        float* box = reinterpret_cast<float*>(lds) + rows_of * (2 * kBlocks * 16 * 64) + lane;
+        __syncthreads();
+        if (turn == 1) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                stats[rows_of][m][0][lane] = top[m], stats[rows_of][m][1][lane] = sum[m];
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) box[((m * kBlocks + b) * 16 + r) * 64] = acc[m][b][r];
+            }
+        }
+        __syncthreads();
+        if (turn == 1) return;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const float top2 = stats[rows_of][m][0][lane], now = fmaxf(top[m], top2);
+            const float own = top[m] == now ? 1.0f : __builtin_amdgcn_exp2f(top[m] - now), by = top2 == now ? 1.0f : __builtin_amdgcn_exp2f(top2 - now);
+            top[m] = now;
+            sum[m] = fmaf(stats[rows_of][m][1][lane], by, sum[m] * own);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[m][b][r] = fmaf(box[((m * kBlocks + b) * 16 + r) * 64], by, acc[m][b][r] * own);
+        }
+    }
 #pragma unroll
     for (int m = 0; m < kMaps; ++m) sum[m] += attn_other_half(sum[m]);
     if (f.splits > 1) {
@@ -303,11 +336,11 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
         if (in * 4 + i < a.e) o[in * 4 + i] = (uint16_t)bf16_bits(v[i]);
 }
 
-template <int D, int WAVES, int KT>
+template <int D, int WAVES, int KT, int SHARE>
 hipError_t launch(AttnForward f, hipStream_t stream)
 {
     f.columns = attn_columns(f.a, f.slots, f.splits);
-    k_attn_forward<D, WAVES, KT><<<attn_blocks(f.a, f.slots, f.splits), 64 * WAVES, 0, stream>>>(f);
+    k_attn_forward<D, WAVES, KT, SHARE><<<attn_blocks(f.a, f.slots, f.splits), 64 * WAVES, 0, stream>>>(f);
     if (f.splits > 1) {
         const int64_t all = (int64_t)f.a.tokens_q * f.a.heads;
         if (f.splits > kFewSplits)
@@ -436,9 +469,9 @@ hipError_t launch_attn_forward(const AttnCall& c, hipStream_t stream)
     f.out = static_cast<uint16_t*>(c.out), f.ldo = c.ldo, f.lse = c.lse, f.slots = s.slots, f.splits = s.splits;
     f.stat = reinterpret_cast<AttnStat*>(place);
     f.part = reinterpret_cast<float*>(place + (int64_t)s.splits * c.tokens_q * c.heads * 16);
-    if (D == 32) return s.waves == 8 ? launch<32, 8, 64>(f, stream) : s.waves == 2 ? launch<32, 2, 32>(f, stream) : launch<32, 1, 64>(f, stream);
-    if (D == 64) return s.waves == 8 ? launch<64, 8, 64>(f, stream) : s.waves == 2 ? launch<64, 2, 32>(f, stream) : launch<64, 1, 32>(f, stream);
-    return s.waves == 8 ? launch<128, 8, 64>(f, stream) : s.waves == 4 ? launch<128, 4, 32>(f, stream) : launch<128, 2, 32>(f, stream);
+    if (D == 32) return s.waves == 8 ? launch<32, 8, 64, 1>(f, stream) : s.waves == 2 ? launch<32, 4, 64, 2>(f, stream) : launch<32, 1, 64, 1>(f, stream);
+    if (D == 64) return s.waves == 8 ? launch<64, 8, 64, 1>(f, stream) : s.waves == 2 ? launch<64, 4, 64, 2>(f, stream) : launch<64, 1, 32, 1>(f, stream);
+    return s.waves == 8 ? launch<128, 8, 64, 1>(f, stream) : s.waves == 4 ? launch<128, 4, 32, 1>(f, stream) : launch<128, 2, 32, 1>(f, stream);
 }
 
 }  // namespace agc

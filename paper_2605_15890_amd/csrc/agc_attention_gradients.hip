@@ -44,11 +44,12 @@ struct AttnGradients {
 enum AttnKeys { kAll, kSplitMeans, kSplitRest };
 
 // ------------------------------------------------------------------ D and dq: a workgroup's rows, all keys in sight, twice
-template <int D, int WAVES, int KT, AttnKeys KEYS>
+// SHARE waves have the same rows, and every SHAREth 32 keys of them each.
+template <int D, int WAVES, int KT, AttnKeys KEYS, int SHARE>
 __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGradients f)
 {
     using Tile = AttnTile<D>;
-    constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
+    constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32, kRows = 32 * WAVES / SHARE;
     constexpr int kTile = KT * Tile::kRow;
     __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile];   // buffer; keys, values
     const Attn& a = f.a;
@@ -58,17 +59,18 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
     if (slot < 0) return;
     const uint32_t group = a.group.d;
 
-    const int s = attn_find(a.q_end, a.n_seqs, a.tokens_q, group, 32 * WAVES, slot);
+    const int s = attn_find(a.q_end, a.n_seqs, a.tokens_q, group, kRows, slot);
     const AttnSeq seq = attn_sequence(a, s);
-    const int first = attn_first_slot(a.q_end, s, a.tokens_q, group, 32 * WAVES);
-    const int rows = seq.lq * (int)group, tiles = (rows + 32 * WAVES - 1) / (32 * WAVES);
+    const int first = attn_first_slot(a.q_end, s, a.tokens_q, group, kRows);
+    const int rows = seq.lq * (int)group, tiles = (rows + kRows - 1) / (kRows);
     const int tile = tiles - 1 - (slot - first);
     if (tile < 0 || tile >= tiles) return;
 
-    const int row_ = tile * 32 * WAVES + wave * 32 + (lane & 31);
+    const int rows_of = wave / SHARE, turn = wave % SHARE;
+    const int row_ = tile * kRows + rows_of * 32 + (lane & 31);
     const int row = min(row_, rows - 1), t = (int)a.group(row), g = row - t * (int)group, head = head_k * (int)group + g;
     const int seen = attn_seen(a, seq, t);
-    const int last_row = min(tile * 32 * WAVES + 32 * WAVES, rows) - 1;
+    const int last_row = min(tile * kRows + kRows, rows) - 1;
     const int keys = attn_seen(a, seq, (int)a.group(last_row));   // of the tile
     const int run = (keys + f.splits * KT - 1) / (f.splits * KT) * KT;
     const int begin = min(split * run, keys), end = min(begin + run, keys);
@@ -104,9 +106,9 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
     const auto over_keys = [&](const auto& use) {
         const auto step = [&](AttnLds from_lds, AttnLds to_lds, int j0) {
             if (j0 + KT < end) fetch(to_lds, j0 + KT);
-            uint32_t k_tile = 0;
+            uint32_t k_tile = turn * 32 * Tile::kRow;
 #pragma unroll 1
-            for (int j = j0; j < min(j0 + KT, seen_most); j += 32, k_tile += 32 * Tile::kRow) {
+            for (int j = j0 + turn * 32; j < min(j0 + KT, seen_most); j += 32 * SHARE, k_tile += 32 * SHARE * Tile::kRow) {
                 const uint32_t v_tile = k_tile + kTile;
                 // two products of dP, one of each map, in turn
                 attn_f32x16 dp{}, score[2] = {};
@@ -159,8 +161,16 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
         });
 #pragma unroll
         for (int m = 0; m < 2; ++m) mean[m] += attn_other_half(mean[m]);
+        if constexpr (SHARE == 2) {
+            __shared__ float means[WAVES][2][64];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) means[wave][m][lane] = mean[m];
+            __syncthreads();
+#pragma unroll
+            for (int m = 0; m < 2; ++m) mean[m] += means[wave ^ 1][m][lane];
+        }
         if constexpr (KEYS == kSplitMeans) {
-            if (row_ < rows && lane < 32) {
+            if (row_ < rows && lane < 32 && turn == 0) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m) f.part_mean[split * f.of_facts + fact + m * (int64_t)a.tokens_q] = mean[m];
             }
@@ -195,6 +205,28 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
             acc[m][b] = attn_mfma(k, d[i][m], acc[m][b]);
         });
     });
+    if constexpr (SHARE == 2) {
+        // the second wave hands its sums to the first, where the tiles were
+        static_assert(WAVES / 2 * 2 * kBlocks * 16 * 64 * 4 <= (int)sizeof(lds), "they fit");
+        float* box = reinterpret_cast<float*>(lds) + rows_of * (2 * kBlocks * 16 * 64) + lane;
+        __syncthreads();
+        if (turn == 1) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) box[((m * kBlocks + b) * 16 + r) * 64] = acc[m][b][r];
+        }
+        __syncthreads();
+        if (turn == 1) return;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[m][b][r] += box[((m * kBlocks + b) * 16 + r) * 64];
+    }
     if (row_ >= rows) return;
     if (lane < 32 && split == 0) {
 #pragma unroll
@@ -501,17 +533,17 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
     return o;
 }
 
-template <int D, int WAVES, int KT>
+template <int D, int WAVES, int KT, int SHARE>
 void launch_dq(const AttnGradients& f, const Shape& s, hipStream_t stream)
 {
     const int blocks = attn_blocks(f.a, f.slots, f.splits);
     if (s.splits_q == 1) {
-        k_attn_dq<D, WAVES, KT, kAll><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dq<D, WAVES, KT, kAll, SHARE><<<blocks, 64 * WAVES, 0, stream>>>(f);
         return;
     }
-    if constexpr (WAVES == kFewWaves) {
-        k_attn_dq<D, WAVES, KT, kSplitMeans><<<blocks, 64 * WAVES, 0, stream>>>(f);
-        k_attn_dq<D, WAVES, KT, kSplitRest><<<blocks, 64 * WAVES, 0, stream>>>(f);
+    if constexpr (SHARE > 1) {
+        k_attn_dq<D, WAVES, KT, kSplitMeans, SHARE><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dq<D, WAVES, KT, kSplitRest, SHARE><<<blocks, 64 * WAVES, 0, stream>>>(f);
     }
 }
 
@@ -543,9 +575,9 @@ hipError_t launch(AttnGradients f, const AttnParts& parts, const Shape& s, hipSt
     if (a.tokens_q > 0) {
         f.slots = s.slots_q, f.splits = s.splits_q, f.columns = attn_columns(a, f.slots, f.splits);
         if (s.waves_q == kFewWaves)
-            launch_dq<D, kFewWaves, 32>(f, s, stream);
+            launch_dq<D, 2 * kFewWaves, 64, 2>(f, s, stream);
         else
-            launch_dq<D, kRowWaves, KT>(f, s, stream);
+            launch_dq<D, kRowWaves, KT, 1>(f, s, stream);
         if (s.splits_q > 1) sums[n++] = {f.part, f.dq, f.lddq, a.tokens_q, 2 * a.heads, a.d, D, s.splits_q, a.q_end + a.n_seqs - 1};
     }
     f.slots = s.slots_k, f.splits = s.splits_k, f.columns = attn_columns(a, f.slots, f.splits), f.part = f.part_k;
