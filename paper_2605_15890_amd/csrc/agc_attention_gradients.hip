@@ -522,7 +522,7 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
         waves = enough ? most : kFewWaves;
         slots = (int)(own / (32 * waves)) + n_seqs;
         const int64_t blocks = std::max<int64_t>(own / (32 * waves), n_seqs) * kv_heads;
-        splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({640 / blocks, other / n_seqs / 256, (int64_t)16}));
+        splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({512 / blocks, other / n_seqs / 128, (int64_t)16}));
     };
     Shape o;
     side(rows, tokens_k, kRowWaves, o.waves_q, o.slots_q, o.splits_q);
