@@ -178,6 +178,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
         }
         __syncthreads();   // nobody reads tiles any more
     } else {
+#pragma unroll 8
         for (int n = 0; n < f.splits; ++n) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) mean[m] += f.part_mean[n * f.of_facts + fact + m * (int64_t)a.tokens_q];
@@ -493,6 +494,7 @@ __global__ __launch_bounds__(256) void k_attn_sum(AttnSums jobs)
     const int row = (int)(n / per), in = (int)(n - (int64_t)row * per), run = in / (j.up / 4), c = (in - run * (j.up / 4)) * 4;
     if (row >= min(max(*j.last, 0), j.rows)) return;
     tile_f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
     for (int s = 0; s < j.splits; ++s) sum += reinterpret_cast<const tile_f32x4*>(j.part)[s * (int64_t)j.rows * per + n];
     uint16_t* to = j.to + row * j.ld + run * j.width + c;
 #pragma unroll
@@ -522,7 +524,7 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
         waves = enough ? most : kFewWaves;
         slots = (int)(own / (32 * waves)) + n_seqs;
         const int64_t blocks = std::max<int64_t>(own / (32 * waves), n_seqs) * kv_heads;
-        splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({512 / blocks, other / n_seqs / 128, (int64_t)16}));
+        splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({512 / blocks, other / n_seqs / 128, (int64_t)64}));
     };
     Shape o;
     side(rows, tokens_k, kRowWaves, o.waves_q, o.slots_q, o.splits_q);
