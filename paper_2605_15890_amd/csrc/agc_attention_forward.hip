@@ -368,7 +368,8 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
     o.waves = enough ? 8 : (rows <= (int64_t)32 * n_seqs ? 1 : 2) * unit;
     const int64_t own = 32 * o.waves / unit;
     o.slots = (int)(rows / own) + n_seqs;
-    const int64_t blocks = std::max<int64_t>(rows / own, n_seqs) * kv_heads;
+    // as many as the card has places for: a few more would make a second round of them
+    const int64_t blocks = std::max<int64_t>((rows + own - 1) / own, n_seqs) * kv_heads;
     o.splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({(own == 32 ? 1024 : 512) / blocks, tokens_k / n_seqs / 128, (int64_t)kMostSplits}));
     return o;
 }

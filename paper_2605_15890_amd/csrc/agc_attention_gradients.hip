@@ -523,7 +523,7 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
         const bool enough = own / n_seqs >= large && own / large * kv_heads >= 192;
         waves = enough ? most : kFewWaves;
         slots = (int)(own / (32 * waves)) + n_seqs;
-        const int64_t blocks = std::max<int64_t>(own / (32 * waves), n_seqs) * kv_heads;
+        const int64_t blocks = std::max<int64_t>((own + 32 * waves - 1) / (32 * waves), n_seqs) * kv_heads;
         splits = enough ? 1 : (int)std::max<int64_t>(1, std::min({512 / blocks, other / n_seqs / 128, (int64_t)64}));
     };
     Shape o;
