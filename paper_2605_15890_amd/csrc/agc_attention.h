@@ -82,7 +82,10 @@ __device__ __forceinline__ int attn_find(const int32_t* end, int n_seqs, int mos
 
 // Workgroup id -> tile, key head, split.  Workgroups go to the eight XCDs in turn.
 //
-// Without `columns` each XCD gets a contiguous run, so that tiles of the same keys meet in its L2.  Under the causal mask a
+// Without `columns` each XCD gets a contiguous run, so that tiles of the same keys meet in its L2 -- or every eighth workgroup,
+// which gives all as much to do where sequences differ: with tiles enough that some of them meet all the same (8111 tokens in
+// five sequences, 8 heads of 128: 256 instead of 288 us), and with one tile a sequence, none of which meet (8 sequences' queries of
+// 131072 keys, 8 heads of 128: 54 instead of 62; but 64 queries each, 4 tiles of a sequence, 122 instead of 80).  Under the causal mask a
 // sequence's first tiles have most to do, and such a run ends with some of them: with columns, an XCD has whole key heads (or a
 // share of one's tiles), every sequence's first tiles come before all second ones, and the last ones fill the gaps.  Tiles
 // count as n_seqs rows of `columns` each, which they are if the sequences are alike; if not, the order is any.
@@ -95,7 +98,8 @@ __device__ __forceinline__ AttnPlace attn_place(const Attn& a, int id, int slots
 {
     if (columns == 0) {
         if (id >= slots * a.kv_heads * splits) return {-1, 0, 0};
-        id = xcd_order(id, slots * a.kv_heads * splits);
+        const bool spread = slots <= 2 * a.n_seqs || (splits == 1 && slots >= 32 * a.n_seqs);
+        if (!spread) id = xcd_order(id, slots * a.kv_heads * splits);
         const int rest = id / splits, head_k = rest / slots;
         return {rest - head_k * slots, head_k, id - rest * splits};
     }
