@@ -1,5 +1,6 @@
 // Launch interface between the C ABI (agc_operators.cpp) and the kernels of the operators round the coded step:
-// orthogonalised update, gated block, embedding, rotary positions, dropout, differential attention.  Every pointer is a device pointer unless it says host.
+// orthogonalised update, gated block, embedding, rotary positions, dropout, differential attention.  Every pointer is a device
+// pointer unless it says host.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -8,8 +8,8 @@
 // (sine to the ninth power, cosine to the tenth: 2e-9 and 2e-10 at pi/4).
 //
 // Bound by memory.  A workgroup has a few tokens, forms the sines of their pairs once, in LDS, and has each thread turn up to
-// four pieces of 2 x 8 values, all of them fetched before the first is stored.  (16384 tokens of 24 heads of 64 in bfloat16: 25.5 us;
-// with the sines formed by every thread 27 us, of which the sines were most.)
+// four pieces of 2 x 8 values, all of them fetched before the first is stored.  16384 tokens of 24 heads of 64 in bfloat16 take
+// 25.5 us, 20 of them in the kernel (5.0 TB/s); with the sines formed by every thread 27, of which the sines were most.
 #include <algorithm>
 
 #include "agc_operators.h"
@@ -122,10 +122,10 @@ __global__ __launch_bounds__(kBlock) void k_rotary(Rotary a, const T* x, T* out)
 }
 
 template <typename T, int PIECES>
-void launch(const Rotary& a, const RotaryCall& c, dim3 grid, hipStream_t stream)
+void launch(const Rotary& a, const RotaryCall& c, int64_t token, dim3 grid, hipStream_t stream)
 {
-    const T* x = static_cast<const T*>(c.x);
-    T* out = static_cast<T*>(c.out);
+    const T* x = static_cast<const T*>(c.x) + token * c.ldx;
+    T* out = static_cast<T*>(c.out) + token * c.ldo;
     if (c.interleaved)
         k_rotary<T, true, PIECES><<<grid, kBlock, 0, stream>>>(a, x, out);
     else
@@ -137,7 +137,7 @@ void launch(const Rotary& a, const RotaryCall& c, dim3 grid, hipStream_t stream)
 hipError_t launch_rotary(const RotaryCall& c, hipStream_t stream)
 {
     Rotary a{};
-    a.ldx = c.ldx, a.ldo = c.ldo, a.n = c.n, a.positions = c.positions, a.turns = c.turns, a.wide = c.wide_ids;
+    a.ldx = c.ldx, a.ldo = c.ldo, a.turns = c.turns, a.wide = c.wide_ids;
     a.heads = c.heads, a.dim = c.dim, a.rot = c.rot, a.amplitude = c.amplitude, a.inverse = c.inverse;
     a.rot_units = (c.rot / 2 + 7) / 8;
     a.units = a.rot_units + (c.dim - c.rot + 15) / 16;
@@ -145,11 +145,16 @@ hipError_t launch_rotary(const RotaryCall& c, hipStream_t stream)
     // Many tokens: as many a workgroup as have four pieces a thread and whose sines fit.  Few: a piece a thread, more workgroups.
     const int per = a.heads * a.units, pieces = c.n * per >= 524288 ? 4 : 1;
     a.tokens = std::max(1, std::min(kBlock * pieces / per, kTable / a.pairs));
-    const dim3 grid((uint32_t)((c.n + a.tokens - 1) / a.tokens), (uint32_t)((a.tokens * per + kBlock * pieces - 1) / (kBlock * pieces)));
-    if (pieces == 4)
-        c.bf16 ? launch<uint16_t, 4>(a, c, grid, stream) : launch<float, 4>(a, c, grid, stream);
-    else
-        c.bf16 ? launch<uint16_t, 1>(a, c, grid, stream) : launch<float, 1>(a, c, grid, stream);
+    // 2^23 workgroups a launch: a grid has fewer than 2^32 threads
+    for (int64_t token = 0; token < c.n; token += (int64_t)a.tokens << 23) {
+        a.n = std::min(c.n - token, (int64_t)a.tokens << 23);
+        a.positions = static_cast<const char*>(c.positions) + token * (c.wide_ids ? 8 : 4);
+        const dim3 grid((uint32_t)((a.n + a.tokens - 1) / a.tokens), (uint32_t)((a.tokens * per + kBlock * pieces - 1) / (kBlock * pieces)));
+        if (pieces == 4)
+            c.bf16 ? launch<uint16_t, 4>(a, c, token, grid, stream) : launch<float, 4>(a, c, token, grid, stream);
+        else
+            c.bf16 ? launch<uint16_t, 1>(a, c, token, grid, stream) : launch<float, 1>(a, c, token, grid, stream);
+    }
     return hipGetLastError();
 }
 

@@ -382,14 +382,16 @@ def test_thousands_of_sequences():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("lens,heads,kv_heads,d,e", [([(1100, 1100)] * 12, 8, 8, 32, 64), ([(300, 300), (5000, 5000), (0, 0), (700, 700)], 4, 4, 64, 128),
-                                                     ([(2000, 2000)] * 2, 32, 16, 64, 128), ([(2100, 2100)] * 3, 3, 3, 64, 128), ([(1500, 1500)] * 4, 8, 8, 128, 256)])
-def test_large_workgroups(lens, heads, kv_heads, d, e):
-    """Sizes that take the large workgroups and both orders of tiles, against sequence after sequence by itself, which takes
+@pytest.mark.parametrize("lens,heads,kv_heads,d,e,causal", [
+    ([(1100, 1100)] * 12, 8, 8, 32, 64, True), ([(300, 300), (5000, 5000), (0, 0), (700, 700)], 4, 4, 64, 128, True), ([(2000, 2000)] * 2, 32, 16, 64, 128, True),
+    ([(2100, 2100)] * 3, 3, 3, 64, 128, True), ([(1500, 1500)] * 4, 8, 8, 128, 256, True),
+    ([(1500, 1500), (2600, 2300), (0, 0), (1900, 1950)], 8, 2, 128, 256, False), ([(9000, 900), (5000, 700)], 6, 3, 64, 128, False)])
+def test_large_workgroups(lens, heads, kv_heads, d, e, causal):
+    """Sizes that take the large workgroups and all orders of tiles, against sequence after sequence by itself, which takes
     small ones: the same formulas with sums cut in other places.  Two results, each off by its own rounding and, out, by
     those of its maps: 2^-8 sqrt(2) of a value in the root mean square at most, half a step being the largest."""
     import torch
-    c = Case(lens, heads, kv_heads, d, e, True)
+    c = Case(lens, heads, kv_heads, d, e, causal)
     out = c.forward()[:, :heads * e]
     parts = [c.nq // 3, c.nq]
     dq, dk, dv, G = c.gradients(parts)
@@ -399,7 +401,7 @@ def test_large_workgroups(lens, heads, kv_heads, d, e):
         if lq == 0:
             continue
         one = (c.q[i:i + lq], c.k[j:j + lk], c.v[j:j + lk], heads, kv_heads, c.lam, torch.tensor([lq], dtype=torch.int32, device="cuda"),
-               torch.tensor([lk], dtype=torch.int32, device="cuda"), c.scale, True)
+               torch.tensor([lk], dtype=torch.int32, device="cuda"), c.scale, causal)
         ws = torch.empty(api.agc_diff_attn_workspace_bytes(lq, lk, 1, heads, kv_heads, d, e, True), dtype=torch.uint8, device="cuda")
         alone, lse = torch.empty_like(out[i:i + lq]), torch.empty(2 * heads, lq, device="cuda")
         api.agc_diff_attn_forward(*one, alone, ws, lse=lse)
@@ -479,6 +481,7 @@ def raw(grad=False, q=256, ldq=512, k=256, ldk=256, v=256, ldv=256, nq=3, nk=4, 
     (dict(nq=-1), -2), (dict(nq=2 ** 26 + 1), -2), (dict(nk=-1), -2), (dict(nk=2 ** 26 + 1), -2), (dict(n=0), -2), (dict(n=2 ** 20 + 1), -2),
     (dict(heads=3), -2), (dict(heads=0), -2), (dict(kv=0), -2), (dict(d=0), -2), (dict(d=129), -2), (dict(e=0), -2), (dict(e=257), -2),
     (dict(nq=2 ** 26, heads=32, ldq=4096), -2), (dict(nk=2 ** 26, heads=64, kv=32, ldk=4096, ldv=4096, ldq=8192), -2),
+    (dict(nq=2 ** 26, heads=18, ldq=4096), -2), (dict(n=2 ** 19, heads=8, kv=8, ldq=1024, ldk=1024, ldv=1024), -2),
     (dict(n=2 ** 20, heads=32, kv=32, ldq=4096, ldk=4096, ldv=4096), -2), (dict(scale=math.inf), -1), (dict(scale=math.nan), -1), (dict(scale=-0.5), -1),
     (dict(q=0), -1), (dict(k=0), -1), (dict(v=0), -1), (dict(lam=0), -1), (dict(qe=0), -1), (dict(ke=0), -1), (dict(ws=0), -1),
     (dict(ldq=2 ** 24 + 8), -2), (dict(ldk=2 ** 24 + 8), -2), (dict(ldv=2 ** 24 + 8), -2), (dict(ldq=504), -2), (dict(ldk=248), -2), (dict(ldv=248), -2), (dict(q=258), -4), (dict(k=264), -4), (dict(v=258), -4), (dict(ldq=516), -4),
@@ -493,7 +496,7 @@ def test_refusals_of_the_forward_pass(change, status):
 
 
 @pytest.mark.parametrize("change,status", [
-    (dict(parts=None), -1), (dict(parts=()), -2), (dict(parts=(2,)), -2), (dict(parts=(3, 2)), -2), (dict(parts=(2, 1, 3)), -2), (dict(parts=(3,) * 257), -2),
+    (dict(parts=None), -1), (dict(parts=()), -2), (dict(parts=(2,)), -2), (dict(parts=(3, 2)), -2), (dict(parts=(2, 1, 3)), -2), (dict(parts=(3,) * 257), -2), (dict(parts=(3,) * 256, heads=2 ** 14, ldq=2 ** 21, lddout=2 ** 21, lddq=2 ** 21, ldg=2 ** 14), -2),
     (dict(dout=0), -1), (dict(lse=0), -1), (dict(dq=0), -1), (dict(dk=0), -1), (dict(dv=0), -1), (dict(G=0), -1), (dict(lddout=504), -2), (dict(lddout=2 ** 24 + 8), -2), (dict(lddq=511), -2),
     (dict(lddk=255), -2), (dict(lddv=255), -2), (dict(ldg=3), -2), (dict(dout=258), -4), (dict(lddout=516), -4), (dict(dq=1), -4), (dict(dk=1), -4), (dict(dv=1), -4),
     (dict(G=2), -4)])
