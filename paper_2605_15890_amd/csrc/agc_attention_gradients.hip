@@ -403,9 +403,12 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
                     for (int m = 0; m < 2; ++m) score[m][r] = in ? (seen == 1 ? 0.0f : score[m][r]) : -INFINITY;
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float p[8], ds[8], lse[8], mean[8];
+            // of 16 rows: dS of the own map, of the other one, the difference of the maps
+            struct Half {
+                AttnTwo own, mixed, second;
+            };
+            const auto of_half = [&](int i) {
+                float p[8], ds[8], lse[8], mean[8], other[8];
                 fact8(half, i, lse);
                 fact8(2 + half, i, mean);
 #pragma unroll
@@ -419,22 +422,32 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
                 if constexpr (kHalves == 1) fact8(3, i, mean);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float other = __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
-                    if (!half) other *= lambda;
-                    if constexpr (kHalves == 1) ds[e] = other * (mean[e] - dp[i * 8 + e]);
-                    p[e] -= other;
+                    other[e] = __builtin_amdgcn_exp2f(fmaf(score[1][i * 8 + e], a.to_log2, -lse[e]));
+                    if (!half) other[e] *= lambda;
+                    if constexpr (kHalves == 1) ds[e] = other[e] * (mean[e] - dp[i * 8 + e]);
+                    p[e] -= other[e];
                 }
-                const AttnTwo mixed(p);
-#pragma unroll
-                for (int b = 0; b < kValues; ++b) acc_v[b] = attn_mfma(reads.turned(from_lds, o_tile + half * 256, i * 16, b), mixed, acc_v[b]);
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) acc_k[0][b] = attn_mfma(reads.turned(from_lds, q_own, i * 16, b), own, acc_k[0][b]);
-                if constexpr (kHalves == 1) {
-                    const AttnTwo second(ds);
-#pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) acc_k[1][b] = attn_mfma(reads.turned(from_lds, q_tile, i * 16, kBlocks + b), second, acc_k[1][b]);
-                }
-            }
+                return Half{own, AttnTwo(p), AttnTwo(ds)};
+            };
+            constexpr int kOfHalf = kValues + 2 / kHalves * kBlocks;
+            const auto read = [&](int n) {
+                const int i = n / kOfHalf, b = n % kOfHalf;
+                return b < kValues ? reads.turned(from_lds, o_tile + half * 256, i * 16, b) : reads.turned(from_lds, q_own, i * 16, b - kValues);
+            };
+            // with four reads ahead, or started before the halves, registers leave for memory (581 and 610 us instead of 555)
+            auto stream = attn_stream<2 * kOfHalf, 2>(read);
+            const Half of[2] = {of_half(0), of_half(1)};
+            stream.start();
+            stream.run([&](int n, const tile_bf16x8& x) {
+                const int b = n % kOfHalf;
+                const Half& h = of[n / kOfHalf];
+                if (b < kValues)
+                    acc_v[b] = attn_mfma(x, h.mixed, acc_v[b]);
+                else if (b < kValues + kBlocks)
+                    acc_k[0][b - kValues] = attn_mfma(x, h.own, acc_k[0][b - kValues]);
+                else
+                    acc_k[kHalves == 1][b - kValues - kBlocks] = attn_mfma(x, h.second, acc_k[kHalves == 1][b - kValues - kBlocks]);
+            });
         }
     };
     int buffer = 0;
