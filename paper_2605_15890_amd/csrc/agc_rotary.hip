@@ -7,9 +7,9 @@
 // by whole turns.  The angle is then brought to an eighth of a turn round the nearest quarter and enters two Taylor sums
 // (sine to the ninth power, cosine to the tenth: 2e-9 and 2e-10 at pi/4).
 //
-// Bound by memory.  A workgroup has a few tokens, forms the sines of their pairs once, in LDS, and has each thread turn up to
-// four pieces of 2 x 8 values, all of them fetched before the first is stored.  16384 tokens of 24 heads of 64 in bfloat16 take
-// 25.5 us, 20 of them in the kernel (5.0 TB/s); with the sines formed by every thread 27, of which the sines were most.
+// Bound by memory.  A workgroup has a few tokens; each thread fetches a piece of 2 x 8 values, the sines of all pairs are formed
+// meanwhile, once for all heads, in LDS, and the pieces turn.  16384 tokens of 24 heads of 64 in bfloat16 take 23 us, 4.4 TB/s
+// (131072 of 8 heads 45.5, 5.9 TB/s); with the sines formed by every thread 27, with four pieces a thread and fewer waves 25.5.
 #include <algorithm>
 
 #include "agc_operators.h"
@@ -55,81 +55,69 @@ __device__ __forceinline__ void turn(uint64_t phase, float amplitude, float& c, 
     s = amplitude * (quarter & 2 ? -b : b);
 }
 
-template <typename T, bool INTERLEAVED, int PIECES>
+template <typename T, bool INTERLEAVED>
 __global__ __launch_bounds__(kBlock) void k_rotary(Rotary a, const T* x, T* out)
 {
-    __shared__ __attribute__((aligned(16))) float table[2][kTable];   // cosines, sines
+    extern __shared__ __attribute__((aligned(16))) float cosines[];
+    float* const sines = cosines + a.tokens * a.pairs;
     const int64_t token0 = (int64_t)blockIdx.x * a.tokens;
     const int tokens = (int)min((int64_t)a.tokens, a.n - token0), half = a.rot >> 1;
 
     // pieces are numbered by token, head and place in the head
-    struct Piece {
-        const T* from;
-        T* to;
-        int at1, count0, count1, pair;   // second run behind the first; lengths of both; place in the table, -1 of what stays
-    } piece[PIECES];
-    float v[PIECES][16];
-    const int per = a.heads * a.units;
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int n = (blockIdx.y * PIECES + i) * kBlock + threadIdx.x, t = n / per, in = n - t * per, h = in / a.units, unit = in - h * a.units;
-        Piece& p = piece[i];
-        p.count0 = 0;
-        if (t >= tokens) continue;
-        const bool turns = unit < a.rot_units;
-        int at;
+    const int per = a.heads * a.units, n = blockIdx.y * blockDim.x + threadIdx.x, t = n / per, in = n - t * per, h = in / a.units, unit = in - h * a.units;
+    const bool turns = unit < a.rot_units;
+    int at, at1, count0 = 0, count1;   // two runs: where they begin and their lengths
+    float v[16];
+    if (t < tokens) {
         if (turns && !INTERLEAVED) {
-            at = unit * 8, p.at1 = half;
-            p.count0 = p.count1 = min(8, half - at);
+            at = unit * 8, at1 = at + half;
+            count0 = count1 = min(8, half - at);
         } else {
-            at = turns ? unit * 16 : a.rot + (unit - a.rot_units) * 16, p.at1 = 8;
+            at = turns ? unit * 16 : a.rot + (unit - a.rot_units) * 16, at1 = at + 8;
             const int end = turns ? a.rot : a.dim;
-            p.count0 = min(8, end - at), p.count1 = max(0, min(8, end - at - 8));
+            count0 = min(8, end - at), count1 = max(0, min(8, end - at1));
         }
-        p.pair = turns ? t * a.pairs + unit * 8 : -1;
-        p.from = x + (token0 + t) * a.ldx + h * a.dim + at;
-        p.to = out + (token0 + t) * a.ldo + h * a.dim + at;
-        load8(p.from, p.count0, v[i]);
-        load8(p.from + p.at1, p.count1, v[i] + 8);
+        const T* from = x + (token0 + t) * a.ldx + h * a.dim;
+        load8(from + at, count0, v);
+        load8(from + at1, count1, v + 8);
     }
-    for (int n = threadIdx.x; n < tokens * a.pairs; n += kBlock) {
-        const int t = n / a.pairs, pair = min(n - t * a.pairs, half - 1);   // places behind the last pair are read, not used
-        const int64_t position = a.wide ? static_cast<const int64_t*>(a.positions)[token0 + t] : static_cast<const int32_t*>(a.positions)[token0 + t];
+    for (int i = threadIdx.x; i < tokens * a.pairs; i += blockDim.x) {
+        const int token = i / a.pairs, pair = min(i - token * a.pairs, half - 1);   // places behind the last pair are read, not used
+        const int64_t position =
+            a.wide ? static_cast<const int64_t*>(a.positions)[token0 + token] : static_cast<const int32_t*>(a.positions)[token0 + token];
         const uint64_t phase = (uint64_t)position * a.turns[pair];
-        turn(a.inverse ? 0 - phase : phase, a.amplitude, table[0][n], table[1][n]);
+        turn(a.inverse ? 0 - phase : phase, a.amplitude, cosines[i], sines[i]);
     }
     __syncthreads();
+    if (count0 == 0) return;
+    if (turns) {
+        float c[8], s[8];
+        load8(cosines + t * a.pairs + unit * 8, 8, c);
+        load8(sines + t * a.pairs + unit * 8, 8, s);
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const Piece& p = piece[i];
-        if (p.count0 == 0) continue;
-        if (p.pair >= 0) {
-            float c[8], s[8];
-            load8(&table[0][p.pair], 8, c);
-            load8(&table[1][p.pair], 8, s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float& p0 = INTERLEAVED ? v[i][2 * e] : v[i][e];
-                float& p1 = INTERLEAVED ? v[i][2 * e + 1] : v[i][8 + e];
-                const float was = p0;
-                p0 = fmaf(was, c[e], -(p1 * s[e]));
-                p1 = fmaf(was, s[e], p1 * c[e]);
-            }
+        for (int e = 0; e < 8; ++e) {
+            float& p0 = INTERLEAVED ? v[2 * e] : v[e];
+            float& p1 = INTERLEAVED ? v[2 * e + 1] : v[8 + e];
+            const float was = p0;
+            p0 = fmaf(was, c[e], -(p1 * s[e]));
+            p1 = fmaf(was, s[e], p1 * c[e]);
         }
-        store8(p.to, p.count0, v[i]);
-        store8(p.to + p.at1, p.count1, v[i] + 8);
     }
+    T* to = out + (token0 + t) * a.ldo + h * a.dim;
+    store8(to + at, count0, v);
+    store8(to + at1, count1, v + 8);
 }
 
-template <typename T, int PIECES>
-void launch(const Rotary& a, const RotaryCall& c, int64_t token, dim3 grid, hipStream_t stream)
+template <typename T>
+void launch(const Rotary& a, const RotaryCall& c, int64_t token, dim3 grid, int threads, hipStream_t stream)
 {
+    const size_t lds = (size_t)a.tokens * a.pairs * 2 * sizeof(float);
     const T* x = static_cast<const T*>(c.x) + token * c.ldx;
     T* out = static_cast<T*>(c.out) + token * c.ldo;
     if (c.interleaved)
-        k_rotary<T, true, PIECES><<<grid, kBlock, 0, stream>>>(a, x, out);
+        k_rotary<T, true><<<grid, threads, lds, stream>>>(a, x, out);
     else
-        k_rotary<T, false, PIECES><<<grid, kBlock, 0, stream>>>(a, x, out);
+        k_rotary<T, false><<<grid, threads, lds, stream>>>(a, x, out);
 }
 
 }  // namespace
@@ -142,18 +130,16 @@ hipError_t launch_rotary(const RotaryCall& c, hipStream_t stream)
     a.rot_units = (c.rot / 2 + 7) / 8;
     a.units = a.rot_units + (c.dim - c.rot + 15) / 16;
     a.pairs = a.rot_units * 8;
-    // Many tokens: as many a workgroup as have four pieces a thread and whose sines fit.  Few: a piece a thread, more workgroups.
-    const int per = a.heads * a.units, pieces = c.n * per >= 524288 ? 4 : 1;
-    a.tokens = std::max(1, std::min(kBlock * pieces / per, kTable / a.pairs));
+    // as many tokens as have a piece a thread and whose sines fit, and no more waves than they need
+    const int per = a.heads * a.units;
+    a.tokens = std::max(1, std::min(kBlock / per, kTable / a.pairs));
+    const int threads = std::min(kBlock, (a.tokens * per + 63) / 64 * 64);
     // 2^23 workgroups a launch: a grid has fewer than 2^32 threads
     for (int64_t token = 0; token < c.n; token += (int64_t)a.tokens << 23) {
         a.n = std::min(c.n - token, (int64_t)a.tokens << 23);
         a.positions = static_cast<const char*>(c.positions) + token * (c.wide_ids ? 8 : 4);
-        const dim3 grid((uint32_t)((a.n + a.tokens - 1) / a.tokens), (uint32_t)((a.tokens * per + kBlock * pieces - 1) / (kBlock * pieces)));
-        if (pieces == 4)
-            c.bf16 ? launch<uint16_t, 4>(a, c, token, grid, stream) : launch<float, 4>(a, c, token, grid, stream);
-        else
-            c.bf16 ? launch<uint16_t, 1>(a, c, token, grid, stream) : launch<float, 1>(a, c, token, grid, stream);
+        const dim3 grid((uint32_t)((a.n + a.tokens - 1) / a.tokens), (uint32_t)((a.tokens * per + threads - 1) / threads));
+        c.bf16 ? launch<uint16_t>(a, c, token, grid, threads, stream) : launch<float>(a, c, token, grid, threads, stream);
     }
     return hipGetLastError();
 }
