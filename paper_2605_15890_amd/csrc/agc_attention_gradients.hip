@@ -282,11 +282,13 @@ __device__ __forceinline__ void attn_lambda(const AttnParts& parts, const Attn& 
 //
 // Wide heads are worked on by two workgroups, since dk and dv of 32 keys would take a wave's registers twice over: each forms
 // both maps and dP, and has dk of one map (its own) and half of dv.  A third more products than one workgroup would need, in a
-// half of the time that it takes when registers leave for memory (8 x 2048 tokens, 8 heads of 128: 1016 instead of 2544 us).
+// half of the time that it takes when registers leave for memory (8 x 2048 tokens, 8 heads of 128: 922 instead of 2544 us).
 constexpr int attn_halves(int D) { return D == 128 ? 2 : 1; }
+// A wave a SIMD, with all of its registers.
+constexpr bool attn_room(int D, int waves) { return D == 128 || waves == 2; }
 
 template <int D, int WAVES, int RT>
-__global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_attn_dkv(AttnGradients f, AttnParts parts)
+__global__ __launch_bounds__(64 * WAVES, attn_room(D, WAVES) ? 1 : 2) void k_attn_dkv(AttnGradients f, AttnParts parts)
 {
     using Tile = AttnTile<D>;
     constexpr int E = 2 * D, kSteps = D / 16, kBlocks = D / 32;
@@ -296,6 +298,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
     const AttnLds all = (AttnLds)&lds[0], values = all + 2 * kBuffer;
     const Attn& a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr bool kRoom = attn_room(D, WAVES);
     constexpr int kHalves = attn_halves(D), kValues = 2 * kBlocks / kHalves;
     const int tiles = f.blocks * kHalves;
     if ((int)blockIdx.x >= tiles) {   // behind the tiles: the rows of G
@@ -384,15 +387,35 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 || WAVES == 2 ? 1 : 2) void k_
                 for (int e = 0; e < 4; ++e) o[e] = lo[e], o[4 + e] = hi[e];
             };
             attn_f32x16 dp{}, score[2] = {};
+            const auto read_q = [&](int m, int i) {
+                return kHalves == 2 ? reads.straight(from_lds, q_tile + (m ^ half) * 256, i) : reads.straight(from_lds, q_tile, m * kSteps + i);
+            };
+            if constexpr (kRoom) {
+                // a product of dP and one of a map in turn (8 x 2048 tokens, 8 heads of 128: 922 instead of 980 us)
+                const auto read = [&](int n) {
+                    const int i = n / 3;
+                    return n % 3 == 0 ? reads.straight(from_lds, o_tile, i) : n % 3 == 1 ? reads.straight(v_lds, 0, i) : read_q(i & 1, i / 2);
+                };
+                auto stream = attn_stream<6 * kSteps, 6>(read);
+                stream.start();
+                tile_bf16x8 o;
+                stream.run([&](int n, const tile_bf16x8& x) {
+                    const int i = n / 3;
+                    if (n % 3 == 0)
+                        o = x;
+                    else if (n % 3 == 1)
+                        dp = attn_mfma(o, x, dp);
+                    else
+                        score[i & 1] = attn_mfma(x, k[i & 1][i / 2], score[i & 1]);
+                });
+            } else {
 #pragma unroll
-            for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(reads.straight(from_lds, o_tile, i), reads.straight(v_lds, 0, i), dp);
+                for (int i = 0; i < 2 * kSteps; ++i) dp = attn_mfma(reads.straight(from_lds, o_tile, i), reads.straight(v_lds, 0, i), dp);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i)
+                for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const tile_bf16x8 x = kHalves == 2 ? reads.straight(from_lds, q_tile + (m ^ half) * 256, i) : reads.straight(from_lds, q_tile, m * kSteps + i);
-                    score[m] = attn_mfma(x, k[m][i], score[m]);
-                }
+                    for (int m = 0; m < 2; ++m) score[m] = attn_mfma(read_q(m, i), k[m][i], score[m]);
+            }
             if (masked) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
