@@ -14,10 +14,10 @@
 // zero, only cancels as far as it is exact (2.5e-3 in the 2-norm where the rounding alone is 1.66e-3).  Sums are binary32.
 //
 // That makes 28 d + 10 e operations a pair of a query and a key, where a single pass of one part would do with 12 d + 4 e.
-// 8 x 2048 tokens, 16 heads of 64 on 4 key heads, causal: the rows' pass 503 us, 0.82 PFLOP/s of products, the keys' pass with
-// its join 560 us, 0.74 (a library product of 8192^3: 1.28).  Counters have the matrix units busy for a third of the
-// time and the vector units for 40 to 49 %: of the two waves a SIMD, which is what the registers of dq or of dk and dv leave
-// room for, neither hides the other's waits.
+// 8 x 2048 tokens, 16 heads of 64, causal: the rows' pass 457 to 504 us, 0.82 to 0.9 PFLOP/s of products, the keys' pass 491 to
+// 555, 0.74 to 0.84 (a library product of 8192^3: 1.28).  Counters have the matrix units busy for 0.39 to 0.45 of the time and
+// the vector units for 0.49 to 0.63: of the two waves a SIMD, which is what the registers of dq or of dk and dv leave room
+// for, neither hides the other's waits, and the clock falls to 2 GHz.
 #include <algorithm>
 
 #include "agc_attention.h"
