@@ -382,8 +382,8 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
  *   q_dev      device, tokens_q x (heads * 2 * head_dim): both maps' queries of a head lie side by side
  *   k_dev, v_dev  device, tokens_k x (kv_heads * 2 * head_dim) and tokens_k x (kv_heads * value_dim)
  *              row strides ldq, ldk, ldv elements.  Where head_dim and value_dim are D and 2 D, D = 32, 64 or 128, rows must begin at
- *              multiples of 16 bytes (AGC_EALIGN) and are read where they lie; other widths may begin anywhere and are
- *              copied to the workspace, widened to the next D that holds both
+ *              multiples of 16 bytes (AGC_EALIGN).  Other widths may begin anywhere, the next D holds both: multiples of 8
+ *              whose rows all begin at multiples of 16 bytes are read where they lie too, the rest is copied to the workspace
  *   lambda_dev device, heads floats
  *   q_end_dev, k_end_dev  device, n_seqs ends of the sequences in queries and in keys, not descending; sequence s has the
  *              queries from q_end[s-1] (0 for the first) to q_end[s], and the keys alike.  Either may be empty.  Rows of out

@@ -27,7 +27,7 @@ typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896f;
 
-// What the kernels know of a call; operands as laid out: heads of D and 2 D values, 16-byte aligned rows.
+// What the kernels know of a call; operands as they are read, with 16-byte aligned rows.
 struct Attn {
     const uint16_t *q, *k, *v;
     int64_t ldq, ldk, ldv;
@@ -35,6 +35,7 @@ struct Attn {
     const int32_t *q_end, *k_begin, *k_end;
     int n_seqs, tokens_q, tokens_k;
     int heads, kv_heads, d, e;
+    int whole;            // heads of D and 2 D values; else of d and e, multiples of 8, whose tiles are filled up with zeros
     Divider group;        // heads that share keys, and the division of row numbers by them
     int causal;
     float scale;          // of the scores
@@ -142,6 +143,30 @@ __device__ __forceinline__ void attn_load4(const float* src, AttnLds dst)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
 }
 
+static __device__ __attribute__((aligned(16))) const uint32_t attn_zeros[4] = {};
+
+// A head of an operand in memory: RUNS runs (two maps or one of values), 2 D values in a tile, WHOLE if here too, `width` a run if
+// not.
+template <int D, int RUNS, bool WHOLE>
+struct AttnHead {
+    static constexpr int kRun = 2 * D / RUNS;
+    int width;
+    __device__ __forceinline__ int run() const { return WHOLE ? kRun : width; }
+    __device__ __forceinline__ int size() const { return RUNS * run(); }
+    // where chunk c of 16 bytes of a row that begins `at` bytes behind base comes from
+    __device__ __forceinline__ const char* chunk(const char* base, uint32_t at, int c) const
+    {
+        if constexpr (WHOLE) return base + (at + c * 16);
+        const int r = c / (kRun / 8), in = c % (kRun / 8) * 8;
+        return in < width ? base + (at + (r * width + in) * 2) : reinterpret_cast<const char*>(attn_zeros);
+    }
+    // values in .. in + 7 of run r
+    __device__ __forceinline__ tile_bf16x8 values(const uint16_t* row, int r, int in) const
+    {
+        return *reinterpret_cast<const tile_bf16x8*>(chunk(reinterpret_cast<const char*>(row), 0, (r * kRun + in) / 8));
+    }
+};
+
 template <int D>
 struct AttnTile {
     static constexpr int kRow = 4 * D, kChunks = kRow / 16;
@@ -154,8 +179,8 @@ struct AttnTile {
 
     // Rows 0 .. ROWS - 1 of a matrix in memory, `base` the first one's address, the same for all lanes, to LDS; those from `rows` on
     // are the last one again.  Whole tiles cost an addition a load.
-    template <int ROWS, int WAVES>
-    static __device__ __forceinline__ void load(AttnLds lds, int wave, int lane, const char* base, uint32_t stride, int rows)
+    template <int ROWS, int WAVES, typename Head>
+    static __device__ __forceinline__ void load(AttnLds lds, int wave, int lane, const Head& head, const char* base, uint32_t stride, int rows)
     {
         constexpr int kPer = 64 / kChunks;   // rows a wave fetches at once
         constexpr int kTimes = ROWS / kPer / WAVES;
@@ -164,13 +189,14 @@ struct AttnTile {
 #pragma unroll
             for (int i = 0; i < kTimes; ++i) {
                 const int c = i * WAVES + wave, row = c * kPer + lane / kChunks;
-                attn_load16(base + (int64_t)(c * kPer) * stride + ((uint32_t)(lane / kChunks) * stride + ((lane % kChunks) ^ mix(row)) * 16), lds + c * 1024);
+                attn_load16(head.chunk(base + (int64_t)(c * kPer) * stride, (uint32_t)(lane / kChunks) * stride, (lane % kChunks) ^ mix(row)),
+                            lds + c * 1024);
             }
         } else {
 #pragma unroll 1
             for (int c = wave; c < ROWS / kPer; c += WAVES) {
                 const int row = c * kPer + lane / kChunks;
-                attn_load16(base + ((uint32_t)min(row, rows - 1) * stride + ((lane % kChunks) ^ mix(row)) * 16), lds + c * 1024);
+                attn_load16(head.chunk(base, (uint32_t)min(row, rows - 1) * stride, (lane % kChunks) ^ mix(row)), lds + c * 1024);
             }
         }
     }
@@ -326,7 +352,7 @@ struct AttnPack {
 // What the gradients take of the workspace beyond that.
 int64_t attn_gradients_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int D);
 hipError_t attn_pack(const AttnPack* jobs, int n, hipStream_t stream);
-// Fills `a` from the call, copying operands of other widths to the workspace; `place` moves on behind them.
+// Fills `a` from the call, copying operands that are not read where they lie to the workspace; `place` moves on behind them.
 hipError_t attn_lay_out(const AttnCall& c, Attn& a, const uint16_t*& dout, int64_t& lddout, char*& place, hipStream_t stream);
 
 }  // namespace agc

@@ -39,7 +39,7 @@ constexpr int attn_maps_of_a_wave(int D) { return D == 128 ? 1 : 2; }
 constexpr float kGrowth = 8.0f;
 
 // SHARE waves have the same rows, and every SHAREth 32 keys of them each.
-template <int D, int WAVES, int KT, int SHARE>
+template <int D, int WAVES, int KT, int SHARE, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1 : 2) void k_attn_forward(AttnForward f)
 {
     using Tile = AttnTile<D>;
@@ -75,19 +75,21 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
     // of the wave's rows: what the first and the last one see
     const int seen_least = min(__builtin_amdgcn_readfirstlane(seen), end), seen_most = min(__builtin_amdgcn_readlane(seen, 31), end);
 
+    const AttnHead<D, 2, WHOLE> maps{a.d};
+    const AttnHead<D, 1, WHOLE> ofv{a.e};
     tile_bf16x8 q[kMaps][kSteps];
     {
-        const uint16_t* p = a.q + (int64_t)(seq.q0 + t) * a.ldq + (int64_t)head * E + map0 * D + (lane >> 5) * 8;
+        const uint16_t* p = a.q + (int64_t)(seq.q0 + t) * a.ldq + (int64_t)head * maps.size();
 #pragma unroll
         for (int m = 0; m < kMaps; ++m)
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) q[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + m * D + i * 16);
+            for (int i = 0; i < kSteps; ++i) q[m][i] = maps.values(p, map0 + m, (lane >> 5) * 8 + i * 16);
     }
-    const char* const keys_at = reinterpret_cast<const char*>(a.k + (int64_t)seq.k0 * a.ldk + head_k * E);
-    const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
+    const char* const keys_at = reinterpret_cast<const char*>(a.k + (int64_t)seq.k0 * a.ldk + head_k * maps.size());
+    const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * ofv.size());
     const auto fetch = [&](AttnLds to, int j0) {
-        Tile::template load<KT, WAVES>(to, wave, lane, keys_at + (int64_t)j0 * a.ldk * 2, (uint32_t)a.ldk * 2, seq.lk - j0);
-        Tile::template load<KT, WAVES>(to + kTile, wave, lane, values_at + (int64_t)j0 * a.ldv * 2, (uint32_t)a.ldv * 2, seq.lk - j0);
+        Tile::template load<KT, WAVES>(to, wave, lane, maps, keys_at + (int64_t)j0 * a.ldk * 2, (uint32_t)a.ldk * 2, seq.lk - j0);
+        Tile::template load<KT, WAVES>(to + kTile, wave, lane, ofv, values_at + (int64_t)j0 * a.ldv * 2, (uint32_t)a.ldv * 2, seq.lk - j0);
     };
 
     attn_f32x16 acc[kMaps][kBlocks];
@@ -340,7 +342,11 @@ template <int D, int WAVES, int KT, int SHARE>
 hipError_t launch(AttnForward f, hipStream_t stream)
 {
     f.columns = attn_columns(f.a, f.slots, f.splits);
-    k_attn_forward<D, WAVES, KT, SHARE><<<attn_blocks(f.a, f.slots, f.splits), 64 * WAVES, 0, stream>>>(f);
+    const int blocks = attn_blocks(f.a, f.slots, f.splits);
+    if (f.a.whole)
+        k_attn_forward<D, WAVES, KT, SHARE, true><<<blocks, 64 * WAVES, 0, stream>>>(f);
+    else
+        k_attn_forward<D, WAVES, KT, SHARE, false><<<blocks, 64 * WAVES, 0, stream>>>(f);
     if (f.splits > 1) {
         const int64_t all = (int64_t)f.a.tokens_q * f.a.heads;
         if (f.splits > kFewSplits)
@@ -430,6 +436,12 @@ hipError_t attn_lay_out(const AttnCall& c, Attn& a, const uint16_t*& dout, int64
     a.heads = c.heads, a.kv_heads = c.kv_heads, a.d = c.d, a.e = c.e;
     a.causal = c.causal, a.scale = c.scale, a.to_log2 = c.scale * kLog2e;
     dout = static_cast<const uint16_t*>(c.dout), lddout = c.lddout;
+    // Other widths than the tiles' are filled up on the way to LDS if their chunks of 16 bytes can be read, else in the workspace
+    // (2999 queries of 40 and 72, forward and gradients: 104 against 118 us; 8 x 2048 of 80 and 160: 1545 against 1650).
+    const auto chunks = [](const void* p, int64_t ld, int64_t rows) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows < 2 || ld % 8 == 0); };
+    a.whole = (c.d == D && c.e == E) || c.d % 8 || c.e % 8 || !chunks(c.q, c.ldq, c.tokens_q) || !chunks(c.k, c.ldk, c.tokens_k) ||
+              !chunks(c.v, c.ldv, c.tokens_k) || (dout && !chunks(dout, lddout, c.tokens_q));
+    if (!a.whole) return hipSuccess;
     AttnPack jobs[4];
     int n = 0;
     const auto lay = [&](const uint16_t*& p, int64_t& ld, int64_t rows, int parts, int width, int up) {

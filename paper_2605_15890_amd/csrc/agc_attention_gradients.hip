@@ -45,7 +45,7 @@ enum AttnKeys { kAll, kSplitMeans, kSplitRest };
 
 // ------------------------------------------------------------------ D and dq: a workgroup's rows, all keys in sight, twice
 // SHARE waves have the same rows, and every SHAREth 32 keys of them each.
-template <int D, int WAVES, int KT, AttnKeys KEYS, int SHARE>
+template <int D, int WAVES, int KT, AttnKeys KEYS, int SHARE, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGradients f)
 {
     using Tile = AttnTile<D>;
@@ -76,16 +76,18 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
     const int begin = min(split * run, keys), end = min(begin + run, keys);
     const int seen_least = min(__builtin_amdgcn_readfirstlane(seen), end), seen_most = min(__builtin_amdgcn_readlane(seen, 31), end);
 
+    const AttnHead<D, 2, WHOLE> maps{a.d};
+    const AttnHead<D, 1, WHOLE> ofv{a.e};
     tile_bf16x8 q[2][kSteps], go[2 * kSteps];
     {
-        const uint16_t* p = a.q + (int64_t)(seq.q0 + t) * a.ldq + (int64_t)head * E + (lane >> 5) * 8;
-        const uint16_t* o = f.dout + (int64_t)(seq.q0 + t) * f.lddout + (int64_t)head * E + (lane >> 5) * 8;
+        const uint16_t* p = a.q + (int64_t)(seq.q0 + t) * a.ldq + (int64_t)head * maps.size();
+        const uint16_t* o = f.dout + (int64_t)(seq.q0 + t) * f.lddout + (int64_t)head * ofv.size();
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) q[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + m * D + i * 16);
+            for (int i = 0; i < kSteps; ++i) q[m][i] = maps.values(p, m, (lane >> 5) * 8 + i * 16);
 #pragma unroll
-        for (int i = 0; i < 2 * kSteps; ++i) go[i] = *reinterpret_cast<const tile_bf16x8*>(o + i * 16);
+        for (int i = 0; i < 2 * kSteps; ++i) go[i] = ofv.values(o, 0, (lane >> 5) * 8 + i * 16);
     }
     float lse[2], mean[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -94,11 +96,11 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGr
         lse[m] = seen <= 1 ? 0.0f : lse[m];   // without keys it is -infinity; a single key's map is 2^0
     }
 
-    const char* const keys_at = reinterpret_cast<const char*>(a.k + (int64_t)seq.k0 * a.ldk + head_k * E);
-    const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
+    const char* const keys_at = reinterpret_cast<const char*>(a.k + (int64_t)seq.k0 * a.ldk + head_k * maps.size());
+    const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * ofv.size());
     const auto fetch = [&](AttnLds to, int j0) {
-        Tile::template load<KT, WAVES>(to, wave, lane, keys_at + (int64_t)j0 * a.ldk * 2, (uint32_t)a.ldk * 2, seq.lk - j0);
-        Tile::template load<KT, WAVES>(to + kTile, wave, lane, values_at + (int64_t)j0 * a.ldv * 2, (uint32_t)a.ldv * 2, seq.lk - j0);
+        Tile::template load<KT, WAVES>(to, wave, lane, maps, keys_at + (int64_t)j0 * a.ldk * 2, (uint32_t)a.ldk * 2, seq.lk - j0);
+        Tile::template load<KT, WAVES>(to + kTile, wave, lane, ofv, values_at + (int64_t)j0 * a.ldv * 2, (uint32_t)a.ldv * 2, seq.lk - j0);
     };
 
     const AttnReads<D> reads(lane);
@@ -287,7 +289,7 @@ constexpr int attn_halves(int D) { return D == 128 ? 2 : 1; }
 // A wave a SIMD, with all of its registers.
 constexpr bool attn_room(int D, int waves) { return D == 128 || waves == 2; }
 
-template <int D, int WAVES, int RT>
+template <int D, int WAVES, int RT, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, attn_room(D, WAVES) ? 1 : 2) void k_attn_dkv(AttnGradients f, AttnParts parts)
 {
     using Tile = AttnTile<D>;
@@ -324,16 +326,18 @@ __global__ __launch_bounds__(64 * WAVES, attn_room(D, WAVES) ? 1 : 2) void k_att
     const int of_head = (seq.lq - seeing + RT - 1) / RT, run = (of_head * (int)group + f.splits - 1) / f.splits;
     const int begin = min(split * run, of_head * (int)group), end = min(begin + run, of_head * (int)group);
 
+    const AttnHead<D, 2, WHOLE> maps{a.d};
+    const AttnHead<D, 1, WHOLE> ofv{a.e};
     // the keys stay in registers, the values in LDS, as far as the waves' registers go
     tile_bf16x8 k[2][kSteps];   // of the own map, of the other one
     {
-        const uint16_t* p = a.k + (int64_t)(seq.k0 + key) * a.ldk + head_k * E + (lane >> 5) * 8;
+        const uint16_t* p = a.k + (int64_t)(seq.k0 + key) * a.ldk + head_k * maps.size();
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) k[m][i] = *reinterpret_cast<const tile_bf16x8*>(p + (m ^ half) * D + i * 16);
-        const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * E);
-        Tile::template load<32 * WAVES, WAVES>(values, wave, lane, values_at + (int64_t)(tile * 32 * WAVES) * a.ldv * 2, (uint32_t)a.ldv * 2,
+            for (int i = 0; i < kSteps; ++i) k[m][i] = maps.values(p, m ^ half, (lane >> 5) * 8 + i * 16);
+        const char* const values_at = reinterpret_cast<const char*>(a.v + (int64_t)seq.k0 * a.ldv + head_k * ofv.size());
+        Tile::template load<32 * WAVES, WAVES>(values, wave, lane, ofv, values_at + (int64_t)(tile * 32 * WAVES) * a.ldv * 2, (uint32_t)a.ldv * 2,
                                                seq.lk - tile * 32 * WAVES);
     }
     // a tile's head of the group and first query, which grow without a division
@@ -346,9 +350,9 @@ __global__ __launch_bounds__(64 * WAVES, attn_room(D, WAVES) ? 1 : 2) void k_att
     };
     const auto fetch = [&](AttnLds to, Rows r) {
         const int head = r.head, t0 = r.t0, rows = seq.lq - t0;
-        Tile::template load<RT, WAVES>(to, wave, lane, reinterpret_cast<const char*>(a.q + (int64_t)(seq.q0 + t0) * a.ldq + (int64_t)head * E),
+        Tile::template load<RT, WAVES>(to, wave, lane, maps, reinterpret_cast<const char*>(a.q + (int64_t)(seq.q0 + t0) * a.ldq + (int64_t)head * maps.size()),
                                        (uint32_t)a.ldq * 2, rows);
-        Tile::template load<RT, WAVES>(to + kTile, wave, lane, reinterpret_cast<const char*>(f.dout + (int64_t)(seq.q0 + t0) * f.lddout + (int64_t)head * E),
+        Tile::template load<RT, WAVES>(to + kTile, wave, lane, ofv, reinterpret_cast<const char*>(f.dout + (int64_t)(seq.q0 + t0) * f.lddout + (int64_t)head * ofv.size()),
                                        (uint32_t)f.lddout * 2, rows);
         // a wave a fact, a lane a row
         for (int w = wave; w < 4; w += WAVES) {
@@ -571,25 +575,25 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
     return o;
 }
 
-template <int D, int WAVES, int KT, int SHARE>
+template <int D, int WAVES, int KT, int SHARE, bool WHOLE>
 void launch_dq(const AttnGradients& f, const Shape& s, hipStream_t stream)
 {
     const int blocks = attn_blocks(f.a, f.slots, f.splits);
     if (s.splits_q == 1) {
-        k_attn_dq<D, WAVES, KT, kAll, SHARE><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dq<D, WAVES, KT, kAll, SHARE, WHOLE><<<blocks, 64 * WAVES, 0, stream>>>(f);
         return;
     }
     if constexpr (SHARE > 1) {
-        k_attn_dq<D, WAVES, KT, kSplitMeans, SHARE><<<blocks, 64 * WAVES, 0, stream>>>(f);
-        k_attn_dq<D, WAVES, KT, kSplitRest, SHARE><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dq<D, WAVES, KT, kSplitMeans, SHARE, WHOLE><<<blocks, 64 * WAVES, 0, stream>>>(f);
+        k_attn_dq<D, WAVES, KT, kSplitRest, SHARE, WHOLE><<<blocks, 64 * WAVES, 0, stream>>>(f);
     }
 }
 
-template <int D, int WAVES, int RT>
+template <int D, int WAVES, int RT, bool WHOLE>
 void launch_dkv(const AttnGradients& f, const AttnParts& parts, const Shape& s, hipStream_t stream)
 {
     const int blocks = f.blocks * attn_halves(D) + f.a.heads * parts.k;
-    k_attn_dkv<D, WAVES, RT><<<blocks, 64 * WAVES, 0, stream>>>(f, parts);
+    k_attn_dkv<D, WAVES, RT, WHOLE><<<blocks, 64 * WAVES, 0, stream>>>(f, parts);
 }
 
 void launch_sums(const AttnSum* job, int n, hipStream_t stream)
@@ -604,7 +608,7 @@ void launch_sums(const AttnSum* job, int n, hipStream_t stream)
     k_attn_sum<<<dim3((uint32_t)((most + 255) / 256), n), 256, 0, stream>>>(all);
 }
 
-template <int D, int KT, int RT>
+template <int D, int KT, int RT, bool WHOLE>
 hipError_t launch(AttnGradients f, const AttnParts& parts, const Shape& s, hipStream_t stream)
 {
     const Attn& a = f.a;
@@ -613,18 +617,18 @@ hipError_t launch(AttnGradients f, const AttnParts& parts, const Shape& s, hipSt
     if (a.tokens_q > 0) {
         f.slots = s.slots_q, f.splits = s.splits_q, f.columns = attn_columns(a, f.slots, f.splits);
         if (s.waves_q == kFewWaves)
-            launch_dq<D, 2 * kFewWaves, 64, 2>(f, s, stream);
+            launch_dq<D, 2 * kFewWaves, 64, 2, WHOLE>(f, s, stream);
         else
-            launch_dq<D, kRowWaves, KT, 1>(f, s, stream);
+            launch_dq<D, kRowWaves, KT, 1, WHOLE>(f, s, stream);
         if (s.splits_q > 1) sums[n++] = {f.part, f.dq, f.lddq, a.tokens_q, 2 * a.heads, a.d, D, s.splits_q, a.q_end + a.n_seqs - 1};
     }
     f.slots = s.slots_k, f.splits = s.splits_k, f.columns = attn_columns(a, f.slots, f.splits), f.part = f.part_k;
     f.blocks = (int)round_up(attn_blocks(a, f.slots, f.splits), 8);   // the halves of eight workgroups follow each other
     f.part_v = f.part + (int64_t)s.splits_k * a.tokens_k * a.kv_heads * 2 * D;
     if (s.waves_k == kFewWaves)
-        launch_dkv<D, kFewWaves, 32>(f, parts, s, stream);
+        launch_dkv<D, kFewWaves, 32, WHOLE>(f, parts, s, stream);
     else
-        launch_dkv<D, key_waves(D), RT>(f, parts, s, stream);
+        launch_dkv<D, key_waves(D), RT, WHOLE>(f, parts, s, stream);
     if (s.splits_k > 1 && a.tokens_k > 0) {
         sums[n++] = {f.part, f.dk, f.lddk, a.tokens_k, 2 * a.kv_heads, a.d, D, s.splits_k, a.k_end + a.n_seqs - 1};
         sums[n++] = {f.part_v, f.dv, f.lddv, a.tokens_k, a.kv_heads, a.e, 2 * D, s.splits_k, a.k_end + a.n_seqs - 1};
@@ -662,8 +666,11 @@ hipError_t launch_attn_gradients(const AttnCall& c, hipStream_t stream)
     AttnParts parts;
     for (int p = 0; p < c.k_parts; ++p) parts.end[p] = (int)c.part_end[p];
     parts.k = c.k_parts, parts.G = c.G, parts.ldg = c.ldg;
-    if (D == 32) return launch<32, 64, 64>(f, parts, s, stream);
-    return D == 64 ? launch<64, 64, 64>(f, parts, s, stream) : launch<128, 64, 32>(f, parts, s, stream);
+    const auto of_width = [&]<int WIDTH, int RT>() {
+        return f.a.whole ? launch<WIDTH, 64, RT, true>(f, parts, s, stream) : launch<WIDTH, 64, RT, false>(f, parts, s, stream);
+    };
+    if (D == 32) return of_width.template operator()<32, 64>();
+    return D == 64 ? of_width.template operator()<64, 64>() : of_width.template operator()<128, 32>();
 }
 
 }  // namespace agc

@@ -133,8 +133,8 @@ struct AttnCall {
     int64_t ldg;
     char* workspace;
 };
-// D of the kernels that take heads of d and e values.  Operands of exactly D and 2 D are read where they lie, others are
-// copied to the workspace.
+// D of the kernels that take heads of d and e values.  Operands of exactly D and 2 D are read where they lie, others if their
+// chunks of 16 bytes can be; else they are copied to the workspace.
 int attn_width(int d, int e);
 int64_t attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int d, int e, int gradients);
 hipError_t launch_attn_forward(const AttnCall& c, hipStream_t stream);

@@ -200,7 +200,7 @@ LENS = {
 @pytest.mark.gpu
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("heads,kv_heads,d,e", [(2, 2, 32, 64), (4, 1, 64, 128), (3, 3, 64, 128), (2, 1, 128, 256), (7, 1, 20, 33), (2, 2, 1, 1), (6, 2, 128, 7),
-                                                (2, 1, 40, 200), (5, 5, 64, 100)])
+                                                (2, 1, 40, 200), (5, 5, 64, 100), (6, 2, 40, 72), (2, 2, 8, 16), (3, 1, 96, 128)])
 @pytest.mark.parametrize("lens", list(LENS))
 def test_against_the_formulas(lens, heads, kv_heads, d, e, causal):
     import torch
@@ -214,7 +214,8 @@ def test_against_the_formulas(lens, heads, kv_heads, d, e, causal):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("d,e,gap,shift", [(64, 128, 8, 8), (64, 128, 64, 16), (20, 40, 1, 1), (32, 60, 8, 0), (33, 64, 8, 8), (128, 256, 24, 40)])
+@pytest.mark.parametrize("d,e,gap,shift", [(64, 128, 8, 8), (64, 128, 64, 16), (20, 40, 1, 1), (32, 60, 8, 0), (33, 64, 8, 8), (128, 256, 24, 40), (40, 72, 24, 16),
+                                             (40, 72, 4, 0), (40, 72, 8, 4), (8, 8, 0, 0)])
 def test_strides_and_rows_behind_the_last_sequence(d, e, gap, shift):
     """NaN lies behind the sequences, between the rows and round the tensors."""
     import torch
@@ -225,6 +226,21 @@ def test_strides_and_rows_behind_the_last_sequence(d, e, gap, shift):
     # rows behind belong to a partition and count for nothing
     parts = [20, c.nq - 5, c.nq]
     c.check_gradients(*c.gradients(parts), parts)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,e", [(24, 40), (40, 72), (56, 64), (24, 120), (80, 136), (120, 248)])
+@pytest.mark.parametrize("lens", ["edge", "empty", "one_query", "long_both"])
+def test_widths_filled_up_on_the_way_or_in_the_workspace(d, e, lens):
+    """Heads whose chunks of 16 bytes can be read where they lie, and the same ones two bytes off: the same sums, bit for bit."""
+    import torch
+    got = []
+    for shift in (8, 9):
+        c = Case(LENS[lens], 4, 2, d, e, True, gap=8, shift=shift, seed=e)
+        out = c.forward()
+        got.append([out, c.lse, *(torch.from_numpy(g) if isinstance(g, np.ndarray) else g for g in c.gradients([c.nq // 2, c.nq]))])
+    for one, other in zip(*got):
+        assert torch.equal(one, other)
 
 
 @pytest.mark.gpu
