@@ -393,7 +393,8 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
  *   out_dev    device, tokens_q x (heads * value_dim), row stride ldo; overwritten
  *   lse_dev    device, (2 * heads) x tokens_q floats, or NULL: receives log2 of the sum over keys of 2^(scale q_m k_m log2 e) of
  *              map m of head h in row 2 h + m, -infinity without keys; what the gradients take
- *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 0) bytes, 256-byte aligned
+ *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 0) bytes, 256-byte aligned; scratch, which calls that may run at
+ *              the same time, captured ones among them, do not share
  * scale is finite, 0 or more.  Scores, maxima, sums and out are held in binary32; the maps enter their product with v as
  * bfloat16, out is rounded once.  The order of the sums is fixed.  NaN or infinity in a sequence reaches that sequence's results
  * alone.  out and lse must not overlap what is read.
