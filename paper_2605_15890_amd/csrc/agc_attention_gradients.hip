@@ -44,7 +44,7 @@ struct AttnGradients {
 enum AttnKeys { kAll, kSplitMeans, kSplitRest };
 
 // ------------------------------------------------------------------ D and dq: a workgroup's rows, all keys in sight, twice
-// SHARE waves have the same rows, and every SHAREth 32 keys of them each.
+// SHARE waves have the same rows, and every SHAREth 32 keys of them each, as in the forward pass (37 instead of 50 us there).
 template <int D, int WAVES, int KT, AttnKeys KEYS, int SHARE, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, D == 128 ? 1 : 2) void k_attn_dq(AttnGradients f)
 {

@@ -498,10 +498,13 @@ def raw(grad=False, q=256, ldq=512, k=256, ldk=256, v=256, ldv=256, nq=3, nk=4, 
     (dict(heads=3), -2), (dict(heads=0), -2), (dict(kv=0), -2), (dict(d=0), -2), (dict(d=129), -2), (dict(e=0), -2), (dict(e=257), -2),
     (dict(nq=2 ** 26, heads=32, ldq=4096), -2), (dict(nk=2 ** 26, heads=64, kv=32, ldk=4096, ldv=4096, ldq=8192), -2),
     (dict(nq=2 ** 26, heads=18, ldq=4096), -2), (dict(n=2 ** 19, heads=8, kv=8, ldq=1024, ldk=1024, ldv=1024), -2),
-    (dict(n=2 ** 20, heads=32, kv=32, ldq=4096, ldk=4096, ldv=4096), -2), (dict(scale=math.inf), -1), (dict(scale=math.nan), -1), (dict(scale=-0.5), -1),
+    (dict(n=2 ** 20, heads=32, kv=32, ldq=4096, ldk=4096, ldv=4096), -2), (dict(scale=math.inf), -1), (dict(scale=math.nan), -1),
+    (dict(scale=-0.5), -1),
     (dict(q=0), -1), (dict(k=0), -1), (dict(v=0), -1), (dict(lam=0), -1), (dict(qe=0), -1), (dict(ke=0), -1), (dict(ws=0), -1),
-    (dict(ldq=2 ** 24 + 8), -2), (dict(ldk=2 ** 24 + 8), -2), (dict(ldv=2 ** 24 + 8), -2), (dict(ldq=504), -2), (dict(ldk=248), -2), (dict(ldv=248), -2), (dict(q=258), -4), (dict(k=264), -4), (dict(v=258), -4), (dict(ldq=516), -4),
-    (dict(ldk=257), -4), (dict(ldv=260), -4), (dict(q=257, d=60), -4), (dict(lam=6), -4), (dict(qe=2), -4), (dict(ke=2), -4), (dict(lse=2), -4), (dict(ws=128), -4)])
+    (dict(ldq=2 ** 24 + 8), -2), (dict(ldk=2 ** 24 + 8), -2), (dict(ldv=2 ** 24 + 8), -2), (dict(ldq=504), -2), (dict(ldk=248), -2),
+    (dict(ldv=248), -2), (dict(q=258), -4), (dict(k=264), -4), (dict(v=258), -4), (dict(ldq=516), -4),
+    (dict(ldk=257), -4), (dict(ldv=260), -4), (dict(q=257, d=60), -4), (dict(lam=6), -4), (dict(qe=2), -4), (dict(ke=2), -4),
+    (dict(lse=2), -4), (dict(ws=128), -4)])
 def test_refusals(grad, change, status):
     assert raw(grad, **change) == status
 
@@ -512,9 +515,12 @@ def test_refusals_of_the_forward_pass(change, status):
 
 
 @pytest.mark.parametrize("change,status", [
-    (dict(parts=None), -1), (dict(parts=()), -2), (dict(parts=(2,)), -2), (dict(parts=(3, 2)), -2), (dict(parts=(2, 1, 3)), -2), (dict(parts=(3,) * 257), -2), (dict(parts=(3,) * 256, heads=2 ** 14, ldq=2 ** 21, lddout=2 ** 21, lddq=2 ** 21, ldg=2 ** 14), -2),
-    (dict(dout=0), -1), (dict(lse=0), -1), (dict(dq=0), -1), (dict(dk=0), -1), (dict(dv=0), -1), (dict(G=0), -1), (dict(lddout=504), -2), (dict(lddout=2 ** 24 + 8), -2), (dict(lddq=511), -2),
-    (dict(lddk=255), -2), (dict(lddv=255), -2), (dict(ldg=3), -2), (dict(dout=258), -4), (dict(lddout=516), -4), (dict(dq=1), -4), (dict(dk=1), -4), (dict(dv=1), -4),
+    (dict(parts=None), -1), (dict(parts=()), -2), (dict(parts=(2,)), -2), (dict(parts=(3, 2)), -2), (dict(parts=(2, 1, 3)), -2),
+    (dict(parts=(3,) * 257), -2), (dict(parts=(3,) * 256, heads=2 ** 14, ldq=2 ** 21, lddout=2 ** 21, lddq=2 ** 21, ldg=2 ** 14), -2),
+    (dict(dout=0), -1), (dict(lse=0), -1), (dict(dq=0), -1), (dict(dk=0), -1), (dict(dv=0), -1), (dict(G=0), -1), (dict(lddout=504), -2),
+    (dict(lddout=2 ** 24 + 8), -2), (dict(lddq=511), -2),
+    (dict(lddk=255), -2), (dict(lddv=255), -2), (dict(ldg=3), -2), (dict(dout=258), -4), (dict(lddout=516), -4), (dict(dq=1), -4),
+    (dict(dk=1), -4), (dict(dv=1), -4),
     (dict(G=2), -4)])
 def test_refusals_of_the_gradients(change, status):
     assert raw(True, **change) == status
