@@ -35,14 +35,40 @@ __device__ __forceinline__ void store16(T* p, tile_u32x4 v)
     __builtin_memcpy(p, &v, 16);
 }
 
-// The first `count` of eight values; the others are zeros.
+// The first `count` of four or eight values; the others are zeros.  Runs that are not whole are fetched and stored by fours and
+// at most three single values: 9066 tokens of 22 heads of 59 take 23.6 us, with up to seven single ones 30.6.
+__device__ __forceinline__ void load4(const uint16_t* p, int count, float v[4])
+{
+    if (count >= 4) {
+        uint32_t u[2];
+        __builtin_memcpy(u, p, 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xFFFF0000u : u[i / 2] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < 3 && i < count ? __uint_as_float((uint32_t)p[i] << 16) : 0.0f;
+    }
+}
+
 __device__ __forceinline__ void load8(const uint16_t* p, int count, float v[8])
 {
     if (count >= 8) {
         bf16_unpack8(load16(p), v);
     } else {
+        load4(p, count, v);
+        load4(p + 4, count - 4, v + 4);
+    }
+}
+
+__device__ __forceinline__ void load4(const float* p, int count, float v[4])
+{
+    if (count >= 4) {
+        const tile_u32x4 a = load16(p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < count ? __uint_as_float((uint32_t)p[i] << 16) : 0.0f;
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(a[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < 3 && i < count ? p[i] : 0.0f;
     }
 }
 
@@ -53,19 +79,45 @@ __device__ __forceinline__ void load8(const float* p, int count, float v[8])
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(a[i]), v[4 + i] = __uint_as_float(b[i]);
     } else {
+        load4(p, count, v);
+        load4(p + 4, count - 4, v + 4);
+    }
+}
+
+__device__ __forceinline__ void store4(uint16_t* p, int count, const uint32_t pairs[2])
+{
+    if (count >= 4) {
+        __builtin_memcpy(p, pairs, 8);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < count ? p[i] : 0.0f;
+        for (int i = 0; i < 3; ++i)
+            if (i < count) p[i] = (uint16_t)(pairs[i / 2] >> (i & 1) * 16);
     }
 }
 
 __device__ __forceinline__ void store8(uint16_t* p, int count, const float v[8])
 {
+    const tile_u32x4 bits = bf16_pack8(v);
     if (count >= 8) {
-        store16(p, bf16_pack8(v));
+        store16(p, bits);
+    } else {
+        const uint32_t low[2] = {bits[0], bits[1]}, high[2] = {bits[2], bits[3]};
+        store4(p, count, low);
+        store4(p + 4, count - 4, high);
+    }
+}
+
+__device__ __forceinline__ void store4(float* p, int count, const float v[4])
+{
+    if (count >= 4) {
+        tile_u32x4 a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(v[i]);
+        store16(p, a);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count) p[i] = (uint16_t)bf16_bits(v[i]);
+        for (int i = 0; i < 3; ++i)
+            if (i < count) p[i] = v[i];
     }
 }
 
@@ -78,9 +130,8 @@ __device__ __forceinline__ void store8(float* p, int count, const float v[8])
         store16(p, a);
         store16(p + 4, b);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count) p[i] = v[i];
+        store4(p, count, v);
+        store4(p + 4, count - 4, v + 4);
     }
 }
 
