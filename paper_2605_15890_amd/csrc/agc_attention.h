@@ -25,8 +25,6 @@ namespace agc {
 typedef float attn_f32x16 __attribute__((ext_vector_type(16)));
 typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLog2e = 1.44269504088896f;
-
 // What the kernels know of a call; operands as they are read, with 16-byte aligned rows.
 struct Attn {
     const uint16_t *q, *k, *v;
@@ -39,7 +37,7 @@ struct Attn {
     Divider group;        // heads that share keys, and the division of row numbers by them
     int causal;
     float scale;          // of the scores
-    float to_log2;        // scale * log2(e): the maps are formed with powers of two
+    float to_log2;        // scale * log2(e), above zero: the maps are formed with powers of two
 };
 
 // A sequence's place in a tile's coordinates.

@@ -109,6 +109,8 @@ struct DropoutCall {
 hipError_t launch_dropout(const DropoutCall& c, hipStream_t stream);
 
 // ------------------------------------------------------------------ differential attention
+constexpr float kLog2e = 1.44269504088896f;
+
 struct AttnCall {
     const void *q, *k, *v;     // bfloat16
     int64_t ldq, ldk, ldv;

@@ -1,0 +1,65 @@
+"""Differential attention at the ends of its ranges, against the formulas in 64 bits; tolerances are those of
+test_gpu_attention.py, whose oracle and operands these tests use."""
+import numpy as np
+import pytest
+
+from test_gpu_attention import Case
+
+
+# ------------------------------------------------------------------ the scale of the scores
+SCALE_LENS = [(90, 130), (33, 33), (1, 700), (40, 7), (0, 5), (64, 64)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -149, 2.0 ** -40])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,d,e", [(2, 2, 32, 64), (4, 2, 64, 128), (2, 1, 128, 256), (3, 1, 20, 33), (2, 1, 40, 72)])
+def test_scales_that_make_the_maps_uniform(scale, causal, heads, kv_heads, d, e):
+    """Every key in sight counts alike, those out of sight not at all."""
+    c = Case(SCALE_LENS, heads, kv_heads, d, e, causal)
+    c.scale = float(np.float32(scale))
+    c.head = (*c.head[:8], c.scale, causal)
+    c.check_forward(c.forward())
+    parts = [50, c.nq]
+    c.check_gradients(*c.gradients(parts), parts)
+
+
+@pytest.mark.gpu
+def test_scale_zero_with_scores_of_any_size():
+    """Scores of up to 2^126 are still all alike."""
+    c = Case([(70, 70), (5, 300)], 2, 1, 64, 128, True)
+    for t in (c.q, c.k):
+        t.mul_(2.0 ** 60)
+    c.qh, c.kh, c.scale = c.q.double().cpu().numpy(), c.k.double().cpu().numpy(), 0.0
+    c.head = (*c.head[:8], 0.0, True)
+    c.check_forward(c.forward())
+    c.q.mul_(2.0 ** -60)     # the products of dk stay finite
+    c.qh = c.q.double().cpu().numpy()
+    c.check_gradients(*c.gradients([c.nq]), [c.nq])
+
+
+@pytest.mark.gpu
+def test_scale_zero_in_large_workgroups():
+    """Under the causal mask query i of as many keys gets the mean of the first i + 1 values times 1 - lambda: a map's value
+    and the result are rounded, 2^-8 each."""
+    import torch
+    n, heads, seqs = 1300, 8, 8
+    c = Case([(n, n)] * seqs, heads, heads, 64, 128, True)
+    c.head = (*c.head[:8], 0.0, True)
+    out = c.forward()[:, :heads * 128].double().view(seqs, n, heads, 128)
+    v = c.v.double().view(seqs, n, heads, 128)
+    count = torch.arange(1, n + 1, device="cuda").double()[:, None, None]
+    lam = c.lam.double()[:, None]
+    want = v.cumsum(1) / count * (1 - lam)
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -8 + c.full({"A": 0.0})) * v.abs().cumsum(1) / count * (1 + lam.abs())
+    assert bool(((out - want).abs() <= tol).all())
+    lse = c.lse.double().view(heads, 2, seqs, n)
+    assert float((lse - torch.log2(count[:, 0, 0])).abs().max()) <= 2.0 ** -20
+    dq, dk, dv, G = c.gradients([c.nq])
+    assert not dq.any() and not dk.any()
+    # every key's dv: the sum over the queries from it on of (1 - lambda) dout / (i + 1)
+    part = (c.dout.double().view(seqs, n, heads, 128) / count).flip(1).cumsum(1).flip(1)
+    size = (c.dout.double().view(seqs, n, heads, 128).abs() / count).flip(1).cumsum(1).flip(1)
+    dv = dv.double().view(seqs, n, heads, 128)
+    tol = 2.0 ** -8 * (part * (1 - lam)).abs() + 2.0 ** -16 * size * (1 - lam).abs() + c.full({"A": 0.0}) * size * (1 + lam.abs())
+    assert bool(((dv - part * (1 - lam)).abs() <= tol).all())
