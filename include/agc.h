@@ -395,9 +395,9 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
  *              map m of head h in row 2 h + m, -infinity without keys; what the gradients take
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 0) bytes, 256-byte aligned; scratch, which calls that may run at
  *              the same time, captured ones among them, do not share
- * scale is finite, 0 or more.  Scores, maxima, sums and out are held in binary32; the maps enter their product with v as
- * bfloat16, out is rounded once.  The order of the sums is fixed.  NaN or infinity in a sequence reaches that sequence's results
- * alone.  out and lse must not overlap what is read.
+ * scale is 0 or more, and scale * log2(e) finite in binary32.  Scores, maxima, sums and out are held in binary32; the maps
+ * enter their product with v as bfloat16, out is rounded once.  The order of the sums is fixed.  NaN or infinity in a sequence
+ * reaches that sequence's results alone.  out and lse must not overlap what is read.
  * Row strides of q, k, v up to 2^24, 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads up to 2^30,
  * 1 <= n_seqs <= 2^20, n_seqs * kv_heads up to 2^21, heads a multiple of kv_heads, 1 <= head_dim <= 128, 1 <= value_dim <= 256. */
 int64_t agc_diff_attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int head_dim,

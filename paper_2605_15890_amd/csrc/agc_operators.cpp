@@ -72,7 +72,8 @@ agc_status attn_arguments(const char* name, const agc::AttnCall& c, bool gradien
     // a grid has fewer than 2^32 threads: at most two a row of a head, and five small workgroups of 256 a sequence and key head
     if (c.tokens_q * c.heads > (1 << 30) || c.tokens_k * c.kv_heads > (1 << 30) || (int64_t)c.n_seqs * c.kv_heads > (1 << 21))
         return refuse(AGC_ESHAPE, n + ": tokens times heads must be up to 2^30, n_seqs * kv_heads up to 2^21");
-    if (!std::isfinite(c.scale) || c.scale < 0) return refuse(AGC_EINVAL, n + ": scale must be finite and not negative");
+    if (!std::isfinite(c.scale * agc::kLog2e) || c.scale < 0)
+        return refuse(AGC_EINVAL, n + ": scale must not be negative, and finite times log2(e)");
     if ((c.tokens_q > 0 && !c.q) || (c.tokens_k > 0 && (!c.k || !c.v)) || !c.lambda || !c.q_end || !c.k_end || !c.workspace)
         return refuse(AGC_EINVAL, n + ": null pointer");
     const int64_t row_q = (int64_t)2 * c.heads * c.d, row_k = (int64_t)2 * c.kv_heads * c.d;

@@ -3,7 +3,8 @@ test_gpu_attention.py, whose oracle and operands these tests use."""
 import numpy as np
 import pytest
 
-from test_gpu_attention import Case
+from paper_2605_15890_amd import api
+from test_gpu_attention import Case, raw
 
 
 # ------------------------------------------------------------------ the scale of the scores
@@ -63,3 +64,10 @@ def test_scale_zero_in_large_workgroups():
     dv = dv.double().view(seqs, n, heads, 128)
     tol = 2.0 ** -8 * (part * (1 - lam)).abs() + 2.0 ** -16 * size * (1 - lam).abs() + c.full({"A": 0.0}) * size * (1 + lam.abs())
     assert bool(((dv - part * (1 - lam)).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
+def test_scales_whose_binary_one_is_infinite_are_refused(grad, scale):
+    """Scores enter powers of two: their factor is scale * log2(e)."""
+    assert raw(grad, scale=scale) == api.AGC_EINVAL
