@@ -66,6 +66,32 @@ def test_scale_zero_in_large_workgroups():
     assert bool(((dv - part * (1 - lam)).abs() <= tol).all())
 
 
+# ------------------------------------------------------------------ rows far apart
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,e,far", [(32, 64, "v"), (64, 128, "v"), (64, 128, "k"), (24, 40, "v"), (64, 128, "q"), (64, 128, "dout")])
+def test_partial_tiles_of_rows_at_the_largest_stride(d, e, far):
+    """The large keys' pass has 256 values a workgroup, and 200 of them span 2^32 bytes at a stride of 2^24: the same results, bit
+    for bit, as from rows side by side."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    heads = 96
+    c = Case([(90, 712)] if far in "kv" else [(712, 712)], heads, heads, d, e, False)
+    want, got = [], []
+    for which in (want, got):
+        out = c.forward()
+        dq, dk, dv, G = c.gradients([c.nq])
+        which.extend((out, c.lse.clone(), dq, dk, dv, torch.from_numpy(G)))
+        if which is want:
+            near = getattr(c, far)
+            wide = torch.empty(len(near), 1 << 24, dtype=torch.bfloat16, device="cuda")
+            moved = wide[:, 4096:4096 + near.shape[1]]
+            moved.copy_(near)
+            setattr(c, far, moved)
+            c.head = (c.q, c.k, c.v, *c.head[3:])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("grad", [False, True])
 @pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
 def test_scales_whose_binary_one_is_infinite_are_refused(grad, scale):
