@@ -307,7 +307,8 @@ agc_status agc_dropout(const void* x_dev, int x_type, int64_t ldx, const void* r
     if (rows > 0 && (!x_dev || !out_dev)) return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
     if (misaligned(x_dev, bytes_of(x_type)) || misaligned(out_dev, bytes_of(out_type)) || misaligned(residual_dev, bytes_of(out_type)))
         return refuse(AGC_EALIGN, std::string(name) + ": a pointer is not aligned to its elements");
-    if (rows > 1 && ((x_dev == out_dev && (ldx != ldo || x_type != out_type)) || (residual_dev == out_dev && ldr != ldo)))
+    // the stride of a single row says nothing
+    if (rows > 0 && ((x_dev == out_dev && (x_type != out_type || (rows > 1 && ldx != ldo))) || (rows > 1 && residual_dev == out_dev && ldr != ldo)))
         return refuse(AGC_EINVAL, std::string(name) + ": in place the types and row strides must be equal");
     if (rows == 0) return AGC_OK;
     agc::DropoutCall c{};

@@ -61,3 +61,10 @@ def test_forward_pass_of_few_tokens_leaves_the_workspace_alone(tokens):
     h, ws = torch.empty(tokens, 30, dtype=bf16, device="cuda"), torch.full((256,), 9, dtype=torch.uint8, device="cuda")
     api.agc_gated_forward(x, w, w, "silu", h, ws)
     assert torch.all(ws == 9) and torch.isfinite(h.float()).all()
+
+
+@pytest.mark.parametrize("rows", [1, 2])
+@pytest.mark.parametrize("x_type,out_type", [(api.AGC_TYPE_BF16, api.AGC_TYPE_F32), (api.AGC_TYPE_F32, api.AGC_TYPE_BF16)])
+def test_dropout_in_place_of_another_type_is_refused(rows, x_type, out_type):
+    """A row's values would be written over others that are not read yet, in a single row too; nothing is dereferenced."""
+    assert api.load().agc_dropout(64, x_type, 64, None, 64, rows, 64, 0.5, 1, 2, 3, 64, out_type, 64, None) == api.AGC_EINVAL
