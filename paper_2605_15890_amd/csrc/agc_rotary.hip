@@ -3,8 +3,8 @@
 // gradient is the turn back (inverse), with the same amplitude.
 //
 // turns_i is a position's share of a whole turn as 64 binary places behind the point: the product wraps at whole turns by
-// itself, so the angle at position 2^31 is as exact as at position 1 (2^-34 of a turn), where a binary32 angle would be off
-// by whole turns.  The angle is then brought to an eighth of a turn round the nearest quarter and enters two Taylor sums
+// itself, so the angle at position 2^31 is as exact as at position 1, where a binary32 angle would be off by whole turns.  The
+// angle is then brought to an eighth of a turn round the nearest quarter, rounded to binary32, and enters two Taylor sums
 // (sine to the ninth power, cosine to the tenth: 2e-9 and 2e-10 at pi/4).
 //
 // Bound by memory.  A workgroup has a few tokens; each thread fetches a piece of 2 x 8 values, the sines of all pairs are formed
@@ -39,7 +39,9 @@ __device__ __forceinline__ void turn(uint64_t phase, float amplitude, float& c, 
 {
     const uint32_t quarter = (uint32_t)((phase + ((uint64_t)1 << 61)) >> 62);
     const int64_t rest = (int64_t)(phase - ((uint64_t)quarter << 62));
-    const float x = (float)(int32_t)(rest >> 30) * 3.6572951981e-10f;   // 2 pi / 2^34
+    // rest = 2^32 top + low with signs of their own, times 2 pi / 2^64: small angles keep their 24 bits too
+    const int32_t low = (int32_t)rest, top = (int32_t)(rest >> 32) + (low < 0);
+    const float x = fmaf((float)top, 1.4629180793e-9f, (float)low * 3.4061215801e-19f);
     const float y = x * x;
     float sine = fmaf(y, 2.7557319224e-6f, -1.9841269841e-4f);
     sine = fmaf(y, sine, 8.3333333333e-3f);
