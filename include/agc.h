@@ -398,8 +398,9 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
  * scale is 0 or more, and scale * log2(e) finite in binary32.  Scores, maxima, sums and out are held in binary32; the maps
  * enter their product with v as bfloat16, out is rounded once.  The order of the sums is fixed.  NaN or infinity in a sequence
  * reaches that sequence's results alone.  out and lse must not overlap what is read.
- * Row strides of q, k, v up to 2^24, 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads up to 2^30,
- * 1 <= n_seqs <= 2^20, n_seqs * kv_heads up to 2^21, heads a multiple of kv_heads, 1 <= head_dim <= 128, 1 <= value_dim <= 256. */
+ * Row strides of q, k, v up to 2^24, 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads up to 2^30 (2^29
+ * where head_dim is above 64 or value_dim above 128), 1 <= n_seqs <= 2^20, n_seqs * kv_heads up to 2^21, heads a multiple of
+ * kv_heads, 1 <= head_dim <= 128, 1 <= value_dim <= 256. */
 int64_t agc_diff_attn_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv_heads, int head_dim,
                                       int value_dim, int gradients);
 agc_status agc_diff_attn_forward(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv,
@@ -419,7 +420,7 @@ agc_status agc_diff_attn_forward(const void* q_dev, int64_t ldq, const void* k_d
  *              may overlap what is read
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 1) bytes, 256-byte aligned (enough for the forward pass too)
  * The maps and dS enter the products with 16 bits, so that results are rounded once; sums are binary32 in a fixed order.
- * 1 <= k_parts <= 256, heads * k_parts up to 2^21. */
+ * 1 <= k_parts <= 256, heads * k_parts below 2^21. */
 agc_status agc_diff_attn_partial_gradients(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev,
                                            int64_t ldv, int64_t tokens_q, int64_t tokens_k, int heads, int kv_heads,
                                            int head_dim, int value_dim, const float* lambda_dev, const int32_t* q_end_dev,

@@ -15,8 +15,7 @@
 // eight neighbouring keys twice, which is what the next product's operand wants, and P never leaves the registers.
 #pragma once
 
-#include <algorithm>
-
+#include "agc_dispatch.h"
 #include "agc_operators.h"
 #include "agc_vector.h"
 
@@ -106,18 +105,6 @@ __device__ __forceinline__ AttnPlace attn_place(const Attn& a, int id, int slots
     const int step = i / rows, row = i - step * rows, head = row / a.n_seqs, column = step * share + x % share;
     const int slot = (row - head * a.n_seqs) * columns + column;
     return {column < columns && slot < slots ? slot : -1, a.kv_heads >= 8 ? x * (a.kv_heads / 8) + head : x / share, 0};
-}
-
-// Columns of a launch, and its workgroups.
-inline int attn_columns(const Attn& a, int slots, int splits)
-{
-    const bool whole = a.kv_heads % 8 == 0 || 8 % a.kv_heads == 0;
-    return a.causal && splits == 1 && whole && slots * a.kv_heads >= 512 ? (slots + a.n_seqs - 1) / a.n_seqs : 0;
-}
-inline int attn_blocks(const Attn& a, int slots, int splits)
-{
-    const int columns = attn_columns(a, slots, splits), share = std::max(8 / a.kv_heads, 1);
-    return columns ? 8 * std::max(a.kv_heads / 8, 1) * a.n_seqs * ((columns + share - 1) / share) : slots * a.kv_heads * splits;
 }
 
 // Keys in sight of query t.

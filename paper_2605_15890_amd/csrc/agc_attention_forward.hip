@@ -343,8 +343,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnForward f)
 template <int D, int WAVES, int KT, int SHARE>
 hipError_t launch(AttnForward f, hipStream_t stream)
 {
-    f.columns = attn_columns(f.a, f.slots, f.splits);
-    const int blocks = attn_blocks(f.a, f.slots, f.splits);
+    f.columns = attn_columns(f.a.causal, f.a.n_seqs, f.a.kv_heads, f.slots, f.splits);
+    const int blocks = attn_blocks(f.columns, f.a.n_seqs, f.a.kv_heads, f.slots, f.splits);
     if (f.a.whole)
         k_attn_forward<D, WAVES, KT, SHARE, true><<<blocks, 64 * WAVES, 0, stream>>>(f);
     else

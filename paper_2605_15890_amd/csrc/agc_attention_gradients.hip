@@ -578,7 +578,7 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
 template <int D, int WAVES, int KT, int SHARE, bool WHOLE>
 void launch_dq(const AttnGradients& f, const Shape& s, hipStream_t stream)
 {
-    const int blocks = attn_blocks(f.a, f.slots, f.splits);
+    const int blocks = attn_blocks(f.columns, f.a.n_seqs, f.a.kv_heads, f.slots, f.splits);
     if (s.splits_q == 1) {
         k_attn_dq<D, WAVES, KT, kAll, SHARE, WHOLE><<<blocks, 64 * WAVES, 0, stream>>>(f);
         return;
@@ -615,15 +615,15 @@ hipError_t launch(AttnGradients f, const AttnParts& parts, const Shape& s, hipSt
     AttnSum sums[3];
     int n = 0;
     if (a.tokens_q > 0) {
-        f.slots = s.slots_q, f.splits = s.splits_q, f.columns = attn_columns(a, f.slots, f.splits);
+        f.slots = s.slots_q, f.splits = s.splits_q, f.columns = attn_columns(a.causal, a.n_seqs, a.kv_heads, f.slots, f.splits);
         if (s.waves_q == kFewWaves)
             launch_dq<D, 2 * kFewWaves, 64, 2, WHOLE>(f, s, stream);
         else
             launch_dq<D, kRowWaves, KT, 1, WHOLE>(f, s, stream);
         if (s.splits_q > 1) sums[n++] = {f.part, f.dq, f.lddq, a.tokens_q, 2 * a.heads, a.d, D, s.splits_q, a.q_end + a.n_seqs - 1};
     }
-    f.slots = s.slots_k, f.splits = s.splits_k, f.columns = attn_columns(a, f.slots, f.splits), f.part = f.part_k;
-    f.blocks = (int)round_up(attn_blocks(a, f.slots, f.splits), 8);   // the halves of eight workgroups follow each other
+    f.slots = s.slots_k, f.splits = s.splits_k, f.columns = attn_columns(a.causal, a.n_seqs, a.kv_heads, f.slots, f.splits), f.part = f.part_k;
+    f.blocks = (int)round_up(attn_blocks(f.columns, a.n_seqs, a.kv_heads, f.slots, f.splits), 8);   // the halves of eight workgroups follow each other
     f.part_v = f.part + (int64_t)s.splits_k * a.tokens_k * a.kv_heads * 2 * D;
     if (s.waves_k == kFewWaves)
         launch_dkv<D, kFewWaves, 32, WHOLE>(f, parts, s, stream);

@@ -289,6 +289,25 @@ inline int ls_fold(int64_t n_rows, int64_t rows_per_part, int n_feat)
 // be eight times as many workgroups (2^17 x 8192, one part: 387 us, now 346; 65536 x 4096, 8 parts 92, now 87).
 constexpr bool ls_reduce_few(int wg_per_part) { return wg_per_part <= 16; }
 
+// Differential attention: whether each XCD gets whole key heads (or a share of one's tiles), in columns of tiles as if sequences
+// were alike, and how many (0: it gets a run of tiles).  Filled up to whole rounds of the XCDs, eight times as many workgroups
+// as there are sequences at least: they stay below 2^22, with up to 512 threads each and rows of G behind them below the
+// 2^32 threads of a launch.
+inline int attn_columns(bool causal, int n_seqs, int kv_heads, int slots, int splits)
+{
+    const int64_t columns = ((int64_t)slots + n_seqs - 1) / n_seqs, share = kv_heads < 8 ? 8 / kv_heads : 1;
+    const int64_t rows = (int64_t)(kv_heads < 8 ? 1 : kv_heads / 8) * n_seqs, blocks = 8 * rows * ((columns + share - 1) / share);
+    const bool whole = kv_heads % 8 == 0 || 8 % kv_heads == 0;
+    return causal && splits == 1 && whole && (int64_t)slots * kv_heads >= 512 && blocks < (1 << 22) ? (int)columns : 0;
+}
+
+// Workgroups of such a launch.
+inline int attn_blocks(int columns, int n_seqs, int kv_heads, int slots, int splits)
+{
+    const int share = kv_heads < 8 ? 8 / kv_heads : 1, rows = (kv_heads < 8 ? 1 : kv_heads / 8) * n_seqs;
+    return columns ? 8 * rows * ((columns + share - 1) / share) : slots * kv_heads * splits;
+}
+
 // A launch takes fewer than 2^32 threads along x: more workgroups lie along y as well, x * y of them or a few more.
 struct FoldedGrid {
     unsigned x, y;

@@ -69,9 +69,11 @@ agc_status attn_arguments(const char* name, const agc::AttnCall& c, bool gradien
         return refuse(AGC_ESHAPE, n + ": tokens_q and tokens_k must be 0..2^26, n_seqs 1..2^20");
     if (c.heads < 1 || c.kv_heads < 1 || c.heads > kMostWidth || c.heads % c.kv_heads || c.d < 1 || c.d > 128 || c.e < 1 || c.e > 256)
         return refuse(AGC_ESHAPE, n + ": heads must be a multiple of kv_heads, head_dim 1..128, value_dim 1..256");
-    // a grid has fewer than 2^32 threads: at most two a row of a head, and five small workgroups of 256 a sequence and key head
-    if (c.tokens_q * c.heads > (1 << 30) || c.tokens_k * c.kv_heads > (1 << 30) || (int64_t)c.n_seqs * c.kv_heads > (1 << 21))
-        return refuse(AGC_ESHAPE, n + ": tokens times heads must be up to 2^30, n_seqs * kv_heads up to 2^21");
+    // a grid has fewer than 2^32 threads: at most two a row of a head (four of wide ones), and five small workgroups of 256 a
+    // sequence and key head
+    const int D = agc::attn_width(c.d, c.e), most = D == 128 ? 1 << 29 : 1 << 30;
+    if (c.tokens_q * c.heads > most || c.tokens_k * c.kv_heads > most || (int64_t)c.n_seqs * c.kv_heads > (1 << 21))
+        return refuse(AGC_ESHAPE, n + ": tokens times heads must be up to 2^30 (2^29 of wide ones), n_seqs * kv_heads up to 2^21");
     if (!std::isfinite(c.scale * agc::kLog2e) || c.scale < 0)
         return refuse(AGC_EINVAL, n + ": scale must not be negative, and finite times log2(e)");
     if ((c.tokens_q > 0 && !c.q) || (c.tokens_k > 0 && (!c.k || !c.v)) || !c.lambda || !c.q_end || !c.k_end || !c.workspace)
@@ -80,7 +82,6 @@ agc_status attn_arguments(const char* name, const agc::AttnCall& c, bool gradien
     if (c.ldq < row_q || c.ldk < row_k || c.ldv < (int64_t)c.kv_heads * c.e) return refuse(AGC_ESHAPE, n + ": a row stride is smaller than the row");
     if (std::max({c.ldq, c.ldk, c.ldv, c.lddout}) > (1 << 24)) return refuse(AGC_ESHAPE, n + ": row strides must be up to 2^24");
     // heads of just the kernels' widths are read where they lie, 16 bytes at a time
-    const int D = agc::attn_width(c.d, c.e);
     const uintptr_t unit_d = c.d == D ? 16 : 2, unit_e = c.e == 2 * D ? 16 : 2;
     const auto strided = [](int64_t ld, int64_t rows, uintptr_t unit) { return unit == 16 && rows > 1 && ld % 8; };
     if (misaligned(c.q, unit_d) || misaligned(c.k, unit_d) || misaligned(c.v, unit_e) || strided(c.ldq, c.tokens_q, unit_d) ||
@@ -369,7 +370,7 @@ agc_status agc_diff_attn_partial_gradients(const void* q_dev, int64_t ldq, const
     if (st != AGC_OK) return st;
     st = partitions(name, part_end_host, k_parts, tokens_q);
     if (st != AGC_OK) return st;
-    if ((int64_t)heads * k_parts > (1 << 21)) return refuse(AGC_ESHAPE, std::string(name) + ": heads * k_parts must be up to 2^21");
+    if ((int64_t)heads * k_parts >= (1 << 21)) return refuse(AGC_ESHAPE, std::string(name) + ": heads * k_parts must be below 2^21");
     if (((!dout_dev || !lse_dev || !dq_dev) && tokens_q > 0) || ((!dk_dev || !dv_dev) && tokens_k > 0) || !G_lambda_dev)
         return refuse(AGC_EINVAL, std::string(name) + ": null pointer");
     if (lddout < (int64_t)heads * value_dim || lddq < (int64_t)2 * heads * head_dim || lddk < (int64_t)2 * kv_heads * head_dim ||

@@ -92,8 +92,44 @@ def test_partial_tiles_of_rows_at_the_largest_stride(d, e, far):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+# ------------------------------------------------------------------ the most sequences
+@pytest.mark.gpu
+def test_a_million_sequences_of_many_rows():
+    """2^20 sequences of 64 queries, four heads on one, and a key each, which the last query alone sees: its map is 1."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB")
+    n, heads, d, e = 1 << 20, 4, 8, 8
+    g = torch.Generator(device="cuda").manual_seed(0)
+    bf16 = torch.bfloat16
+    q = torch.randn(64 * n, heads * 2 * d, generator=g, device="cuda").to(bf16)
+    k, v = (torch.randn(n, w, generator=g, device="cuda").to(bf16) for w in (2 * d, e))
+    lam = torch.tensor([0.25, -0.5, 1.0, 0.75], device="cuda")
+    q_end = (torch.arange(1, n + 1, device="cuda") * 64).to(torch.int32)
+    k_end = torch.arange(1, n + 1, device="cuda", dtype=torch.int32)
+    out = torch.full((64 * n, heads * e), 3.0, dtype=bf16, device="cuda")
+    ws = torch.empty(api.agc_diff_attn_workspace_bytes(64 * n, n, n, heads, 1, d, e), dtype=torch.uint8, device="cuda")
+    api.agc_diff_attn_forward(q, k, v, heads, 1, lam, q_end, k_end, 0.25, True, out, ws)
+    rows = out.view(n, 64, heads, e)
+    assert not rows[:, :63].any()
+    want = v.float()[:, None] * (1 - lam[:, None])
+    # the one power of two that a map consists of is rounded, and so is the result
+    assert bool(((rows[:, 63].float() - want).abs() <= 2.0 ** -8 * (v.float().abs()[:, None] * (1 + lam.abs()[:, None]) + want.abs())).all())
+
+
 @pytest.mark.parametrize("grad", [False, True])
 @pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
 def test_scales_whose_binary_one_is_infinite_are_refused(grad, scale):
     """Scores enter powers of two: their factor is scale * log2(e)."""
     assert raw(grad, scale=scale) == api.AGC_EINVAL
+
+
+@pytest.mark.parametrize("change", [
+    dict(nq=2 ** 26, heads=10, ldq=4096, d=8, e=136), dict(nk=2 ** 26, heads=10, kv=10, ldq=2048, ldk=2048, ldv=2048, d=72, e=8)])
+def test_more_wide_heads_than_a_launch_has_threads_for_are_refused(change):
+    for grad in (False, True):
+        assert raw(grad, **change) == api.AGC_ESHAPE
+
+
+def test_more_rows_of_G_than_a_launch_has_threads_for_are_refused():
+    assert raw(True, parts=(3,) * 256, heads=8192, kv=1, d=8, e=8, ldq=2 ** 17, lddq=2 ** 17, lddout=2 ** 16, ldg=8192) == api.AGC_ESHAPE
