@@ -180,9 +180,9 @@ struct AttnTile {
         } else {
 #pragma unroll 1
             for (int c = wave; c < ROWS / kPer; c += WAVES) {
-                // 64 bits to the first row of a fetch: 256 rows of 2^25 bytes lie further apart than 32 reach, those of a fetch do not
-                const int row = c * kPer + lane / kChunks, first = min(c * kPer, rows - 1);
-                attn_load16(head.chunk(base + (int64_t)first * stride, (uint32_t)min(lane / kChunks, rows - 1 - first) * stride, (lane % kChunks) ^ mix(row)),
+                // more than 128 rows, 2^25 bytes apart at most, lie further than 32 bits reach: those count from a fetch's first one
+                const int row = c * kPer + lane / kChunks, first = ROWS > 128 ? min(c * kPer, rows - 1) : 0;
+                attn_load16(head.chunk(base + (int64_t)first * stride, (uint32_t)(min(row, rows - 1) - first) * stride, (lane % kChunks) ^ mix(row)),
                             lds + c * 1024);
             }
         }
