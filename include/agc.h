@@ -370,7 +370,8 @@ agc_status agc_rotary_apply(const void* x_dev, int type, int64_t ldx, int64_t n_
  * times as long as original_len, the one that a model was trained for,
  *   AGC_ROTARY_LINEAR    f_i / factor
  *   AGC_ROTARY_BY_PARTS  f_i / factor where the pair turns once or less over original_len, f_i where it turns 32 times or more,
- *                        a linear ramp over the pairs between;  *amplitude_out = 0.1 ln(factor) + 1 (else 1). */
+ *                        a linear ramp over the pairs between, which begins with the first pair at the earliest and leaves f_i
+ *                        where it begins;  *amplitude_out = 0.1 ln(factor) + 1 (else 1). */
 typedef enum { AGC_ROTARY_PLAIN = 0, AGC_ROTARY_LINEAR = 1, AGC_ROTARY_BY_PARTS = 2 } agc_rotary_scaling;
 agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double factor, double original_len,
                                   uint64_t* turns_out, double* amplitude_out);
@@ -395,9 +396,11 @@ agc_status agc_rotary_frequencies(int rot_dim, double base, int scaling, double 
  *              map m of head h in row 2 h + m, -infinity without keys; what the gradients take
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 0) bytes, 256-byte aligned; scratch, which calls that may run at
  *              the same time, captured ones among them, do not share
- * scale is 0 or more, and scale * log2(e) finite in binary32.  Scores, maxima, sums and out are held in binary32; the maps
- * enter their product with v as bfloat16, out is rounded once.  The order of the sums is fixed.  NaN or infinity in a sequence
- * reaches that sequence's results alone.  out and lse must not overlap what is read.
+ * scale is 0 or more, and scale * log2(e) finite in binary32; scores, scale q_m k_m, are up to 2^29.  Scores, maxima, sums and out
+ * are held in binary32; the maps enter their product with v as bfloat16, out is rounded once.  The order of the sums is fixed.
+ * NaN or infinity in a sequence reaches that sequence's results alone.  out and lse must not overlap what is read.
+ * Few queries have their keys split among workgroups, into as many parts as keys of the sequences' mean length, tokens_k / n_seqs,
+ * need: a call whose sequences differ many times over takes what its longest one takes with those parts.
  * Row strides of q, k, v up to 2^24, 0 <= tokens_q, tokens_k <= 2^26, tokens_q * heads and tokens_k * kv_heads up to 2^30 (2^29
  * where head_dim is above 64 or value_dim above 128), 1 <= n_seqs <= 2^20, n_seqs * kv_heads up to 2^21, heads a multiple of
  * kv_heads, 1 <= head_dim <= 128, 1 <= value_dim <= 256. */
@@ -419,7 +422,8 @@ agc_status agc_diff_attn_forward(const void* q_dev, int64_t ldq, const void* k_d
  *   G_lambda_dev  device, where row 0 of G holds the gradients of lambda; row p lies p * ldg floats on; overwritten.  No result
  *              may overlap what is read
  *   workspace_dev  device, agc_diff_attn_workspace_bytes(..., 1) bytes, 256-byte aligned (enough for the forward pass too)
- * The maps and dS enter the products with 16 bits, so that results are rounded once; sums are binary32 in a fixed order.
+ * The maps and dS enter the products with 16 bits, so that results are rounded once; sums are binary32 in a fixed order.  Maps
+ * formed again from lse are off by up to 2^-24 |lse| of themselves (2^-17 at 128).
  * 1 <= k_parts <= 256, heads * k_parts below 2^21. */
 agc_status agc_diff_attn_partial_gradients(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev,
                                            int64_t ldv, int64_t tokens_q, int64_t tokens_k, int heads, int kv_heads,

@@ -3,10 +3,9 @@
 //
 // A workgroup has 32 rows a wave, both maps of them (wide heads: one map a wave), and tiles of 64 keys pass two buffers.  For 32
 // rows, 32 keys, both maps 64 wide and values of 128, a SIMD's matrix unit is busy for 768 cycles (24 products), its vector
-// unit for about 950 with powers, sums and maxima, and the compute unit's LDS for 128 times four waves.  No one of them is
-// the bound: 4 x 4096 tokens, 16 heads on 4 key heads, causal, were 490 us traced at the step where this was tried, 404
-// without powers, sums and maxima, 406 without reads of LDS, 303 without both and without loads.  Now they take 390: 1.05
-// PFLOP/s of products at the 1.6 to 1.9 GHz that the card's power then allows, where a library product of 8192^3 reaches 1.28.
+// unit for about 950 with powers, sums and maxima, and the compute unit's LDS for 128 times four waves.  4 x 4096 tokens, 16
+// heads on 4 key heads, causal, take 390 us: 1.05 PFLOP/s of products, matrix units busy for 0.50 and vector units for 0.64 of
+// the time at the 1.6 to 1.9 GHz that the card's power then allows, where a library product of 8192^3 reaches 1.28.
 // Few rows leave memory as the bound: 8 sequences' queries over 131072 keys, 16 heads on 4, 50 us, 5.4 TB/s, and 5 to join.
 #include <algorithm>
 #include <limits>
@@ -153,6 +152,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
             const auto read_v = [&](int n) { return reads.turned(from_lds, v_tile, n / kBlocks * 16, n % kBlocks); };
             auto of_v = attn_stream<2 * kBlocks, kBlocks % 4 ? 2 : 4>(read_v);
             of_v.start();
+            // The maps are rounded to one bfloat16 part: out is off by 1.8e-3 to 2.0e-3 in the 2-norm where its own rounding
+            // leaves 1.66e-3.  Two parts, as in the gradients, would take 617 instead of 415 us (4 x 4096 tokens, 16 heads on 4),
+            // 353 instead of 248 (8 x 2048, 16 heads) and 309 instead of 221 (8111 tokens, 8 heads of 128 on 2).
             tile_bf16x8 p[kMaps][2];
 #pragma unroll
             for (int m = 0; m < kMaps; ++m) {
@@ -369,6 +371,8 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
     Shape o;
     const int64_t rows = tokens_q * (heads / kv_heads);
     const int unit = 2 / attn_maps_of_a_wave(D);   // waves of 32 rows
+    // Lengths lie on the device, the rules go by their mean: 32 queries, one of 100000 keys and 31 of 1000, take 528 us, of 4094 keys
+    // each 57 (16 heads of 64 on 4).
     // Large workgroups read the keys least often; small ones of 64 rows where those would leave compute units without work, down
     // to one wave (of each map) that has a sequence's up to 32 rows; and where these are too few, the keys split among several.
     const int64_t large = 32 * 8 / unit;
@@ -441,7 +445,8 @@ hipError_t attn_lay_out(const AttnCall& c, Attn& a, const uint16_t*& dout, int64
     a.causal = c.causal, a.scale = c.scale, a.to_log2 = std::max(c.scale * kLog2e, std::numeric_limits<float>::denorm_min());
     dout = static_cast<const uint16_t*>(c.dout), lddout = c.lddout;
     // Other widths than the tiles' are filled up on the way to LDS if their chunks of 16 bytes can be read, else in the workspace
-    // (2999 queries of 40 and 72, forward and gradients: 104 against 118 us; 8 x 2048 of 80 and 160: 1545 against 1650).
+    // (forward and gradients of 2999 queries, 6 heads of 40 and 72 on 2: 104 against 118 us; 8 x 2048, 8 heads of 80 and 160: 1575
+    // against 1675).
     const auto chunks = [](const void* p, int64_t ld, int64_t rows) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows < 2 || ld % 8 == 0); };
     a.whole = (c.d == D && c.e == E) || c.d % 8 || c.e % 8 || !chunks(c.q, c.ldq, c.tokens_q) || !chunks(c.k, c.ldk, c.tokens_k) ||
               !chunks(c.v, c.ldv, c.tokens_k) || (dout && !chunks(dout, lddout, c.tokens_q));

@@ -570,7 +570,9 @@ Shape shape_of(int64_t tokens_q, int64_t tokens_k, int n_seqs, int heads, int kv
     side(rows, tokens_k, kRowWaves, o.waves_q, o.slots_q, o.splits_q);
     side(tokens_k, rows, key_waves(D), o.waves_k, o.slots_k, o.splits_k);
     // A large workgroup with a sequence's first keys has twice the mean to do under the causal mask: where there is about one a
-    // compute unit, two halves each (8 x 2048 tokens, 4 heads that 16 share: 712 with their join against 789 us).
+    // compute unit, two halves each.  Both passes with the join, us in halves | whole: 8 x 2048 tokens, 4 heads that 16 share 1033 |
+    // 1093, 2 x 8192, 4 heads 985 | 1209;  4 x 2048, 8 heads 333 | 321, 5 x 2048 386 | 366, 4 heads of 128 477 | 426, of 32 (8
+    // of them) 238 | 239: what long sequences and shared heads gain is more than what short ones lose.
     if (causal && o.waves_k > kFewWaves && tokens_k / (32 * o.waves_k) * kv_heads < 400) o.splits_k = 2;
     return o;
 }

@@ -66,6 +66,29 @@ def test_scale_zero_in_large_workgroups():
     assert bool(((dv - part * (1 - lam)).abs() <= tol).all())
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,e", [(32, 64), (64, 128), (128, 256)])
+def test_scores_of_two_to_the_29th(d, e):
+    """Products that are exact, 2^21 and more apart: each query takes the one key of its largest score in each map, whose power is
+    within 2^32 of 1 and rounded with the map, and the result: 2^-8 each, and 2^-22 for the division."""
+    import torch
+    c = Case([(40, 250), (70, 70)], 2, 1, d, e, True)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    level = torch.stack([torch.cat([torch.randperm(n, generator=g, device="cuda") for n in c.lk]) for _ in range(2)], 1) + 1     # of a key and map
+    c.q.fill_(2.0 ** 14)
+    c.k.view(-1, 2, d).copy_((level.float() * (2.0 ** 7 / d))[:, :, None])
+    c.head = (*c.head[:8], 1.0, True)
+    out = c.forward()[:, :2 * e].double().view(-1, 2, e)
+    lam, v, i, j = c.lam.double()[:, None], c.v.double(), 0, 0
+    for lq, lk in c.lens:
+        for t in range(lq):
+            seen = t + lk - lq + 1
+            first, second = (v[j + int(level[j:j + seen, m].argmax())] for m in range(2))
+            want, size = first - lam * second, first.abs() + lam.abs() * second.abs()
+            assert bool(((out[i + t] - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -21) * size).all())
+        i, j = i + lq, j + lk
+
+
 # ------------------------------------------------------------------ rows far apart
 @pytest.mark.gpu
 @pytest.mark.parametrize("d,e,far", [(32, 64, "v"), (64, 128, "v"), (64, 128, "k"), (24, 40, "v"), (64, 128, "q"), (64, 128, "dout")])
