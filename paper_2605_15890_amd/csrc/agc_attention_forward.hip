@@ -152,7 +152,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES * attn_maps_of_a_wave(D) == 2 ? 1
             const auto read_v = [&](int n) { return reads.turned(from_lds, v_tile, n / kBlocks * 16, n % kBlocks); };
             auto of_v = attn_stream<2 * kBlocks, kBlocks % 4 ? 2 : 4>(read_v);
             of_v.start();
-            // The maps are rounded to one bfloat16 part: out is off by 1.8e-3 to 2.0e-3 in the 2-norm where its own rounding
+            // The maps are rounded to one bfloat16 part: out is off by 1.7e-3 to 2.1e-3 in the 2-norm where its own rounding
             // leaves 1.66e-3.  Two parts, as in the gradients, would take 617 instead of 415 us (4 x 4096 tokens, 16 heads on 4),
             // 353 instead of 248 (8 x 2048, 16 heads) and 309 instead of 221 (8111 tokens, 8 heads of 128 on 2).
             tile_bf16x8 p[kMaps][2];
