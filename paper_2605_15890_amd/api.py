@@ -798,6 +798,8 @@ def agc_dropout(x, p, seed, step, site, out, residual=None, stream=None, check=T
     x_kind, out_kind = _type_of(x, "x"), _type_of(out, "out")
     if x.dim() != 2:
         raise AgcError(AGC_ESHAPE, "x must be (rows, cols)")
+    if not 0 <= site <= 65535:   # ctypes would keep the lower 32 bits
+        raise AgcError(AGC_ESHAPE, "agc_dropout: site must be 0..65535")
     rows, cols = x.shape
     ldx, ldo, ldr = _rows_of(x, rows, cols, x.dtype, "x"), _rows_of(out, rows, cols, out.dtype, "out"), cols
     if residual is not None:

@@ -68,3 +68,12 @@ def test_forward_pass_of_few_tokens_leaves_the_workspace_alone(tokens):
 def test_dropout_in_place_of_another_type_is_refused(rows, x_type, out_type):
     """A row's values would be written over others that are not read yet, in a single row too; nothing is dereferenced."""
     assert api.load().agc_dropout(64, x_type, 64, None, 64, rows, 64, 0.5, 1, 2, 3, 64, out_type, 64, None) == api.AGC_EINVAL
+
+
+@pytest.mark.parametrize("site", [-1, 65536, 2 ** 32, 2 ** 32 + 3])
+def test_dropout_sites_beyond_their_range_are_refused(site):
+    """Also those whose lower 32 bits name another site."""
+    x = torch.zeros(3, 16)
+    with pytest.raises(api.AgcError, match="site") as e:
+        api.agc_dropout(x, 0.5, 1, 2, site, torch.empty_like(x))
+    assert e.value.status == api.AGC_ESHAPE
