@@ -440,8 +440,8 @@ hipError_t attn_lay_out(const AttnCall& c, Attn& a, const uint16_t*& dout, int64
     a.lambda = c.lambda, a.q_end = c.q_end, a.k_begin = c.k_begin, a.k_end = c.k_end;
     a.n_seqs = c.n_seqs, a.tokens_q = (int)c.tokens_q, a.tokens_k = (int)c.tokens_k;
     a.heads = c.heads, a.kv_heads = c.kv_heads, a.d = c.d, a.e = c.e;
-    // Keys out of sight have scores of -infinity, which a factor of zero would make NaN.  The smallest number that is more than
-    // zero leaves them, and no other score, below 2^128, counts for more than 2^-21 with it: every key in sight weighs alike.
+    // Keys out of sight have scores of -infinity, which a factor of zero would make NaN.  The smallest number above zero, 2^-149,
+    // leaves them what they are, and the largest other score, 2^128, is 2^-21 with it: every key in sight weighs alike.
     a.causal = c.causal, a.scale = c.scale, a.to_log2 = std::max(c.scale * kLog2e, std::numeric_limits<float>::denorm_min());
     dout = static_cast<const uint16_t*>(c.dout), lddout = c.lddout;
     // Other widths than the tiles' are filled up on the way to LDS if their chunks of 16 bytes can be read, else in the workspace
